@@ -51,6 +51,9 @@ typedef enum { KGE_OPT_SGD = 0, KGE_OPT_ADAM = 1, KGE_OPT_ROWWISE_ADAGRAD = 2 } 
 /* Arithmetic of the B x N score block (and of full-entity scoring). */
 typedef enum { KGE_PREC_FP32 = 0, KGE_PREC_BF16_TC = 1 } kge_prec_t;
 
+/* Element types of the operators on rows (below); the tables bound to a handle are fp32. */
+typedef enum { KGE_F32 = 0, KGE_BF16 = 1, KGE_F16 = 2, KGE_E4M3 = 3, KGE_E5M2 = 4 } kge_dtype_t;
+
 typedef enum {
     KGE_OK = 0,
     KGE_ERR_BAD_ARG = -1,        /* NULL / out-of-range argument, misaligned pointer */
@@ -364,6 +367,65 @@ float kge_lr_linear_decay(float lr0, uint64_t step, uint64_t total_steps);
 int kge_ensemble_rank_scores(double power, int32_t k_list, double* table /*[host]*/);
 int kge_ensemble_topk(const int32_t* lists, int32_t num_models, int32_t nq, int32_t k_list, const double* table,
                       int32_t top_n, int32_t* out_ids, double* out_scores, void* stream);
+
+/*
+ * Operators on rows, for scoring functions, encoders and projections that a caller writes around the library's steps.  They take
+ * no handle: tables, lists and results are the caller's device arrays on the current device, `ld...` are distances between rows in
+ * elements, types are kge_dtype_t, arithmetic is fp32 with one rounding at the end.  They enqueue on `stream`, allocate nothing,
+ * and may be captured into a CUDA graph.  status: device int32 (or NULL) that receives the first code found on the device, as the
+ * status word of a handle does; the caller clears it.  A call on no rows returns KGE_OK without touching its arrays.
+ *
+ * kge_embedding_lookup    out[i, :] = scale table[ids[i], :] for i < n.  An id equal to padding_id (-1, as the top-k lists leave
+ *                         in unused places, or any other) gives a row of zeros, an id outside [0, rows) does so too and records
+ *                         KGE_ERR_ID_RANGE.  Types fp32, bf16, fp16, each side its own.
+ * kge_embedding_grad      its gradient: table_grad[e, :] = scale sum of grads[i, :] over the i with ids[i] = e, added in fp32 in an
+ *                         order that depends on ids alone.  accumulate = 0 writes every row (zeros where no id points), 1 adds
+ *                         to what the touched rows hold and leaves the others alone.  Padding and bad ids contribute nothing.
+ *                         scratch: kge_embedding_grad_scratch_bytes(rows, dim, n) bytes, 256-byte aligned; calls that may
+ *                         overlap (two streams, two captured graphs) need one each.
+ */
+int kge_embedding_lookup(const void* table, int32_t table_type, int64_t rows, int32_t dim, int64_t ld_table, const int32_t* ids, int32_t n,
+                         float scale, int32_t padding_id, void* out, int32_t out_type, int64_t ld_out, int32_t* status, void* stream);
+size_t kge_embedding_grad_scratch_bytes(int64_t rows, int32_t dim, int32_t n);
+int kge_embedding_grad(const int32_t* ids, int32_t n, const void* grads, int32_t grads_type, int64_t ld_grads, float scale, int32_t padding_id,
+                       int32_t accumulate, void* table_grad, int32_t table_type, int64_t rows, int32_t dim, int64_t ld_table, void* scratch,
+                       size_t scratch_bytes, int32_t* status, void* stream);
+
+/*
+ * Dropout of n <= 2^34 contiguous elements with probability p, no mask stored: with T = rint(65536 p), element i stays if
+ * half i mod 8 (word (i mod 8) / 2, low half first) of Philox4x32-10 with key = seed and counter = (i / 8, step lo, step hi,
+ * 2^31 + site) is at least T; it is then multiplied by 65536 / (65536 - T), else it leaves 0 (an infinity or a NaN too).
+ * out = that (+ residual, of out's type, if given).  The backward pass is the same call on the gradient, without residual.
+ * site (>= 0) keeps the masks of a model's places apart; the sampler's and the initialisation's streams lie below 2^31.
+ * step_dev: device int64 added to step when the call runs (or NULL), so that a captured call draws a new mask at every replay.
+ * out may be x or residual itself (same type), not overlap them otherwise.
+ */
+int kge_dropout(const void* x, int32_t x_type, const void* residual, void* out, int32_t out_type, int64_t n, double p,
+                uint64_t seed, uint64_t step, const int64_t* step_dev, int32_t site, void* stream);
+
+/*
+ * 8-bit floating point (KGE_E4M3, largest value 448; KGE_E5M2, 57344) with a scale for each block of 128 along the contraction
+ * index, and the product of two such operands.  An operand is a row-major byte matrix [R, K] whose rows lie ld (a multiple of 16,
+ * base 16-byte aligned) bytes apart, and fp32 scales laid out block of K by block of K: [ceil(K / 128), R] for blocks of 1 x 128,
+ * [ceil(K / 128), ceil(R / 128)] for blocks of 128 x 128.  What lies between K and ld is neither read nor written.
+ *
+ * kge_fp8_quantize   x [rows, cols] (fp32, bf16, fp16) -> q [rows, cols] with blocks along the columns, and / or qt [cols, rows], the
+ *                    operand x^T with blocks along x's rows; either may be NULL.  scale = largest magnitude of the block / largest
+ *                    value of the type (at least 2^-126; 1 for a block of zeros), with pow2 = 1 rounded up to a power of two;
+ *                    the value stored is the one nearest to x / scale, ties to even.  A block that holds an infinity or a NaN
+ *                    stands for NaN throughout.
+ * kge_fp8_matmul     out [M, N] = A [M, K] . B [N, K]^T (+ addend [M, N], of out's type; it may be out itself): products within a
+ *                    block of 128 summed by the tensor cores, each block's sum times its two scales added in fp32.  out fp32,
+ *                    bf16 or fp16; a_block, b_block: 1 or 128 rows to a scale; the operands' types may differ.
+ *                    The forward pass of a projection y = x W^T multiplies the forms along the columns of x and W; its gradients
+ *                    dx = dy W and dW = dy^T x multiply dy with W^T and dy^T with x^T.
+ */
+int kge_fp8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, int32_t fp8_type, int32_t block_rows, int32_t pow2,
+                     void* q, int64_t ldq, float* scales, void* qt, int64_t ldqt, float* scales_t, void* stream);
+size_t kge_fp8_matmul_scratch_bytes(int64_t M, int64_t N, int64_t K);
+int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_scales, int32_t a_block, const void* b, int32_t b_type, int64_t ldb,
+                   const float* b_scales, int32_t b_block, const void* addend, int64_t ld_addend, void* out, int32_t out_type, int64_t ld_out,
+                   int64_t M, int64_t N, int64_t K, void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
 
 /* Synchronise `stream`, return the sticky device status word (0 or a negative code), clear it. */
 int kge_get_status(kge_handle* h, void* stream);

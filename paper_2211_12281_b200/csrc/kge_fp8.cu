@@ -1,0 +1,528 @@
+// 8-bit floating point with a scale for each block of 128 along the contraction index: making such operands, and their product.
+//   quantise   s = amax / top (or the next power of two), q = the 8-bit value nearest to x / s; one scale per 1 x 128 or 128 x 128 block
+//   product    C[m, n] = sum_kb sA[kb, m] sB[kb, n] sum_{k in kb} A[m, k] B[n, k]   (+ C0[m, n])
+#include <cuda.h>
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "kge_ops.cuh"
+
+namespace kge {
+
+namespace {
+
+// ---- quantisation ----------------------------------------------------------------------------------------------------
+
+struct QuantParams {
+    const void* x; int64_t ldx;
+    int64_t rows, cols;
+    uint8_t *q, *qt; int64_t ldq, ldqt;
+    float *scales, *scales_t;
+    int vec;                         // rows of x start at multiples of 16 bytes
+    int pow2;
+    int64_t tiles_c;
+};
+
+template <int FMT> struct Fp8Traits;
+template <> struct Fp8Traits<KGE_E4M3> { static constexpr float top = 448.f, least = 0.015625f; static constexpr uint32_t drop = 20; };
+template <> struct Fp8Traits<KGE_E5M2> { static constexpr float top = 57344.f, least = 6.103515625e-5f; static constexpr uint32_t drop = 21; };
+
+// Scale of a block whose largest magnitude has the bit pattern `amax`.  A block of zeros has scale 1; an infinity or a NaN makes
+// the scale one, and with it every value that the block stands for NaN.
+template <int FMT>
+__device__ __forceinline__ float block_scale(uint32_t amax, bool pow2) {
+    float s = __uint_as_float(amax) / Fp8Traits<FMT>::top;
+    if (amax < 0x7F800000u) {
+        s = amax == 0u ? 1.f : fmaxf(s, 1.17549435e-38f);
+        if (pow2) s = __uint_as_float((__float_as_uint(s) + 0x007FFFFFu) & 0x7F800000u);
+    }
+    return s;
+}
+
+// x / s in fp32 such that rounding it to 8 bits rounds the true quotient.  x * (1 / s) is within three units in the last place
+// of it, which only matters next to the middle of two 8-bit values: there (and below the normal range, whose middles lie
+// elsewhere) the quotient is cut off and its last bit set if anything was cut, so that no rounding falls on a middle by itself.
+template <int FMT>
+__device__ __forceinline__ float quotient(float x, float s, float inv, bool pow2) {
+    float t = x * inv;
+    if (!pow2) {
+        constexpr uint32_t drop = Fp8Traits<FMT>::drop, mid = 1u << (drop - 1);
+        const uint32_t off = (__float_as_uint(t) & ((1u << drop) - 1u)) - (mid - 4u);
+        if ((off <= 8u || fabsf(t) < Fp8Traits<FMT>::least) && x != 0.f) {
+            t = __fdiv_rz(x, s);
+            if (fmaf(-t, s, x) != 0.f) t = __uint_as_float(__float_as_uint(t) | 1u);
+        }
+    }
+    return t;
+}
+
+template <int FMT>
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+    constexpr __nv_fp8_interpretation_t f = FMT == KGE_E4M3 ? __NV_E4M3 : __NV_E5M2;
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, f), hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, f);
+    return lo | hi << 16;
+}
+
+// One CTA per 128 x 128 tile: thread (rg, cg) holds rows 8 rg .. + 8 and columns 8 cg .. + 8.
+template <typename TX, int FMT, bool SQUARE>
+__global__ void __launch_bounds__(256, 2) quantize_kernel(QuantParams p) {
+    __shared__ uint32_t part[16][128];
+    __shared__ float2 col_scale[128];
+    __shared__ alignas(16) uint2 turned[128][16];
+    const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
+    const int64_t tr = blockIdx.x / p.tiles_c, tc = blockIdx.x - tr * p.tiles_c;
+    const int64_t r0 = tr * 128 + rg * 8, c0 = tc * 128 + cg * 8;
+    float v[8][8];
+    const TX* x = static_cast<const TX*>(p.x) + c0;
+    const bool whole = p.vec && c0 + 8 <= p.cols;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + i;
+        if (whole && r < p.rows) {
+            const Pack<TX, 8> w = *reinterpret_cast<const Pack<TX, 8>*>(x + r * p.ldx);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = to_float(w.v[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = r < p.rows && c0 + j < p.cols ? to_float(x[r * p.ldx + j]) : 0.f;
+        }
+    }
+    auto bits = [](float f) { return __float_as_uint(f) & 0x7FFFFFFFu; };
+    float s_all = 1.f, inv_all = 1.f;
+    if (SQUARE) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, bits(v[i][j]));
+        m = __reduce_max_sync(0xffffffffu, m);
+        if ((tid & 31) == 0) part[0][tid >> 5] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 8; ++w) m = max(m, part[0][w]);
+        s_all = block_scale<FMT>(m, p.pow2);
+        inv_all = 1.f / s_all;
+        if (tid == 0) {
+            const int64_t row_blocks = (p.rows + 127) / 128;
+            if (p.q) p.scales[tc * row_blocks + tr] = s_all;
+            if (p.qt) p.scales_t[tr * p.tiles_c + tc] = s_all;
+        }
+    }
+    if (p.q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float s = s_all, inv = inv_all;
+            if (!SQUARE) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max(m, bits(v[i][j]));
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                s = block_scale<FMT>(m, p.pow2);
+                inv = 1.f / s;
+                if (cg == 0 && r0 + i < p.rows) p.scales[tc * p.rows + r0 + i] = s;
+            }
+            if (r0 + i >= p.rows) continue;
+            float t[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = quotient<FMT>(v[i][j], s, inv, p.pow2);
+            const uint2 w = make_uint2(pack4<FMT>(t[0], t[1], t[2], t[3]), pack4<FMT>(t[4], t[5], t[6], t[7]));
+            uint8_t* dst = p.q + (r0 + i) * p.ldq + c0;
+            if (c0 + 8 <= p.cols) *reinterpret_cast<uint2*>(dst) = w;
+            else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) if (c0 + j < p.cols) dst[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+            }
+        }
+    }
+    if (p.qt) {
+        if (!SQUARE) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, bits(v[i][j]));
+                part[rg][cg * 8 + j] = m;
+            }
+            __syncthreads();
+            if (tid < 128) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int g = 0; g < 16; ++g) m = max(m, part[g][tid]);
+                const float s = block_scale<FMT>(m, p.pow2);
+                col_scale[tid] = make_float2(s, 1.f / s);
+                const int64_t c = tc * 128 + tid;
+                if (c < p.cols) p.scales_t[tr * p.cols + c] = s;
+            }
+            __syncthreads();
+        }
+        // columns become rows of 128 bytes in shared memory; 8-byte unit u of row c lies at u ^ (c / 8), free of bank conflicts
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float2 cs = SQUARE ? make_float2(s_all, inv_all) : col_scale[cg * 8 + j];
+            float t[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = quotient<FMT>(v[i][j], cs.x, cs.y, p.pow2);
+            turned[cg * 8 + j][rg ^ cg] = make_uint2(pack4<FMT>(t[0], t[1], t[2], t[3]), pack4<FMT>(t[4], t[5], t[6], t[7]));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int c = k * 32 + (tid >> 3), piece = tid & 7;
+            const int64_t col = tc * 128 + c, row = tr * 128 + piece * 16;
+            if (col >= p.cols || row >= p.rows) continue;
+            const uint2 a = turned[c][(2 * piece) ^ (c >> 3)], b = turned[c][(2 * piece + 1) ^ (c >> 3)];
+            uint8_t* dst = p.qt + col * p.ldqt + row;
+            if (row + 16 <= p.rows) *reinterpret_cast<uint4*>(dst) = make_uint4(a.x, a.y, b.x, b.y);
+            else {
+                const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+                for (int j = 0; j < 16; ++j) if (row + j < p.rows) dst[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+            }
+        }
+    }
+}
+
+template <typename TX>
+int launch_quantize(const QuantParams& p, int fmt, bool square, cudaStream_t s) {
+    const dim3 grid((unsigned)(p.tiles_c * ceil_div(p.rows, 128)));
+    if (fmt == KGE_E4M3) {
+        if (square) quantize_kernel<TX, KGE_E4M3, true><<<grid, 256, 0, s>>>(p);
+        else quantize_kernel<TX, KGE_E4M3, false><<<grid, 256, 0, s>>>(p);
+    } else {
+        if (square) quantize_kernel<TX, KGE_E5M2, true><<<grid, 256, 0, s>>>(p);
+        else quantize_kernel<TX, KGE_E5M2, false><<<grid, 256, 0, s>>>(p);
+    }
+    return launch_status(cudaGetLastError());
+}
+
+// ---- product ---------------------------------------------------------------------------------------------------------
+
+constexpr int FP_BM = 128, FP_BK = 128;                   // BK bytes = one 128-byte swizzle row
+constexpr int FP_STAGES = 4, FP_EPI_WARPS = 8;
+constexpr int FP_THREADS = 32 * (2 + FP_EPI_WARPS);
+constexpr uint32_t FP_BOX_BYTES = 128 * FP_BK;            // 128 rows of an operand
+constexpr uint32_t FP_STORE_BYTES = 4096;                 // per epilogue warp: 32 rows x 32 fp32 on their way to memory
+__host__ __device__ constexpr uint32_t fp_stage_bytes(int bn) { return FP_BOX_BYTES + (uint32_t)bn * FP_BK; }
+__host__ __device__ constexpr size_t fp_smem_bytes(int bn) { return 1024 + (size_t)FP_STAGES * fp_stage_bytes(bn) + 256 + FP_EPI_WARPS * FP_STORE_BYTES; }
+
+struct ProductParams {
+    int64_t M, N;
+    int kblocks;
+    int64_t tiles_n, items;
+    const float *sa, *sb;
+    int64_t sa_ld, sb_ld;                 // scales per block of K
+    int a_square, b_square;               // a scale serves 128 rows
+    const void* addend; int64_t ld_addend;
+    void* out; int64_t ld_out; int out_type;
+    int vec;                              // packs of four columns of out (and addend) are aligned
+    int32_t* status; int wait_limit;
+    uint32_t idesc;
+};
+
+__device__ __forceinline__ void fp_tma_load(void* dst, const CUtensorMap* tm, int x, int y, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(smem_u32(dst)), "l"(tm), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+// Shared-memory descriptor of a K-major operand tile with the 128-byte swizzle: rows of 128 bytes, groups of eight rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t fp_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Instruction descriptor: D fp32, A and B 8-bit (0 = e4m3, 1 = e5m2), both K-major.
+constexpr uint32_t fp_idesc(int m, int n, int fa, int fb) {
+    return (1u << 4) | ((uint32_t)fa << 7) | ((uint32_t)fb << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void fp_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void fp_commit(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void fp_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fp_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fp_tmem_ld32(uint32_t taddr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// Four columns of a row: addend and conversion.
+template <typename TO>
+__device__ __forceinline__ void fp_put4(const ProductParams& p, int64_t row, int64_t col, float4 v) {
+    TO* dst = static_cast<TO*>(p.out) + row * p.ld_out + col;
+    const TO* add = p.addend ? static_cast<const TO*>(p.addend) + row * p.ld_addend + col : nullptr;
+    const float f[4] = {v.x, v.y, v.z, v.w};
+    if (p.vec && col + 4 <= p.N) {
+        Pack<TO, 4> o, a;
+        if (add) a = *reinterpret_cast<const Pack<TO, 4>*>(add);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o.v[e] = from_float<TO>(add ? f[e] + to_float(a.v[e]) : f[e]);
+        *reinterpret_cast<Pack<TO, 4>*>(dst) = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (col + e < p.N) dst[e] = from_float<TO>(add ? f[e] + to_float(add[e]) : f[e]);
+    }
+}
+
+// Persistent CTAs, a 128 x BN tile of C at a time.  Warp 0 feeds a ring of shared-memory stages by TMA, warp 1 issues the MMAs of
+// one block of 128 k into one of the accumulators in tensor memory, eight warps multiply the finished block sums by their
+// scales and add them up in registers (a block's sum times two scales: the tensor cores cannot carry a scale over blocks).
+template <int BN>
+__global__ void __launch_bounds__(FP_THREADS, 1) fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                                                                    const __grid_constant__ ProductParams p) {
+    constexpr uint32_t STAGE = fp_stage_bytes(BN);
+    constexpr int NACC = 512 / BN, COLS = BN / 2;
+    extern __shared__ unsigned char fp_smem_raw[];
+    unsigned char* base = fp_smem_raw + ((1024u - (smem_u32(fp_smem_raw) & 1023u)) & 1023u);
+    uint64_t* full = reinterpret_cast<uint64_t*>(base + (size_t)FP_STAGES * STAGE);
+    uint64_t* empty = full + FP_STAGES;
+    uint64_t* acc_full = empty + FP_STAGES;
+    uint64_t* acc_empty = acc_full + NACC;
+    uint64_t* done = acc_empty + NACC;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    volatile uint32_t* stop = tmem_slot + 1;
+    volatile uint32_t* filled = tmem_slot + 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < FP_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < NACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], FP_EPI_WARPS); }
+        mbar_init(done, 1);
+        *stop = 0;
+        mbar_init_fence();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fp_fence_before();
+    __syncthreads();
+    fp_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int64_t ring = 0;
+            for (int64_t item = blockIdx.x; item < p.items && !*stop; item += gridDim.x) {
+                const int m0 = (int)(item / p.tiles_n) * FP_BM, n0 = (int)(item % p.tiles_n) * BN;
+                for (int kb = 0; kb < p.kblocks; ++kb, ++ring) {
+                    const int s = (int)(ring % FP_STAGES);
+                    if (!mbar_wait_idle(&empty[s], (uint32_t)((ring / FP_STAGES) & 1) ^ 1u, p.wait_limit)) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); break; }
+                    unsigned char* sa = base + (size_t)s * STAGE;
+                    mbar_arrive_expect_tx(&full[s], STAGE);
+                    fp_tma_load(sa, &tmA, kb * FP_BK, m0, &full[s]);
+#pragma unroll
+                    for (int g = 0; g < BN / 128; ++g) fp_tma_load(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
+                }
+            }
+            *filled = (uint32_t)min(ring, (int64_t)1 << 30);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int64_t ring = 0;
+            bool ok = true;
+            for (int64_t item = blockIdx.x; item < p.items && ok && !*stop; item += gridDim.x) {
+                for (int kb = 0; kb < p.kblocks; ++kb, ++ring) {
+                    const int s = (int)(ring % FP_STAGES), buf = (int)(ring % NACC);
+                    if (!mbar_wait_idle(&acc_empty[buf], (uint32_t)((ring / NACC) & 1) ^ 1u, p.wait_limit) ||
+                        !mbar_wait_idle(&full[s], (uint32_t)(ring / FP_STAGES) & 1u, p.wait_limit)) { ok = false; break; }
+                    fp_fence_after();
+                    const uint32_t sa = smem_u32(base + (size_t)s * STAGE);
+#pragma unroll
+                    for (int k = 0; k < FP_BK / 32; ++k)
+                        fp_mma(tmem + (uint32_t)(buf * BN), fp_desc(sa + k * 32), fp_desc(sa + FP_BOX_BYTES + k * 32), p.idesc, k != 0);
+                    fp_commit(&empty[s]);
+                    fp_commit(&acc_full[buf]);
+                }
+            }
+            if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        float4* st = reinterpret_cast<float4*>(base + (size_t)FP_STAGES * STAGE + 256) + (size_t)(warp - 2) * (FP_STORE_BYTES / 16);
+        int64_t ring = 0;
+        bool ok = true;
+        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const int64_t m0 = (item / p.tiles_n) * FP_BM, n0 = (item % p.tiles_n) * BN + half * COLS;
+            const int64_t row = m0 + quarter * 32 + lane;
+            float acc[COLS];
+#pragma unroll
+            for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
+            for (int kb = 0; kb < p.kblocks; ++kb, ++ring) {
+                const int buf = (int)(ring % NACC);
+                float sa = 0.f;
+                if (row < p.M) sa = p.sa[kb * p.sa_ld + (p.a_square ? row >> 7 : row)];
+                if (p.b_square && n0 < p.N) sa *= p.sb[kb * p.sb_ld + (n0 >> 7)];
+                ok = mbar_wait_bounded(&acc_full[buf], (uint32_t)(ring / NACC) & 1u, p.wait_limit) && !*stop;
+                ok = __all_sync(0xffffffffu, ok);
+                fp_fence_after();
+                if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
+                const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + half * COLS);
+#pragma unroll
+                for (int c = 0; c < COLS; c += 32) {
+                    float v[32];
+                    fp_tmem_ld32(taddr + (uint32_t)c, v);
+                    if (p.b_square) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[c + i] = fmaf(v[i], sa, acc[c + i]);
+                    } else {
+                        const float* sb = p.sb + kb * p.sb_ld + n0 + c;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) acc[c + i] = fmaf(v[i], sa * (n0 + c + i < p.N ? sb[i] : 0.f), acc[c + i]);
+                    }
+                }
+                fp_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[buf]);
+            }
+            if (!ok) break;
+            // through shared memory: a store instruction covers four rows' 32 columns
+            const int sw = lane & 7;
+#pragma unroll
+            for (int c = 0; c < COLS; c += 32) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) st[lane * 8 + (i ^ sw)] = make_float4(acc[c + 4 * i], acc[c + 4 * i + 1], acc[c + 4 * i + 2], acc[c + 4 * i + 3]);
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int r = j * 4 + (lane >> 3), q = lane & 7;
+                    const float4 val = st[r * 8 + (q ^ (r & 7))];
+                    const int64_t orow = m0 + quarter * 32 + r, ocol = n0 + c + 4 * q;
+                    if (orow < p.M && ocol < p.N) {
+                        if (p.out_type == KGE_F32) fp_put4<float>(p, orow, ocol, val);
+                        else if (p.out_type == KGE_BF16) fp_put4<__nv_bfloat16>(p, orow, ocol, val);
+                        else fp_put4<__half>(p, orow, ocol, val);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    fp_fence_before();
+    __syncthreads();
+    if (*stop) {       // copies and MMAs in flight are waited for before the CTA's memory is given back
+        if (lane == 0) {
+            if (warp == 0) { const int n = (int)*filled; for (int r = max(0, n - FP_STAGES); r < n; ++r) mbar_wait_idle(&full[r % FP_STAGES], (r / FP_STAGES) & 1, kDefaultWaitLimit); }
+            if (warp == 1) { fp_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
+        }
+        __syncthreads();
+    }
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t k, int64_t ld) {
+    static const EncodeTiledFn fn = [] {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
+    }();
+    if (!fn) return KGE_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+    const cuuint32_t box[2] = {FP_BK, 128}, one[2] = {1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? KGE_OK : KGE_ERR_CUDA;
+}
+
+// Streaming multiprocessors of the current device.
+int sm_count(int* sms) {
+    static std::atomic<int> known[kMaxDevices];
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return KGE_ERR_CUDA;
+    const bool tracked = dev >= 0 && dev < kMaxDevices;
+    *sms = tracked ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (*sms == 0) {
+        e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return KGE_ERR_CUDA;
+        if (tracked) known[dev].store(*sms, std::memory_order_relaxed);
+    }
+    return KGE_OK;
+}
+
+template <int BN>
+int launch_product(const CUtensorMap& a, const CUtensorMap& b, ProductParams& p, int sms, cudaStream_t s) {
+    constexpr size_t smem = fp_smem_bytes(BN);
+    static DeviceOnce configured;
+    cudaError_t e = once_per_device(configured, [] {
+        return cudaFuncSetAttribute(fp8_product_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    });
+    if (e != cudaSuccess) return KGE_ERR_CUDA;
+    p.tiles_n = ceil_div(p.N, BN);
+    p.items = ceil_div(p.M, FP_BM) * p.tiles_n;
+    fp8_product_kernel<BN><<<(unsigned)std::min<int64_t>(p.items, sms), FP_THREADS, smem, s>>>(a, b, p);
+    return launch_status(cudaGetLastError());
+}
+
+}  // namespace
+}  // namespace kge
+
+using namespace kge;
+
+extern "C" {
+
+int kge_fp8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, int32_t fp8_type, int32_t block_rows, int32_t pow2,
+                     void* q, int64_t ldq, float* scales, void* qt, int64_t ldqt, float* scales_t, void* stream) {
+    if (!is_float_type(x_type) || !is_fp8_type(fp8_type) || rows < 0 || rows > INT32_MAX || cols < 0 || cols > INT32_MAX || ldx < cols ||
+        (block_rows != 1 && block_rows != 128) || (pow2 != 0 && pow2 != 1) || (!q && !qt)) return KGE_ERR_BAD_ARG;
+    if ((q && (!scales || ldq < cols || ldq % 16 || !aligned_to(q, 16) || !aligned_to(scales, 4))) ||
+        (qt && (!scales_t || ldqt < rows || ldqt % 16 || !aligned_to(qt, 16) || !aligned_to(scales_t, 4)))) return KGE_ERR_BAD_ARG;
+    if (rows == 0 || cols == 0) return KGE_OK;
+    if (!x || !aligned_to(x, type_bytes(x_type))) return KGE_ERR_BAD_ARG;
+    QuantParams p{};
+    p.x = x; p.ldx = ldx; p.rows = rows; p.cols = cols;
+    p.q = static_cast<uint8_t*>(q); p.ldq = ldq; p.scales = scales;
+    p.qt = static_cast<uint8_t*>(qt); p.ldqt = ldqt; p.scales_t = scales_t;
+    p.pow2 = pow2; p.tiles_c = ceil_div(cols, 128);
+    p.vec = aligned_to(x, 16) && ldx * type_bytes(x_type) % 16 == 0;
+    if (p.tiles_c * ceil_div(rows, 128) > INT32_MAX) return KGE_ERR_UNSUPPORTED;
+    return with_type(x_type, [&](auto t) { return launch_quantize<decltype(t)>(p, fp8_type, block_rows == 128, static_cast<cudaStream_t>(stream)); });
+}
+
+size_t kge_fp8_matmul_scratch_bytes(int64_t M, int64_t N, int64_t K) { return 0; }
+
+int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_scales, int32_t a_block, const void* b, int32_t b_type, int64_t ldb,
+                   const float* b_scales, int32_t b_block, const void* addend, int64_t ld_addend, void* out, int32_t out_type, int64_t ld_out,
+                   int64_t M, int64_t N, int64_t K, void* scratch, size_t scratch_bytes, int32_t* status, void* stream) {
+    if (!is_fp8_type(a_type) || !is_fp8_type(b_type) || !is_float_type(out_type) || (a_block != 1 && a_block != 128) || (b_block != 1 && b_block != 128) ||
+        M < 0 || N < 0 || K < 1 || M > INT32_MAX - 256 || N > INT32_MAX - 256 || K > INT32_MAX - 256 || ld_out < N || (addend && ld_addend < N))
+        return KGE_ERR_BAD_ARG;
+    if (M == 0 || N == 0) return KGE_OK;
+    if (!a || !b || !a_scales || !b_scales || !out || lda < K || ldb < K || lda % 16 || ldb % 16 || !aligned_to(a, 16) || !aligned_to(b, 16) ||
+        !aligned_to(a_scales, 4) || !aligned_to(b_scales, 4) || !aligned_to(out, type_bytes(out_type)) ||
+        (addend && !aligned_to(addend, type_bytes(out_type))) || !aligned_to(status, 4)) return KGE_ERR_BAD_ARG;
+    ProductParams p{};
+    p.M = M; p.N = N; p.kblocks = (int)ceil_div(K, FP_BK);
+    p.sa = a_scales; p.sb = b_scales; p.a_square = a_block == 128; p.b_square = b_block == 128;
+    p.sa_ld = p.a_square ? ceil_div(M, 128) : M; p.sb_ld = p.b_square ? ceil_div(N, 128) : N;
+    p.addend = addend; p.ld_addend = ld_addend; p.out = out; p.ld_out = ld_out; p.out_type = out_type;
+    const int ob = type_bytes(out_type);
+    p.vec = ld_out % 4 == 0 && aligned_to(out, 4 * ob) && (!addend || (ld_addend % 4 == 0 && aligned_to(addend, 4 * ob)));
+    p.status = status; p.wait_limit = kDefaultWaitLimit;
+    alignas(64) CUtensorMap ma, mb;
+    int sms = 0, rc = operand_map(&ma, a, M, K, lda);
+    if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb);
+    if (rc == KGE_OK) rc = sm_count(&sms);
+    if (rc != KGE_OK) return rc;
+    const int bn = N > 128 ? 256 : 128;
+    p.idesc = fp_idesc(FP_BM, bn, a_type == KGE_E5M2, b_type == KGE_E5M2);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return bn == 256 ? launch_product<256>(ma, mb, p, sms, s) : launch_product<128>(ma, mb, p, sms, s);
+}
+
+}  // extern "C"
