@@ -200,23 +200,28 @@ int launch_quantize(const QuantParams& p, int fmt, bool square, cudaStream_t s) 
 // ---- product ---------------------------------------------------------------------------------------------------------
 
 constexpr int FP_BM = 128, FP_BK = 128;                   // BK bytes = one 128-byte swizzle row
-constexpr int FP_STAGES = 4, FP_EPI_WARPS = 8;
-constexpr int FP_THREADS = 32 * (2 + FP_EPI_WARPS);
 constexpr uint32_t FP_BOX_BYTES = 128 * FP_BK;            // 128 rows of an operand
-constexpr uint32_t FP_STORE_BYTES = 4096;                 // per epilogue warp: 32 rows x 32 fp32 on their way to memory
+constexpr int FP_NACC = 2;                                // block sums in tensor memory
+constexpr int FP_COLS = 64;                               // columns of the tile per epilogue warp
+constexpr uint32_t FP_STORE_BYTES = 1024;                 // per epilogue warp: 32 rows x 32 bytes of the output on their way to memory
+constexpr int FP_SLOTS = 8;                               // blocks of K whose scales are in shared memory: more than stages and block sums together
+__host__ __device__ constexpr int fp_stages(int bn) { return bn == 256 ? 4 : 3; }
+__host__ __device__ constexpr int fp_epi_warps(int bn) { return 4 * bn / FP_COLS; }
+__host__ __device__ constexpr int fp_threads(int bn) { return 32 * (2 + fp_epi_warps(bn)); }
+__host__ __device__ constexpr int fp_ctas_per_sm(int bn) { return bn == 256 ? 1 : 2; }
 __host__ __device__ constexpr uint32_t fp_stage_bytes(int bn) { return FP_BOX_BYTES + (uint32_t)bn * FP_BK; }
-__host__ __device__ constexpr size_t fp_smem_bytes(int bn) { return 1024 + (size_t)FP_STAGES * fp_stage_bytes(bn) + 256 + FP_EPI_WARPS * FP_STORE_BYTES; }
+__host__ __device__ constexpr size_t fp_smem_bytes(int bn) { return (size_t)fp_stages(bn) * fp_stage_bytes(bn) + fp_epi_warps(bn) * FP_STORE_BYTES + FP_SLOTS * (128 + bn) * 4 + 256; }
 
 struct ProductParams {
     int64_t M, N;
-    int kblocks;
-    int64_t tiles_n, items;
+    int kblocks, kper;                    // blocks of K in all, and per CTA of a cluster
+    int tiles_n, items;
     const float *sa, *sb;
     int64_t sa_ld, sb_ld;                 // scales per block of K
     int a_square, b_square;               // a scale serves 128 rows
     const void* addend; int64_t ld_addend;
     void* out; int64_t ld_out; int out_type;
-    int vec;                              // packs of four columns of out (and addend) are aligned
+    int vec;                              // rows of out (and addend) start at multiples of 16 bytes
     int32_t* status; int wait_limit;
     uint32_t idesc;
 };
@@ -240,71 +245,188 @@ __device__ __forceinline__ void fp_mma(uint32_t d, uint64_t a, uint64_t b, uint3
 __device__ __forceinline__ void fp_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ void fp_copy4(uint32_t dst, const float* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void fp_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fp_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fp_tmem_ld32(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
+// 16 consecutive columns of this thread's tensor-memory lane; the registers are valid after fp_tmem_wait.
+__device__ __forceinline__ void fp_tmem_ld16(uint32_t taddr, uint64_t (&v)[8]) {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-        "tcgen05.wait::ld.sync.aligned;\n"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr) : "memory");
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 8; ++i) asm("mov.b64 %0, {%1, %2};" : "=l"(v[i]) : "r"(r[2 * i]), "r"(r[2 * i + 1]));
+}
+// Waits for this thread's tensor-memory loads; the registers pass through, so that nothing that uses them moves ahead.
+__device__ __forceinline__ void fp_tmem_wait(uint64_t (&v)[8]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+l"(v[0]), "+l"(v[1]), "+l"(v[2]), "+l"(v[3]), "+l"(v[4]), "+l"(v[5]), "+l"(v[6]), "+l"(v[7])::"memory");
+}
+// Two fp32 operations in one instruction, each rounded as a single one would be.
+__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 unpair(uint64_t a) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a)); return r; }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+
+// Calls f with a value of the output type.
+template <class F> __device__ __forceinline__ void fp_with_out(int t, F&& f) {
+    if (t == KGE_F32) f(float());
+    else if (t == KGE_BF16) f(__nv_bfloat16());
+    else f(__half());
 }
 
-// Four columns of a row: addend and conversion.
-template <typename TO>
-__device__ __forceinline__ void fp_put4(const ProductParams& p, int64_t row, int64_t col, float4 v) {
+// A pack of a row's columns.
+template <typename TO, int V>
+__device__ __forceinline__ void fp_put(const ProductParams& p, int row, int col, const Pack<TO, V>& o) {
     TO* dst = static_cast<TO*>(p.out) + row * p.ld_out + col;
-    const TO* add = p.addend ? static_cast<const TO*>(p.addend) + row * p.ld_addend + col : nullptr;
-    const float f[4] = {v.x, v.y, v.z, v.w};
-    if (p.vec && col + 4 <= p.N) {
-        Pack<TO, 4> o, a;
-        if (add) a = *reinterpret_cast<const Pack<TO, 4>*>(add);
+    if (p.vec && col + V <= p.N) *reinterpret_cast<Pack<TO, V>*>(dst) = o;
+    else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o.v[e] = from_float<TO>(add ? f[e] + to_float(a.v[e]) : f[e]);
-        *reinterpret_cast<Pack<TO, 4>*>(dst) = o;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) if (col + e < p.N) dst[e] = from_float<TO>(add ? f[e] + to_float(add[e]) : f[e]);
+        for (int e = 0; e < V; ++e) if (col + e < p.N) dst[e] = o.v[e];
     }
 }
 
-// Persistent CTAs, a 128 x BN tile of C at a time.  Warp 0 feeds a ring of shared-memory stages by TMA, warp 1 issues the MMAs of
-// one block of 128 k into one of the accumulators in tensor memory, eight warps multiply the finished block sums by their
-// scales and add them up in registers (a block's sum times two scales: the tensor cores cannot carry a scale over blocks).
-template <int BN>
-__global__ void __launch_bounds__(FP_THREADS, 1) fp8_product_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                                                                    const __grid_constant__ ProductParams p) {
-    constexpr uint32_t STAGE = fp_stage_bytes(BN);
-    constexpr int NACC = 512 / BN, COLS = BN / 2;
-    extern __shared__ unsigned char fp_smem_raw[];
-    unsigned char* base = fp_smem_raw + ((1024u - (smem_u32(fp_smem_raw) & 1023u)) & 1023u);
-    uint64_t* full = reinterpret_cast<uint64_t*>(base + (size_t)FP_STAGES * STAGE);
-    uint64_t* empty = full + FP_STAGES;
-    uint64_t* acc_full = empty + FP_STAGES;
-    uint64_t* acc_empty = acc_full + NACC;
-    uint64_t* done = acc_empty + NACC;
+// A warp's 32 rows x 64 columns, 32 bytes of each row at a time through shared memory: a store instruction covers whole 32-byte
+// sectors of sixteen rows.  Without an addend the values are rounded before they pass, with one after it is added.
+template <typename TO>
+__device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int col0, const uint64_t (&acc)[FP_COLS / 2], float4* st, int lane) {
+    constexpr int V = 16 / sizeof(TO);                    // columns per lane and store; two lanes cover a row's 32 bytes
+    const int unit = lane & 1;
+#pragma unroll
+    for (int c = 0; c < FP_COLS; c += 2 * V) {
+        Pack<TO, V> own[2];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float2 x = unpair(acc[c / 2 + e]);
+            own[2 * e / V].v[2 * e % V] = from_float<TO>(x.x);
+            own[2 * e / V].v[2 * e % V + 1] = from_float<TO>(x.y);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) st[lane * 2 + (i ^ (lane >> 2 & 1))] = *reinterpret_cast<const float4*>(&own[i]);
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = j * 16 + (lane >> 1), row = row0 + r, col = col0 + c + V * unit;
+            if (row < p.M && col < p.N) {
+                const float4 w = st[r * 2 + (unit ^ (r >> 2 & 1))];
+                fp_put<TO, V>(p, row, col, *reinterpret_cast<const Pack<TO, V>*>(&w));
+            }
+        }
+        __syncwarp();
+    }
+}
+
+// The addend of the same tile joins the accumulators in fp32 before they are rounded.  A lane reads its own row, a 32-byte sector at a
+// time (fetched into L2 when the tile began): through shared memory, as the stores go, the loads on their way took registers
+// from the accumulators.
+template <typename TO>
+__device__ __forceinline__ void fp_add(const ProductParams& p, int row, int col0, uint64_t (&acc)[FP_COLS / 2]) {
+    constexpr int V = 16 / sizeof(TO);
+    if (row >= p.M) return;
+    const TO* const add = static_cast<const TO*>(p.addend) + row * p.ld_addend + col0;
+    if (p.vec && col0 + FP_COLS <= p.N) {
+#pragma unroll
+        for (int c = 0; c < FP_COLS; c += V) {
+            const Pack<TO, V> a = *reinterpret_cast<const Pack<TO, V>*>(add + c);
+#pragma unroll
+            for (int e = 0; e < V; e += 2) acc[(c + e) / 2] = add2(acc[(c + e) / 2], pair(to_float(a.v[e]), to_float(a.v[e + 1])));
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < FP_COLS; ++c) {
+            if (col0 + c < p.N) acc[c / 2] = add2(acc[c / 2], c & 1 ? pair(0.f, to_float(add[c])) : pair(to_float(add[c]), 0.f));
+        }
+    }
+}
+template <typename TO>
+__device__ __forceinline__ void fp_prefetch_addend(const ProductParams& p, int row, int col0) {
+    if (row >= p.M) return;
+    const char* add = reinterpret_cast<const char*>(static_cast<const TO*>(p.addend) + row * p.ld_addend + col0);
+#pragma unroll
+    for (int b = 0; b < FP_COLS * (int)sizeof(TO); b += 128)
+        if (col0 + b / (int)sizeof(TO) < p.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(add + b));
+}
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ float4 cluster_ld(uint32_t addr, uint32_t rank) {
+    uint32_t at;
+    float4 v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+// A cluster's CTAs hold partial sums of one tile in their shared memory; each adds up a share of it in the order of their ranks.
+template <typename TO, int BN>
+__device__ __forceinline__ void fp_join(const ProductParams& p, uint32_t part, int m0, int n0, int tid) {
+    const int rows = min(FP_BM, (int)p.M - m0);
+    const uint32_t size = cluster_size();
+    constexpr int THREADS = 32 * fp_epi_warps(BN), PER_ROW = BN / 4;
+    for (int u = (int)cluster_rank() * THREADS + tid; u < rows * PER_ROW; u += (int)size * THREADS) {
+        const int r = u / PER_ROW, q = u % PER_ROW, row = m0 + r, col = n0 + 4 * q;
+        if (col >= p.N) continue;
+        float4 v[8];
+#pragma unroll
+        for (int z = 0; z < 8; ++z) v[z] = z < (int)size ? cluster_ld(part + (uint32_t)(r * PER_ROW + (q ^ (r & 7))) * 16, z) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int z = 1; z < 8; ++z) { v[0].x += v[z].x; v[0].y += v[z].y; v[0].z += v[z].z; v[0].w += v[z].w; }
+        float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+        Pack<TO, 4> o;
+        if (p.addend) {
+            const TO* add = static_cast<const TO*>(p.addend) + row * p.ld_addend + col;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) if (col + e < p.N) f[e] += to_float(add[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o.v[e] = from_float<TO>(f[e]);
+        fp_put<TO, 4>(p, row, col, o);
+    }
+}
+
+// A 128 x BN tile of C at a time (persistent CTAs), or one per cluster, whose CTAs share its blocks of K (SPLIT).  Warp 0 feeds a
+// ring of shared-memory stages by TMA, warp 1 issues the MMAs of one block of 128 k into one of two accumulators in tensor memory,
+// the other warps, 64 columns each, multiply finished block sums by their scales and add them up in registers (the tensor cores
+// cannot carry an fp32 scale from block to block).
+template <int BN, bool SPLIT>
+__global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_product_kernel(const __grid_constant__ CUtensorMap tmA,
+                                                                                          const __grid_constant__ CUtensorMap tmB,
+                                                                                          const __grid_constant__ ProductParams p) {
+    constexpr uint32_t STAGE = fp_stage_bytes(BN), TMEM_COLS = FP_NACC * BN;
+    constexpr int STAGES = fp_stages(BN), EW = fp_epi_warps(BN);
+    extern __shared__ __align__(1024) unsigned char fp_smem[];
+    float4* const stores = reinterpret_cast<float4*>(fp_smem + (size_t)STAGES * STAGE);
+    float* const scales = reinterpret_cast<float*>(fp_smem + (size_t)STAGES * STAGE + EW * FP_STORE_BYTES);     // per slot: 128 of A, BN of B
+    uint64_t* full = reinterpret_cast<uint64_t*>(scales + FP_SLOTS * (128 + BN));
+    uint64_t* empty = full + STAGES;
+    uint64_t* sc_full = empty + STAGES;
+    uint64_t* sc_empty = sc_full + FP_SLOTS;
+    uint64_t* acc_full = sc_empty + FP_SLOTS;
+    uint64_t* acc_empty = acc_full + FP_NACC;
+    uint64_t* done = acc_empty + FP_NACC;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
     volatile uint32_t* stop = tmem_slot + 1;
     volatile uint32_t* filled = tmem_slot + 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < FP_STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < NACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], FP_EPI_WARPS); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < FP_SLOTS; ++s) { mbar_init(&sc_full[s], 32); mbar_init(&sc_empty[s], EW); }
+        for (int b = 0; b < FP_NACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], EW); }
         mbar_init(done, 1);
         *stop = 0;
         mbar_init_fence();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     fp_fence_before();
@@ -312,101 +434,128 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp8_product_kernel(const __grid
     fp_fence_after();
     const uint32_t tmem = *tmem_slot;
 
+    const int step = SPLIT ? p.items : (int)gridDim.x;
+    const int first = SPLIT ? (int)(blockIdx.x / cluster_size()) : (int)blockIdx.x;
+    const int kb0 = SPLIT ? (int)cluster_rank() * p.kper : 0, kb1 = SPLIT ? min(p.kblocks, kb0 + p.kper) : p.kblocks;
+
     if (warp == 0) {
-        if (lane == 0) {
-            int64_t ring = 0;
-            for (int64_t item = blockIdx.x; item < p.items && !*stop; item += gridDim.x) {
-                const int m0 = (int)(item / p.tiles_n) * FP_BM, n0 = (int)(item % p.tiles_n) * BN;
-                for (int kb = 0; kb < p.kblocks; ++kb, ++ring) {
-                    const int s = (int)(ring % FP_STAGES);
-                    if (!mbar_wait_idle(&empty[s], (uint32_t)((ring / FP_STAGES) & 1) ^ 1u, p.wait_limit)) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); break; }
-                    unsigned char* sa = base + (size_t)s * STAGE;
+        // lane 0 the operands, all lanes the scales (four bytes each: a row of scales may begin anywhere)
+        uint32_t s = 0, phase = 1, count = 0, slot = 0, slot_phase = 1;
+        bool ok = true;
+        for (int item = first; item < p.items && ok; item += step) {
+            const int m0 = item / p.tiles_n * FP_BM, n0 = item % p.tiles_n * BN;
+            const float* const sa0 = p.sa + (p.a_square ? m0 >> 7 : m0 + lane);
+            const float* const sb0 = p.sb + (p.b_square ? (n0 >> 7) + lane : n0 + lane);
+            const int na = p.a_square ? (lane == 0 ? 1 : 0) : (int)p.M - m0 - lane;         // (values to copy are those i with 32 i < na)
+            const int nb = p.b_square ? (lane < BN / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = mbar_wait_idle(&sc_empty[slot], slot_phase, p.wait_limit) && mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop;
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
+                if (lane == 0) {
+                    unsigned char* sa = fp_smem + s * STAGE;
                     mbar_arrive_expect_tx(&full[s], STAGE);
                     fp_tma_load(sa, &tmA, kb * FP_BK, m0, &full[s]);
 #pragma unroll
                     for (int g = 0; g < BN / 128; ++g) fp_tma_load(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
                 }
+                const uint32_t at = smem_u32(scales + slot * (128 + BN) + lane);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (32 * i < na) fp_copy4(at + 128 * i, sa0 + kb * p.sa_ld + 32 * i);
+#pragma unroll
+                for (int i = 0; i < BN / 32; ++i) if (32 * i < nb) fp_copy4(at + 512 + 128 * i, sb0 + kb * p.sb_ld + 32 * i);
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sc_full[slot])) : "memory");
+                ++count;
+                if (++s == STAGES) { s = 0; phase ^= 1; }
+                if (++slot == FP_SLOTS) { slot = 0; slot_phase ^= 1; }
             }
-            *filled = (uint32_t)min(ring, (int64_t)1 << 30);
         }
+        if (lane == 0) *filled = count;
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp == 1) {
         if (lane == 0) {
-            int64_t ring = 0;
+            uint32_t s = 0, phase = 0, buf = 0, acc_phase = 1;
             bool ok = true;
-            for (int64_t item = blockIdx.x; item < p.items && ok && !*stop; item += gridDim.x) {
-                for (int kb = 0; kb < p.kblocks; ++kb, ++ring) {
-                    const int s = (int)(ring % FP_STAGES), buf = (int)(ring % NACC);
-                    if (!mbar_wait_idle(&acc_empty[buf], (uint32_t)((ring / NACC) & 1) ^ 1u, p.wait_limit) ||
-                        !mbar_wait_idle(&full[s], (uint32_t)(ring / FP_STAGES) & 1u, p.wait_limit)) { ok = false; break; }
+            for (int item = first; item < p.items && ok && !*stop; item += step) {
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (!mbar_wait_idle(&acc_empty[buf], acc_phase, p.wait_limit) || !mbar_wait_idle(&full[s], phase, p.wait_limit)) { ok = false; break; }
                     fp_fence_after();
-                    const uint32_t sa = smem_u32(base + (size_t)s * STAGE);
+                    const uint32_t sa = smem_u32(fp_smem + s * STAGE);
 #pragma unroll
                     for (int k = 0; k < FP_BK / 32; ++k)
-                        fp_mma(tmem + (uint32_t)(buf * BN), fp_desc(sa + k * 32), fp_desc(sa + FP_BOX_BYTES + k * 32), p.idesc, k != 0);
+                        fp_mma(tmem + buf * BN, fp_desc(sa + k * 32), fp_desc(sa + FP_BOX_BYTES + k * 32), p.idesc, k != 0);
                     fp_commit(&empty[s]);
                     fp_commit(&acc_full[buf]);
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
+                    if (++buf == FP_NACC) { buf = 0; acc_phase ^= 1; }
                 }
             }
             if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
         }
     } else {
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        float4* st = reinterpret_cast<float4*>(base + (size_t)FP_STAGES * STAGE + 256) + (size_t)(warp - 2) * (FP_STORE_BYTES / 16);
-        int64_t ring = 0;
+        const int quarter = warp & 3, group = (warp - 2) >> 2;      // tensor-memory lanes and columns of this warp
+        float4* const st = stores + (warp - 2) * (FP_STORE_BYTES / 16);
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group * FP_COLS);
+        uint32_t buf = 0, phase = 0, slot = 0, slot_phase = 0;
         bool ok = true;
-        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            const int64_t m0 = (item / p.tiles_n) * FP_BM, n0 = (item % p.tiles_n) * BN + half * COLS;
-            const int64_t row = m0 + quarter * 32 + lane;
-            float acc[COLS];
+        for (int item = first; item < p.items && ok; item += step) {
+            const int m0 = item / p.tiles_n * FP_BM + quarter * 32, n0 = item % p.tiles_n * BN + group * FP_COLS;
+            uint64_t acc[FP_COLS / 2];
 #pragma unroll
-            for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
-            for (int kb = 0; kb < p.kblocks; ++kb, ++ring) {
-                const int buf = (int)(ring % NACC);
-                float sa = 0.f;
-                if (row < p.M) sa = p.sa[kb * p.sa_ld + (p.a_square ? row >> 7 : row)];
-                if (p.b_square && n0 < p.N) sa *= p.sb[kb * p.sb_ld + (n0 >> 7)];
-                ok = mbar_wait_bounded(&acc_full[buf], (uint32_t)(ring / NACC) & 1u, p.wait_limit) && !*stop;
+            for (int i = 0; i < FP_COLS / 2; ++i) acc[i] = 0ull;
+            if (!SPLIT && p.addend) fp_with_out(p.out_type, [&](auto t) { fp_prefetch_addend<decltype(t)>(p, m0 + lane, n0); });
+#pragma unroll 1
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = mbar_wait_bounded(&sc_full[slot], slot_phase, p.wait_limit) && mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit) && !*stop;
                 ok = __all_sync(0xffffffffu, ok);
                 fp_fence_after();
                 if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
-                const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + half * COLS);
+                const float* const sc = scales + slot * (128 + BN);
+                const float4* const sb = reinterpret_cast<const float4*>(sc + 128 + group * FP_COLS);
+                float s = sc[p.a_square ? 0 : quarter * 32 + lane];
+                if (p.b_square) s *= sc[128 + group * FP_COLS / 128];
+                const uint64_t s2 = pair(s, s);
 #pragma unroll
-                for (int c = 0; c < COLS; c += 32) {
-                    float v[32];
-                    fp_tmem_ld32(taddr + (uint32_t)c, v);
+                for (int c = 0; c < FP_COLS / 16; ++c) {
+                    uint64_t v[8];
+                    fp_tmem_ld16(taddr + buf * BN + (uint32_t)c * 16, v);
+                    fp_tmem_wait(v);
+                    if (c + 1 == FP_COLS / 16) {       // the accumulator is read: the next block's MMAs may begin
+                        fp_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&acc_empty[buf]);
+                    }
                     if (p.b_square) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[c + i] = fmaf(v[i], sa, acc[c + i]);
+                        for (int i = 0; i < 8; ++i) acc[c * 8 + i] = fma2(v[i], s2, acc[c * 8 + i]);
                     } else {
-                        const float* sb = p.sb + kb * p.sb_ld + n0 + c;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) acc[c + i] = fmaf(v[i], sa * (n0 + c + i < p.N ? sb[i] : 0.f), acc[c + i]);
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 b = sb[c * 4 + i];
+                            acc[c * 8 + 2 * i] = fma2(v[2 * i], mul2(s2, pair(b.x, b.y)), acc[c * 8 + 2 * i]);
+                            acc[c * 8 + 2 * i + 1] = fma2(v[2 * i + 1], mul2(s2, pair(b.z, b.w)), acc[c * 8 + 2 * i + 1]);
+                        }
                     }
                 }
-                fp_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[buf]);
+                if (lane == 0) mbar_arrive(&sc_empty[slot]);
+                if (++buf == FP_NACC) { buf = 0; phase ^= 1; }
+                if (++slot == FP_SLOTS) { slot = 0; slot_phase ^= 1; }
             }
             if (!ok) break;
-            // through shared memory: a store instruction covers four rows' 32 columns
-            const int sw = lane & 7;
+            if (SPLIT) {       // the ring's stages are free: every copy has been multiplied, every product read
+                float4* part = reinterpret_cast<float4*>(fp_smem);
+                const int r = quarter * 32 + lane;
 #pragma unroll
-            for (int c = 0; c < COLS; c += 32) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) st[lane * 8 + (i ^ sw)] = make_float4(acc[c + 4 * i], acc[c + 4 * i + 1], acc[c + 4 * i + 2], acc[c + 4 * i + 3]);
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int r = j * 4 + (lane >> 3), q = lane & 7;
-                    const float4 val = st[r * 8 + (q ^ (r & 7))];
-                    const int64_t orow = m0 + quarter * 32 + r, ocol = n0 + c + 4 * q;
-                    if (orow < p.M && ocol < p.N) {
-                        if (p.out_type == KGE_F32) fp_put4<float>(p, orow, ocol, val);
-                        else if (p.out_type == KGE_BF16) fp_put4<__nv_bfloat16>(p, orow, ocol, val);
-                        else fp_put4<__half>(p, orow, ocol, val);
-                    }
+                for (int i = 0; i < FP_COLS / 4; ++i) {
+                    const float2 a = unpair(acc[2 * i]), b = unpair(acc[2 * i + 1]);
+                    part[r * (BN / 4) + ((group * (FP_COLS / 4) + i) ^ (r & 7))] = make_float4(a.x, a.y, b.x, b.y);
                 }
-                __syncwarp();
+            } else {
+                fp_with_out(p.out_type, [&](auto t) {
+                    if (p.addend) fp_add<decltype(t)>(p, m0 + lane, n0, acc);
+                    fp_store<decltype(t)>(p, m0, n0, acc, st, lane);
+                });
             }
         }
     }
@@ -414,12 +563,20 @@ __global__ void __launch_bounds__(FP_THREADS, 1) fp8_product_kernel(const __grid
     __syncthreads();
     if (*stop) {       // copies and MMAs in flight are waited for before the CTA's memory is given back
         if (lane == 0) {
-            if (warp == 0) { const int n = (int)*filled; for (int r = max(0, n - FP_STAGES); r < n; ++r) mbar_wait_idle(&full[r % FP_STAGES], (r / FP_STAGES) & 1, kDefaultWaitLimit); }
+            if (warp == 0) { const int n = (int)*filled; for (int r = max(0, n - STAGES); r < n; ++r) mbar_wait_idle(&full[r % STAGES], (r / STAGES) & 1, kDefaultWaitLimit); }
             if (warp == 1) { fp_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
         }
         __syncthreads();
     }
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (SPLIT) {           // (every CTA of the cluster comes here, also after a wait that ran out)
+        cluster_sync();
+        if (warp >= 2) {
+            const int m0 = first / p.tiles_n * FP_BM, n0 = first % p.tiles_n * BN;
+            fp_with_out(p.out_type, [&](auto t) { fp_join<decltype(t), BN>(p, smem_u32(fp_smem), m0, n0, threadIdx.x - 64); });
+        }
+        cluster_sync();    // no CTA leaves while another reads its partial sums
+    }
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -455,18 +612,38 @@ int sm_count(int* sms) {
     return KGE_OK;
 }
 
-template <int BN>
-int launch_product(const CUtensorMap& a, const CUtensorMap& b, ProductParams& p, int sms, cudaStream_t s) {
+// How a product is cut up: columns of a tile, and CTAs that share a tile's blocks of K.
+struct ProductPlan { int bn, split; };
+ProductPlan product_plan(int64_t M, int64_t N, int kblocks, int sms) {
+    const int64_t tiles128 = ceil_div(M, FP_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, FP_BM) * ceil_div(N, 256);
+    if (tiles128 < sms && kblocks > 1) {
+        int split = (int)std::min<int64_t>({8, kblocks, std::max<int64_t>(1, sms / tiles128)});
+        const int per = (kblocks + split - 1) / split;
+        split = (kblocks + per - 1) / per;              // every CTA has a block
+        if (split > 1) return {128, split};
+    }
+    return {tiles256 >= sms && kblocks >= 16 ? 256 : 128, 1};
+}
+
+template <int BN, bool SPLIT>
+int launch_product(const CUtensorMap& a, const CUtensorMap& b, ProductParams& p, int split, int sms, cudaStream_t s) {
     constexpr size_t smem = fp_smem_bytes(BN);
     static DeviceOnce configured;
     cudaError_t e = once_per_device(configured, [] {
-        return cudaFuncSetAttribute(fp8_product_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        return cudaFuncSetAttribute(fp8_product_kernel<BN, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
     if (e != cudaSuccess) return KGE_ERR_CUDA;
-    p.tiles_n = ceil_div(p.N, BN);
-    p.items = ceil_div(p.M, FP_BM) * p.tiles_n;
-    fp8_product_kernel<BN><<<(unsigned)std::min<int64_t>(p.items, sms), FP_THREADS, smem, s>>>(a, b, p);
-    return launch_status(cudaGetLastError());
+    p.tiles_n = (int)ceil_div(p.N, BN);
+    p.items = (int)(ceil_div(p.M, FP_BM) * p.tiles_n);
+    p.kper = (p.kblocks + split - 1) / split;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(SPLIT ? p.items * split : std::min<int64_t>(p.items, (int64_t)sms * fp_ctas_per_sm(BN))));
+    cfg.blockDim = dim3(fp_threads(BN)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = SPLIT ? 1 : 0;
+    return launch_status(cudaLaunchKernelEx(&cfg, fp8_product_kernel<BN, SPLIT>, a, b, p));
 }
 
 }  // namespace
@@ -512,17 +689,19 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
     p.sa_ld = p.a_square ? ceil_div(M, 128) : M; p.sb_ld = p.b_square ? ceil_div(N, 128) : N;
     p.addend = addend; p.ld_addend = ld_addend; p.out = out; p.ld_out = ld_out; p.out_type = out_type;
     const int ob = type_bytes(out_type);
-    p.vec = ld_out % 4 == 0 && aligned_to(out, 4 * ob) && (!addend || (ld_addend % 4 == 0 && aligned_to(addend, 4 * ob)));
+    p.vec = ld_out * ob % 16 == 0 && aligned_to(out, 16) && (!addend || (ld_addend * ob % 16 == 0 && aligned_to(addend, 16)));
     p.status = status; p.wait_limit = kDefaultWaitLimit;
     alignas(64) CUtensorMap ma, mb;
     int sms = 0, rc = operand_map(&ma, a, M, K, lda);
     if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb);
     if (rc == KGE_OK) rc = sm_count(&sms);
     if (rc != KGE_OK) return rc;
-    const int bn = N > 128 ? 256 : 128;
-    p.idesc = fp_idesc(FP_BM, bn, a_type == KGE_E5M2, b_type == KGE_E5M2);
+    if (ceil_div(M, 128) * ceil_div(N, 128) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;
+    const ProductPlan plan = product_plan(M, N, p.kblocks, sms);
+    p.idesc = fp_idesc(FP_BM, plan.bn, a_type == KGE_E5M2, b_type == KGE_E5M2);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return bn == 256 ? launch_product<256>(ma, mb, p, sms, s) : launch_product<128>(ma, mb, p, sms, s);
+    if (plan.split > 1) return launch_product<128, true>(ma, mb, p, plan.split, sms, s);
+    return plan.bn == 256 ? launch_product<256, false>(ma, mb, p, 1, sms, s) : launch_product<128, false>(ma, mb, p, 1, sms, s);
 }
 
 }  // extern "C"
