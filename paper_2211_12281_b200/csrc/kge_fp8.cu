@@ -204,10 +204,13 @@ constexpr uint32_t FP_BOX_BYTES = 128 * FP_BK;            // 128 rows of an oper
 constexpr int FP_NACC = 2;                                // block sums in tensor memory
 constexpr int FP_COLS = 64;                               // columns of the tile per epilogue warp
 constexpr uint32_t FP_STORE_BYTES = 1024;                 // per epilogue warp: 32 rows x 32 bytes of the output on their way to memory
-constexpr int FP_SLOTS = 8;                               // blocks of K whose scales are in shared memory: more than stages and block sums together
+// Blocks of K whose scales are in shared memory.  A slot needs no barrier of its own: its block's scales are read before the epilogue
+// hands back the block sum after the next one, without which no MMA of the block FP_NACC later is issued, without which no stage
+// that follows by fp_stages() more is filled again -- at least stages + FP_NACC + 1 blocks later.
+constexpr int FP_SLOTS = 8;
 __host__ __device__ constexpr int fp_stages(int bn) { return bn == 256 ? 4 : 3; }
 __host__ __device__ constexpr int fp_epi_warps(int bn) { return 4 * bn / FP_COLS; }
-__host__ __device__ constexpr int fp_threads(int bn) { return 32 * (2 + fp_epi_warps(bn)); }
+__host__ __device__ constexpr int fp_threads(int bn) { return 32 * (4 + fp_epi_warps(bn)); }     // (four more: copies, MMAs, two idle)
 __host__ __device__ constexpr int fp_ctas_per_sm(int bn) { return bn == 256 ? 1 : 2; }
 __host__ __device__ constexpr uint32_t fp_stage_bytes(int bn) { return FP_BOX_BYTES + (uint32_t)bn * FP_BK; }
 __host__ __device__ constexpr size_t fp_smem_bytes(int bn) { return (size_t)fp_stages(bn) * fp_stage_bytes(bn) + fp_epi_warps(bn) * FP_STORE_BYTES + FP_SLOTS * (128 + bn) * 4 + 256; }
@@ -272,6 +275,10 @@ __device__ __forceinline__ float2 unpair(uint64_t a) { float2 r; asm("mov.b64 {%
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+
+// Registers of a warpgroup, out of what the block was launched with.
+template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // Calls f with a value of the output type.
 template <class F> __device__ __forceinline__ void fp_with_out(int t, F&& f) {
@@ -402,14 +409,16 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
                                                                                           const __grid_constant__ ProductParams p) {
     constexpr uint32_t STAGE = fp_stage_bytes(BN), TMEM_COLS = FP_NACC * BN;
     constexpr int STAGES = fp_stages(BN), EW = fp_epi_warps(BN);
+    // registers per thread as launched (20 warps x 96, or 12 x 80 twice), and how they are shared out: the epilogue's 64 sums and 32
+    // loaded values do not fit the launch's share
+    constexpr int REGS = BN == 256 ? 96 : 80, REGS_CONTROL = 32, REGS_EPI = REGS + 4 * (REGS - REGS_CONTROL) / EW / 8 * 8;
+    static_assert(4 * REGS_CONTROL + EW * REGS_EPI <= (4 + EW) * REGS, "register shares exceed the launch's");
     extern __shared__ __align__(1024) unsigned char fp_smem[];
     float4* const stores = reinterpret_cast<float4*>(fp_smem + (size_t)STAGES * STAGE);
     float* const scales = reinterpret_cast<float*>(fp_smem + (size_t)STAGES * STAGE + EW * FP_STORE_BYTES);     // per slot: 128 of A, BN of B
     uint64_t* full = reinterpret_cast<uint64_t*>(scales + FP_SLOTS * (128 + BN));
     uint64_t* empty = full + STAGES;
-    uint64_t* sc_full = empty + STAGES;
-    uint64_t* sc_empty = sc_full + FP_SLOTS;
-    uint64_t* acc_full = sc_empty + FP_SLOTS;
+    uint64_t* acc_full = empty + STAGES;
     uint64_t* acc_empty = acc_full + FP_NACC;
     uint64_t* done = acc_empty + FP_NACC;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
@@ -418,9 +427,8 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int s = 0; s < FP_SLOTS; ++s) { mbar_init(&sc_full[s], 32); mbar_init(&sc_empty[s], EW); }
-        for (int b = 0; b < FP_NACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], EW); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 33); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < FP_NACC; ++b) { mbar_init(&acc_full[b], 2); mbar_init(&acc_empty[b], EW); }
         mbar_init(done, 1);
         *stop = 0;
         mbar_init_fence();
@@ -438,65 +446,71 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
     const int first = SPLIT ? (int)(blockIdx.x / cluster_size()) : (int)blockIdx.x;
     const int kb0 = SPLIT ? (int)cluster_rank() * p.kper : 0, kb1 = SPLIT ? min(p.kblocks, kb0 + p.kper) : p.kblocks;
 
-    if (warp == 0) {
-        // lane 0 the operands, all lanes the scales (four bytes each: a row of scales may begin anywhere)
-        uint32_t s = 0, phase = 1, count = 0, slot = 0, slot_phase = 1;
-        bool ok = true;
-        for (int item = first; item < p.items && ok; item += step) {
-            const int m0 = item / p.tiles_n * FP_BM, n0 = item % p.tiles_n * BN;
-            const float* const sa0 = p.sa + (p.a_square ? m0 >> 7 : m0 + lane);
-            const float* const sb0 = p.sb + (p.b_square ? (n0 >> 7) + lane : n0 + lane);
-            const int na = p.a_square ? (lane == 0 ? 1 : 0) : (int)p.M - m0 - lane;         // (values to copy are those i with 32 i < na)
-            const int nb = p.b_square ? (lane < BN / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                ok = mbar_wait_idle(&sc_empty[slot], slot_phase, p.wait_limit) && mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop;
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
-                if (lane == 0) {
-                    unsigned char* sa = fp_smem + s * STAGE;
-                    mbar_arrive_expect_tx(&full[s], STAGE);
-                    fp_tma_load(sa, &tmA, kb * FP_BK, m0, &full[s]);
-#pragma unroll
-                    for (int g = 0; g < BN / 128; ++g) fp_tma_load(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
-                }
-                const uint32_t at = smem_u32(scales + slot * (128 + BN) + lane);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) if (32 * i < na) fp_copy4(at + 128 * i, sa0 + kb * p.sa_ld + 32 * i);
-#pragma unroll
-                for (int i = 0; i < BN / 32; ++i) if (32 * i < nb) fp_copy4(at + 512 + 128 * i, sb0 + kb * p.sb_ld + 32 * i);
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sc_full[slot])) : "memory");
-                ++count;
-                if (++s == STAGES) { s = 0; phase ^= 1; }
-                if (++slot == FP_SLOTS) { slot = 0; slot_phase ^= 1; }
-            }
-        }
-        if (lane == 0) *filled = count;
-        asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (warp == 1) {
-        if (lane == 0) {
-            uint32_t s = 0, phase = 0, buf = 0, acc_phase = 1;
+    if (warp < 4) {
+        registers_down<REGS_CONTROL>();
+        if (warp == 0) {
+            // lane 0 the operands, all lanes the scales (four bytes each: a row of scales may begin anywhere)
+            uint32_t s = 0, phase = 1, count = 0, slot = 0;
             bool ok = true;
-            for (int item = first; item < p.items && ok && !*stop; item += step) {
+            for (int item = first; item < p.items && ok; item += step) {
+                const int m0 = item / p.tiles_n * FP_BM, n0 = item % p.tiles_n * BN;
+                const float* const sa0 = p.sa + (p.a_square ? m0 >> 7 : m0 + lane);
+                const float* const sb0 = p.sb + (p.b_square ? (n0 >> 7) + lane : n0 + lane);
+                const int na = p.a_square ? (lane == 0 ? 1 : 0) : (int)p.M - m0 - lane;         // (values to copy are those i with 32 i < na)
+                const int nb = p.b_square ? (lane < BN / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
                 for (int kb = kb0; kb < kb1; ++kb) {
-                    if (!mbar_wait_idle(&acc_empty[buf], acc_phase, p.wait_limit) || !mbar_wait_idle(&full[s], phase, p.wait_limit)) { ok = false; break; }
-                    fp_fence_after();
-                    const uint32_t sa = smem_u32(fp_smem + s * STAGE);
-#pragma unroll
-                    for (int k = 0; k < FP_BK / 32; ++k)
-                        fp_mma(tmem + buf * BN, fp_desc(sa + k * 32), fp_desc(sa + FP_BOX_BYTES + k * 32), p.idesc, k != 0);
-                    fp_commit(&empty[s]);
-                    fp_commit(&acc_full[buf]);
+                    ok = mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop;
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
+                    if (lane == 0) {
+                        unsigned char* sa = fp_smem + s * STAGE;
+                        mbar_arrive_expect_tx(&full[s], STAGE);
+                        fp_tma_load(sa, &tmA, kb * FP_BK, m0, &full[s]);
+    #pragma unroll
+                        for (int g = 0; g < BN / 128; ++g) fp_tma_load(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
+                    }
+                    const uint32_t at = smem_u32(scales + slot * (128 + BN) + lane);
+    #pragma unroll
+                    for (int i = 0; i < 4; ++i) if (32 * i < na) fp_copy4(at + 128 * i, sa0 + kb * p.sa_ld + 32 * i);
+    #pragma unroll
+                    for (int i = 0; i < BN / 32; ++i) if (32 * i < nb) fp_copy4(at + 512 + 128 * i, sb0 + kb * p.sb_ld + 32 * i);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
+                    ++count;
                     if (++s == STAGES) { s = 0; phase ^= 1; }
-                    if (++buf == FP_NACC) { buf = 0; acc_phase ^= 1; }
+                    if (++slot == FP_SLOTS) slot = 0;
                 }
             }
-            if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
+            if (lane == 0) *filled = count;
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        } else if (warp == 1) {
+            if (lane == 0) {
+                uint32_t s = 0, phase = 0, buf = 0, acc_phase = 1;
+                bool ok = true;
+                for (int item = first; item < p.items && ok && !*stop; item += step) {
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        if (!mbar_wait_idle(&acc_empty[buf], acc_phase, p.wait_limit) || !mbar_wait_idle(&full[s], phase, p.wait_limit)) { ok = false; break; }
+                        fp_fence_after();
+                        const uint32_t sa = smem_u32(fp_smem + s * STAGE);
+    #pragma unroll
+                        for (int k = 0; k < FP_BK / 32; ++k)
+                            fp_mma(tmem + buf * BN, fp_desc(sa + k * 32), fp_desc(sa + FP_BOX_BYTES + k * 32), p.idesc, k != 0);
+                        fp_commit(&empty[s]);
+                        mbar_arrive(&acc_full[buf]);       // (hands on what the wait for the stage made visible: the scales)
+                        fp_commit(&acc_full[buf]);
+                        if (++s == STAGES) { s = 0; phase ^= 1; }
+                        if (++buf == FP_NACC) { buf = 0; acc_phase ^= 1; }
+                    }
+                }
+                if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
+            }
         }
+        if (SPLIT) { cluster_sync(); cluster_sync(); }
     } else {
-        const int quarter = warp & 3, group = (warp - 2) >> 2;      // tensor-memory lanes and columns of this warp
-        float4* const st = stores + (warp - 2) * (FP_STORE_BYTES / 16);
+        registers_up<REGS_EPI>();
+        const int quarter = warp & 3, group = (warp - 4) >> 2;      // tensor-memory lanes and columns of this warp
+        float4* const st = stores + (warp - 4) * (FP_STORE_BYTES / 16);
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group * FP_COLS);
-        uint32_t buf = 0, phase = 0, slot = 0, slot_phase = 0;
+        uint32_t buf = 0, phase = 0, slot = 0;
         bool ok = true;
         for (int item = first; item < p.items && ok; item += step) {
             const int m0 = item / p.tiles_n * FP_BM + quarter * 32, n0 = item % p.tiles_n * BN + group * FP_COLS;
@@ -506,10 +520,12 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
             if (!SPLIT && p.addend) fp_with_out(p.out_type, [&](auto t) { fp_prefetch_addend<decltype(t)>(p, m0 + lane, n0); });
 #pragma unroll 1
             for (int kb = kb0; kb < kb1; ++kb) {
-                ok = mbar_wait_bounded(&sc_full[slot], slot_phase, p.wait_limit) && mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit) && !*stop;
-                ok = __all_sync(0xffffffffu, ok);
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit));
                 fp_fence_after();
                 if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
+                const uint32_t from = taddr + buf * BN;
+                uint64_t v[2][8];
+                fp_tmem_ld16(from, v[0]);
                 const float* const sc = scales + slot * (128 + BN);
                 const float4* const sb = reinterpret_cast<const float4*>(sc + 128 + group * FP_COLS);
                 float s = sc[p.a_square ? 0 : quarter * 32 + lane];
@@ -517,30 +533,28 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
                 const uint64_t s2 = pair(s, s);
 #pragma unroll
                 for (int c = 0; c < FP_COLS / 16; ++c) {
-                    uint64_t v[8];
-                    fp_tmem_ld16(taddr + buf * BN + (uint32_t)c * 16, v);
-                    fp_tmem_wait(v);
-                    if (c + 1 == FP_COLS / 16) {       // the accumulator is read: the next block's MMAs may begin
+                    uint64_t (&w)[8] = v[c & 1];
+                    fp_tmem_wait(w);
+                    if (c + 1 < FP_COLS / 16) fp_tmem_ld16(from + (uint32_t)(c + 1) * 16, v[(c + 1) & 1]);
+                    else {                 // the accumulator is read: the next block's MMAs may begin
                         fp_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&acc_empty[buf]);
                     }
                     if (p.b_square) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) acc[c * 8 + i] = fma2(v[i], s2, acc[c * 8 + i]);
+                        for (int i = 0; i < 8; ++i) acc[c * 8 + i] = fma2(w[i], s2, acc[c * 8 + i]);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float4 b = sb[c * 4 + i];
-                            acc[c * 8 + 2 * i] = fma2(v[2 * i], mul2(s2, pair(b.x, b.y)), acc[c * 8 + 2 * i]);
-                            acc[c * 8 + 2 * i + 1] = fma2(v[2 * i + 1], mul2(s2, pair(b.z, b.w)), acc[c * 8 + 2 * i + 1]);
+                            acc[c * 8 + 2 * i] = fma2(w[2 * i], mul2(s2, pair(b.x, b.y)), acc[c * 8 + 2 * i]);
+                            acc[c * 8 + 2 * i + 1] = fma2(w[2 * i + 1], mul2(s2, pair(b.z, b.w)), acc[c * 8 + 2 * i + 1]);
                         }
                     }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sc_empty[slot]);
                 if (++buf == FP_NACC) { buf = 0; phase ^= 1; }
-                if (++slot == FP_SLOTS) { slot = 0; slot_phase ^= 1; }
+                if (++slot == FP_SLOTS) slot = 0;
             }
             if (!ok) break;
             if (SPLIT) {       // the ring's stages are free: every copy has been multiplied, every product read
@@ -558,6 +572,12 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
                 });
             }
         }
+        if (SPLIT) {       // (every warp of the cluster comes here, also after a wait that ran out)
+            cluster_sync();
+            const int m0 = first / p.tiles_n * FP_BM, n0 = first % p.tiles_n * BN;
+            fp_with_out(p.out_type, [&](auto t) { fp_join<decltype(t), BN>(p, smem_u32(fp_smem), m0, n0, threadIdx.x - 128); });
+            cluster_sync();        // no CTA leaves while another reads its partial sums
+        }
     }
     fp_fence_before();
     __syncthreads();
@@ -567,14 +587,6 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
             if (warp == 1) { fp_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
         }
         __syncthreads();
-    }
-    if (SPLIT) {           // (every CTA of the cluster comes here, also after a wait that ran out)
-        cluster_sync();
-        if (warp >= 2) {
-            const int m0 = first / p.tiles_n * FP_BM, n0 = first % p.tiles_n * BN;
-            fp_with_out(p.out_type, [&](auto t) { fp_join<decltype(t), BN>(p, smem_u32(fp_smem), m0, n0, threadIdx.x - 64); });
-        }
-        cluster_sync();    // no CTA leaves while another reads its partial sums
     }
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
 }
