@@ -206,87 +206,115 @@ def ensemble_topk(lists, table, top_n, out_ids, out_scores=None) -> int:
 
 
 # ---- operators on rows: no handle, every tensor on one device ----
+# (The smallest of these calls take a few microseconds on the GPU: what is looked at here is looked at once and without detours.)
 
 KGE_ERR_BAD_ARG = -1
-_DTYPES = {}        # torch dtype -> kge_dtype_t (filled on first use: importing this module does not import torch)
+_FLOAT, _FP8 = {}, {}      # torch dtype -> kge_dtype_t, filled on first use: importing this module does not import torch
+_torch = _raw_stream = None
 
 
-def _dtype(t, where, floating=True):
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.float8_e5m2: 4})
-    code = _DTYPES.get(t.dtype, -1)
-    if not (0 <= code <= 2 if floating else 3 <= code <= 4):
-        raise KgeError(KGE_ERR_BAD_ARG, where, f"tensor of type {t.dtype}")
+def _load_torch():
+    global _torch, _raw_stream
+    import torch
+    _FLOAT.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    _FP8.update({torch.float8_e4m3fn: 3, torch.float8_e5m2: 4})
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    _torch = torch
+
+
+def _bad(where, what):
+    return KgeError(KGE_ERR_BAD_ARG, where, what)
+
+
+def _type_of(t, where, name, table):
+    if _torch is None:
+        _load_torch()
+    code = table.get(t.dtype)
+    if code is None:
+        raise _bad(where, f"{name} has type {t.dtype}")
     return code
 
 
-def _need(ok, where, what):
-    if not ok:
-        raise KgeError(KGE_ERR_BAD_ARG, where, what)
-
-
 def _matrix(t, where, name):
-    """Rows of a 2-dimensional tensor may lie apart; elements of a row may not."""
-    _need(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1) and (t.stride(0) >= t.shape[1] or t.shape[0] <= 1), where,
-          f"{name} is not a matrix of contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    """(rows, columns, distance of rows) of a 2-dimensional tensor: its rows may lie apart, the elements of a row may not."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1) or (stride[0] < shape[1] and shape[0] > 1):
+        raise _bad(where, f"{name} is not a matrix of contiguous rows")
+    return shape[0], shape[1], stride[0] if stride[0] > shape[1] else shape[1]
 
 
-def _call(where, fn, device, *args):
-    """Calls the entry point on the current stream of the tensors' device and raises on an error code."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+def _ids_of(ids, where):
+    if _torch is None:
+        _load_torch()
+    if ids.dtype is not _torch.int32 or ids.dim() != 1 or not ids.is_contiguous():
+        raise _bad(where, "ids is not a contiguous int32 list")
+    return _int32(ids.numel(), where, "number of ids")
+
+
+def _int32(v, where, name):
+    if not -1 << 31 <= v < 1 << 31:
+        raise _bad(where, f"{name} {v} is not a 32-bit number")
+    return v
+
+
+def _status_word(status, where):
+    if status is None:
+        return None
+    if status.dtype is not _torch.int32 or status.numel() < 1:
+        raise _bad(where, "status is not an int32 tensor")
+    return status.data_ptr()
+
+
+def _device_of(where, *tensors):
+    """The ordinal of the GPU that all of the tensors (None: not given) are on."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != dev or dev < 0):
+            raise _bad(where, "tensors are not on one GPU")
+    return dev
+
+
+def _call(where, fn, dev, *args):
+    """Calls the entry point on the current stream of device `dev` and raises on an error code."""
+    if _torch.cuda.current_device() == dev:
+        rc = fn(*args, _raw_stream(dev))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        with _torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
     if rc != 0:
         raise KgeError(rc, where, lib().kge_error_string(rc).decode())
-
-
-def _same_device(where, first, *others):
-    _need(first.is_cuda, where, "tensors are not on a GPU")
-    for t in others:
-        if t is not None:
-            _need(t.device == first.device, where, "tensors are on different devices")
 
 
 def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _list_of_ids(ids, where):
-    _need(ids.dim() == 1 and ids.is_contiguous() and str(ids.dtype) == "torch.int32", where, "ids is not a contiguous int32 list")
-    return ids.numel()
-
-
-def _status_word(status, where):
-    _need(status is None or (str(status.dtype) == "torch.int32" and status.numel() >= 1), where, "status is not an int32 tensor")
-    return _addr(status)
-
-
-def _scratch(scratch, need, device, where):
-    """(address, bytes) of at least `need` bytes at a multiple of 256: the caller's tensor, or a new one of the stream's allocator."""
-    import torch
+def _scratch(scratch, need, dev, where):
+    """(address, bytes, tensor) of at least `need` bytes at a multiple of 256: the caller's tensor, or a new one of torch's allocator,
+    which hands it on only to what follows on the same stream (and keeps a captured graph's to that graph)."""
     if need == 0:
         return None, 0, None
     if scratch is None:
-        scratch = torch.empty(need + 256, dtype=torch.uint8, device=device)
-    _need(scratch.device == device and scratch.is_contiguous(), where, "scratch is not a contiguous tensor of the operands' device")
-    off = -scratch.data_ptr() % 256
-    return scratch.data_ptr() + off, max(0, scratch.numel() * scratch.element_size() - off), scratch
+        scratch = _torch.empty(need + 256, dtype=_torch.uint8, device=dev)
+    elif scratch.get_device() != dev or not scratch.is_contiguous():
+        raise _bad(where, "scratch is not a contiguous tensor of the operands' device")
+    at = scratch.data_ptr()
+    off = -at % 256
+    return at + off, max(0, scratch.numel() * scratch.element_size() - off), scratch
 
 
 def embedding_lookup(table, ids, out, scale=1.0, padding_id=-1, status=None):
     """kge_embedding_lookup: out[i] = scale * table[ids[i]]; table [E, d], ids int32 [n], out [n, d] (float32, bfloat16, float16)."""
     w = "kge_embedding_lookup"
-    n = _list_of_ids(ids, w)
-    tt, to, lt, lo = _dtype(table, w), _dtype(out, w), _matrix(table, w, "table"), _matrix(out, w, "out")
-    _need(out.shape[0] == n and out.shape[1] == table.shape[1], w, "out is not [number of ids, width of table]")
-    _same_device(w, table, ids, out, status)
-    _call(w, lib().kge_embedding_lookup, table.device, table.data_ptr(), tt, table.shape[0], table.shape[1], lt, ids.data_ptr(), n, scale,
-          padding_id, out.data_ptr(), to, lo, _status_word(status, w))
+    n = _ids_of(ids, w)
+    tt, to = _type_of(table, w, "table", _FLOAT), _type_of(out, w, "out", _FLOAT)
+    (rows, dim, lt), (out_rows, out_dim, lo) = _matrix(table, w, "table"), _matrix(out, w, "out")
+    if out_rows != n or out_dim != dim:
+        raise _bad(w, "out is not [number of ids, width of table]")
+    dev = _device_of(w, table, ids, out, status)
+    _call(w, lib().kge_embedding_lookup, dev, table.data_ptr(), tt, rows, _int32(dim, w, "width"), lt, ids.data_ptr(), n, scale,
+          _int32(padding_id, w, "padding_id"), out.data_ptr(), to, lo,
+          _status_word(status, w))
 
 
 def embedding_grad_scratch_bytes(rows, dim, n) -> int:
@@ -297,62 +325,63 @@ def embedding_grad_scratch_bytes(rows, dim, n) -> int:
 def embedding_grad(ids, grads, table_grad, scale=1.0, padding_id=-1, accumulate=False, scratch=None, status=None):
     """kge_embedding_grad: table_grad[e] (+)= scale * sum of grads[i] over ids[i] = e; grads [n, d], table_grad [E, d]."""
     w = "kge_embedding_grad"
-    n = _list_of_ids(ids, w)
-    tg, tt, lg, lt = _dtype(grads, w), _dtype(table_grad, w), _matrix(grads, w, "grads"), _matrix(table_grad, w, "table_grad")
-    rows, dim = table_grad.shape
-    _need(grads.shape[0] == n and grads.shape[1] == dim, w, "grads is not [number of ids, width of table_grad]")
-    _same_device(w, table_grad, ids, grads, status)
-    at, size, keep = _scratch(scratch, embedding_grad_scratch_bytes(rows, dim, n), table_grad.device, w)
-    _call(w, lib().kge_embedding_grad, table_grad.device, ids.data_ptr(), n, grads.data_ptr(), tg, lg, scale, padding_id, int(accumulate),
+    n = _ids_of(ids, w)
+    tg, tt = _type_of(grads, w, "grads", _FLOAT), _type_of(table_grad, w, "table_grad", _FLOAT)
+    (grad_rows, grad_dim, lg), (rows, dim, lt) = _matrix(grads, w, "grads"), _matrix(table_grad, w, "table_grad")
+    if grad_rows != n or grad_dim != dim:
+        raise _bad(w, "grads is not [number of ids, width of table_grad]")
+    dev = _device_of(w, table_grad, ids, grads, status)
+    at, size, keep = _scratch(scratch, lib().kge_embedding_grad_scratch_bytes(rows, _int32(dim, w, "width"), n), dev, w)
+    _call(w, lib().kge_embedding_grad, dev, ids.data_ptr(), n, grads.data_ptr(), tg, lg, scale, _int32(padding_id, w, "padding_id"), 1 if accumulate else 0,
           table_grad.data_ptr(), tt, rows, dim, lt, at, size, _status_word(status, w))
 
 
 def dropout(x, out, p, seed, step=0, site=0, residual=None, step_dev=None):
     """kge_dropout of a contiguous tensor of any shape; the backward pass is the same call on the gradient (without residual)."""
     w = "kge_dropout"
-    tx, to = _dtype(x, w), _dtype(out, w)
-    _need(x.is_contiguous() and out.is_contiguous() and x.numel() == out.numel(), w, "x and out are not contiguous tensors of one size")
-    _need(residual is None or (residual.is_contiguous() and residual.dtype == out.dtype and residual.numel() == out.numel()), w,
-          "residual is not a contiguous tensor of out's size and type")
-    _need(step_dev is None or str(step_dev.dtype) == "torch.int64", w, "step_dev is not an int64 tensor")
-    _need(0 <= seed < 1 << 64 and 0 <= step < 1 << 64, w, "seed and step are 64-bit numbers")
-    _need(0 <= site < 1 << 31, w, "site is not in [0, 2^31)")
-    _same_device(w, x, out, residual, step_dev)
-    _call(w, lib().kge_dropout, x.device, x.data_ptr(), tx, _addr(residual), out.data_ptr(), to, x.numel(), p, seed, step, _addr(step_dev), site)
+    tx, to, n = _type_of(x, w, "x", _FLOAT), _type_of(out, w, "out", _FLOAT), x.numel()
+    if not (x.is_contiguous() and out.is_contiguous() and out.numel() == n):
+        raise _bad(w, "x and out are not contiguous tensors of one size")
+    if residual is not None and not (residual.is_contiguous() and residual.dtype is out.dtype and residual.numel() == n):
+        raise _bad(w, "residual is not a contiguous tensor of out's size and type")
+    if step_dev is not None and step_dev.dtype is not _torch.int64:
+        raise _bad(w, "step_dev is not an int64 tensor")
+    if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64 and 0 <= site < 1 << 31):
+        raise _bad(w, "seed and step are 64-bit numbers, site a 31-bit one")
+    dev = _device_of(w, x, out, residual, step_dev)
+    _call(w, lib().kge_dropout, dev, x.data_ptr(), tx, _addr(residual), out.data_ptr(), to, n, p, seed, step, _addr(step_dev), site)
 
 
 def _operand(q, scales, where, name):
-    """(type, distance of rows, rows to a scale) of an 8-bit operand [R, K] and its scales [ceil(K / 128), R or ceil(R / 128)]."""
-    code, ld = _dtype(q, where, floating=False), _matrix(q, where, name)
-    rows, k = q.shape
+    """(type, rows, columns, distance of rows, rows to a scale) of an 8-bit operand [R, K] and its scales [ceil(K / 128), R or ceil(R / 128)]."""
+    code, (rows, k, ld) = _type_of(q, where, name, _FP8), _matrix(q, where, name)
     if rows <= 1:
-        ld = (max(ld, k) + 15) // 16 * 16
-    _need(scales is not None and scales.dim() == 2 and scales.is_contiguous() and str(scales.dtype) == "torch.float32", where,
-          f"the scales of {name} are not a contiguous float32 matrix")
-    _need(scales.shape[0] == (k + 127) // 128 and scales.shape[1] in (rows, (rows + 127) // 128), where, f"the scales of {name} do not fit it")
-    return code, ld, 1 if scales.shape[1] == rows else 128
+        ld = (ld + 15) // 16 * 16
+    if scales is None or scales.dtype is not _torch.float32 or not scales.is_contiguous() or scales.dim() != 2:
+        raise _bad(where, f"the scales of {name} are not a contiguous float32 matrix")
+    kb, per = scales.shape
+    if kb != (k + 127) // 128 or per not in (rows, (rows + 127) // 128):
+        raise _bad(where, f"the scales of {name} do not fit it")
+    return code, rows, k, ld, 1 if per == rows else 128
 
 
 def fp8_quantize(x, q=None, scales=None, qt=None, scales_t=None, block_rows=1, pow2=False):
     """kge_fp8_quantize: x [R, K] -> q [R, K] (float8_e4m3fn or float8_e5m2, rows a multiple of 16 bytes apart) with scales
     [ceil(K / 128), R] (block_rows = 1) or [ceil(K / 128), ceil(R / 128)] (128), and / or the same of x^T in qt [K, R], scales_t."""
     w = "kge_fp8_quantize"
-    tx, lx = _dtype(x, w), _matrix(x, w, "x")
-    rows, cols = x.shape
-    code, lq, lt = None, 0, 0
-    for name, t, s, shape in (("q", q, scales, (rows, cols)), ("qt", qt, scales_t, (cols, rows))):
+    tx, (rows, cols, lx) = _type_of(x, w, "x", _FLOAT), _matrix(x, w, "x")
+    code, at, ld = None, [None, None, None, None], [0, 0]
+    for i, (name, t, s, r, k) in enumerate((("q", q, scales, rows, cols), ("qt", qt, scales_t, cols, rows))):
         if t is None:
             continue
-        _need(tuple(t.shape) == shape, w, f"{name} has another shape than x")
-        c, ld, block = _operand(t, s, w, name)
-        _need(code in (None, c), w, "q and qt have different types")
-        _need(block == block_rows or (shape[0] + block_rows - 1) // block_rows == s.shape[1], w, f"the scales of {name} are for another block")
-        code = c
-        lq, lt = (ld, lt) if name == "q" else (lq, ld)
-    _need(code is not None, w, "neither q nor qt is given")
-    _same_device(w, x, q, scales, qt, scales_t)
-    _call(w, lib().kge_fp8_quantize, x.device, x.data_ptr(), tx, rows, cols, lx, code, block_rows, int(pow2), _addr(q), lq, _addr(scales if q is not None else None),
-          _addr(qt), lt, _addr(scales_t if qt is not None else None))
+        c, tr, tk, ld[i], block = _operand(t, s, w, name)
+        if tr != r or tk != k or (block != block_rows and (r + block_rows - 1) // block_rows != s.shape[1]) or code not in (None, c):
+            raise _bad(w, f"{name} has another shape than x, scales for another block or another type than q")
+        code, at[2 * i], at[2 * i + 1] = c, t.data_ptr(), s.data_ptr()
+    if code is None:
+        raise _bad(w, "neither q nor qt is given")
+    dev = _device_of(w, x, q, scales, qt, scales_t)
+    _call(w, lib().kge_fp8_quantize, dev, x.data_ptr(), tx, rows, cols, lx, code, block_rows, 1 if pow2 else 0, at[0], ld[0], at[1], at[2], ld[1], at[3])
 
 
 def fp8_matmul_scratch_bytes(m, n, k) -> int:
@@ -363,19 +392,19 @@ def fp8_matmul_scratch_bytes(m, n, k) -> int:
 def fp8_matmul(a, a_scales, b, b_scales, out, addend=None, scratch=None, status=None):
     """kge_fp8_matmul: out [M, N] = a [M, K] . b [N, K]^T (+ addend) of operands as fp8_quantize makes them."""
     w = "kge_fp8_matmul"
-    ta, la, ba = _operand(a, a_scales, w, "a")
-    tb, lb, bb = _operand(b, b_scales, w, "b")
-    (m, k), n = a.shape, b.shape[0]
-    to, lo = _dtype(out, w), _matrix(out, w, "out")
-    _need(b.shape[1] == k and tuple(out.shape) == (m, n), w, "shapes of a [M, K], b [N, K] and out [M, N] do not fit")
-    ladd = 0
+    ta, m, k, la, ba = _operand(a, a_scales, w, "a")
+    tb, n, kb, lb, bb = _operand(b, b_scales, w, "b")
+    to, (om, on, lo), ladd = _type_of(out, w, "out", _FLOAT), _matrix(out, w, "out"), 0
+    if kb != k or om != m or on != n:
+        raise _bad(w, "shapes of a [M, K], b [N, K] and out [M, N] do not fit")
     if addend is not None:
-        ladd = _matrix(addend, w, "addend")
-        _need(addend.dtype == out.dtype and addend.shape == out.shape, w, "addend is not of out's shape and type")
-    _same_device(w, a, a_scales, b, b_scales, out, addend, status)
-    at, size, keep = _scratch(scratch, fp8_matmul_scratch_bytes(m, n, k), out.device, w)
-    _call(w, lib().kge_fp8_matmul, out.device, a.data_ptr(), ta, la, a_scales.data_ptr(), ba, b.data_ptr(), tb, lb, b_scales.data_ptr(), bb,
-          _addr(addend), ladd, out.data_ptr(), to, lo, m, n, k, at, size, _status_word(status, w))
+        am, an, ladd = _matrix(addend, w, "addend")
+        if am != m or an != n or addend.dtype is not out.dtype:
+            raise _bad(w, "addend is not of out's shape and type")
+    dev = _device_of(w, a, a_scales, b, b_scales, out, addend, status)
+    at, size, keep = _scratch(scratch, lib().kge_fp8_matmul_scratch_bytes(m, n, k), dev, w)
+    _call(w, lib().kge_fp8_matmul, dev, a.data_ptr(), ta, la, a_scales.data_ptr(), ba, b.data_ptr(), tb, lb, b_scales.data_ptr(), bb, _addr(addend), ladd,
+          out.data_ptr(), to, lo, m, n, k, at, size, _status_word(status, w))
 
 
 class Kge:

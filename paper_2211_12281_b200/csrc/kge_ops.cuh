@@ -17,10 +17,15 @@ inline bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<u
 // An error that an earlier, unrelated call left behind is not this launch's: the launch's own code is what is looked at.
 inline int launch_status(cudaError_t e) { return e == cudaSuccess ? KGE_OK : KGE_ERR_CUDA; }
 
-// Largest of `most`, most / 2, ..., 1 elements that divides a row of `dim` and its stride and keeps base addresses aligned.
+// Largest of `most`, most / 2, ..., 1 elements that divides a row of `dim` and starts at multiples of its bytes (of 16, if it has more)
+// in every row of both matrices.
 inline int vector_length(int most, int64_t dim, int64_t ld0, int bytes0, const void* p0, int64_t ld1, int bytes1, const void* p1) {
+    auto fits = [](int v, int64_t ld, int bytes, const void* p) {
+        const int64_t step = v * bytes < 16 ? v * bytes : 16;
+        return ld * bytes % step == 0 && aligned_to(p, (size_t)step);
+    };
     for (int v = most; v > 1; v >>= 1)
-        if (dim % v == 0 && ld0 % v == 0 && ld1 % v == 0 && aligned_to(p0, (size_t)v * bytes0) && aligned_to(p1, (size_t)v * bytes1)) return v;
+        if (dim % v == 0 && fits(v, ld0, bytes0, p0) && fits(v, ld1, bytes1, p1)) return v;
     return 1;
 }
 

@@ -3,12 +3,16 @@
 //   gradient  dT[e] = scale sum_{i : ids[i] = e} g[i]      (+ the old dT[e])
 // The gradient sorts the ids (stable radix sort of (id, position) pairs), walks the sorted list in chunks of rows, adds a chunk's
 // rows of one id in fp32 in ascending position, and joins the ids that span chunks in a second, fixed order: the result is a
-// function of the inputs alone.
-//   hist      digit counts of every tile; clears the later passes' counts and, side by side with that, the dense gradient
-//   scatter   one stable split by a digit of up to eleven bits; counts the next digit on the way
-//   sum       chunks of sorted rows; what ends inside its chunk or the next one is final, the rest leaves partial sums
-//   join      one CTA per (id that spans more, 32 columns): partial sums in a fixed order
+// function of the inputs alone.  Rows of the dense gradient that no id names are set to zero by CTAs beside the sort's.
+//   up to 1,024 ids     one launch: every CTA owns a range of table rows, picks the ids that fall into it and sorts those
+//   up to 65,536        one cluster of eight CTAs sorts in shared memory, exchanging counts and pairs between its CTAs
+//   more                hist     digit counts of every tile; clears the later passes' counts
+//                       scan     the counts become sums over the tiles before
+//                       scatter  one stable split by a digit; counts the next digit on the way
+//   then                sum      chunks of sorted rows; what ends inside its chunk or the next one is final, the rest leaves partial sums
+//                       join     one CTA per (id that spans more, 32 columns): partial sums in a fixed order
 #include <algorithm>
+#include <type_traits>
 
 #include "kge_ops.cuh"
 
@@ -76,9 +80,11 @@ __global__ void __launch_bounds__(LOOKUP_THREADS) lookup_kernel(LookupParams p) 
 // ---- gradient --------------------------------------------------------------------------------------------------------
 
 constexpr int GS_THREADS = 256, GS_WARPS = GS_THREADS / 32, GS_ITEMS = 8;
-constexpr int GS_TILE = GS_THREADS * GS_ITEMS;     // ids per CTA of the sort
-constexpr int GS_MAX_BITS = 11, GS_MAX_PASSES = 4;
-constexpr int GS_DIRECT_TILES = 256;               // up to here every scatter CTA adds up the tiles' counts itself
+constexpr int GS_TILE = GS_THREADS * GS_ITEMS;     // ids per CTA of the sort in global memory
+constexpr int GS_MAX_BITS = 9, GS_MAX_PASSES = 4;
+constexpr int CS_CTAS = 8, CS_THREADS = 512, CS_WARPS = CS_THREADS / 32, CS_ITEMS = 16;      // the cluster's sort
+constexpr int CS_SHARE = CS_THREADS * CS_ITEMS, CS_MAX = CS_CTAS * CS_SHARE, CS_MAX_BITS = 11;
+constexpr int SMALL_MAX = 1024, SMALL_THREADS = 256;
 constexpr int SUM_THREADS = 256;
 constexpr int JOIN_THREADS = 256;
 
@@ -89,8 +95,7 @@ SortPlan sort_plan(int64_t rows, int n) {
     s.tiles = (int)ceil_div(n, GS_TILE);
     s.key_bits = 1;
     while (s.key_bits < 31 && (1ll << s.key_bits) <= rows) ++s.key_bits;      // keys 0 .. rows (rows: no row of the table)
-    // few tiles: wide digits, two passes up to four million rows; many: the counts of 2,048 digits a tile cost more than a pass
-    const int most = s.tiles <= 64 ? GS_MAX_BITS : 9;
+    const int most = n <= CS_MAX ? CS_MAX_BITS : GS_MAX_BITS;
     s.passes = (s.key_bits + most - 1) / most;
     s.bits = (s.key_bits + s.passes - 1) / s.passes;
     return s;
@@ -100,7 +105,7 @@ int chunk_rows(int n) { return n < (1 << 17) ? 8 : 32; }
 struct GradScratch {
     uint32_t *keys[2], *pos[2];      // [n] sorted ids and positions, in turn
     uint32_t* hist;                  // [passes][tiles][1 << bits]
-    uint32_t* total;                 // [1 << bits] (many tiles only)
+    uint32_t* total;                 // [1 << bits]
     float* part;                     // [chunks][2][dim rounded up to 4]
     int32_t *list, *list_count;      // chunks in which an id begins that spans more
     size_t bytes;
@@ -112,9 +117,12 @@ GradScratch carve_grad(char* base, int64_t rows, int dim, int n) {
     const SortPlan s = sort_plan(rows, n);
     const int64_t chunks = ceil_div(n, chunk_rows(n));
     GradScratch g{};
-    for (int i = 0; i < 2; ++i) { g.keys[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4 + 128)); g.pos[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4 + 128)); }
-    g.hist = reinterpret_cast<uint32_t*>(take((size_t)s.passes * s.tiles * (4u << s.bits)));
-    g.total = reinterpret_cast<uint32_t*>(take((size_t)4 << s.bits));
+    if (n <= SMALL_MAX) return g;       // (one launch: nothing is kept)
+    for (int i = 0; i < (n > CS_MAX ? 2 : 1); ++i) { g.keys[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4)); g.pos[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4)); }
+    if (n > CS_MAX) {
+        g.hist = reinterpret_cast<uint32_t*>(take((size_t)s.passes * s.tiles * (4u << s.bits)));
+        g.total = reinterpret_cast<uint32_t*>(take((size_t)4 << s.bits));
+    }
     g.part = reinterpret_cast<float*>(take((size_t)chunks * 2 * ((dim + 3) / 4 * 4) * 4));
     g.list = reinterpret_cast<int32_t*>(take((size_t)chunks * 4));
     g.list_count = reinterpret_cast<int32_t*>(take(256));
@@ -130,10 +138,9 @@ struct SortParams {
     const uint32_t *keys_in, *pos_in;
     uint32_t *keys_out, *pos_out;
     uint32_t *hist, *hist_next, *total;   // this pass's and the next one's [tiles][1 << bits]
-    int scanned;                          // hist holds sums over the tiles before, total the digits' counts
     int32_t *list_count, *status;
-    // dense gradient rows set to zero side by side with the first counts
-    void* zero; int64_t zero_rows, zero_row_bytes, zero_ld_bytes;
+    // dense gradient rows set to zero by CTAs beside the sort's
+    char* zero; int64_t zero_row_bytes, zero_ld_bytes, zero_first, zero_last;     // the rows, and which of them in this launch
     int zero_vec;                         // rows are whole 16-byte words and lie back to back
 };
 
@@ -144,24 +151,29 @@ __device__ __forceinline__ uint32_t grad_key(const SortParams& p, int i) {
     return (uint32_t)id;
 }
 
+// Rows [zero_first, zero_last) by CTA `cta` of `ctas`.
+__device__ __forceinline__ void zero_rows(const SortParams& p, int64_t cta, int64_t ctas) {
+    const int64_t first = cta * blockDim.x + threadIdx.x, step = ctas * blockDim.x;
+    char* const base = p.zero + p.zero_first * p.zero_ld_bytes;
+    const int64_t rows = p.zero_last - p.zero_first;
+    if (p.zero_vec) {
+        uint4* z = reinterpret_cast<uint4*>(base);
+        const int64_t words = rows * (p.zero_row_bytes / 16);
+#pragma unroll 4
+        for (int64_t i = first; i < words; i += step) z[i] = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+        const int64_t halves = p.zero_row_bytes / 2, all = rows * halves;
+        for (int64_t i = first; i < all; i += step) {
+            const int64_t r = i / halves;
+            *reinterpret_cast<uint16_t*>(base + r * p.zero_ld_bytes + (i - r * halves) * 2) = 0;
+        }
+    }
+}
+
 __global__ void __launch_bounds__(GS_THREADS) grad_hist_kernel(SortParams p) {
     __shared__ uint32_t count[1 << GS_MAX_BITS];
     const int digits = 1 << p.bits, tid = threadIdx.x;
-    if ((int)blockIdx.x >= p.tiles) {
-        const int64_t first = (int64_t)(blockIdx.x - p.tiles) * GS_THREADS + tid, step = (int64_t)(gridDim.x - p.tiles) * GS_THREADS;
-        if (p.zero_vec) {
-            uint4* z = static_cast<uint4*>(p.zero);
-            const int64_t words = p.zero_rows * (p.zero_row_bytes / 16);
-            for (int64_t i = first; i < words; i += step) z[i] = make_uint4(0u, 0u, 0u, 0u);
-        } else {
-            const int64_t halves = p.zero_row_bytes / 2, all = p.zero_rows * halves;
-            for (int64_t i = first; i < all; i += step) {
-                const int64_t r = i / halves;
-                *reinterpret_cast<uint16_t*>(static_cast<char*>(p.zero) + r * p.zero_ld_bytes + (i - r * halves) * 2) = 0;
-            }
-        }
-        return;
-    }
+    if ((int)blockIdx.x >= p.tiles) { zero_rows(p, blockIdx.x - p.tiles, gridDim.x - p.tiles); return; }
     for (int d = tid; d < digits; d += GS_THREADS) {
         count[d] = 0;
         for (int q = 1; q < p.passes; ++q) p.hist[((int64_t)q * p.tiles + blockIdx.x) * digits + d] = 0;
@@ -170,26 +182,33 @@ __global__ void __launch_bounds__(GS_THREADS) grad_hist_kernel(SortParams p) {
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < GS_ITEMS; ++k) {
-        const int i = blockIdx.x * GS_TILE + k * GS_THREADS + tid;
-        if (i < p.n) atomicAdd(&count[grad_key(p, i) & (digits - 1)], 1u);
+        const int64_t i = (int64_t)blockIdx.x * GS_TILE + k * GS_THREADS + tid;
+        if (i < p.n) atomicAdd(&count[grad_key(p, (int)i) & (digits - 1)], 1u);
     }
     __syncthreads();
     for (int d = tid; d < digits; d += GS_THREADS) p.hist[(int64_t)blockIdx.x * digits + d] = count[d];
 }
 
-// Many tiles: one thread per digit turns the tiles' counts into sums over the tiles before.
-__global__ void __launch_bounds__(32) grad_scan_kernel(SortParams p) {
-    const int digits = 1 << p.bits, d = blockIdx.x * 32 + threadIdx.x;
+// A warp per digit turns the tiles' counts into sums over the tiles before.
+__global__ void __launch_bounds__(256) grad_scan_kernel(SortParams p) {
+    const int digits = 1 << p.bits, d = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
     if (d >= digits) return;
     uint32_t run = 0;
-    for (int t0 = 0; t0 < p.tiles; t0 += 16) {
-        uint32_t c[16];
+    for (int t0 = 0; t0 < p.tiles; t0 += 256) {
+        uint32_t c[8], sum = 0;                     // lane l: tiles t0 + 8 l ... + 8
 #pragma unroll
-        for (int u = 0; u < 16; ++u) c[u] = t0 + u < p.tiles ? p.hist[(int64_t)(t0 + u) * digits + d] : 0u;
+        for (int u = 0; u < 8; ++u) { const int t = t0 + 8 * lane + u; c[u] = t < p.tiles ? p.hist[(int64_t)t * digits + d] : 0u; }
 #pragma unroll
-        for (int u = 0; u < 16; ++u) if (t0 + u < p.tiles) { p.hist[(int64_t)(t0 + u) * digits + d] = run; run += c[u]; }
+        for (int u = 0; u < 8; ++u) sum += c[u];
+        uint32_t incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+        uint32_t at = run + incl - sum;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { const int t = t0 + 8 * lane + u; if (t < p.tiles) p.hist[(int64_t)t * digits + d] = at; at += c[u]; }
+        run += __shfl_sync(0xffffffffu, incl, 31);
     }
-    p.total[d] = run;
+    if (lane == 0) p.total[d] = run;
 }
 
 // Stable split of one tile by a digit: a warp takes its 256 elements 32 at a time in order, lanes of one digit find each other
@@ -199,15 +218,16 @@ __global__ void __launch_bounds__(GS_THREADS) grad_scatter_kernel(SortParams p) 
     __shared__ uint32_t base[1 << GS_MAX_BITS];
     __shared__ uint32_t warp_tot[GS_WARPS];
     const int digits = 1 << p.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, tile = blockIdx.x;
+    if (tile >= p.tiles) { zero_rows(p, tile - p.tiles, gridDim.x - p.tiles); return; }
     for (int d = lane; d < digits; d += 32) cnt[warp][d] = 0;
     __syncwarp();
     uint32_t key[GS_ITEMS], pos[GS_ITEMS], at[GS_ITEMS];
-    const int i0 = tile * GS_TILE + warp * 32 * GS_ITEMS;
+    const int64_t i0 = (int64_t)tile * GS_TILE + warp * 32 * GS_ITEMS;
 #pragma unroll
     for (int k = 0; k < GS_ITEMS; ++k) {
-        const int i = i0 + k * 32 + lane;
+        const int64_t i = i0 + k * 32 + lane;
         if (i < p.n) {
-            key[k] = p.pass == 0 ? grad_key(p, i) : p.keys_in[i];
+            key[k] = p.pass == 0 ? grad_key(p, (int)i) : p.keys_in[i];
             pos[k] = p.pass == 0 ? (uint32_t)i : p.pos_in[i];
         }
     }
@@ -226,23 +246,13 @@ __global__ void __launch_bounds__(GS_THREADS) grad_scatter_kernel(SortParams p) 
     __syncthreads();
     // where this tile's share of a digit begins: the smaller digits of all tiles, and this one's in the tiles before
     const int per = max(1, digits / GS_THREADS), d0 = tid * per;
-    uint32_t sum = 0, tot[8], mine[8];
+    constexpr int PER = (1 << GS_MAX_BITS) / GS_THREADS;
+    uint32_t sum = 0, tot[PER], mine[PER];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { tot[j] = 0; mine[j] = 0; }
-    if (d0 < digits) {
-        if (p.scanned) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) if (j < per) { tot[j] = p.total[d0 + j]; mine[j] = p.hist[(int64_t)tile * digits + d0 + j]; }
-        } else {
-#pragma unroll 4
-            for (int t = 0; t < p.tiles; ++t) {
-                const uint32_t* h = p.hist + (int64_t)t * digits + d0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) if (j < per) { const uint32_t c = h[j]; tot[j] += c; if (t < tile) mine[j] += c; }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += tot[j];
+    for (int j = 0; j < PER; ++j) {
+        tot[j] = mine[j] = 0;
+        if (d0 < digits && j < per) { tot[j] = p.total[d0 + j]; mine[j] = p.hist[(int64_t)tile * digits + d0 + j]; }
+        sum += tot[j];
     }
     uint32_t incl = sum;
 #pragma unroll
@@ -253,7 +263,7 @@ __global__ void __launch_bounds__(GS_THREADS) grad_scatter_kernel(SortParams p) 
     for (int w = 0; w < warp; ++w) run += warp_tot[w];
     if (d0 < digits) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) if (j < per) {
+        for (int j = 0; j < PER; ++j) if (j < per) {
             base[d0 + j] = run + mine[j];
             run += tot[j];
             uint32_t w_run = 0;
@@ -272,6 +282,111 @@ __global__ void __launch_bounds__(GS_THREADS) grad_scatter_kernel(SortParams p) 
     }
 }
 
+// ---- up to 65,536 ids: one cluster sorts them in shared memory ----
+
+__device__ __forceinline__ void cs_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cs_map(uint32_t addr, uint32_t rank) { uint32_t r; asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank)); return r; }
+__device__ __forceinline__ uint32_t cs_load(uint32_t addr) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory"); return v; }
+__device__ __forceinline__ void cs_store2(uint32_t addr, uint32_t a, uint32_t b) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory"); }
+
+size_t cluster_sort_smem(int n, int bits) {       // pairs twice, warps' counts, digits' counts and bases
+    return (size_t)ceil_div(n, CS_CTAS) * 16 + ((size_t)CS_WARPS * 2 + 8) * ((size_t)1 << bits) + 128;
+}
+
+// Cluster 0 sorts: each of its CTAs holds a share of the list, a warp a contiguous piece of that.  Per pass a warp ranks its elements
+// among its own (as in grad_scatter_kernel), the CTAs read each other's digit counts, and every pair is stored into the CTA that
+// holds its new place; the last pass stores to global memory.  The other clusters set rows to zero.
+__global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortParams p) {
+    extern __shared__ __align__(16) unsigned char cs_smem[];
+    if (blockIdx.x >= CS_CTAS) { zero_rows(p, blockIdx.x - CS_CTAS, gridDim.x - CS_CTAS); return; }
+    __shared__ uint32_t warp_tot[CS_WARPS];
+    const int digits = 1 << p.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int share = (p.n + CS_CTAS - 1) / CS_CTAS, rank = blockIdx.x;
+    const int have = max(0, min(share, p.n - rank * share));                        // of this CTA
+    const int per_warp = ((share + CS_WARPS - 1) / CS_WARPS + 31) / 32 * 32;        // at most 32 CS_ITEMS
+    uint2* const pairs[2] = {reinterpret_cast<uint2*>(cs_smem), reinterpret_cast<uint2*>(cs_smem) + share};
+    uint32_t* const count = reinterpret_cast<uint32_t*>(pairs[1] + share);          // [digits] of this CTA
+    uint32_t* const base = count + digits;                                          // [digits]
+    uint16_t* const cnt = reinterpret_cast<uint16_t*>(base + digits);               // [CS_WARPS][digits]
+    if (rank == 0 && tid == 0) *p.list_count = 0;
+    const int rounds = per_warp / 32, first = warp * per_warp;
+    uint32_t key[CS_ITEMS], pos[CS_ITEMS], at[CS_ITEMS];
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = pass * p.bits;
+        for (int d = lane; d < digits; d += 32) cnt[warp * digits + d] = 0;
+#pragma unroll
+        for (int k = 0; k < CS_ITEMS; ++k) {
+            const int i = first + k * 32 + lane;
+            if (k < rounds && i < have) {
+                if (pass == 0) { pos[k] = (uint32_t)(rank * share + i); key[k] = grad_key(p, (int)pos[k]); }
+                else { const uint2 v = pairs[pass & 1][i]; key[k] = v.x; pos[k] = v.y; }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < CS_ITEMS; ++k) {
+            if (k >= rounds) break;
+            const bool in = first + k * 32 + lane < have;
+            const uint32_t digit = in ? (key[k] >> shift) & (digits - 1) : 1u << CS_MAX_BITS;
+            const unsigned same = __match_any_sync(0xffffffffu, digit), before = same & ((1u << lane) - 1u);
+            uint32_t seen = 0;
+            if (in) seen = cnt[warp * digits + digit];
+            __syncwarp();
+            if (in && before == 0) cnt[warp * digits + digit] = (uint16_t)(seen + __popc(same));
+            __syncwarp();
+            at[k] = seen + __popc(before);
+        }
+        __syncthreads();
+        for (int d = tid; d < digits; d += CS_THREADS) {       // the warps' counts become sums over the warps before
+            uint32_t run = 0;
+#pragma unroll
+            for (int w = 0; w < CS_WARPS; ++w) { const uint32_t c = cnt[w * digits + d]; cnt[w * digits + d] = (uint16_t)run; run += c; }
+            count[d] = run;
+        }
+        cs_sync();
+        // first place of every digit's elements of this CTA: smaller digits of all CTAs, this digit in the CTAs before
+        const int per = max(1, digits / CS_THREADS), d0 = tid * per;
+        constexpr int PER = (1 << CS_MAX_BITS) / CS_THREADS;
+        uint32_t sum = 0, tot[PER], mine[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) { tot[j] = 0; mine[j] = 0; }
+        if (d0 < digits) {
+            const uint32_t from = smem_u32(count + d0);
+#pragma unroll
+            for (int r = 0; r < CS_CTAS; ++r) {
+                const uint32_t there = cs_map(from, r);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) if (j < per) { const uint32_t c = cs_load(there + 4 * j); tot[j] += c; if (r < rank) mine[j] += c; }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) sum += tot[j];
+        uint32_t incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+        if (lane == 31) warp_tot[warp] = incl;
+        __syncthreads();
+        uint32_t run = incl - sum;
+        for (int w = 0; w < warp; ++w) run += warp_tot[w];
+        if (d0 < digits) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) if (j < per) { base[d0 + j] = run + mine[j]; run += tot[j]; }
+        }
+        __syncthreads();
+        const bool last = pass + 1 == p.passes;
+        const uint32_t out = smem_u32(pairs[(pass + 1) & 1]);
+#pragma unroll
+        for (int k = 0; k < CS_ITEMS; ++k) {
+            if (k >= rounds || first + k * 32 + lane >= have) continue;
+            const uint32_t digit = (key[k] >> shift) & (digits - 1);
+            const uint32_t dst = base[digit] + cnt[warp * digits + digit] + at[k];
+            if (last) { p.keys_out[dst] = key[k]; p.pos_out[dst] = pos[k]; }
+            else { const uint32_t r = dst / share; cs_store2(cs_map(out + (dst - r * share) * 8, r), key[k], pos[k]); }
+        }
+        cs_sync();         // the pairs are in place; nobody reads this pass's counts any more
+    }
+}
+
 struct SumParams {
     const uint32_t *keys, *pos;
     int n, chunks, dim, part_ld;
@@ -283,6 +398,7 @@ struct SumParams {
     float* part;
     int32_t *list, *list_count;
     FastDiv vecs;
+    const int32_t* ids; int32_t padding_id; int rows_per_cta; int32_t* status;     // grad_small_kernel
 };
 
 template <typename TO, int V>
@@ -293,6 +409,143 @@ __device__ __forceinline__ void finish_pack(const SumParams& p, uint32_t row, in
 #pragma unroll
     for (int e = 0; e < V; ++e) o.v[e] = from_float<TO>(p.accumulate ? fmaf(a[e], p.scale, to_float(o.v[e])) : a[e] * p.scale);
     *reinterpret_cast<Pack<TO, V>*>(dst) = o;
+}
+
+// ---- up to 1,024 ids: one launch ----
+
+// CTA c owns the table rows [c rows_per_cta, + rows_per_cta): it picks the ids that name them, sorts those as (row, position) words
+// in shared memory, and adds up each row's gradients: runs of up to SHORT by one group of threads (a pack of columns each),
+// longer ones by all groups in turn, whose sums are then added in order.
+template <typename TG, typename TO, int V>
+__global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) {
+    constexpr int SHORT = 32, U = 8;
+    __shared__ uint32_t list[SMALL_MAX];       // local row << 10 | position
+    __shared__ uint16_t start[SMALL_MAX + 1];
+    __shared__ uint32_t warp_cnt[SMALL_THREADS / 32];
+    __shared__ float red[SMALL_THREADS * V];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_cta;
+    const int nr = (int)min((int64_t)p.rows_per_cta, (int64_t)p.rows - r0);
+    // the ids of this CTA's rows, four to a thread in the list's order
+    int32_t id[SMALL_MAX / SMALL_THREADS];
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < SMALL_MAX / SMALL_THREADS; ++k) {
+        const int i = tid * (SMALL_MAX / SMALL_THREADS) + k;
+        id[k] = -1;
+        if (i < p.n) {
+            const int32_t v = p.ids[i];
+            if (v != p.padding_id) {
+                if (v < 0 || (uint32_t)v >= p.rows) { if (blockIdx.x == 0) note_status(p.status, KGE_ERR_ID_RANGE); }
+                else if (v >= r0 && v < r0 + nr) { id[k] = (int32_t)(v - r0); ++mine; }
+            }
+        }
+    }
+    if (!p.accumulate) {
+        const uint32_t items = (uint32_t)nr * p.vecs.d;       // (rows_per_cta keeps this below 2^31)
+        Pack<TO, V> z;
+#pragma unroll
+        for (int e = 0; e < V; ++e) z.v[e] = from_float<TO>(0.f);
+        for (uint32_t i = tid; i < items; i += SMALL_THREADS) {
+            const uint32_t r = p.vecs.div(i);
+            *reinterpret_cast<Pack<TO, V>*>(static_cast<TO*>(p.out) + (r0 + r) * p.ld_out + (int64_t)(i - r * p.vecs.d) * V) = z;
+        }
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+    if (lane == 31) warp_cnt[warp] = incl;
+    __syncthreads();
+    int at = incl - mine, m = 0;
+#pragma unroll
+    for (int w = 0; w < SMALL_THREADS / 32; ++w) { if (w < warp) at += warp_cnt[w]; m += warp_cnt[w]; }
+    if (m == 0) return;
+#pragma unroll
+    for (int k = 0; k < SMALL_MAX / SMALL_THREADS; ++k)
+        if (id[k] >= 0) list[at++] = (uint32_t)id[k] << 10 | (uint32_t)(tid * (SMALL_MAX / SMALL_THREADS) + k);
+    int m2 = 1;
+    while (m2 < m) m2 <<= 1;
+    for (int i = m + tid; i < m2; i += SMALL_THREADS) list[i] = ~0u;
+    __syncthreads();
+    for (int size = 2; size <= m2; size <<= 1)
+        for (int stride = size >> 1; stride > 0; stride >>= 1) {
+            for (int t = tid; t < m2 / 2; t += SMALL_THREADS) {
+                const int lo = 2 * t - (t & (stride - 1)), hi = lo + stride;
+                const uint32_t x = list[lo], y = list[hi];
+                if ((x > y) == ((lo & size) == 0)) { list[lo] = y; list[hi] = x; }
+            }
+            __syncthreads();
+        }
+    // where each row's run begins
+    int heads = 0;
+#pragma unroll
+    for (int k = 0; k < SMALL_MAX / SMALL_THREADS; ++k) {
+        const int i = tid * (SMALL_MAX / SMALL_THREADS) + k;
+        if (i < m && (i == 0 || list[i] >> 10 != list[i - 1] >> 10)) heads |= 1 << k;
+    }
+    incl = __popc(heads);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+    if (lane == 31) warp_cnt[warp] = incl;
+    __syncthreads();
+    int u = incl - __popc(heads), runs = 0;
+#pragma unroll
+    for (int w = 0; w < SMALL_THREADS / 32; ++w) { if (w < warp) u += warp_cnt[w]; runs += warp_cnt[w]; }
+#pragma unroll
+    for (int k = 0; k < SMALL_MAX / SMALL_THREADS; ++k) if (heads >> k & 1) start[u++] = (uint16_t)(tid * (SMALL_MAX / SMALL_THREADS) + k);
+    if (tid == 0) start[runs] = (uint16_t)m;
+    __syncthreads();
+
+    const int vecs = (int)p.vecs.d, wide = min(vecs, SMALL_THREADS), groups = SMALL_THREADS / wide;
+    const int group = tid / wide, v0 = tid - group * wide;
+    const TG* grads = static_cast<const TG*>(p.grads);
+    auto add_rows = [&](int i, int end, int step, int64_t col, float (&a)[V]) {       // entries i, i + step, ... before `end`, in order
+        for (; i < end; i += U * step) {
+            Pack<TG, V> g[U];
+#pragma unroll
+            for (int q = 0; q < U; ++q)
+                if (i + q * step < end) g[q] = *reinterpret_cast<const Pack<TG, V>*>(grads + (int64_t)(list[i + q * step] & 1023u) * p.ld_grads + col);
+#pragma unroll
+            for (int q = 0; q < U; ++q)
+                if (i + q * step < end) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) a[e] += to_float(g[q].v[e]);
+                }
+        }
+    };
+    if (group < groups)
+        for (int r = group; r < runs; r += groups) {
+            const int s = start[r], e = start[r + 1];
+            if (e - s > SHORT) continue;
+            for (int c = v0; c < vecs; c += wide) {
+                float a[V];
+#pragma unroll
+                for (int q = 0; q < V; ++q) a[q] = 0.f;
+                add_rows(s, e, 1, (int64_t)c * V, a);
+                finish_pack<TO, V>(p, (uint32_t)(r0 + (list[s] >> 10)), (int64_t)c * V, a);
+            }
+        }
+    for (int r = 0; r < runs; ++r) {
+        const int s = start[r], e = start[r + 1];
+        if (e - s <= SHORT) continue;
+        for (int c = v0; c - v0 < vecs; c += wide) {
+            float a[V];
+#pragma unroll
+            for (int q = 0; q < V; ++q) a[q] = 0.f;
+            if (group < groups && c < vecs) add_rows(s + group, e, groups, (int64_t)c * V, a);
+#pragma unroll
+            for (int q = 0; q < V; ++q) red[tid * V + q] = a[q];
+            __syncthreads();
+            if (group == 0 && c < vecs) {
+                for (int g = 1; g < groups; ++g) {
+#pragma unroll
+                    for (int q = 0; q < V; ++q) a[q] += red[(g * wide + v0) * V + q];
+                }
+                finish_pack<TO, V>(p, (uint32_t)(r0 + (list[s] >> 10)), (int64_t)c * V, a);
+            }
+            __syncthreads();
+        }
+    }
 }
 
 // One thread per (chunk of L sorted positions, pack of V columns).  An id whose rows lie within its first chunk and the next one
@@ -424,6 +677,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
     }
 }
 
+// Calls f with the pack length as a constant (eight: only where a side is a 16-bit type).
+template <typename TG, typename TO, class F> int with_vector(int vec, F&& f) {
+    if constexpr (sizeof(TG) == 2 || sizeof(TO) == 2) { if (vec == 8) return f(std::integral_constant<int, 8>()); }
+    if (vec == 4) return f(std::integral_constant<int, 4>());
+    if (vec == 2) return f(std::integral_constant<int, 2>());
+    return f(std::integral_constant<int, 1>());
+}
+
 int launch_lookup(LookupParams& p, int tt, int to, int vec, int dim, cudaStream_t s) {
     p.vecs = FastDiv((uint32_t)(dim / vec));
     p.rows_per_cta = (int)std::max<int64_t>(1, LOOKUP_THREADS * LOOKUP_UNROLL / p.vecs.d);
@@ -431,13 +692,24 @@ int launch_lookup(LookupParams& p, int tt, int to, int vec, int dim, cudaStream_
     return with_type(tt, [&](auto a) {
         return with_type(to, [&](auto b) {
             using TT = decltype(a); using TO = decltype(b);
-            constexpr bool wide = sizeof(TT) == 2 && sizeof(TO) == 2;
-            if (wide && vec == 8) lookup_kernel<TT, TO, wide ? 8 : 4><<<grid, LOOKUP_THREADS, 0, s>>>(p);
-            else if (vec == 4) lookup_kernel<TT, TO, 4><<<grid, LOOKUP_THREADS, 0, s>>>(p);
-            else if (vec == 2) lookup_kernel<TT, TO, 2><<<grid, LOOKUP_THREADS, 0, s>>>(p);
-            else lookup_kernel<TT, TO, 1><<<grid, LOOKUP_THREADS, 0, s>>>(p);
-            return launch_status(cudaGetLastError());
+            return with_vector<TT, TO>(vec, [&](auto v) {
+                lookup_kernel<TT, TO, decltype(v)::value><<<grid, LOOKUP_THREADS, 0, s>>>(p);
+                return launch_status(cudaGetLastError());
+            });
         });
+    });
+}
+
+template <typename TG, typename TO>
+int launch_small(SumParams& p, int vec, cudaStream_t s) {
+    p.vecs = FastDiv((uint32_t)(p.dim / vec));
+    // four CTAs an SM, more where a CTA's words would not fit 31 bits or its rows 22
+    int64_t per = ceil_div(p.rows, 148 * 4);
+    per = std::max<int64_t>(1, std::min<int64_t>({per, (1ll << 22) - 1, ((1ll << 31) - 1) / p.vecs.d}));
+    p.rows_per_cta = (int)per;
+    return with_vector<TG, TO>(vec, [&](auto v) {
+        grad_small_kernel<TG, TO, decltype(v)::value><<<(unsigned)ceil_div(p.rows, per), SMALL_THREADS, 0, s>>>(p);
+        return launch_status(cudaGetLastError());
     });
 }
 
@@ -445,16 +717,64 @@ template <typename TG, typename TO, int L>
 int launch_sum(SumParams& p, int vec, cudaStream_t s) {
     p.vecs = FastDiv((uint32_t)(p.dim / vec));
     const dim3 grid((unsigned)ceil_div((int64_t)p.chunks * p.vecs.d, SUM_THREADS));
-    constexpr bool wide = sizeof(TG) == 2 && sizeof(TO) == 2;
-    if (wide && vec == 8) grad_sum_kernel<TG, TO, wide ? 8 : 4, L><<<grid, SUM_THREADS, 0, s>>>(p);
-    else if (vec == 4) grad_sum_kernel<TG, TO, 4, L><<<grid, SUM_THREADS, 0, s>>>(p);
-    else if (vec == 2) grad_sum_kernel<TG, TO, 2, L><<<grid, SUM_THREADS, 0, s>>>(p);
-    else grad_sum_kernel<TG, TO, 1, L><<<grid, SUM_THREADS, 0, s>>>(p);
-    int rc = launch_status(cudaGetLastError());
+    const int rc = with_vector<TG, TO>(vec, [&](auto v) {
+        grad_sum_kernel<TG, TO, decltype(v)::value, L><<<grid, SUM_THREADS, 0, s>>>(p);
+        return launch_status(cudaGetLastError());
+    });
     if (rc != KGE_OK || p.chunks < 3) return rc;
     const dim3 joins((unsigned)std::min<int64_t>(p.chunks / 2, 592), (unsigned)ceil_div(p.dim, 32));
     grad_join_kernel<TO, L><<<joins, JOIN_THREADS, 0, s>>>(p);
     return launch_status(cudaGetLastError());
+}
+
+// Keys and positions in the order of the ids, in g.keys / g.pos of the returned index; the rows of a dense gradient set to zero.
+int sort_ids(const GradScratch& g, const SortPlan& plan, SortParams& q, bool zero, int64_t rows, int* where, cudaStream_t s) {
+    const int digits = 1 << plan.bits;
+    if (q.n <= CS_MAX) {
+        static DeviceOnce configured;
+        const cudaError_t e = once_per_device(configured, [] {
+            return cudaFuncSetAttribute(grad_cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cluster_sort_smem(CS_MAX, CS_MAX_BITS));
+        });
+        if (e != cudaSuccess) return KGE_ERR_CUDA;
+        q.keys_out = g.keys[0]; q.pos_out = g.pos[0];
+        q.zero_first = 0; q.zero_last = rows;
+        *where = 0;
+        const int zero_clusters = zero ? (int)std::min<int64_t>(16, ceil_div(rows * q.zero_row_bytes, 64 * 1024)) : 0;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)(CS_CTAS * (1 + zero_clusters))); cfg.blockDim = dim3(CS_THREADS); cfg.stream = s;
+        cfg.dynamicSmemBytes = cluster_sort_smem(q.n, plan.bits);
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = CS_CTAS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        return launch_status(cudaLaunchKernelEx(&cfg, grad_cluster_sort_kernel, q));
+    }
+    // the zeroing is shared out over the launches: the sort leaves most of the memory's bandwidth unused
+    const int launches = 1 + plan.passes;
+    int nth = 0;
+    auto zero_ctas = [&] {
+        q.zero_first = rows * nth / launches; q.zero_last = rows * (nth + 1) / launches;
+        ++nth;
+        return zero ? (int)std::min<int64_t>(148 * 6, ceil_div((q.zero_last - q.zero_first) * q.zero_row_bytes, 16 * GS_THREADS)) : 0;
+    };
+    int beside = zero_ctas();
+    grad_hist_kernel<<<plan.tiles + beside, GS_THREADS, 0, s>>>(q);
+    int rc = launch_status(cudaGetLastError());
+    for (int pass = 0; pass < plan.passes && rc == KGE_OK; ++pass) {
+        q.pass = pass; q.shift = pass * plan.bits;
+        q.keys_in = g.keys[(pass + 1) & 1]; q.pos_in = g.pos[(pass + 1) & 1];
+        q.keys_out = g.keys[pass & 1]; q.pos_out = g.pos[pass & 1];
+        q.hist = g.hist + (int64_t)pass * plan.tiles * digits;
+        q.hist_next = pass + 1 < plan.passes ? q.hist + (int64_t)plan.tiles * digits : nullptr;
+        grad_scan_kernel<<<(digits * 32 + 255) / 256, 256, 0, s>>>(q);
+        rc = launch_status(cudaGetLastError());
+        if (rc != KGE_OK) break;
+        beside = zero_ctas();
+        grad_scatter_kernel<<<plan.tiles + beside, GS_THREADS, 0, s>>>(q);
+        rc = launch_status(cudaGetLastError());
+    }
+    *where = (plan.passes - 1) & 1;
+    return rc;
 }
 
 }  // namespace
@@ -475,7 +795,7 @@ int kge_embedding_lookup(const void* table, int32_t table_type, int64_t rows, in
     p.table = table; p.out = out; p.ids = ids; p.rows = rows; p.ld_table = ld_table; p.ld_out = ld_out; p.n = n;
     p.padding_id = padding_id; p.scale = scale; p.status = status;
     const int tb = type_bytes(table_type), ob = type_bytes(out_type);
-    const int vec = vector_length(tb == 2 && ob == 2 ? 8 : 4, dim, ld_table, tb, table, ld_out, ob, out);
+    const int vec = vector_length(tb == 2 || ob == 2 ? 8 : 4, dim, ld_table, tb, table, ld_out, ob, out);
     return launch_lookup(p, table_type, out_type, vec, dim, static_cast<cudaStream_t>(stream));
 }
 
@@ -497,44 +817,28 @@ int kge_embedding_grad(const int32_t* ids, int32_t n, const void* grads, int32_t
         if (accumulate) return KGE_OK;
         return launch_status(cudaMemset2DAsync(table_grad, (size_t)ld_table * tb, 0, (size_t)dim * tb, (size_t)rows, s));
     }
-    if (!scratch || !aligned_to(scratch, 256) || scratch_bytes < kge_embedding_grad_scratch_bytes(rows, dim, n)) return KGE_ERR_WORKSPACE;
+    const size_t need = kge_embedding_grad_scratch_bytes(rows, dim, n);
+    if (need > 0 && (!scratch || !aligned_to(scratch, 256) || scratch_bytes < need)) return KGE_ERR_WORKSPACE;
+    const int vec = vector_length(gb == 2 || tb == 2 ? 8 : 4, dim, ld_grads, gb, grads, ld_table, tb, table_grad);
+    SumParams p{};
+    p.n = n; p.dim = dim; p.part_ld = (dim + 3) / 4 * 4; p.rows = (uint32_t)rows;
+    p.grads = grads; p.ld_grads = ld_grads; p.out = table_grad; p.ld_out = ld_table; p.scale = scale; p.accumulate = accumulate;
+    p.ids = ids; p.padding_id = padding_id; p.status = status;
+    if (n <= SMALL_MAX)
+        return with_type(grads_type, [&](auto a) { return with_type(table_type, [&](auto b) { return launch_small<decltype(a), decltype(b)>(p, vec, s); }); });
     const GradScratch g = carve_grad(static_cast<char*>(scratch), rows, dim, n);
     const SortPlan plan = sort_plan(rows, n);
-    const int digits = 1 << plan.bits;
     SortParams q{};
     q.ids = ids; q.n = n; q.tiles = plan.tiles; q.bits = plan.bits; q.passes = plan.passes; q.rows = (uint32_t)rows; q.padding_id = padding_id;
     q.hist = g.hist; q.total = g.total; q.list_count = g.list_count; q.status = status;
-    q.scanned = plan.tiles > GS_DIRECT_TILES;
-    int zero_ctas = 0;
-    if (!accumulate) {
-        q.zero = table_grad; q.zero_rows = rows; q.zero_row_bytes = (int64_t)dim * tb; q.zero_ld_bytes = ld_table * tb;
-        q.zero_vec = ld_table == dim && aligned_to(table_grad, 16) && q.zero_row_bytes % 16 == 0;
-        zero_ctas = (int)std::min<int64_t>(148 * 8, ceil_div(rows * q.zero_row_bytes, 16 * GS_THREADS));
-    }
-    grad_hist_kernel<<<plan.tiles + zero_ctas, GS_THREADS, 0, s>>>(q);
-    int rc = launch_status(cudaGetLastError());
-    for (int pass = 0; pass < plan.passes && rc == KGE_OK; ++pass) {
-        q.pass = pass; q.shift = pass * plan.bits;
-        q.keys_in = g.keys[(pass + 1) & 1]; q.pos_in = g.pos[(pass + 1) & 1];
-        q.keys_out = g.keys[pass & 1]; q.pos_out = g.pos[pass & 1];
-        q.hist = g.hist + (int64_t)pass * plan.tiles * digits;
-        q.hist_next = pass + 1 < plan.passes ? q.hist + (int64_t)plan.tiles * digits : nullptr;
-        if (q.scanned) {
-            grad_scan_kernel<<<(digits + 31) / 32, 32, 0, s>>>(q);
-            rc = launch_status(cudaGetLastError());
-            if (rc != KGE_OK) break;
-        }
-        grad_scatter_kernel<<<plan.tiles, GS_THREADS, 0, s>>>(q);
-        rc = launch_status(cudaGetLastError());
-    }
+    q.zero = static_cast<char*>(table_grad); q.zero_row_bytes = (int64_t)dim * tb; q.zero_ld_bytes = ld_table * tb;
+    q.zero_vec = ld_table == dim && aligned_to(table_grad, 16) && q.zero_row_bytes % 16 == 0;
+    int where = 0;
+    const int rc = sort_ids(g, plan, q, !accumulate, rows, &where, s);
     if (rc != KGE_OK) return rc;
-    SumParams p{};
-    p.keys = g.keys[(plan.passes - 1) & 1]; p.pos = g.pos[(plan.passes - 1) & 1];
-    p.n = n; p.dim = dim; p.part_ld = (dim + 3) / 4 * 4; p.rows = (uint32_t)rows;
+    p.keys = g.keys[where]; p.pos = g.pos[where];
     p.chunks = (int)ceil_div(n, chunk_rows(n));
-    p.grads = grads; p.ld_grads = ld_grads; p.out = table_grad; p.ld_out = ld_table; p.scale = scale; p.accumulate = accumulate;
     p.part = g.part; p.list = g.list; p.list_count = g.list_count;
-    const int vec = vector_length(gb == 2 && tb == 2 ? 8 : 4, dim, ld_grads, gb, grads, ld_table, tb, table_grad);
     return with_type(grads_type, [&](auto a) {
         return with_type(table_type, [&](auto b) {
             using TG = decltype(a); using TO = decltype(b);

@@ -21,7 +21,7 @@ def _call(K, name, order, base, /, **over):
 
 LOOKUP = dict(table=PTR, table_type=F32, rows=10, dim=8, ld_table=8, ids=PTR, n=4, scale=1.0, padding_id=-1, out=PTR, out_type=F32, ld_out=8,
               status=None, stream=None)
-GRAD = dict(ids=PTR, n=4, grads=PTR, grads_type=F32, ld_grads=8, scale=1.0, padding_id=-1, accumulate=0, table_grad=PTR, table_type=F32, rows=10,
+GRAD = dict(ids=PTR, n=4000, grads=PTR, grads_type=F32, ld_grads=8, scale=1.0, padding_id=-1, accumulate=0, table_grad=PTR, table_type=F32, rows=10,
             dim=8, ld_table=8, scratch=PTR, scratch_bytes=1 << 30, status=None, stream=None)
 DROPOUT = dict(x=PTR, x_type=F32, residual=None, out=PTR, out_type=F32, n=8, p=0.1, seed=1, step=0, step_dev=None, site=0, stream=None)
 QUANT = dict(x=PTR, x_type=F32, rows=4, cols=64, ldx=64, fp8_type=E4M3, block_rows=1, pow2=0, q=PTR, ldq=64, scales=PTR, qt=None, ldqt=0,
@@ -84,10 +84,11 @@ def test_matmul_scratch_is_checked(K):
 
 
 def test_scratch_sizes_cover_their_lists(K):
-    # two lists of (id, position) pairs and two partial rows per chunk of at least eight ids
-    for rows, dim, n in ((10, 8, 1), (1000, 32, 256), (91_000_000, 128, 24_576), (100, 256, 600_000)):
+    # a list of (id, position) pairs and partial rows for chunks of ids; short lists keep nothing
+    for rows, dim, n in ((10, 8, 1025), (91_000_000, 128, 24_576), (100, 256, 600_000)):
         got = K.embedding_grad_scratch_bytes(rows, dim, n)
-        assert got >= 16 * n and got % 256 == 0
+        assert got >= 8 * n and got % 256 == 0
+    assert K.embedding_grad_scratch_bytes(10, 8, 1) == 0 and K.embedding_grad_scratch_bytes(1000, 32, 1024) == 0
     assert K.embedding_grad_scratch_bytes(0, 8, 4) == 0 and K.embedding_grad_scratch_bytes(10, 8, 0) == 0
 
 
@@ -100,6 +101,7 @@ def test_binding_refuses_tensors_that_do_not_fit(K):
            lambda: K.embedding_lookup(f(10, 8), i(4).long(), f(4, 8)),
            lambda: K.embedding_lookup(f(10, 8).t(), i(4), f(4, 10)),
            lambda: K.embedding_lookup(f(10, 8).double(), i(4), f(4, 8)),
+           lambda: K.embedding_lookup(f(10, 8), i(4), f(4, 8), padding_id=1 << 32),
            lambda: K.embedding_grad(i(4), f(3, 8), f(10, 8)),
            lambda: K.embedding_grad(i(4), f(4, 8), f(10, 9)),
            lambda: K.dropout(f(8), f(9), 0.1, 1),
