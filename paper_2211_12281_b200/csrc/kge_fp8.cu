@@ -5,6 +5,7 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kge_ops.cuh"
 
@@ -25,115 +26,209 @@ struct QuantParams {
 };
 
 template <int FMT> struct Fp8Traits;
-template <> struct Fp8Traits<KGE_E4M3> { static constexpr float top = 448.f, least = 0.015625f; static constexpr uint32_t drop = 20; };
-template <> struct Fp8Traits<KGE_E5M2> { static constexpr float top = 57344.f, least = 6.103515625e-5f; static constexpr uint32_t drop = 21; };
+template <> struct Fp8Traits<KGE_E4M3> { static constexpr float top = 448.f; };
+template <> struct Fp8Traits<KGE_E5M2> { static constexpr float top = 57344.f; };
 
-// Scale of a block whose largest magnitude has the bit pattern `amax`.  A block of zeros has scale 1; an infinity or a NaN makes
-// the scale one, and with it every value that the block stands for NaN.
-template <int FMT>
-__device__ __forceinline__ float block_scale(uint32_t amax, bool pow2) {
-    float s = __uint_as_float(amax) / Fp8Traits<FMT>::top;
-    if (amax < 0x7F800000u) {
-        s = amax == 0u ? 1.f : fmaxf(s, 1.17549435e-38f);
-        if (pow2) s = __uint_as_float((__float_as_uint(s) + 0x007FFFFFu) & 0x7F800000u);
+// Eight consecutive values of a row, and their magnitudes as integers that order as they do (a NaN above all).
+template <typename TX> struct Eight;
+template <> struct Eight<float> {
+    float v[8];
+    __device__ __forceinline__ void load(const void* p) { *reinterpret_cast<Pack<float, 8>*>(v) = *static_cast<const Pack<float, 8>*>(p); }
+    __device__ __forceinline__ void set(int j, float x) { v[j] = x; }
+    __device__ __forceinline__ float value(int j) const { return v[j]; }
+    __device__ __forceinline__ uint32_t key(int j) const { return __float_as_uint(v[j]) & 0x7FFFFFFFu; }
+    __device__ __forceinline__ uint32_t most() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, key(j));
+        return m;
     }
-    return s;
-}
-
-// x / s in fp32 such that rounding it to 8 bits rounds the true quotient.  x * (1 / s) is within three units in the last place
-// of it, which only matters next to the middle of two 8-bit values: there (and below the normal range, whose middles lie
-// elsewhere) the quotient is cut off and its last bit set if anything was cut, so that no rounding falls on a middle by itself.
-template <int FMT>
-__device__ __forceinline__ float quotient(float x, float s, float inv, bool pow2) {
-    float t = x * inv;
-    if (!pow2) {
-        constexpr uint32_t drop = Fp8Traits<FMT>::drop, mid = 1u << (drop - 1);
-        const uint32_t off = (__float_as_uint(t) & ((1u << drop) - 1u)) - (mid - 4u);
-        if ((off <= 8u || fabsf(t) < Fp8Traits<FMT>::least) && x != 0.f) {
-            t = __fdiv_rz(x, s);
-            if (fmaf(-t, s, x) != 0.f) t = __uint_as_float(__float_as_uint(t) | 1u);
-        }
+};
+template <typename T16> struct Eight16 {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const void* p) { *reinterpret_cast<uint4*>(w) = *static_cast<const uint4*>(p); }
+    __device__ __forceinline__ void set(int j, T16 x) {
+        const uint32_t b = *reinterpret_cast<const uint16_t*>(&x);
+        w[j >> 1] = j & 1 ? (w[j >> 1] & 0xFFFFu) | b << 16 : b;
     }
-    return t;
-}
+    __device__ __forceinline__ uint32_t key(int j) const { return (j & 1 ? w[j >> 1] >> 16 : w[j >> 1]) & 0x7FFFu; }
+    __device__ __forceinline__ uint32_t most() const {
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int j = 1; j < 4; ++j) m = __vmaxu2(m, w[j] & 0x7FFF7FFFu);
+        return max(m & 0xFFFFu, m >> 16);
+    }
+};
+template <> struct Eight<__nv_bfloat16> : Eight16<__nv_bfloat16> {
+    __device__ __forceinline__ float value(int j) const { return __uint_as_float(j & 1 ? w[j >> 1] & 0xFFFF0000u : w[j >> 1] << 16); }
+};
+template <> struct Eight<__half> : Eight16<__half> {
+    __device__ __forceinline__ float value(int j) const {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j >> 1]));
+        return j & 1 ? f.y : f.x;
+    }
+};
+template <typename TX> __device__ __forceinline__ float key_value(uint32_t key);
+template <> __device__ __forceinline__ float key_value<float>(uint32_t key) { return __uint_as_float(key); }
+template <> __device__ __forceinline__ float key_value<__nv_bfloat16>(uint32_t key) { return __uint_as_float(key << 16); }
+template <> __device__ __forceinline__ float key_value<__half>(uint32_t key) { return __half2float(__ushort_as_half((unsigned short)key)); }
 
+// A block's scale, and what its values are multiplied by.  A block of zeros has scale 1; an infinity or a NaN makes the scale one,
+// and with it every value that the block stands for NaN.
+//
+// The 8-bit value stored is the one nearest to the true quotient x / s; t = x (1 / s) is within 2^-23 of it, which matters where a
+// middle of two 8-bit values is that close.  With 16-bit inputs that has structure.  s = (a / 7 2^k) (1 + e) with a the block's
+// largest value, |e| <= 2^-24 the rounding of s; x / a times 7 either is such a middle exactly, or off it by 2^-16 at least (x and
+// a have at most 11 bits, a middle 5).  In the first case the true quotient lies on the side of the middle that the sign of e
+// says, the same for all values of the block: `inv` leans by 2^-21 to that side.  Where e = 0 the quotient is the middle
+// itself, and t is brought back to the multiple of 16 units next to it; the last bit of `inv` says so.  With fp32 inputs
+// quotient() compares each value.
+struct Block { float s, inv; };
+template <typename TX, int FMT, bool POW2>
+__device__ __forceinline__ Block block_of(uint32_t key) {
+    const float a = key_value<TX>(key);
+    Block b;
+    b.s = a / Fp8Traits<FMT>::top;
+    const bool finite = a < __int_as_float(0x7F800000);       // (false for a NaN)
+    float e = 0.f;
+    if (finite) {
+        if (!POW2 && b.s > 1.17549435e-38f) e = fmaf(-b.s, Fp8Traits<FMT>::top, a);
+        b.s = a == 0.f ? 1.f : fmaxf(b.s, 1.17549435e-38f);
+        if (POW2) b.s = __uint_as_float((__float_as_uint(b.s) + 0x007FFFFFu) & 0x7F800000u);
+    }
+    b.inv = 1.f / b.s;
+    if (!POW2 && sizeof(TX) == 2) {
+        const float lean = e > 0.f ? 4.76837158e-7f : (e < 0.f ? -4.76837158e-7f : 0.f);
+        b.inv = __uint_as_float((__float_as_uint(fmaf(b.inv, lean, b.inv)) & ~1u) | (e == 0.f ? 1u : 0u));
+    }
+    return b;
+}
+// |x| / s in fp32 such that rounding it to 8 bits rounds the true quotient: m, the multiple of 16 units next to t (all middles are
+// such), is compared with it exactly (the sign of |x| - m s, one fused operation); the result is m or the value next to it.
+__device__ __forceinline__ float quotient(float x, float s, float inv) {
+    int32_t m = (int32_t)(__float_as_uint(fabsf(x) * inv) + 8u) & ~15;
+    const float r = fmaf(-__int_as_float(m), s, fabsf(x));
+    if (r > 0.f) ++m;
+    if (r < 0.f) --m;
+    return __uint_as_float((uint32_t)m | (__float_as_uint(x) & 0x80000000u));
+}
 template <int FMT>
 __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
     constexpr __nv_fp8_interpretation_t f = FMT == KGE_E4M3 ? __NV_E4M3 : __NV_E5M2;
     const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, f), hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, f);
     return lo | hi << 16;
 }
+template <typename TX, int FMT, bool POW2>
+__device__ __forceinline__ uint2 round8(float (&v)[8], const Block& b) {
+    if constexpr (POW2) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= b.inv;
+    } else if constexpr (sizeof(TX) == 2) {
+        const uint32_t snap = __float_as_uint(b.inv) & 1u, add = snap << 3, mask = ~(snap * 15u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float((__float_as_uint(v[j] * b.inv) + add) & mask);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = quotient(v[j], b.s, b.inv);
+    }
+    return make_uint2(pack4<FMT>(v[0], v[1], v[2], v[3]), pack4<FMT>(v[4], v[5], v[6], v[7]));
+}
+__device__ __forceinline__ void put8(uint8_t* dst, uint2 w, int64_t valid) {
+    if (valid >= 8) *reinterpret_cast<uint2*>(dst) = w;
+    else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (j < valid) dst[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+    }
+}
+
+// Largest of R rows' magnitudes over sixteen lanes (offsets 8 ... 1 of a warp's halves): every exchange halves the rows a lane keeps,
+// so that lane l is left with row row_of_lane<R>(l)'s, ready for one division a lane instead of R in all of them.
+template <int R>
+__device__ __forceinline__ uint32_t rows_max(uint32_t (&m)[R], int lane) {
+    int off = 8;
+#pragma unroll
+    for (int n = R; n > 1; n >>= 1, off >>= 1) {
+#pragma unroll
+        for (int i = 0; i < n / 2; ++i) {
+            const bool upper = lane & off;
+            const uint32_t keep = upper ? m[n / 2 + i] : m[i], give = upper ? m[i] : m[n / 2 + i];
+            m[i] = max(keep, __shfl_xor_sync(0xffffffffu, give, off));
+        }
+    }
+#pragma unroll
+    for (; off > 0; off >>= 1) m[0] = max(m[0], __shfl_xor_sync(0xffffffffu, m[0], off));
+    return m[0];
+}
+// A lane (of its half) that holds row i, and the row that lane l holds.
+template <int R> __device__ __forceinline__ int lane_of_row(int i) { return R == 8 ? i << 1 : (R == 4 ? i << 2 : i << 3); }
+template <int R> __device__ __forceinline__ int row_of_lane(int l) { return R == 8 ? (l & 15) >> 1 : (R == 4 ? (l & 15) >> 2 : (l & 15) >> 3); }
+template <typename TX, int R>
+__device__ __forceinline__ Block block_of_row(const Block& mine, int i) {
+    Block b;
+    b.inv = __shfl_sync(0xffffffffu, mine.inv, lane_of_row<R>(i), 16);
+    b.s = sizeof(TX) == 4 ? __shfl_sync(0xffffffffu, mine.s, lane_of_row<R>(i), 16) : 0.f;       // (only fp32 inputs look at it again)
+    return b;
+}
+
+// Values c0 ... c0 + 7 of row r; zeros beyond the matrix.
+template <typename TX>
+__device__ __forceinline__ void load8(const QuantParams& p, Eight<TX>& e, int64_t r, int64_t c0) {
+    const TX* x = static_cast<const TX*>(p.x) + r * p.ldx + c0;
+    if (p.vec && c0 + 8 <= p.cols && r < p.rows) e.load(x);
+    else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e.set(j, r < p.rows && c0 + j < p.cols ? x[j] : from_float<TX>(0.f));
+    }
+}
 
 // One CTA per 128 x 128 tile: thread (rg, cg) holds rows 8 rg .. + 8 and columns 8 cg .. + 8.
-template <typename TX, int FMT, bool SQUARE>
-__global__ void __launch_bounds__(256, 2) quantize_kernel(QuantParams p) {
+template <typename TX, int FMT, bool SQUARE, bool POW2>
+__global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 3 : 2) quantize_kernel(QuantParams p) {
     __shared__ uint32_t part[16][128];
-    __shared__ float2 col_scale[128];
+    __shared__ Block col_block[128];
     __shared__ alignas(16) uint2 turned[128][16];
     const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
     const int64_t tr = blockIdx.x / p.tiles_c, tc = blockIdx.x - tr * p.tiles_c;
     const int64_t r0 = tr * 128 + rg * 8, c0 = tc * 128 + cg * 8;
-    float v[8][8];
-    const TX* x = static_cast<const TX*>(p.x) + c0;
-    const bool whole = p.vec && c0 + 8 <= p.cols;
+    Eight<TX> x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t r = r0 + i;
-        if (whole && r < p.rows) {
-            const Pack<TX, 8> w = *reinterpret_cast<const Pack<TX, 8>*>(x + r * p.ldx);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = to_float(w.v[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = r < p.rows && c0 + j < p.cols ? to_float(x[r * p.ldx + j]) : 0.f;
-        }
-    }
-    auto bits = [](float f) { return __float_as_uint(f) & 0x7FFFFFFFu; };
-    float s_all = 1.f, inv_all = 1.f;
+    for (int i = 0; i < 8; ++i) load8<TX>(p, x[i], r0 + i, c0);
+    Block all{};
     if (SQUARE) {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) m = max(m, bits(v[i][j]));
+        for (int i = 0; i < 8; ++i) m = max(m, x[i].most());
         m = __reduce_max_sync(0xffffffffu, m);
         if ((tid & 31) == 0) part[0][tid >> 5] = m;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < 8; ++w) m = max(m, part[0][w]);
-        s_all = block_scale<FMT>(m, p.pow2);
-        inv_all = 1.f / s_all;
+        all = block_of<TX, FMT, POW2>(m);
         if (tid == 0) {
             const int64_t row_blocks = (p.rows + 127) / 128;
-            if (p.q) p.scales[tc * row_blocks + tr] = s_all;
-            if (p.qt) p.scales_t[tr * p.tiles_c + tc] = s_all;
+            if (p.q) p.scales[tc * row_blocks + tr] = all.s;
+            if (p.qt) p.scales_t[tr * p.tiles_c + tc] = all.s;
         }
     }
     if (p.q) {
+        Block mine = all;
+        if (!SQUARE) {
+            uint32_t m[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m[i] = x[i].most();
+            const int lane = tid & 31;
+            mine = block_of<TX, FMT, POW2>(rows_max<8>(m, lane));
+            const int64_t r = r0 + row_of_lane<8>(lane);
+            if ((lane & 1) == 0 && r < p.rows) p.scales[tc * p.rows + r] = mine.s;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float s = s_all, inv = inv_all;
-            if (!SQUARE) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, bits(v[i][j]));
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-                s = block_scale<FMT>(m, p.pow2);
-                inv = 1.f / s;
-                if (cg == 0 && r0 + i < p.rows) p.scales[tc * p.rows + r0 + i] = s;
-            }
-            if (r0 + i >= p.rows) continue;
+            const Block b = SQUARE ? all : block_of_row<TX, 8>(mine, i);
             float t[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = quotient<FMT>(v[i][j], s, inv, p.pow2);
-            const uint2 w = make_uint2(pack4<FMT>(t[0], t[1], t[2], t[3]), pack4<FMT>(t[4], t[5], t[6], t[7]));
-            uint8_t* dst = p.q + (r0 + i) * p.ldq + c0;
-            if (c0 + 8 <= p.cols) *reinterpret_cast<uint2*>(dst) = w;
-            else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) if (c0 + j < p.cols) dst[j] = (uint8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
-            }
+            for (int j = 0; j < 8; ++j) t[j] = x[i].value(j);
+            const uint2 w = round8<TX, FMT, POW2>(t, b);
+            if (r0 + i < p.rows) put8(p.q + (r0 + i) * p.ldq + c0, w, p.cols - c0);
         }
     }
     if (p.qt) {
@@ -142,7 +237,7 @@ __global__ void __launch_bounds__(256, 2) quantize_kernel(QuantParams p) {
             for (int j = 0; j < 8; ++j) {
                 uint32_t m = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) m = max(m, bits(v[i][j]));
+                for (int i = 0; i < 8; ++i) m = max(m, x[i].key(j));
                 part[rg][cg * 8 + j] = m;
             }
             __syncthreads();
@@ -150,21 +245,21 @@ __global__ void __launch_bounds__(256, 2) quantize_kernel(QuantParams p) {
                 uint32_t m = 0;
 #pragma unroll
                 for (int g = 0; g < 16; ++g) m = max(m, part[g][tid]);
-                const float s = block_scale<FMT>(m, p.pow2);
-                col_scale[tid] = make_float2(s, 1.f / s);
+                const Block b = block_of<TX, FMT, POW2>(m);
+                col_block[tid] = b;
                 const int64_t c = tc * 128 + tid;
-                if (c < p.cols) p.scales_t[tr * p.cols + c] = s;
+                if (c < p.cols) p.scales_t[tr * p.cols + c] = b.s;
             }
             __syncthreads();
         }
         // columns become rows of 128 bytes in shared memory; 8-byte unit u of row c lies at u ^ (c / 8), free of bank conflicts
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float2 cs = SQUARE ? make_float2(s_all, inv_all) : col_scale[cg * 8 + j];
+            const Block b = SQUARE ? all : col_block[cg * 8 + j];
             float t[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = quotient<FMT>(v[i][j], cs.x, cs.y, p.pow2);
-            turned[cg * 8 + j][rg ^ cg] = make_uint2(pack4<FMT>(t[0], t[1], t[2], t[3]), pack4<FMT>(t[4], t[5], t[6], t[7]));
+            for (int i = 0; i < 8; ++i) t[i] = x[i].value(j);
+            turned[cg * 8 + j][rg ^ cg] = round8<TX, FMT, POW2>(t, b);
         }
         __syncthreads();
 #pragma unroll
@@ -175,25 +270,71 @@ __global__ void __launch_bounds__(256, 2) quantize_kernel(QuantParams p) {
             const uint2 a = turned[c][(2 * piece) ^ (c >> 3)], b = turned[c][(2 * piece + 1) ^ (c >> 3)];
             uint8_t* dst = p.qt + col * p.ldqt + row;
             if (row + 16 <= p.rows) *reinterpret_cast<uint4*>(dst) = make_uint4(a.x, a.y, b.x, b.y);
-            else {
-                const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+            else { put8(dst, a, p.rows - row); if (p.rows - row > 8) put8(dst + 8, b, p.rows - row - 8); }
+        }
+    }
+}
+
+// Blocks of 1 x 128 along the rows only: a warp takes thirty-two rows of one block of columns, eight or four at a time (sixteen lanes of
+// eight columns each), the next ones' loads under way.
+template <typename TX, int FMT, bool POW2>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(QuantParams p) {
+    constexpr int STEP = sizeof(TX) == 2 ? 4 : 2, ROWS = 32, STEPS = ROWS / (2 * STEP);
+    const int lane = threadIdx.x & 31, cg = lane & 15;
+    const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t tr = unit / p.tiles_c, tc = unit - tr * p.tiles_c;
+    const int64_t r_first = tr * ROWS + (lane >> 4), c0 = tc * 128 + cg * 8;
+    if (tr * ROWS >= p.rows) return;
+    Eight<TX> x[2][STEP];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) if (row + j < p.rows) dst[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
-            }
+    for (int i = 0; i < STEP; ++i) load8<TX>(p, x[0][i], r_first + 2 * i, c0);
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k) {
+        if (tr * ROWS + 2 * STEP * k >= p.rows) break;
+        if (k + 1 < STEPS) {
+#pragma unroll
+            for (int i = 0; i < STEP; ++i) load8<TX>(p, x[(k + 1) & 1][i], r_first + 2 * (STEP * (k + 1) + i), c0);
+        }
+        uint32_t m[STEP];
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) m[i] = x[k & 1][i].most();
+        const Block mine = block_of<TX, FMT, POW2>(rows_max<STEP>(m, lane));
+        const int64_t r_mine = r_first + 2 * (STEP * k + row_of_lane<STEP>(lane));
+        if ((lane & (16 / STEP - 1)) == 0 && r_mine < p.rows) p.scales[tc * p.rows + r_mine] = mine.s;
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+            const int64_t r = r_first + 2 * (STEP * k + i);
+            const Block b = block_of_row<TX, STEP>(mine, i);
+            float t[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = x[k & 1][i].value(j);
+            const uint2 w = round8<TX, FMT, POW2>(t, b);
+            if (r < p.rows) put8(p.q + r * p.ldq + c0, w, p.cols - c0);
         }
     }
 }
 
 template <typename TX>
 int launch_quantize(const QuantParams& p, int fmt, bool square, cudaStream_t s) {
-    const dim3 grid((unsigned)(p.tiles_c * ceil_div(p.rows, 128)));
-    if (fmt == KGE_E4M3) {
-        if (square) quantize_kernel<TX, KGE_E4M3, true><<<grid, 256, 0, s>>>(p);
-        else quantize_kernel<TX, KGE_E4M3, false><<<grid, 256, 0, s>>>(p);
-    } else {
-        if (square) quantize_kernel<TX, KGE_E5M2, true><<<grid, 256, 0, s>>>(p);
-        else quantize_kernel<TX, KGE_E5M2, false><<<grid, 256, 0, s>>>(p);
-    }
+    auto with_format = [&](auto pow2) {
+        constexpr bool P = decltype(pow2)::value;
+        if (!square && !p.qt) {
+            const dim3 grid((unsigned)ceil_div(p.tiles_c * ceil_div(p.rows, 32), 8));
+            if (fmt == KGE_E4M3) quantize_rows_kernel<TX, KGE_E4M3, P><<<grid, 256, 0, s>>>(p);
+            else quantize_rows_kernel<TX, KGE_E5M2, P><<<grid, 256, 0, s>>>(p);
+            return;
+        }
+        const dim3 grid((unsigned)(p.tiles_c * ceil_div(p.rows, 128)));
+        if (fmt == KGE_E4M3) {
+            if (square) quantize_kernel<TX, KGE_E4M3, true, P><<<grid, 256, 0, s>>>(p);
+            else quantize_kernel<TX, KGE_E4M3, false, P><<<grid, 256, 0, s>>>(p);
+        } else {
+            if (square) quantize_kernel<TX, KGE_E5M2, true, P><<<grid, 256, 0, s>>>(p);
+            else quantize_kernel<TX, KGE_E5M2, false, P><<<grid, 256, 0, s>>>(p);
+        }
+    };
+    if (p.pow2) with_format(std::true_type());
+    else with_format(std::false_type());
     return launch_status(cudaGetLastError());
 }
 
