@@ -344,17 +344,24 @@ constexpr int FP_BM = 128, FP_BK = 128;                   // BK bytes = one 128-
 constexpr uint32_t FP_BOX_BYTES = 128 * FP_BK;            // 128 rows of an operand
 constexpr int FP_NACC = 2;                                // block sums in tensor memory
 constexpr int FP_COLS = 64;                               // columns of the tile per epilogue warp
-constexpr uint32_t FP_STORE_BYTES = 1024;                 // per epilogue warp: 32 rows x 32 bytes of the output on their way to memory
+// Three forms of the kernel: tiles of 256 columns, one CTA an SM, for many blocks of K; tiles of 128, two CTAs an SM (one loads and
+// multiplies while the other stores), for few; tiles of 128 whose blocks of K a cluster shares, where tiles are few.
+enum { FP_WIDE = 0, FP_PAIR = 1, FP_SPLIT = 2 };
+__host__ __device__ constexpr int fp_bn(int form) { return form == FP_WIDE ? 256 : 128; }
+__host__ __device__ constexpr int fp_stages(int form) { return form == FP_WIDE ? 4 : (form == FP_PAIR ? 2 : 6); }
+__host__ __device__ constexpr int fp_epi_warps(int form) { return 4 * fp_bn(form) / FP_COLS; }
+__host__ __device__ constexpr int fp_threads(int form) { return 32 * (4 + fp_epi_warps(form)); }     // (four more: copies, MMAs, two idle)
+__host__ __device__ constexpr int fp_ctas_per_sm(int form) { return form == FP_PAIR ? 2 : 1; }
+__host__ __device__ constexpr uint32_t fp_stage_bytes(int form) { return FP_BOX_BYTES + (uint32_t)fp_bn(form) * FP_BK; }
+// Per epilogue warp: 32 rows x 32 or 128 bytes of the output on their way to memory.
+__host__ __device__ constexpr uint32_t fp_store_row(int form) { return form == FP_PAIR ? 128 : 32; }
 // Blocks of K whose scales are in shared memory.  A slot needs no barrier of its own: its block's scales are read before the epilogue
 // hands back the block sum after the next one, without which no MMA of the block FP_NACC later is issued, without which no stage
 // that follows by fp_stages() more is filled again -- at least stages + FP_NACC + 1 blocks later.
-constexpr int FP_SLOTS = 8;
-__host__ __device__ constexpr int fp_stages(int bn) { return bn == 256 ? 4 : 3; }
-__host__ __device__ constexpr int fp_epi_warps(int bn) { return 4 * bn / FP_COLS; }
-__host__ __device__ constexpr int fp_threads(int bn) { return 32 * (4 + fp_epi_warps(bn)); }     // (four more: copies, MMAs, two idle)
-__host__ __device__ constexpr int fp_ctas_per_sm(int bn) { return bn == 256 ? 1 : 2; }
-__host__ __device__ constexpr uint32_t fp_stage_bytes(int bn) { return FP_BOX_BYTES + (uint32_t)bn * FP_BK; }
-__host__ __device__ constexpr size_t fp_smem_bytes(int bn) { return (size_t)fp_stages(bn) * fp_stage_bytes(bn) + fp_epi_warps(bn) * FP_STORE_BYTES + FP_SLOTS * (128 + bn) * 4 + 256; }
+__host__ __device__ constexpr int fp_slots(int form) { return fp_stages(form) + FP_NACC + 2; }
+__host__ __device__ constexpr size_t fp_smem_bytes(int form) {
+    return (size_t)fp_stages(form) * fp_stage_bytes(form) + fp_epi_warps(form) * 32 * fp_store_row(form) + fp_slots(form) * (128 + fp_bn(form)) * 4 + 256;
+}
 
 struct ProductParams {
     int64_t M, N;
@@ -439,29 +446,31 @@ __device__ __forceinline__ void fp_put(const ProductParams& p, int row, int col,
     }
 }
 
-// A warp's 32 rows x 64 columns, 32 bytes of each row at a time through shared memory: a store instruction covers whole 32-byte
-// sectors of sixteen rows.  Without an addend the values are rounded before they pass, with one after it is added.
-template <typename TO>
+// A warp's 32 rows x 64 columns, ROW bytes of each row at a time through shared memory, so that a store instruction covers whole
+// 32-byte sectors, or, with 128 bytes, whole lines.  (16-byte unit i of row r lies at i ^ (r mod units): no bank conflicts.)
+template <typename TO, int ROW>
 __device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int col0, const uint64_t (&acc)[FP_COLS / 2], float4* st, int lane) {
-    constexpr int V = 16 / sizeof(TO);                    // columns per lane and store; two lanes cover a row's 32 bytes
-    const int unit = lane & 1;
+    constexpr int V = 16 / sizeof(TO), UNITS = ROW / 16, PASS = ROW / sizeof(TO);      // columns per unit, units and columns per pass
+    constexpr int TURN = UNITS == 2 ? 2 : 0;                                            // rows 4 apart share banks at 32 bytes a row
 #pragma unroll
-    for (int c = 0; c < FP_COLS; c += 2 * V) {
-        Pack<TO, V> own[2];
+    for (int c = 0; c < FP_COLS; c += PASS) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float2 x = unpair(acc[c / 2 + e]);
-            own[2 * e / V].v[2 * e % V] = from_float<TO>(x.x);
-            own[2 * e / V].v[2 * e % V + 1] = from_float<TO>(x.y);
+        for (int i = 0; i < UNITS; ++i) {
+            Pack<TO, V> own;
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+                const float2 x = unpair(acc[(c + i * V + e) / 2]);
+                own.v[e] = from_float<TO>(x.x);
+                own.v[e + 1] = from_float<TO>(x.y);
+            }
+            st[lane * UNITS + (i ^ ((lane >> TURN) & (UNITS - 1)))] = *reinterpret_cast<const float4*>(&own);
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) st[lane * 2 + (i ^ (lane >> 2 & 1))] = *reinterpret_cast<const float4*>(&own[i]);
         __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int r = j * 16 + (lane >> 1), row = row0 + r, col = col0 + c + V * unit;
+        for (int j = 0; j < UNITS; ++j) {
+            const int r = j * (32 / UNITS) + lane / UNITS, unit = lane % UNITS, row = row0 + r, col = col0 + c + V * unit;
             if (row < p.M && col < p.N) {
-                const float4 w = st[r * 2 + (unit ^ (r >> 2 & 1))];
+                const float4 w = st[r * UNITS + (unit ^ ((r >> TURN) & (UNITS - 1)))];
                 fp_put<TO, V>(p, row, col, *reinterpret_cast<const Pack<TO, V>*>(&w));
             }
         }
@@ -469,11 +478,43 @@ __device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int c
     }
 }
 
-// The addend of the same tile joins the accumulators in fp32 before they are rounded.  A lane reads its own row, a 32-byte sector at a
-// time (fetched into L2 when the tile began): through shared memory, as the stores go, the loads on their way took registers
-// from the accumulators.
+// The addend of the same tile joins the accumulators in fp32 before they are rounded.
+// With 128-byte rows it passes through the warp's shared memory: fp_fetch_addend starts the copies of a pass (the first one's while
+// the tile is computed), fp_add waits for them.
 template <typename TO>
-__device__ __forceinline__ void fp_add(const ProductParams& p, int row, int col0, uint64_t (&acc)[FP_COLS / 2]) {
+__device__ __forceinline__ void fp_fetch_addend(const ProductParams& p, int row0, int col0, int c, float4* st, int lane) {
+    constexpr int V = 16 / sizeof(TO);
+    const int unit = lane & 7, col = col0 + c + V * unit;
+    const int bytes = min(V, (int)p.N - col) * (int)sizeof(TO);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int r = j * 4 + (lane >> 3), row = row0 + r;
+        if (row < p.M && bytes > 0)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(st + r * 8 + (unit ^ (r & 7)))),
+                         "l"(static_cast<const TO*>(p.addend) + row * p.ld_addend + col), "r"(bytes) : "memory");
+    }
+}
+template <typename TO>
+__device__ __forceinline__ void fp_add_staged(const ProductParams& p, int row0, int col0, uint64_t (&acc)[FP_COLS / 2], float4* st, int lane) {
+    constexpr int V = 16 / sizeof(TO), PASS = 128 / sizeof(TO);
+#pragma unroll
+    for (int c = 0; c < FP_COLS; c += PASS) {
+        if (c > 0) fp_fetch_addend<TO>(p, row0, col0, c, st, lane);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 w = st[lane * 8 + (i ^ (lane & 7))];
+            const Pack<TO, V> a = *reinterpret_cast<const Pack<TO, V>*>(&w);
+#pragma unroll
+            for (int e = 0; e < V; e += 2) acc[(c + i * V + e) / 2] = add2(acc[(c + i * V + e) / 2], pair(to_float(a.v[e]), to_float(a.v[e + 1])));
+        }
+        __syncwarp();
+    }
+}
+// Otherwise a lane reads its own row, a 32-byte sector at a time (fetched into L2 when the tile began).
+template <typename TO>
+__device__ __forceinline__ void fp_add_rows(const ProductParams& p, int row, int col0, uint64_t (&acc)[FP_COLS / 2]) {
     constexpr int V = 16 / sizeof(TO);
     if (row >= p.M) return;
     const TO* const add = static_cast<const TO*>(p.addend) + row * p.ld_addend + col0;
@@ -514,11 +555,11 @@ __device__ __forceinline__ float4 cluster_ld(uint32_t addr, uint32_t rank) {
 }
 
 // A cluster's CTAs hold partial sums of one tile in their shared memory; each adds up a share of it in the order of their ranks.
-template <typename TO, int BN>
+template <typename TO>
 __device__ __forceinline__ void fp_join(const ProductParams& p, uint32_t part, int m0, int n0, int tid) {
     const int rows = min(FP_BM, (int)p.M - m0);
     const uint32_t size = cluster_size();
-    constexpr int THREADS = 32 * fp_epi_warps(BN), PER_ROW = BN / 4;
+    constexpr int THREADS = 32 * fp_epi_warps(FP_SPLIT), PER_ROW = fp_bn(FP_SPLIT) / 4;
     for (int u = (int)cluster_rank() * THREADS + tid; u < rows * PER_ROW; u += (int)size * THREADS) {
         const int r = u / PER_ROW, q = u % PER_ROW, row = m0 + r, col = n0 + 4 * q;
         if (col >= p.N) continue;
@@ -544,20 +585,22 @@ __device__ __forceinline__ void fp_join(const ProductParams& p, uint32_t part, i
 // ring of shared-memory stages by TMA, warp 1 issues the MMAs of one block of 128 k into one of two accumulators in tensor memory,
 // the other warps, 64 columns each, multiply finished block sums by their scales and add them up in registers (the tensor cores
 // cannot carry an fp32 scale from block to block).
-template <int BN, bool SPLIT>
-__global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_product_kernel(const __grid_constant__ CUtensorMap tmA,
-                                                                                          const __grid_constant__ CUtensorMap tmB,
-                                                                                          const __grid_constant__ ProductParams p) {
-    constexpr uint32_t STAGE = fp_stage_bytes(BN), TMEM_COLS = FP_NACC * BN;
-    constexpr int STAGES = fp_stages(BN), EW = fp_epi_warps(BN);
-    // registers per thread as launched (20 warps x 96, or 12 x 80 twice), and how they are shared out: the epilogue's 64 sums and 32
-    // loaded values do not fit the launch's share
-    constexpr int REGS = BN == 256 ? 96 : 80, REGS_CONTROL = 32, REGS_EPI = REGS + 4 * (REGS - REGS_CONTROL) / EW / 8 * 8;
+template <int FORM>
+__global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_product_kernel(const __grid_constant__ CUtensorMap tmA,
+                                                                                              const __grid_constant__ CUtensorMap tmB,
+                                                                                              const __grid_constant__ ProductParams p) {
+    constexpr bool SPLIT = FORM == FP_SPLIT;
+    constexpr int BN = fp_bn(FORM), STAGES = fp_stages(FORM), EW = fp_epi_warps(FORM), SLOTS = fp_slots(FORM), STORE_ROW = fp_store_row(FORM);
+    constexpr uint32_t STAGE = fp_stage_bytes(FORM), TMEM_COLS = FP_NACC * BN;
+    // registers per thread as launched (20 warps x 96, 12 x 80 twice, or 12 x 168), and how they are shared out: the epilogue's 64 sums
+    // and 32 loaded values do not fit the launch's share
+    constexpr int REGS = FORM == FP_WIDE ? 96 : (FORM == FP_PAIR ? 80 : 168), REGS_CONTROL = 32;
+    constexpr int REGS_EPI = FORM == FP_SPLIT ? 168 : REGS + 4 * (REGS - REGS_CONTROL) / EW / 8 * 8;
     static_assert(4 * REGS_CONTROL + EW * REGS_EPI <= (4 + EW) * REGS, "register shares exceed the launch's");
     extern __shared__ __align__(1024) unsigned char fp_smem[];
     float4* const stores = reinterpret_cast<float4*>(fp_smem + (size_t)STAGES * STAGE);
-    float* const scales = reinterpret_cast<float*>(fp_smem + (size_t)STAGES * STAGE + EW * FP_STORE_BYTES);     // per slot: 128 of A, BN of B
-    uint64_t* full = reinterpret_cast<uint64_t*>(scales + FP_SLOTS * (128 + BN));
+    float* const scales = reinterpret_cast<float*>(fp_smem + (size_t)STAGES * STAGE + EW * 32 * STORE_ROW);     // per slot: 128 of A, BN of B
+    uint64_t* full = reinterpret_cast<uint64_t*>(scales + SLOTS * (128 + BN));
     uint64_t* empty = full + STAGES;
     uint64_t* acc_full = empty + STAGES;
     uint64_t* acc_empty = acc_full + FP_NACC;
@@ -618,7 +661,7 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
                     ++count;
                     if (++s == STAGES) { s = 0; phase ^= 1; }
-                    if (++slot == FP_SLOTS) slot = 0;
+                    if (++slot == SLOTS) slot = 0;
                 }
             }
             if (lane == 0) *filled = count;
@@ -649,7 +692,7 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
     } else {
         registers_up<REGS_EPI>();
         const int quarter = warp & 3, group = (warp - 4) >> 2;      // tensor-memory lanes and columns of this warp
-        float4* const st = stores + (warp - 4) * (FP_STORE_BYTES / 16);
+        float4* const st = stores + (warp - 4) * (32 * STORE_ROW / 16);
         const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group * FP_COLS);
         uint32_t buf = 0, phase = 0, slot = 0;
         bool ok = true;
@@ -658,7 +701,11 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
             uint64_t acc[FP_COLS / 2];
 #pragma unroll
             for (int i = 0; i < FP_COLS / 2; ++i) acc[i] = 0ull;
-            if (!SPLIT && p.addend) fp_with_out(p.out_type, [&](auto t) { fp_prefetch_addend<decltype(t)>(p, m0 + lane, n0); });
+            if (!SPLIT && p.addend) fp_with_out(p.out_type, [&](auto t) {
+                using TO = decltype(t);
+                if (STORE_ROW == 128 && p.vec) fp_fetch_addend<TO>(p, m0, n0, 0, st, lane);
+                if (STORE_ROW != 128 || !p.vec || sizeof(TO) == 4) fp_prefetch_addend<TO>(p, m0 + lane, n0);
+            });
 #pragma unroll 1
             for (int kb = kb0; kb < kb1; ++kb) {
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit));
@@ -695,7 +742,7 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
                     }
                 }
                 if (++buf == FP_NACC) { buf = 0; phase ^= 1; }
-                if (++slot == FP_SLOTS) slot = 0;
+                if (++slot == SLOTS) slot = 0;
             }
             if (!ok) break;
             if (SPLIT) {       // the ring's stages are free: every copy has been multiplied, every product read
@@ -708,15 +755,20 @@ __global__ void __launch_bounds__(fp_threads(BN), fp_ctas_per_sm(BN)) fp8_produc
                 }
             } else {
                 fp_with_out(p.out_type, [&](auto t) {
-                    if (p.addend) fp_add<decltype(t)>(p, m0 + lane, n0, acc);
-                    fp_store<decltype(t)>(p, m0, n0, acc, st, lane);
+                    using TO = decltype(t);
+                    if (p.addend) {
+                        if (STORE_ROW == 128 && p.vec) fp_add_staged<TO>(p, m0, n0, acc, st, lane);
+                        else fp_add_rows<TO>(p, m0 + lane, n0, acc);
+                    }
+                    fp_store<TO, STORE_ROW>(p, m0, n0, acc, st, lane);
                 });
             }
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");       // (an addend's copies, after a wait that ran out)
         if (SPLIT) {       // (every warp of the cluster comes here, also after a wait that ran out)
             cluster_sync();
             const int m0 = first / p.tiles_n * FP_BM, n0 = first % p.tiles_n * BN;
-            fp_with_out(p.out_type, [&](auto t) { fp_join<decltype(t), BN>(p, smem_u32(fp_smem), m0, n0, threadIdx.x - 128); });
+            fp_with_out(p.out_type, [&](auto t) { fp_join<decltype(t)>(p, smem_u32(fp_smem), m0, n0, threadIdx.x - 128); });
             cluster_sync();        // no CTA leaves while another reads its partial sums
         }
     }
@@ -766,37 +818,38 @@ int sm_count(int* sms) {
 }
 
 // How a product is cut up: columns of a tile, and CTAs that share a tile's blocks of K.
-struct ProductPlan { int bn, split; };
+struct ProductPlan { int form, split; };
 ProductPlan product_plan(int64_t M, int64_t N, int kblocks, int sms) {
     const int64_t tiles128 = ceil_div(M, FP_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, FP_BM) * ceil_div(N, 256);
     if (tiles128 < sms && kblocks > 1) {
         int split = (int)std::min<int64_t>({8, kblocks, std::max<int64_t>(1, sms / tiles128)});
         const int per = (kblocks + split - 1) / split;
         split = (kblocks + per - 1) / per;              // every CTA has a block
-        if (split > 1) return {128, split};
+        if (split > 1) return {FP_SPLIT, split};
     }
-    return {tiles256 >= sms && kblocks >= 16 ? 256 : 128, 1};
+    return {tiles256 >= sms && kblocks >= 16 ? FP_WIDE : FP_PAIR, 1};
 }
 
-template <int BN, bool SPLIT>
+template <int FORM>
 int launch_product(const CUtensorMap& a, const CUtensorMap& b, ProductParams& p, int split, int sms, cudaStream_t s) {
-    constexpr size_t smem = fp_smem_bytes(BN);
+    constexpr size_t smem = fp_smem_bytes(FORM);
+    static_assert((smem + 1024) * fp_ctas_per_sm(FORM) <= 228 * 1024, "shared memory of an SM");
     static DeviceOnce configured;
     cudaError_t e = once_per_device(configured, [] {
-        return cudaFuncSetAttribute(fp8_product_kernel<BN, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        return cudaFuncSetAttribute(fp8_product_kernel<FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     });
     if (e != cudaSuccess) return KGE_ERR_CUDA;
-    p.tiles_n = (int)ceil_div(p.N, BN);
+    p.tiles_n = (int)ceil_div(p.N, fp_bn(FORM));
     p.items = (int)(ceil_div(p.M, FP_BM) * p.tiles_n);
     p.kper = (p.kblocks + split - 1) / split;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(SPLIT ? p.items * split : std::min<int64_t>(p.items, (int64_t)sms * fp_ctas_per_sm(BN))));
-    cfg.blockDim = dim3(fp_threads(BN)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)(FORM == FP_SPLIT ? p.items * split : std::min<int64_t>(p.items, (int64_t)sms * fp_ctas_per_sm(FORM))));
+    cfg.blockDim = dim3(fp_threads(FORM)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = SPLIT ? 1 : 0;
-    return launch_status(cudaLaunchKernelEx(&cfg, fp8_product_kernel<BN, SPLIT>, a, b, p));
+    cfg.attrs = attr; cfg.numAttrs = FORM == FP_SPLIT ? 1 : 0;
+    return launch_status(cudaLaunchKernelEx(&cfg, fp8_product_kernel<FORM>, a, b, p));
 }
 
 }  // namespace
@@ -851,10 +904,10 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
     if (rc != KGE_OK) return rc;
     if (ceil_div(M, 128) * ceil_div(N, 128) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;
     const ProductPlan plan = product_plan(M, N, p.kblocks, sms);
-    p.idesc = fp_idesc(FP_BM, plan.bn, a_type == KGE_E5M2, b_type == KGE_E5M2);
+    p.idesc = fp_idesc(FP_BM, fp_bn(plan.form), a_type == KGE_E5M2, b_type == KGE_E5M2);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (plan.split > 1) return launch_product<128, true>(ma, mb, p, plan.split, sms, s);
-    return plan.bn == 256 ? launch_product<256, false>(ma, mb, p, 1, sms, s) : launch_product<128, false>(ma, mb, p, 1, sms, s);
+    if (plan.form == FP_SPLIT) return launch_product<FP_SPLIT>(ma, mb, p, plan.split, sms, s);
+    return plan.form == FP_WIDE ? launch_product<FP_WIDE>(ma, mb, p, 1, sms, s) : launch_product<FP_PAIR>(ma, mb, p, 1, sms, s);
 }
 
 }  // extern "C"
