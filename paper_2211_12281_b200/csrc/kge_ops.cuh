@@ -51,6 +51,29 @@ template <typename T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
 // fp32 in packs of eight are two 16-byte accesses
 template <> struct alignas(16) Pack<float, 8> { float v[8]; };
 
+// A pack of read-only memory, loaded here and not where the compiler would rather have it (it moves a load whose value is used under
+// a condition to that condition, behind the loads and uses before it).
+template <typename P> __device__ __forceinline__ P load_now(const void* p) {
+    P r;
+    if constexpr (sizeof(P) == 2) {
+        uint16_t a;
+        asm volatile("ld.global.nc.u16 %0, [%1];" : "=h"(a) : "l"(p));
+        *reinterpret_cast<uint16_t*>(&r) = a;
+    } else if constexpr (sizeof(P) == 4) {
+        asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(*reinterpret_cast<uint32_t*>(&r)) : "l"(p));
+    } else if constexpr (sizeof(P) == 8) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+        asm volatile("ld.global.nc.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    } else {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(P) / 16; ++i)
+            asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
+                         : "l"(static_cast<const char*>(p) + 16 * i));
+    }
+    return r;
+}
+
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }

@@ -6,9 +6,9 @@
 // function of the inputs alone.  Rows of the dense gradient that no id names are set to zero by CTAs beside the sort's.
 //   up to 1,024 ids     one launch: every CTA owns a range of table rows, picks the ids that fall into it and sorts those
 //   up to 65,536        one cluster of eight CTAs sorts in shared memory, exchanging counts and pairs between its CTAs
-//   more                hist     digit counts of every tile; clears the later passes' counts
+//   more                hist     digit counts of every tile, per pass (counted by atomics while the pass before scatters, frequent ids cost 12 us of 24)
 //                       scan     the counts become sums over the tiles before
-//                       scatter  one stable split by a digit; counts the next digit on the way
+//                       scatter  one stable split by a digit
 //   then                sum      chunks of sorted rows; what ends inside its chunk or the next one is final, the rest leaves partial sums
 //                       join     one CTA per (id that spans more, 32 columns): partial sums in a fixed order
 #include <algorithm>
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(LOOKUP_THREADS) lookup_kernel(LookupParams p) 
 
 constexpr int GS_THREADS = 256, GS_WARPS = GS_THREADS / 32, GS_ITEMS = 8;
 constexpr int GS_TILE = GS_THREADS * GS_ITEMS;     // ids per CTA of the sort in global memory
-constexpr int GS_MAX_BITS = 9, GS_MAX_PASSES = 4;
+constexpr int GS_MAX_BITS = 9;
 constexpr int CS_CTAS = 8, CS_THREADS = 512, CS_WARPS = CS_THREADS / 32, CS_ITEMS = 16;      // the cluster's sort
 constexpr int CS_SHARE = CS_THREADS * CS_ITEMS, CS_MAX = CS_CTAS * CS_SHARE, CS_MAX_BITS = 11;
 constexpr int SMALL_MAX = 1024, SMALL_THREADS = 256;
@@ -103,11 +103,11 @@ SortPlan sort_plan(int64_t rows, int n) {
 int chunk_rows(int n) { return n < (1 << 17) ? 8 : 32; }
 
 struct GradScratch {
-    uint32_t *keys[2], *pos[2];      // [n] sorted ids and positions, in turn
-    uint32_t* hist;                  // [passes][tiles][1 << bits]
+    uint2* pairs[2];                 // [n] (id, position) in the order of a pass, in turn
+    uint32_t* hist;                  // [tiles][1 << bits]
     uint32_t* total;                 // [1 << bits]
     float* part;                     // [chunks][2][dim rounded up to 4]
-    int32_t *list, *list_count;      // chunks in which an id begins that spans more
+    int2* list; int32_t* list_count; // (chunk in which an id begins that spans more, id)
     size_t bytes;
 };
 
@@ -118,13 +118,13 @@ GradScratch carve_grad(char* base, int64_t rows, int dim, int n) {
     const int64_t chunks = ceil_div(n, chunk_rows(n));
     GradScratch g{};
     if (n <= SMALL_MAX) return g;       // (one launch: nothing is kept)
-    for (int i = 0; i < (n > CS_MAX ? 2 : 1); ++i) { g.keys[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4)); g.pos[i] = reinterpret_cast<uint32_t*>(take((size_t)n * 4)); }
+    for (int i = 0; i < (n > CS_MAX ? 2 : 1); ++i) g.pairs[i] = reinterpret_cast<uint2*>(take((size_t)n * 8));
     if (n > CS_MAX) {
-        g.hist = reinterpret_cast<uint32_t*>(take((size_t)s.passes * s.tiles * (4u << s.bits)));
+        g.hist = reinterpret_cast<uint32_t*>(take((size_t)s.tiles * (4u << s.bits)));
         g.total = reinterpret_cast<uint32_t*>(take((size_t)4 << s.bits));
     }
     g.part = reinterpret_cast<float*>(take((size_t)chunks * 2 * ((dim + 3) / 4 * 4) * 4));
-    g.list = reinterpret_cast<int32_t*>(take((size_t)chunks * 4));
+    g.list = reinterpret_cast<int2*>(take((size_t)chunks * 8));
     g.list_count = reinterpret_cast<int32_t*>(take(256));
     g.bytes = used;
     return g;
@@ -135,17 +135,16 @@ struct SortParams {
     int n, tiles, bits, shift, pass, passes;
     uint32_t rows;
     int32_t padding_id;
-    const uint32_t *keys_in, *pos_in;
-    uint32_t *keys_out, *pos_out;
-    uint32_t *hist, *hist_next, *total;   // this pass's and the next one's [tiles][1 << bits]
+    const uint2* pairs_in;
+    uint2* pairs_out;
+    uint32_t *hist, *total;               // [tiles][1 << bits] counts of a pass, then sums over the tiles before; [1 << bits]
     int32_t *list_count, *status;
     // dense gradient rows set to zero by CTAs beside the sort's
     char* zero; int64_t zero_row_bytes, zero_ld_bytes, zero_first, zero_last;     // the rows, and which of them in this launch
     int zero_vec;                         // rows are whole 16-byte words and lie back to back
 };
 
-__device__ __forceinline__ uint32_t grad_key(const SortParams& p, int i) {
-    const int32_t id = p.ids[i];
+__device__ __forceinline__ uint32_t grad_key(const SortParams& p, int32_t id) {
     if (id == p.padding_id) return p.rows;
     if (id < 0 || (uint32_t)id >= p.rows) { note_status(p.status, KGE_ERR_ID_RANGE); return p.rows; }
     return (uint32_t)id;
@@ -170,20 +169,40 @@ __device__ __forceinline__ void zero_rows(const SortParams& p, int64_t cta, int6
     }
 }
 
+// The lanes (of those that are `in`) that hold this lane's digit of at most BITS bits: a vote per bit, all of them independent.
+template <int BITS>
+__device__ __forceinline__ unsigned same_digit(uint32_t digit, bool in) {
+    unsigned same = __ballot_sync(0xffffffffu, in);
+#pragma unroll
+    for (int b = 0; b < BITS; ++b) {
+        const bool one = digit >> b & 1;
+        const unsigned v = __ballot_sync(0xffffffffu, one);
+        same &= one ? v : ~v;
+    }
+    return same;
+}
+
 __global__ void __launch_bounds__(GS_THREADS) grad_hist_kernel(SortParams p) {
     __shared__ uint32_t count[1 << GS_MAX_BITS];
+    grid_dependency_wait();
+    allow_dependents();
     const int digits = 1 << p.bits, tid = threadIdx.x;
     if ((int)blockIdx.x >= p.tiles) { zero_rows(p, blockIdx.x - p.tiles, gridDim.x - p.tiles); return; }
-    for (int d = tid; d < digits; d += GS_THREADS) {
-        count[d] = 0;
-        for (int q = 1; q < p.passes; ++q) p.hist[((int64_t)q * p.tiles + blockIdx.x) * digits + d] = 0;
-    }
+    for (int d = tid; d < digits; d += GS_THREADS) count[d] = 0;
     if (blockIdx.x == 0 && tid == 0) *p.list_count = 0;
     __syncthreads();
+    uint32_t v[GS_ITEMS];
+#pragma unroll
+    for (int k = 0; k < GS_ITEMS; ++k) {
+        const int64_t i = min((int64_t)blockIdx.x * GS_TILE + k * GS_THREADS + tid, (int64_t)p.n - 1);
+        v[k] = load_now<uint32_t>(p.pass == 0 ? reinterpret_cast<const uint32_t*>(p.ids) + i : &p.pairs_in[i].x);
+    }
+#pragma unroll
+    for (int k = 0; k < GS_ITEMS; ++k) asm volatile("" ::"r"(v[k]));
 #pragma unroll
     for (int k = 0; k < GS_ITEMS; ++k) {
         const int64_t i = (int64_t)blockIdx.x * GS_TILE + k * GS_THREADS + tid;
-        if (i < p.n) atomicAdd(&count[grad_key(p, (int)i) & (digits - 1)], 1u);
+        if (i < p.n) atomicAdd(&count[((p.pass == 0 ? grad_key(p, (int32_t)v[k]) : v[k]) >> p.shift) & (digits - 1)], 1u);
     }
     __syncthreads();
     for (int d = tid; d < digits; d += GS_THREADS) p.hist[(int64_t)blockIdx.x * digits + d] = count[d];
@@ -191,6 +210,8 @@ __global__ void __launch_bounds__(GS_THREADS) grad_hist_kernel(SortParams p) {
 
 // A warp per digit turns the tiles' counts into sums over the tiles before.
 __global__ void __launch_bounds__(256) grad_scan_kernel(SortParams p) {
+    grid_dependency_wait();
+    allow_dependents();
     const int digits = 1 << p.bits, d = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
     if (d >= digits) return;
     uint32_t run = 0;
@@ -218,6 +239,8 @@ __global__ void __launch_bounds__(GS_THREADS) grad_scatter_kernel(SortParams p) 
     __shared__ uint32_t base[1 << GS_MAX_BITS];
     __shared__ uint32_t warp_tot[GS_WARPS];
     const int digits = 1 << p.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, tile = blockIdx.x;
+    grid_dependency_wait();
+    allow_dependents();
     if (tile >= p.tiles) { zero_rows(p, tile - p.tiles, gridDim.x - p.tiles); return; }
     for (int d = lane; d < digits; d += 32) cnt[warp][d] = 0;
     __syncwarp();
@@ -225,17 +248,21 @@ __global__ void __launch_bounds__(GS_THREADS) grad_scatter_kernel(SortParams p) 
     const int64_t i0 = (int64_t)tile * GS_TILE + warp * 32 * GS_ITEMS;
 #pragma unroll
     for (int k = 0; k < GS_ITEMS; ++k) {
-        const int64_t i = i0 + k * 32 + lane;
-        if (i < p.n) {
-            key[k] = p.pass == 0 ? grad_key(p, (int)i) : p.keys_in[i];
-            pos[k] = p.pass == 0 ? (uint32_t)i : p.pos_in[i];
-        }
+        const int64_t i = min(i0 + k * 32 + lane, (int64_t)p.n - 1);
+        if (p.pass == 0) { key[k] = load_now<uint32_t>(p.ids + i); pos[k] = (uint32_t)i; }
+        else { const uint2 v = load_now<uint2>(p.pairs_in + i); key[k] = v.x; pos[k] = v.y; }
+    }
+#pragma unroll
+    for (int k = 0; k < GS_ITEMS; ++k) asm volatile("" ::"r"(key[k]), "r"(pos[k]));
+    if (p.pass == 0) {
+#pragma unroll
+        for (int k = 0; k < GS_ITEMS; ++k) if (i0 + k * 32 + lane < p.n) key[k] = grad_key(p, (int32_t)key[k]);
     }
 #pragma unroll
     for (int k = 0; k < GS_ITEMS; ++k) {
         const bool in = i0 + k * 32 + lane < p.n;
-        const uint32_t digit = in ? (key[k] >> p.shift) & (digits - 1) : 1u << GS_MAX_BITS;     // (lanes beyond the list: a digit of their own)
-        const unsigned same = __match_any_sync(0xffffffffu, digit), before = same & ((1u << lane) - 1u);
+        const uint32_t digit = (key[k] >> p.shift) & (digits - 1);
+        const unsigned same = same_digit<GS_MAX_BITS>(digit, in), before = same & ((1u << lane) - 1u);
         uint32_t seen = 0;
         if (in) seen = cnt[warp][digit];
         __syncwarp();
@@ -276,9 +303,7 @@ __global__ void __launch_bounds__(GS_THREADS) grad_scatter_kernel(SortParams p) 
         if (i0 + k * 32 + lane >= p.n) continue;
         const uint32_t digit = (key[k] >> p.shift) & (digits - 1);
         const uint32_t dst = base[digit] + cnt[warp][digit] + at[k];
-        p.keys_out[dst] = key[k];
-        p.pos_out[dst] = pos[k];
-        if (p.hist_next) atomicAdd(&p.hist_next[(int64_t)(dst / GS_TILE) * digits + ((key[k] >> (p.shift + p.bits)) & (digits - 1))], 1u);
+        p.pairs_out[dst] = make_uint2(key[k], pos[k]);
     }
 }
 
@@ -298,6 +323,8 @@ size_t cluster_sort_smem(int n, int bits) {       // pairs twice, warps' counts,
 // holds its new place; the last pass stores to global memory.  The other clusters set rows to zero.
 __global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortParams p) {
     extern __shared__ __align__(16) unsigned char cs_smem[];
+    grid_dependency_wait();
+    allow_dependents();
     if (blockIdx.x >= CS_CTAS) { zero_rows(p, blockIdx.x - CS_CTAS, gridDim.x - CS_CTAS); return; }
     __shared__ uint32_t warp_tot[CS_WARPS];
     const int digits = 1 << p.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -314,12 +341,21 @@ __global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortPa
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * p.bits;
         for (int d = lane; d < digits; d += 32) cnt[warp * digits + d] = 0;
+        if (pass == 0) {
 #pragma unroll
-        for (int k = 0; k < CS_ITEMS; ++k) {
-            const int i = first + k * 32 + lane;
-            if (k < rounds && i < have) {
-                if (pass == 0) { pos[k] = (uint32_t)(rank * share + i); key[k] = grad_key(p, (int)pos[k]); }
-                else { const uint2 v = pairs[pass & 1][i]; key[k] = v.x; pos[k] = v.y; }
+            for (int k = 0; k < CS_ITEMS; ++k) {
+                pos[k] = (uint32_t)min((int64_t)rank * share + first + k * 32 + lane, (int64_t)p.n - 1);
+                key[k] = k < rounds ? load_now<uint32_t>(reinterpret_cast<const uint32_t*>(p.ids) + pos[k]) : 0u;
+            }
+#pragma unroll
+            for (int k = 0; k < CS_ITEMS; ++k) asm volatile("" ::"r"(key[k]));
+#pragma unroll
+            for (int k = 0; k < CS_ITEMS; ++k) if (k < rounds && first + k * 32 + lane < have) key[k] = grad_key(p, (int32_t)key[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < CS_ITEMS; ++k) {
+                const int i = first + k * 32 + lane;
+                if (k < rounds && i < have) { const uint2 v = pairs[pass & 1][i]; key[k] = v.x; pos[k] = v.y; }
             }
         }
         __syncwarp();
@@ -327,8 +363,8 @@ __global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortPa
         for (int k = 0; k < CS_ITEMS; ++k) {
             if (k >= rounds) break;
             const bool in = first + k * 32 + lane < have;
-            const uint32_t digit = in ? (key[k] >> shift) & (digits - 1) : 1u << CS_MAX_BITS;
-            const unsigned same = __match_any_sync(0xffffffffu, digit), before = same & ((1u << lane) - 1u);
+            const uint32_t digit = (key[k] >> shift) & (digits - 1);
+            const unsigned same = same_digit<CS_MAX_BITS>(digit, in), before = same & ((1u << lane) - 1u);
             uint32_t seen = 0;
             if (in) seen = cnt[warp * digits + digit];
             __syncwarp();
@@ -380,7 +416,7 @@ __global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortPa
             if (k >= rounds || first + k * 32 + lane >= have) continue;
             const uint32_t digit = (key[k] >> shift) & (digits - 1);
             const uint32_t dst = base[digit] + cnt[warp * digits + digit] + at[k];
-            if (last) { p.keys_out[dst] = key[k]; p.pos_out[dst] = pos[k]; }
+            if (last) p.pairs_out[dst] = make_uint2(key[k], pos[k]);
             else { const uint32_t r = dst / share; cs_store2(cs_map(out + (dst - r * share) * 8, r), key[k], pos[k]); }
         }
         cs_sync();         // the pairs are in place; nobody reads this pass's counts any more
@@ -388,7 +424,7 @@ __global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortPa
 }
 
 struct SumParams {
-    const uint32_t *keys, *pos;
+    const uint2* pairs;                    // (id, position) in order
     int n, chunks, dim, part_ld;
     uint32_t rows;
     const void* grads; int64_t ld_grads;
@@ -396,7 +432,7 @@ struct SumParams {
     float scale;
     int accumulate;
     float* part;
-    int32_t *list, *list_count;
+    int2* list; int32_t* list_count;
     FastDiv vecs;
     const int32_t* ids; int32_t padding_id; int rows_per_cta; int32_t* status;     // grad_small_kernel
 };
@@ -503,14 +539,12 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
         for (; i < end; i += U * step) {
             Pack<TG, V> g[U];
 #pragma unroll
-            for (int q = 0; q < U; ++q)
-                if (i + q * step < end) g[q] = *reinterpret_cast<const Pack<TG, V>*>(grads + (int64_t)(list[i + q * step] & 1023u) * p.ld_grads + col);
+            for (int q = 0; q < U; ++q)        // (beyond the end: the first again, for nothing -- a load under a condition waits for its use)
+                g[q] = load_now<Pack<TG, V>>(grads + (int64_t)(list[i + q * step < end ? i + q * step : i] & 1023u) * p.ld_grads + col);
 #pragma unroll
             for (int q = 0; q < U; ++q)
-                if (i + q * step < end) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) a[e] += to_float(g[q].v[e]);
-                }
+                for (int e = 0; e < V; ++e) a[e] += i + q * step < end ? to_float(g[q].v[e]) : 0.f;
         }
     };
     if (group < groups)
@@ -548,123 +582,149 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
     }
 }
 
+// Where a run's sum goes: a partial sum (slot 0: of the chunk's first run, 1: of its last) or the row itself.
+template <typename TO, int V>
+__device__ __forceinline__ void flush_run(const SumParams& p, int c, bool head, bool tail, uint32_t row, int64_t col, const float (&a)[V]) {
+    if (head || tail) {
+        float* dst = p.part + ((int64_t)c * 2 + (head ? 0 : 1)) * p.part_ld + col;
+        if constexpr (V % 4 == 0) {
+#pragma unroll
+            for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(a[e], a[e + 1], a[e + 2], a[e + 3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) dst[e] = a[e];
+        }
+        if (!head && col == 0) p.list[atomicAdd(p.list_count, 1)] = make_int2(c, (int)row);
+    } else finish_pack<TO, V>(p, row, col, a);
+}
+
 // One thread per (chunk of L sorted positions, pack of V columns).  An id whose rows lie within its first chunk and the next one
 // is added up by the thread that meets its first row; one that reaches further leaves a partial sum per chunk.
+// A thread's packs of the next DEPTH rows are on their way into its own places in shared memory, so the loop over the rows is one short
+// body: unrolled by eight with the packs in registers it did not stay in the instruction cache (136 us against XX at 500,000 x 256).
+constexpr int SUM_DEPTH = 8;
 template <typename TG, typename TO, int V, int L>
 __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
+    constexpr int BYTES = V * (int)sizeof(TG);
+    constexpr bool ASYNC = BYTES >= 4;                    // (asynchronous copies take 4, 8 or 16 bytes)
+    __shared__ alignas(16) unsigned char ring[ASYNC ? SUM_DEPTH * SUM_THREADS * BYTES : 16];
+    grid_dependency_wait();
+    allow_dependents();
     const int64_t item = (int64_t)blockIdx.x * SUM_THREADS + threadIdx.x;
     const int64_t vecs = p.vecs.d;
     const int c = item < (1ll << 31) ? (int)p.vecs.div((uint32_t)item) : (int)(item / vecs);
     if (c >= p.chunks) return;
     const int64_t col = (item - c * vecs) * V;
-    const int first = c * L, last = min(p.n, first + L);        // [first, last): this chunk
+    const int64_t first = (int64_t)c * L, last = min((int64_t)p.n, first + L);        // [first, last): this chunk
     const TG* grads = static_cast<const TG*>(p.grads) + col;
-    const uint32_t none = p.rows;
-    const uint32_t lead = p.keys[first];
+    const uint32_t none = p.rows, beyond = ~0u;
+    const uint32_t lead = p.pairs[first].x, end_key = p.pairs[last - 1].x;
+    const uint32_t before = c > 0 ? p.pairs[first - 1].x : beyond, early = first - L - 1 >= 0 ? p.pairs[first - L - 1].x : beyond;
+    const uint32_t after = last < p.n ? p.pairs[last].x : beyond, far = first + 2 * L < p.n ? p.pairs[first + 2 * L].x : beyond;
     if (lead == none) return;                                   // only ids of no row from here on
-    // the first run: does it begin here, in the chunk before, or earlier?
-    int r = first;
-    bool head_part = false;
-    if (c > 0 && p.keys[first - 1] == lead) {
-        const bool early = first - L - 1 >= 0 && p.keys[first - L - 1] == lead;      // it has rows before the chunk before
-        const bool through = last < p.n && p.keys[last] == lead;                     // and beyond this one
-        if (early || through) head_part = true;
-        else { while (r < last && p.keys[r] == lead) ++r; }                          // the chunk before adds these rows
-    }
+    // a first run that began in the chunk before is that chunk's, unless it reaches across a whole chunk: then a partial sum
+    const bool head_part = before == lead && (early == lead || after == lead), skip = before == lead && !head_part;
+    // a run that goes on beyond this chunk is taken along if it ends within the next one, else a partial sum
+    const bool on = end_key != none && after == end_key && !(head_part && end_key == lead);
+    const bool tail_part = on && far == end_key;
+    const int64_t stop = on && !tail_part ? min((int64_t)p.n, first + 2 * L) : last;       // one past the last row that may be this thread's
+    const uint32_t place = smem_u32(ring) + threadIdx.x * BYTES;
+    // the row at sorted position r, or `beyond`: rows past the last run, skipped ones, ids of no row
+    auto key_at = [&](int64_t r) {
+        if (r >= stop) return beyond;
+        const uint32_t k = p.pairs[r].x;
+        return (r >= last && k != end_key) || (skip && k == lead) || k == none ? beyond : k;
+    };
+    auto issue = [&](int64_t r, int slot) {
+        if constexpr (ASYNC) {
+            if (key_at(r) != beyond) {
+                const TG* src = grads + (int64_t)p.pairs[r].y * p.ld_grads;
+                const uint32_t dst = place + slot * (SUM_THREADS * BYTES);
+                if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < SUM_DEPTH - 1; ++u) issue(first + u, u);
     float a[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) a[e] = 0.f;
-    int stop = last;                  // one past the last row this thread adds
-    bool tail_part = false;
-    if (r < last) {
-        const uint32_t end_key = p.keys[last - 1];
-        // a run that goes on beyond the chunk: taken along if it ends within the next one, else a partial sum
-        if (end_key != none && last < p.n && p.keys[last] == end_key && !(head_part && end_key == lead)) {
-            const int far = first + 2 * L;
-            if (far < p.n && p.keys[far] == end_key) tail_part = true;
-            else { const int most = min(p.n, far); while (stop < most && p.keys[stop] == end_key) ++stop; }
-        }
-    }
-    if (r >= stop) return;
-    uint32_t cur = p.keys[r];
+    uint32_t cur = beyond;                                      // (no run yet)
     bool is_head = head_part;
-    constexpr int U = 8;
-    for (int r0 = r; r0 < stop; r0 += U) {
-        uint32_t k[U];
-        Pack<TG, V> g[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            k[u] = r0 + u < stop ? p.keys[r0 + u] : none;
-            if (k[u] != none) g[u] = *reinterpret_cast<const Pack<TG, V>*>(grads + (int64_t)p.pos[r0 + u] * p.ld_grads);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (r0 + u >= stop) break;
-            if (k[u] != cur) {
-                if (is_head) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) p.part[(int64_t)c * 2 * p.part_ld + col + e] = a[e];
-                    is_head = false;
-                } else if (cur != none) finish_pack<TO, V>(p, cur, col, a);
-                cur = k[u];
+    int slot = 0;
+#pragma unroll 1
+    for (int64_t r = first; r < stop; ++r) {
+        issue(r + SUM_DEPTH - 1, slot == 0 ? SUM_DEPTH - 1 : slot - 1);
+        const uint32_t k = key_at(r);
+        if (k != beyond) {
+            if (k != cur) {
+                if (cur != beyond) { flush_run<TO, V>(p, c, is_head, false, cur, col, a); is_head = false; }
+                cur = k;
 #pragma unroll
                 for (int e = 0; e < V; ++e) a[e] = 0.f;
             }
-            if (k[u] != none) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) a[e] += to_float(g[u].v[e]);
+            Pack<TG, V> g;
+            if constexpr (ASYNC) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(SUM_DEPTH - 1) : "memory");
+                g = *reinterpret_cast<const Pack<TG, V>*>(ring + (size_t)slot * (SUM_THREADS * BYTES) + threadIdx.x * BYTES);
+            } else {
+                g = *reinterpret_cast<const Pack<TG, V>*>(grads + (int64_t)p.pairs[r].y * p.ld_grads);
             }
-        }
-    }
-    if (cur == none) return;
-    if (is_head || tail_part) {
-        float* dst = p.part + ((int64_t)c * 2 + (is_head ? 0 : 1)) * p.part_ld + col;
 #pragma unroll
-        for (int e = 0; e < V; ++e) dst[e] = a[e];
-        if (!is_head && col == 0) p.list[atomicAdd(p.list_count, 1)] = c;
-    } else finish_pack<TO, V>(p, cur, col, a);
+            for (int e = 0; e < V; ++e) a[e] += to_float(g.v[e]);
+        }
+        slot = slot + 1 == SUM_DEPTH ? 0 : slot + 1;
+    }
+    if (cur != beyond) flush_run<TO, V>(p, c, is_head, tail_part && cur == end_key, cur, col, a);
 }
 
-// Ids that span more than two chunks: CTA (x, y) takes the x-th, (x + grid)-th, ... of the list and 32 columns.  Thirty-two stripes
-// of eight threads add every 32nd chunk's partial sum, then the stripes are added in order.
+// Ids that span more than two chunks: CTA (x, y) takes the x-th, (x + grid)-th, ... of the list and 64 columns.  Sixteen stripes
+// of sixteen threads add every 16th chunk's partial sum, then the stripes are added in order.
+constexpr int JOIN_COLS = 64;
 template <typename TO, int L>
 __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
-    constexpr int STRIPES = JOIN_THREADS / 8;
-    __shared__ float4 red[STRIPES][8];
-    const int lane8 = threadIdx.x & 7, stripe = threadIdx.x >> 3;
-    const int col = blockIdx.y * 32 + lane8 * 4;
+    constexpr int LANES = JOIN_COLS / 4, STRIPES = JOIN_THREADS / LANES, U = 8;
+    __shared__ float4 red[STRIPES][LANES];
+    __shared__ float4 ring[U][JOIN_THREADS];
+    grid_dependency_wait();
+    const int lane = threadIdx.x % LANES, stripe = threadIdx.x / LANES;
+    const int col = blockIdx.y * JOIN_COLS + lane * 4;
     const int count = *p.list_count;
     for (int x = blockIdx.x; x < count; x += gridDim.x) {
-        const int c0 = p.list[x];
-        const uint32_t key = p.keys[(c0 + 1) * L];
+        const int2 run = p.list[x];
+        const int c0 = run.x;
+        const uint32_t key = (uint32_t)run.y;
         // the last chunk that begins with this id: 256 chunks looked at per round
-        int end = c0 + 1;
+        int64_t end = (int64_t)c0 + 1;
         for (;;) {
-            const int64_t at = (int64_t)end + 1 + threadIdx.x;
-            const bool more = at * L < p.n && p.keys[at * L] == key;
-            const int got = __syncthreads_count(more);
+            const int64_t at = end + 1 + threadIdx.x;
+            const int got = __syncthreads_count(at < p.chunks && p.pairs[at * L].x == key);
             end += got;
             if (got < JOIN_THREADS) break;
         }
+        // partial sum j of the id: slot 1 of chunk c0, then slot 0 of the following ones; eight of a thread's on their way into shared
+        // memory at a time (with registers as their target they came one by one, 4.5 us a round of eight)
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (col < p.part_ld) {
-            // partial sum j of the id: slot 1 of chunk c0, then slot 0 of the following ones
-            for (int j0 = stripe; j0 <= end - c0; j0 += 4 * STRIPES) {
-                float4 v[4];
+        const int64_t parts = end - c0 + 1;
+        for (int64_t j0 = stripe; j0 < parts && col < p.part_ld; j0 += U * STRIPES) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int j = j0 + u * STRIPES;
-                    v[u] = j <= end - c0 ? *reinterpret_cast<const float4*>(p.part + ((int64_t)(c0 + j) * 2 + (j == 0)) * p.part_ld + col) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u) { a.x += v[u].x; a.y += v[u].y; a.z += v[u].z; a.w += v[u].w; }
+            for (int u = 0; u < U; ++u) {
+                const int64_t j = j0 + u * STRIPES;
+                if (j < parts)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&ring[u][threadIdx.x])),
+                                 "l"(p.part + ((c0 + j) * 2 + (j == 0)) * p.part_ld + col) : "memory");
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (j0 + u * STRIPES < parts) { const float4 v = ring[u][threadIdx.x]; a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
         }
+        red[stripe][lane] = a;
         __syncthreads();
-        red[stripe][lane8] = a;
-        __syncthreads();
-        if (threadIdx.x < 32) {
-            const int cc = blockIdx.y * 32 + threadIdx.x;
+        if (threadIdx.x < JOIN_COLS) {
+            const int cc = blockIdx.y * JOIN_COLS + threadIdx.x;
             if (cc < p.dim) {
                 float sum = 0.f;
 #pragma unroll
@@ -677,9 +737,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
     }
 }
 
-// Calls f with the pack length as a constant (eight: only where a side is a 16-bit type).
-template <typename TG, typename TO, class F> int with_vector(int vec, F&& f) {
-    if constexpr (sizeof(TG) == 2 || sizeof(TO) == 2) { if (vec == 8) return f(std::integral_constant<int, 8>()); }
+// Calls f with the pack length as a constant.
+template <bool EIGHT, class F> int with_vector(int vec, F&& f) {
+    if constexpr (EIGHT) { if (vec == 8) return f(std::integral_constant<int, 8>()); }
     if (vec == 4) return f(std::integral_constant<int, 4>());
     if (vec == 2) return f(std::integral_constant<int, 2>());
     return f(std::integral_constant<int, 1>());
@@ -692,7 +752,7 @@ int launch_lookup(LookupParams& p, int tt, int to, int vec, int dim, cudaStream_
     return with_type(tt, [&](auto a) {
         return with_type(to, [&](auto b) {
             using TT = decltype(a); using TO = decltype(b);
-            return with_vector<TT, TO>(vec, [&](auto v) {
+            return with_vector<sizeof(TT) == 2 || sizeof(TO) == 2>(vec, [&](auto v) {
                 lookup_kernel<TT, TO, decltype(v)::value><<<grid, LOOKUP_THREADS, 0, s>>>(p);
                 return launch_status(cudaGetLastError());
             });
@@ -707,7 +767,7 @@ int launch_small(SumParams& p, int vec, cudaStream_t s) {
     int64_t per = ceil_div(p.rows, 148 * 4);
     per = std::max<int64_t>(1, std::min<int64_t>({per, (1ll << 22) - 1, ((1ll << 31) - 1) / p.vecs.d}));
     p.rows_per_cta = (int)per;
-    return with_vector<TG, TO>(vec, [&](auto v) {
+    return with_vector<sizeof(TG) == 2>(vec, [&](auto v) {
         grad_small_kernel<TG, TO, decltype(v)::value><<<(unsigned)ceil_div(p.rows, per), SMALL_THREADS, 0, s>>>(p);
         return launch_status(cudaGetLastError());
     });
@@ -717,17 +777,15 @@ template <typename TG, typename TO, int L>
 int launch_sum(SumParams& p, int vec, cudaStream_t s) {
     p.vecs = FastDiv((uint32_t)(p.dim / vec));
     const dim3 grid((unsigned)ceil_div((int64_t)p.chunks * p.vecs.d, SUM_THREADS));
-    const int rc = with_vector<TG, TO>(vec, [&](auto v) {
-        grad_sum_kernel<TG, TO, decltype(v)::value, L><<<grid, SUM_THREADS, 0, s>>>(p);
-        return launch_status(cudaGetLastError());
+    const int rc = with_vector<sizeof(TG) == 2>(vec, [&](auto v) {
+        return launch_status(launch_dependent(grad_sum_kernel<TG, TO, decltype(v)::value, L>, grid, dim3(SUM_THREADS), 0, s, p));
     });
     if (rc != KGE_OK || p.chunks < 3) return rc;
-    const dim3 joins((unsigned)std::min<int64_t>(p.chunks / 2, 592), (unsigned)ceil_div(p.dim, 32));
-    grad_join_kernel<TO, L><<<joins, JOIN_THREADS, 0, s>>>(p);
-    return launch_status(cudaGetLastError());
+    const dim3 joins((unsigned)std::min<int64_t>(p.chunks / 2, 592), (unsigned)ceil_div(p.dim, JOIN_COLS));
+    return launch_status(launch_dependent(grad_join_kernel<TO, L>, joins, dim3(JOIN_THREADS), 0, s, p));
 }
 
-// Keys and positions in the order of the ids, in g.keys / g.pos of the returned index; the rows of a dense gradient set to zero.
+// The (id, position) pairs in order, in g.pairs[*where]; the rows of a dense gradient set to zero.
 int sort_ids(const GradScratch& g, const SortPlan& plan, SortParams& q, bool zero, int64_t rows, int* where, cudaStream_t s) {
     const int digits = 1 << plan.bits;
     if (q.n <= CS_MAX) {
@@ -736,7 +794,7 @@ int sort_ids(const GradScratch& g, const SortPlan& plan, SortParams& q, bool zer
             return cudaFuncSetAttribute(grad_cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cluster_sort_smem(CS_MAX, CS_MAX_BITS));
         });
         if (e != cudaSuccess) return KGE_ERR_CUDA;
-        q.keys_out = g.keys[0]; q.pos_out = g.pos[0];
+        q.pairs_out = g.pairs[0];
         q.zero_first = 0; q.zero_last = rows;
         *where = 0;
         const int zero_clusters = zero ? (int)std::min<int64_t>(16, ceil_div(rows * q.zero_row_bytes, 64 * 1024)) : 0;
@@ -750,28 +808,22 @@ int sort_ids(const GradScratch& g, const SortPlan& plan, SortParams& q, bool zer
         return launch_status(cudaLaunchKernelEx(&cfg, grad_cluster_sort_kernel, q));
     }
     // the zeroing is shared out over the launches: the sort leaves most of the memory's bandwidth unused
-    const int launches = 1 + plan.passes;
-    int nth = 0;
+    const int launches = 2 * plan.passes;
+    int nth = 0, rc = KGE_OK;
     auto zero_ctas = [&] {
         q.zero_first = rows * nth / launches; q.zero_last = rows * (nth + 1) / launches;
         ++nth;
         return zero ? (int)std::min<int64_t>(148 * 6, ceil_div((q.zero_last - q.zero_first) * q.zero_row_bytes, 16 * GS_THREADS)) : 0;
     };
-    int beside = zero_ctas();
-    grad_hist_kernel<<<plan.tiles + beside, GS_THREADS, 0, s>>>(q);
-    int rc = launch_status(cudaGetLastError());
     for (int pass = 0; pass < plan.passes && rc == KGE_OK; ++pass) {
         q.pass = pass; q.shift = pass * plan.bits;
-        q.keys_in = g.keys[(pass + 1) & 1]; q.pos_in = g.pos[(pass + 1) & 1];
-        q.keys_out = g.keys[pass & 1]; q.pos_out = g.pos[pass & 1];
-        q.hist = g.hist + (int64_t)pass * plan.tiles * digits;
-        q.hist_next = pass + 1 < plan.passes ? q.hist + (int64_t)plan.tiles * digits : nullptr;
-        grad_scan_kernel<<<(digits * 32 + 255) / 256, 256, 0, s>>>(q);
-        rc = launch_status(cudaGetLastError());
-        if (rc != KGE_OK) break;
-        beside = zero_ctas();
-        grad_scatter_kernel<<<plan.tiles + beside, GS_THREADS, 0, s>>>(q);
-        rc = launch_status(cudaGetLastError());
+        q.pairs_in = g.pairs[(pass + 1) & 1];
+        q.pairs_out = g.pairs[pass & 1];
+        int ctas = plan.tiles + zero_ctas();
+        rc = launch_status(launch_dependent(grad_hist_kernel, dim3((unsigned)ctas), dim3(GS_THREADS), 0, s, q));
+        if (rc == KGE_OK) rc = launch_status(launch_dependent(grad_scan_kernel, dim3((unsigned)((digits * 32 + 255) / 256)), dim3(256), 0, s, q));
+        ctas = plan.tiles + zero_ctas();
+        if (rc == KGE_OK) rc = launch_status(launch_dependent(grad_scatter_kernel, dim3((unsigned)ctas), dim3(GS_THREADS), 0, s, q));
     }
     *where = (plan.passes - 1) & 1;
     return rc;
@@ -819,7 +871,7 @@ int kge_embedding_grad(const int32_t* ids, int32_t n, const void* grads, int32_t
     }
     const size_t need = kge_embedding_grad_scratch_bytes(rows, dim, n);
     if (need > 0 && (!scratch || !aligned_to(scratch, 256) || scratch_bytes < need)) return KGE_ERR_WORKSPACE;
-    const int vec = vector_length(gb == 2 || tb == 2 ? 8 : 4, dim, ld_grads, gb, grads, ld_table, tb, table_grad);
+    const int vec = vector_length(gb == 2 ? 8 : 4, dim, ld_grads, gb, grads, ld_table, tb, table_grad);
     SumParams p{};
     p.n = n; p.dim = dim; p.part_ld = (dim + 3) / 4 * 4; p.rows = (uint32_t)rows;
     p.grads = grads; p.ld_grads = ld_grads; p.out = table_grad; p.ld_out = ld_table; p.scale = scale; p.accumulate = accumulate;
@@ -836,7 +888,7 @@ int kge_embedding_grad(const int32_t* ids, int32_t n, const void* grads, int32_t
     int where = 0;
     const int rc = sort_ids(g, plan, q, !accumulate, rows, &where, s);
     if (rc != KGE_OK) return rc;
-    p.keys = g.keys[where]; p.pos = g.pos[where];
+    p.pairs = g.pairs[where];
     p.chunks = (int)ceil_div(n, chunk_rows(n));
     p.part = g.part; p.list = g.list; p.list_count = g.list_count;
     return with_type(grads_type, [&](auto a) {
