@@ -5,7 +5,7 @@
 // rows of one id in fp32 in ascending position, and joins the ids that span chunks in a second, fixed order: the result is a
 // function of the inputs alone.  Rows of the dense gradient that no id names are set to zero by CTAs beside the sort's.
 //   up to 1,024 ids     one launch: every CTA owns a range of table rows, picks the ids that fall into it and sorts those
-//   up to 65,536        one cluster of eight CTAs sorts in shared memory, exchanging counts and pairs between its CTAs
+//   up to 65,536        one cluster of sixteen CTAs sorts in shared memory, exchanging counts and pairs between its CTAs
 //   more                hist     digit counts of every tile, per pass (counted by atomics while the pass before scatters, frequent ids cost 12 us of 24)
 //                       scan     the counts become sums over the tiles before
 //                       scatter  one stable split by a digit
@@ -82,8 +82,8 @@ __global__ void __launch_bounds__(LOOKUP_THREADS) lookup_kernel(LookupParams p) 
 constexpr int GS_THREADS = 256, GS_WARPS = GS_THREADS / 32, GS_ITEMS = 8;
 constexpr int GS_TILE = GS_THREADS * GS_ITEMS;     // ids per CTA of the sort in global memory
 constexpr int GS_MAX_BITS = 9;
-constexpr int CS_CTAS = 8, CS_THREADS = 512, CS_WARPS = CS_THREADS / 32, CS_ITEMS = 16;      // the cluster's sort
-constexpr int CS_SHARE = CS_THREADS * CS_ITEMS, CS_MAX = CS_CTAS * CS_SHARE, CS_MAX_BITS = 11;
+constexpr int CS_CTAS = 16, CS_CTAS_PORTABLE = 8, CS_THREADS = 512, CS_WARPS = CS_THREADS / 32, CS_ITEMS = 16;      // the cluster's sort
+constexpr int CS_SHARE = CS_THREADS * CS_ITEMS, CS_MAX = CS_CTAS_PORTABLE * CS_SHARE, CS_MAX_BITS = 11;
 constexpr int SMALL_MAX = 1024, SMALL_THREADS = 256;
 constexpr int SUM_THREADS = 256;
 constexpr int JOIN_THREADS = 256;
@@ -314,21 +314,22 @@ __device__ __forceinline__ uint32_t cs_map(uint32_t addr, uint32_t rank) { uint3
 __device__ __forceinline__ uint32_t cs_load(uint32_t addr) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory"); return v; }
 __device__ __forceinline__ void cs_store2(uint32_t addr, uint32_t a, uint32_t b) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory"); }
 
-size_t cluster_sort_smem(int n, int bits) {       // pairs twice, warps' counts, digits' counts and bases
-    return (size_t)ceil_div(n, CS_CTAS) * 16 + ((size_t)CS_WARPS * 2 + 8) * ((size_t)1 << bits) + 128;
+size_t cluster_sort_smem(int n, int bits, int ctas) {       // pairs twice, warps' counts, digits' counts and bases
+    return (size_t)ceil_div(n, ctas) * 16 + ((size_t)CS_WARPS * 2 + 8) * ((size_t)1 << bits) + 128;
 }
 
 // Cluster 0 sorts: each of its CTAs holds a share of the list, a warp a contiguous piece of that.  Per pass a warp ranks its elements
 // among its own (as in grad_scatter_kernel), the CTAs read each other's digit counts, and every pair is stored into the CTA that
 // holds its new place; the last pass stores to global memory.  The other clusters set rows to zero.
+template <int CTAS>
 __global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortParams p) {
     extern __shared__ __align__(16) unsigned char cs_smem[];
     grid_dependency_wait();
     allow_dependents();
-    if (blockIdx.x >= CS_CTAS) { zero_rows(p, blockIdx.x - CS_CTAS, gridDim.x - CS_CTAS); return; }
+    if (blockIdx.x >= CTAS) { zero_rows(p, blockIdx.x - CTAS, gridDim.x - CTAS); return; }
     __shared__ uint32_t warp_tot[CS_WARPS];
     const int digits = 1 << p.bits, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int share = (p.n + CS_CTAS - 1) / CS_CTAS, rank = blockIdx.x;
+    const int share = (p.n + CTAS - 1) / CTAS, rank = blockIdx.x;
     const int have = max(0, min(share, p.n - rank * share));                        // of this CTA
     const int per_warp = ((share + CS_WARPS - 1) / CS_WARPS + 31) / 32 * 32;        // at most 32 CS_ITEMS
     uint2* const pairs[2] = {reinterpret_cast<uint2*>(cs_smem), reinterpret_cast<uint2*>(cs_smem) + share};
@@ -389,10 +390,15 @@ __global__ void __launch_bounds__(CS_THREADS, 1) grad_cluster_sort_kernel(SortPa
         if (d0 < digits) {
             const uint32_t from = smem_u32(count + d0);
 #pragma unroll
-            for (int r = 0; r < CS_CTAS; ++r) {
-                const uint32_t there = cs_map(from, r);
+            for (int j = 0; j < PER; ++j) {
+                if (j >= per) break;
+                uint32_t c[CTAS];                       // (all of them under way together)
 #pragma unroll
-                for (int j = 0; j < PER; ++j) if (j < per) { const uint32_t c = cs_load(there + 4 * j); tot[j] += c; if (r < rank) mine[j] += c; }
+                for (int r = 0; r < CTAS; ++r) c[r] = cs_load(cs_map(from + 4 * j, r));
+#pragma unroll
+                for (int r = 0; r < CTAS; ++r) asm volatile("" ::"r"(c[r]));
+#pragma unroll
+                for (int r = 0; r < CTAS; ++r) { tot[j] += c[r]; if (r < rank) mine[j] += c[r]; }
             }
         }
 #pragma unroll
@@ -785,27 +791,57 @@ int launch_sum(SumParams& p, int vec, cudaStream_t s) {
     return launch_status(launch_dependent(grad_join_kernel<TO, L>, joins, dim3(JOIN_THREADS), 0, s, p));
 }
 
-// The (id, position) pairs in order, in g.pairs[*where]; the rows of a dense gradient set to zero.
-int sort_ids(const GradScratch& g, const SortPlan& plan, SortParams& q, bool zero, int64_t rows, int* where, cudaStream_t s) {
-    const int digits = 1 << plan.bits;
-    if (q.n <= CS_MAX) {
-        static DeviceOnce configured;
-        const cudaError_t e = once_per_device(configured, [] {
-            return cudaFuncSetAttribute(grad_cluster_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cluster_sort_smem(CS_MAX, CS_MAX_BITS));
-        });
-        if (e != cudaSuccess) return KGE_ERR_CUDA;
-        q.pairs_out = g.pairs[0];
-        q.zero_first = 0; q.zero_last = rows;
-        *where = 0;
-        const int zero_clusters = zero ? (int)std::min<int64_t>(16, ceil_div(rows * q.zero_row_bytes, 64 * 1024)) : 0;
+// Clusters of sixteen CTAs are no promise of the architecture: asked for once per device.
+int wide_clusters(bool* wide) {
+    static std::atomic<int> known[kMaxDevices];        // 1: no, 2: yes
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KGE_ERR_CUDA;
+    const bool tracked = dev >= 0 && dev < kMaxDevices;
+    int state = tracked ? known[dev].load(std::memory_order_acquire) : 0;
+    if (state == 0) {
+        const int most = (int)cluster_sort_smem(CS_MAX, CS_MAX_BITS, CS_CTAS), most8 = (int)cluster_sort_smem(CS_MAX, CS_MAX_BITS, CS_CTAS_PORTABLE);
+        if (cudaFuncSetAttribute(grad_cluster_sort_kernel<CS_CTAS_PORTABLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, most8) != cudaSuccess ||
+            cudaFuncSetAttribute(grad_cluster_sort_kernel<CS_CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess ||
+            cudaFuncSetAttribute(grad_cluster_sort_kernel<CS_CTAS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return KGE_ERR_CUDA;
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)(CS_CTAS * (1 + zero_clusters))); cfg.blockDim = dim3(CS_THREADS); cfg.stream = s;
-        cfg.dynamicSmemBytes = cluster_sort_smem(q.n, plan.bits);
+        cfg.gridDim = dim3(CS_CTAS); cfg.blockDim = dim3(CS_THREADS); cfg.dynamicSmemBytes = (size_t)most;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = CS_CTAS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = 1;
-        return launch_status(cudaLaunchKernelEx(&cfg, grad_cluster_sort_kernel, q));
+        int fit = 0;
+        if (cudaOccupancyMaxActiveClusters(&fit, grad_cluster_sort_kernel<CS_CTAS>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); fit = 0; }
+        state = fit > 0 ? 2 : 1;
+        if (tracked) known[dev].store(state, std::memory_order_release);
+    }
+    *wide = state == 2;
+    return KGE_OK;
+}
+
+template <int CTAS>
+int launch_cluster_sort(SortParams& q, const SortPlan& plan, bool zero, int64_t rows, cudaStream_t s) {
+    const int zero_clusters = zero ? (int)std::min<int64_t>(128 / CTAS, ceil_div(rows * q.zero_row_bytes, 8192 * CTAS)) : 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(CTAS * (1 + zero_clusters))); cfg.blockDim = dim3(CS_THREADS); cfg.stream = s;
+    cfg.dynamicSmemBytes = cluster_sort_smem(q.n, plan.bits, CTAS);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CTAS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    return launch_status(cudaLaunchKernelEx(&cfg, grad_cluster_sort_kernel<CTAS>, q));
+}
+
+// The (id, position) pairs in order, in g.pairs[*where]; the rows of a dense gradient set to zero.
+int sort_ids(const GradScratch& g, const SortPlan& plan, SortParams& q, bool zero, int64_t rows, int* where, cudaStream_t s) {
+    const int digits = 1 << plan.bits;
+    if (q.n <= CS_MAX) {
+        q.pairs_out = g.pairs[0];
+        q.zero_first = 0; q.zero_last = rows;
+        *where = 0;
+        bool wide = false;
+        int rc = wide_clusters(&wide);
+        if (rc != KGE_OK) return rc;
+        return wide ? launch_cluster_sort<CS_CTAS>(q, plan, zero, rows, s) : launch_cluster_sort<CS_CTAS_PORTABLE>(q, plan, zero, rows, s);
     }
     // the zeroing is shared out over the launches: the sort leaves most of the memory's bandwidth unused
     const int launches = 2 * plan.passes;
