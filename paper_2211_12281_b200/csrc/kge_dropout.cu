@@ -18,44 +18,73 @@ struct DropoutParams {
     int64_t n;
     uint32_t cut, site;
     float scale;
-    uint64_t seed, step;
+    uint32_t key[20];             // the generator's round keys: k0 + r w0, k1 + r w1
+    uint64_t step;
     const int64_t* step_dev;      // added to step, or NULL
     int vec;                      // all arrays start at multiples of 16 bytes
 };
 
+// Philox4x32 with 10 rounds; the round keys come with the launch, and 32 x 32 -> 64-bit products are one instruction each.
+__device__ __forceinline__ Philox4 dropout_words(const DropoutParams& p, uint32_t group, uint64_t step) {
+    uint32_t c0 = group, c1 = (uint32_t)step, c2 = (uint32_t)(step >> 32), c3 = p.site;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ p.key[2 * r]; c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ p.key[2 * r + 1]; c3 = (uint32_t)a;
+    }
+    return Philox4{c0, c1, c2, c3};
+}
+
+// Two groups of eight elements a thread, 256 groups apart: their loads are under way while the generator runs.
+constexpr int DROPOUT_GROUPS = 2;
 template <typename TX, typename TO, bool RES>
-__global__ void __launch_bounds__(256) dropout_kernel(DropoutParams p) {
-    const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x, i0 = g * 8;
-    if (i0 >= p.n) return;
+__global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropoutParams p) {
+    const TX* x = static_cast<const TX*>(p.x);
+    const TO* res = static_cast<const TO*>(p.residual);
+    TO* out = static_cast<TO*>(p.out);
+    const int64_t g0 = (int64_t)blockIdx.x * (256 * DROPOUT_GROUPS) + threadIdx.x;
+    Pack<TX, 8> a[DROPOUT_GROUPS];
+    Pack<TO, 8> r[DROPOUT_GROUPS];
+    if (p.vec && (g0 + 256 * (DROPOUT_GROUPS - 1)) * 8 + 8 <= p.n) {
+#pragma unroll
+        for (int u = 0; u < DROPOUT_GROUPS; ++u) {
+            a[u] = load_stream<Pack<TX, 8>>(x + (g0 + 256 * u) * 8);
+            if (RES) r[u] = load_stream<Pack<TO, 8>>(res + (g0 + 256 * u) * 8);
+        }
+        const uint64_t step = p.step + (p.step_dev ? (uint64_t)*p.step_dev : 0ull);
+#pragma unroll
+        for (int u = 0; u < DROPOUT_GROUPS; ++u) {
+            const Philox4 w = dropout_words(p, (uint32_t)(g0 + 256 * u), step);
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+            Pack<TO, 8> o;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool keep = (i & 1 ? words[i >> 1] >> 16 : words[i >> 1] & 0xFFFFu) >= p.cut;
+                const float v = keep ? to_float(a[u].v[i]) : 0.f;          // a dropped infinity or NaN leaves nothing: selected, not multiplied
+                o.v[i] = from_float<TO>(RES ? fmaf(v, p.scale, to_float(r[u].v[i])) : v * p.scale);
+            }
+            *reinterpret_cast<Pack<TO, 8>*>(out + (g0 + 256 * u) * 8) = o;
+        }
+        return;
+    }
+    // the end of the list, and arrays that start between multiples of 16 bytes
     const uint64_t step = p.step + (p.step_dev ? (uint64_t)*p.step_dev : 0ull);
-    const TX* x = static_cast<const TX*>(p.x) + i0;
-    const TO* res = static_cast<const TO*>(p.residual) + (RES ? i0 : 0);
-    TO* out = static_cast<TO*>(p.out) + i0;
-    const int m = (int)min((int64_t)8, p.n - i0);
-    Pack<TX, 8> a;
-    Pack<TO, 8> r;
-    const bool whole = p.vec && m == 8;
-    if (whole) {
-        a = *reinterpret_cast<const Pack<TX, 8>*>(x);
-        if (RES) r = *reinterpret_cast<const Pack<TO, 8>*>(res);
-    } else {
+#pragma unroll 1
+    for (int u = 0; u < DROPOUT_GROUPS; ++u) {
+        const int64_t g = g0 + 256 * u;
+        const int m = (int)max((int64_t)0, min((int64_t)8, p.n - g * 8));
+        if (m == 0) return;
+        const Philox4 w = dropout_words(p, (uint32_t)g, step);
+        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < m) { a.v[i] = x[i]; if (RES) r.v[i] = res[i]; }
-    }
-    const Philox4 w = philox4x32_10((uint32_t)g, (uint32_t)step, (uint32_t)(step >> 32), p.site, (uint32_t)p.seed, (uint32_t)(p.seed >> 32));
-    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
-    Pack<TO, 8> o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t h = i & 1 ? words[i >> 1] >> 16 : words[i >> 1] & 0xFFFFu;
-        const bool keep = h >= p.cut;          // a dropped infinity or NaN leaves nothing: selected, not multiplied
-        const float v = keep ? to_float(a.v[i]) : 0.f;
-        o.v[i] = from_float<TO>(RES ? fmaf(v, p.scale, to_float(r.v[i])) : v * p.scale);
-    }
-    if (whole) *reinterpret_cast<Pack<TO, 8>*>(out) = o;
-    else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (i < m) out[i] = o.v[i];
+        for (int i = 0; i < 8; ++i)
+            if (i < m) {
+                const int64_t at = g * 8 + i;
+                const bool keep = (i & 1 ? words[i >> 1] >> 16 : words[i >> 1] & 0xFFFFu) >= p.cut;
+                const float v = keep ? to_float(x[at]) : 0.f;
+                out[at] = from_float<TO>(RES ? fmaf(v, p.scale, to_float(res[at])) : v * p.scale);
+            }
     }
 }
 
@@ -74,10 +103,11 @@ extern "C" int kge_dropout(const void* x, int32_t x_type, const void* residual, 
     q.x = x; q.residual = residual; q.out = out; q.n = n;
     q.cut = (uint32_t)std::nearbyint(p * 65536.0);
     q.scale = q.cut < 65536u ? (float)(65536.0 / (65536.0 - q.cut)) : 0.f;
-    q.seed = seed; q.step = step; q.step_dev = step_dev; q.site = 0x80000000u | (uint32_t)site;
+    for (uint32_t r = 0; r < 10; ++r) { q.key[2 * r] = (uint32_t)seed + r * 0x9E3779B9u; q.key[2 * r + 1] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u; }
+    q.step = step; q.step_dev = step_dev; q.site = 0x80000000u | (uint32_t)site;
     q.vec = aligned_to(x, 16) && aligned_to(out, 16) && (!residual || aligned_to(residual, 16));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const dim3 grid((unsigned)ceil_div(n, 8 * 256));
+    const dim3 grid((unsigned)ceil_div(n, 8 * 256 * DROPOUT_GROUPS));
     return with_type(x_type, [&](auto tx) {
         return with_type(out_type, [&](auto to) {
             using TX = decltype(tx); using TO = decltype(to);

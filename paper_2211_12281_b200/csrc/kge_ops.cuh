@@ -74,6 +74,15 @@ template <typename P> __device__ __forceinline__ P load_now(const void* p) {
     return r;
 }
 
+// A pack that is read once, in 16-byte pieces past the L1 cache (it may be overwritten in place by its own thread afterwards).
+template <typename P> __device__ __forceinline__ P load_stream(const void* p) {
+    P r;
+    uint4* w = reinterpret_cast<uint4*>(&r);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(P) / 16; ++i) w[i] = __ldcs(static_cast<const uint4*>(p) + i);
+    return r;
+}
+
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
