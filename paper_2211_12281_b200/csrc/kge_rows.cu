@@ -623,29 +623,36 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
     const int64_t col = (item - c * vecs) * V;
     const int64_t first = (int64_t)c * L, last = min((int64_t)p.n, first + L);        // [first, last): this chunk
     const TG* grads = static_cast<const TG*>(p.grads) + col;
+    const uint2* const pairs = p.pairs + first;               // (indices below count from here)
+    const int size = (int)(last - first), room = (int)min((int64_t)p.n - first, (int64_t)2 * L);
     const uint32_t none = p.rows, beyond = ~0u;
-    const uint32_t lead = p.pairs[first].x, end_key = p.pairs[last - 1].x;
-    const uint32_t before = c > 0 ? p.pairs[first - 1].x : beyond, early = first - L - 1 >= 0 ? p.pairs[first - L - 1].x : beyond;
-    const uint32_t after = last < p.n ? p.pairs[last].x : beyond, far = first + 2 * L < p.n ? p.pairs[first + 2 * L].x : beyond;
+    const uint32_t lead = pairs[0].x, end_key = pairs[size - 1].x;
+    const uint32_t before = c > 0 ? pairs[-1].x : beyond, early = c > 1 ? pairs[-L - 1].x : beyond;
+    const uint32_t after = size < room ? pairs[size].x : beyond, far = first + 2 * L < p.n ? pairs[2 * L].x : beyond;
     if (lead == none) return;                                   // only ids of no row from here on
     // a first run that began in the chunk before is that chunk's, unless it reaches across a whole chunk: then a partial sum
     const bool head_part = before == lead && (early == lead || after == lead), skip = before == lead && !head_part;
     // a run that goes on beyond this chunk is taken along if it ends within the next one, else a partial sum
     const bool on = end_key != none && after == end_key && !(head_part && end_key == lead);
     const bool tail_part = on && far == end_key;
-    const int64_t stop = on && !tail_part ? min((int64_t)p.n, first + 2 * L) : last;       // one past the last row that may be this thread's
-    const uint32_t place = smem_u32(ring) + threadIdx.x * BYTES;
-    // the row at sorted position r, or `beyond`: rows past the last run, skipped ones, ids of no row
-    auto key_at = [&](int64_t r) {
-        if (r >= stop) return beyond;
-        const uint32_t k = p.pairs[r].x;
-        return (r >= last && k != end_key) || (skip && k == lead) || k == none ? beyond : k;
+    // this thread's rows: [from, to), without a skipped run at the front and ids of no row at the end
+    auto bound = [&](int lo, int hi, uint32_t key, bool above) {       // first index whose key is not below (above: greater than) `key`
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            const uint32_t k = pairs[mid].x;
+            if (above ? k <= key : k < key) lo = mid + 1; else hi = mid;
+        }
+        return lo;
     };
-    auto issue = [&](int64_t r, int slot) {
+    const int from = skip ? bound(0, size, lead, true) : 0;
+    const int to = end_key == none ? bound(from, size, none, false) : (on && !tail_part ? bound(size, room, end_key, true) : size);
+    if (from >= to) return;
+    const uint32_t place = smem_u32(ring) + threadIdx.x * BYTES;
+    auto issue = [&](int i) {
         if constexpr (ASYNC) {
-            if (key_at(r) != beyond) {
-                const TG* src = grads + (int64_t)p.pairs[r].y * p.ld_grads;
-                const uint32_t dst = place + slot * (SUM_THREADS * BYTES);
+            if (i < to) {
+                const TG* src = grads + (int64_t)pairs[i].y * p.ld_grads;
+                const uint32_t dst = place + (i % SUM_DEPTH) * (SUM_THREADS * BYTES);
                 if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
                 else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
             }
@@ -653,37 +660,34 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
         }
     };
 #pragma unroll
-    for (int u = 0; u < SUM_DEPTH - 1; ++u) issue(first + u, u);
+    for (int u = 0; u < SUM_DEPTH - 1; ++u) issue(from + u);
     float a[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) a[e] = 0.f;
-    uint32_t cur = beyond;                                      // (no run yet)
+    uint32_t cur = pairs[from].x;
     bool is_head = head_part;
-    int slot = 0;
 #pragma unroll 1
-    for (int64_t r = first; r < stop; ++r) {
-        issue(r + SUM_DEPTH - 1, slot == 0 ? SUM_DEPTH - 1 : slot - 1);
-        const uint32_t k = key_at(r);
-        if (k != beyond) {
-            if (k != cur) {
-                if (cur != beyond) { flush_run<TO, V>(p, c, is_head, false, cur, col, a); is_head = false; }
-                cur = k;
+    for (int i = from; i < to; ++i) {
+        issue(i + SUM_DEPTH - 1);
+        const uint32_t k = pairs[i].x;
+        if (k != cur) {
+            flush_run<TO, V>(p, c, is_head, false, cur, col, a);
+            is_head = false;
+            cur = k;
 #pragma unroll
-                for (int e = 0; e < V; ++e) a[e] = 0.f;
-            }
-            Pack<TG, V> g;
-            if constexpr (ASYNC) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(SUM_DEPTH - 1) : "memory");
-                g = *reinterpret_cast<const Pack<TG, V>*>(ring + (size_t)slot * (SUM_THREADS * BYTES) + threadIdx.x * BYTES);
-            } else {
-                g = *reinterpret_cast<const Pack<TG, V>*>(grads + (int64_t)p.pairs[r].y * p.ld_grads);
-            }
-#pragma unroll
-            for (int e = 0; e < V; ++e) a[e] += to_float(g.v[e]);
+            for (int e = 0; e < V; ++e) a[e] = 0.f;
         }
-        slot = slot + 1 == SUM_DEPTH ? 0 : slot + 1;
+        Pack<TG, V> g;
+        if constexpr (ASYNC) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(SUM_DEPTH - 1) : "memory");
+            g = *reinterpret_cast<const Pack<TG, V>*>(ring + (i % SUM_DEPTH) * (SUM_THREADS * BYTES) + threadIdx.x * BYTES);
+        } else {
+            g = *reinterpret_cast<const Pack<TG, V>*>(grads + (int64_t)pairs[i].y * p.ld_grads);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) a[e] += to_float(g.v[e]);
     }
-    if (cur != beyond) flush_run<TO, V>(p, c, is_head, tail_part && cur == end_key, cur, col, a);
+    flush_run<TO, V>(p, c, is_head, tail_part && cur == end_key, cur, col, a);
 }
 
 // Ids that span more than two chunks: CTA (x, y) takes the x-th, (x + grid)-th, ... of the list and 64 columns.  Sixteen stripes
