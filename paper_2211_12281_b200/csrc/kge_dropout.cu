@@ -40,6 +40,8 @@ __device__ __forceinline__ Philox4 dropout_words(const DropoutParams& p, uint32_
 constexpr int DROPOUT_GROUPS = 2;
 template <typename TX, typename TO, bool RES>
 __global__ void __launch_bounds__(256) dropout_kernel(const __grid_constant__ DropoutParams p) {
+    grid_dependency_wait();
+    allow_dependents();
     const TX* x = static_cast<const TX*>(p.x);
     const TO* res = static_cast<const TO*>(p.residual);
     TO* out = static_cast<TO*>(p.out);
@@ -111,9 +113,8 @@ extern "C" int kge_dropout(const void* x, int32_t x_type, const void* residual, 
     return with_type(x_type, [&](auto tx) {
         return with_type(out_type, [&](auto to) {
             using TX = decltype(tx); using TO = decltype(to);
-            if (residual) dropout_kernel<TX, TO, true><<<grid, 256, 0, s>>>(q);
-            else dropout_kernel<TX, TO, false><<<grid, 256, 0, s>>>(q);
-            return launch_status(cudaGetLastError());
+            return launch_status(residual ? launch_dependent(dropout_kernel<TX, TO, true>, grid, dim3(256), 0, s, q)
+                                          : launch_dependent(dropout_kernel<TX, TO, false>, grid, dim3(256), 0, s, q));
         });
     });
 }

@@ -187,6 +187,8 @@ __global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 3 : 2) quantize_kernel(
     __shared__ uint32_t part[16][128];
     __shared__ Block col_block[128];
     __shared__ alignas(16) uint2 turned[128][16];
+    grid_dependency_wait();
+    allow_dependents();
     const int tid = threadIdx.x, cg = tid & 15, rg = tid >> 4;
     const int64_t tr = blockIdx.x / p.tiles_c, tc = blockIdx.x - tr * p.tiles_c;
     const int64_t r0 = tr * 128 + rg * 8, c0 = tc * 128 + cg * 8;
@@ -280,6 +282,8 @@ __global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 3 : 2) quantize_kernel(
 template <typename TX, int FMT, bool POW2>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantParams p) {
     constexpr int STEP = sizeof(TX) == 2 ? 4 : 2, ROWS = 32, STEPS = ROWS / (2 * STEP);
+    grid_dependency_wait();
+    allow_dependents();
     const int lane = threadIdx.x & 31, cg = lane & 15;
     const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int64_t tr = unit / p.tiles_c, tc = unit - tr * p.tiles_c;
@@ -320,22 +324,17 @@ int launch_quantize(const QuantParams& p, int fmt, bool square, cudaStream_t s) 
         constexpr bool P = decltype(pow2)::value;
         if (!square && !p.qt) {
             const dim3 grid((unsigned)ceil_div(p.tiles_c * ceil_div(p.rows, 32), 8));
-            if (fmt == KGE_E4M3) quantize_rows_kernel<TX, KGE_E4M3, P><<<grid, 256, 0, s>>>(p);
-            else quantize_rows_kernel<TX, KGE_E5M2, P><<<grid, 256, 0, s>>>(p);
-            return;
+            return fmt == KGE_E4M3 ? launch_dependent(quantize_rows_kernel<TX, KGE_E4M3, P>, grid, dim3(256), 0, s, p)
+                                   : launch_dependent(quantize_rows_kernel<TX, KGE_E5M2, P>, grid, dim3(256), 0, s, p);
         }
         const dim3 grid((unsigned)(p.tiles_c * ceil_div(p.rows, 128)));
-        if (fmt == KGE_E4M3) {
-            if (square) quantize_kernel<TX, KGE_E4M3, true, P><<<grid, 256, 0, s>>>(p);
-            else quantize_kernel<TX, KGE_E4M3, false, P><<<grid, 256, 0, s>>>(p);
-        } else {
-            if (square) quantize_kernel<TX, KGE_E5M2, true, P><<<grid, 256, 0, s>>>(p);
-            else quantize_kernel<TX, KGE_E5M2, false, P><<<grid, 256, 0, s>>>(p);
-        }
+        if (square)
+            return fmt == KGE_E4M3 ? launch_dependent(quantize_kernel<TX, KGE_E4M3, true, P>, grid, dim3(256), 0, s, p)
+                                   : launch_dependent(quantize_kernel<TX, KGE_E5M2, true, P>, grid, dim3(256), 0, s, p);
+        return fmt == KGE_E4M3 ? launch_dependent(quantize_kernel<TX, KGE_E4M3, false, P>, grid, dim3(256), 0, s, p)
+                               : launch_dependent(quantize_kernel<TX, KGE_E5M2, false, P>, grid, dim3(256), 0, s, p);
     };
-    if (p.pow2) with_format(std::true_type());
-    else with_format(std::false_type());
-    return launch_status(cudaGetLastError());
+    return launch_status(p.pow2 ? with_format(std::true_type()) : with_format(std::false_type()));
 }
 
 // ---- product ---------------------------------------------------------------------------------------------------------
@@ -625,6 +624,8 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
     __syncthreads();
     fp_fence_after();
     const uint32_t tmem = *tmem_slot;
+    grid_dependency_wait();          // (nothing of global memory was touched so far)
+    allow_dependents();
 
     const int step = SPLIT ? p.items : (int)gridDim.x;
     const int first = SPLIT ? (int)(blockIdx.x / cluster_size()) : (int)blockIdx.x;
@@ -845,10 +846,12 @@ int launch_product(const CUtensorMap& a, const CUtensorMap& b, ProductParams& p,
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(FORM == FP_SPLIT ? p.items * split : std::min<int64_t>(p.items, (int64_t)sms * fp_ctas_per_sm(FORM))));
     cfg.blockDim = dim3(fp_threads(FORM)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = FORM == FP_SPLIT ? 1 : 0;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = FORM == FP_SPLIT ? 2 : 1;
     return launch_status(cudaLaunchKernelEx(&cfg, fp8_product_kernel<FORM>, a, b, p));
 }
 

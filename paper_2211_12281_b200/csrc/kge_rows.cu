@@ -37,6 +37,8 @@ constexpr int LOOKUP_THREADS = 256, LOOKUP_UNROLL = 4;
 
 template <typename TT, typename TO, int V>
 __global__ void __launch_bounds__(LOOKUP_THREADS) lookup_kernel(LookupParams p) {
+    grid_dependency_wait();
+    allow_dependents();
     const TT* table = static_cast<const TT*>(p.table);
     TO* out = static_cast<TO*>(p.out);
     const int r0 = blockIdx.x * p.rows_per_cta, nr = min(p.rows_per_cta, p.n - r0);
@@ -465,6 +467,8 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
     __shared__ uint16_t start[SMALL_MAX + 1];
     __shared__ uint32_t warp_cnt[SMALL_THREADS / 32];
     __shared__ float red[SMALL_THREADS * V];
+    grid_dependency_wait();
+    allow_dependents();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_cta;
     const int nr = (int)min((int64_t)p.rows_per_cta, (int64_t)p.rows - r0);
@@ -763,8 +767,7 @@ int launch_lookup(LookupParams& p, int tt, int to, int vec, int dim, cudaStream_
         return with_type(to, [&](auto b) {
             using TT = decltype(a); using TO = decltype(b);
             return with_vector<sizeof(TT) == 2 || sizeof(TO) == 2>(vec, [&](auto v) {
-                lookup_kernel<TT, TO, decltype(v)::value><<<grid, LOOKUP_THREADS, 0, s>>>(p);
-                return launch_status(cudaGetLastError());
+                return launch_status(launch_dependent(lookup_kernel<TT, TO, decltype(v)::value>, grid, dim3(LOOKUP_THREADS), 0, s, p));
             });
         });
     });
@@ -778,8 +781,7 @@ int launch_small(SumParams& p, int vec, cudaStream_t s) {
     per = std::max<int64_t>(1, std::min<int64_t>({per, (1ll << 22) - 1, ((1ll << 31) - 1) / p.vecs.d}));
     p.rows_per_cta = (int)per;
     return with_vector<sizeof(TG) == 2>(vec, [&](auto v) {
-        grad_small_kernel<TG, TO, decltype(v)::value><<<(unsigned)ceil_div(p.rows, per), SMALL_THREADS, 0, s>>>(p);
-        return launch_status(cudaGetLastError());
+        return launch_status(launch_dependent(grad_small_kernel<TG, TO, decltype(v)::value>, dim3((unsigned)ceil_div(p.rows, per)), dim3(SMALL_THREADS), 0, s, p));
     });
 }
 
@@ -828,10 +830,12 @@ int launch_cluster_sort(SortParams& q, const SortPlan& plan, bool zero, int64_t 
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(CTAS * (1 + zero_clusters))); cfg.blockDim = dim3(CS_THREADS); cfg.stream = s;
     cfg.dynamicSmemBytes = cluster_sort_smem(q.n, plan.bits, CTAS);
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CTAS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
     return launch_status(cudaLaunchKernelEx(&cfg, grad_cluster_sort_kernel<CTAS>, q));
 }
 
