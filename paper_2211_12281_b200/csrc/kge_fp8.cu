@@ -343,17 +343,19 @@ constexpr int FP_BM = 128, FP_BK = 128;                   // BK bytes = one 128-
 constexpr uint32_t FP_BOX_BYTES = 128 * FP_BK;            // 128 rows of an operand
 constexpr int FP_NACC = 2;                                // block sums in tensor memory
 constexpr int FP_COLS = 64;                               // columns of the tile per epilogue warp
-// Three forms of the kernel: tiles of 256 columns, one CTA an SM, for many blocks of K; tiles of 128, two CTAs an SM (one loads and
-// multiplies while the other stores), for few; tiles of 128 whose blocks of K a cluster shares, where tiles are few.
-enum { FP_WIDE = 0, FP_PAIR = 1, FP_SPLIT = 2 };
-__host__ __device__ constexpr int fp_bn(int form) { return form == FP_WIDE ? 256 : 128; }
-__host__ __device__ constexpr int fp_stages(int form) { return form == FP_WIDE ? 4 : (form == FP_PAIR ? 2 : 6); }
+// Four forms of the kernel: tiles of 256 columns, one CTA an SM, for many blocks of K; tiles of 128, two CTAs an SM (one loads and
+// multiplies while the other stores), or of 64, three CTAs an SM, for few; tiles of 128 whose blocks of K a cluster shares, where
+// tiles are few.
+enum { FP_WIDE = 0, FP_PAIR = 1, FP_SPLIT = 2, FP_NARROW = 3 };
+__host__ __device__ constexpr int fp_bn(int form) { return form == FP_WIDE ? 256 : (form == FP_NARROW ? 64 : 128); }
+__host__ __device__ constexpr int fp_box_rows(int form) { return form == FP_NARROW ? 64 : 128; }             // of B per copy
+__host__ __device__ constexpr int fp_stages(int form) { return form == FP_WIDE ? 4 : (form == FP_SPLIT ? 6 : 2); }
 __host__ __device__ constexpr int fp_epi_warps(int form) { return 4 * fp_bn(form) / FP_COLS; }
 __host__ __device__ constexpr int fp_threads(int form) { return 32 * (4 + fp_epi_warps(form)); }     // (four more: copies, MMAs, two idle)
-__host__ __device__ constexpr int fp_ctas_per_sm(int form) { return form == FP_PAIR ? 2 : 1; }
+__host__ __device__ constexpr int fp_ctas_per_sm(int form) { return form == FP_PAIR ? 2 : (form == FP_NARROW ? 3 : 1); }
 __host__ __device__ constexpr uint32_t fp_stage_bytes(int form) { return FP_BOX_BYTES + (uint32_t)fp_bn(form) * FP_BK; }
 // Per epilogue warp: 32 rows x 32 or 128 bytes of the output on their way to memory.
-__host__ __device__ constexpr uint32_t fp_store_row(int form) { return form == FP_PAIR ? 128 : 32; }
+__host__ __device__ constexpr uint32_t fp_store_row(int form) { return form == FP_PAIR || form == FP_NARROW ? 128 : 32; }
 // Blocks of K whose scales are in shared memory.  A slot needs no barrier of its own: its block's scales are read before the epilogue
 // hands back the block sum after the next one, without which no MMA of the block FP_NACC later is issued, without which no stage
 // that follows by fp_stages() more is filled again -- at least stages + FP_NACC + 1 blocks later.
@@ -591,9 +593,9 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
     constexpr bool SPLIT = FORM == FP_SPLIT;
     constexpr int BN = fp_bn(FORM), STAGES = fp_stages(FORM), EW = fp_epi_warps(FORM), SLOTS = fp_slots(FORM), STORE_ROW = fp_store_row(FORM);
     constexpr uint32_t STAGE = fp_stage_bytes(FORM), TMEM_COLS = FP_NACC * BN;
-    // registers per thread as launched (20 warps x 96, 12 x 80 twice, or 12 x 168), and how they are shared out: the epilogue's 64 sums
+    // registers per thread as launched (20 warps x 96, 12 x 80 twice, 8 x 80 three times, or 12 x 168), and how they are shared out: the epilogue's 64 sums
     // and 32 loaded values do not fit the launch's share
-    constexpr int REGS = FORM == FP_WIDE ? 96 : (FORM == FP_PAIR ? 80 : 168), REGS_CONTROL = 32;
+    constexpr int REGS = FORM == FP_WIDE ? 96 : (FORM == FP_SPLIT ? 168 : 80), REGS_CONTROL = 32;
     constexpr int REGS_EPI = FORM == FP_SPLIT ? 168 : REGS + 4 * (REGS - REGS_CONTROL) / EW / 8 * 8;
     static_assert(4 * REGS_CONTROL + EW * REGS_EPI <= (4 + EW) * REGS, "register shares exceed the launch's");
     extern __shared__ __align__(1024) unsigned char fp_smem[];
@@ -642,7 +644,7 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 const float* const sa0 = p.sa + (p.a_square ? m0 >> 7 : m0 + lane);
                 const float* const sb0 = p.sb + (p.b_square ? (n0 >> 7) + lane : n0 + lane);
                 const int na = p.a_square ? (lane == 0 ? 1 : 0) : (int)p.M - m0 - lane;         // (values to copy are those i with 32 i < na)
-                const int nb = p.b_square ? (lane < BN / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
+                const int nb = p.b_square ? (lane < (BN + 127) / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
                 for (int kb = kb0; kb < kb1; ++kb) {
                     ok = mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop;
                     ok = __all_sync(0xffffffffu, ok);
@@ -652,7 +654,7 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                         mbar_arrive_expect_tx(&full[s], STAGE);
                         fp_tma_load(sa, &tmA, kb * FP_BK, m0, &full[s]);
     #pragma unroll
-                        for (int g = 0; g < BN / 128; ++g) fp_tma_load(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
+                        for (int g = 0; g < (BN + 127) / 128; ++g) fp_tma_load(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
                     }
                     const uint32_t at = smem_u32(scales + slot * (128 + BN) + lane);
     #pragma unroll
@@ -788,7 +790,7 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-int operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t k, int64_t ld) {
+int operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t k, int64_t ld, int box_rows) {
     static const EncodeTiledFn fn = [] {
         void* ptr = nullptr;
         cudaDriverEntryPointQueryResult q;
@@ -797,7 +799,7 @@ int operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t k, int
     }();
     if (!fn) return KGE_ERR_CUDA;
     const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {FP_BK, 128}, one[2] = {1, 1};
+    const cuuint32_t box[2] = {FP_BK, (cuuint32_t)box_rows}, one[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? KGE_OK : KGE_ERR_CUDA;
 }
@@ -828,7 +830,10 @@ ProductPlan product_plan(int64_t M, int64_t N, int kblocks, int sms) {
         split = (kblocks + per - 1) / per;              // every CTA has a block
         if (split > 1) return {FP_SPLIT, split};
     }
-    return {tiles256 >= sms && kblocks >= 16 ? FP_WIDE : FP_PAIR, 1};
+    if (tiles256 >= sms && kblocks >= 16) return {FP_WIDE, 1};
+    // few blocks of K: memory sets the pace, and what counts is how well whole rounds of tiles fill the SMs
+    const int64_t pair = ceil_div(tiles128, 2 * sms) * 256, narrow = ceil_div(ceil_div(M, FP_BM) * ceil_div(N, 64), 3 * sms) * 192;
+    return {narrow < pair ? FP_NARROW : FP_PAIR, 1};
 }
 
 template <int FORM>
@@ -900,17 +905,22 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
     const int ob = type_bytes(out_type);
     p.vec = ld_out * ob % 16 == 0 && aligned_to(out, 16) && (!addend || (ld_addend * ob % 16 == 0 && aligned_to(addend, 16)));
     p.status = status; p.wait_limit = kDefaultWaitLimit;
-    alignas(64) CUtensorMap ma, mb;
-    int sms = 0, rc = operand_map(&ma, a, M, K, lda);
-    if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb);
-    if (rc == KGE_OK) rc = sm_count(&sms);
+    int sms = 0, rc = sm_count(&sms);
     if (rc != KGE_OK) return rc;
-    if (ceil_div(M, 128) * ceil_div(N, 128) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;
+    if (ceil_div(M, 128) * ceil_div(N, 64) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;
     const ProductPlan plan = product_plan(M, N, p.kblocks, sms);
+    alignas(64) CUtensorMap ma, mb;
+    rc = operand_map(&ma, a, M, K, lda, FP_BM);
+    if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb, fp_box_rows(plan.form));
+    if (rc != KGE_OK) return rc;
     p.idesc = fp_idesc(FP_BM, fp_bn(plan.form), a_type == KGE_E5M2, b_type == KGE_E5M2);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (plan.form == FP_SPLIT) return launch_product<FP_SPLIT>(ma, mb, p, plan.split, sms, s);
-    return plan.form == FP_WIDE ? launch_product<FP_WIDE>(ma, mb, p, 1, sms, s) : launch_product<FP_PAIR>(ma, mb, p, 1, sms, s);
+    switch (plan.form) {
+        case FP_SPLIT: return launch_product<FP_SPLIT>(ma, mb, p, plan.split, sms, s);
+        case FP_WIDE: return launch_product<FP_WIDE>(ma, mb, p, 1, sms, s);
+        case FP_NARROW: return launch_product<FP_NARROW>(ma, mb, p, 1, sms, s);
+        default: return launch_product<FP_PAIR>(ma, mb, p, 1, sms, s);
+    }
 }
 
 }  // extern "C"
