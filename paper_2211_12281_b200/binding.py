@@ -79,6 +79,7 @@ SIGNATURES = {
     "kge_workspace_bytes": (C.c_size_t, [_vp, C.c_int64, C.c_int32, C.c_int32]),
     "kge_bind": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_size_t, C.c_int64, C.c_int32, C.c_int32, _vp]),
     "kge_bind_features": (C.c_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "kge_bind_features_fp8": (C.c_int, [_vp, _vp, C.c_int32, C.c_int64, _vp, _vp, _vp, _vp, _vp, _vp]),
     "kge_graph_load": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int64, _vp]),
     "kge_graph_load_device": (C.c_int, [_vp, _vp, _vp, _vp, C.c_int64, _vp]),
     "kge_init_tables": (C.c_int, [_vp, C.c_float, _vp]),
@@ -457,6 +458,16 @@ class Kge:
         self._keep += [feat, MH, MT, MH_state, MT_state]
         self._check(lib().kge_bind_features(self._h, _ptr(feat), _ptr(MH), _ptr(MT), _ptr(MH_state), _ptr(MT_state), _stream()),
                     "kge_bind_features")
+
+    def bind_features_fp8(self, feat, scales, MH, MT, MH_state=None, MT_state=None):
+        """feat: float8 [E, F] and its scales [ceil(F / 128), E] as fp8_quantize makes them; the rest as in bind_features."""
+        w = "kge_bind_features_fp8"
+        code, rows, cols, ld, block = _operand(feat, scales, w, "feat")
+        if rows != self.cfg.num_entities or cols != self.cfg.feat_dim or block != 1:
+            raise _bad(w, "feat is not [entities, feat_dim] with a scale per row and block of 128")
+        self._keep += [feat, scales, MH, MT, MH_state, MT_state]
+        self._check(lib().kge_bind_features_fp8(self._h, feat.data_ptr(), code, ld, scales.data_ptr(), _ptr(MH), _ptr(MT), _ptr(MH_state),
+                                                _ptr(MT_state), _stream()), w)
 
     def graph_load(self, heads, rels, tails):
         """heads / rels / tails: numpy int32 host arrays."""

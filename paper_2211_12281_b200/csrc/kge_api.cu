@@ -429,8 +429,7 @@ int kge_bind(kge_handle* h, float* ent, float* rel, float* relw, float* ent_stat
     return KGE_OK;
 }
 
-int kge_bind_features(kge_handle* h, const uint16_t* feat, float* MH, float* MT, float* MH_state, float* MT_state, void* stream) {
-    (void)stream;
+static int bind_matrices(kge_handle* h, const void* feat, float* MH, float* MT, float* MH_state, float* MT_state) {
     if (!h || !feat || !MH || !MT) return KGE_ERR_BAD_ARG;
     if (h->cfg.feat_dim <= 0) return KGE_ERR_UNSUPPORTED;
     if (!h->bound) return KGE_ERR_NOT_READY;
@@ -438,10 +437,29 @@ int kge_bind_features(kge_handle* h, const uint16_t* feat, float* MH, float* MT,
     if (h->cfg.opt != KGE_OPT_SGD && (!MH_state || !MT_state)) return KGE_ERR_BAD_ARG;
     auto misaligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) % 16) != 0; };
     if (misaligned(feat) || misaligned(MH) || misaligned(MT)) return KGE_ERR_BAD_ARG;
-    h->feat = feat; h->MH = MH; h->MT = MT; h->MH_state = MH_state; h->MT_state = MT_state;
+    h->MH = MH; h->MT = MT; h->MH_state = MH_state; h->MT_state = MT_state;
     const int rc = encoder_make_maps(h);
     if (rc != KGE_OK) return rc;
     h->features_bound = true;
+    return KGE_OK;
+}
+
+int kge_bind_features(kge_handle* h, const uint16_t* feat, float* MH, float* MT, float* MH_state, float* MT_state, void* stream) {
+    (void)stream;
+    const int rc = bind_matrices(h, feat, MH, MT, MH_state, MT_state);
+    if (rc != KGE_OK) return rc;
+    h->feat = feat; h->feat8 = nullptr;
+    return KGE_OK;
+}
+
+int kge_bind_features_fp8(kge_handle* h, const void* feat, int32_t fp8_type, int64_t ld, const float* scales, float* MH, float* MT, float* MH_state,
+                          float* MT_state, void* stream) {
+    (void)stream;
+    if (!h || !scales || (fp8_type != KGE_E4M3 && fp8_type != KGE_E5M2) || ld % 16 != 0 || ld < h->cfg.feat_dim ||
+        reinterpret_cast<uintptr_t>(scales) % 4 != 0) return KGE_ERR_BAD_ARG;
+    const int rc = bind_matrices(h, feat, MH, MT, MH_state, MT_state);
+    if (rc != KGE_OK) return rc;
+    h->feat = nullptr; h->feat8 = static_cast<const uint8_t*>(feat); h->feat8_scales = scales; h->feat8_ld = ld; h->feat8_type = fp8_type;
     return KGE_OK;
 }
 

@@ -142,7 +142,9 @@ struct kge_handle {
     // encoder: features of the head / tail+negative slots and M_H / M_T (K-major, 128-row boxes) for the projection; the
     // slots' gradient rows and features again (MN-major, 64-row boxes) for dM = dE^T . F
     alignas(64) unsigned char tm_fh[128], tm_ft[128], tm_mh[128], tm_mt[128], tm_gh64[128], tm_gt64[128], tm_fh64[128], tm_ft64[128];
-    const uint16_t* feat;   // [E, F] bf16 text features (fixed)
+    const uint16_t* feat;   // [E, F] bf16 text features (fixed), or NULL:
+    const uint8_t* feat8;   // [E, F] the same as 8-bit values with scales [ceil(F / 128), E]
+    const float* feat8_scales; int64_t feat8_ld; int feat8_type;
     float *MH, *MT, *MH_state, *MT_state;   // [d, F] projection matrices and their optimiser state
     int split_mh, split_mt; // K splits of the two dM contractions (heads; tails and negatives)
     bool features_bound;

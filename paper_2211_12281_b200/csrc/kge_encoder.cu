@@ -9,6 +9,7 @@
 #include <cmath>
 
 #include <cuda_bf16.h>
+#include <cuda_fp8.h>
 
 #include "kge_sample.cuh"
 
@@ -18,6 +19,8 @@ namespace {
 
 struct PrepareParams {
     const uint16_t* feat; int F8;        // [E, F] bf16 features, F / 8 16-byte words per row
+    const uint8_t* feat8; int64_t ld8;   // or [E, F] 8-bit features, rows ld8 bytes apart, with fp32 scales [ceil(F / 128), E]
+    const float* scales; int e5m2;
     int64_t E;
     const int32_t *heads, *tails, *negs;
     int B, N;
@@ -40,9 +43,37 @@ __device__ __forceinline__ void copy_row(uint4* dst, const uint4* src, int n, in
     }
 }
 
+// The same of a row of 8-bit features: value times scale, rounded to bf16, eight to a lane.
+__device__ __forceinline__ void copy_row8(uint4* dst, const PrepareParams& p, int64_t id, int lane) {
+    const uint2* src = reinterpret_cast<const uint2*>(p.feat8 + id * p.ld8);
+    for (int c0 = 0; c0 < p.F8; c0 += 64) {
+        uint2 v[2];
+        float s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) { const int c = c0 + 32 * u + lane; if (c < p.F8) { v[u] = src[c]; s[u] = p.scales[(int64_t)(c >> 4) * p.E + id]; } }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int c = c0 + 32 * u + lane;
+            if (c >= p.F8) continue;
+            uint32_t o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t two = ((i < 2 ? v[u].x : v[u].y) >> (16 * (i & 1))) & 0xFFFFu;
+                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, p.e5m2 ? __NV_E5M2 : __NV_E4M3);
+                const float2 f = __half22float2(__half2(h));
+                const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * s[u], f.y * s[u]);
+                o[i] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            dst[c] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
 // Everything the projection reads, in one launch (the sampling, the gather and two casts took a launch each, 18 us at
 // B = 512, N = 1024, d = 256, F = 768): CTAs [0, pos_ctas) the feature rows of eight positives' heads and tails (a warp
 // each; with fused_sample it draws its positive first), then those of eight negatives each, then the bf16 copies of the matrices.
+// FP8: the features are 8-bit operands as kge_fp8_quantize makes them.
+template <bool FP8>
 __global__ void __launch_bounds__(256) encoder_prepare_kernel(PrepareParams p) {
     extern __shared__ uint64_t bucket_wcum[];   // fused sampling: cumulative weights of this CTA's buckets
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -51,6 +82,11 @@ __global__ void __launch_bounds__(256) encoder_prepare_kernel(PrepareParams p) {
     allow_dependents();
     const uint4* feat = reinterpret_cast<const uint4*>(p.feat);
     uint4* out = reinterpret_cast<uint4*>(p.out);
+    auto copy = [&](int64_t slot, int32_t entity) {
+        const int64_t id = checked_id(entity, p.E, p.status);
+        if (FP8) copy_row8(out + slot * p.F8, p, id, lane);
+        else copy_row(out + slot * p.F8, feat + id * p.F8, p.F8, lane);
+    };
     if (blk < p.pos_ctas) {
         const int b = blk * 8 + warp;
         int32_t ih, ir, it;
@@ -67,8 +103,8 @@ __global__ void __launch_bounds__(256) encoder_prepare_kernel(PrepareParams p) {
             if (b >= p.B) return;
             ih = p.heads[b]; it = p.tails[b];
         }
-        copy_row(out + (int64_t)b * p.F8, feat + checked_id(ih, p.E, p.status) * p.F8, p.F8, lane);
-        copy_row(out + (int64_t)(p.B + b) * p.F8, feat + checked_id(it, p.E, p.status) * p.F8, p.F8, lane);
+        copy(b, ih);
+        copy(p.B + b, it);
         return;
     }
     blk -= p.pos_ctas;
@@ -78,7 +114,7 @@ __global__ void __launch_bounds__(256) encoder_prepare_kernel(PrepareParams p) {
         int32_t neg;
         if (p.fused_sample) { neg = sample_negative(p.sp, n); if (lane == 0) p.sp.negs[n] = neg; }
         else neg = p.negs[n];
-        copy_row(out + (int64_t)(2 * p.B + n) * p.F8, feat + checked_id(neg, p.E, p.status) * p.F8, p.F8, lane);
+        copy(2 * p.B + n, neg);
         return;
     }
     blk -= p.neg_ctas;
@@ -174,7 +210,7 @@ int launch_encoder_forward(kge_handle* h, const int32_t* heads, const int32_t* t
     const Workspace& w = h->ws;
     const int B = c.batch, N = c.num_neg, d = c.dim, F = c.feat_dim;
     PrepareParams p{};
-    p.feat = h->feat; p.F8 = F / 8; p.E = c.num_entities;
+    p.feat = h->feat; p.feat8 = h->feat8; p.ld8 = h->feat8_ld; p.scales = h->feat8_scales; p.e5m2 = h->feat8_type == KGE_E5M2; p.F8 = F / 8; p.E = c.num_entities;
     p.heads = heads; p.tails = tails; p.negs = negs; p.B = B; p.N = N; p.out = w.Fb;
     p.MH = reinterpret_cast<const float4*>(h->MH); p.MT = c.feat_shared ? nullptr : reinterpret_cast<const float4*>(h->MT);
     p.Mb = reinterpret_cast<uint2*>(w.Mb); p.m4 = (int64_t)d * F / 4;
@@ -185,7 +221,7 @@ int launch_encoder_forward(kge_handle* h, const int32_t* heads, const int32_t* t
     p.sp.heads = w.heads; p.sp.rels = w.rels; p.sp.tails = w.tails; p.sp.negs = w.negs;
     p.status = w.status;
     const int64_t cast_ctas = ((p.MT ? 2 : 1) * p.m4 + 255) / 256;
-    KGE_CUDA_CHECK(h, launch_dependent(encoder_prepare_kernel, dim3((unsigned)(p.pos_ctas + p.neg_ctas + cast_ctas)), dim3(256),
+    KGE_CUDA_CHECK(h, launch_dependent(h->feat8 ? encoder_prepare_kernel<true> : encoder_prepare_kernel<false>, dim3((unsigned)(p.pos_ctas + p.neg_ctas + cast_ctas)), dim3(256),
                                        fused_sample ? (size_t)fused_sample_smem(c.num_relations, p.slots_per_bucket) : 0, s, p));
     KGE_LAUNCH_CHECK(h);
     return launch_tc_dual_nt(h, h->tm_fh, h->tm_mh, h->tm_ft, c.feat_shared ? h->tm_mh : h->tm_mt, B, B + N, d, F, w.proj,

@@ -414,6 +414,31 @@ def test_quantize_rounds_the_true_quotient(T, K, fmt):
     assert T.equal(s, ws) and T.equal(q.float().double(), want), int((q.float().double() != want).sum())
 
 
+@pytest.mark.parametrize("tx,fmt,block", [("bf16", "e4m3", 1), ("bf16", "e5m2", 1), ("f16", "e4m3", 1), ("f16", "e5m2", 1), ("bf16", "e4m3", 128), ("f16", "e5m2", 128)])
+def test_quantize_rounds_the_true_quotient_of_16_bit_values(T, K, tx, fmt, block):
+    """Every mantissa of a block's largest value against a spread of the others' mantissas and exponents: with 16-bit values the
+    quotient falls on the middle of two 8-bit values, or a rounding of the scale beside it, two times in a thousand."""
+    bits = 7 if tx == "bf16" else 10
+    rows, cols = (1 << bits), 128
+    top = (1 + T.arange(rows, device="cuda").double() / rows) * 2.0 ** -2
+    if block == 128:
+        rows = min(rows, 512)
+        top = top[:: len(top) // rows].repeat_interleave(128)[: 128 * rows]          # one largest value per block of 128 rows
+    g = _gen(T, 6)
+    n = top.numel()
+    mant = 1 + T.randint(0, 1 << bits, (n, cols * 8), generator=g, device="cuda").double() / (1 << bits)
+    x = mant * T.exp2(-T.randint(0, 12 if tx == "bf16" else 9, mant.shape, generator=g, device="cuda").double())
+    x = T.where(x < 1, x, x / 2) * top[:, None]                                      # below the largest value ...
+    x = x.to(_type(T, tx))
+    x = T.where(x.double() > top[:, None], top[:, None].to(x.dtype), x)
+    x[:, ::128] = top[:, None].to(x.dtype)                                           # ... which stands first in every block
+    want, ws = _quantized(T, x, fmt, block, False)
+    q = _empty8(T, n, cols * 8, fmt)
+    s = T.empty((cols * 8 // 128, n if block == 1 else (n + 127) // 128), device="cuda")
+    K.fp8_quantize(x, q, s, block_rows=block)
+    assert T.equal(s, ws) and T.equal(q.float().double(), want), int((q.float().double() != want).sum())
+
+
 @pytest.mark.parametrize("block", [1, 128])
 def test_quantize_of_extreme_blocks(T, K, block):
     x = T.ones((256, 256), device="cuda")
@@ -582,6 +607,51 @@ def test_encoder_of_rows_and_features(T, K, case):
     full = dpre.t() @ feat.double()
     bound = (2.0 ** -3 + 2.0 ** -4 + 2.0 ** -7) * (dpre.abs().t() @ feat.double().abs())
     assert ((got["dm"].double() - full).abs() <= bound + 1e-3).all()
+
+
+@pytest.mark.parametrize("fmt,F,d,opt,own", [("e4m3", 768, 64, "sgd", True), ("e5m2", 192, 40, "adagrad", False), ("e4m3", 64, 32, "adam", True),
+                                              ("e4m3", 1088, 72, "sgd", False)])
+def test_training_step_on_features_in_8_bits(T, K, fmt, F, d, opt, own):
+    """A step on 8-bit features is, bit for bit, the step on the bf16 values that they stand for."""
+    from parity_util import GpuSide, Problem
+    sides = []
+    for eight in (True, False):
+        prob = Problem(E=900, R=5, T=9000, d=d, score="distmult", loss="softmax", opt=opt, B=64, N=128, P=2, lr=0.02, graph_seed=29)
+        prob.kw.update(feat_dim=F, feat_shared=0)
+        gpu = GpuSide(prob)
+        g = _gen(T, 3)
+        x = T.randn((prob.E, F), generator=g, device="cuda") * T.exp(T.randn((prob.E, 1), generator=g, device="cuda")) * F ** -0.5
+        mats = [T.randn((d, F), generator=g, device="cuda").mul_(0.3) for _ in range(2)]
+        shape = {"sgd": None, "adam": (d, 2 * F), "adagrad": (d,)}[opt]
+        states = [None if shape is None else T.zeros(shape, device="cuda") for _ in range(2)]
+        q, s = _empty8(T, prob.E, F, fmt, 16), T.empty(((F + 127) // 128, prob.E), device="cuda")
+        K.fp8_quantize(x, q, s)
+        if eight:
+            gpu.kge.bind_features_fp8(q, s, *mats, *states)
+        else:
+            gpu.kge.bind_features(_stands_for(T, q, s).to(T.bfloat16), *mats, *states)      # (a product of 4 and 24 bits is exact in 64: one rounding)
+        loss = T.zeros(1, device="cuda")
+        for step in range(2):
+            ids = () if own else [gpu.dev_i32(a) for a in gpu.sample(step)]
+            gpu.kge.train_step(step, prob.lr, *ids, loss_out=loss)
+        assert gpu.kge.get_status() == 0
+        sides.append([gpu.ent, gpu.rel, loss, *mats] + [v for v in states if v is not None])
+    for a, b in zip(*sides):
+        assert T.isfinite(a).all() and T.equal(a, b)
+
+
+def test_features_in_8_bits_are_checked(T, K):
+    from parity_util import GpuSide, Problem
+    prob = Problem(E=90, R=3, T=500, d=32, score="transe", B=4, N=4, P=1)
+    prob.kw.update(feat_dim=64)
+    gpu = GpuSide(prob)
+    mats = [T.zeros((32, 64), device="cuda") for _ in range(2)]
+    q, s = _empty8(T, 90, 64, "e4m3"), T.ones((1, 90), device="cuda")
+    for feat, scales in ((q[:89], s[:, :89].contiguous()), (q[:, :48], s), (q, T.ones((1, 1), device="cuda"))):
+        with pytest.raises(K.KgeError) as e:
+            gpu.kge.bind_features_fp8(feat, scales, *mats)
+        assert e.value.code == -1
+    gpu.kge.bind_features_fp8(q, s, *mats)
 
 
 def test_captured_runs_replay_beside_eager_ones(T, K):

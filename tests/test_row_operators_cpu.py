@@ -83,6 +83,16 @@ def test_matmul_scratch_is_checked(K):
     assert K.fp8_matmul_scratch_bytes(0, 32, 64) == 0 and K.fp8_matmul_scratch_bytes(-1, 32, 64) == 0
 
 
+def test_binding_features_in_8_bits_refuses(K):
+    h = K.Kge(K.KgeConfig.make(num_entities=100, num_relations=3, dim=32, score="transe", batch=4, num_neg=4, feat_dim=64))
+    fn = K.lib().kge_bind_features_fp8
+    assert fn(None, PTR, E4M3, 64, PTR, PTR, PTR * 2, None, None, None) == -1
+    assert fn(h._h, PTR, E4M3, 64, PTR, PTR, PTR * 2, None, None, None) == -6          # tables not bound
+    for feat, code, ld, scales in ((PTR, F32, 64, PTR), (PTR, E4M3, 48, PTR), (PTR, E4M3, 72, PTR), (PTR, E4M3, 64, None), (PTR, E4M3, 64, PTR + 2),
+                                   (None, E4M3, 64, PTR)):
+        assert fn(h._h, feat, code, ld, scales, PTR, PTR * 2, None, None, None) == -1
+
+
 def test_scratch_sizes_cover_their_lists(K):
     # a list of (id, position) pairs and partial rows for chunks of ids; short lists keep nothing
     for rows, dim, n in ((10, 8, 1025), (91_000_000, 128, 24_576), (100, 256, 600_000)):
