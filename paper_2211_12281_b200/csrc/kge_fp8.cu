@@ -183,7 +183,7 @@ __device__ __forceinline__ void load8(const QuantParams& p, Eight<TX>& e, int64_
 
 // One CTA per 128 x 128 tile: thread (rg, cg) holds rows 8 rg .. + 8 and columns 8 cg .. + 8.
 template <typename TX, int FMT, bool SQUARE, bool POW2>
-__global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 3 : 2) quantize_kernel(QuantParams p) {
+__global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 4 : 2) quantize_kernel(QuantParams p) {
     __shared__ uint32_t part[16][128];
     __shared__ Block col_block[128];
     __shared__ alignas(16) uint2 turned[128][16];
@@ -235,12 +235,22 @@ __global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 3 : 2) quantize_kernel(
     }
     if (p.qt) {
         if (!SQUARE) {
+            if constexpr (sizeof(TX) == 2) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                uint32_t m = 0;
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t m = x[0].w[j] & 0x7FFF7FFFu;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) m = max(m, x[i].key(j));
-                part[rg][cg * 8 + j] = m;
+                    for (int i = 1; i < 8; ++i) m = __vmaxu2(m, x[i].w[j] & 0x7FFF7FFFu);
+                    *reinterpret_cast<uint2*>(&part[rg][cg * 8 + 2 * j]) = make_uint2(m & 0xFFFFu, m >> 16);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) m = max(m, x[i].key(j));
+                    part[rg][cg * 8 + j] = m;
+                }
             }
             __syncthreads();
             if (tid < 128) {
@@ -277,11 +287,11 @@ __global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 3 : 2) quantize_kernel(
     }
 }
 
-// Blocks of 1 x 128 along the rows only: a warp takes thirty-two rows of one block of columns, eight or four at a time (sixteen lanes of
+// Blocks of 1 x 128 along the rows only: a warp takes sixteen rows of one block of columns, eight or four at a time (sixteen lanes of
 // eight columns each), the next ones' loads under way.
 template <typename TX, int FMT, bool POW2>
-__global__ void __launch_bounds__(256) quantize_rows_kernel(QuantParams p) {
-    constexpr int STEP = sizeof(TX) == 2 ? 4 : 2, ROWS = 32, STEPS = ROWS / (2 * STEP);
+__global__ void __launch_bounds__(256, 4) quantize_rows_kernel(QuantParams p) {
+    constexpr int STEP = sizeof(TX) == 2 ? 4 : 2, ROWS = 16, STEPS = ROWS / (2 * STEP);
     grid_dependency_wait();
     allow_dependents();
     const int lane = threadIdx.x & 31, cg = lane & 15;
@@ -323,7 +333,7 @@ int launch_quantize(const QuantParams& p, int fmt, bool square, cudaStream_t s) 
     auto with_format = [&](auto pow2) {
         constexpr bool P = decltype(pow2)::value;
         if (!square && !p.qt) {
-            const dim3 grid((unsigned)ceil_div(p.tiles_c * ceil_div(p.rows, 32), 8));
+            const dim3 grid((unsigned)ceil_div(p.tiles_c * ceil_div(p.rows, 16), 8));
             return fmt == KGE_E4M3 ? launch_dependent(quantize_rows_kernel<TX, KGE_E4M3, P>, grid, dim3(256), 0, s, p)
                                    : launch_dependent(quantize_rows_kernel<TX, KGE_E5M2, P>, grid, dim3(256), 0, s, p);
         }
