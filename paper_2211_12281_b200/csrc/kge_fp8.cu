@@ -463,6 +463,10 @@ template <typename TO, int ROW>
 __device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int col0, const uint64_t (&acc)[FP_COLS / 2], float4* st, int lane) {
     constexpr int V = 16 / sizeof(TO), UNITS = ROW / 16, PASS = ROW / sizeof(TO);      // columns per unit, units and columns per pass
     constexpr int TURN = UNITS == 2 ? 2 : 0;                                            // rows 4 apart share banks at 32 bytes a row
+    // a warp's part that lies inside the matrix is stored without a look at its edges
+    const bool inside = p.vec && row0 + 32 <= p.M && col0 + FP_COLS <= p.N;
+    TO* const first = static_cast<TO*>(p.out) + (row0 + lane / UNITS) * p.ld_out + col0 + V * (lane % UNITS);
+    const int64_t step = (32 / UNITS) * p.ld_out;
 #pragma unroll
     for (int c = 0; c < FP_COLS; c += PASS) {
 #pragma unroll
@@ -477,12 +481,23 @@ __device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int c
             st[lane * UNITS + (i ^ ((lane >> TURN) & (UNITS - 1)))] = *reinterpret_cast<const float4*>(&own);
         }
         __syncwarp();
+        const int r0 = lane / UNITS, unit = lane % UNITS;
+        if (inside) {
+            TO* dst = first + c;
 #pragma unroll
-        for (int j = 0; j < UNITS; ++j) {
-            const int r = j * (32 / UNITS) + lane / UNITS, unit = lane % UNITS, row = row0 + r, col = col0 + c + V * unit;
-            if (row < p.M && col < p.N) {
-                const float4 w = st[r * UNITS + (unit ^ ((r >> TURN) & (UNITS - 1)))];
-                fp_put<TO, V>(p, row, col, *reinterpret_cast<const Pack<TO, V>*>(&w));
+            for (int j = 0; j < UNITS; ++j) {
+                const int r = j * (32 / UNITS) + r0;
+                *reinterpret_cast<float4*>(dst) = st[r * UNITS + (unit ^ ((r >> TURN) & (UNITS - 1)))];
+                dst += step;
+            }
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < UNITS; ++j) {
+                const int r = j * (32 / UNITS) + r0, row = row0 + r, col = col0 + c + V * unit;
+                if (row < p.M && col < p.N) {
+                    const float4 w = st[r * UNITS + (unit ^ ((r >> TURN) & (UNITS - 1)))];
+                    fp_put<TO, V>(p, row, col, *reinterpret_cast<const Pack<TO, V>*>(&w));
+                }
             }
         }
         __syncwarp();
