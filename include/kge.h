@@ -431,10 +431,9 @@ int kge_dropout(const void* x, int32_t x_type, const void* residual, void* out, 
  */
 int kge_fp8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, int32_t fp8_type, int32_t block_rows, int32_t pow2,
                      void* q, int64_t ldq, float* scales, void* qt, int64_t ldqt, float* scales_t, void* stream);
-size_t kge_fp8_matmul_scratch_bytes(int64_t M, int64_t N, int64_t K);
 int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_scales, int32_t a_block, const void* b, int32_t b_type, int64_t ldb,
                    const float* b_scales, int32_t b_block, const void* addend, int64_t ld_addend, void* out, int32_t out_type, int64_t ld_out,
-                   int64_t M, int64_t N, int64_t K, void* scratch, size_t scratch_bytes, int32_t* status, void* stream);
+                   int64_t M, int64_t N, int64_t K, int32_t* status, void* stream);
 
 /* Synchronise `stream`, return the sticky device status word (0 or a negative code), clear it. */
 int kge_get_status(kge_handle* h, void* stream);

@@ -118,9 +118,8 @@ SIGNATURES = {
     "kge_dropout": (C.c_int, [_vp, C.c_int32, _vp, _vp, C.c_int32, C.c_int64, C.c_double, C.c_uint64, C.c_uint64, _vp, C.c_int32, _vp]),
     "kge_fp8_quantize": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _vp, C.c_int64, _vp, _vp,
                                    C.c_int64, _vp, _vp]),
-    "kge_fp8_matmul_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int64, C.c_int64]),
     "kge_fp8_matmul": (C.c_int, [_vp, C.c_int32, C.c_int64, _vp, C.c_int32, _vp, C.c_int32, C.c_int64, _vp, C.c_int32, _vp, C.c_int64, _vp,
-                                 C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_size_t, _vp, _vp]),
+                                 C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, _vp, _vp]),
     "kge_get_status": (C.c_int, [_vp, _vp]),
     "kge_launch_count": (C.c_int64, [_vp]),
     "kge_profile": (C.c_int, [_vp, C.c_int]),
@@ -385,12 +384,7 @@ def fp8_quantize(x, q=None, scales=None, qt=None, scales_t=None, block_rows=1, p
     _call(w, lib().kge_fp8_quantize, dev, x.data_ptr(), tx, rows, cols, lx, code, block_rows, 1 if pow2 else 0, at[0], ld[0], at[1], at[2], ld[1], at[3])
 
 
-def fp8_matmul_scratch_bytes(m, n, k) -> int:
-    """Bytes of scratch an fp8_matmul of these sizes needs (a tensor of 256 more is always enough); 0: none."""
-    return int(lib().kge_fp8_matmul_scratch_bytes(m, n, k))
-
-
-def fp8_matmul(a, a_scales, b, b_scales, out, addend=None, scratch=None, status=None):
+def fp8_matmul(a, a_scales, b, b_scales, out, addend=None, status=None):
     """kge_fp8_matmul: out [M, N] = a [M, K] . b [N, K]^T (+ addend) of operands as fp8_quantize makes them."""
     w = "kge_fp8_matmul"
     ta, m, k, la, ba = _operand(a, a_scales, w, "a")
@@ -403,9 +397,8 @@ def fp8_matmul(a, a_scales, b, b_scales, out, addend=None, scratch=None, status=
         if am != m or an != n or addend.dtype is not out.dtype:
             raise _bad(w, "addend is not of out's shape and type")
     dev = _device_of(w, a, a_scales, b, b_scales, out, addend, status)
-    at, size, keep = _scratch(scratch, lib().kge_fp8_matmul_scratch_bytes(m, n, k), dev, w)
     _call(w, lib().kge_fp8_matmul, dev, a.data_ptr(), ta, la, a_scales.data_ptr(), ba, b.data_ptr(), tb, lb, b_scales.data_ptr(), bb, _addr(addend), ladd,
-          out.data_ptr(), to, lo, m, n, k, at, size, _status_word(status, w))
+          out.data_ptr(), to, lo, m, n, k, _status_word(status, w))
 
 
 class Kge:

@@ -910,11 +910,9 @@ int kge_fp8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, 
     return with_type(x_type, [&](auto t) { return launch_quantize<decltype(t)>(p, fp8_type, block_rows == 128, static_cast<cudaStream_t>(stream)); });
 }
 
-size_t kge_fp8_matmul_scratch_bytes(int64_t M, int64_t N, int64_t K) { return 0; }
-
 int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_scales, int32_t a_block, const void* b, int32_t b_type, int64_t ldb,
                    const float* b_scales, int32_t b_block, const void* addend, int64_t ld_addend, void* out, int32_t out_type, int64_t ld_out,
-                   int64_t M, int64_t N, int64_t K, void* scratch, size_t scratch_bytes, int32_t* status, void* stream) {
+                   int64_t M, int64_t N, int64_t K, int32_t* status, void* stream) {
     if (!is_fp8_type(a_type) || !is_fp8_type(b_type) || !is_float_type(out_type) || (a_block != 1 && a_block != 128) || (b_block != 1 && b_block != 128) ||
         M < 0 || N < 0 || K < 1 || M > INT32_MAX - 256 || N > INT32_MAX - 256 || K > INT32_MAX - 256 || ld_out < N || (addend && ld_addend < N))
         return KGE_ERR_BAD_ARG;

@@ -441,6 +441,7 @@ struct SumParams {
     int accumulate;
     float* part;
     int2* list; int32_t* list_count;
+    int group;                             // chunks per CTA of grad_sum_kernel, where its threads are whole chunks, else 1
     FastDiv vecs;
     const int32_t* ids; int32_t padding_id; int rows_per_cta; int32_t* status;     // grad_small_kernel
 };
@@ -617,7 +618,8 @@ template <typename TG, typename TO, int V, int L>
 __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
     constexpr int BYTES = V * (int)sizeof(TG);
     constexpr bool ASYNC = BYTES >= 4;                    // (asynchronous copies take 4, 8 or 16 bytes)
-    __shared__ alignas(16) unsigned char ring[ASYNC ? SUM_DEPTH * SUM_THREADS * BYTES : 16];
+    constexpr int RING = ASYNC ? SUM_DEPTH * SUM_THREADS * BYTES : 0, SUMS = SUM_THREADS * V * 4;
+    __shared__ alignas(16) unsigned char ring[RING > SUMS ? RING : SUMS];
     grid_dependency_wait();
     allow_dependents();
     const int64_t item = (int64_t)blockIdx.x * SUM_THREADS + threadIdx.x;
@@ -691,12 +693,29 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
 #pragma unroll
         for (int e = 0; e < V; ++e) a[e] += to_float(g.v[e]);
     }
+    // a CTA whose chunks all lie inside one run leaves one partial sum, its first chunk's, for all of them
+    if (p.group > 1 && is_head) {
+        const int64_t c0 = (int64_t)blockIdx.x * p.group, r1 = (c0 + p.group) * L;       // (the same answer in all its threads)
+        if (c0 > 0 && r1 < p.n && p.pairs[c0 * L - 1].x == cur && p.pairs[r1].x == cur) {
+            float* const sums = reinterpret_cast<float*>(ring);
+            __syncthreads();                                                              // (the ring has been read)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sums[e * SUM_THREADS + threadIdx.x] = a[e];
+            __syncthreads();
+            if (c != c0) return;
+            for (int g = 1; g < p.group; ++g) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) a[e] += sums[e * SUM_THREADS + g * (int)p.vecs.d + threadIdx.x];
+            }
+        }
+    }
     flush_run<TO, V>(p, c, is_head, tail_part && cur == end_key, cur, col, a);
 }
 
 // Ids that span more than two chunks: CTA (x, y) takes the x-th, (x + grid)-th, ... of the list and 64 columns.  Sixteen stripes
 // of sixteen threads add every 16th chunk's partial sum, then the stripes are added in order.
 constexpr int JOIN_COLS = 64;
+__device__ __forceinline__ int64_t ceil_div_dev(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <typename TO, int L>
 __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
     constexpr int LANES = JOIN_COLS / 4, STRIPES = JOIN_THREADS / LANES, U = 8;
@@ -718,17 +737,21 @@ __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
             end += got;
             if (got < JOIN_THREADS) break;
         }
-        // partial sum j of the id: slot 1 of chunk c0, then slot 0 of the following ones; eight of a thread's on their way into shared
-        // memory at a time (with registers as their target they came one by one, 4.5 us a round of eight)
+        // partial sum j of the id: slot 1 of chunk c0, then slot 0 of the following ones, where a CTA of grad_sum_kernel that lies inside the
+        // run counts as one; eight of a thread's on their way into shared memory at a time (with registers as their target they came
+        // one by one, 4.5 us a round of eight)
+        const int64_t g0 = ceil_div_dev(c0 + 1, p.group), g1 = max(g0, end / p.group);    // those CTAs: [g0, g1)
+        const int64_t lead = g1 > g0 ? g0 * p.group - c0 : end - c0 + 1;                  // parts before the first of them
+        const int64_t parts = g1 > g0 ? lead + (g1 - g0) + (end - g1 * p.group + 1) : lead;
+        auto chunk_of = [&](int64_t j) { return j < lead ? c0 + j : (j < lead + g1 - g0 ? (g0 + j - lead) * p.group : g1 * p.group + j - lead - (g1 - g0)); };
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int64_t parts = end - c0 + 1;
         for (int64_t j0 = stripe; j0 < parts && col < p.part_ld; j0 += U * STRIPES) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t j = j0 + u * STRIPES;
                 if (j < parts)
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&ring[u][threadIdx.x])),
-                                 "l"(p.part + ((c0 + j) * 2 + (j == 0)) * p.part_ld + col) : "memory");
+                                 "l"(p.part + (chunk_of(j) * 2 + (j == 0)) * p.part_ld + col) : "memory");
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
@@ -788,6 +811,7 @@ int launch_small(SumParams& p, int vec, cudaStream_t s) {
 template <typename TG, typename TO, int L>
 int launch_sum(SumParams& p, int vec, cudaStream_t s) {
     p.vecs = FastDiv((uint32_t)(p.dim / vec));
+    p.group = SUM_THREADS % p.vecs.d == 0 ? SUM_THREADS / (int)p.vecs.d : 1;
     const dim3 grid((unsigned)ceil_div((int64_t)p.chunks * p.vecs.d, SUM_THREADS));
     const int rc = with_vector<sizeof(TG) == 2>(vec, [&](auto v) {
         return launch_status(launch_dependent(grad_sum_kernel<TG, TO, decltype(v)::value, L>, grid, dim3(SUM_THREADS), 0, s, p));

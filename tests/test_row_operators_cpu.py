@@ -27,7 +27,7 @@ DROPOUT = dict(x=PTR, x_type=F32, residual=None, out=PTR, out_type=F32, n=8, p=0
 QUANT = dict(x=PTR, x_type=F32, rows=4, cols=64, ldx=64, fp8_type=E4M3, block_rows=1, pow2=0, q=PTR, ldq=64, scales=PTR, qt=None, ldqt=0,
              scales_t=None, stream=None)
 MATMUL = dict(a=PTR, a_type=E4M3, lda=64, a_scales=PTR, a_block=1, b=PTR, b_type=E4M3, ldb=64, b_scales=PTR, b_block=128, addend=None, ld_addend=0,
-              out=PTR, out_type=F32, ld_out=32, M=16, N=32, K=64, scratch=PTR, scratch_bytes=1 << 40, status=None, stream=None)
+              out=PTR, out_type=F32, ld_out=32, M=16, N=32, K=64, status=None, stream=None)
 
 
 @pytest.mark.parametrize("over", [dict(table=None), dict(ids=None), dict(out=None), dict(table_type=E4M3), dict(out_type=7), dict(rows=0),
@@ -73,14 +73,6 @@ def test_calls_on_nothing_return_at_once(K):
     assert _call(K, "kge_dropout", DROPOUT, DROPOUT, n=0, x=None, out=None) == 0
     assert _call(K, "kge_fp8_quantize", QUANT, QUANT, rows=0) == 0
     assert _call(K, "kge_fp8_matmul", MATMUL, MATMUL, M=0, a=None) == 0
-
-
-def test_matmul_scratch_is_checked(K):
-    need = K.fp8_matmul_scratch_bytes(16, 32, 1 << 16)
-    if need:
-        assert _call(K, "kge_fp8_matmul", MATMUL, MATMUL, K=1 << 16, lda=1 << 16, ldb=1 << 16, scratch_bytes=need - 1) == -4
-        assert _call(K, "kge_fp8_matmul", MATMUL, MATMUL, K=1 << 16, lda=1 << 16, ldb=1 << 16, scratch=None) == -4
-    assert K.fp8_matmul_scratch_bytes(0, 32, 64) == 0 and K.fp8_matmul_scratch_bytes(-1, 32, 64) == 0
 
 
 def test_binding_features_in_8_bits_refuses(K):
