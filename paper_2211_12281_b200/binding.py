@@ -381,6 +381,8 @@ def fp8_quantize(x, q=None, scales=None, qt=None, scales_t=None, block_rows=1, p
     if code is None:
         raise _bad(w, "neither q nor qt is given")
     dev = _device_of(w, x, q, scales, qt, scales_t)
+    if rows == 0 or cols == 0:
+        return
     _call(w, lib().kge_fp8_quantize, dev, x.data_ptr(), tx, rows, cols, lx, code, block_rows, 1 if pow2 else 0, at[0], ld[0], at[1], at[2], ld[1], at[3])
 
 

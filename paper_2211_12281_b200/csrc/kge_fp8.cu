@@ -716,6 +716,7 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
             }
         }
+        __syncwarp();
         if (SPLIT) { cluster_sync(); cluster_sync(); }
     } else {
         registers_up<REGS_EPI>();

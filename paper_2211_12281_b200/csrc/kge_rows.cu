@@ -143,7 +143,7 @@ struct SortParams {
     int32_t *list_count, *status;
     // dense gradient rows set to zero by CTAs beside the sort's
     char* zero; int64_t zero_row_bytes, zero_ld_bytes, zero_first, zero_last;     // the rows, and which of them in this launch
-    int zero_vec;                         // rows are whole 16-byte words and lie back to back
+    int zero_flat;                        // the rows lie back to back
 };
 
 __device__ __forceinline__ uint32_t grad_key(const SortParams& p, int32_t id) {
@@ -157,11 +157,13 @@ __device__ __forceinline__ void zero_rows(const SortParams& p, int64_t cta, int6
     const int64_t first = cta * blockDim.x + threadIdx.x, step = ctas * blockDim.x;
     char* const base = p.zero + p.zero_first * p.zero_ld_bytes;
     const int64_t rows = p.zero_last - p.zero_first;
-    if (p.zero_vec) {
-        uint4* z = reinterpret_cast<uint4*>(base);
-        const int64_t words = rows * (p.zero_row_bytes / 16);
+    if (p.zero_flat) {
+        const int64_t all = rows * p.zero_row_bytes, head = min(all, (int64_t)(-reinterpret_cast<intptr_t>(base) & 15)), words = (all - head) / 16;
+        uint4* z = reinterpret_cast<uint4*>(base + head);
 #pragma unroll 4
         for (int64_t i = first; i < words; i += step) z[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (int64_t i = 2 * first; i < head; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
+        for (int64_t i = head + words * 16 + 2 * first; i < all; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
     } else {
         const int64_t halves = p.zero_row_bytes / 2, all = rows * halves;
         for (int64_t i = first; i < all; i += step) {
@@ -952,7 +954,7 @@ int kge_embedding_grad(const int32_t* ids, int32_t n, const void* grads, int32_t
     q.ids = ids; q.n = n; q.tiles = plan.tiles; q.bits = plan.bits; q.passes = plan.passes; q.rows = (uint32_t)rows; q.padding_id = padding_id;
     q.hist = g.hist; q.total = g.total; q.list_count = g.list_count; q.status = status;
     q.zero = static_cast<char*>(table_grad); q.zero_row_bytes = (int64_t)dim * tb; q.zero_ld_bytes = ld_table * tb;
-    q.zero_vec = ld_table == dim && aligned_to(table_grad, 16) && q.zero_row_bytes % 16 == 0;
+    q.zero_flat = ld_table == dim;
     int where = 0;
     const int rc = sort_ids(g, plan, q, !accumulate, rows, &where, s);
     if (rc != KGE_OK) return rc;

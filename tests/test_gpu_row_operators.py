@@ -173,15 +173,15 @@ def test_grad_of_strided_and_shifted_rows(T, K, n):
     g = _gen(T, n)
     E, d = 61, 24
     ids = _id_list(T, g, "zipf", n, E)
-    for extra, shift in ((8, 0), (3, 0), (0, 1), (4, 2)):
-        grads, out = _strided(T, n, d, T.bfloat16, extra, shift), _strided(T, E, d, T.float32, extra, shift)
+    for extra, shift, to in ((8, 0, T.float32), (3, 0, T.float32), (0, 1, T.float32), (4, 2, T.float32), (0, 3, T.bfloat16), (5, 1, T.float16)):
+        grads, out = _strided(T, n, d, T.bfloat16, extra, shift), _strided(T, E, d, to, extra, shift)
         grads.copy_(T.randn((n, d), generator=g, device="cuda"))
         all_of = out.as_strided((E, d + extra), (d + extra, 1), out.storage_offset()) if extra else None
         if extra:
             all_of[:-1, d:] = 5.0
         out.fill_(3.0)
         K.embedding_grad(ids, grads, out)
-        plain = T.full((E, d), 3.0, device="cuda")
+        plain = T.full((E, d), 3.0, device="cuda", dtype=to)
         K.embedding_grad(ids, grads.contiguous(), plain)
         assert T.equal(out, plain)                   # where the rows lie changes nothing
         if extra:
@@ -678,6 +678,52 @@ def test_captured_runs_replay_beside_eager_ones(T, K):
         for _, _, got, want, _ in made:
             for k in want:
                 assert T.equal(got[k], want[k]), k
+
+
+def test_first_calls_of_a_process_can_be_captured():
+    """Nothing that a first call sets up (kernel attributes, tensor maps, what the device offers) needs to happen outside a capture."""
+    import subprocess
+    import sys
+    from pathlib import Path
+    code = r"""
+import torch
+import paper_2211_12281_b200 as K
+dev = "cuda"
+e8 = lambda r, c: torch.empty((r, c), dtype=torch.float8_e4m3fn, device=dev)
+ids = torch.arange(5000, dtype=torch.int32, device=dev) % 700
+table, rows, dt = torch.randn((700, 64), device=dev), torch.zeros((5000, 64), device=dev), torch.zeros((700, 64), device=dev)
+w, wq, ws = torch.randn((128, 64), device=dev), e8(128, 64), torch.empty((1, 1), device=dev)
+q, s, y = e8(5000, 64), torch.empty((1, 5000), device=dev), torch.zeros((5000, 128), device=dev)
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    K.embedding_lookup(table, ids, rows)
+    K.dropout(rows, rows, 0.5, 3)
+    K.fp8_quantize(rows, q, s)
+    K.fp8_quantize(w, wq, ws, block_rows=128)
+    K.fp8_matmul(q, s, wq, ws, y)
+    K.embedding_grad(ids, rows, dt)
+g.replay()
+torch.cuda.synchronize()
+a = [t.clone() for t in (rows, y, dt)]
+K.embedding_lookup(table, ids, rows)
+K.dropout(rows, rows, 0.5, 3)
+K.fp8_quantize(rows, q, s)
+K.fp8_quantize(w, wq, ws, block_rows=128)
+K.fp8_matmul(q, s, wq, ws, y)
+K.embedding_grad(ids, rows, dt)
+assert all(torch.equal(x, t) for x, t in zip(a, (rows, y, dt))) and float(a[1].abs().sum()) > 0 and float(a[2].abs().sum()) > 0
+"""
+    res = subprocess.run([sys.executable, "-c", code], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stderr[-2000:]
+
+
+def test_calls_on_nothing(T, K):
+    i0 = T.empty(0, dtype=T.int32, device="cuda")
+    K.embedding_lookup(T.ones((3, 8), device="cuda"), i0, T.empty((0, 8), device="cuda"))
+    K.dropout(T.empty(0, device="cuda"), T.empty(0, device="cuda"), 0.5, 1)
+    K.fp8_quantize(T.empty((0, 64), device="cuda"), _empty8(T, 0, 64, "e4m3"), T.empty((1, 0), device="cuda"))
+    b, sb = _operand(T, K, _gen(T, 1), 32, 64, "e4m3", 1)
+    K.fp8_matmul(_empty8(T, 0, 64, "e4m3"), T.empty((1, 0), device="cuda"), b, sb, T.empty((0, 32), device="cuda"))
 
 
 def test_scratch_of_the_callers_is_used_and_checked(T, K):
