@@ -383,7 +383,7 @@ struct ProductParams {
     int a_square, b_square;               // a scale serves 128 rows
     const void* addend; int64_t ld_addend;
     void* out; int64_t ld_out; int out_type;
-    int vec;                              // rows of out (and addend) start at multiples of 16 bytes
+    int vec, twos;                        // rows of out (and addend) start at multiples of 16 bytes; of two elements, N even
     int32_t* status; int wait_limit;
     uint32_t idesc;
 };
@@ -457,6 +457,19 @@ __device__ __forceinline__ void fp_put(const ProductParams& p, int row, int col,
     }
 }
 
+// Where rows do not start at multiples of 16 bytes, and at the matrix's edges: f(row, column, place in shared memory) for W elements at a
+// time of the warp's 32 rows x ROW bytes, lanes side by side along the columns.
+template <typename TO, int ROW, int W, class F>
+__device__ __forceinline__ void fp_each(const ProductParams& p, int row0, int col0, float4* st, int lane, F&& f) {
+    constexpr int V = 16 / sizeof(TO), UNITS = ROW / 16, TURN = UNITS == 2 ? 2 : 0, PER_ROW = ROW / (int)sizeof(TO) / W;
+#pragma unroll 4
+    for (int i = 0; i < PER_ROW; ++i) {
+        const int at = i * 32 + lane, r = at / PER_ROW, c = at % PER_ROW * W;
+        if (row0 + r < p.M && col0 + c < p.N)
+            f(row0 + r, col0 + c, reinterpret_cast<TO*>(st) + (r * UNITS + ((c / V) ^ ((r >> TURN) & (UNITS - 1)))) * V + c % V);
+    }
+}
+
 // A warp's 32 rows x 64 columns, ROW bytes of each row at a time through shared memory, so that a store instruction covers whole
 // 32-byte sectors, or, with 128 bytes, whole lines.  (16-byte unit i of row r lies at i ^ (r mod units): no bank conflicts.)
 template <typename TO, int ROW>
@@ -490,15 +503,12 @@ __device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int c
                 *reinterpret_cast<float4*>(dst) = st[r * UNITS + (unit ^ ((r >> TURN) & (UNITS - 1)))];
                 dst += step;
             }
+        } else if (sizeof(TO) == 2 && p.twos) {
+            fp_each<TO, ROW, 2>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) {
+                *reinterpret_cast<uint32_t*>(static_cast<TO*>(p.out) + row * p.ld_out + col) = *reinterpret_cast<const uint32_t*>(at);
+            });
         } else {
-#pragma unroll 1
-            for (int j = 0; j < UNITS; ++j) {
-                const int r = j * (32 / UNITS) + r0, row = row0 + r, col = col0 + c + V * unit;
-                if (row < p.M && col < p.N) {
-                    const float4 w = st[r * UNITS + (unit ^ ((r >> TURN) & (UNITS - 1)))];
-                    fp_put<TO, V>(p, row, col, *reinterpret_cast<const Pack<TO, V>*>(&w));
-                }
-            }
+            fp_each<TO, ROW, 1>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { static_cast<TO*>(p.out)[row * p.ld_out + col] = *at; });
         }
         __syncwarp();
     }
@@ -506,18 +516,26 @@ __device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int c
 
 // The addend of the same tile joins the accumulators in fp32 before they are rounded.
 // With 128-byte rows it passes through the warp's shared memory: fp_fetch_addend starts the copies of a pass (the first one's while
-// the tile is computed), fp_add waits for them.
+// the tile is computed), fp_add_staged waits for them.
+// (a copy takes 16 bytes, or 4: two 16-bit elements; rows of 16-bit elements that start in between are read by the lanes themselves)
 template <typename TO>
 __device__ __forceinline__ void fp_fetch_addend(const ProductParams& p, int row0, int col0, int c, float4* st, int lane) {
-    constexpr int V = 16 / sizeof(TO);
-    const int unit = lane & 7, col = col0 + c + V * unit;
-    const int bytes = min(V, (int)p.N - col) * (int)sizeof(TO);
+    constexpr int V = 16 / sizeof(TO), FOUR = 4 / (int)sizeof(TO);
+    const TO* const add = static_cast<const TO*>(p.addend);
+    if (p.vec) {
+        const int unit = lane & 7, col = col0 + c + V * unit;
+        const int bytes = min(V, (int)p.N - col) * (int)sizeof(TO);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int r = j * 4 + (lane >> 3), row = row0 + r;
-        if (row < p.M && bytes > 0)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(st + r * 8 + (unit ^ (r & 7)))),
-                         "l"(static_cast<const TO*>(p.addend) + row * p.ld_addend + col), "r"(bytes) : "memory");
+        for (int j = 0; j < 8; ++j) {
+            const int r = j * 4 + (lane >> 3), row = row0 + r;
+            if (row < p.M && bytes > 0)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(st + r * 8 + (unit ^ (r & 7)))), "l"(add + row * p.ld_addend + col),
+                             "r"(bytes) : "memory");
+        }
+    } else if (sizeof(TO) == 4 || p.twos) {
+        fp_each<TO, 128, FOUR>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { fp_copy4(smem_u32(at), reinterpret_cast<const float*>(add + row * p.ld_addend + col)); });
+    } else {
+        fp_each<TO, 128, 1>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { *at = add[row * p.ld_addend + col]; });
     }
 }
 template <typename TO>
@@ -538,7 +556,7 @@ __device__ __forceinline__ void fp_add_staged(const ProductParams& p, int row0, 
         __syncwarp();
     }
 }
-// Otherwise a lane reads its own row, a 32-byte sector at a time (fetched into L2 when the tile began).
+// Or a lane reads its own row, a 32-byte sector at a time (fetched into L2 when the tile began).
 template <typename TO>
 __device__ __forceinline__ void fp_add_rows(const ProductParams& p, int row, int col0, uint64_t (&acc)[FP_COLS / 2]) {
     constexpr int V = 16 / sizeof(TO);
@@ -732,8 +750,8 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
             for (int i = 0; i < FP_COLS / 2; ++i) acc[i] = 0ull;
             if (!SPLIT && p.addend) fp_with_out(p.out_type, [&](auto t) {
                 using TO = decltype(t);
-                if (STORE_ROW == 128 && p.vec) fp_fetch_addend<TO>(p, m0, n0, 0, st, lane);
-                if (STORE_ROW != 128 || !p.vec || sizeof(TO) == 4) fp_prefetch_addend<TO>(p, m0 + lane, n0);
+                if constexpr (STORE_ROW == 128) fp_fetch_addend<TO>(p, m0, n0, 0, st, lane);
+                if (STORE_ROW != 128 || sizeof(TO) == 4) fp_prefetch_addend<TO>(p, m0 + lane, n0);
             });
 #pragma unroll 1
             for (int kb = kb0; kb < kb1; ++kb) {
@@ -786,7 +804,7 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 fp_with_out(p.out_type, [&](auto t) {
                     using TO = decltype(t);
                     if (p.addend) {
-                        if (STORE_ROW == 128 && p.vec) fp_add_staged<TO>(p, m0, n0, acc, st, lane);
+                        if constexpr (STORE_ROW == 128) fp_add_staged<TO>(p, m0, n0, acc, st, lane);
                         else fp_add_rows<TO>(p, m0 + lane, n0, acc);
                     }
                     fp_store<TO, STORE_ROW>(p, m0, n0, acc, st, lane);
@@ -848,7 +866,7 @@ int sm_count(int* sms) {
 
 // How a product is cut up: columns of a tile, and CTAs that share a tile's blocks of K.
 struct ProductPlan { int form, split; };
-ProductPlan product_plan(int64_t M, int64_t N, int kblocks, int sms) {
+ProductPlan product_plan(int64_t M, int64_t N, int kblocks, bool ragged_addend, int sms) {
     const int64_t tiles128 = ceil_div(M, FP_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, FP_BM) * ceil_div(N, 256);
     if (tiles128 < sms && kblocks > 1) {
         int split = (int)std::min<int64_t>({8, kblocks, std::max<int64_t>(1, sms / tiles128)});
@@ -856,7 +874,9 @@ ProductPlan product_plan(int64_t M, int64_t N, int kblocks, int sms) {
         split = (kblocks + per - 1) / per;              // every CTA has a block
         if (split > 1) return {FP_SPLIT, split};
     }
-    if (tiles256 >= sms && kblocks >= 16) return {FP_WIDE, 1};
+    // (an addend whose rows are not whole 16-byte words passes through shared memory that the wide form has not: 187 us there, 137 in
+    // pairs at 4096 x 4095 x 4096)
+    if (tiles256 >= sms && kblocks >= 16 && !ragged_addend) return {FP_WIDE, 1};
     // few blocks of K: memory sets the pace, and what counts is how well whole rounds of tiles fill the SMs
     const int64_t pair = ceil_div(tiles128, 2 * sms) * 256, narrow = ceil_div(ceil_div(M, FP_BM) * ceil_div(N, 64), 3 * sms) * 192;
     return {narrow < pair ? FP_NARROW : FP_PAIR, 1};
@@ -928,11 +948,12 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
     p.addend = addend; p.ld_addend = ld_addend; p.out = out; p.ld_out = ld_out; p.out_type = out_type;
     const int ob = type_bytes(out_type);
     p.vec = ld_out * ob % 16 == 0 && aligned_to(out, 16) && (!addend || (ld_addend * ob % 16 == 0 && aligned_to(addend, 16)));
+    p.twos = N % 2 == 0 && ld_out % 2 == 0 && aligned_to(out, 2 * ob) && (!addend || (ld_addend % 2 == 0 && aligned_to(addend, 2 * ob)));
     p.status = status; p.wait_limit = kDefaultWaitLimit;
     int sms = 0, rc = sm_count(&sms);
     if (rc != KGE_OK) return rc;
     if (ceil_div(M, 128) * ceil_div(N, 64) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;
-    const ProductPlan plan = product_plan(M, N, p.kblocks, sms);
+    const ProductPlan plan = product_plan(M, N, p.kblocks, addend && !p.vec, sms);
     alignas(64) CUtensorMap ma, mb;
     rc = operand_map(&ma, a, M, K, lda, FP_BM);
     if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb, fp_box_rows(plan.form));

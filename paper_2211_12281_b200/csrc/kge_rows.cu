@@ -4,7 +4,7 @@
 // The gradient sorts the ids (stable radix sort of (id, position) pairs), walks the sorted list in chunks of rows, adds a chunk's
 // rows of one id in fp32 in ascending position, and joins the ids that span chunks in a second, fixed order: the result is a
 // function of the inputs alone.  Rows of the dense gradient that no id names are set to zero by CTAs beside the sort's.
-//   up to 1,024 ids     one launch: every CTA owns a range of table rows, picks the ids that fall into it and sorts those
+//   short lists         one launch: every CTA owns a range of table rows, picks the ids that fall into it and sorts those
 //   up to 65,536        one cluster of sixteen CTAs sorts in shared memory, exchanging counts and pairs between its CTAs
 //   more                hist     digit counts of every tile, per pass (counted by atomics while the pass before scatters, frequent ids cost 12 us of 24)
 //                       scan     the counts become sums over the tiles before
@@ -26,10 +26,10 @@ struct LookupParams {
     const void* table; void* out;
     const int32_t* ids;
     int64_t rows, ld_table, ld_out;
-    int n, rows_per_cta;
+    int n, dim, rows_per_cta;
     int32_t padding_id;
     float scale;
-    FastDiv vecs;                 // packs per row
+    FastDiv vecs;                 // packs per row (of four single elements in lookup_single_kernel)
     int32_t* status;
 };
 
@@ -79,6 +79,31 @@ __global__ void __launch_bounds__(LOOKUP_THREADS) lookup_kernel(LookupParams p) 
     }
 }
 
+// Rows that are no whole packs: four single elements an item, so that finding an item's row and place is shared by four.
+template <typename TT, typename TO>
+__global__ void __launch_bounds__(LOOKUP_THREADS) lookup_single_kernel(LookupParams p) {
+    grid_dependency_wait();
+    allow_dependents();
+    const TT* table = static_cast<const TT*>(p.table);
+    TO* out = static_cast<TO*>(p.out);
+    const int r0 = blockIdx.x * p.rows_per_cta, nr = min(p.rows_per_cta, p.n - r0);
+    const uint32_t items = (uint32_t)nr * p.vecs.d;
+    for (uint32_t i = threadIdx.x; i < items; i += LOOKUP_THREADS) {
+        const uint32_t r = p.vecs.div(i), col = (i - r * p.vecs.d) * 4;
+        const int row = r0 + (int)r, m = min(4, p.dim - (int)col);
+        const int32_t id = p.ids[row];
+        const bool in = id >= 0 && id < p.rows, real = in && id != p.padding_id;
+        if (!in && id != p.padding_id) note_status(p.status, KGE_ERR_ID_RANGE);
+        const TT* src = table + (real ? id : 0) * p.ld_table + col;
+        TO* dst = out + row * p.ld_out + col;
+        TT v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = src[e < m ? e : 0];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (e < m) dst[e] = from_float<TO>(real ? to_float(v[e]) * p.scale : 0.f);
+    }
+}
+
 // ---- gradient --------------------------------------------------------------------------------------------------------
 
 constexpr int GS_THREADS = 256, GS_WARPS = GS_THREADS / 32, GS_ITEMS = 8;
@@ -86,7 +111,8 @@ constexpr int GS_TILE = GS_THREADS * GS_ITEMS;     // ids per CTA of the sort in
 constexpr int GS_MAX_BITS = 9;
 constexpr int CS_CTAS = 16, CS_CTAS_PORTABLE = 8, CS_THREADS = 512, CS_WARPS = CS_THREADS / 32, CS_ITEMS = 16;      // the cluster's sort
 constexpr int CS_SHARE = CS_THREADS * CS_ITEMS, CS_MAX = CS_CTAS_PORTABLE * CS_SHARE, CS_MAX_BITS = 11;
-constexpr int SMALL_MAX = 1024, SMALL_THREADS = 256;
+constexpr int SMALL_MAX = 2048, SMALL_THREADS = 256, SMALL_BITS = 11;      // (SMALL_BITS: of a position)
+static_assert(SMALL_MAX == 1 << SMALL_BITS, "positions of a short list");
 constexpr int SUM_THREADS = 256;
 constexpr int JOIN_THREADS = 256;
 
@@ -102,6 +128,9 @@ SortPlan sort_plan(int64_t rows, int n) {
     s.bits = (s.key_bits + s.passes - 1) / s.passes;
     return s;
 }
+// One CTA adds up all rows of an id: longer lists only where ids can be expected to differ (a list of one id takes 25 us at 1,024
+// rows of 1 KB, about what the sort does).
+bool short_list(int64_t rows, int n) { return n <= SMALL_MAX / 2 || (n <= SMALL_MAX && rows >= 4ll * n); }
 int chunk_rows(int n) { return n < (1 << 17) ? 8 : 32; }
 
 struct GradScratch {
@@ -119,7 +148,7 @@ GradScratch carve_grad(char* base, int64_t rows, int dim, int n) {
     const SortPlan s = sort_plan(rows, n);
     const int64_t chunks = ceil_div(n, chunk_rows(n));
     GradScratch g{};
-    if (n <= SMALL_MAX) return g;       // (one launch: nothing is kept)
+    if (short_list(rows, n)) return g;       // (one launch: nothing is kept)
     for (int i = 0; i < (n > CS_MAX ? 2 : 1); ++i) g.pairs[i] = reinterpret_cast<uint2*>(take((size_t)n * 8));
     if (n > CS_MAX) {
         g.hist = reinterpret_cast<uint32_t*>(take((size_t)s.tiles * (4u << s.bits)));
@@ -152,25 +181,28 @@ __device__ __forceinline__ uint32_t grad_key(const SortParams& p, int32_t id) {
     return (uint32_t)id;
 }
 
+// Bytes [base, base + all) (whole 16-bit elements) set to zero by thread `first` of `step`.
+__device__ __forceinline__ void zero_bytes(char* base, int64_t all, int64_t first, int64_t step) {
+    const int64_t head = min(all, (int64_t)(-reinterpret_cast<intptr_t>(base) & 15)), words = (all - head) / 16;
+    uint4* z = reinterpret_cast<uint4*>(base + head);
+#pragma unroll 4
+    for (int64_t i = first; i < words; i += step) z[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int64_t i = 2 * first; i < head; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
+    for (int64_t i = head + words * 16 + 2 * first; i < all; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
+}
+__device__ __forceinline__ void zero_strided(char* base, int64_t rows, int64_t row_bytes, int64_t ld_bytes, int64_t first, int64_t step) {
+    const int64_t halves = row_bytes / 2, all = rows * halves;
+    for (int64_t i = first; i < all; i += step) {
+        const int64_t r = i / halves;
+        *reinterpret_cast<uint16_t*>(base + r * ld_bytes + (i - r * halves) * 2) = 0;
+    }
+}
 // Rows [zero_first, zero_last) by CTA `cta` of `ctas`.
 __device__ __forceinline__ void zero_rows(const SortParams& p, int64_t cta, int64_t ctas) {
-    const int64_t first = cta * blockDim.x + threadIdx.x, step = ctas * blockDim.x;
+    const int64_t first = cta * blockDim.x + threadIdx.x, step = ctas * blockDim.x, rows = p.zero_last - p.zero_first;
     char* const base = p.zero + p.zero_first * p.zero_ld_bytes;
-    const int64_t rows = p.zero_last - p.zero_first;
-    if (p.zero_flat) {
-        const int64_t all = rows * p.zero_row_bytes, head = min(all, (int64_t)(-reinterpret_cast<intptr_t>(base) & 15)), words = (all - head) / 16;
-        uint4* z = reinterpret_cast<uint4*>(base + head);
-#pragma unroll 4
-        for (int64_t i = first; i < words; i += step) z[i] = make_uint4(0u, 0u, 0u, 0u);
-        for (int64_t i = 2 * first; i < head; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
-        for (int64_t i = head + words * 16 + 2 * first; i < all; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
-    } else {
-        const int64_t halves = p.zero_row_bytes / 2, all = rows * halves;
-        for (int64_t i = first; i < all; i += step) {
-            const int64_t r = i / halves;
-            *reinterpret_cast<uint16_t*>(base + r * p.zero_ld_bytes + (i - r * halves) * 2) = 0;
-        }
-    }
+    if (p.zero_flat) zero_bytes(base, rows * p.zero_row_bytes, first, step);
+    else zero_strided(base, rows, p.zero_row_bytes, p.zero_ld_bytes, first, step);
 }
 
 // The lanes (of those that are `in`) that hold this lane's digit of at most BITS bits: a vote per bit, all of them independent.
@@ -458,7 +490,7 @@ __device__ __forceinline__ void finish_pack(const SumParams& p, uint32_t row, in
     *reinterpret_cast<Pack<TO, V>*>(dst) = o;
 }
 
-// ---- up to 1,024 ids: one launch ----
+// ---- short lists: one launch ----
 
 // CTA c owns the table rows [c rows_per_cta, + rows_per_cta): it picks the ids that name them, sorts those as (row, position) words
 // in shared memory, and adds up each row's gradients: runs of up to SHORT by one group of threads (a pack of columns each),
@@ -466,7 +498,7 @@ __device__ __forceinline__ void finish_pack(const SumParams& p, uint32_t row, in
 template <typename TG, typename TO, int V>
 __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) {
     constexpr int SHORT = 32, U = 8;
-    __shared__ uint32_t list[SMALL_MAX];       // local row << 10 | position
+    __shared__ uint32_t list[SMALL_MAX];       // local row << SMALL_BITS | position
     __shared__ uint16_t start[SMALL_MAX + 1];
     __shared__ uint32_t warp_cnt[SMALL_THREADS / 32];
     __shared__ float red[SMALL_THREADS * V];
@@ -491,14 +523,10 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
         }
     }
     if (!p.accumulate) {
-        const uint32_t items = (uint32_t)nr * p.vecs.d;       // (rows_per_cta keeps this below 2^31)
-        Pack<TO, V> z;
-#pragma unroll
-        for (int e = 0; e < V; ++e) z.v[e] = from_float<TO>(0.f);
-        for (uint32_t i = tid; i < items; i += SMALL_THREADS) {
-            const uint32_t r = p.vecs.div(i);
-            *reinterpret_cast<Pack<TO, V>*>(static_cast<TO*>(p.out) + (r0 + r) * p.ld_out + (int64_t)(i - r * p.vecs.d) * V) = z;
-        }
+        char* const base = static_cast<char*>(p.out) + r0 * p.ld_out * (int64_t)sizeof(TO);
+        const int64_t row = (int64_t)p.dim * sizeof(TO);
+        if (p.ld_out == p.dim) zero_bytes(base, nr * row, tid, SMALL_THREADS);
+        else zero_strided(base, nr, row, p.ld_out * (int64_t)sizeof(TO), tid, SMALL_THREADS);
     }
     int incl = mine;
 #pragma unroll
@@ -511,7 +539,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
     if (m == 0) return;
 #pragma unroll
     for (int k = 0; k < SMALL_MAX / SMALL_THREADS; ++k)
-        if (id[k] >= 0) list[at++] = (uint32_t)id[k] << 10 | (uint32_t)(tid * (SMALL_MAX / SMALL_THREADS) + k);
+        if (id[k] >= 0) list[at++] = (uint32_t)id[k] << SMALL_BITS | (uint32_t)(tid * (SMALL_MAX / SMALL_THREADS) + k);
     int m2 = 1;
     while (m2 < m) m2 <<= 1;
     for (int i = m + tid; i < m2; i += SMALL_THREADS) list[i] = ~0u;
@@ -530,7 +558,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
 #pragma unroll
     for (int k = 0; k < SMALL_MAX / SMALL_THREADS; ++k) {
         const int i = tid * (SMALL_MAX / SMALL_THREADS) + k;
-        if (i < m && (i == 0 || list[i] >> 10 != list[i - 1] >> 10)) heads |= 1 << k;
+        if (i < m && (i == 0 || list[i] >> SMALL_BITS != list[i - 1] >> SMALL_BITS)) heads |= 1 << k;
     }
     incl = __popc(heads);
 #pragma unroll
@@ -553,7 +581,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
             Pack<TG, V> g[U];
 #pragma unroll
             for (int q = 0; q < U; ++q)        // (beyond the end: the first again, for nothing -- a load under a condition waits for its use)
-                g[q] = load_now<Pack<TG, V>>(grads + (int64_t)(list[i + q * step < end ? i + q * step : i] & 1023u) * p.ld_grads + col);
+                g[q] = load_now<Pack<TG, V>>(grads + (int64_t)(list[i + q * step < end ? i + q * step : i] & (SMALL_MAX - 1)) * p.ld_grads + col);
 #pragma unroll
             for (int q = 0; q < U; ++q)
 #pragma unroll
@@ -569,7 +597,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
 #pragma unroll
                 for (int q = 0; q < V; ++q) a[q] = 0.f;
                 add_rows(s, e, 1, (int64_t)c * V, a);
-                finish_pack<TO, V>(p, (uint32_t)(r0 + (list[s] >> 10)), (int64_t)c * V, a);
+                finish_pack<TO, V>(p, (uint32_t)(r0 + (list[s] >> SMALL_BITS)), (int64_t)c * V, a);
             }
         }
     for (int r = 0; r < runs; ++r) {
@@ -588,7 +616,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
 #pragma unroll
                     for (int q = 0; q < V; ++q) a[q] += red[(g * wide + v0) * V + q];
                 }
-                finish_pack<TO, V>(p, (uint32_t)(r0 + (list[s] >> 10)), (int64_t)c * V, a);
+                finish_pack<TO, V>(p, (uint32_t)(r0 + (list[s] >> SMALL_BITS)), (int64_t)c * V, a);
             }
             __syncthreads();
         }
@@ -674,10 +702,7 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
     for (int e = 0; e < V; ++e) a[e] = 0.f;
     uint32_t cur = pairs[from].x;
     bool is_head = head_part;
-#pragma unroll 1
-    for (int i = from; i < to; ++i) {
-        issue(i + SUM_DEPTH - 1);
-        const uint32_t k = pairs[i].x;
+    auto add = [&](uint32_t k, const Pack<TG, V>& g) {
         if (k != cur) {
             flush_run<TO, V>(p, c, is_head, false, cur, col, a);
             is_head = false;
@@ -685,15 +710,33 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
 #pragma unroll
             for (int e = 0; e < V; ++e) a[e] = 0.f;
         }
-        Pack<TG, V> g;
-        if constexpr (ASYNC) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(SUM_DEPTH - 1) : "memory");
-            g = *reinterpret_cast<const Pack<TG, V>*>(ring + (i % SUM_DEPTH) * (SUM_THREADS * BYTES) + threadIdx.x * BYTES);
-        } else {
-            g = *reinterpret_cast<const Pack<TG, V>*>(grads + (int64_t)pairs[i].y * p.ld_grads);
-        }
 #pragma unroll
         for (int e = 0; e < V; ++e) a[e] += to_float(g.v[e]);
+    };
+    if constexpr (ASYNC) {
+#pragma unroll 1
+        for (int i = from; i < to; ++i) {
+            issue(i + SUM_DEPTH - 1);
+            const uint32_t k = pairs[i].x;
+            asm volatile("cp.async.wait_group %0;" ::"n"(SUM_DEPTH - 1) : "memory");
+            add(k, *reinterpret_cast<const Pack<TG, V>*>(ring + (i % SUM_DEPTH) * (SUM_THREADS * BYTES) + threadIdx.x * BYTES));
+        }
+    } else {             // single 16-bit elements: eight rows' loads together
+#pragma unroll 1
+        for (int i0 = from; i0 < to; i0 += SUM_DEPTH) {
+            Pack<TG, V> g[SUM_DEPTH];
+            uint32_t k[SUM_DEPTH];
+#pragma unroll
+            for (int u = 0; u < SUM_DEPTH; ++u) {
+                const uint2 at = pairs[min(i0 + u, to - 1)];
+                k[u] = at.x;
+                g[u] = load_now<Pack<TG, V>>(grads + (int64_t)at.y * p.ld_grads);
+            }
+#pragma unroll
+            for (int u = 0; u < SUM_DEPTH; ++u) asm volatile("" ::"h"(*reinterpret_cast<const uint16_t*>(&g[u])));
+#pragma unroll
+            for (int u = 0; u < SUM_DEPTH; ++u) if (i0 + u < to) add(k[u], g[u]);
+        }
     }
     // a CTA whose chunks all lie inside one run leaves one partial sum, its first chunk's, for all of them
     if (p.group > 1 && is_head) {
@@ -785,12 +828,14 @@ template <bool EIGHT, class F> int with_vector(int vec, F&& f) {
 }
 
 int launch_lookup(LookupParams& p, int tt, int to, int vec, int dim, cudaStream_t s) {
-    p.vecs = FastDiv((uint32_t)(dim / vec));
+    p.dim = dim;
+    p.vecs = FastDiv((uint32_t)(vec == 1 ? ceil_div(dim, 4) : dim / vec));
     p.rows_per_cta = (int)std::max<int64_t>(1, LOOKUP_THREADS * LOOKUP_UNROLL / p.vecs.d);
     const dim3 grid((unsigned)ceil_div(p.n, p.rows_per_cta));
     return with_type(tt, [&](auto a) {
         return with_type(to, [&](auto b) {
             using TT = decltype(a); using TO = decltype(b);
+            if (vec == 1) return launch_status(launch_dependent(lookup_single_kernel<TT, TO>, grid, dim3(LOOKUP_THREADS), 0, s, p));
             return with_vector<sizeof(TT) == 2 || sizeof(TO) == 2>(vec, [&](auto v) {
                 return launch_status(launch_dependent(lookup_kernel<TT, TO, decltype(v)::value>, grid, dim3(LOOKUP_THREADS), 0, s, p));
             });
@@ -801,9 +846,9 @@ int launch_lookup(LookupParams& p, int tt, int to, int vec, int dim, cudaStream_
 template <typename TG, typename TO>
 int launch_small(SumParams& p, int vec, cudaStream_t s) {
     p.vecs = FastDiv((uint32_t)(p.dim / vec));
-    // four CTAs an SM, more where a CTA's words would not fit 31 bits or its rows 22
+    // four CTAs an SM, more where a CTA's rows would not fit the words it sorts
     int64_t per = ceil_div(p.rows, 148 * 4);
-    per = std::max<int64_t>(1, std::min<int64_t>({per, (1ll << 22) - 1, ((1ll << 31) - 1) / p.vecs.d}));
+    per = std::max<int64_t>(1, std::min<int64_t>(per, (1ll << (32 - SMALL_BITS)) - 1));
     p.rows_per_cta = (int)per;
     return with_vector<sizeof(TG) == 2>(vec, [&](auto v) {
         return launch_status(launch_dependent(grad_small_kernel<TG, TO, decltype(v)::value>, dim3((unsigned)ceil_div(p.rows, per)), dim3(SMALL_THREADS), 0, s, p));
@@ -946,7 +991,7 @@ int kge_embedding_grad(const int32_t* ids, int32_t n, const void* grads, int32_t
     p.n = n; p.dim = dim; p.part_ld = (dim + 3) / 4 * 4; p.rows = (uint32_t)rows;
     p.grads = grads; p.ld_grads = ld_grads; p.out = table_grad; p.ld_out = ld_table; p.scale = scale; p.accumulate = accumulate;
     p.ids = ids; p.padding_id = padding_id; p.status = status;
-    if (n <= SMALL_MAX)
+    if (short_list(rows, n))
         return with_type(grads_type, [&](auto a) { return with_type(table_type, [&](auto b) { return launch_small<decltype(a), decltype(b)>(p, vec, s); }); });
     const GradScratch g = carve_grad(static_cast<char*>(scratch), rows, dim, n);
     const SortPlan plan = sort_plan(rows, n);

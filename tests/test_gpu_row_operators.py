@@ -57,7 +57,7 @@ def _strided(T, rows, cols, dtype, extra=0, shift=0):
     (1, 1, 1, "f32", "f32", 1.0, 0, 0), (1, 1000, 256, "bf16", "bf16", 16.0, 0, 0), (5, 7, 5, "f32", "bf16", 0.3, 0, 0),
     (33, 100, 8, "bf16", "f32", 1.0, 0, 0), (1000, 50, 200, "f16", "f16", -2.5, 0, 0), (257, 300, 33, "f16", "f32", 1.7, 3, 1),
     (64, 300, 64, "f32", "f32", 1.0, 4, 0), (64, 300, 64, "f32", "f32", 1.0, 0, 1), (4097, 900, 128, "f32", "f16", 0.125, 0, 0),
-    (77, 9, 4096, "bf16", "bf16", 1.0, 8, 0), (3, 9, 1000, "bf16", "f16", 3.0, 0, 2), (24_576, 5000, 20, "f32", "f32", 4.472, 0, 0)])
+    (77, 9, 4096, "bf16", "bf16", 1.0, 8, 0), (3000, 70, 45, "bf16", "f16", 2.0, 0, 0), (100, 70, 46, "f32", "bf16", 2.0, 1, 1), (9, 70, 3, "f16", "f32", 2.0, 0, 0), (3, 9, 1000, "bf16", "f16", 3.0, 0, 2), (24_576, 5000, 20, "f32", "f32", 4.472, 0, 0)])
 def test_lookup(T, K, n, E, d, tt, to, scale, extra, shift):
     g = _gen(T, n + d)
     table = _strided(T, E, d, _type(T, tt), extra, shift)
@@ -134,7 +134,8 @@ def _id_list(T, g, kind, n, E):
     (1, 1, 1, "one", "f32", "f32", 1.0, False), (1, 1000, 32, "zipf", "f32", "f32", 2.0, True), (7, 3, 5, "zipf", "bf16", "f32", 0.5, False),
     (33, 50, 8, "padded", "f16", "f16", 1.0, False), (256, 1000, 32, "zipf", "f32", "f32", 1.0, False), (256, 1000, 32, "one", "f32", "bf16", 1.0, True),
     (1000, 100_000, 64, "distinct", "bf16", "bf16", 1.0, False), (1025, 77, 100, "blocks", "f32", "f32", -1.5, True),
-    (2048, 5, 24, "zipf", "f32", "f32", 1.0, False), (2049, 4000, 200, "blocks", "bf16", "f32", 1.0, False), (2049, 2100, 8, "distinct", "f32", "f32", 1.0, False),
+    (2048, 5, 24, "zipf", "f32", "f32", 1.0, False), (2048, 8192, 40, "one", "f32", "f32", 1.0, False), (2047, 70_001, 33, "blocks", "bf16", "bf16", 0.5, True),
+    (2000, 900_000, 9, "padded", "f32", "f16", 1.0, False), (30_000, 255, 141, "zipf", "bf16", "bf16", 1.0, False), (150_000, 255, 15, "blocks", "f16", "f32", 1.0, True), (2049, 4000, 200, "blocks", "bf16", "f32", 1.0, False), (2049, 2100, 8, "distinct", "f32", "f32", 1.0, False),
     (5000, 300, 33, "blocks", "f16", "f32", 1.0, False), (5000, 1, 260, "one", "f32", "f32", 0.01, False), (24_576, 100_000, 128, "zipf", "f32", "f32", 1.0, False),
     (24_576, 3000, 520, "padded", "bf16", "f16", 0.01, True), (40_000, 70_000, 7, "blocks", "f32", "f32", 1.0, False),
     (131_071, 999, 16, "blocks", "bf16", "f32", 1.0, False), (131_072, 1000, 16, "blocks", "bf16", "f32", 1.0, False),

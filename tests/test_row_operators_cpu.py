@@ -87,10 +87,11 @@ def test_binding_features_in_8_bits_refuses(K):
 
 def test_scratch_sizes_cover_their_lists(K):
     # a list of (id, position) pairs and partial rows for chunks of ids; short lists keep nothing
-    for rows, dim, n in ((10, 8, 1025), (91_000_000, 128, 24_576), (100, 256, 600_000)):
+    for rows, dim, n in ((10, 8, 1025), (1_000_000, 8, 2049), (91_000_000, 128, 24_576), (100, 256, 600_000)):
         got = K.embedding_grad_scratch_bytes(rows, dim, n)
         assert got >= 8 * n and got % 256 == 0
     assert K.embedding_grad_scratch_bytes(10, 8, 1) == 0 and K.embedding_grad_scratch_bytes(1000, 32, 1024) == 0
+    assert K.embedding_grad_scratch_bytes(8192, 32, 2048) == 0 < K.embedding_grad_scratch_bytes(8191, 32, 2048)
     assert K.embedding_grad_scratch_bytes(0, 8, 4) == 0 and K.embedding_grad_scratch_bytes(10, 8, 0) == 0
 
 
