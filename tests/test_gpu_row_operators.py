@@ -491,7 +491,11 @@ def _product_tol(T, a, b, k):
     (7, 33, 100, "e4m3", "e5m2", 1, 1, "f32", True), (128, 128, 128, "e5m2", "e4m3", 128, 128, "f16", False), (130, 257, 300, "e4m3", "e4m3", 1, 128, "f32", True),
     (129, 130, 129, "e5m2", "e5m2", 128, 1, "bf16", True), (300, 1000, 1000, "e4m3", "e4m3", 1, 1, "f32", False), (513, 384, 2048, "e4m3", "e4m3", 128, 128, "f32", True),
     (2000, 256, 768, "e4m3", "e4m3", 1, 128, "f32", True), (256, 768, 24_576, "e4m3", "e4m3", 1, 1, "f32", True), (40, 64, 70_000, "e5m2", "e4m3", 1, 1, "f32", False),
-    (3, 5000, 4000, "e4m3", "e4m3", 1, 128, "f16", False), (5000, 3, 515, "e4m3", "e4m3", 1, 128, "f32", False), (20_000, 640, 256, "e4m3", "e4m3", 1, 1, "bf16", False)])
+    (3, 5000, 4000, "e4m3", "e4m3", 1, 128, "f16", False), (5000, 3, 515, "e4m3", "e4m3", 1, 128, "f32", False), (20_000, 640, 256, "e4m3", "e4m3", 1, 1, "bf16", False),
+    (3000, 2502, 125, "e4m3", "e4m3", 1, 128, "bf16", True), (3000, 2501, 130, "e5m2", "e4m3", 1, 1, "f16", True), (3000, 2503, 200, "e4m3", "e4m3", 1, 128, "f32", True),
+    (30_000, 60, 300, "e4m3", "e4m3", 1, 128, "f32", True), (30_000, 200, 300, "e4m3", "e4m3", 128, 1, "bf16", True), (2600, 2051, 2300, "e4m3", "e4m3", 1, 128, "bf16", True),
+    (2600, 2053, 2300, "e4m3", "e4m3", 1, 1, "f32", False), (2600, 2048, 2300, "e4m3", "e4m3", 1, 128, "f32", True), (2600, 2048, 2300, "e5m2", "e4m3", 128, 1, "bf16", False),
+    (4096, 2816, 2049, "e4m3", "e4m3", 1, 1, "f16", True), (120, 38_000, 2100, "e4m3", "e4m3", 1, 128, "bf16", False), (120, 38_000, 2100, "e4m3", "e4m3", 1, 1, "f32", True)])
 def test_product(T, K, M, N, Kd, fa, fb, ba, bb, to, add):
     g = _gen(T, M + N + Kd)
     a, sa = _operand(T, K, g, M, Kd, fa, ba)
