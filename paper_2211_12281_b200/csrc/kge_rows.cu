@@ -111,6 +111,8 @@ constexpr int GS_THREADS = 256, GS_WARPS = GS_THREADS / 32, GS_ITEMS = 8;
 constexpr int GS_TILE = GS_THREADS * GS_ITEMS;     // ids per CTA of the sort in global memory
 constexpr int GS_MAX_BITS = 9;
 constexpr int CS_CTAS = 16, CS_CTAS_PORTABLE = 8, CS_THREADS = 512, CS_WARPS = CS_THREADS / 32, CS_ITEMS = 16;      // the cluster's sort
+// (At 128 columns 65,536 ids take 33.5 us with the cluster, 65,537 with the sort in global memory 31.8: about where they meet, and where
+// a cluster of eight has no room for more.)
 constexpr int CS_SHARE = CS_THREADS * CS_ITEMS, CS_MAX = CS_CTAS_PORTABLE * CS_SHARE, CS_MAX_BITS = 11;
 constexpr int SMALL_MAX = 2048, SMALL_THREADS = 256, SMALL_BITS = 11;      // (SMALL_BITS: of a position)
 static_assert(SMALL_MAX == 1 << SMALL_BITS, "positions of a short list");
@@ -132,6 +134,9 @@ SortPlan sort_plan(int64_t rows, int n) {
 // One CTA adds up all rows of an id, so longer lists go this way only where ids can be expected to differ: 2,048 rows of 1 KB take 8.9
 // us against 13.8 with the sort if they do, 53 against 15 if all are one id's (1,024: 29 against 15).
 bool short_list(int64_t rows, int n) { return n <= SMALL_MAX / 2 || (n <= SMALL_MAX && rows >= 4ll * n); }
+// Rows to a thread of grad_sum_kernel: few where there would be too few threads (24,576 x 128: 23.7 us a call with 8, 28.2 with 32; 131,071 x
+// 256: 70 and 74), else enough that the partial sums of frequent ids stay few (500,000 x 256, sum + join: 66 + 21 us with 32, 61 + 38 with
+// 16, 79 + 13 with 64).
 int chunk_rows(int n) { return n < (1 << 17) ? 8 : 32; }
 
 struct GradScratch {
@@ -191,11 +196,19 @@ __device__ __forceinline__ void zero_bytes(char* base, int64_t all, int64_t firs
     for (int64_t i = 2 * first; i < head; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
     for (int64_t i = head + words * 16 + 2 * first; i < all; i += 2 * step) *reinterpret_cast<uint16_t*>(base + i) = 0;
 }
+// Rows apart: a warp to a row, or, where a warp would mostly idle, a thread to an element (55,864 x 496 fp32, 504 apart, and 3,010 ids: 31 to
+// 34 us, element by element 281).
 __device__ __forceinline__ void zero_strided(char* base, int64_t rows, int64_t row_bytes, int64_t ld_bytes, int64_t first, int64_t step) {
-    const int64_t halves = row_bytes / 2, all = rows * halves;
-    for (int64_t i = first; i < all; i += step) {
-        const int64_t r = i / halves;
-        *reinterpret_cast<uint16_t*>(base + r * ld_bytes + (i - r * halves) * 2) = 0;
+    if (row_bytes >= 64) {
+        for (int64_t r = first >> 5; r < rows; r += step >> 5) zero_bytes(base + r * ld_bytes, row_bytes, first & 31, 32);
+        return;
+    }
+    const int unit = ((reinterpret_cast<intptr_t>(base) | row_bytes | ld_bytes) & 3) == 0 ? 4 : 2, units = (int)row_bytes / unit;
+    for (int64_t i = first; i < rows * units; i += step) {
+        const int64_t r = i >> 32 ? i / units : (uint32_t)i / (uint32_t)units;
+        char* const at = base + r * ld_bytes + (i - r * units) * unit;
+        if (unit == 4) *reinterpret_cast<uint32_t*>(at) = 0;
+        else *reinterpret_cast<uint16_t*>(at) = 0;
     }
 }
 // Rows [zero_first, zero_last) by CTA `cta` of `ctas`.
@@ -496,7 +509,7 @@ __device__ __forceinline__ void finish_pack(const SumParams& p, uint32_t row, in
 
 // CTA c owns the table rows [c rows_per_cta, + rows_per_cta): it picks the ids that name them, sorts those as (row, position) words
 // in shared memory, and adds up each row's gradients: runs of up to SHORT by one group of threads (a pack of columns each),
-// longer ones by all groups in turn, whose sums are then added in order.
+// longer ones by all groups in turn, whose sums are then added in order.  Bound by latency: 256 ids of 1,000 x 32 fp32 in 7.9 us a call.
 template <typename TG, typename TO, int V>
 __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) {
     constexpr int SHORT = 32, U = 8;
@@ -839,7 +852,7 @@ int launch_lookup(LookupParams& p, int tt, int to, int vec, int dim, cudaStream_
         return with_type(to, [&](auto b) {
             using TT = decltype(a); using TO = decltype(b);
             if (vec == 1) return launch_status(launch_dependent(lookup_single_kernel<TT, TO>, grid, dim3(LOOKUP_THREADS), 0, s, p));
-            return with_vector<sizeof(TT) == 2 || sizeof(TO) == 2>(vec, [&](auto v) {
+            return with_vector<sizeof(TT) == 2 && sizeof(TO) == 2>(vec, [&](auto v) {
                 return launch_status(launch_dependent(lookup_kernel<TT, TO, decltype(v)::value>, grid, dim3(LOOKUP_THREADS), 0, s, p));
             });
         });
@@ -871,9 +884,9 @@ int launch_sum(SumParams& p, int vec, cudaStream_t s) {
     return launch_status(launch_dependent(grad_join_kernel<TO, L>, joins, dim3(JOIN_THREADS), 0, s, p));
 }
 
-// Clusters of sixteen CTAs are no promise of the architecture: asked for once per device.
-int wide_clusters(bool* wide) {
-    static std::atomic<int> known[kMaxDevices];        // 1: no, 2: yes
+// Clusters of sixteen CTAs are no promise of the architecture: how many of them the device runs at a time is asked once.
+int wide_clusters(int* clusters) {
+    static std::atomic<int> known[kMaxDevices];        // one more than their number
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return KGE_ERR_CUDA;
     const bool tracked = dev >= 0 && dev < kMaxDevices;
@@ -891,16 +904,18 @@ int wide_clusters(bool* wide) {
         cfg.attrs = attr; cfg.numAttrs = 1;
         int fit = 0;
         if (cudaOccupancyMaxActiveClusters(&fit, grad_cluster_sort_kernel<CS_CTAS>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); fit = 0; }
-        state = fit > 0 ? 2 : 1;
+        state = 1 + std::max(fit, 0);
         if (tracked) known[dev].store(state, std::memory_order_release);
     }
-    *wide = state == 2;
+    *clusters = state - 1;
     return KGE_OK;
 }
 
+// `beside`: clusters that set rows to zero while the first one sorts, no more than run at the same time (55,864 x 496 fp32 and 3,010
+// ids: 30 us a call with six, 38 with a seventh, which waits until one ends).
 template <int CTAS>
-int launch_cluster_sort(SortParams& q, const SortPlan& plan, bool zero, int64_t rows, cudaStream_t s) {
-    const int zero_clusters = zero ? (int)std::min<int64_t>(128 / CTAS, ceil_div(rows * q.zero_row_bytes, 8192 * CTAS)) : 0;
+int launch_cluster_sort(SortParams& q, const SortPlan& plan, bool zero, int64_t rows, int beside, cudaStream_t s) {
+    const int zero_clusters = zero ? (int)std::min<int64_t>(std::max(1, beside), ceil_div(rows * q.zero_row_bytes, 8192 * CTAS)) : 0;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(CTAS * (1 + zero_clusters))); cfg.blockDim = dim3(CS_THREADS); cfg.stream = s;
     cfg.dynamicSmemBytes = cluster_sort_smem(q.n, plan.bits, CTAS);
@@ -920,10 +935,11 @@ int sort_ids(const GradScratch& g, const SortPlan& plan, SortParams& q, bool zer
         q.pairs_out = g.pairs[0];
         q.zero_first = 0; q.zero_last = rows;
         *where = 0;
-        bool wide = false;
-        int rc = wide_clusters(&wide);
+        int wide = 0;
+        const int rc = wide_clusters(&wide);
         if (rc != KGE_OK) return rc;
-        return wide ? launch_cluster_sort<CS_CTAS>(q, plan, zero, rows, s) : launch_cluster_sort<CS_CTAS_PORTABLE>(q, plan, zero, rows, s);
+        return wide > 0 ? launch_cluster_sort<CS_CTAS>(q, plan, zero, rows, wide - 1, s)
+                        : launch_cluster_sort<CS_CTAS_PORTABLE>(q, plan, zero, rows, 128 / CS_CTAS_PORTABLE, s);
     }
     // the zeroing is shared out over the launches: the sort leaves most of the memory's bandwidth unused
     const int launches = 2 * plan.passes;
@@ -965,7 +981,7 @@ int kge_embedding_lookup(const void* table, int32_t table_type, int64_t rows, in
     p.table = table; p.out = out; p.ids = ids; p.rows = rows; p.ld_table = ld_table; p.ld_out = ld_out; p.n = n;
     p.padding_id = padding_id; p.scale = scale; p.status = status;
     const int tb = type_bytes(table_type), ob = type_bytes(out_type);
-    const int vec = vector_length(tb == 2 || ob == 2 ? 8 : 4, dim, ld_table, tb, table, ld_out, ob, out);
+    const int vec = vector_length(tb == 2 && ob == 2 ? 8 : 4, dim, ld_table, tb, table, ld_out, ob, out);
     return launch_lookup(p, table_type, out_type, vec, dim, static_cast<cudaStream_t>(stream));
 }
 
