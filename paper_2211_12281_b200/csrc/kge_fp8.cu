@@ -359,6 +359,7 @@ constexpr int FP_COLS = 64;                               // columns of the tile
 // multiplies while the other stores), or of 64, three CTAs an SM, for few; tiles of 128 whose blocks of K a cluster shares, where
 // tiles are few.
 enum { FP_WIDE = 0, FP_PAIR = 1, FP_SPLIT = 2, FP_NARROW = 3 };
+constexpr int FP_MAX_SPLIT = 8;           // CTAs that share a tile's blocks of K
 __host__ __device__ constexpr int fp_bn(int form) { return form == FP_WIDE ? 256 : (form == FP_NARROW ? 64 : 128); }
 __host__ __device__ constexpr int fp_box_rows(int form) { return form == FP_NARROW ? 64 : 128; }             // of B per copy
 __host__ __device__ constexpr int fp_stages(int form) { return form == FP_WIDE ? 4 : (form == FP_SPLIT ? 6 : 2); }
@@ -609,11 +610,11 @@ __device__ __forceinline__ void fp_join(const ProductParams& p, uint32_t part, i
     for (int u = (int)cluster_rank() * THREADS + tid; u < rows * PER_ROW; u += (int)size * THREADS) {
         const int r = u / PER_ROW, q = u % PER_ROW, row = m0 + r, col = n0 + 4 * q;
         if (col >= p.N) continue;
-        float4 v[8];
+        float4 v[FP_MAX_SPLIT];
 #pragma unroll
-        for (int z = 0; z < 8; ++z) v[z] = z < (int)size ? cluster_ld(part + (uint32_t)(r * PER_ROW + (q ^ (r & 7))) * 16, z) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int z = 0; z < FP_MAX_SPLIT; ++z) v[z] = z < (int)size ? cluster_ld(part + (uint32_t)(r * PER_ROW + (q ^ (r & 7))) * 16, z) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int z = 1; z < 8; ++z) { v[0].x += v[z].x; v[0].y += v[z].y; v[0].z += v[z].z; v[0].w += v[z].w; }
+        for (int z = 1; z < FP_MAX_SPLIT; ++z) { v[0].x += v[z].x; v[0].y += v[z].y; v[0].z += v[z].z; v[0].w += v[z].w; }
         float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
         Pack<TO, 4> o;
         if (p.addend) {
@@ -866,33 +867,71 @@ int sm_count(int* sms) {
     return KGE_OK;
 }
 
+template <int FORM> int configure_product() {
+    static DeviceOnce configured;
+    return once_per_device(configured, [] {
+        return cudaFuncSetAttribute(fp8_product_kernel<FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)fp_smem_bytes(FORM));
+    }) == cudaSuccess ? KGE_OK : KGE_ERR_CUDA;
+}
+
+// How many clusters of `split` CTAs the device runs at a time: asked for once (what is left of a part of the chip takes none).
+int split_clusters(int split, int* clusters) {
+    static std::atomic<int> known[kMaxDevices][FP_MAX_SPLIT + 1];        // one more than their number
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KGE_ERR_CUDA;
+    const bool tracked = dev >= 0 && dev < kMaxDevices;
+    int state = tracked ? known[dev][split].load(std::memory_order_acquire) : 0;
+    if (state == 0) {
+        const int rc = configure_product<FP_SPLIT>();
+        if (rc != KGE_OK) return rc;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)split); cfg.blockDim = dim3(fp_threads(FP_SPLIT)); cfg.dynamicSmemBytes = fp_smem_bytes(FP_SPLIT);
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        int fit = 0;
+        if (cudaOccupancyMaxActiveClusters(&fit, fp8_product_kernel<FP_SPLIT>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); fit = 0; }
+        state = 1 + std::max(fit, 0);
+        if (tracked) known[dev][split].store(state, std::memory_order_release);
+    }
+    *clusters = state - 1;
+    return KGE_OK;
+}
+
 // How a product is cut up: columns of a tile, and CTAs that share a tile's blocks of K.
+//   shared K      as many CTAs to a tile as run at a time (512 x 768 x 4096: six to each of 24 tiles, of which some wait, 16.0 us, four 9.3,
+//                 one 16.2), where the blocks that a CTA is spared outweigh the join: a block takes 0.4 us, the join 0.4 + 2 for 128 rows
+//                 (128 x 768 x 512: 5.8 us shared, 4.5 not; x 4096: 7.5 and 15.5; one row, 256 x 512: 4.2 and 4.9)
+//   256 columns   where K is long and they fill the SMs (8192 x 4096 x 8192 bf16: 278 us, in pairs of 128 columns 315; 4096 x 4096 x 4096: 85
+//                 and 82; 2048 x 4096 x 1024 and 16,384 x 8192 x 512: no difference)
+//   64 columns    or pairs: 24,576 x 256 x 768 with an addend 19.6 and 21.7 us, 24,576 x 768 x 256 24.5 and 22.9
 struct ProductPlan { int form, split; };
-ProductPlan product_plan(int64_t M, int64_t N, int kblocks, bool ragged_addend, int sms) {
+int product_plan(int64_t M, int64_t N, int kblocks, bool ragged_addend, int sms, ProductPlan* plan) {
     const int64_t tiles128 = ceil_div(M, FP_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, FP_BM) * ceil_div(N, 256);
-    if (tiles128 < sms && kblocks > 1) {
-        int split = (int)std::min<int64_t>({8, kblocks, std::max<int64_t>(1, sms / tiles128)});
-        const int per = (kblocks + split - 1) / split;
-        split = (kblocks + per - 1) / per;              // every CTA has a block
-        if (split > 1) return {FP_SPLIT, split};
+    for (int most = (int)std::min<int64_t>({FP_MAX_SPLIT, kblocks, sms / tiles128}); most > 1; --most) {
+        const int per = (kblocks + most - 1) / most, split = (kblocks + per - 1) / per;          // every CTA has a block
+        if (128 * (kblocks - per - 1) <= 5 * std::min<int64_t>(M, FP_BM)) break;
+        int room = 0;
+        const int rc = split_clusters(split, &room);
+        if (rc != KGE_OK) return rc;
+        if (tiles128 <= room) { *plan = {FP_SPLIT, split}; return KGE_OK; }
     }
     // (an addend whose rows are not whole 16-byte words passes through shared memory that the wide form has not: 187 us there, 165 in
     // pairs at 4096 x 4095 x 4096)
-    if (tiles256 >= sms && kblocks >= 16 && !ragged_addend) return {FP_WIDE, 1};
+    if (tiles256 >= sms && kblocks >= 16 && !ragged_addend) { *plan = {FP_WIDE, 1}; return KGE_OK; }
     // few blocks of K: memory sets the pace, and what counts is how well whole rounds of tiles fill the SMs
     const int64_t pair = ceil_div(tiles128, 2 * sms) * 256, narrow = ceil_div(ceil_div(M, FP_BM) * ceil_div(N, 64), 3 * sms) * 192;
-    return {narrow < pair ? FP_NARROW : FP_PAIR, 1};
+    *plan = {narrow < pair ? FP_NARROW : FP_PAIR, 1};
+    return KGE_OK;
 }
 
 template <int FORM>
 int launch_product(const CUtensorMap& a, const CUtensorMap& b, ProductParams& p, int split, int sms, cudaStream_t s) {
     constexpr size_t smem = fp_smem_bytes(FORM);
     static_assert((smem + 1024) * fp_ctas_per_sm(FORM) <= 228 * 1024, "shared memory of an SM");
-    static DeviceOnce configured;
-    cudaError_t e = once_per_device(configured, [] {
-        return cudaFuncSetAttribute(fp8_product_kernel<FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    });
-    if (e != cudaSuccess) return KGE_ERR_CUDA;
+    const int rc = configure_product<FORM>();
+    if (rc != KGE_OK) return rc;
     p.tiles_n = (int)ceil_div(p.N, fp_bn(FORM));
     p.items = (int)(ceil_div(p.M, FP_BM) * p.tiles_n);
     p.kper = (p.kblocks + split - 1) / split;
@@ -955,7 +994,9 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
     int sms = 0, rc = sm_count(&sms);
     if (rc != KGE_OK) return rc;
     if (ceil_div(M, 128) * ceil_div(N, 64) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;
-    const ProductPlan plan = product_plan(M, N, p.kblocks, addend && !p.vec, sms);
+    ProductPlan plan;
+    rc = product_plan(M, N, p.kblocks, addend && !p.vec, sms, &plan);
+    if (rc != KGE_OK) return rc;
     alignas(64) CUtensorMap ma, mb;
     rc = operand_map(&ma, a, M, K, lda, FP_BM);
     if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb, fp_box_rows(plan.form));

@@ -170,9 +170,9 @@ def test_grad(T, K, n, E, d, kind, tg, to, scale, acc):
 
 
 @pytest.mark.parametrize("n", [40, 3000, 140_000])
-def test_grad_of_strided_and_shifted_rows(T, K, n):
+@pytest.mark.parametrize("E,d", [(61, 24), (700, 3), (90, 70), (40, 515)])
+def test_grad_of_strided_and_shifted_rows(T, K, n, E, d):
     g = _gen(T, n)
-    E, d = 61, 24
     ids = _id_list(T, g, "zipf", n, E)
     for extra, shift, to in ((8, 0, T.float32), (3, 0, T.float32), (0, 1, T.float32), (4, 2, T.float32), (0, 3, T.bfloat16), (5, 1, T.float16)):
         grads, out = _strided(T, n, d, T.bfloat16, extra, shift), _strided(T, E, d, to, extra, shift)
@@ -495,7 +495,9 @@ def _product_tol(T, a, b, k):
     (3000, 2502, 125, "e4m3", "e4m3", 1, 128, "bf16", True), (3000, 2501, 130, "e5m2", "e4m3", 1, 1, "f16", True), (3000, 2503, 200, "e4m3", "e4m3", 1, 128, "f32", True),
     (30_000, 60, 300, "e4m3", "e4m3", 1, 128, "f32", True), (30_000, 200, 300, "e4m3", "e4m3", 128, 1, "bf16", True), (2600, 2051, 2300, "e4m3", "e4m3", 1, 128, "bf16", True),
     (2600, 2053, 2300, "e4m3", "e4m3", 1, 1, "f32", False), (2600, 2048, 2300, "e4m3", "e4m3", 1, 128, "f32", True), (2600, 2048, 2300, "e5m2", "e4m3", 128, 1, "bf16", False),
-    (4096, 2816, 2049, "e4m3", "e4m3", 1, 1, "f16", True), (120, 38_000, 2100, "e4m3", "e4m3", 1, 128, "bf16", False), (120, 38_000, 2100, "e4m3", "e4m3", 1, 1, "f32", True)])
+    (4096, 2816, 2049, "e4m3", "e4m3", 1, 1, "f16", True), (120, 38_000, 2100, "e4m3", "e4m3", 1, 128, "bf16", False), (120, 38_000, 2100, "e4m3", "e4m3", 1, 1, "f32", True),
+    (130, 700, 2050, "e4m3", "e4m3", 1, 128, "f32", True), (500, 760, 4000, "e4m3", "e5m2", 1, 1, "bf16", True), (1000, 1100, 4100, "e4m3", "e4m3", 1, 128, "f32", False),
+    (250, 900, 1030, "e4m3", "e4m3", 128, 128, "f16", True), (17, 4000, 900, "e4m3", "e4m3", 1, 128, "bf16", False), (2, 300, 260, "e5m2", "e4m3", 1, 1, "f32", True)])
 def test_product(T, K, M, N, Kd, fa, fb, ba, bb, to, add):
     g = _gen(T, M + N + Kd)
     a, sa = _operand(T, K, g, M, Kd, fa, ba)
