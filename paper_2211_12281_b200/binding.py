@@ -344,7 +344,7 @@ def dropout(x, out, p, seed, step=0, site=0, residual=None, step_dev=None):
         raise _bad(w, "x and out are not contiguous tensors of one size")
     if residual is not None and not (residual.is_contiguous() and residual.dtype is out.dtype and residual.numel() == n):
         raise _bad(w, "residual is not a contiguous tensor of out's size and type")
-    if step_dev is not None and step_dev.dtype is not _torch.int64:
+    if step_dev is not None and (step_dev.dtype is not _torch.int64 or step_dev.numel() < 1):
         raise _bad(w, "step_dev is not an int64 tensor")
     if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64 and 0 <= site < 1 << 31):
         raise _bad(w, "seed and step are 64-bit numbers, site a 31-bit one")
@@ -460,6 +460,7 @@ class Kge:
         code, rows, cols, ld, block = _operand(feat, scales, w, "feat")
         if rows != self.cfg.num_entities or cols != self.cfg.feat_dim or block != 1:
             raise _bad(w, "feat is not [entities, feat_dim] with a scale per row and block of 128")
+        _device_of(w, feat, scales, MH, MT, MH_state, MT_state)
         self._keep += [feat, scales, MH, MT, MH_state, MT_state]
         self._check(lib().kge_bind_features_fp8(self._h, feat.data_ptr(), code, ld, scales.data_ptr(), _ptr(MH), _ptr(MT), _ptr(MH_state),
                                                 _ptr(MT_state), _stream()), w)

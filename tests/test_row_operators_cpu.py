@@ -85,6 +85,14 @@ def test_binding_features_in_8_bits_refuses(K):
         assert fn(h._h, feat, code, ld, scales, PTR, PTR * 2, None, None, None) == -1
 
 
+def test_binding_features_in_8_bits_takes_gpu_tensors_only(K):
+    import torch
+    h = K.Kge(K.KgeConfig.make(num_entities=100, num_relations=3, dim=32, score="transe", batch=4, num_neg=4, feat_dim=64))
+    with pytest.raises(K.KgeError) as e:
+        h.bind_features_fp8(torch.zeros((100, 64), dtype=torch.float8_e4m3fn), torch.zeros((1, 100)), torch.zeros((32, 64)), torch.zeros((32, 64)))
+    assert e.value.code == -1 and "GPU" in str(e.value)
+
+
 def test_scratch_sizes_cover_their_lists(K):
     # a list of (id, position) pairs and partial rows for chunks of ids; short lists keep nothing
     for rows, dim, n in ((10, 8, 1025), (1_000_000, 8, 2049), (91_000_000, 128, 24_576), (100, 256, 600_000)):
@@ -111,6 +119,7 @@ def test_binding_refuses_tensors_that_do_not_fit(K):
            lambda: K.dropout(f(8, 8).t(), f(8, 8), 0.1, 1),
            lambda: K.dropout(f(8), f(8), 0.1, 1, residual=f(8).half()),
            lambda: K.dropout(f(8), f(8), 0.1, -1),
+           lambda: K.dropout(f(8), f(8), 0.1, 1, step_dev=torch.zeros(0, dtype=torch.int64)),
            lambda: K.fp8_quantize(f(4, 64)),
            lambda: K.fp8_quantize(f(4, 64), e8(4, 64), f(1, 3)),
            lambda: K.fp8_quantize(f(4, 64), e8(4, 64), f(1, 4), block_rows=128),
