@@ -76,6 +76,20 @@ def test_lookup(T, K, n, E, d, tt, to, scale, extra, shift):
         assert (guard[:, d:] == 7.0).all()          # what lies between the rows stays
 
 
+@pytest.mark.parametrize("tt,to", [("bf16", "f16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("n,d", [(1, 1), (999, 1), (85, 45), (86, 45), (3000, 45), (5, 1021), (3, 4095), (2, 4097), (2, 9001)])
+@pytest.mark.parametrize("shift", [8, 9, 11, 15])
+def test_lookup_of_odd_widths_leaves_its_neighbours(T, K, tt, to, n, d, shift):
+    g = _gen(T, n * d + shift)
+    table = T.randn((70, d), generator=g, device="cuda").to(_type(T, tt))
+    ids = T.randint(-1, 70, (n,), generator=g, device="cuda", dtype=T.int32)
+    around = T.full((n * d + shift + 17,), 7.0, device="cuda", dtype=_type(T, to))
+    K.embedding_lookup(table, ids, around[shift:shift + n * d].view(n, d), scale=0.5)
+    want = T.where(ids[:, None] < 0, T.zeros((), device="cuda"), table[ids.clamp(min=0).long()].float() * 0.5).to(_type(T, to))
+    assert T.equal(around[shift:shift + n * d].view(n, d), want)          # half of a value is exact, then one rounding on both sides
+    assert (around[:shift] == 7.0).all() and (around[shift + n * d:] == 7.0).all()
+
+
 def test_lookup_padding_and_bad_ids(T, K):
     table = T.full((10, 24), float("nan"), device="cuda")
     table[2:5] = 1.5
