@@ -73,8 +73,8 @@ template <> __device__ __forceinline__ float key_value<float>(uint32_t key) { re
 template <> __device__ __forceinline__ float key_value<__nv_bfloat16>(uint32_t key) { return __uint_as_float(key << 16); }
 template <> __device__ __forceinline__ float key_value<__half>(uint32_t key) { return __half2float(__ushort_as_half((unsigned short)key)); }
 
-// A block's scale, and what its values are multiplied by.  A block of zeros has scale 1; an infinity or a NaN makes the scale one,
-// and with it every value that the block stands for NaN.
+// A block's scale, and what its values are multiplied by.  A block of zeros has scale 1; an infinity or a NaN makes the scale one, and
+// the factor 0: the block's values become 0, or NaN where they are an infinity or a NaN themselves, and stand for NaN all of them.
 //
 // The 8-bit value stored is the one nearest to the true quotient x / s; t = x (1 / s) is within 2^-23 of it, which matters where a
 // middle of two 8-bit values is that close.  With 16-bit inputs that has structure.  s = (a / 7 2^k) (1 + e) with a the block's
@@ -96,8 +96,8 @@ __device__ __forceinline__ Block block_of(uint32_t key) {
         b.s = a == 0.f ? 1.f : fmaxf(b.s, 1.17549435e-38f);
         if (POW2) b.s = __uint_as_float((__float_as_uint(b.s) + 0x007FFFFFu) & 0x7F800000u);
     }
-    b.inv = 1.f / b.s;
-    if (!POW2 && sizeof(TX) == 2) {
+    b.inv = finite ? 1.f / b.s : 0.f;
+    if (!POW2 && sizeof(TX) == 2 && finite) {
         const float lean = e > 0.f ? 4.76837158e-7f : (e < 0.f ? -4.76837158e-7f : 0.f);
         b.inv = __uint_as_float((__float_as_uint(fmaf(b.inv, lean, b.inv)) & ~1u) | (e == 0.f ? 1u : 0u));
     }

@@ -1,0 +1,54 @@
+"""The operators on rows where they could go wrong: non-finite values in every input type, sums whose order must not follow the layout,
+scales far from one, very wide rows, waits that run out, and arrays beyond 2^31 elements.  Tolerances count roundings: half a step of
+the output's type for the last one, 2^-24 for each fp32 operation before it."""
+import numpy as np
+import pytest
+
+from test_gpu_row_operators import K, T, U, _check, _empty8, _gen, _id_list, _product_tol, _quantized, _stands_for, _strided, _type  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- 8-bit quantisation ----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tx", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("block,pow2", [(1, False), (1, True), (128, False), (128, True)])
+def test_a_block_with_an_infinity_or_a_nan_stands_for_nan(T, K, tx, fmt, block, pow2):
+    """Each value of such a block is NaN, the infinity itself too, in both orientations and alone; the other blocks are as without it."""
+    g = _gen(T, 17)
+    x = T.randn((300, 400), generator=g, device="cuda").to(_type(T, tx))
+    clean = x.clone()
+    inf = float("inf")
+    spots = [(3, 5, inf), (3, 390, -inf), (140, 200, -inf), (141, 201, inf), (299, 399, float("nan")), (260, 130, inf), (260, 131, -inf)]
+    for r, c, v in spots:
+        x[r, c] = v
+    shape = lambda r, c: ((c + 127) // 128, r if block == 1 else (r + 127) // 128)
+    q, s = _empty8(T, 300, 400, fmt), T.empty(shape(300, 400), device="cuda")
+    qt, st = _empty8(T, 400, 300, fmt), T.empty(shape(400, 300), device="cuda")
+    q1, s1 = _empty8(T, 300, 400, fmt), T.empty_like(s)
+    K.fp8_quantize(x, q, s, qt, st, block_rows=block, pow2=pow2)
+    K.fp8_quantize(x, q1, s1, block_rows=block, pow2=pow2)
+    for codes, scales, src, at in ((q, s, clean, spots), (q1, s1, clean, spots), (qt, st, clean.t(), [(c, r, v) for r, c, v in spots])):
+        bad = T.zeros(tuple(src.shape), dtype=T.bool, device="cuda")
+        for r, c, _ in at:
+            r0 = r // block * block
+            bad[r0:r0 + block, c // 128 * 128:c // 128 * 128 + 128] = True
+        got, (want, ws) = _stands_for(T, codes, scales), _quantized(T, src, fmt, block, pow2)
+        assert T.isnan(got[bad]).all(), (int((~T.isnan(got[bad])).sum()), got[bad][~T.isnan(got[bad])][:4])
+        assert T.equal(codes.float().double()[~bad], want[~bad]) and T.isfinite(got[~bad]).all()
+
+
+@pytest.mark.parametrize("tx", ["f32", "bf16", "f16"])
+def test_an_infinity_makes_its_rows_products_nan(T, K, tx):
+    g = _gen(T, 18)
+    x, w = (T.randn((r, 400), generator=g, device="cuda").to(_type(T, tx)) for r in (300, 270))
+    x[131, 390], x[7, 0], w[9, 3] = -float("inf"), float("inf"), float("inf")
+    a, sa, b, sb = _empty8(T, 300, 400, "e4m3"), T.empty((4, 300), device="cuda"), _empty8(T, 270, 400, "e4m3"), T.empty((4, 270), device="cuda")
+    K.fp8_quantize(x, a, sa)
+    K.fp8_quantize(w, b, sb)
+    out = T.zeros((300, 270), device="cuda")
+    K.fp8_matmul(a, sa, b, sb, out)
+    bad = T.zeros((300, 270), dtype=T.bool, device="cuda")
+    bad[[7, 131]], bad[:, 9] = True, True
+    assert T.isnan(out[bad]).all() and T.isfinite(out[~bad]).all()
