@@ -415,22 +415,22 @@ __device__ __forceinline__ void fp_copy4(uint32_t dst, const float* src) {
 }
 __device__ __forceinline__ void fp_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fp_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// 16 consecutive columns of this thread's tensor-memory lane; the registers are valid after fp_tmem_wait.
-__device__ __forceinline__ void fp_tmem_ld16(uint32_t taddr, uint64_t (&v)[8]) {
-    uint32_t r[16];
+// 16 consecutive columns of this thread's tensor-memory lane.  Nothing may look at the registers before fp_tmem_wait has passed them on.
+__device__ __forceinline__ void fp_tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) asm("mov.b64 %0, {%1, %2};" : "=l"(v[i]) : "r"(r[2 * i]), "r"(r[2 * i + 1]));
 }
 // Waits for this thread's tensor-memory loads; the registers pass through, so that nothing that uses them moves ahead.
-__device__ __forceinline__ void fp_tmem_wait(uint64_t (&v)[8]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+l"(v[0]), "+l"(v[1]), "+l"(v[2]), "+l"(v[3]), "+l"(v[4]), "+l"(v[5]), "+l"(v[6]), "+l"(v[7])::"memory");
+__device__ __forceinline__ void fp_tmem_wait(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
+__device__ __forceinline__ uint64_t two_words(uint32_t a, uint32_t b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b)); return r; }
 // Two fp32 operations in one instruction, each rounded as a single one would be.
 __device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float2 unpair(uint64_t a) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a)); return r; }
@@ -762,7 +762,7 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 fp_fence_after();
                 if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
                 const uint32_t from = taddr + buf * BN;
-                uint64_t v[2][8];
+                uint32_t v[2][16];
                 fp_tmem_ld16(from, v[0]);
                 const float* const sc = scales + slot * (128 + BN);
                 const float4* const sb = reinterpret_cast<const float4*>(sc + 128 + group * FP_COLS);
@@ -771,8 +771,10 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 const uint64_t s2 = pair(s, s);
 #pragma unroll
                 for (int c = 0; c < FP_COLS / 16; ++c) {
-                    uint64_t (&w)[8] = v[c & 1];
-                    fp_tmem_wait(w);
+                    fp_tmem_wait(v[c & 1]);
+                    uint64_t w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = two_words(v[c & 1][2 * i], v[c & 1][2 * i + 1]);
                     if (c + 1 < FP_COLS / 16) fp_tmem_ld16(from + (uint32_t)(c + 1) * 16, v[(c + 1) & 1]);
                     else {                 // the accumulator is read: the next block's MMAs may begin
                         fp_fence_before();
