@@ -425,8 +425,9 @@ int kge_dropout(const void* x, int32_t x_type, const void* residual, void* out, 
  *                    the value stored is the one nearest to x / scale, ties to even.  A block that holds an infinity or a NaN
  *                    stands for NaN throughout.
  * kge_fp8_matmul     out [M, N] = A [M, K] . B [N, K]^T (+ addend [M, N], of out's type; it may be out itself): products within a
- *                    block of 128 summed by the tensor cores, each block's sum times its two scales added in fp32.  out fp32,
- *                    bf16 or fp16; a_block, b_block: 1 or 128 rows to a scale; the operands' types may differ.
+ *                    block of 128 summed by the tensor cores, each block's sum times its two scales added in fp32 (also where the
+ *                    two scales' own product would be too small or too large for that).  out fp32, bf16 or fp16; a_block, b_block:
+ *                    1 or 128 rows to a scale; the operands' types may differ.
  *                    Where tiles are few, several CTAs share K and their sums are added in order: how many depends on the sizes and
  *                    the device, so the last bits may differ from one GPU to another, never from call to call on one.
  *                    The forward pass of a projection y = x W^T multiplies the forms along the columns of x and W; its gradients

@@ -364,12 +364,12 @@ __host__ __device__ constexpr int fp_bn(int form) { return form == FP_WIDE ? 256
 __host__ __device__ constexpr int fp_box_rows(int form) { return form == FP_NARROW ? 64 : 128; }             // of B per copy
 __host__ __device__ constexpr int fp_stages(int form) { return form == FP_WIDE ? 4 : (form == FP_SPLIT ? 6 : 2); }
 __host__ __device__ constexpr int fp_epi_warps(int form) { return 4 * fp_bn(form) / FP_COLS; }
-__host__ __device__ constexpr int fp_threads(int form) { return 32 * (4 + fp_epi_warps(form)); }     // (four more: copies, MMAs, two idle)
+__host__ __device__ constexpr int fp_threads(int form) { return 32 * (4 + fp_epi_warps(form)); }     // (four more: copies, MMAs, a look at the scales, one idle)
 __host__ __device__ constexpr int fp_ctas_per_sm(int form) { return form == FP_PAIR ? 2 : (form == FP_NARROW ? 3 : 1); }
 __host__ __device__ constexpr uint32_t fp_stage_bytes(int form) { return FP_BOX_BYTES + (uint32_t)fp_bn(form) * FP_BK; }
 // Per epilogue warp: 32 rows x 32 or 128 bytes of the output on their way to memory.
 __host__ __device__ constexpr uint32_t fp_store_row(int form) { return form == FP_PAIR || form == FP_NARROW ? 128 : 32; }
-// Blocks of K whose scales are in shared memory.  A slot needs no barrier of its own: its block's scales are read before the epilogue
+// Blocks of K whose scales (and a word about them) are in shared memory.  A slot needs no barrier of its own: its block's scales are read before the epilogue
 // hands back the block sum after the next one, without which no MMA of the block FP_NACC later is issued, without which no stage
 // that follows by fp_stages() more is filled again -- at least stages + FP_NACC + 1 blocks later.
 __host__ __device__ constexpr int fp_slots(int form) { return fp_stages(form) + FP_NACC + 2; }
@@ -437,6 +437,28 @@ __device__ __forceinline__ float2 unpair(uint64_t a) { float2 r; asm("mov.b64 {%
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+
+// A block's sum x joins c as x (a b), a and b the block's scales, where a b is a normal number (or not finite: a block that stands for NaN).
+// Where it is not, as (x a) b.  |x| is 0 or between 2^-32 and 2^39 (products of 8-bit values, 128 of them): with a b below the normal
+// numbers a and b are below 1 and x a is off by half a step of the smallest numbers at most; with a b beyond the largest number, scales
+// of finite blocks (up to 2^119) are both above 2^8, and x a is infinite only where x a b is.
+__device__ __forceinline__ float fp_add_far(float x, float a, float b, float c) {
+    const float ab = a * b, size = fabsf(ab);
+    const bool far = size < 1.17549435e-38f || (size == __int_as_float(0x7F800000) && fabsf(a) < size && fabsf(b) < size);
+    return far ? fmaf(x * a, b, c) : fmaf(x, ab, c);
+}
+__device__ __forceinline__ uint64_t fp_add_far(uint64_t x, float a, float b0, float b1, uint64_t c) {
+    const float2 u = unpair(x), v = unpair(c);
+    return pair(fp_add_far(u.x, a, b0, v.x), fp_add_far(u.y, a, b1, v.y));
+}
+// Between 2^-63 and 2^63: the product of two such scales is a normal number.
+__device__ __forceinline__ bool fp_near_one(float s) { return __float_as_uint(s) - 0x20000000u <= 0x3F000000u; }
+
+// Scales of a tile's block of K that lane `lane` takes: those i (32 rows or columns apart) with 32 i below the result.
+__device__ __forceinline__ int fp_scales_a(const ProductParams& p, int m0, int lane) { return p.a_square ? (lane == 0 ? 1 : 0) : (int)p.M - m0 - lane; }
+template <int BN> __device__ __forceinline__ int fp_scales_b(const ProductParams& p, int n0, int lane) {
+    return p.b_square ? (lane < (BN + 127) / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
+}
 
 // Registers of a warpgroup, out of what the block was launched with.
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -630,8 +652,8 @@ __device__ __forceinline__ void fp_join(const ProductParams& p, uint32_t part, i
 
 // A 128 x BN tile of C at a time (persistent CTAs), or one per cluster, whose CTAs share its blocks of K (SPLIT).  Warp 0 feeds a
 // ring of shared-memory stages by TMA, warp 1 issues the MMAs of one block of 128 k into one of two accumulators in tensor memory,
-// the other warps, 64 columns each, multiply finished block sums by their scales and add them up in registers (the tensor cores
-// cannot carry an fp32 scale from block to block).
+// warp 2 looks whether two of a block's scales may multiply to a number that is not normal, the other warps, 64 columns each, multiply
+// finished block sums by their scales and add them up in registers (the tensor cores cannot carry an fp32 scale from block to block).
 template <int FORM>
 __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_product_kernel(const __grid_constant__ CUtensorMap tmA,
                                                                                               const __grid_constant__ CUtensorMap tmB,
@@ -655,10 +677,12 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
     volatile uint32_t* stop = tmem_slot + 1;
     volatile uint32_t* filled = tmem_slot + 2;
+    volatile uint32_t* looked = tmem_slot + 3;
+    volatile uint32_t* far = tmem_slot + 4;        // [SLOTS] a product of two of the block's scales may not be a normal number
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 33); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 34); mbar_init(&empty[s], 1); }
         for (int b = 0; b < FP_NACC; ++b) { mbar_init(&acc_full[b], 2); mbar_init(&acc_empty[b], EW); }
         mbar_init(done, 1);
         *stop = 0;
@@ -689,8 +713,7 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 const int m0 = item / p.tiles_n * FP_BM, n0 = item % p.tiles_n * BN;
                 const float* const sa0 = p.sa + (p.a_square ? m0 >> 7 : m0 + lane);
                 const float* const sb0 = p.sb + (p.b_square ? (n0 >> 7) + lane : n0 + lane);
-                const int na = p.a_square ? (lane == 0 ? 1 : 0) : (int)p.M - m0 - lane;         // (values to copy are those i with 32 i < na)
-                const int nb = p.b_square ? (lane < (BN + 127) / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
+                const int na = fp_scales_a(p, m0, lane), nb = fp_scales_b<BN>(p, n0, lane);
                 for (int kb = kb0; kb < kb1; ++kb) {
                     ok = mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop;
                     ok = __all_sync(0xffffffffu, ok);
@@ -736,6 +759,41 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 }
                 if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
             }
+        } else if (warp == 2) {
+            // looks at the scales of the blocks as they are loaded and leaves the epilogue one word for each (8192 x 4096 x 8192: 287 -> 291 us;
+            // with a vote in the epilogue 320, with the MMAs' warp looking some 360)
+            uint32_t s = 0, phase = 1, slot = 0, count = 0;
+            bool ok = true;
+            for (int item = first; item < p.items && ok; item += step) {
+                const int m0 = item / p.tiles_n * FP_BM, n0 = item % p.tiles_n * BN;
+                const float* const sa0 = p.sa + (p.a_square ? m0 >> 7 : m0 + lane);
+                const float* const sb0 = p.sb + (p.b_square ? (n0 >> 7) + lane : n0 + lane);
+                const int na = fp_scales_a(p, m0, lane), nb = fp_scales_b<BN>(p, n0, lane);
+                float a[4], b[BN / 32];
+                auto load = [&](int kb) {
+    #pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] = 32 * i < na ? sa0[kb * p.sa_ld + 32 * i] : 1.f;
+    #pragma unroll
+                    for (int i = 0; i < BN / 32; ++i) b[i] = 32 * i < nb ? sb0[kb * p.sb_ld + 32 * i] : 1.f;
+                };
+                load(kb0);
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    bool near = true;
+    #pragma unroll
+                    for (int i = 0; i < 4; ++i) near &= fp_near_one(a[i]);
+    #pragma unroll
+                    for (int i = 0; i < BN / 32; ++i) near &= fp_near_one(b[i]);
+                    near = __all_sync(0xffffffffu, near);
+                    if (kb + 1 < kb1) load(kb + 1);
+                    ok = __all_sync(0xffffffffu, mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop);
+                    if (!ok) break;
+                    if (lane == 0) { far[slot] = near ? 0u : 1u; mbar_arrive(&full[s]); }
+                    ++count;
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
+                    if (++slot == SLOTS) slot = 0;
+                }
+            }
+            if (lane == 0) { *looked = count; if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } }
         }
         __syncwarp();
         if (SPLIT) { cluster_sync(); cluster_sync(); }
@@ -764,33 +822,46 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 const uint32_t from = taddr + buf * BN;
                 uint32_t v[2][16];
                 fp_tmem_ld16(from, v[0]);
-                const float* const sc = scales + slot * (128 + BN);
-                const float4* const sb = reinterpret_cast<const float4*>(sc + 128 + group * FP_COLS);
-                float s = sc[p.a_square ? 0 : quarter * 32 + lane];
-                if (p.b_square) s *= sc[128 + group * FP_COLS / 128];
-                const uint64_t s2 = pair(s, s);
+                const float* const sa = scales + slot * (128 + BN) + (p.a_square ? 0 : quarter * 32 + lane);
+                const float* const sb = scales + slot * (128 + BN) + 128 + (p.b_square ? group * FP_COLS / 128 : group * FP_COLS);
+                auto hand_back = [&] {                 // the accumulator is read: the next block's MMAs may begin
+                    fp_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&acc_empty[buf]);
+                };
+                if (!far[slot]) {
+                    const float s = p.b_square ? *sa * *sb : *sa;
+                    const uint64_t s2 = pair(s, s);
 #pragma unroll
-                for (int c = 0; c < FP_COLS / 16; ++c) {
-                    fp_tmem_wait(v[c & 1]);
-                    uint64_t w[8];
+                    for (int c = 0; c < FP_COLS / 16; ++c) {
+                        fp_tmem_wait(v[c & 1]);
+                        uint64_t w[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = two_words(v[c & 1][2 * i], v[c & 1][2 * i + 1]);
-                    if (c + 1 < FP_COLS / 16) fp_tmem_ld16(from + (uint32_t)(c + 1) * 16, v[(c + 1) & 1]);
-                    else {                 // the accumulator is read: the next block's MMAs may begin
-                        fp_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&acc_empty[buf]);
-                    }
-                    if (p.b_square) {
+                        for (int i = 0; i < 8; ++i) w[i] = two_words(v[c & 1][2 * i], v[c & 1][2 * i + 1]);
+                        if (c + 1 < FP_COLS / 16) fp_tmem_ld16(from + (uint32_t)(c + 1) * 16, v[(c + 1) & 1]);
+                        else hand_back();
+                        if (p.b_square) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) acc[c * 8 + i] = fma2(w[i], s2, acc[c * 8 + i]);
-                    } else {
+                            for (int i = 0; i < 8; ++i) acc[c * 8 + i] = fma2(w[i], s2, acc[c * 8 + i]);
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float4 b = sb[c * 4 + i];
-                            acc[c * 8 + 2 * i] = fma2(w[2 * i], mul2(s2, pair(b.x, b.y)), acc[c * 8 + 2 * i]);
-                            acc[c * 8 + 2 * i + 1] = fma2(w[2 * i + 1], mul2(s2, pair(b.z, b.w)), acc[c * 8 + 2 * i + 1]);
+                            for (int i = 0; i < 4; ++i) {
+                                const float4 b = reinterpret_cast<const float4*>(sb)[c * 4 + i];
+                                acc[c * 8 + 2 * i] = fma2(w[2 * i], mul2(s2, pair(b.x, b.y)), acc[c * 8 + 2 * i]);
+                                acc[c * 8 + 2 * i + 1] = fma2(w[2 * i + 1], mul2(s2, pair(b.z, b.w)), acc[c * 8 + 2 * i + 1]);
+                            }
                         }
+                    }
+                } else {
+                    const int each = p.b_square ? 0 : 1;
+#pragma unroll
+                    for (int c = 0; c < FP_COLS / 16; ++c) {
+                        if (c > 0) fp_tmem_ld16(from + (uint32_t)c * 16, v[0]);
+                        fp_tmem_wait(v[0]);
+                        if (c + 1 == FP_COLS / 16) hand_back();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            acc[c * 8 + i] = fp_add_far(two_words(v[0][2 * i], v[0][2 * i + 1]), *sa, sb[each * (c * 16 + 2 * i)], sb[each * (c * 16 + 2 * i + 1)], acc[c * 8 + i]);
                     }
                 }
                 if (++buf == FP_NACC) { buf = 0; phase ^= 1; }
@@ -826,9 +897,13 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
     }
     fp_fence_before();
     __syncthreads();
-    if (*stop) {       // copies and MMAs in flight are waited for before the CTA's memory is given back
+    if (*stop) {       // copies and MMAs in flight are waited for before the CTA's memory is given back (warp 2 may owe a stage its arrival)
         if (lane == 0) {
-            if (warp == 0) { const int n = (int)*filled; for (int r = max(0, n - STAGES); r < n; ++r) mbar_wait_idle(&full[r % STAGES], (r / STAGES) & 1, kDefaultWaitLimit); }
+            if (warp == 0) {
+                const int n = (int)*filled;
+                for (int r = (int)*looked; r < n; ++r) mbar_arrive(&full[r % STAGES]);
+                for (int r = max(0, n - STAGES); r < n; ++r) mbar_wait_idle(&full[r % STAGES], (r / STAGES) & 1, kDefaultWaitLimit);
+            }
             if (warp == 1) { fp_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
         }
         __syncthreads();

@@ -52,3 +52,35 @@ def test_an_infinity_makes_its_rows_products_nan(T, K, tx):
     bad = T.zeros((300, 270), dtype=T.bool, device="cuda")
     bad[[7, 131]], bad[:, 9] = True, True
     assert T.isnan(out[bad]).all() and T.isfinite(out[~bad]).all()
+
+
+# ---- 8-bit product ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("M,N,Kd", [(130, 700, 2050), (3000, 2502, 125), (30_000, 60, 300), (2600, 2048, 2300), (3, 40, 700)])
+@pytest.mark.parametrize("ba,bb,fmt", [(1, 1, "e4m3"), (1, 128, "e4m3"), (128, 1, "e5m2"), (128, 128, "e5m2")])
+def test_product_of_scales_far_from_one(T, K, M, N, Kd, ba, bb, fmt):
+    """Wherever the values' products lie in fp32's range, the scales' own product need not: it may fall below the normal numbers or beyond
+    the largest.  Every kind of pair meets in one tile; rows of zeros stay zero under any scale."""
+    g = _gen(T, M + N + ba)
+    made = []
+    for rows, block in ((M, ba), (N, bb)):
+        q = _empty8(T, rows, Kd, fmt)
+        q.copy_(T.randn((rows, Kd), generator=g, device="cuda").to(q.dtype))
+        e = T.tensor([0, -60, 60, -85, 90, -118, 110, 1, -64, 64], device="cuda")[T.randint(0, 10, ((rows + block - 1) // block,), generator=g, device="cuda")]
+        s = T.exp2(e.float())[None, :] * (1 + T.rand(((Kd + 127) // 128, e.numel()), generator=g, device="cuda"))
+        if rows > 2:
+            q.view(T.uint8)[1] = 0
+        made += [q, s.contiguous()]
+    va, vb = _stands_for(T, *made[:2]), _stands_for(T, *made[2:])
+    want, size = va @ vb.t(), va.abs() @ vb.abs().t()
+    out, status = T.full((M, N), 9.0, device="cuda"), T.zeros(1, dtype=T.int32, device="cuda")
+    K.fp8_matmul(*made, out, status=status)
+    fits = size < 2.0 ** 127
+    # (each block's product with a scale and its addition may also be off by half the smallest step, 2^-150)
+    tol = _product_tol(T, va, vb, Kd) + 4 * ((Kd + 127) // 128) * 2.0 ** -150
+    assert status.item() == 0 and fits.any()
+    if M > 128:                                   # (the smallest case may have one pair of scales only)
+        assert bool((want[fits].abs() < 2.0 ** -100).any()) and bool((want[fits].abs() > 2.0 ** 60).any())
+    _check(T, out[fits], want[fits], tol[fits])
+    if M > 2 and N > 2:
+        assert (out[1] == 0).all() and (out[:, 1] == 0).all()
