@@ -2,8 +2,8 @@
 //   lookup    out[i] = scale T[ids[i]]
 //   gradient  dT[e] = scale sum_{i : ids[i] = e} g[i]      (+ the old dT[e])
 // The gradient sorts the ids (stable radix sort of (id, position) pairs), walks the sorted list in chunks of rows, adds a chunk's
-// rows of one id in fp32 in ascending position, and joins the ids that span chunks in a second, fixed order: the result is a
-// function of the inputs alone.  Rows of the dense gradient that no id names are set to zero by CTAs beside the sort's.
+// rows of one id in fp32 in ascending position, and joins the ids that span chunks in a second, fixed order: what is added to what
+// follows from the ids, their number, the table's rows and the width alone.  Rows of the dense gradient that no id names are set to zero by CTAs beside the sort's.
 //   short lists         one launch: every CTA owns a range of table rows, picks the ids that fall into it and sorts those
 //   up to 65,536        one cluster of sixteen CTAs sorts in shared memory, exchanging counts and pairs between its CTAs
 //   more                hist     digit counts of every tile, per pass (counted by atomics while the pass before scatters, frequent ids cost 12 us of 24)
@@ -158,6 +158,16 @@ bool short_list(int64_t rows, int n) { return n <= SMALL_MAX / 2 || (n <= SMALL_
 // 256: 70 and 74), else enough that the partial sums of frequent ids stay few (500,000 x 256, sum + join: 66 + 21 us with 32, 61 + 38 with
 // 16, 79 + 13 with 64).
 int chunk_rows(int n) { return n < (1 << 17) ? 8 : 32; }
+
+// In what order an id's rows are added must follow from the ids, the list's and the table's length and the width: not from the packs that
+// the types and the rows' alignment allow.  So the sizes of what is added together first are functions of the width: chunks that a CTA
+// joins (a power of two; its threads are whole groups whatever the pack, at most 1,024 of them), and stripes of a run in a short list.
+// (Groups of 2,048 columns instead of 1,024, which single columns' threads cannot hold: 300,000 x 256 bf16 of one id 64 us, with 1,024 71.)
+int group_chunks(int dim) { return 1024 % dim == 0 ? std::min(1024 / dim, SUM_THREADS) : 1; }
+int run_stripes(int dim) {
+    const int pack = dim % 8 == 0 ? 8 : (dim % 4 == 0 ? 4 : (dim % 2 == 0 ? 2 : 1));
+    return SMALL_THREADS / std::min(dim / pack, SMALL_THREADS);
+}
 
 struct GradScratch {
     uint2* pairs[2];                 // [n] (id, position) in the order of a pass, in turn
@@ -510,9 +520,9 @@ struct SumParams {
     int accumulate;
     float* part;
     int2* list; int32_t* list_count;
-    int group;                             // chunks per CTA of grad_sum_kernel, where its threads are whole chunks, else 1
+    int group;                             // chunks of one id that a CTA of grad_sum_kernel joins
     FastDiv vecs;
-    const int32_t* ids; int32_t padding_id; int rows_per_cta; int32_t* status;     // grad_small_kernel
+    const int32_t* ids; int32_t padding_id; int rows_per_cta, stripes; int32_t* status;     // grad_small_kernel
 };
 
 template <typename TO, int V>
@@ -529,14 +539,14 @@ __device__ __forceinline__ void finish_pack(const SumParams& p, uint32_t row, in
 
 // CTA c owns the table rows [c rows_per_cta, + rows_per_cta): it picks the ids that name them, sorts those as (row, position) words
 // in shared memory, and adds up each row's gradients: runs of up to SHORT by one group of threads (a pack of columns each),
-// longer ones by all groups in turn, whose sums are then added in order.  Bound by latency: 256 ids of 1,000 x 32 fp32 in 7.9 us a call.
+// longer ones in stripes, every stripes-th row to one, by all groups, and then the stripes in order.  Bound by latency: 256 ids of 1,000 x 32 fp32 in 7.9 us a call.
 template <typename TG, typename TO, int V>
 __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) {
     constexpr int SHORT = 32, U = 8;
     __shared__ uint32_t list[SMALL_MAX];       // local row << SMALL_BITS | position
     __shared__ uint16_t start[SMALL_MAX + 1];
     __shared__ uint32_t warp_cnt[SMALL_THREADS / 32];
-    __shared__ float red[SMALL_THREADS * V];
+    __shared__ float red[SMALL_THREADS * 8];      // stripes x columns at a time x V are at most as many
     grid_dependency_wait();
     allow_dependents();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -638,18 +648,25 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
     for (int r = 0; r < runs; ++r) {
         const int s = start[r], e = start[r + 1];
         if (e - s <= SHORT) continue;
+        const int parts = min(p.stripes, e - s);
         for (int c = v0; c - v0 < vecs; c += wide) {
-            float a[V];
+            if (group < groups && c < vecs)
+                for (int k = group; k < parts; k += groups) {
+                    float a[V];
 #pragma unroll
-            for (int q = 0; q < V; ++q) a[q] = 0.f;
-            if (group < groups && c < vecs) add_rows(s + group, e, groups, (int64_t)c * V, a);
+                    for (int q = 0; q < V; ++q) a[q] = 0.f;
+                    add_rows(s + k, e, p.stripes, (int64_t)c * V, a);
 #pragma unroll
-            for (int q = 0; q < V; ++q) red[tid * V + q] = a[q];
+                    for (int q = 0; q < V; ++q) red[(k * wide + v0) * V + q] = a[q];
+                }
             __syncthreads();
             if (group == 0 && c < vecs) {
-                for (int g = 1; g < groups; ++g) {
+                float a[V];
 #pragma unroll
-                    for (int q = 0; q < V; ++q) a[q] += red[(g * wide + v0) * V + q];
+                for (int q = 0; q < V; ++q) a[q] = red[v0 * V + q];
+                for (int k = 1; k < parts; ++k) {
+#pragma unroll
+                    for (int q = 0; q < V; ++q) a[q] += red[(k * wide + v0) * V + q];
                 }
                 finish_pack<TO, V>(p, (uint32_t)(r0 + (list[s] >> SMALL_BITS)), (int64_t)c * V, a);
             }
@@ -679,16 +696,20 @@ __device__ __forceinline__ void flush_run(const SumParams& p, int c, bool head, 
 // A thread's packs of the next DEPTH rows are on their way into its own places in shared memory, so the loop over the rows is one short
 // body: unrolled by eight with the packs in registers it did not stay in the instruction cache (136 us against 84 at 500,000 x 256, 60 now
 // that the rows are found by bisection: 4.9 TB/s).
+// CTAs have 256 threads, or, where smaller packs take more for a group of chunks, 512 or 1,024.
 constexpr int SUM_DEPTH = 8;
+__host__ __device__ constexpr int sum_threads(int v) { return v >= 4 ? SUM_THREADS : 1024 / v; }       // at most
+__host__ __device__ constexpr int sum_ring_bytes(int pack_bytes) { return pack_bytes >= 4 ? SUM_DEPTH * pack_bytes : 4; }       // per thread: rows on their way, then V sums
 template <typename TG, typename TO, int V, int L>
-__global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
+__global__ void __launch_bounds__(sum_threads(V)) grad_sum_kernel(SumParams p) {
     constexpr int BYTES = V * (int)sizeof(TG);
     constexpr bool ASYNC = BYTES >= 4;                    // (asynchronous copies take 4, 8 or 16 bytes)
-    constexpr int RING = ASYNC ? SUM_DEPTH * SUM_THREADS * BYTES : 0, SUMS = SUM_THREADS * V * 4;
-    __shared__ alignas(16) unsigned char ring[RING > SUMS ? RING : SUMS];
+    static_assert(sum_ring_bytes(BYTES) >= 4 * V && sum_ring_bytes(BYTES) * sum_threads(V) <= 48 * 1024, "a thread's places in shared memory");
+    extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_wait();
     allow_dependents();
-    const int64_t item = (int64_t)blockIdx.x * SUM_THREADS + threadIdx.x;
+    const int threads = V >= 4 ? SUM_THREADS : (int)blockDim.x;
+    const int64_t item = (int64_t)blockIdx.x * threads + threadIdx.x;
     const int64_t vecs = p.vecs.d;
     const int c = item < (1ll << 31) ? (int)p.vecs.div((uint32_t)item) : (int)(item / vecs);
     if (c >= p.chunks) return;
@@ -724,7 +745,7 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
         if constexpr (ASYNC) {
             if (i < to) {
                 const TG* src = grads + (int64_t)pairs[i].y * p.ld_grads;
-                const uint32_t dst = place + (i % SUM_DEPTH) * (SUM_THREADS * BYTES);
+                const uint32_t dst = place + (i % SUM_DEPTH) * (threads * BYTES);
                 if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
                 else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
             }
@@ -755,7 +776,7 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
             issue(i + SUM_DEPTH - 1);
             const uint32_t k = pairs[i].x;
             asm volatile("cp.async.wait_group %0;" ::"n"(SUM_DEPTH - 1) : "memory");
-            add(k, *reinterpret_cast<const Pack<TG, V>*>(ring + (i % SUM_DEPTH) * (SUM_THREADS * BYTES) + threadIdx.x * BYTES));
+            add(k, *reinterpret_cast<const Pack<TG, V>*>(ring + (i % SUM_DEPTH) * (threads * BYTES) + threadIdx.x * BYTES));
         }
     } else {             // single 16-bit elements: eight rows' loads together
 #pragma unroll 1
@@ -774,19 +795,24 @@ __global__ void __launch_bounds__(SUM_THREADS) grad_sum_kernel(SumParams p) {
             for (int u = 0; u < SUM_DEPTH; ++u) if (i0 + u < to) add(k[u], g[u]);
         }
     }
-    // a CTA whose chunks all lie inside one run leaves one partial sum, its first chunk's, for all of them
+    // a group of chunks that lies inside one run leaves one partial sum, its first chunk's
     if (p.group > 1 && is_head) {
-        const int64_t c0 = (int64_t)blockIdx.x * p.group, r1 = (c0 + p.group) * L;       // (the same answer in all its threads)
+        const int64_t c0 = c & ~(p.group - 1), r1 = (c0 + p.group) * L;                   // (the same answer in all threads of the group)
         if (c0 > 0 && r1 < p.n && p.pairs[c0 * L - 1].x == cur && p.pairs[r1].x == cur) {
-            float* const sums = reinterpret_cast<float*>(ring);
-            __syncthreads();                                                              // (the ring has been read)
+            const int vecs32 = (int)vecs, size = p.group * vecs32, at = (int)threadIdx.x / size;           // (128 threads or more)
+            // a thread's sums lie in its own places of the ring, which it has read
+            auto sum_of = [&](int thread, int e) -> float& {
+                constexpr int PLACE = ASYNC ? BYTES : 4;
+                return *reinterpret_cast<float*>(ring + (e * 4 / PLACE) * (threads * PLACE) + thread * PLACE + e * 4 % PLACE);
+            };
 #pragma unroll
-            for (int e = 0; e < V; ++e) sums[e * SUM_THREADS + threadIdx.x] = a[e];
-            __syncthreads();
+            for (int e = 0; e < V; ++e) sum_of(threadIdx.x, e) = a[e];
+            if (V == 8 && at) asm volatile("barrier.sync 2, %0;" ::"r"(size) : "memory");                  // (at most two groups, and those with packs of eight)
+            else asm volatile("barrier.sync 1, %0;" ::"r"(size) : "memory");
             if (c != c0) return;
             for (int g = 1; g < p.group; ++g) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) a[e] += sums[e * SUM_THREADS + g * (int)p.vecs.d + threadIdx.x];
+                for (int e = 0; e < V; ++e) a[e] += sum_of(threadIdx.x + g * vecs32, e);
             }
         }
     }
@@ -818,10 +844,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
             end += got;
             if (got < JOIN_THREADS) break;
         }
-        // partial sum j of the id: slot 1 of chunk c0, then slot 0 of the following ones, where a CTA of grad_sum_kernel that lies inside the
+        // partial sum j of the id: slot 1 of chunk c0, then slot 0 of the following ones, where a group of chunks that lies inside the
         // run counts as one; eight of a thread's on their way into shared memory at a time (with registers as their target they came
         // one by one, 4.5 us a round of eight)
-        const int64_t g0 = ceil_div_dev(c0 + 1, p.group), g1 = max(g0, end / p.group);    // those CTAs: [g0, g1)
+        const int64_t g0 = ceil_div_dev(c0 + 1, p.group), g1 = max(g0, end / p.group);    // those groups: [g0, g1)
         const int64_t lead = g1 > g0 ? g0 * p.group - c0 : end - c0 + 1;                  // parts before the first of them
         const int64_t parts = g1 > g0 ? lead + (g1 - g0) + (end - g1 * p.group + 1) : lead;
         auto chunk_of = [&](int64_t j) { return j < lead ? c0 + j : (j < lead + g1 - g0 ? (g0 + j - lead) * p.group : g1 * p.group + j - lead - (g1 - g0)); };
@@ -886,6 +912,7 @@ int launch_small(SumParams& p, int vec, cudaStream_t s) {
     int64_t per = ceil_div(p.rows, 148 * 4);
     per = std::max<int64_t>(1, std::min<int64_t>(per, (1ll << (32 - SMALL_BITS)) - 1));
     p.rows_per_cta = (int)per;
+    p.stripes = run_stripes(p.dim);
     return with_vector<sizeof(TG) == 2>(vec, [&](auto v) {
         return launch_status(launch_dependent(grad_small_kernel<TG, TO, decltype(v)::value>, dim3((unsigned)ceil_div(p.rows, per)), dim3(SMALL_THREADS), 0, s, p));
     });
@@ -894,10 +921,12 @@ int launch_small(SumParams& p, int vec, cudaStream_t s) {
 template <typename TG, typename TO, int L>
 int launch_sum(SumParams& p, int vec, cudaStream_t s) {
     p.vecs = FastDiv((uint32_t)(p.dim / vec));
-    p.group = SUM_THREADS % p.vecs.d == 0 ? SUM_THREADS / (int)p.vecs.d : 1;
-    const dim3 grid((unsigned)ceil_div((int64_t)p.chunks * p.vecs.d, SUM_THREADS));
+    p.group = group_chunks(p.dim);
+    const int threads = p.group > 1 ? std::max(SUM_THREADS, p.group * (int)p.vecs.d) : SUM_THREADS;
+    const dim3 grid((unsigned)ceil_div((int64_t)p.chunks * p.vecs.d, threads));
     const int rc = with_vector<sizeof(TG) == 2>(vec, [&](auto v) {
-        return launch_status(launch_dependent(grad_sum_kernel<TG, TO, decltype(v)::value, L>, grid, dim3(SUM_THREADS), 0, s, p));
+        constexpr int V = decltype(v)::value;
+        return launch_status(launch_dependent(grad_sum_kernel<TG, TO, V, L>, grid, dim3((unsigned)threads), (size_t)threads * sum_ring_bytes(V * (int)sizeof(TG)), s, p));
     });
     if (rc != KGE_OK || p.chunks < 3) return rc;
     const dim3 joins((unsigned)std::min<int64_t>(p.chunks / 2, 592), (unsigned)ceil_div(p.dim, JOIN_COLS));

@@ -84,3 +84,25 @@ def test_product_of_scales_far_from_one(T, K, M, N, Kd, ba, bb, fmt):
     _check(T, out[fits], want[fits], tol[fits])
     if M > 2 and N > 2:
         assert (out[1] == 0).all() and (out[:, 1] == 0).all()
+
+
+# ---- gradient --------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,E,kind", [(40, 3, "one"), (300, 5, "one"), (700, 40, "zipf"), (1024, 9, "blocks"), (2048, 8192, "one"), (3000, 7, "zipf"),
+                                      (3000, 2, "one"), (20_000, 30, "zipf"), (140_000, 11, "zipf"), (140_000, 3, "one")])
+@pytest.mark.parametrize("d", [1, 2, 4, 8, 16, 24, 64, 128, 256, 300, 512, 1024, 2304])
+def test_grad_adds_in_an_order_that_follows_the_ids_alone(T, K, n, E, kind, d):
+    """The same values in rows apart, rows shifted off their alignment and other types give the same bits, also where an id has a long run."""
+    if n * d > 40_000_000:
+        n = 40_000_000 // d
+    g = _gen(T, n + d)
+    ids = _id_list(T, g, kind, n, E)
+    values = T.randn((n, d), generator=g, device="cuda").to(T.bfloat16)
+    want = T.empty((E, d), device="cuda")
+    K.embedding_grad(ids, values, want, scale=0.75)
+    for tg, to, extra, shift in ((T.bfloat16, T.float32, 0, 1), (T.bfloat16, T.float32, 0, 2), (T.bfloat16, T.float32, 4, 4), (T.float32, T.float32, 0, 0),
+                                 (T.float32, T.float32, 1, 0), (T.float32, T.float32, 0, 2), (T.bfloat16, T.bfloat16, 0, 0), (T.float32, T.float16, 3, 1)):
+        grads, out = _strided(T, n, d, tg, extra, shift), _strided(T, E, d, to, extra, shift)
+        grads.copy_(values)
+        K.embedding_grad(ids, grads, out, scale=0.75)
+        assert T.equal(out, want.to(to)), (tg, to, extra, shift, int((out != want.to(to)).any(0).sum()))
