@@ -106,3 +106,44 @@ def test_grad_adds_in_an_order_that_follows_the_ids_alone(T, K, n, E, kind, d):
         grads.copy_(values)
         K.embedding_grad(ids, grads, out, scale=0.75)
         assert T.equal(out, want.to(to)), (tg, to, extra, shift, int((out != want.to(to)).any(0).sum()))
+
+
+@pytest.mark.parametrize("n,E,kind", [(900, 4, "one"), (1024, 50, "zipf"), (2048, 9000, "one"), (3000, 2, "one"), (5000, 600, "blocks"), (60_000, 70_000, "zipf"),
+                                      (65_536, 3, "one"), (65_537, 900, "zipf"), (131_071, 40, "one"), (131_072, 40, "one"), (140_003, 5000, "blocks"),
+                                      (200_000, 2_100_000, "zipf"), (300_000, 5000, "one"), (450_000, 77, "padded")])
+@pytest.mark.parametrize("d,tg,to", [(256, "bf16", "f32"), (32, "f32", "f32"), (36, "bf16", "f32"), (12, "f16", "f32"), (5, "f32", "f32"), (4, "bf16", "bf16")])
+def test_grad_of_whole_numbers_is_exact(T, K, n, E, kind, d, tg, to):
+    """Sums of small whole numbers stay below 2^24 (450,000 times 8), so every order of fp32 additions gives the same: no row may be lost or
+    counted twice, however long its id's run."""
+    if E * d > 30_000_000:
+        E = 30_000_000 // d
+    g = _gen(T, n + d + E)
+    ids = _id_list(T, g, kind, n, E)
+    grads = T.randint(-6, 9, (n, d), generator=g, device="cuda").to(_type(T, tg))
+    out, old = T.full((E, d), float("nan"), device="cuda", dtype=_type(T, to)), T.randint(-50, 50, (E, d), generator=g, device="cuda").to(_type(T, to))
+    keep = ids >= 0
+    want = T.zeros((E, d), dtype=T.float64, device="cuda").index_add_(0, ids[keep].long(), grads[keep].double())
+    assert want.abs().max() < 2 ** 24
+    K.embedding_grad(ids, grads, out)
+    assert T.equal(out, want.to(out.dtype)), int((out.double() != want).any(1).sum())
+    more = old.clone()
+    K.embedding_grad(ids, grads, more, accumulate=True)
+    assert T.equal(more, (want + old.double()).to(more.dtype))
+
+
+@pytest.mark.parametrize("n,E,d,kind,tg", [(24_576, 100_000, 128, "zipf", "f32"), (200_000, 500_000, 12, "zipf", "f32"), (300_000, 5000, 36, "one", "bf16"),
+                                           (500_000, 2, 16, "one", "bf16"), (150_000, 1000, 256, "zipf", "bf16"), (1000, 3, 40, "one", "f32")])
+def test_grad_is_as_near_as_its_depth_of_additions(T, K, n, E, d, kind, tg):
+    """A value passes through at most: the rows of two chunks (8 or 32 each) in turn, the chunks that are joined in a CTA, every 16th partial
+    sum of its run, and 16 stripes; in a list of one launch, every 51st row of its run (256 threads over five packs) and the 51 sums of those.
+    Each addition rounds once."""
+    g = _gen(T, n)
+    ids = _id_list(T, g, kind, n, E)
+    grads = T.randn((n, d), generator=g, device="cuda").to(_type(T, tg))
+    out = T.empty((E, d), device="cuda")
+    K.embedding_grad(ids, grads, out)
+    zeros = lambda: T.zeros((E, d), dtype=T.float64, device="cuda")
+    want, size = zeros().index_add_(0, ids.long(), grads.double()), zeros().index_add_(0, ids.long(), grads.double().abs())
+    chunk, group = 8 if n < 1 << 17 else 32, 1024 // d if 1024 % d == 0 else 1
+    depth = 2 * chunk + group + -(-n // (chunk * group * 16)) + -(-2 * group // 16) + 16 if n > 2048 else -(-n // 51) + 51
+    _check(T, out, want, depth * U * size, kind)
