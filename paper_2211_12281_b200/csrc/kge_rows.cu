@@ -521,6 +521,7 @@ struct SumParams {
     float* part;
     int2* list; int32_t* list_count;
     int group;                             // chunks of one id that a CTA of grad_sum_kernel joins
+    int first_col;                         // of a launch of grad_join_kernel
     FastDiv vecs;
     const int32_t* ids; int32_t padding_id; int rows_per_cta, stripes; int32_t* status;     // grad_small_kernel
 };
@@ -819,8 +820,8 @@ __global__ void __launch_bounds__(sum_threads(V)) grad_sum_kernel(SumParams p) {
     flush_run<TO, V>(p, c, is_head, tail_part && cur == end_key, cur, col, a);
 }
 
-// Ids that span more than two chunks: CTA (x, y) takes the x-th, (x + grid)-th, ... of the list and 64 columns.  Sixteen stripes
-// of sixteen threads add every 16th chunk's partial sum, then the stripes are added in order.
+// Ids that span more than two chunks: CTA (x, y) takes the x-th, (x + grid)-th, ... of the list and 64 columns from first_col on.  Sixteen
+// stripes of sixteen threads add every 16th chunk's partial sum, then the stripes are added in order.
 constexpr int JOIN_COLS = 64;
 __device__ __forceinline__ int64_t ceil_div_dev(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <typename TO, int L>
@@ -830,7 +831,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
     __shared__ float4 ring[U][JOIN_THREADS];
     grid_dependency_wait();
     const int lane = threadIdx.x % LANES, stripe = threadIdx.x / LANES;
-    const int col = blockIdx.y * JOIN_COLS + lane * 4;
+    const int col0 = p.first_col + blockIdx.y * JOIN_COLS, col = col0 + lane * 4;
     const int count = *p.list_count;
     for (int x = blockIdx.x; x < count; x += gridDim.x) {
         const int2 run = p.list[x];
@@ -868,7 +869,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) grad_join_kernel(SumParams p) {
         red[stripe][lane] = a;
         __syncthreads();
         if (threadIdx.x < JOIN_COLS) {
-            const int cc = blockIdx.y * JOIN_COLS + threadIdx.x;
+            const int cc = col0 + threadIdx.x;
             if (cc < p.dim) {
                 float sum = 0.f;
 #pragma unroll
@@ -929,8 +930,14 @@ int launch_sum(SumParams& p, int vec, cudaStream_t s) {
         return launch_status(launch_dependent(grad_sum_kernel<TG, TO, V, L>, grid, dim3((unsigned)threads), (size_t)threads * sum_ring_bytes(V * (int)sizeof(TG)), s, p));
     });
     if (rc != KGE_OK || p.chunks < 3) return rc;
-    const dim3 joins((unsigned)std::min<int64_t>(p.chunks / 2, 592), (unsigned)ceil_div(p.dim, JOIN_COLS));
-    return launch_status(launch_dependent(grad_join_kernel<TO, L>, joins, dim3(JOIN_THREADS), 0, s, p));
+    constexpr int64_t COLS = 65535ll * JOIN_COLS;           // a grid is no higher
+    for (int64_t first = 0; first < p.dim; first += COLS) {
+        p.first_col = (int)first;
+        const dim3 joins((unsigned)std::min<int64_t>(p.chunks / 2, 592), (unsigned)ceil_div(std::min(p.dim - first, COLS), JOIN_COLS));
+        const int rj = launch_status(launch_dependent(grad_join_kernel<TO, L>, joins, dim3(JOIN_THREADS), 0, s, p));
+        if (rj != KGE_OK) return rj;
+    }
+    return KGE_OK;
 }
 
 // Clusters of sixteen CTAs are no promise of the architecture: how many of them the device runs at a time is asked once.

@@ -147,3 +147,21 @@ def test_grad_is_as_near_as_its_depth_of_additions(T, K, n, E, d, kind, tg):
     chunk, group = 8 if n < 1 << 17 else 32, 1024 // d if 1024 % d == 0 else 1
     depth = 2 * chunk + group + -(-n // (chunk * group * 16)) + -(-2 * group // 16) + 16 if n > 2048 else -(-n // 51) + 51
     _check(T, out, want, depth * U * size, kind)
+
+
+def test_grad_of_rows_wider_than_a_grid_is_high(T, K):
+    """65,535 times 64 columns and more in a list whose ids are joined from partial sums."""
+    n, d = 1025, 65_535 * 64 + 72
+    ids = T.ones(n, dtype=T.int32, device="cuda")
+    ids[::100] = 0
+    grads = T.empty((n, d), dtype=T.bfloat16, device="cuda")
+    for i in range(n):
+        grads[i] = T.arange(d, device="cuda") % 7 + i % 3
+    out = T.full((3, d), float("nan"), device="cuda")
+    K.embedding_grad(ids, grads, out)
+    at = T.arange(n, device="cuda")
+    base = (T.arange(d, device="cuda") % 7).float()
+    for e in range(2):
+        mine = at[ids == e]
+        assert T.equal(out[e], base * len(mine) + float((mine % 3).sum()))
+    assert (out[2] == 0).all()
