@@ -391,6 +391,7 @@ int kge_ensemble_topk(const int32_t* lists, int32_t num_models, int32_t nq, int3
  * kge_embedding_grad      its gradient: table_grad[e, :] = scale sum of grads[i, :] over the i with ids[i] = e, added in fp32 in an
  *                         order that depends on ids, n, rows and dim alone (not on types, distances or addresses).  accumulate = 0 writes every row (zeros where no id points), 1 adds
  *                         to what the touched rows hold and leaves the others alone.  Padding and bad ids contribute nothing.
+ *                         dim at most 2^31 - 1025 (KGE_ERR_UNSUPPORTED above).
  *                         scratch: kge_embedding_grad_scratch_bytes(rows, dim, n) bytes, 256-byte aligned; calls that may
  *                         overlap (two streams, two captured graphs) need one each.
  */

@@ -138,6 +138,7 @@ constexpr int SMALL_MAX = 2048, SMALL_THREADS = 256, SMALL_BITS = 11;      // (S
 static_assert(SMALL_MAX == 1 << SMALL_BITS, "positions of a short list");
 constexpr int SUM_THREADS = 256;
 constexpr int JOIN_THREADS = 256;
+constexpr int GRAD_MAX_DIM = INT32_MAX - 1024;    // columns are counted in 32 bits, up to 256 past the last one
 
 struct SortPlan { int tiles, key_bits, passes, bits; };
 
@@ -1042,7 +1043,7 @@ int kge_embedding_lookup(const void* table, int32_t table_type, int64_t rows, in
 }
 
 size_t kge_embedding_grad_scratch_bytes(int64_t rows, int32_t dim, int32_t n) {
-    if (rows < 1 || rows > INT32_MAX || dim < 1 || n < 1) return 0;
+    if (rows < 1 || rows > INT32_MAX || dim < 1 || dim > GRAD_MAX_DIM || n < 1) return 0;
     return carve_grad(nullptr, rows, dim, n).bytes;
 }
 
@@ -1051,6 +1052,7 @@ int kge_embedding_grad(const int32_t* ids, int32_t n, const void* grads, int32_t
                        size_t scratch_bytes, int32_t* status, void* stream) {
     if (!is_float_type(grads_type) || !is_float_type(table_type) || rows < 1 || rows > INT32_MAX || dim < 1 || ld_grads < dim || ld_table < dim ||
         n < 0 || (accumulate != 0 && accumulate != 1)) return KGE_ERR_BAD_ARG;
+    if (dim > GRAD_MAX_DIM) return KGE_ERR_UNSUPPORTED;
     if (!table_grad || !aligned_to(table_grad, type_bytes(table_type)) || !aligned_to(status, 4)) return KGE_ERR_BAD_ARG;
     if (n > 0 && (!ids || !grads || !aligned_to(ids, 4) || !aligned_to(grads, type_bytes(grads_type)))) return KGE_ERR_BAD_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -1,0 +1,14 @@
+"""Refusals and sizes of the operators on rows at the ends of their ranges, without a GPU (the pointers are never followed)."""
+import pytest
+
+from test_row_operators_cpu import GRAD, K, _call  # noqa: F401
+
+INT32_MAX = (1 << 31) - 1
+
+
+@pytest.mark.parametrize("n", [4, 4000])
+@pytest.mark.parametrize("dim", [INT32_MAX, INT32_MAX - 200, INT32_MAX - 1023])
+def test_grad_refuses_widths_that_its_counters_do_not_hold(K, n, dim):
+    """Columns are counted in 32 bits, in steps of up to 256 beyond the last one; widths that this would carry past 2^31 are turned down."""
+    assert _call(K, "kge_embedding_grad", GRAD, GRAD, n=n, dim=dim, ld_grads=dim, ld_table=dim, scratch_bytes=1 << 62) == -5
+    assert K.embedding_grad_scratch_bytes(10, dim, n) == 0
