@@ -429,6 +429,7 @@ int kge_dropout(const void* x, int32_t x_type, const void* residual, void* out, 
  *                    block of 128 summed by the tensor cores, each block's sum times its two scales added in fp32 (also where the
  *                    two scales' own product would be too small or too large for that).  out fp32, bf16 or fp16; a_block, b_block:
  *                    1 or 128 rows to a scale; the operands' types may differ.
+ *                    status receives KGE_ERR_TIMEOUT if a wait in the kernel ran out; out is not what it should be then.
  *                    Where tiles are few, several CTAs share K and their sums are added in order: how many depends on the sizes and
  *                    the device, so the last bits may differ from one GPU to another, never from call to call on one.
  *                    The forward pass of a projection y = x W^T multiplies the forms along the columns of x and W; its gradients
@@ -525,6 +526,8 @@ int kge_debug_init_words(kge_handle* h, float* out, int64_t rows, int32_t width,
 
 int kge_debug_set_wait_limit(kge_handle* h, int32_t tries);
 int kge_debug_wait_probe(kge_handle* h, void* stream);
+/* The same limit for the calls of kge_fp8_matmul, which have no handle, in this process. */
+int kge_debug_set_product_wait_limit(int32_t tries);
 
 #ifdef __cplusplus
 }

@@ -107,6 +107,7 @@ SIGNATURES = {
     "kge_debug_capture_scores": (C.c_int, [_vp, _vp]),
     "kge_debug_set_wait_limit": (C.c_int, [_vp, C.c_int32]),
     "kge_debug_wait_probe": (C.c_int, [_vp, _vp]),
+    "kge_debug_set_product_wait_limit": (C.c_int, [C.c_int32]),
     "kge_lr_linear_decay": (C.c_float, [C.c_float, C.c_uint64, C.c_uint64]),
     "kge_ensemble_rank_scores": (C.c_int, [C.c_double, C.c_int32, _vp]),
     "kge_ensemble_topk": (C.c_int, [_vp, C.c_int32, C.c_int32, C.c_int32, _vp, C.c_int32, _vp, _vp, _vp]),

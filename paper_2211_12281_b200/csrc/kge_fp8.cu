@@ -951,6 +951,8 @@ template <int FORM> int configure_product() {
     }) == cudaSuccess ? KGE_OK : KGE_ERR_CUDA;
 }
 
+std::atomic<int> product_wait_limit{kDefaultWaitLimit};       // tries of a bounded wait, unless a test shortens it
+
 // How many clusters of `split` CTAs the device runs at a time: asked for once (what is left of a part of the chip takes none).
 int split_clusters(int split, int* clusters) {
     static std::atomic<int> known[kMaxDevices][FP_MAX_SPLIT + 1];        // one more than their number
@@ -1067,7 +1069,7 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
     const int ob = type_bytes(out_type);
     p.vec = ld_out * ob % 16 == 0 && aligned_to(out, 16) && (!addend || (ld_addend * ob % 16 == 0 && aligned_to(addend, 16)));
     p.twos = N % 2 == 0 && ld_out % 2 == 0 && aligned_to(out, 2 * ob) && (!addend || (ld_addend % 2 == 0 && aligned_to(addend, 2 * ob)));
-    p.status = status; p.wait_limit = kDefaultWaitLimit;
+    p.status = status; p.wait_limit = product_wait_limit.load(std::memory_order_relaxed);
     int sms = 0, rc = sm_count(&sms);
     if (rc != KGE_OK) return rc;
     if (ceil_div(M, 128) * ceil_div(N, 64) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;
@@ -1086,6 +1088,12 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
         case FP_NARROW: return launch_product<FP_NARROW>(ma, mb, p, 1, sms, s);
         default: return launch_product<FP_PAIR>(ma, mb, p, 1, sms, s);
     }
+}
+
+int kge_debug_set_product_wait_limit(int32_t tries) {
+    if (tries < 0) return KGE_ERR_BAD_ARG;
+    product_wait_limit.store(tries == 0 ? kDefaultWaitLimit : tries, std::memory_order_relaxed);
+    return KGE_OK;
 }
 
 }  // extern "C"

@@ -86,6 +86,37 @@ def test_product_of_scales_far_from_one(T, K, M, N, Kd, ba, bb, fmt):
         assert (out[1] == 0).all() and (out[:, 1] == 0).all()
 
 
+def test_product_waits_that_run_out_leave_the_context_usable(T, K):
+    """Limits so short that a wait runs out anywhere in any form of the kernel: the call reports KGE_ERR_TIMEOUT (or got by), and the next one is
+    right."""
+    sizes = [(130, 700, 2050, 1), (3000, 2502, 125, 128), (30_000, 60, 300, 128), (2600, 2048, 2300, 128), (2600, 2048, 2300, 1)]
+    ran_out = 0
+    for M, N, Kd, bb in sizes:
+        g = _gen(T, M)
+        a, sa = _empty8(T, M, Kd, "e4m3"), T.empty(((Kd + 127) // 128, M), device="cuda")
+        b, sb = _empty8(T, N, Kd, "e4m3"), T.empty(((Kd + 127) // 128, N if bb == 1 else (N + 127) // 128), device="cuda")
+        K.fp8_quantize(T.randn((M, Kd), generator=g, device="cuda"), a, sa)
+        K.fp8_quantize(T.randn((N, Kd), generator=g, device="cuda"), b, sb, block_rows=bb)
+        want, out, status = T.empty((M, N), device="cuda"), T.empty((M, N), device="cuda"), T.zeros(1, dtype=T.int32, device="cuda")
+        K.fp8_matmul(a, sa, b, sb, want, status=status)
+        assert status.item() == 0
+        try:
+            for tries in (1, 1, 1, 1, 2, 4, 8, 16, 64):
+                assert K.lib().kge_debug_set_product_wait_limit(tries) == 0
+                K.fp8_matmul(a, sa, b, sb, out, status=status)
+                assert status.item() in (0, -11)
+                ran_out += status.item() != 0
+                if status.item() == 0:
+                    assert T.equal(out, want)
+                status.zero_()
+        finally:
+            K.lib().kge_debug_set_product_wait_limit(0)
+        out.fill_(float("nan"))
+        K.fp8_matmul(a, sa, b, sb, out, status=status)
+        assert status.item() == 0 and T.equal(out, want)
+    assert ran_out
+
+
 # ---- gradient --------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,E,kind", [(40, 3, "one"), (300, 5, "one"), (700, 40, "zipf"), (1024, 9, "blocks"), (2048, 8192, "one"), (3000, 7, "zipf"),

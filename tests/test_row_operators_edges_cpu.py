@@ -12,3 +12,8 @@ def test_grad_refuses_widths_that_its_counters_do_not_hold(K, n, dim):
     """Columns are counted in 32 bits, in steps of up to 256 beyond the last one; widths that this would carry past 2^31 are turned down."""
     assert _call(K, "kge_embedding_grad", GRAD, GRAD, n=n, dim=dim, ld_grads=dim, ld_table=dim, scratch_bytes=1 << 62) == -5
     assert K.embedding_grad_scratch_bytes(10, dim, n) == 0
+
+
+def test_wait_limit_of_the_product_is_checked(K):
+    fn = K.lib().kge_debug_set_product_wait_limit
+    assert fn(-1) == -1 and fn(5) == 0 and fn(0) == 0
