@@ -196,3 +196,78 @@ def test_grad_of_rows_wider_than_a_grid_is_high(T, K):
         mine = at[ids == e]
         assert T.equal(out[e], base * len(mine) + float((mine % 3).sum()))
     assert (out[2] == 0).all()
+
+
+# ---- arrays beyond 2^31 elements -------------------------------------------------------------------------------------
+
+def _halves_of(groups, seed, step, site):
+    """The documented 16-bit numbers of these groups of eight elements."""
+    x = [np.asarray(groups, dtype=np.uint64)] + [np.full(len(groups), v, dtype=np.uint64) for v in (step & 0xFFFFFFFF, step >> 32, (1 << 31) + site)]
+    k0, k1, low, m = seed & 0xFFFFFFFF, seed >> 32, np.uint64(0xFFFFFFFF), np.uint64(32)
+    for _ in range(10):
+        p, q = x[0] * np.uint64(0xD2511F53), x[2] * np.uint64(0xCD9E8D57)
+        x = [(q >> m) ^ x[1] ^ np.uint64(k0), q & low, (p >> m) ^ x[3] ^ np.uint64(k1), p & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    return np.stack([h for w in x for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))], 1).reshape(-1)
+
+
+def test_dropout_of_2_to_the_34_elements(T, K):
+    n = 1 << 34
+    x = T.ones(n, dtype=T.bfloat16, device="cuda")
+    K.dropout(x, x, 0.25, 77, 5, site=3)
+    for at in (0, (1 << 31) - 4096, (1 << 32) - 4096, (1 << 33) - 4096, n - 8192):
+        keep = T.from_numpy(_halves_of(np.arange(at // 8, at // 8 + 1024), 77, 5, 3) >= 16384).cuda()
+        assert T.equal(x[at:at + 8192], T.where(keep, 4.0 / 3.0, 0.0).to(T.bfloat16))
+    del x
+
+
+def test_quantize_and_product_beyond_two_to_the_31_elements(T, K):
+    """2.2 M rows of 1,024: values in and out in both orientations, then as an operand; and an output of 70,000 x 32,000."""
+    g = _gen(T, 31)
+    rows, cols = 2_200_000, 1024
+    x = T.empty((rows, cols), dtype=T.bfloat16, device="cuda")
+    for r in range(0, rows, 100_000):
+        x[r:r + 100_000] = T.randn((100_000, cols), generator=g, device="cuda")
+    q, s = _empty8(T, rows, cols, "e4m3"), T.empty((8, rows), device="cuda")
+    qt, st = _empty8(T, cols, rows, "e4m3"), T.empty(((rows + 127) // 128, cols), device="cuda")
+    K.fp8_quantize(x, q, s, qt, st)
+    for r in (0, 2_097_152 - 128, 2_097_152, rows // 128 * 128 - 128):         # (2,097,152 rows are 2^31 values)
+        some = x[r:r + 256]
+        want, ws = _quantized(T, some, "e4m3", 1, False)
+        assert T.equal(q[r:r + 256].float().double(), want) and T.equal(s[:, r:r + 256], ws)
+        want, ws = _quantized(T, some.t(), "e4m3", 1, False)
+        assert T.equal(qt[:, r:r + 256].float().double(), want) and T.equal(st[r // 128:r // 128 + 2], ws)
+    del x, qt, st
+    w, ws = _empty8(T, 40, cols, "e4m3"), T.empty((8, 1), device="cuda")
+    K.fp8_quantize(T.randn((40, cols), generator=g, device="cuda"), w, ws, block_rows=128)
+    out, status = T.empty((rows, 40), device="cuda"), T.zeros(1, dtype=T.int32, device="cuda")
+    K.fp8_matmul(q, s, w, ws, out, status=status)
+    vw = _stands_for(T, w, ws)
+    for r in (0, 2_097_152 - 150, rows - 300):
+        va = _stands_for(T, q[r:r + 300], s[:, r:r + 300])
+        _check(T, out[r:r + 300], va @ vw.t(), _product_tol(T, va, vw, cols))
+    del out, w
+    a, sa, b, sb = q[:70_000, :64], s[:1, :70_000].contiguous(), q[100_000:132_000, :64], s[:1, 100_000:132_000].contiguous()
+    out = T.empty((70_000, 32_000), dtype=T.bfloat16, device="cuda")
+    K.fp8_matmul(a, sa, b, sb, out, status=status)
+    vb = _stands_for(T, b, sb)
+    for r in (0, 67_100, 69_800):                                              # (67,109 rows are 2^31 values)
+        va = _stands_for(T, a[r:r + 200], sa[:, r:r + 200])
+        _check(T, out[r:r + 200], va @ vb.t(), _product_tol(T, va, vb, 64))
+    assert status.item() == 0
+
+
+def test_lookup_and_grad_of_more_than_two_to_the_31_elements_in_a_list(T, K):
+    n, E, d = 8_500_000, 1000, 256
+    g = _gen(T, 32)
+    ids = T.randint(0, E, (n,), generator=g, device="cuda", dtype=T.int32)
+    table = T.randint(-9, 10, (E, d), generator=g, device="cuda").to(T.bfloat16)
+    rows = T.empty((n, d), dtype=T.bfloat16, device="cuda")
+    K.embedding_lookup(table, ids, rows, scale=2.0)
+    out, want = T.empty((E, d), device="cuda"), T.zeros((E, d), dtype=T.float64, device="cuda")
+    for r in range(0, n, 500_000):
+        some = rows[r:r + 500_000]
+        assert T.equal(some, table[ids[r:r + 500_000].long()] * 2)
+        want.index_add_(0, ids[r:r + 500_000].long(), some.double())
+    K.embedding_grad(ids, rows, out)
+    assert T.equal(out.double(), want)                    # (whole numbers: 8,500 rows of at most 18 to an id or so)
