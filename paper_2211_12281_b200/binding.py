@@ -371,6 +371,8 @@ def fp8_quantize(x, q=None, scales=None, qt=None, scales_t=None, block_rows=1, p
     [ceil(K / 128), R] (block_rows = 1) or [ceil(K / 128), ceil(R / 128)] (128), and / or the same of x^T in qt [K, R], scales_t."""
     w = "kge_fp8_quantize"
     tx, (rows, cols, lx) = _type_of(x, w, "x", _FLOAT), _matrix(x, w, "x")
+    if block_rows not in (1, 128):
+        raise _bad(w, f"block_rows is {block_rows}, not 1 or 128")
     code, at, ld = None, [None, None, None, None], [0, 0]
     for i, (name, t, s, r, k) in enumerate((("q", q, scales, rows, cols), ("qt", qt, scales_t, cols, rows))):
         if t is None:

@@ -17,3 +17,11 @@ def test_grad_refuses_widths_that_its_counters_do_not_hold(K, n, dim):
 def test_wait_limit_of_the_product_is_checked(K):
     fn = K.lib().kge_debug_set_product_wait_limit
     assert fn(-1) == -1 and fn(5) == 0 and fn(0) == 0
+
+
+@pytest.mark.parametrize("block_rows", [0, -1, 64, 256])
+def test_binding_refuses_blocks_of_other_heights(K, block_rows):
+    import torch
+    with pytest.raises(K.KgeError) as e:
+        K.fp8_quantize(torch.zeros((4, 64)), torch.zeros((4, 64), dtype=torch.float8_e4m3fn), torch.zeros((1, 4)), block_rows=block_rows)
+    assert e.value.code == -1 and "block_rows" in str(e.value)
