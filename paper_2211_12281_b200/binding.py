@@ -320,7 +320,8 @@ def embedding_lookup(table, ids, out, scale=1.0, padding_id=-1, status=None):
 
 def embedding_grad_scratch_bytes(rows, dim, n) -> int:
     """Bytes of scratch an embedding_grad of n ids into a table of `rows` rows needs (a tensor of 256 more is always enough)."""
-    return int(lib().kge_embedding_grad_scratch_bytes(rows, dim, n))
+    w = "kge_embedding_grad_scratch_bytes"
+    return int(lib().kge_embedding_grad_scratch_bytes(_int32(rows, w, "rows"), _int32(dim, w, "width"), _int32(n, w, "number of ids")))
 
 
 def embedding_grad(ids, grads, table_grad, scale=1.0, padding_id=-1, accumulate=False, scratch=None, status=None):

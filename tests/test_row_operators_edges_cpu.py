@@ -25,3 +25,11 @@ def test_binding_refuses_blocks_of_other_heights(K, block_rows):
     with pytest.raises(K.KgeError) as e:
         K.fp8_quantize(torch.zeros((4, 64)), torch.zeros((4, 64), dtype=torch.float8_e4m3fn), torch.zeros((1, 4)), block_rows=block_rows)
     assert e.value.code == -1 and "block_rows" in str(e.value)
+
+
+@pytest.mark.parametrize("rows,dim,n", [(10, 8, (1 << 32) + 5), (10, (1 << 32) + 8, 5000), (1 << 70, 8, 5000), (10, 8, -(1 << 40))])
+def test_scratch_sizes_of_numbers_that_are_cut_off_are_refused(K, rows, dim, n):
+    """Not the size for what is left of the number in 32 (or 64) bits."""
+    with pytest.raises(K.KgeError) as e:
+        K.embedding_grad_scratch_bytes(rows, dim, n)
+    assert e.value.code == -1
