@@ -182,7 +182,7 @@ __device__ __forceinline__ void load8(const QuantParams& p, Eight<TX>& e, int64_
 }
 
 // One CTA per 128 x 128 tile: thread (rg, cg) holds rows 8 rg .. + 8 and columns 8 cg .. + 8, so both forms come of one read.  24,576 x 768
-// bf16 in 17 us (one form alone 10 to 11); issue slots two thirds busy at four CTAs an SM.
+// bf16 in 17.5 us, calls in a row (one form alone 10 to 11; 22 with cold caches); issue slots two thirds busy at four CTAs an SM.
 template <typename TX, int FMT, bool SQUARE, bool POW2>
 __global__ void __launch_bounds__(256, sizeof(TX) == 2 ? 4 : 2) quantize_kernel(QuantParams p) {
     __shared__ uint32_t part[16][128];
@@ -982,9 +982,10 @@ int split_clusters(int split, int* clusters) {
 //   shared K      as many CTAs to a tile as run at a time (512 x 768 x 4096: six to each of 24 tiles, of which some wait, 16.0 us, four 9.3,
 //                 one 16.2), where the blocks that a CTA is spared outweigh the join: a block takes 0.4 us, the join 0.4 + 2 for 128 rows
 //                 (128 x 768 x 512: 5.8 us shared, 4.5 not; x 4096: 7.5 and 15.5; one row, 256 x 512: 4.2 and 4.9)
-//   256 columns   where K is long and they fill the SMs (8192 x 4096 x 8192 bf16: 278 us, in pairs of 128 columns 315; 4096 x 4096 x 4096: 85
-//                 and 82; 2048 x 4096 x 1024 and 16,384 x 8192 x 512: no difference)
-//   64 columns    or pairs: 24,576 x 256 x 768 with an addend 19.6 and 21.7 us, 24,576 x 768 x 256 24.5 and 22.9
+//   256 columns   where K is long and they fill the SMs (8192 x 4096 x 8192 bf16: 291 us, in pairs of 128 columns 334; 4096 x 4096 x 4096: 90
+//                 and 96; 2048 x 4096 x 1024: no difference; 16,384 x 8192 x 512: 145 and 128)
+//   64 columns    or pairs: 24,576 x 256 x 768 with an addend 18.2 and 21.2 us, 24,576 x 768 x 256 21.1 and 20.8, 500,000 x 256 x 768
+//                 295 and 280
 struct ProductPlan { int form, split; };
 int product_plan(int64_t M, int64_t N, int kblocks, bool ragged_addend, int sms, ProductPlan* plan) {
     const int64_t tiles128 = ceil_div(M, FP_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, FP_BM) * ceil_div(N, 256);
@@ -996,7 +997,7 @@ int product_plan(int64_t M, int64_t N, int kblocks, bool ragged_addend, int sms,
         if (rc != KGE_OK) return rc;
         if (tiles128 <= room) { *plan = {FP_SPLIT, split}; return KGE_OK; }
     }
-    // (an addend whose rows are not whole 16-byte words passes through shared memory that the wide form has not: 187 us there, 165 in
+    // (an addend whose rows are not whole 16-byte words passes through shared memory that the wide form has not: 187 us there, 149 in
     // pairs at 4096 x 4095 x 4096)
     if (tiles256 >= sms && kblocks >= 16 && !ragged_addend) { *plan = {FP_WIDE, 1}; return KGE_OK; }
     // few blocks of K: memory sets the pace, and what counts is how well whole rounds of tiles fill the SMs

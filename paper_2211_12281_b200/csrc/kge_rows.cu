@@ -10,7 +10,7 @@
 //                       scan     the counts become sums over the tiles before
 //                       scatter  one stable split by a digit
 //   then                sum      chunks of sorted rows; what ends inside its chunk or the next one is final, the rest leaves partial sums
-//                       join     one CTA per (id that spans more, 32 columns): partial sums in a fixed order
+//                       join     one CTA per (id that spans more, 64 columns): partial sums in a fixed order
 #include <algorithm>
 #include <type_traits>
 
@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) grad_small_kernel(SumParams p) 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t r0 = (int64_t)blockIdx.x * p.rows_per_cta;
     const int nr = (int)min((int64_t)p.rows_per_cta, (int64_t)p.rows - r0);
-    // the ids of this CTA's rows, four to a thread in the list's order
+    // the ids of this CTA's rows, eight to a thread in the list's order
     int32_t id[SMALL_MAX / SMALL_THREADS];
     int mine = 0;
 #pragma unroll
