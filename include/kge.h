@@ -382,8 +382,8 @@ int kge_ensemble_topk(const int32_t* lists, int32_t num_models, int32_t nq, int3
  * no handle: tables, lists and results are the caller's device arrays on the current device, `ld...` are distances between rows in
  * elements, types are kge_dtype_t, arithmetic is fp32 with one rounding at the end.  They enqueue on `stream`, allocate nothing,
  * and may be captured into a CUDA graph.  status: device int32 (or NULL) that receives the first code found on the device, as the
- * status word of a handle does; the caller clears it.  A call on no rows returns KGE_OK without touching its arrays.  Results must
- * not overlap what a call reads, but where it says so.
+ * status word of a handle does; the caller clears it.  A call on no rows returns KGE_OK without touching its arrays (but for a dense
+ * gradient of no ids, which is zeros).  Results must not overlap what a call reads, but where it says so.
  *
  * kge_embedding_lookup    out[i, :] = scale table[ids[i], :] for i < n.  An id equal to padding_id (-1, as the top-k lists leave
  *                         in unused places, or any other) gives a row of zeros, an id outside [0, rows) does so too and records
