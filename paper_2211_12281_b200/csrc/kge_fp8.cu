@@ -1,13 +1,12 @@
 // 8-bit floating point with a scale for each block of 128 along the contraction index: making such operands, and their product.
 //   quantise   s = amax / top (or the next power of two), q = the 8-bit value nearest to x / s; one scale per 1 x 128 or 128 x 128 block
 //   product    C[m, n] = sum_kb sA[kb, m] sB[kb, n] sum_{k in kb} A[m, k] B[n, k]   (+ C0[m, n])
-#include <cuda.h>
 #include <cuda_fp8.h>
 
 #include <algorithm>
 #include <type_traits>
 
-#include "kge_ops.cuh"
+#include "kge_product.cuh"
 
 namespace kge {
 
@@ -354,7 +353,6 @@ int launch_quantize(const QuantParams& p, int fmt, bool square, cudaStream_t s) 
 constexpr int FP_BM = 128, FP_BK = 128;                   // BK bytes = one 128-byte swizzle row
 constexpr uint32_t FP_BOX_BYTES = 128 * FP_BK;            // 128 rows of an operand
 constexpr int FP_NACC = 2;                                // block sums in tensor memory
-constexpr int FP_COLS = 64;                               // columns of the tile per epilogue warp
 // Four forms of the kernel: tiles of 256 columns, one CTA an SM, for many blocks of K; tiles of 128, two CTAs an SM (one loads and
 // multiplies while the other stores), or of 64, three CTAs an SM, for few; tiles of 128 whose blocks of K a cluster shares, where
 // tiles are few.
@@ -363,7 +361,7 @@ constexpr int FP_MAX_SPLIT = 8;           // CTAs that share a tile's blocks of 
 __host__ __device__ constexpr int fp_bn(int form) { return form == FP_WIDE ? 256 : (form == FP_NARROW ? 64 : 128); }
 __host__ __device__ constexpr int fp_box_rows(int form) { return form == FP_NARROW ? 64 : 128; }             // of B per copy
 __host__ __device__ constexpr int fp_stages(int form) { return form == FP_WIDE ? 4 : (form == FP_SPLIT ? 6 : 2); }
-__host__ __device__ constexpr int fp_epi_warps(int form) { return 4 * fp_bn(form) / FP_COLS; }
+__host__ __device__ constexpr int fp_epi_warps(int form) { return 4 * fp_bn(form) / OUT_COLS; }
 __host__ __device__ constexpr int fp_threads(int form) { return 32 * (4 + fp_epi_warps(form)); }     // (four more: copies, MMAs, a look at the scales, one idle)
 __host__ __device__ constexpr int fp_ctas_per_sm(int form) { return form == FP_PAIR ? 2 : (form == FP_NARROW ? 3 : 1); }
 __host__ __device__ constexpr uint32_t fp_stage_bytes(int form) { return FP_BOX_BYTES + (uint32_t)fp_bn(form) * FP_BK; }
@@ -377,28 +375,16 @@ __host__ __device__ constexpr size_t fp_smem_bytes(int form) {
     return (size_t)fp_stages(form) * fp_stage_bytes(form) + fp_epi_warps(form) * 32 * fp_store_row(form) + fp_slots(form) * (128 + fp_bn(form)) * 4 + 256;
 }
 
-struct ProductParams {
-    int64_t M, N;
+struct ProductParams : ProductOut {
     int kblocks, kper;                    // blocks of K in all, and per CTA of a cluster
     int tiles_n, items;
     const float *sa, *sb;
     int64_t sa_ld, sb_ld;                 // scales per block of K
     int a_square, b_square;               // a scale serves 128 rows
-    const void* addend; int64_t ld_addend;
-    void* out; int64_t ld_out; int out_type;
-    int vec, twos;                        // rows of out (and addend) start at multiples of 16 bytes; of two elements, N even
     int32_t* status; int wait_limit;
     uint32_t idesc;
 };
 
-__device__ __forceinline__ void fp_tma_load(void* dst, const CUtensorMap* tm, int x, int y, uint64_t* bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(smem_u32(dst)), "l"(tm), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
-}
-// Shared-memory descriptor of a K-major operand tile with the 128-byte swizzle: rows of 128 bytes, groups of eight rows 1024 bytes apart.
-__device__ __forceinline__ uint64_t fp_desc(uint32_t addr) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-}
 // Instruction descriptor: D fp32, A and B 8-bit (0 = e4m3, 1 = e5m2), both K-major.
 constexpr uint32_t fp_idesc(int m, int n, int fa, int fb) {
     return (1u << 4) | ((uint32_t)fa << 7) | ((uint32_t)fb << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
@@ -407,37 +393,6 @@ __device__ __forceinline__ void fp_mma(uint32_t d, uint64_t a, uint64_t b, uint3
     asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void fp_commit(uint64_t* bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void fp_copy4(uint32_t dst, const float* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void fp_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fp_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// 16 consecutive columns of this thread's tensor-memory lane.  Nothing may look at the registers before fp_tmem_wait has passed them on.
-__device__ __forceinline__ void fp_tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr));
-}
-// Waits for this thread's tensor-memory loads; the registers pass through, so that nothing that uses them moves ahead.
-__device__ __forceinline__ void fp_tmem_wait(uint32_t (&r)[16]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
-}
-__device__ __forceinline__ uint64_t two_words(uint32_t a, uint32_t b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b)); return r; }
-// Two fp32 operations in one instruction, each rounded as a single one would be.
-__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ float2 unpair(uint64_t a) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a)); return r; }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-
 // A block's sum x joins c as x (a b), a and b the block's scales, where a b is a normal number (or not finite: a block that stands for NaN).
 // Where it is not, as (x a) b.  |x| is 0 or between 2^-32 and 2^39 (products of 8-bit values, 128 of them): with a b below the normal
 // numbers a and b are below 1 and x a is off by half a step of the smallest numbers at most; with a b beyond the largest number, scales
@@ -458,169 +413,6 @@ __device__ __forceinline__ bool fp_near_one(float s) { return __float_as_uint(s)
 __device__ __forceinline__ int fp_scales_a(const ProductParams& p, int m0, int lane) { return p.a_square ? (lane == 0 ? 1 : 0) : (int)p.M - m0 - lane; }
 template <int BN> __device__ __forceinline__ int fp_scales_b(const ProductParams& p, int n0, int lane) {
     return p.b_square ? (lane < (BN + 127) / 128 && n0 + 128 * lane < p.N ? 1 : 0) : (int)p.N - n0 - lane;
-}
-
-// Registers of a warpgroup, out of what the block was launched with.
-template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-
-// Calls f with a value of the output type.
-template <class F> __device__ __forceinline__ void fp_with_out(int t, F&& f) {
-    if (t == KGE_F32) f(float());
-    else if (t == KGE_BF16) f(__nv_bfloat16());
-    else f(__half());
-}
-
-// A pack of a row's columns.
-template <typename TO, int V>
-__device__ __forceinline__ void fp_put(const ProductParams& p, int row, int col, const Pack<TO, V>& o) {
-    TO* dst = static_cast<TO*>(p.out) + row * p.ld_out + col;
-    if (p.vec && col + V <= p.N) *reinterpret_cast<Pack<TO, V>*>(dst) = o;
-    else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) if (col + e < p.N) dst[e] = o.v[e];
-    }
-}
-
-// Where rows do not start at multiples of 16 bytes, and at the matrix's edges: f(row, column, place in shared memory) for W elements at a
-// time of the warp's 32 rows x ROW bytes, lanes side by side along the columns.
-template <typename TO, int ROW, int W, class F>
-__device__ __forceinline__ void fp_each(const ProductParams& p, int row0, int col0, float4* st, int lane, F&& f) {
-    constexpr int V = 16 / sizeof(TO), UNITS = ROW / 16, TURN = UNITS == 2 ? 2 : 0, PER_ROW = ROW / (int)sizeof(TO) / W;
-#pragma unroll 4
-    for (int i = 0; i < PER_ROW; ++i) {
-        const int at = i * 32 + lane, r = at / PER_ROW, c = at % PER_ROW * W;
-        if (row0 + r < p.M && col0 + c < p.N)
-            f(row0 + r, col0 + c, reinterpret_cast<TO*>(st) + (r * UNITS + ((c / V) ^ ((r >> TURN) & (UNITS - 1)))) * V + c % V);
-    }
-}
-
-// A warp's 32 rows x 64 columns, ROW bytes of each row at a time through shared memory, so that a store instruction covers whole
-// 32-byte sectors, or, with 128 bytes, whole lines.  (16-byte unit i of row r lies at i ^ (r mod units): no bank conflicts.)
-template <typename TO, int ROW>
-__device__ __forceinline__ void fp_store(const ProductParams& p, int row0, int col0, const uint64_t (&acc)[FP_COLS / 2], float4* st, int lane) {
-    constexpr int V = 16 / sizeof(TO), UNITS = ROW / 16, PASS = ROW / sizeof(TO);      // columns per unit, units and columns per pass
-    constexpr int TURN = UNITS == 2 ? 2 : 0;                                            // rows 4 apart share banks at 32 bytes a row
-    // a warp's part that lies inside the matrix is stored without a look at its edges
-    const bool inside = p.vec && row0 + 32 <= p.M && col0 + FP_COLS <= p.N;
-    TO* const first = static_cast<TO*>(p.out) + (row0 + lane / UNITS) * p.ld_out + col0 + V * (lane % UNITS);
-    const int64_t step = (32 / UNITS) * p.ld_out;
-#pragma unroll
-    for (int c = 0; c < FP_COLS; c += PASS) {
-#pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            Pack<TO, V> own;
-#pragma unroll
-            for (int e = 0; e < V; e += 2) {
-                const float2 x = unpair(acc[(c + i * V + e) / 2]);
-                own.v[e] = from_float<TO>(x.x);
-                own.v[e + 1] = from_float<TO>(x.y);
-            }
-            st[lane * UNITS + (i ^ ((lane >> TURN) & (UNITS - 1)))] = *reinterpret_cast<const float4*>(&own);
-        }
-        __syncwarp();
-        const int r0 = lane / UNITS, unit = lane % UNITS;
-        if (inside) {
-            TO* dst = first + c;
-#pragma unroll
-            for (int j = 0; j < UNITS; ++j) {
-                const int r = j * (32 / UNITS) + r0;
-                *reinterpret_cast<float4*>(dst) = st[r * UNITS + (unit ^ ((r >> TURN) & (UNITS - 1)))];
-                dst += step;
-            }
-        } else if (sizeof(TO) == 2 && p.twos) {
-            fp_each<TO, ROW, 2>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) {
-                *reinterpret_cast<uint32_t*>(static_cast<TO*>(p.out) + row * p.ld_out + col) = *reinterpret_cast<const uint32_t*>(at);
-            });
-        } else {
-            fp_each<TO, ROW, 1>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { static_cast<TO*>(p.out)[row * p.ld_out + col] = *at; });
-        }
-        __syncwarp();
-    }
-}
-
-// The addend of the same tile joins the accumulators in fp32 before they are rounded.
-// With 128-byte rows it passes through the warp's shared memory: fp_fetch_addend starts the copies of a pass (the first one's while
-// the tile is computed), fp_add_staged waits for them.
-// (a copy takes 16 bytes, or 4: two 16-bit elements; rows of 16-bit elements that start in between are read by the lanes themselves)
-template <typename TO>
-__device__ __forceinline__ void fp_fetch_addend(const ProductParams& p, int row0, int col0, int c, float4* st, int lane) {
-    constexpr int V = 16 / sizeof(TO), FOUR = 4 / (int)sizeof(TO);
-    const TO* const add = static_cast<const TO*>(p.addend);
-    if (p.vec) {
-        const int unit = lane & 7, col = col0 + c + V * unit;
-        const int bytes = min(V, (int)p.N - col) * (int)sizeof(TO);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = j * 4 + (lane >> 3), row = row0 + r;
-            if (row < p.M && bytes > 0)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(st + r * 8 + (unit ^ (r & 7)))), "l"(add + row * p.ld_addend + col),
-                             "r"(bytes) : "memory");
-        }
-    } else if (sizeof(TO) == 4 || p.twos) {
-        fp_each<TO, 128, FOUR>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { fp_copy4(smem_u32(at), reinterpret_cast<const float*>(add + row * p.ld_addend + col)); });
-    } else {
-        fp_each<TO, 128, 1>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { *at = add[row * p.ld_addend + col]; });
-    }
-}
-template <typename TO>
-__device__ __forceinline__ void fp_add_staged(const ProductParams& p, int row0, int col0, uint64_t (&acc)[FP_COLS / 2], float4* st, int lane) {
-    constexpr int V = 16 / sizeof(TO), PASS = 128 / sizeof(TO);
-#pragma unroll
-    for (int c = 0; c < FP_COLS; c += PASS) {
-        if (c > 0) fp_fetch_addend<TO>(p, row0, col0, c, st, lane);
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 w = st[lane * 8 + (i ^ (lane & 7))];
-            const Pack<TO, V> a = *reinterpret_cast<const Pack<TO, V>*>(&w);
-#pragma unroll
-            for (int e = 0; e < V; e += 2) acc[(c + i * V + e) / 2] = add2(acc[(c + i * V + e) / 2], pair(to_float(a.v[e]), to_float(a.v[e + 1])));
-        }
-        __syncwarp();
-    }
-}
-// Or a lane reads its own row, a 32-byte sector at a time (fetched into L2 when the tile began).
-template <typename TO>
-__device__ __forceinline__ void fp_add_rows(const ProductParams& p, int row, int col0, uint64_t (&acc)[FP_COLS / 2]) {
-    constexpr int V = 16 / sizeof(TO);
-    if (row >= p.M) return;
-    const TO* const add = static_cast<const TO*>(p.addend) + row * p.ld_addend + col0;
-    if (p.vec && col0 + FP_COLS <= p.N) {
-#pragma unroll
-        for (int c = 0; c < FP_COLS; c += V) {
-            const Pack<TO, V> a = *reinterpret_cast<const Pack<TO, V>*>(add + c);
-#pragma unroll
-            for (int e = 0; e < V; e += 2) acc[(c + e) / 2] = add2(acc[(c + e) / 2], pair(to_float(a.v[e]), to_float(a.v[e + 1])));
-        }
-    } else {
-#pragma unroll
-        for (int c = 0; c < FP_COLS; ++c) {
-            if (col0 + c < p.N) acc[c / 2] = add2(acc[c / 2], c & 1 ? pair(0.f, to_float(add[c])) : pair(to_float(add[c]), 0.f));
-        }
-    }
-}
-template <typename TO>
-__device__ __forceinline__ void fp_prefetch_addend(const ProductParams& p, int row, int col0) {
-    if (row >= p.M) return;
-    const char* add = reinterpret_cast<const char*>(static_cast<const TO*>(p.addend) + row * p.ld_addend + col0);
-#pragma unroll
-    for (int b = 0; b < FP_COLS * (int)sizeof(TO); b += 128)
-        if (col0 + b / (int)sizeof(TO) < p.N) asm volatile("prefetch.global.L2 [%0];" ::"l"(add + b));
-}
-
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ float4 cluster_ld(uint32_t addr, uint32_t rank) {
-    uint32_t at;
-    float4 v;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-    return v;
 }
 
 // A cluster's CTAs hold partial sums of one tile in their shared memory; each adds up a share of it in the order of their ranks.
@@ -646,7 +438,7 @@ __device__ __forceinline__ void fp_join(const ProductParams& p, uint32_t part, i
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) o.v[e] = from_float<TO>(f[e]);
-        fp_put<TO, 4>(p, row, col, o);
+        out_put<TO, 4>(p, row, col, o);
     }
 }
 
@@ -692,9 +484,9 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    fp_fence_before();
+    tmem_fence_before();
     __syncthreads();
-    fp_fence_after();
+    tmem_fence_after();
     const uint32_t tmem = *tmem_slot;
     grid_dependency_wait();          // (nothing of global memory was touched so far)
     allow_dependents();
@@ -721,15 +513,15 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                     if (lane == 0) {
                         unsigned char* sa = fp_smem + s * STAGE;
                         mbar_arrive_expect_tx(&full[s], STAGE);
-                        fp_tma_load(sa, &tmA, kb * FP_BK, m0, &full[s]);
+                        tma_load_2d(sa, &tmA, kb * FP_BK, m0, &full[s]);
     #pragma unroll
-                        for (int g = 0; g < (BN + 127) / 128; ++g) fp_tma_load(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
+                        for (int g = 0; g < (BN + 127) / 128; ++g) tma_load_2d(sa + FP_BOX_BYTES * (1 + g), &tmB, kb * FP_BK, n0 + 128 * g, &full[s]);
                     }
                     const uint32_t at = smem_u32(scales + slot * (128 + BN) + lane);
     #pragma unroll
-                    for (int i = 0; i < 4; ++i) if (32 * i < na) fp_copy4(at + 128 * i, sa0 + kb * p.sa_ld + 32 * i);
+                    for (int i = 0; i < 4; ++i) if (32 * i < na) copy4_async(at + 128 * i, sa0 + kb * p.sa_ld + 32 * i);
     #pragma unroll
-                    for (int i = 0; i < BN / 32; ++i) if (32 * i < nb) fp_copy4(at + 512 + 128 * i, sb0 + kb * p.sb_ld + 32 * i);
+                    for (int i = 0; i < BN / 32; ++i) if (32 * i < nb) copy4_async(at + 512 + 128 * i, sb0 + kb * p.sb_ld + 32 * i);
                     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&full[s])) : "memory");
                     ++count;
                     if (++s == STAGES) { s = 0; phase ^= 1; }
@@ -745,14 +537,14 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 for (int item = first; item < p.items && ok && !*stop; item += step) {
                     for (int kb = kb0; kb < kb1; ++kb) {
                         if (!mbar_wait_idle(&acc_empty[buf], acc_phase, p.wait_limit) || !mbar_wait_idle(&full[s], phase, p.wait_limit)) { ok = false; break; }
-                        fp_fence_after();
+                        tmem_fence_after();
                         const uint32_t sa = smem_u32(fp_smem + s * STAGE);
     #pragma unroll
                         for (int k = 0; k < FP_BK / 32; ++k)
-                            fp_mma(tmem + buf * BN, fp_desc(sa + k * 32), fp_desc(sa + FP_BOX_BYTES + k * 32), p.idesc, k != 0);
-                        fp_commit(&empty[s]);
+                            fp_mma(tmem + buf * BN, operand_desc(sa + k * 32), operand_desc(sa + FP_BOX_BYTES + k * 32), p.idesc, k != 0);
+                        mma_commit(&empty[s]);
                         mbar_arrive(&acc_full[buf]);       // (hands on what the wait for the stage made visible: the scales)
-                        fp_commit(&acc_full[buf]);
+                        mma_commit(&acc_full[buf]);
                         if (++s == STAGES) { s = 0; phase ^= 1; }
                         if (++buf == FP_NACC) { buf = 0; acc_phase ^= 1; }
                     }
@@ -801,31 +593,31 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
         registers_up<REGS_EPI>();
         const int quarter = warp & 3, group = (warp - 4) >> 2;      // tensor-memory lanes and columns of this warp
         float4* const st = stores + (warp - 4) * (32 * STORE_ROW / 16);
-        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group * FP_COLS);
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group * OUT_COLS);
         uint32_t buf = 0, phase = 0, slot = 0;
         bool ok = true;
         for (int item = first; item < p.items && ok; item += step) {
-            const int m0 = item / p.tiles_n * FP_BM + quarter * 32, n0 = item % p.tiles_n * BN + group * FP_COLS;
-            uint64_t acc[FP_COLS / 2];
+            const int m0 = item / p.tiles_n * FP_BM + quarter * 32, n0 = item % p.tiles_n * BN + group * OUT_COLS;
+            uint64_t acc[OUT_COLS / 2];
 #pragma unroll
-            for (int i = 0; i < FP_COLS / 2; ++i) acc[i] = 0ull;
-            if (!SPLIT && p.addend) fp_with_out(p.out_type, [&](auto t) {
+            for (int i = 0; i < OUT_COLS / 2; ++i) acc[i] = 0ull;
+            if (!SPLIT && p.addend) with_out_type(p.out_type, [&](auto t) {
                 using TO = decltype(t);
-                if constexpr (STORE_ROW == 128) fp_fetch_addend<TO>(p, m0, n0, 0, st, lane);
-                if (STORE_ROW != 128 || sizeof(TO) == 4) fp_prefetch_addend<TO>(p, m0 + lane, n0);
+                if constexpr (STORE_ROW == 128) out_fetch_addend<TO>(p, m0, n0, 0, st, lane);
+                if (STORE_ROW != 128 || sizeof(TO) == 4) out_prefetch_addend<TO>(p, m0 + lane, n0);
             });
 #pragma unroll 1
             for (int kb = kb0; kb < kb1; ++kb) {
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit));
-                fp_fence_after();
+                tmem_fence_after();
                 if (!ok) { if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
                 const uint32_t from = taddr + buf * BN;
                 uint32_t v[2][16];
-                fp_tmem_ld16(from, v[0]);
+                tmem_ld16(from, v[0]);
                 const float* const sa = scales + slot * (128 + BN) + (p.a_square ? 0 : quarter * 32 + lane);
-                const float* const sb = scales + slot * (128 + BN) + 128 + (p.b_square ? group * FP_COLS / 128 : group * FP_COLS);
+                const float* const sb = scales + slot * (128 + BN) + 128 + (p.b_square ? group * OUT_COLS / 128 : group * OUT_COLS);
                 auto hand_back = [&] {                 // the accumulator is read: the next block's MMAs may begin
-                    fp_fence_before();
+                    tmem_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&acc_empty[buf]);
                 };
@@ -833,12 +625,12 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                     const float s = p.b_square ? *sa * *sb : *sa;
                     const uint64_t s2 = pair(s, s);
 #pragma unroll
-                    for (int c = 0; c < FP_COLS / 16; ++c) {
-                        fp_tmem_wait(v[c & 1]);
+                    for (int c = 0; c < OUT_COLS / 16; ++c) {
+                        tmem_wait16(v[c & 1]);
                         uint64_t w[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) w[i] = two_words(v[c & 1][2 * i], v[c & 1][2 * i + 1]);
-                        if (c + 1 < FP_COLS / 16) fp_tmem_ld16(from + (uint32_t)(c + 1) * 16, v[(c + 1) & 1]);
+                        if (c + 1 < OUT_COLS / 16) tmem_ld16(from + (uint32_t)(c + 1) * 16, v[(c + 1) & 1]);
                         else hand_back();
                         if (p.b_square) {
 #pragma unroll
@@ -855,10 +647,10 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 } else {
                     const int each = p.b_square ? 0 : 1;
 #pragma unroll
-                    for (int c = 0; c < FP_COLS / 16; ++c) {
-                        if (c > 0) fp_tmem_ld16(from + (uint32_t)c * 16, v[0]);
-                        fp_tmem_wait(v[0]);
-                        if (c + 1 == FP_COLS / 16) hand_back();
+                    for (int c = 0; c < OUT_COLS / 16; ++c) {
+                        if (c > 0) tmem_ld16(from + (uint32_t)c * 16, v[0]);
+                        tmem_wait16(v[0]);
+                        if (c + 1 == OUT_COLS / 16) hand_back();
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             acc[c * 8 + i] = fp_add_far(two_words(v[0][2 * i], v[0][2 * i + 1]), *sa, sb[each * (c * 16 + 2 * i)], sb[each * (c * 16 + 2 * i + 1)], acc[c * 8 + i]);
@@ -872,18 +664,18 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 float4* part = reinterpret_cast<float4*>(fp_smem);
                 const int r = quarter * 32 + lane;
 #pragma unroll
-                for (int i = 0; i < FP_COLS / 4; ++i) {
+                for (int i = 0; i < OUT_COLS / 4; ++i) {
                     const float2 a = unpair(acc[2 * i]), b = unpair(acc[2 * i + 1]);
-                    part[r * (BN / 4) + ((group * (FP_COLS / 4) + i) ^ (r & 7))] = make_float4(a.x, a.y, b.x, b.y);
+                    part[r * (BN / 4) + ((group * (OUT_COLS / 4) + i) ^ (r & 7))] = make_float4(a.x, a.y, b.x, b.y);
                 }
             } else {
-                fp_with_out(p.out_type, [&](auto t) {
+                with_out_type(p.out_type, [&](auto t) {
                     using TO = decltype(t);
                     if (p.addend) {
-                        if constexpr (STORE_ROW == 128) fp_add_staged<TO>(p, m0, n0, acc, st, lane);
-                        else fp_add_rows<TO>(p, m0 + lane, n0, acc);
+                        if constexpr (STORE_ROW == 128) out_add_staged<TO>(p, m0, n0, acc, st, lane);
+                        else out_add_rows<TO>(p, m0 + lane, n0, acc);
                     }
-                    fp_store<TO, STORE_ROW>(p, m0, n0, acc, st, lane);
+                    out_store<TO, STORE_ROW>(p, m0, n0, acc, st, lane);
                 });
             }
         }
@@ -891,11 +683,11 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
         if (SPLIT) {       // (every warp of the cluster comes here, also after a wait that ran out)
             cluster_sync();
             const int m0 = first / p.tiles_n * FP_BM, n0 = first % p.tiles_n * BN;
-            fp_with_out(p.out_type, [&](auto t) { fp_join<decltype(t)>(p, smem_u32(fp_smem), m0, n0, threadIdx.x - 128); });
+            with_out_type(p.out_type, [&](auto t) { fp_join<decltype(t)>(p, smem_u32(fp_smem), m0, n0, threadIdx.x - 128); });
             cluster_sync();        // no CTA leaves while another reads its partial sums
         }
     }
-    fp_fence_before();
+    tmem_fence_before();
     __syncthreads();
     if (*stop) {       // copies and MMAs in flight are waited for before the CTA's memory is given back (warp 2 may owe a stage its arrival)
         if (lane == 0) {
@@ -904,44 +696,11 @@ __global__ void __launch_bounds__(fp_threads(FORM), fp_ctas_per_sm(FORM)) fp8_pr
                 for (int r = (int)*looked; r < n; ++r) mbar_arrive(&full[r % STAGES]);
                 for (int r = max(0, n - STAGES); r < n; ++r) mbar_wait_idle(&full[r % STAGES], (r / STAGES) & 1, kDefaultWaitLimit);
             }
-            if (warp == 1) { fp_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
+            if (warp == 1) { mma_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
         }
         __syncthreads();
     }
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
-}
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-int operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t k, int64_t ld, int box_rows) {
-    static const EncodeTiledFn fn = [] {
-        void* ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &q);
-        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiledFn>(ptr) : nullptr;
-    }();
-    if (!fn) return KGE_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
-    const cuuint32_t box[2] = {FP_BK, (cuuint32_t)box_rows}, one[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? KGE_OK : KGE_ERR_CUDA;
-}
-
-// Streaming multiprocessors of the current device.
-int sm_count(int* sms) {
-    static std::atomic<int> known[kMaxDevices];
-    int dev = -1;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return KGE_ERR_CUDA;
-    const bool tracked = dev >= 0 && dev < kMaxDevices;
-    *sms = tracked ? known[dev].load(std::memory_order_relaxed) : 0;
-    if (*sms == 0) {
-        e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
-        if (e != cudaSuccess) return KGE_ERR_CUDA;
-        if (tracked) known[dev].store(*sms, std::memory_order_relaxed);
-    }
-    return KGE_OK;
 }
 
 template <int FORM> int configure_product() {
@@ -950,8 +709,6 @@ template <int FORM> int configure_product() {
         return cudaFuncSetAttribute(fp8_product_kernel<FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)fp_smem_bytes(FORM));
     }) == cudaSuccess ? KGE_OK : KGE_ERR_CUDA;
 }
-
-std::atomic<int> product_wait_limit{kDefaultWaitLimit};       // tries of a bounded wait, unless a test shortens it
 
 // How many clusters of `split` CTAs the device runs at a time: asked for once (what is left of a part of the chip takes none).
 int split_clusters(int split, int* clusters) {
