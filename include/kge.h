@@ -441,6 +441,85 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
                    const float* b_scales, int32_t b_block, const void* addend, int64_t ld_addend, void* out, int32_t out_type, int64_t ld_out,
                    int64_t M, int64_t N, int64_t K, int32_t* status, void* stream);
 
+/*
+ * 8-bit integers with a scale for each row (a token's, or an output channel's), and the product of two such operands.  An operand is a
+ * row-major int8 matrix [R, K] whose rows lie ld (a multiple of 16, base 16-byte aligned) bytes apart, and fp32 scales [R]; it stands for
+ * q times its row's scale.  What lies between K and ld is neither read nor written.
+ *
+ * kge_int8_quantize  x [rows, cols] (fp32, bf16, fp16) -> q, scales: scale = largest magnitude of the row / 127 (at least 2^-126; 1 for
+ *                    a row of zeros), q the integer nearest to x / scale, ties to even.  A row that holds an infinity or a NaN stands
+ *                    for NaN throughout.
+ * kge_int8_matmul    out [M, N] = A [M, K] . B [N, K]^T (+ addend [M, N], of out's type; it may be out itself): the products summed exactly
+ *                    in 32-bit integers (K at most 131,071, else KGE_ERR_UNSUPPORTED), the sum times its two scales and the addend in fp32.  out fp32,
+ *                    bf16 or fp16.  The same bits on every GPU and however the work is shared out.
+ *                    status receives KGE_ERR_TIMEOUT if a wait in the kernel ran out; out is not what it should be then.
+ */
+int kge_int8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, void* q, int64_t ldq, float* scales, void* stream);
+int kge_int8_matmul(const void* a, int64_t lda, const float* a_scales, const void* b, int64_t ldb, const float* b_scales, const void* addend, int64_t ld_addend,
+                    void* out, int32_t out_type, int64_t ld_out, int64_t M, int64_t N, int64_t K, int32_t* status, void* stream);
+
+/*
+ * The norms after and before a block, fused with its gate and residual scale, row by row (d columns):
+ *   a = N1(y), or y where post_weight is NULL;   h = x + scale act(gate) a, or x where y is NULL;   z = N2(h)
+ *   N(u) = (u - mu) r weight + bias,  r = 1 / sqrt(mean((u - mu)^2) + eps),  mu = mean(u) where layer = 1, else 0
+ * x and h are of x_type, y, gate and z of block_type (fp32, bf16, fp16 each), the vectors [d] fp32 (bias, scale, gate: NULL where there is none).
+ * act: gate_act 0 the gate itself, 1 its sigmoid, 2 gate times its sigmoid.  z is made of the unrounded h.
+ * kge_block_norm       h or z may be NULL, not both; without y only z is given.  z_int8 = 1: z is int8 [n, d] with a scale for each row in z_scales
+ *                      [n], as kge_int8_quantize would make them of the unrounded z.  stats (or NULL): [n, 4], 16-byte aligned, receives mu and r
+ *                      of the norm after the block, then of the one before the next (0 where a norm is not taken), for the gradients.
+ * kge_block_norm_grad  from dz (block_type, or NULL: no gradient came through z) and dh (x_type, or NULL) the gradients that are not NULL in
+ *                      `out`; those of the vectors are sums over the rows in an order that follows from n, d and alignment alone, written, or added to what is there
+ *                      (accumulate = 1).  x, y, gate and the vectors are the forward pass's, stats what it left.  scratch: kge_block_norm_grad_scratch_bytes(n, d)
+ *                      bytes, 256-byte aligned, where a vector's gradient is asked for; calls that may overlap need one each.
+ * h, z, dx, dy, dgate may be one of the call's inputs of the same type whose rows lie at the same distance; they overlap nothing otherwise.
+ * Rows of more than 8,192 (gradients: 4,096) columns are read from cache several times.
+ */
+typedef struct {
+    const void *x, *y, *gate;
+    const float *post_weight, *post_bias, *scale, *pre_weight, *pre_bias;
+    int64_t ldx, ldy, ld_gate;
+    int32_t x_type, block_type, gate_act, layer;
+} kge_norm_block;
+typedef struct {
+    void *dx, *dy, *dgate;
+    float *dpost_weight, *dpost_bias, *dscale, *dpre_weight, *dpre_bias;
+    int64_t ld_dx, ld_dy, ld_dgate;
+} kge_norm_grads;
+int kge_block_norm(const kge_norm_block* block /*[host]*/, int64_t n, int32_t d, void* h, int64_t ldh, void* z, int32_t z_int8, int64_t ldz,
+                   float* z_scales, float eps, float* stats, void* stream);
+size_t kge_block_norm_grad_scratch_bytes(int64_t n, int32_t d);
+int kge_block_norm_grad(const kge_norm_block* block /*[host]*/, int64_t n, int32_t d, const float* stats, const void* dz, int64_t ld_dz, const void* dh,
+                        int64_t ld_dh, const kge_norm_grads* out /*[host]*/, int32_t accumulate, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * One AdamW step over a list of tensors: with t = step + 1 and g the gradient times grad_scale, element by element
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2 (each product and sum rounded to fp32 on its own),
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps), rounded once to its type;
+ * copy (or NULL) receives the new parameters in bf16 or fp16 as well.  A tensor is n <= 2^40 contiguous elements; param and grad fp32, bf16
+ * or fp16, each its own; one whose grad is NULL, or whose n is 0, is passed over.  Tensors of a call must not overlap each other.
+ * state_bits = 32   m, v fp32 [n]; the scales are not looked at.
+ * state_bits = 8    m e4m3 [n], v e5m2 [n], fp32 scales [ceil(n / 128)] of both, powers of two, one to each 128 elements of the tensor: the
+ *                   state is the value times its scale (zeros in all four arrays, or scale 1, begin a run).  A new value's |x| / scale
+ *                   lies between two 8-bit values; it becomes the upper one with a probability of its distance to the lower one, in
+ *                   65,536ths, decided by the halves of word i mod 4 of Philox4x32-10 with key = seed and counter = (i / 4 lo, 64 * place of the tensor
+ *                   in the list + i / 4 hi, step lo, 2^30 + step hi): the low half for m, the high one for v.  A positive v
+ *                   never becomes 0.  scale = 2^(e - 7) for m, 2^(e - 14) for v, 2^e <= largest magnitude < 2^(e + 1), at least 2^-126; 1 for
+ *                   zeros alone.  A block of 128 in which a new m (or v) is infinite or NaN stands for NaN from then on.
+ * step_dev, lr_dev, grad_scale_dev: device numbers added to step, multiplied by lr, multiplied by grad_scale when the call runs (or
+ * NULL), so that a captured call can be replayed.  eps > 0 in fp32; 0 <= beta1, beta2 < 1; step (with *step_dev) < 2^62.
+ * A launch carries up to 340 tensors.
+ */
+typedef struct {
+    void* param; const void* grad; void* m; void* v;
+    float *m_scales, *v_scales;
+    void* copy;
+    int64_t n;
+    int32_t param_type, grad_type, copy_type;
+    float weight_decay;
+} kge_adamw_tensor;
+int kge_adamw(const kge_adamw_tensor* tensors /*[host]*/, int32_t count, int32_t state_bits, double lr, double beta1, double beta2, double eps,
+              double grad_scale, uint64_t step, const int64_t* step_dev, const float* lr_dev, const float* grad_scale_dev, uint64_t seed, void* stream);
+
 /* Synchronise `stream`, return the sticky device status word (0 or a negative code), clear it. */
 int kge_get_status(kge_handle* h, void* stream);
 
@@ -526,7 +605,7 @@ int kge_debug_init_words(kge_handle* h, float* out, int64_t rows, int32_t width,
 
 int kge_debug_set_wait_limit(kge_handle* h, int32_t tries);
 int kge_debug_wait_probe(kge_handle* h, void* stream);
-/* The same limit for the calls of kge_fp8_matmul, which have no handle, in this process. */
+/* The same limit for the calls of kge_fp8_matmul and kge_int8_matmul, which have no handle, in this process. */
 int kge_debug_set_product_wait_limit(int32_t tries);
 
 #ifdef __cplusplus

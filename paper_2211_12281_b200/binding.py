@@ -65,6 +65,26 @@ class KgeConfig(C.Structure):
                    lr, beta1, beta2, eps, seed, reg_lambda, reg_form, feat_dim, feat_shared)
 
 
+class KgeNormBlock(C.Structure):
+    """Mirror of ``kge_norm_block``."""
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("gate", C.c_void_p), ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("scale", C.c_void_p),
+                ("pre_weight", C.c_void_p), ("pre_bias", C.c_void_p), ("ldx", C.c_int64), ("ldy", C.c_int64), ("ld_gate", C.c_int64),
+                ("x_type", C.c_int32), ("block_type", C.c_int32), ("gate_act", C.c_int32), ("layer", C.c_int32)]
+
+
+class KgeNormGrads(C.Structure):
+    """Mirror of ``kge_norm_grads``."""
+    _fields_ = [("dx", C.c_void_p), ("dy", C.c_void_p), ("dgate", C.c_void_p), ("dpost_weight", C.c_void_p), ("dpost_bias", C.c_void_p), ("dscale", C.c_void_p),
+                ("dpre_weight", C.c_void_p), ("dpre_bias", C.c_void_p), ("ld_dx", C.c_int64), ("ld_dy", C.c_int64), ("ld_dgate", C.c_int64)]
+
+
+class KgeAdamwTensor(C.Structure):
+    """Mirror of ``kge_adamw_tensor``."""
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("copy", C.c_void_p), ("n", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("copy_type", C.c_int32),
+                ("weight_decay", C.c_float)]
+
+
 def library_path() -> Path:
     return _PKG / "libkge.so"
 
@@ -121,6 +141,13 @@ SIGNATURES = {
                                    C.c_int64, _vp, _vp]),
     "kge_fp8_matmul": (C.c_int, [_vp, C.c_int32, C.c_int64, _vp, C.c_int32, _vp, C.c_int32, C.c_int64, _vp, C.c_int32, _vp, C.c_int64, _vp,
                                  C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, _vp, _vp]),
+    "kge_int8_quantize": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, _vp]),
+    "kge_int8_matmul": (C.c_int, [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, _vp, _vp]),
+    "kge_block_norm": (C.c_int, [C.POINTER(KgeNormBlock), C.c_int64, C.c_int32, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, _vp, C.c_float, _vp, _vp]),
+    "kge_block_norm_grad_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int32]),
+    "kge_block_norm_grad": (C.c_int, [C.POINTER(KgeNormBlock), C.c_int64, C.c_int32, _vp, _vp, C.c_int64, _vp, C.c_int64, C.POINTER(KgeNormGrads), C.c_int32,
+                                      _vp, C.c_size_t, _vp]),
+    "kge_adamw": (C.c_int, [_vp, C.c_int32, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, C.c_uint64, _vp, _vp, _vp, C.c_uint64, _vp]),
     "kge_get_status": (C.c_int, [_vp, _vp]),
     "kge_launch_count": (C.c_int64, [_vp]),
     "kge_profile": (C.c_int, [_vp, C.c_int]),
@@ -405,6 +432,246 @@ def fp8_matmul(a, a_scales, b, b_scales, out, addend=None, status=None):
     dev = _device_of(w, a, a_scales, b, b_scales, out, addend, status)
     _call(w, lib().kge_fp8_matmul, dev, a.data_ptr(), ta, la, a_scales.data_ptr(), ba, b.data_ptr(), tb, lb, b_scales.data_ptr(), bb, _addr(addend), ladd,
           out.data_ptr(), to, lo, m, n, k, _status_word(status, w))
+
+
+def _int8_operand(q, scales, where, name):
+    """(rows, columns, distance of rows) of an int8 operand [R, K] with scales [R]."""
+    if _torch is None:
+        _load_torch()
+    if q.dtype is not _torch.int8:
+        raise _bad(where, f"{name} has type {q.dtype}")
+    rows, k, ld = _matrix(q, where, name)
+    if rows <= 1:
+        ld = (ld + 15) // 16 * 16
+    if scales is None or scales.dtype is not _torch.float32 or not scales.is_contiguous() or scales.dim() != 1 or scales.shape[0] != rows:
+        raise _bad(where, f"the scales of {name} are not a contiguous float32 list of its {rows} rows")
+    return rows, k, ld
+
+
+def int8_quantize(x, q, scales):
+    """kge_int8_quantize: x [R, K] (float32, bfloat16, float16) -> q int8 [R, K] (rows a multiple of 16 bytes apart) with scales float32 [R]."""
+    w = "kge_int8_quantize"
+    tx, (rows, cols, lx) = _type_of(x, w, "x", _FLOAT), _matrix(x, w, "x")
+    qr, qc, lq = _int8_operand(q, scales, w, "q")
+    if qr != rows or qc != cols:
+        raise _bad(w, "q has another shape than x")
+    dev = _device_of(w, x, q, scales)
+    _call(w, lib().kge_int8_quantize, dev, x.data_ptr(), tx, rows, cols, lx, q.data_ptr(), lq, scales.data_ptr())
+
+
+def int8_matmul(a, a_scales, b, b_scales, out, addend=None, status=None):
+    """kge_int8_matmul: out [M, N] = a [M, K] . b [N, K]^T (+ addend) of operands as int8_quantize makes them."""
+    w = "kge_int8_matmul"
+    m, k, la = _int8_operand(a, a_scales, w, "a")
+    n, kb, lb = _int8_operand(b, b_scales, w, "b")
+    to, (om, on, lo), ladd = _type_of(out, w, "out", _FLOAT), _matrix(out, w, "out"), 0
+    if kb != k or om != m or on != n:
+        raise _bad(w, "shapes of a [M, K], b [N, K] and out [M, N] do not fit")
+    if addend is not None:
+        am, an, ladd = _matrix(addend, w, "addend")
+        if am != m or an != n or addend.dtype is not out.dtype:
+            raise _bad(w, "addend is not of out's shape and type")
+    dev = _device_of(w, a, a_scales, b, b_scales, out, addend, status)
+    _call(w, lib().kge_int8_matmul, dev, a.data_ptr(), la, a_scales.data_ptr(), b.data_ptr(), lb, b_scales.data_ptr(), _addr(addend), ladd,
+          out.data_ptr(), to, lo, m, n, k, _status_word(status, w))
+
+
+_GATE_ACTS = {"plain": 0, "sigmoid": 1, "silu": 2}
+_NORM_KINDS = {"rms": 0, "layer": 1}
+
+
+def _norm_block(w, x, block, y, gate, gate_act, vectors, kind):
+    """(kge_norm_block, rows, columns) of the operands: block is a tensor that says what type y, gate and z are of; vectors by their field's name."""
+    b = KgeNormBlock()
+    n, d, b.ldx = _matrix(x, w, "x")
+    b.x_type, b.block_type, b.x = _type_of(x, w, "x", _FLOAT), _type_of(block, w, "y, gate, z or dz", _FLOAT), x.data_ptr()
+    for name, t, field in (("y", y, "ldy"), ("gate", gate, "ld_gate")):
+        if t is None:
+            continue
+        rows, cols, ld = _matrix(t, w, name)
+        if rows != n or cols != d or t.dtype is not block.dtype:
+            raise _bad(w, f"{name} has another shape than x or another type than the block's other tensors")
+        setattr(b, name, t.data_ptr())
+        setattr(b, field, ld)
+    for name, v in vectors.items():
+        if v is not None:
+            _vector(v, d, w, name)
+            setattr(b, name, v.data_ptr())
+    if gate_act not in _GATE_ACTS or kind not in _NORM_KINDS:
+        raise _bad(w, f"gate_act is one of {list(_GATE_ACTS)}, kind one of {list(_NORM_KINDS)}")
+    b.gate_act, b.layer = _GATE_ACTS[gate_act], _NORM_KINDS[kind]
+    return b, n, _int32(d, w, "width")
+
+
+def _vector(v, d, w, name):
+    if v.dtype is not _torch.float32 or v.dim() != 1 or v.shape[0] != d or not v.is_contiguous():
+        raise _bad(w, f"{name} is not a contiguous float32 vector of {d}")
+
+
+def _stats_of(stats, n, w):
+    if stats is not None and (stats.dtype is not _torch.float32 or tuple(stats.shape) != (n, 4) or not stats.is_contiguous()):
+        raise _bad(w, f"stats is not a contiguous float32 matrix [{n}, 4]")
+    return _addr(stats)
+
+
+def block_norm(x, z=None, pre_weight=None, pre_bias=None, y=None, h=None, gate=None, gate_act="plain", post_weight=None, post_bias=None, scale=None, kind="rms",
+               eps=1e-6, stats=None, z_scales=None):
+    """kge_block_norm: h = x + scale act(gate) N(y), z = N(h), row by row.
+
+    x, h [n, d] of one type, y, gate, z of one type; N after the block where post_weight is given, before the next where z (and pre_weight) is; without
+    y it is z = N(x).  z may be int8 with scales float32 [n] in z_scales.  gate_act: "plain", "sigmoid", "silu"; kind: "rms", "layer".
+    stats float32 [n, 4] receives what block_norm_grad needs.  h may be x, z may be y or gate."""
+    w = "kge_block_norm"
+    if _torch is None:
+        _load_torch()
+    z8 = z is not None and z.dtype is _torch.int8
+    block = y if y is not None else (x if z8 or z is None else z)
+    b, n, d = _norm_block(w, x, block, y, gate, gate_act, dict(post_weight=post_weight, post_bias=post_bias, scale=scale, pre_weight=pre_weight, pre_bias=pre_bias), kind)
+    ldh = ldz = 0
+    if h is not None:
+        hr, hd, ldh = _matrix(h, w, "h")
+        if hr != n or hd != d or h.dtype is not x.dtype:
+            raise _bad(w, "h is not of x's shape and type")
+    if z8:
+        zr, zd, ldz = _int8_operand(z, z_scales, w, "z")
+    elif z is not None:
+        zr, zd, ldz = _matrix(z, w, "z")
+        if z.dtype is not block.dtype or z_scales is not None:
+            raise _bad(w, "z is not of y's type, or scales are given for a z that is not int8")
+    if z is not None and (zr != n or zd != d):
+        raise _bad(w, "z is not of x's shape")
+    at = _stats_of(stats, n, w)
+    dev = _device_of(w, x, y, gate, h, z, post_weight, post_bias, scale, pre_weight, pre_bias, stats, z_scales)
+    _call(w, lib().kge_block_norm, dev, b, n, d, _addr(h), ldh, _addr(z), 1 if z8 else 0, ldz, _addr(z_scales), eps, at)
+
+
+def block_norm_grad_scratch_bytes(n, d) -> int:
+    """Bytes of scratch a block_norm_grad of n rows of d columns needs (a tensor of 256 more is always enough)."""
+    w = "kge_block_norm_grad_scratch_bytes"
+    return int(lib().kge_block_norm_grad_scratch_bytes(_int32(n, w, "rows"), _int32(d, w, "width")))
+
+
+def block_norm_grad(x, stats, dx=None, dz=None, dh=None, pre_weight=None, dpre_weight=None, dpre_bias=None, y=None, dy=None, gate=None, dgate=None, gate_act="plain",
+                    post_weight=None, post_bias=None, dpost_weight=None, dpost_bias=None, scale=None, dscale=None, kind="rms", accumulate=False, scratch=None):
+    """kge_block_norm_grad: the gradients of block_norm's operands from dz (of z's type, or None) and dh (of h's, or None), those that are given; dx, dy, dgate of their operands' types,
+    the vectors' float32, written or (accumulate) added to what is there.  x, y, gate and the vectors are the forward call's, stats what it left."""
+    w = "kge_block_norm_grad"
+    block = y if y is not None else (dz if dz is not None else x)
+    b, n, d = _norm_block(w, x, block, y, gate, gate_act, dict(post_weight=post_weight, post_bias=post_bias, scale=scale, pre_weight=pre_weight), kind)
+    ld = {}
+    for name, t, like in (("dz", dz, block), ("dh", dh, x), ("dx", dx, x), ("dy", dy, block), ("dgate", dgate, block)):
+        if t is None:
+            ld[name] = 0
+            continue
+        rows, cols, ld[name] = _matrix(t, w, name)
+        if rows != n or cols != d or t.dtype is not like.dtype:
+            raise _bad(w, f"{name} has another shape than x or another type than its operand")
+    o, wanted = KgeNormGrads(), False
+    o.dx, o.dy, o.dgate, o.ld_dx, o.ld_dy, o.ld_dgate = _addr(dx), _addr(dy), _addr(dgate), ld["dx"], ld["dy"], ld["dgate"]
+    for name, v in (("dpost_weight", dpost_weight), ("dpost_bias", dpost_bias), ("dscale", dscale), ("dpre_weight", dpre_weight), ("dpre_bias", dpre_bias)):
+        if v is not None:
+            _vector(v, d, w, name)
+            setattr(o, name, v.data_ptr())
+            wanted = True
+    if stats is None:
+        raise _bad(w, "stats is not given")
+    at = _stats_of(stats, n, w)
+    dev = _device_of(w, x, y, gate, dz, dh, dx, dy, dgate, post_weight, post_bias, scale, pre_weight, dpost_weight, dpost_bias, dscale, dpre_weight, dpre_bias, stats)
+    place, size, keep = _scratch(scratch, lib().kge_block_norm_grad_scratch_bytes(n, d) if wanted else 0, dev, w)
+    _call(w, lib().kge_block_norm_grad, dev, b, n, d, at, _addr(dz), ld["dz"], _addr(dh), ld["dh"], o, 1 if accumulate else 0, place, size)
+
+
+class AdamW:
+    """kge_adamw over a list of tensors: made once for a model's parameters, then step() after every backward pass.
+
+    params, grads: contiguous tensors (float32, bfloat16, float16) of one size each; a grad may be None (its parameter stays).
+    m, v: float32 of the same sizes, or float8_e4m3fn and float8_e5m2 with float32 scales [ceil(n / 128)] in m_scales, v_scales; all zeros begin a run.
+    copies: bfloat16 or float16 tensors (or None) that receive the new parameters too.  weight_decay: a number, or one for each tensor.
+    The object keeps the tensors and their addresses: gradients are read where they are when step() runs, new ones are named by set_grads()."""
+
+    def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, copies=None, weight_decay=0.0):
+        w = "kge_adamw"
+        params, count = list(params), len(params)
+        lists = {}
+        for name, given in (("m", m), ("v", v), ("m_scales", m_scales), ("v_scales", v_scales), ("copies", copies)):
+            lists[name] = [None] * count if given is None else list(given)
+            if len(lists[name]) != count:
+                raise _bad(w, f"{name} is not a list of {count}")
+        decay = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+        if len(decay) != count:
+            raise _bad(w, f"weight_decay is not a number or a list of {count}")
+        if _torch is None:
+            _load_torch()
+        self._at = (KgeAdamwTensor * max(count, 1))()
+        self._count, self._dev, self.bits = count, -1, 32
+        self._keep = (params, lists)
+        if count == 0:
+            return
+        self.bits = 32 if lists["m"][0] is not None and lists["m"][0].dtype is _torch.float32 else 8
+        self._dev = params[0].get_device()
+        spans = []
+        for i, p in enumerate(params):
+            t, n = self._at[i], p.numel()
+            mi, vi, si, ti, ci = (lists[k][i] for k in ("m", "v", "m_scales", "v_scales", "copies"))
+            t.param_type, t.n, t.weight_decay, t.param = _type_of(p, w, f"params[{i}]", _FLOAT), n, decay[i], p.data_ptr()
+            states = (_torch.float32, _torch.float32) if self.bits == 32 else (_torch.float8_e4m3fn, _torch.float8_e5m2)
+            for name, s, dtype in (("m", mi, states[0]), ("v", vi, states[1])):
+                if s is None or s.dtype is not dtype or s.numel() != n or not s.is_contiguous():
+                    raise _bad(w, f"{name}[{i}] is not a contiguous tensor of {n} elements and type {dtype}")
+            t.m, t.v = mi.data_ptr(), vi.data_ptr()
+            if self.bits == 8:
+                for name, s in (("m_scales", si), ("v_scales", ti)):
+                    if s is None or s.dtype is not _torch.float32 or s.numel() != (n + 127) // 128 or not s.is_contiguous():
+                        raise _bad(w, f"{name}[{i}] is not a contiguous float32 tensor of {(n + 127) // 128}")
+                t.m_scales, t.v_scales = si.data_ptr(), ti.data_ptr()
+            else:
+                si = ti = None
+            if ci is not None:
+                t.copy_type, t.copy = _type_of(ci, w, f"copies[{i}]", _FLOAT), ci.data_ptr()
+                if t.copy_type == 0 or ci.numel() != n or not ci.is_contiguous():
+                    raise _bad(w, f"copies[{i}] is not a contiguous bfloat16 or float16 tensor of {n} elements")
+            if not p.is_contiguous():
+                raise _bad(w, f"params[{i}] is not contiguous")
+            _device_of(w, p, mi, vi, si, ti, ci)
+            if p.get_device() != self._dev:
+                raise _bad(w, "tensors are not on one GPU")
+            spans += [(a.data_ptr(), a.data_ptr() + a.numel() * a.element_size()) for a in (p, mi, vi, si, ti, ci) if a is not None and a.numel() > 0]
+        spans.sort()
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise _bad(w, "two of the tensors overlap")
+        self._spans = spans
+        self.set_grads(grads)
+
+    def set_grads(self, grads):
+        """Other gradients from now on: as many tensors (or Nones) as there are parameters."""
+        w, grads = "kge_adamw", list(grads)
+        if len(grads) != self._count:
+            raise _bad(w, f"grads is not a list of {self._count}")
+        at = []
+        for i, g in enumerate(grads):
+            if g is None:
+                at.append((0, None))
+                continue
+            code = _type_of(g, w, f"grads[{i}]", _FLOAT)
+            if g.numel() != self._at[i].n or not g.is_contiguous() or g.get_device() != self._dev:
+                raise _bad(w, f"grads[{i}] is not a contiguous tensor of {self._at[i].n} elements on the parameters' GPU")
+            at.append((code, g.data_ptr()))
+        for t, (code, ptr) in zip(self._at, at):
+            t.grad_type, t.grad = code, ptr
+        self._grads = grads
+
+    def step(self, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, grad_scale=1.0, step_dev=None, lr_dev=None, grad_scale_dev=None):
+        """The step-th step (from 0).  step_dev (int64), lr_dev, grad_scale_dev (float32): numbers on the device, for a captured step."""
+        w = "kge_adamw"
+        if not (0 <= step < 1 << 62 and 0 <= seed < 1 << 64):
+            raise _bad(w, "step is a 62-bit number, seed a 64-bit one")
+        for name, t, dtype in (("step_dev", step_dev, "int64"), ("lr_dev", lr_dev, "float32"), ("grad_scale_dev", grad_scale_dev, "float32")):
+            if t is not None and (t.dtype is not getattr(_torch, dtype) or t.numel() < 1 or t.get_device() != self._dev):
+                raise _bad(w, f"{name} is not a tensor of {dtype} on the parameters' GPU")
+        if self._count == 0:
+            return
+        _call(w, lib().kge_adamw, self._dev, self._at, self._count, self.bits, lr, beta1, beta2, eps, grad_scale, step, _addr(step_dev), _addr(lr_dev),
+              _addr(grad_scale_dev), seed)
 
 
 class Kge:

@@ -1,0 +1,496 @@
+// 8-bit integers with a scale for each row: making such operands, and their product.
+//   quantise   s = amax / 127, q = the integer nearest to x / s
+//   product    C[m, n] = sA[m] sB[n] sum_k A[m, k] B[n, k]   (+ C0[m, n])
+// The sum is exact: 32-bit integers hold 131,071 products of 8-bit ones, so neither the order of k nor how many CTAs share it matters.
+#include <algorithm>
+
+#include "kge_int8.cuh"
+#include "kge_product.cuh"
+
+namespace kge {
+
+namespace {
+
+// ---- quantisation ----------------------------------------------------------------------------------------------------
+
+struct QuantParams {
+    const void* x; int64_t ldx;
+    int8_t* q; int64_t ldq;
+    float* scales;
+    int rows, cols;
+    int vec;                         // rows of x start at multiples of eight elements
+};
+
+template <typename T> struct alignas(16) Eight { T v[8]; };
+template <typename T> __device__ __forceinline__ Eight<T> load8(const QuantParams& p, int64_t r, int c) {
+    const T* x = static_cast<const T*>(p.x) + r * p.ldx + c;
+    if (p.vec && c + 8 <= p.cols) return *reinterpret_cast<const Eight<T>*>(x);
+    Eight<T> e;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e.v[j] = c + j < p.cols ? x[j] : from_float<T>(0.f);
+    return e;
+}
+// Magnitudes as integers, which order as they do (a NaN above all).
+template <typename T> __device__ __forceinline__ uint32_t most_of(const Eight<T>& e) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(to_float(e.v[j])) & 0x7FFFFFFFu);
+    return m;
+}
+template <typename T> __device__ __forceinline__ void store8(const QuantParams& p, int64_t r, int c, const Eight<T>& e, const RowScale& s) {
+    int q[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = round_quotient(to_float(e.v[j]), s);
+    int8_t* out = p.q + r * p.ldq + c;
+    if (c + 8 <= p.cols) {
+        uint2 w;
+        w.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | (uint32_t)q[3] << 24;
+        w.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | (uint32_t)q[7] << 24;
+        *reinterpret_cast<uint2*>(out) = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (c + j < p.cols) out[j] = (int8_t)q[j];
+    }
+}
+
+// A row to a CTA of THREADS threads, or to each of its warps (WARP); K packs of eight a thread are kept, what is beyond them read again.
+constexpr int QUANT_THREADS = 256, QUANT_PACKS = 4;
+template <typename T, bool WARP>
+__global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const __grid_constant__ QuantParams p) {
+    __shared__ uint32_t part[QUANT_THREADS / 32];
+    grid_dependency_wait();
+    allow_dependents();
+    const int lanes = WARP ? 32 : QUANT_THREADS, t = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    const int64_t r = WARP ? (int64_t)blockIdx.x * (QUANT_THREADS / 32) + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
+    if (r >= p.rows) return;
+    Eight<T> x[QUANT_PACKS];
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < QUANT_PACKS; ++k) x[k] = load8<T>(p, r, (k * lanes + t) * 8);
+#pragma unroll
+    for (int k = 0; k < QUANT_PACKS; ++k) m = max(m, most_of(x[k]));
+    const int kept = QUANT_PACKS * lanes * 8;
+    for (int64_t c = kept + t * 8; c < p.cols; c += lanes * 8) m = max(m, most_of(load8<T>(p, r, (int)c)));
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (!WARP) {
+        if ((t & 31) == 0) part[t >> 5] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < QUANT_THREADS / 32; ++w) m = max(m, part[w]);
+    }
+    const RowScale s = row_scale(__uint_as_float(m));
+    if (t == 0) p.scales[r] = s.s;
+#pragma unroll
+    for (int k = 0; k < QUANT_PACKS; ++k) if ((k * lanes + t) * 8 < p.cols) store8(p, r, (k * lanes + t) * 8, x[k], s);
+    for (int64_t c = kept + t * 8; c < p.cols; c += lanes * 8) store8(p, r, (int)c, load8<T>(p, r, (int)c), s);
+}
+
+// ---- product ---------------------------------------------------------------------------------------------------------
+
+constexpr int I8_BM = 128;
+constexpr uint32_t I8_BOX_BYTES = 128 * OPERAND_BK;
+constexpr int I8_NACC = 2;                                // accumulators in tensor memory: one is stored while the other is summed up
+enum { I8_WIDE = 0, I8_PAIR = 1, I8_NARROW = 2, I8_SPLIT = 3 };
+constexpr int I8_MAX_SPLIT = 8;           // CTAs that share a tile's K
+__host__ __device__ constexpr int i8_bn(int form) { return form == I8_WIDE ? 256 : (form == I8_NARROW ? 64 : 128); }
+__host__ __device__ constexpr int i8_box_rows(int form) { return form == I8_NARROW ? 64 : 128; }             // of B per copy
+__host__ __device__ constexpr int i8_stages(int form) { return form == I8_WIDE ? 3 : (form == I8_SPLIT ? 6 : 2); }
+__host__ __device__ constexpr int i8_epi_warps(int form) { return 4 * i8_bn(form) / OUT_COLS; }
+__host__ __device__ constexpr int i8_threads(int form) { return 32 * (4 + i8_epi_warps(form)); }     // (four more: copies, MMAs, two idle)
+__host__ __device__ constexpr int i8_ctas_per_sm(int form) { return form == I8_PAIR ? 2 : (form == I8_NARROW ? 3 : 1); }
+__host__ __device__ constexpr uint32_t i8_stage_bytes(int form) { return I8_BOX_BYTES + (uint32_t)i8_bn(form) * OPERAND_BK; }
+constexpr uint32_t I8_STORE_ROW = 128;                    // bytes of a row on their way to memory, per epilogue warp and turn
+__host__ __device__ constexpr size_t i8_smem_bytes(int form) {
+    return (size_t)i8_stages(form) * i8_stage_bytes(form) + i8_epi_warps(form) * (32 * I8_STORE_ROW + OUT_COLS * 4) + 256;
+}
+
+struct IntProductParams : ProductOut {
+    int kblocks, kper;                    // blocks of K in all, and per CTA of a cluster
+    int tiles_n, items;
+    const float *sa, *sb;
+    int32_t* status; int wait_limit;
+    uint32_t idesc;
+};
+
+// Instruction descriptor: D int32, A and B signed 8-bit integers, both K-major.
+constexpr uint32_t i8_idesc(int m, int n) { return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
+__device__ __forceinline__ void i8_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// A sum times its two scales, the smaller one first: |x| >= 1 keeps that product a normal number where the scale is one, and it leaves the
+// range upwards only where the result does.  (The sum's own rounding to fp32 is half a step of 24 bits.)
+__device__ __forceinline__ float scaled(int x, float a, float b) { return (float)x * fminf(a, b) * fmaxf(a, b); }
+// (fminf and fmaxf drop a NaN: a row that stands for NaN has an infinite or a NaN scale, and this looks after it.)
+__device__ __forceinline__ float scaled_any(int x, float a, float b) {
+    const float y = scaled(x, a, b);
+    return a != a || b != b ? a + b : y;
+}
+
+// A warp's 32 rows x 64 columns: 128 bytes of each row at a time from tensor memory through shared memory, so that a store instruction covers whole lines.
+template <typename TO, class F>
+__device__ __forceinline__ void i8_store(const IntProductParams& p, int row0, int col0, uint32_t from, float sa, const float* sb, float4* st, int lane, F&& read_all) {
+    constexpr int V = 16 / sizeof(TO), PASS = 128 / sizeof(TO);
+    const bool inside = p.vec && row0 + 32 <= p.M && col0 + OUT_COLS <= p.N;
+#pragma unroll
+    for (int c = 0; c < OUT_COLS; c += PASS) {
+        if (p.addend) {
+            if (c > 0) out_fetch_addend<TO>(p, row0, col0, c, st, lane);
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+        }
+#pragma unroll
+        for (int h = 0; h < PASS; h += 16) {
+            uint32_t v[16];
+            tmem_ld16(from + c + h, v);
+            tmem_wait16(v);
+            if (c + h + 16 == OUT_COLS) read_all();
+#pragma unroll
+            for (int i = 0; i < 16 / V; ++i) {
+                float4* const at = st + lane * 8 + ((h / V + i) ^ (lane & 7));
+                Pack<TO, V> o;
+                if (p.addend) o = *reinterpret_cast<const Pack<TO, V>*>(at);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float x = scaled_any((int)v[i * V + e], sa, sb[c + h + i * V + e]);
+                    o.v[e] = from_float<TO>(p.addend ? x + to_float(o.v[e]) : x);
+                }
+                *at = *reinterpret_cast<const float4*>(&o);
+            }
+        }
+        __syncwarp();
+        if (inside) {
+            const int r0 = lane / 8, unit = lane % 8;
+            TO* dst = static_cast<TO*>(p.out) + (row0 + r0) * p.ld_out + col0 + c + V * unit;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = j * 4 + r0;
+                *reinterpret_cast<float4*>(dst) = st[r * 8 + (unit ^ (r & 7))];
+                dst += 4 * p.ld_out;
+            }
+        } else if (sizeof(TO) == 2 && p.twos) {
+            out_each<TO, 128, 2>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) {
+                *reinterpret_cast<uint32_t*>(static_cast<TO*>(p.out) + row * p.ld_out + col) = *reinterpret_cast<const uint32_t*>(at);
+            });
+        } else {
+            out_each<TO, 128, 1>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { static_cast<TO*>(p.out)[row * p.ld_out + col] = *at; });
+        }
+        __syncwarp();
+    }
+}
+
+// A cluster's CTAs hold partial sums of one tile in their shared memory; each adds up a share of it.
+template <typename TO>
+__device__ __forceinline__ void i8_join(const IntProductParams& p, uint32_t part, int m0, int n0, int tid) {
+    const int rows = min(I8_BM, (int)p.M - m0);
+    const uint32_t size = cluster_size();
+    constexpr int THREADS = 32 * i8_epi_warps(I8_SPLIT), PER_ROW = i8_bn(I8_SPLIT) / 4;
+    for (int u = (int)cluster_rank() * THREADS + tid; u < rows * PER_ROW; u += (int)size * THREADS) {
+        const int r = u / PER_ROW, q = u % PER_ROW, row = m0 + r, col = n0 + 4 * q;
+        if (col >= p.N) continue;
+        int sum[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int z = 0; z < I8_MAX_SPLIT; ++z) {
+            if (z >= (int)size) break;
+            const float4 v = cluster_ld(part + (uint32_t)(r * PER_ROW + (q ^ (r & 7))) * 16, z);
+            sum[0] += __float_as_int(v.x); sum[1] += __float_as_int(v.y); sum[2] += __float_as_int(v.z); sum[3] += __float_as_int(v.w);
+        }
+        const TO* add = static_cast<const TO*>(p.addend) + (p.addend ? row * p.ld_addend + col : 0);
+        const float sa = p.sa[row];
+        Pack<TO, 4> o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = col + e < p.N ? scaled_any(sum[e], sa, p.sb[col + e]) : 0.f;
+            o.v[e] = from_float<TO>(p.addend && col + e < p.N ? x + to_float(add[e]) : x);
+        }
+        out_put<TO, 4>(p, row, col, o);
+    }
+}
+
+// A 128 x BN tile of C at a time (persistent CTAs), or one per cluster, whose CTAs share its K (SPLIT).  Warp 0 feeds a ring of
+// shared-memory stages by TMA, warp 1 issues the MMAs of a whole tile into one of two accumulators in tensor memory; the other warps, 64
+// columns each, scale and store the tile before it meanwhile.
+template <int FORM>
+__global__ void __launch_bounds__(i8_threads(FORM), i8_ctas_per_sm(FORM)) int8_product_kernel(const __grid_constant__ CUtensorMap tmA,
+                                                                                               const __grid_constant__ CUtensorMap tmB,
+                                                                                               const __grid_constant__ IntProductParams p) {
+    constexpr bool SPLIT = FORM == I8_SPLIT;
+    constexpr int BN = i8_bn(FORM), STAGES = i8_stages(FORM), EW = i8_epi_warps(FORM);
+    constexpr uint32_t STAGE = i8_stage_bytes(FORM), TMEM_COLS = I8_NACC * BN;
+    extern __shared__ __align__(1024) unsigned char i8_smem[];
+    float4* const stores = reinterpret_cast<float4*>(i8_smem + (size_t)STAGES * STAGE);
+    float* const column_scales = reinterpret_cast<float*>(i8_smem + (size_t)STAGES * STAGE + EW * 32 * I8_STORE_ROW);
+    uint64_t* full = reinterpret_cast<uint64_t*>(column_scales + EW * OUT_COLS);
+    uint64_t* empty = full + STAGES;
+    uint64_t* acc_full = empty + STAGES;
+    uint64_t* acc_empty = acc_full + I8_NACC;
+    uint64_t* done = acc_empty + I8_NACC;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    volatile uint32_t* stop = tmem_slot + 1;
+    volatile uint32_t* filled = tmem_slot + 2;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < I8_NACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], EW); }
+        mbar_init(done, 1);
+        *stop = 0;
+        *filled = 0;
+        mbar_init_fence();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_dependency_wait();          // (nothing of global memory was touched so far)
+    allow_dependents();
+
+    const int step = SPLIT ? p.items : (int)gridDim.x;
+    const int first = SPLIT ? (int)(blockIdx.x / cluster_size()) : (int)blockIdx.x;
+    const int kb0 = SPLIT ? (int)cluster_rank() * p.kper : 0, kb1 = SPLIT ? min(p.kblocks, kb0 + p.kper) : p.kblocks;
+
+    if (warp < 4) {
+        if (warp == 0 && lane == 0) {
+            uint32_t s = 0, phase = 1, count = 0;
+            bool ok = true;
+            for (int item = first; item < p.items && ok; item += step) {
+                const int m0 = item / p.tiles_n * I8_BM, n0 = item % p.tiles_n * BN;
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop;
+                    if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); break; }
+                    unsigned char* sa = i8_smem + s * STAGE;
+                    mbar_arrive_expect_tx(&full[s], STAGE);
+                    tma_load_2d(sa, &tmA, kb * OPERAND_BK, m0, &full[s]);
+#pragma unroll
+                    for (int g = 0; g < (BN + 127) / 128; ++g) tma_load_2d(sa + I8_BOX_BYTES * (1 + g), &tmB, kb * OPERAND_BK, n0 + 128 * g, &full[s]);
+                    ++count;
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
+                }
+            }
+            *filled = count;
+        } else if (warp == 1 && lane == 0) {
+            uint32_t s = 0, phase = 0, buf = 0, acc_phase = 1;
+            bool ok = true;
+            for (int item = first; item < p.items && ok && !*stop; item += step) {
+                ok = mbar_wait_idle(&acc_empty[buf], acc_phase, p.wait_limit);
+                for (int kb = kb0; kb < kb1 && ok; ++kb) {
+                    ok = mbar_wait_idle(&full[s], phase, p.wait_limit);
+                    if (!ok) break;
+                    tmem_fence_after();
+                    const uint32_t sa = smem_u32(i8_smem + s * STAGE);
+#pragma unroll
+                    for (int k = 0; k < OPERAND_BK / 32; ++k)
+                        i8_mma(tmem + buf * BN, operand_desc(sa + k * 32), operand_desc(sa + I8_BOX_BYTES + k * 32), p.idesc, kb != kb0 || k != 0);
+                    mma_commit(&empty[s]);
+                    if (++s == STAGES) { s = 0; phase ^= 1; }
+                }
+                mma_commit(&acc_full[buf]);
+                if (++buf == I8_NACC) { buf = 0; acc_phase ^= 1; }
+            }
+            if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
+        }
+        __syncwarp();
+        if (SPLIT) { cluster_sync(); cluster_sync(); }
+    } else {
+        const int quarter = warp & 3, group = (warp - 4) >> 2;      // tensor-memory lanes and columns of this warp
+        float4* const st = stores + (warp - 4) * (32 * I8_STORE_ROW / 16);
+        float* const sb = column_scales + (warp - 4) * OUT_COLS;
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group * OUT_COLS);
+        uint32_t buf = 0, phase = 0;
+        bool ok = true;
+        for (int item = first; item < p.items && ok; item += step) {
+            const int m0 = item / p.tiles_n * I8_BM + quarter * 32, n0 = item % p.tiles_n * BN + group * OUT_COLS;
+            float sa = 0.f;
+            if (!SPLIT) {
+                sa = m0 + lane < p.M ? __ldg(p.sa + m0 + lane) : 0.f;
+#pragma unroll
+                for (int i = 0; i < OUT_COLS; i += 32) sb[i + lane] = n0 + i + lane < p.N ? __ldg(p.sb + n0 + i + lane) : 0.f;
+                if (p.addend) with_out_type(p.out_type, [&](auto t) { out_fetch_addend<decltype(t)>(p, m0, n0, 0, st, lane); });
+                __syncwarp();
+            }
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit)) && !*stop;
+            tmem_fence_after();
+            if (!__all_sync(0xffffffffu, ok)) { ok = false; if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
+            const uint32_t from = taddr + buf * BN;
+            auto hand_back = [&] {                 // the accumulator is read: another tile's MMAs may begin
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&acc_empty[buf]);
+            };
+            if (SPLIT) {       // the ring's stages are free: every copy has been multiplied
+                float4* part = reinterpret_cast<float4*>(i8_smem);
+                const int r = quarter * 32 + lane;
+#pragma unroll
+                for (int c = 0; c < OUT_COLS; c += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(from + c, v);
+                    tmem_wait16(v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        part[r * (BN / 4) + ((group * (OUT_COLS / 4) + c / 4 + i) ^ (r & 7))] =
+                            make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+                }
+            } else {
+                with_out_type(p.out_type, [&](auto t) { i8_store<decltype(t)>(p, m0, n0, from, sa, sb, st, lane, hand_back); });
+            }
+            if (++buf == I8_NACC) { buf = 0; phase ^= 1; }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");       // (an addend's copies, after a wait that ran out)
+        if (SPLIT) {       // (every warp of the cluster comes here, also after a wait that ran out)
+            cluster_sync();
+            const int m0 = first / p.tiles_n * I8_BM, n0 = first % p.tiles_n * BN;
+            with_out_type(p.out_type, [&](auto t) { i8_join<decltype(t)>(p, smem_u32(i8_smem), m0, n0, threadIdx.x - 128); });
+            cluster_sync();        // no CTA leaves while another reads its partial sums
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    if (*stop) {       // copies and MMAs in flight are waited for before the CTA's memory is given back
+        if (lane == 0) {
+            if (warp == 0) {
+                const int n = (int)*filled;
+                for (int r = max(0, n - STAGES); r < n; ++r) mbar_wait_idle(&full[r % STAGES], (r / STAGES) & 1, kDefaultWaitLimit);
+            }
+            if (warp == 1) { mma_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
+        }
+        __syncthreads();
+    }
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+}
+
+template <int FORM> int configure_product() {
+    static DeviceOnce configured;
+    return once_per_device(configured, [] {
+        return cudaFuncSetAttribute(int8_product_kernel<FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)i8_smem_bytes(FORM));
+    }) == cudaSuccess ? KGE_OK : KGE_ERR_CUDA;
+}
+
+// How many clusters of `split` CTAs the device runs at a time: asked for once (what is left of a part of the chip takes none).
+int split_clusters(int split, int* clusters) {
+    static std::atomic<int> known[kMaxDevices][I8_MAX_SPLIT + 1];        // one more than their number
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return KGE_ERR_CUDA;
+    const bool tracked = dev >= 0 && dev < kMaxDevices;
+    int state = tracked ? known[dev][split].load(std::memory_order_acquire) : 0;
+    if (state == 0) {
+        const int rc = configure_product<I8_SPLIT>();
+        if (rc != KGE_OK) return rc;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)split); cfg.blockDim = dim3(i8_threads(I8_SPLIT)); cfg.dynamicSmemBytes = i8_smem_bytes(I8_SPLIT);
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        int fit = 0;
+        if (cudaOccupancyMaxActiveClusters(&fit, int8_product_kernel<I8_SPLIT>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); fit = 0; }
+        state = 1 + std::max(fit, 0);
+        if (tracked) known[dev][split].store(state, std::memory_order_release);
+    }
+    *clusters = state - 1;
+    return KGE_OK;
+}
+
+struct ProductPlan { int form, split; };
+int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) {
+    const int64_t tiles128 = ceil_div(M, I8_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, I8_BM) * ceil_div(N, 256);
+    for (int most = (int)std::min<int64_t>({I8_MAX_SPLIT, kblocks, sms / tiles128}); most > 1; --most) {
+        const int per = (kblocks + most - 1) / most, split = (kblocks + per - 1) / per;          // every CTA has a block
+        if (128 * (kblocks - per - 1) <= 5 * std::min<int64_t>(M, I8_BM)) break;
+        int room = 0;
+        const int rc = split_clusters(split, &room);
+        if (rc != KGE_OK) return rc;
+        if (tiles128 <= room) { *plan = {I8_SPLIT, split}; return KGE_OK; }
+    }
+    if (tiles256 >= sms && kblocks >= 16) { *plan = {I8_WIDE, 1}; return KGE_OK; }
+    const int64_t pair = ceil_div(tiles128, 2 * sms) * 256, narrow = ceil_div(ceil_div(M, I8_BM) * ceil_div(N, 64), 3 * sms) * 192;
+    *plan = {narrow < pair ? I8_NARROW : I8_PAIR, 1};
+    return KGE_OK;
+}
+
+template <int FORM>
+int launch_product(const CUtensorMap& a, const CUtensorMap& b, IntProductParams& p, int split, int sms, cudaStream_t s) {
+    constexpr size_t smem = i8_smem_bytes(FORM);
+    static_assert((smem + 1024) * i8_ctas_per_sm(FORM) <= 228 * 1024, "shared memory of an SM");
+    const int rc = configure_product<FORM>();
+    if (rc != KGE_OK) return rc;
+    p.tiles_n = (int)ceil_div(p.N, i8_bn(FORM));
+    p.items = (int)(ceil_div(p.M, I8_BM) * p.tiles_n);
+    p.kper = (p.kblocks + split - 1) / split;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(FORM == I8_SPLIT ? p.items * split : std::min<int64_t>(p.items, (int64_t)sms * i8_ctas_per_sm(FORM))));
+    cfg.blockDim = dim3(i8_threads(FORM)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = FORM == I8_SPLIT ? 2 : 1;
+    return launch_status(cudaLaunchKernelEx(&cfg, int8_product_kernel<FORM>, a, b, p));
+}
+
+}  // namespace
+}  // namespace kge
+
+using namespace kge;
+
+extern "C" {
+
+int kge_int8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, void* q, int64_t ldq, float* scales, void* stream) {
+    if (!is_float_type(x_type) || rows < 0 || rows > INT32_MAX || cols < 0 || cols > INT32_MAX - 65536 || ldx < cols || ldq < cols || ldq % 16 || !aligned_to(q, 16) ||
+        !aligned_to(scales, 4)) return KGE_ERR_BAD_ARG;
+    if (rows == 0 || cols == 0) return KGE_OK;
+    if (!x || !q || !scales || !aligned_to(x, type_bytes(x_type))) return KGE_ERR_BAD_ARG;
+    QuantParams p{};
+    p.x = x; p.ldx = ldx; p.q = static_cast<int8_t*>(q); p.ldq = ldq; p.scales = scales; p.rows = (int)rows; p.cols = (int)cols;
+    p.vec = aligned_to(x, 16) && ldx * type_bytes(x_type) % 16 == 0;
+    return with_type(x_type, [&](auto t) {
+        using T = decltype(t);
+        if (cols <= QUANT_PACKS * 32 * 8)
+            return launch_status(launch_dependent(quantize_rows_kernel<T, true>, dim3((unsigned)ceil_div(rows, QUANT_THREADS / 32)), dim3(QUANT_THREADS), 0,
+                                                  static_cast<cudaStream_t>(stream), p));
+        return launch_status(launch_dependent(quantize_rows_kernel<T, false>, dim3((unsigned)rows), dim3(QUANT_THREADS), 0, static_cast<cudaStream_t>(stream), p));
+    });
+}
+
+int kge_int8_matmul(const void* a, int64_t lda, const float* a_scales, const void* b, int64_t ldb, const float* b_scales, const void* addend, int64_t ld_addend,
+                    void* out, int32_t out_type, int64_t ld_out, int64_t M, int64_t N, int64_t K, int32_t* status, void* stream) {
+    if (!is_float_type(out_type) || M < 0 || N < 0 || K < 1 || M > INT32_MAX - 256 || N > INT32_MAX - 256 || ld_out < N || (addend && ld_addend < N))
+        return KGE_ERR_BAD_ARG;
+    if (M == 0 || N == 0) return KGE_OK;
+    if (!a || !b || !a_scales || !b_scales || !out || lda < K || ldb < K || lda % 16 || ldb % 16 || !aligned_to(a, 16) || !aligned_to(b, 16) ||
+        !aligned_to(a_scales, 4) || !aligned_to(b_scales, 4) || !aligned_to(out, type_bytes(out_type)) ||
+        (addend && !aligned_to(addend, type_bytes(out_type))) || !aligned_to(status, 4)) return KGE_ERR_BAD_ARG;
+    if (K > 131071 || ceil_div(M, 128) * ceil_div(N, 64) > INT32_MAX / 8) return KGE_ERR_UNSUPPORTED;        // (sums beyond 32 bits; tiles beyond their counters)
+    IntProductParams p{};
+    p.M = M; p.N = N; p.kblocks = (int)ceil_div(K, OPERAND_BK);
+    p.sa = a_scales; p.sb = b_scales;
+    p.addend = addend; p.ld_addend = ld_addend; p.out = out; p.ld_out = ld_out; p.out_type = out_type;
+    const int ob = type_bytes(out_type);
+    p.vec = ld_out * ob % 16 == 0 && aligned_to(out, 16) && (!addend || (ld_addend * ob % 16 == 0 && aligned_to(addend, 16)));
+    p.twos = N % 2 == 0 && ld_out % 2 == 0 && aligned_to(out, 2 * ob) && (!addend || (ld_addend % 2 == 0 && aligned_to(addend, 2 * ob)));
+    p.status = status; p.wait_limit = product_wait_limit.load(std::memory_order_relaxed);
+    int sms = 0, rc = sm_count(&sms);
+    if (rc != KGE_OK) return rc;
+    ProductPlan plan;
+    rc = product_plan(M, N, p.kblocks, sms, &plan);
+    if (rc != KGE_OK) return rc;
+    alignas(64) CUtensorMap ma, mb;
+    rc = operand_map(&ma, a, M, K, lda, I8_BM);
+    if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb, i8_box_rows(plan.form));
+    if (rc != KGE_OK) return rc;
+    p.idesc = i8_idesc(I8_BM, i8_bn(plan.form));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    switch (plan.form) {
+        case I8_SPLIT: return launch_product<I8_SPLIT>(ma, mb, p, plan.split, sms, s);
+        case I8_WIDE: return launch_product<I8_WIDE>(ma, mb, p, 1, sms, s);
+        case I8_NARROW: return launch_product<I8_NARROW>(ma, mb, p, 1, sms, s);
+        default: return launch_product<I8_PAIR>(ma, mb, p, 1, sms, s);
+    }
+}
+
+}  // extern "C"
