@@ -42,12 +42,8 @@ template <typename T> __device__ __forceinline__ void store8(const QuantParams& 
 #pragma unroll
     for (int j = 0; j < 8; ++j) q[j] = round_quotient(to_float(e.v[j]), s);
     int8_t* out = p.q + r * p.ldq + c;
-    if (c + 8 <= p.cols) {
-        uint2 w;
-        w.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | (uint32_t)q[3] << 24;
-        w.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | (uint32_t)q[7] << 24;
-        *reinterpret_cast<uint2*>(out) = w;
-    } else {
+    if (c + 8 <= p.cols) *reinterpret_cast<uint2*>(out) = pack_bytes(q);
+    else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) if (c + j < p.cols) out[j] = (int8_t)q[j];
     }

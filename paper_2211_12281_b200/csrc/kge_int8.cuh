@@ -29,6 +29,10 @@ __device__ __forceinline__ int round_quotient(float x, const RowScale& r) {
     const int q = __float2int_rn(__int_as_float(m));
     return x < 0.f ? -q : q;
 }
+__device__ __forceinline__ uint2 pack_bytes(const int (&q)[8]) {
+    return make_uint2((q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | (uint32_t)q[3] << 24,
+                      (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | (uint32_t)q[7] << 24);
+}
 #endif
 
 }  // namespace kge

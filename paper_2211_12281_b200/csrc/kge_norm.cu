@@ -1,6 +1,7 @@
 // The norms after and before a block, fused with its gate and residual scale:
 //   a = N1(y) (or y),  h = x + s act(g) a,  z = N2(h);   N(u) = (u - mu) r w + b,  r = 1 / sqrt(mean((u - mu)^2) + eps),  mu = mean(u), or 0
 // h is rounded once, when it is stored; z is made of the unrounded one.  z may leave as 8-bit integers with a scale for each row.
+#include <algorithm>
 #include <cmath>
 
 #include "kge_int8.cuh"
@@ -24,134 +25,91 @@ struct NormParams {
 
 __device__ __forceinline__ float deviation(const NormParams& p, float squares) { return rsqrtf(fmaf(squares, p.inv_d, p.eps)); }
 
-// Mean and reciprocal deviation of a row, in two passes over the registers (a mean far from zero does not eat the deviation's digits).
-template <class T, int K>
-__device__ __forceinline__ float2 row_stats(const NormParams& p, T& team, const float (&u)[K][8], const Place (&at)[K]) {
-    float mu = 0.f, sq = 0.f;
+// Takes the mean out of a row (of its team; zeros beyond it, before and after); returns it and the reciprocal deviation.  Two passes over the registers: a
+// mean far from zero does not eat the deviation's digits.
+template <int L, bool WIDE>
+__device__ __forceinline__ float2 centre(const NormParams& p, Team<L>& team, F8& u, const Place<WIDE>& at) {
+    float mu = 0.f;
     if (p.layer) {
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) mu += u[k][e];          // (zeros beyond the row)
-        mu = team.sum(mu) * p.inv_d;
+        mu = team.sum(total(u)) * p.inv_d;
+        u = u + at.spread(-mu);
     }
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float c = at[k].holds(e) ? u[k][e] - mu : 0.f;
-            sq = fmaf(c, c, sq);
-        }
-    return make_float2(mu, deviation(p, team.sum(sq)));
+    return make_float2(mu, deviation(p, team.sum(dot(u, u))));
 }
 
-template <typename TB>
-__device__ __forceinline__ void store_z8(const NormParams& p, int64_t row, const Place& at, const float (&z)[8], const RowScale& s) {
+template <bool WIDE>
+__device__ __forceinline__ void store_z8(const NormParams& p, int64_t row, const Place<WIDE>& at, const F8& z, const RowScale& s) {
     int8_t* out = static_cast<int8_t*>(p.z) + row * p.ldz;
     int q[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = round_quotient(z[e], s);
-    if (p.wide) {
-        if (!at.any()) return;
-        uint2 w;
-        w.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | (uint32_t)q[3] << 24;
-        w.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | (uint32_t)q[7] << 24;
-        *reinterpret_cast<uint2*>(out + at.first) = w;
+    for (int e = 0; e < 8; ++e) q[e] = round_quotient(z.get(e), s);
+    if constexpr (WIDE) {
+        if (at.any()) *reinterpret_cast<uint2*>(out + at.first) = pack_bytes(q);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) if (at.holds(e)) out[at.at(e)] = (int8_t)q[e];
     }
 }
 
-// L lanes hold a row (L = 0: the CTA's threads), K packs of eight elements each.
-template <typename TX, typename TB, int L, int K>
-__global__ void __launch_bounds__(L == 0 ? NORM_MOST / 8 : NORM_THREADS) norm_kernel(const __grid_constant__ NormParams p) {
+template <typename TX, typename TB> struct NormRow { Raw8<TX> x; Raw8<TB> y, gate; };
+template <typename TX, typename TB, bool WIDE>
+__device__ __forceinline__ NormRow<TX, TB> load_norm_row(const NormParams& p, int64_t r, const Place<WIDE>& at) {
+    NormRow<TX, TB> v;
+    v.x = at.load(static_cast<const TX*>(p.x) + r * p.ldx, r < p.n);
+    if (p.y) v.y = at.load(static_cast<const TB*>(p.y) + r * p.ldy, r < p.n);
+    if (p.gate) v.gate = at.load(static_cast<const TB*>(p.gate) + r * p.ldg, r < p.n);
+    return v;
+}
+
+// Teams of L threads (L = 0: the CTA) take rows in turn, the next one's loads under way.
+template <typename TX, typename TB, int L, bool WIDE>
+__global__ void __launch_bounds__(L == 0 ? NORM_MOST / 8 : NORM_THREADS, L == 0 ? 1 : NORM_CTAS) norm_kernel(const __grid_constant__ NormParams p) {
     __shared__ float parts[2][2][32];
     Team<L> team{parts};
-    const int lanes = L == 0 ? (int)blockDim.x : L, t = L == 0 ? (int)threadIdx.x : (int)threadIdx.x % L;
-    const int64_t r = L == 0 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (NORM_THREADS / (L == 0 ? 1 : L)) + threadIdx.x / (L == 0 ? 1 : L);
-    const bool live = r < p.n;
-    const bool wide = p.wide;
-    Place at[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) at[k] = Place(wide, lanes, t, k, live ? p.d : 0);
+    const int t = Team<L>::thread();
+    const Place<WIDE> row(Team<L>::size(), t, p.d);
+    const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
     grid_dependency_wait();
     allow_dependents();
-    float u[K][8];
-    {
-        Raw8<TX> x[K];
-        Raw8<TB> y[K], g[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) x[k] = load_row(static_cast<const TX*>(p.x) + r * p.ldx, at[k], wide);
+    NormRow<TX, TB> next = load_norm_row<TX, TB>(p, (int64_t)blockIdx.x * Team<L>::COUNT + Team<L>::index(), row);
+    for (int64_t r0 = (int64_t)blockIdx.x * Team<L>::COUNT; r0 < p.n; r0 += step) {
+        const int64_t r = r0 + Team<L>::index();
+        const bool live = r < p.n;
+        const Place<WIDE> at(Team<L>::size(), t, live ? p.d : 0);
+        const NormRow<TX, TB> now = next;
+        if (r0 + step < p.n) next = load_norm_row<TX, TB>(p, r + step, row);
+        float* const stats = p.stats && live && t == 0 ? p.stats + 4 * r : nullptr;
+        F8 u = wide_of(now.x);
+        float2 s = make_float2(0.f, 0.f);
         if (p.y) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) y[k] = load_row(static_cast<const TB*>(p.y) + r * p.ldy, at[k], wide);
-            if (p.gate) {
-#pragma unroll
-                for (int k = 0; k < K; ++k) g[k] = load_row(static_cast<const TB*>(p.gate) + r * p.ldg, at[k], wide);
-            }
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[k][e] = to_float(y[k].v[e]);
+            F8 a = wide_of(now.y);
             if (p.post) {
-                const float2 s = row_stats(p, team, u, at);
-                if (p.stats && live && t == 0) *reinterpret_cast<float2*>(p.stats + 4 * r) = s;
-#pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    float w[8], b[8];
-                    load_vector(p.w1, at[k], wide, 0.f, w);
-                    load_vector(p.b1, at[k], wide, 0.f, b);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[k][e] = fmaf((u[k][e] - s.x) * s.y, w[e], b[e]);
-                }
+                s = centre(p, team, a, at);
+                a = a * s.y * at.vector(p.w1);
+                if (p.b1) a = a + at.vector(p.b1);
             }
-            if (p.gate) {
-#pragma unroll
-                for (int k = 0; k < K; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[k][e] *= act_of(to_float(g[k].v[e]), p.act);
-            }
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float w[8];
-                load_vector(p.scale, at[k], wide, 1.f, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[k][e] = at[k].holds(e) ? fmaf(u[k][e], w[e], to_float(x[k].v[e])) : 0.f;
-                if (p.h) store_row(static_cast<TX*>(p.h) + r * p.ldh, at[k], wide, u[k]);
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[k][e] = to_float(x[k].v[e]);
+            if (p.gate) a = a * act_of(wide_of(now.gate), p.act);
+            u = p.scale ? fma8(a, at.vector(p.scale), u) : a + u;
+            if (p.h) at.store(static_cast<TX*>(p.h) + r * p.ldh, u);
         }
-    }
-    if (p.stats && !p.post && live && t == 0) *reinterpret_cast<float2*>(p.stats + 4 * r) = make_float2(0.f, 0.f);
-    if (!p.z) {
-        if (p.stats && live && t == 0) *reinterpret_cast<float2*>(p.stats + 4 * r + 2) = make_float2(0.f, 0.f);
-        return;
-    }
-    const float2 s = row_stats(p, team, u, at);
-    if (p.stats && live && t == 0) *reinterpret_cast<float2*>(p.stats + 4 * r + 2) = s;
-    float most = 0.f;
+        if (stats) *reinterpret_cast<float2*>(stats) = s;
+        s = make_float2(0.f, 0.f);
+        if (p.z) {
+            s = centre(p, team, u, at);
+            u = u * s.y * at.vector(p.w2);
+            if (p.b2) u = u + at.vector(p.b2);
+            if (p.z8) {
+                float most = 0.f;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        float w[8], b[8];
-        load_vector(p.w2, at[k], wide, 0.f, w);
-        load_vector(p.b2, at[k], wide, 0.f, b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            u[k][e] = fmaf((u[k][e] - s.x) * s.y, w[e], b[e]);
-            if (at[k].holds(e)) most = Team<L>::template join<true>(most, fabsf(u[k][e]));
+                for (int e = 0; e < 8; ++e) most = Team<L>::template join<true>(most, fabsf(u.get(e)));
+                const RowScale q = row_scale(team.most(most));
+                if (live && t == 0) p.z_scales[r] = q.s;
+                store_z8(p, r, at, u, q);
+            } else {
+                at.store(static_cast<TB*>(p.z) + r * p.ldz, u);
+            }
         }
-        if (!p.z8) store_row(static_cast<TB*>(p.z) + r * p.ldz, at[k], wide, u[k]);
-    }
-    if (p.z8) {
-        const RowScale q = row_scale(team.most(most));
-        if (live && t == 0) p.z_scales[r] = q.s;
-#pragma unroll
-        for (int k = 0; k < K; ++k) store_z8<TB>(p, r, at[k], u[k], q);
+        if (stats) *reinterpret_cast<float2*>(stats + 2) = s;
     }
 }
 
@@ -208,16 +166,30 @@ __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_loop_kernel(const __gr
     if (p.stats && threadIdx.x == 0) *reinterpret_cast<float4*>(p.stats + 4 * r) = make_float4(s1.x, s1.y, s2.x, s2.y);
 }
 
+// As many CTAs as run at a time, or fewer, so that each has as many rows as the others.
+template <typename TX, typename TB, int L, bool WIDE>
+int launch_rows(const NormParams& p, int sms, cudaStream_t s) {
+    const int threads = L == 0 ? (int)ceil_div(p.d, 256) * 32 : NORM_THREADS;
+    const int64_t all = ceil_div(p.n, Team<L>::COUNT), room = (int64_t)sms * (L == 0 ? std::max(1, 1024 / threads) : NORM_CTAS), turns = ceil_div(all, room);
+    return launch_status(launch_dependent(norm_kernel<TX, TB, L, WIDE>, dim3((unsigned)ceil_div(all, turns)), dim3((unsigned)threads), 0, s, p));
+}
+
 template <typename TX, typename TB>
 int launch_norm(const NormParams& p, cudaStream_t s) {
-    auto lanes = [&](auto kernel, int per) { return launch_status(launch_dependent(kernel, dim3((unsigned)ceil_div(p.n, NORM_THREADS / per)), dim3(NORM_THREADS), 0, s, p)); };
-    if (p.d <= 64) return lanes(norm_kernel<TX, TB, 8, 1>, 8);
-    if (p.d <= 128) return lanes(norm_kernel<TX, TB, 16, 1>, 16);
-    if (p.d <= 256) return lanes(norm_kernel<TX, TB, 32, 1>, 32);
-    if (p.d <= 512) return lanes(norm_kernel<TX, TB, 32, 2>, 32);
-    if (p.d <= 1024) return lanes(norm_kernel<TX, TB, 32, 4>, 32);
-    if (p.d <= NORM_MOST) return launch_status(launch_dependent(norm_kernel<TX, TB, 0, 1>, dim3((unsigned)p.n), dim3((unsigned)(ceil_div(p.d, 256) * 32)), 0, s, p));
-    return launch_status(launch_dependent(norm_loop_kernel<TX, TB>, dim3((unsigned)p.n), dim3(NORM_LOOP_THREADS), 0, s, p));
+    int sms = 0;
+    const int rc = sm_count(&sms);
+    if (rc != KGE_OK) return rc;
+    if (p.d > NORM_MOST) return launch_status(launch_dependent(norm_loop_kernel<TX, TB>, dim3((unsigned)p.n), dim3(NORM_LOOP_THREADS), 0, s, p));
+    const int team = norm_team(p.d);
+    if (!p.wide) return team == 0 ? launch_rows<TX, TB, 0, false>(p, sms, s) : (team > 32 ? launch_rows<TX, TB, 128, false>(p, sms, s) : launch_rows<TX, TB, 32, false>(p, sms, s));
+    switch (team) {
+        case 8: return launch_rows<TX, TB, 8, true>(p, sms, s);
+        case 16: return launch_rows<TX, TB, 16, true>(p, sms, s);
+        case 32: return launch_rows<TX, TB, 32, true>(p, sms, s);
+        case 64: return launch_rows<TX, TB, 64, true>(p, sms, s);
+        case 128: return launch_rows<TX, TB, 128, true>(p, sms, s);
+        default: return launch_rows<TX, TB, 0, true>(p, sms, s);
+    }
 }
 
 }  // namespace

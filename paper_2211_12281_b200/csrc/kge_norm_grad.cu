@@ -27,157 +27,128 @@ struct NormGradParams {
     float inv_d;
 };
 
-constexpr int GRAD_CTAS = 592;                 // at most, each with sums of its own; a constant, so that the order of additions is the sizes' alone
 constexpr int GRAD_HELD = 4096;                // widest row that a CTA's threads hold with its sums
+constexpr int GRAD_SMS = 148;                  // CTAs are as many as this many SMs run, each with sums of its own: a constant, so that the order of additions is the sizes' alone
 
-// CTAs that share n rows, `per` at a time.
-inline int grad_ctas(int64_t n, int per) { return (int)std::min<int64_t>(GRAD_CTAS, ceil_div(n, per)); }
-inline int grad_lanes(int d) { return d <= 64 ? 8 : (d <= 128 ? 16 : 32); }
-inline int grad_ctas_of(int64_t n, int d) { return grad_ctas(n, d <= 512 ? NORM_THREADS / grad_lanes(d) : 1); }
+// CTAs that share n rows, each as many as the others.
+inline int grad_ctas_of(int64_t n, int d) {
+    const int team = norm_team(d), threads = (int)std::min<int64_t>(ceil_div(d, 256) * 32, 512);
+    const int64_t all = team == 0 ? n : ceil_div(n, NORM_THREADS / team), room = GRAD_SMS * (team == 0 ? std::max(1, 512 / threads) : 2);
+    return (int)ceil_div(all, ceil_div(all, room));
+}
 
-struct Sums { float t1[8], t0[8], s1[8], s0[8]; };
-
-// One row: L lanes of a warp, or the CTA's threads.
-template <typename TX, typename TB, int L, int K>
-__device__ __forceinline__ void grad_row(const NormGradParams& p, Team<L>& team, int64_t r, const Place (&at)[K], Sums (&sums)[K]) {
-    const bool wide = p.wide, live = at[0].d > 0;
-    float dh[K][8], yn[K][8], gate[K][8];
-    const float4 st = live ? __ldg(reinterpret_cast<const float4*>(p.stats + 4 * r)) : make_float4(0.f, 0.f, 0.f, 0.f);
-    {
-        Raw8<TX> x[K], dhr[K];
-        Raw8<TB> y[K], g[K], dz[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (p.dh) dhr[k] = load_row(static_cast<const TX*>(p.dh) + r * p.ldh, at[k], wide);
-            if (p.dz) {
-                x[k] = load_row(static_cast<const TX*>(p.x) + r * p.ldx, at[k], wide);
-                dz[k] = load_row(static_cast<const TB*>(p.dz) + r * p.ldz, at[k], wide);
-            }
-            if (p.y) y[k] = load_row(static_cast<const TB*>(p.y) + r * p.ldy, at[k], wide);
-            if (p.gate) g[k] = load_row(static_cast<const TB*>(p.gate) + r * p.ldg, at[k], wide);
-        }
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                dh[k][e] = p.dh ? to_float(dhr[k].v[e]) : 0.f;
-                yn[k][e] = p.y && at[k].holds(e) ? (to_float(y[k].v[e]) - st.x) * (p.post ? st.y : 1.f) : 0.f;
-                gate[k][e] = p.gate ? to_float(g[k].v[e]) : 0.f;
-            }
-        if (p.dz) {
-            float hn[K][8], c[K][8], mean = 0.f, dot = 0.f;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float w1[8], b1[8], s[8], w2[8];
-                load_vector(p.w1, at[k], wide, 1.f, w1);
-                load_vector(p.b1, at[k], wide, 0.f, b1);
-                load_vector(p.scale, at[k], wide, 1.f, s);
-                load_vector(p.w2, at[k], wide, 0.f, w2);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float h = to_float(x[k].v[e]);
-                    if (p.y) h = fmaf(fmaf(yn[k][e], w1[e], b1[e]) * (p.gate ? act_of(gate[k][e], p.act) : 1.f), s[e], h);
-                    const float z = to_float(dz[k].v[e]);
-                    hn[k][e] = at[k].holds(e) ? (h - st.z) * st.w : 0.f;
-                    c[k][e] = z * w2[e];
-                    mean += c[k][e];
-                    dot = fmaf(c[k][e], hn[k][e], dot);
-                    sums[k].t1[e] = fmaf(z, hn[k][e], sums[k].t1[e]);
-                    sums[k].t0[e] += z;
-                }
-            }
-            if (p.layer) team.sum(mean, dot);
-            else { dot = team.sum(dot); mean = 0.f; }
-            mean *= p.inv_d; dot *= p.inv_d;
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dh[k][e] = fmaf(st.w, c[k][e] - mean - hn[k][e] * dot, dh[k][e]);
-        }
+template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y, gate, dz; float4 stats; };
+template <typename TX, typename TB, bool WIDE>
+__device__ __forceinline__ GradRow<TX, TB> load_grad_row(const NormGradParams& p, int64_t r, const Place<WIDE>& at) {
+    GradRow<TX, TB> v{};
+    const bool there = r < p.n;
+    if (p.dh) v.dh = at.load(static_cast<const TX*>(p.dh) + r * p.ldh, there);
+    if (p.dz) {
+        v.dz = at.load(static_cast<const TB*>(p.dz) + r * p.ldz, there);
+        v.x = at.load(static_cast<const TX*>(p.x) + r * p.ldx, there);
     }
-    if (p.dx) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) store_row(static_cast<TX*>(p.dx) + r * p.ldox, at[k], wide, dh[k]);
+    if (p.y) v.y = at.load(static_cast<const TB*>(p.y) + r * p.ldy, there);
+    if (p.gate) v.gate = at.load(static_cast<const TB*>(p.gate) + r * p.ldg, there);
+    if (there) v.stats = __ldg(reinterpret_cast<const float4*>(p.stats + 4 * r));
+    return v;
+}
+
+struct Sums { F8 t1, s1, t0, s0; };
+__device__ __forceinline__ const F8& sum_of(const Sums& s, int q) { return q == 0 ? s.t1 : (q == 1 ? s.s1 : (q == 2 ? s.t0 : s.s0)); }
+
+// One row of a team.
+template <typename TX, typename TB, int L, bool WIDE>
+__device__ __forceinline__ void grad_row(const NormGradParams& p, Team<L>& team, int64_t r, const Place<WIDE>& at, const GradRow<TX, TB>& v, Sums& sums) {
+    F8 dh = p.dh ? wide_of(v.dh) : all8(0.f), yn = all8(0.f), sigmoid = all8(0.f);
+    if (p.y) {
+        yn = wide_of(v.y);
+        if (p.post) yn = (yn + at.spread(-v.stats.x)) * v.stats.y;
     }
+    if (p.gate && p.act != NORM_PLAIN) sigmoid = each8(wide_of(v.gate), sigmoid_of);
+    float mean = 0.f, along = 0.f;
+    if (p.dz) {
+        F8 h = wide_of(v.x);
+        if (p.y) {
+            F8 a = yn;
+            if (p.w1) a = a * at.vector(p.w1);
+            if (p.b1) a = a + at.vector(p.b1);
+            if (p.gate) a = a * act_with(wide_of(v.gate), sigmoid, p.act);
+            h = p.scale ? fma8(a, at.vector(p.scale), h) : a + h;
+        }
+        const F8 hn = (h + at.spread(-v.stats.z)) * v.stats.w, dz = wide_of(v.dz), c = dz * at.vector(p.w2);
+        sums.t1 = fma8(dz, hn, sums.t1);
+        sums.t0 = sums.t0 + dz;
+        along = dot(c, hn);
+        if (p.layer) { mean = total(c); team.sum(mean, along); }
+        else along = team.sum(along);
+        dh = fma8(fma8(hn, -along * p.inv_d, c + at.spread(-mean * p.inv_d)), v.stats.w, dh);
+    }
+    if (p.dx) at.store(static_cast<TX*>(p.dx) + r * p.ldox, dh);
     if (!p.y) return;
-    float f[K][8], mean = 0.f, dot = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        float w1[8], b1[8], s[8], dg[8];
-        load_vector(p.w1, at[k], wide, 1.f, w1);
-        load_vector(p.b1, at[k], wide, 0.f, b1);
-        load_vector(p.scale, at[k], wide, 1.f, s);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float2 act = p.gate ? act_and_slope(gate[k][e], p.act) : make_float2(1.f, 0.f);
-            const float u = at[k].holds(e) ? act.x * dh[k][e] : 0.f, ee = s[e] * dh[k][e];
-            dg[e] = act.y * fmaf(yn[k][e], w1[e], b1[e]) * ee;
-            sums[k].s1[e] = fmaf(u, yn[k][e], sums[k].s1[e]);
-            sums[k].s0[e] += u;
-            f[k][e] = u * s[e] * w1[e];
-            mean += f[k][e];
-            dot = fmaf(f[k][e], yn[k][e], dot);
-        }
-        if (p.dgate) store_row(static_cast<TB*>(p.dgate) + r * p.ldog, at[k], wide, dg);
+    F8 f = dh;
+    if (p.gate) f = f * act_with(wide_of(v.gate), sigmoid, p.act);
+    sums.s1 = fma8(f, yn, sums.s1);
+    sums.s0 = sums.s0 + f;
+    if (p.scale) {
+        const F8 s = at.vector(p.scale);
+        f = f * s;
+        dh = dh * s;
+    }
+    if (p.dgate) {
+        F8 a = yn;
+        if (p.w1) a = a * at.vector(p.w1);
+        if (p.b1) a = a + at.vector(p.b1);
+        at.store(static_cast<TB*>(p.dgate) + r * p.ldog, slope_with(wide_of(v.gate), sigmoid, p.act) * a * dh);
     }
     if (!p.dy) return;
     if (p.post) {
-        if (p.layer) team.sum(mean, dot);
-        else { dot = team.sum(dot); mean = 0.f; }
-        mean *= p.inv_d; dot *= p.inv_d;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[k][e] = st.y * (f[k][e] - mean - yn[k][e] * dot);
+        f = f * at.vector(p.w1);
+        along = dot(f, yn);
+        if (p.layer) { mean = total(f); team.sum(mean, along); }
+        else { along = team.sum(along); mean = 0.f; }
+        f = fma8(yn, -along * p.inv_d, f + at.spread(-mean * p.inv_d)) * v.stats.y;
     }
-#pragma unroll
-    for (int k = 0; k < K; ++k) store_row(static_cast<TB*>(p.dy) + r * p.ldoy, at[k], wide, f[k]);
+    at.store(static_cast<TB*>(p.dy) + r * p.ldoy, f);
 }
 
-template <typename TX, typename TB, int L, int K>
-__global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
+// Teams take rows in turn, the next one's loads under way, and add up the columns' sums of theirs in registers.
+template <typename TX, typename TB, int L, bool WIDE>
+__global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
     __shared__ float parts[2][2][32];
-    __shared__ float joined[L == 0 ? 1 : NORM_THREADS * 8 * K];
+    __shared__ float joined[L == 0 ? 1 : NORM_THREADS * 8];
     Team<L> team{parts};
-    constexpr int TEAMS = L == 0 ? 1 : NORM_THREADS / (L == 0 ? 1 : L);
-    const int lanes = L == 0 ? (int)blockDim.x : L, t = L == 0 ? (int)threadIdx.x : (int)threadIdx.x % L, mine = L == 0 ? 0 : threadIdx.x / (L == 0 ? 1 : L);
+    const int t = Team<L>::thread();
+    const Place<WIDE> row(Team<L>::size(), t, p.d);
+    const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
     grid_dependency_wait();
     allow_dependents();
-    Sums sums[K] = {};
-    for (int64_t r0 = (int64_t)blockIdx.x * TEAMS; r0 < p.n; r0 += (int64_t)gridDim.x * TEAMS) {
-        const int64_t r = r0 + mine;
-        Place at[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) at[k] = Place(p.wide, lanes, t, k, r < p.n ? p.d : 0);
-        grad_row<TX, TB, L, K>(p, team, r, at, sums);
+    Sums sums{all8(0.f), all8(0.f), all8(0.f), all8(0.f)};
+    GradRow<TX, TB> next = load_grad_row<TX, TB>(p, (int64_t)blockIdx.x * Team<L>::COUNT + Team<L>::index(), row);
+    for (int64_t r0 = (int64_t)blockIdx.x * Team<L>::COUNT; r0 < p.n; r0 += step) {
+        const int64_t r = r0 + Team<L>::index();
+        const Place<WIDE> at(Team<L>::size(), t, r < p.n ? p.d : 0);
+        const GradRow<TX, TB> now = next;
+        if (r0 + step < p.n) next = load_grad_row<TX, TB>(p, r + step, row);
+        grad_row<TX, TB, L, WIDE>(p, team, r, at, now, sums);
     }
     if (p.sums == 0) return;
     float* part = p.part + (int64_t)blockIdx.x * p.sums * p.d;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (q >= p.sums) break;
-        // (order: T1, S1, T0, S0)
         if constexpr (L == 0) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const Place at(p.wide, lanes, t, k, p.d);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (at.holds(e)) part[(int64_t)q * p.d + at.at(e)] = q == 0 ? sums[k].t1[e] : (q == 1 ? sums[k].s1[e] : (q == 2 ? sums[k].t0[e] : sums[k].s0[e]));
-            }
+            row.store(part + (int64_t)q * p.d, sum_of(sums, q));
         } else {
-            constexpr int WIDTH = L * 8 * K;
+            constexpr int WIDTH = L * 8;
             __syncthreads();
+            const Place<WIDE> at(L, t, WIDTH);
+            const Raw8<float> mine = narrow_of<float>(sum_of(sums, q));
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const Place at(p.wide, lanes, t, k, WIDTH);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) joined[mine * WIDTH + at.at(e)] = q == 0 ? sums[k].t1[e] : (q == 1 ? sums[k].s1[e] : (q == 2 ? sums[k].t0[e] : sums[k].s0[e]));
-            }
+            for (int e = 0; e < 8; ++e) joined[Team<L>::index() * WIDTH + at.at(e)] = mine.v[e];       // (shared memory: no access by load_wide's kind)
             __syncthreads();
             for (int i = threadIdx.x; i < p.d; i += NORM_THREADS) {
                 float v = joined[i];
-                for (int m = 1; m < TEAMS; ++m) v += joined[m * WIDTH + i];
+                for (int m = 1; m < Team<L>::COUNT; ++m) v += joined[m * WIDTH + i];
                 part[(int64_t)q * p.d + i] = v;
             }
         }
@@ -293,12 +264,27 @@ __global__ void __launch_bounds__(JOIN_COLS * JOIN_ROWS) norm_join_kernel(const 
 template <typename TX, typename TB>
 int launch_norm_grad(const NormGradParams& p, int ctas, cudaStream_t s) {
     auto launch = [&](auto kernel, int threads) { return launch_status(launch_dependent(kernel, dim3((unsigned)ctas), dim3((unsigned)threads), 0, s, p)); };
-    if (p.d <= 64) return launch(norm_grad_kernel<TX, TB, 8, 1>, NORM_THREADS);
-    if (p.d <= 128) return launch(norm_grad_kernel<TX, TB, 16, 1>, NORM_THREADS);
-    if (p.d <= 256) return launch(norm_grad_kernel<TX, TB, 32, 1>, NORM_THREADS);
-    if (p.d <= 512) return launch(norm_grad_kernel<TX, TB, 32, 2>, NORM_THREADS);
-    if (p.d <= GRAD_HELD) return launch(norm_grad_kernel<TX, TB, 0, 1>, (int)ceil_div(p.d, 256) * 32);
-    return launch(norm_grad_loop_kernel<TX, TB>, NORM_LOOP_THREADS);
+    if (p.d > GRAD_HELD) return launch(norm_grad_loop_kernel<TX, TB>, NORM_LOOP_THREADS);
+    const int team = norm_team(p.d), threads = (int)ceil_div(p.d, 256) * 32;
+    if (!p.wide) {
+        // (teams as for wide rows, so that the columns' sums are the same)
+        switch (team) {
+            case 8: return launch(norm_grad_kernel<TX, TB, 8, false>, NORM_THREADS);
+            case 16: return launch(norm_grad_kernel<TX, TB, 16, false>, NORM_THREADS);
+            case 32: return launch(norm_grad_kernel<TX, TB, 32, false>, NORM_THREADS);
+            case 64: return launch(norm_grad_kernel<TX, TB, 64, false>, NORM_THREADS);
+            case 128: return launch(norm_grad_kernel<TX, TB, 128, false>, NORM_THREADS);
+            default: return launch(norm_grad_kernel<TX, TB, 0, false>, threads);
+        }
+    }
+    switch (team) {
+        case 8: return launch(norm_grad_kernel<TX, TB, 8, true>, NORM_THREADS);
+        case 16: return launch(norm_grad_kernel<TX, TB, 16, true>, NORM_THREADS);
+        case 32: return launch(norm_grad_kernel<TX, TB, 32, true>, NORM_THREADS);
+        case 64: return launch(norm_grad_kernel<TX, TB, 64, true>, NORM_THREADS);
+        case 128: return launch(norm_grad_kernel<TX, TB, 128, true>, NORM_THREADS);
+        default: return launch(norm_grad_kernel<TX, TB, 0, true>, threads);
+    }
 }
 
 }  // namespace

@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "kge_common.cuh"
 
 namespace kge {
@@ -45,6 +47,22 @@ struct FastDiv {
     __device__ __forceinline__ uint32_t div(uint32_t n) const { return d == 1 ? n : __umulhi(n, m) >> s; }
 #endif
 };
+
+// Streaming multiprocessors of the current device.
+inline int sm_count(int* sms) {
+    static std::atomic<int> known[kMaxDevices];
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return KGE_ERR_CUDA;
+    const bool tracked = dev >= 0 && dev < kMaxDevices;
+    *sms = tracked ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (*sms == 0) {
+        e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e != cudaSuccess) return KGE_ERR_CUDA;
+        if (tracked) known[dev].store(*sms, std::memory_order_relaxed);
+    }
+    return KGE_OK;
+}
 
 #ifdef __CUDACC__
 template <typename T, int N> struct alignas(sizeof(T) * N) Pack { T v[N]; };
@@ -90,6 +108,13 @@ template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// Two fp32 operations in one instruction, each rounded as a single one would be.
+__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 unpair(uint64_t a) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a)); return r; }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 
 __device__ __forceinline__ void note_status(int32_t* status, int code) { if (status) set_status(status, code); }
 

@@ -56,13 +56,6 @@ __device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
 __device__ __forceinline__ uint64_t two_words(uint32_t a, uint32_t b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b)); return r; }
-// Two fp32 operations in one instruction, each rounded as a single one would be.
-__device__ __forceinline__ uint64_t pair(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
-__device__ __forceinline__ float2 unpair(uint64_t a) { float2 r; asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a)); return r; }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-
 // Registers of a warpgroup, out of what the block was launched with.
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -243,22 +236,6 @@ inline int operand_map(CUtensorMap* map, const void* base, int64_t rows, int64_t
     const cuuint32_t box[2] = {OPERAND_BK, (cuuint32_t)box_rows}, one[2] = {1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS ? KGE_OK : KGE_ERR_CUDA;
-}
-
-// Streaming multiprocessors of the current device.
-inline int sm_count(int* sms) {
-    static std::atomic<int> known[kMaxDevices];
-    int dev = -1;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return KGE_ERR_CUDA;
-    const bool tracked = dev >= 0 && dev < kMaxDevices;
-    *sms = tracked ? known[dev].load(std::memory_order_relaxed) : 0;
-    if (*sms == 0) {
-        e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
-        if (e != cudaSuccess) return KGE_ERR_CUDA;
-        if (tracked) known[dev].store(*sms, std::memory_order_relaxed);
-    }
-    return KGE_OK;
 }
 
 }  // namespace kge
