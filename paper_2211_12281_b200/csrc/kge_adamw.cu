@@ -8,7 +8,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "kge_ops.cuh"
+#include "kge_eight.cuh"
 
 namespace kge {
 
@@ -62,66 +62,44 @@ __device__ __forceinline__ uint4 adam_words(const AdamCommon& c, uint64_t group,
     return make_uint4(c0, c1, c2, c3);
 }
 
-// Eight elements as one access of 8, 16 or 32 bytes.
-template <typename T> struct Eight { T v[8]; };
-template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T* p) {
-    Eight<T> r;
-    uint32_t* w = reinterpret_cast<uint32_t*>(r.v);
-    if constexpr (sizeof(T) == 4)
-        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
-    else if constexpr (sizeof(T) == 2)
-        asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
-    else
-        asm volatile("ld.global.L1::no_allocate.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-    return r;
-}
-template <typename T> __device__ __forceinline__ void store_eight(T* p, const Eight<T>& r) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(r.v);
-    if constexpr (sizeof(T) == 4)
-        asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
-                     ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p) : "memory");
-    else if constexpr (sizeof(T) == 2)
-        asm volatile("st.global.v4.b32 [%4], {%0, %1, %2, %3};" ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(p) : "memory");
-    else
-        asm volatile("st.global.v2.b32 [%2], {%0, %1};" ::"r"(w[0]), "r"(w[1]), "l"(p) : "memory");
-}
-template <typename T> __device__ __forceinline__ Eight<T> get(const void* base, int64_t at, int valid, bool vec) {
+template <typename T> __device__ __forceinline__ Raw8<T> get(const void* base, int64_t at, int valid, bool vec) {
     const T* p = static_cast<const T*>(base) + at;
-    if (vec && valid == 8) return load_eight(p);
-    Eight<T> r;
+    if (vec && valid == 8) return load_wide(p);
+    Raw8<T> r = {};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r.v[j] = j < valid ? p[j] : T();
+    for (int e = 0; e < 8; ++e) if (e < valid) set_element(r, e, p[e]);
     return r;
 }
-template <typename T> __device__ __forceinline__ void put(void* base, int64_t at, int valid, bool vec, const Eight<T>& r) {
+template <typename T> __device__ __forceinline__ void put(void* base, int64_t at, int valid, bool vec, const Raw8<T>& r) {
     T* p = static_cast<T*>(base) + at;
-    if (vec && valid == 8) { store_eight(p, r); return; }
+    if (vec && valid == 8) { store_wide(p, r); return; }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) if (j < valid) p[j] = r.v[j];
+    for (int e = 0; e < 8; ++e) if (e < valid) p[e] = element(r, e);
 }
 
-// An e4m3 value is the half whose bits the conversion instruction gives; an e5m2 value is a half without its low byte.
-__device__ __forceinline__ void decode_m(const Eight<uint8_t>& q, float scale, float (&x)[8]) {
-    const uint16_t* w = reinterpret_cast<const uint16_t*>(q.v);
+// An e4m3 value is the half that the conversion instruction gives; an e5m2 value is a half without its low byte.
+__device__ __forceinline__ F8 decode_m(const Raw8<uint8_t>& q, float scale) {
+    F8 x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t h;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(w[i]));
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)(q.w[i >> 1] >> (16 * (i & 1)))));
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        x[2 * i] = f.x * scale;
-        x[2 * i + 1] = f.y * scale;
+        x.v[2 * i] = f.x * scale;
+        x.v[2 * i + 1] = f.y * scale;
     }
+    return x;
 }
-__device__ __forceinline__ void decode_v(const Eight<uint8_t>& q, float scale, float (&x)[8]) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(q.v);
+__device__ __forceinline__ F8 decode_v(const Raw8<uint8_t>& q, float scale) {
+    F8 x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t h = __byte_perm(w[i >> 1], 0, i & 1 ? 0x3424 : 0x1404);
+        const uint32_t h = __byte_perm(q.w[i >> 1], 0, i & 1 ? 0x3424 : 0x1404);
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        x[2 * i] = f.x * scale;
-        x[2 * i + 1] = f.y * scale;
+        x.v[2 * i] = f.x * scale;
+        x.v[2 * i + 1] = f.y * scale;
     }
+    return x;
 }
 
 // The scale of a block whose largest magnitude has the bits `most`: the power of two that puts it into the binade of exponent `top`,
@@ -158,55 +136,45 @@ __device__ __forceinline__ void adam_chunk(const AdamCommon& c, const AdamTensor
         if (BITS == 32 && valid == 0) return;
         if (BITS == 8 && from + turn * ADAM_THREADS * ADAM_PER + (int64_t)(threadIdx.x & ~31u) * ADAM_PER >= t.n) return;       // (a warp's lanes stay together)
         const bool vec = t.vec;
-        const Eight<TG> g8 = get<TG>(t.g, at, valid, vec);
-        const Eight<TS> m8 = get<TS>(t.m, at, valid, vec);
-        const Eight<TS> v8 = get<TS>(t.v, at, valid, vec);
-        const Eight<TP> p8 = get<TP>(t.p, at, valid, vec);
-        float m[8], v[8];
+        const Raw8<TG> g8 = get<TG>(t.g, at, valid, vec);
+        const Raw8<TS> m8 = get<TS>(t.m, at, valid, vec);
+        const Raw8<TS> v8 = get<TS>(t.v, at, valid, vec);
+        const Raw8<TP> p8 = get<TP>(t.p, at, valid, vec);
+        F8 m, v;
         const int64_t block = at / ADAM_BLOCK;
         if constexpr (BITS == 8) {
             const float ms = valid ? t.ms[block] : 0.f, vs = valid ? t.vs[block] : 0.f;
-            decode_m(m8, ms, m);
-            decode_v(v8, vs, v);
+            m = decode_m(m8, ms);
+            v = decode_v(v8, vs);
         } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { m[j] = m8.v[j]; v[j] = v8.v[j]; }
+            m = wide_of(m8);
+            v = wide_of(v8);
         }
+        const F8 g = wide_of(g8);
+        F8 p = wide_of(p8);
         // products and sums of the moments are rounded one by one: the 8-bit rounding below is a function of their last bits
         uint32_t most_m = 0, most_v = 0;
-        Eight<TP> pn;
-        float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float g = __fmul_rn(to_float(g8.v[j]), s.grad_scale);
-            m[j] = __fadd_rn(__fmul_rn(m[j], c.b1), __fmul_rn(g, c.o1));
-            v[j] = __fadd_rn(__fmul_rn(v[j], c.b2), __fmul_rn(__fmul_rn(g, g), c.o2));
-            const float change = __fdiv_rn(m[j], fmaf(__fsqrt_rn(v[j]), s.root, c.eps));
-            p[j] = fmaf(-s.size, change, to_float(p8.v[j]) * s.keep);
-            pn.v[j] = from_float<TP>(p[j]);
+        for (int e = 0; e < 8; ++e) {
+            const float x = __fmul_rn(g.v[e], s.grad_scale);
+            m.v[e] = __fadd_rn(__fmul_rn(m.v[e], c.b1), __fmul_rn(x, c.o1));
+            v.v[e] = __fadd_rn(__fmul_rn(v.v[e], c.b2), __fmul_rn(__fmul_rn(x, x), c.o2));
+            const float change = __fdiv_rn(m.v[e], fmaf(__fsqrt_rn(v.v[e]), s.root, c.eps));
+            p.v[e] = fmaf(-s.size, change, p.v[e] * s.keep);
             if (BITS == 8) {
-                most_m = max(most_m, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-                most_v = max(most_v, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+                most_m = max(most_m, __float_as_uint(m.v[e]) & 0x7FFFFFFFu);
+                most_v = max(most_v, __float_as_uint(v.v[e]) & 0x7FFFFFFFu);
             }
         }
-        if (valid) put(t.p, at, valid, vec, pn);
-        if (t.copy && valid) {
-            if (t.copy_type == KGE_BF16) {
-                Eight<__nv_bfloat16> o;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o.v[j] = from_float<__nv_bfloat16>(p[j]);
-                put(t.copy, at, valid, vec, o);
-            } else {
-                Eight<__half> o;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o.v[j] = from_float<__half>(p[j]);
-                put(t.copy, at, valid, vec, o);
-            }
+        if (valid) {
+            put(t.p, at, valid, vec, narrow_of<TP>(p));
+            if (t.copy && t.copy_type == KGE_BF16) put(t.copy, at, valid, vec, narrow_of<__nv_bfloat16>(p));
+            if (t.copy && t.copy_type == KGE_F16) put(t.copy, at, valid, vec, narrow_of<__half>(p));
         }
-        Eight<TS> mn, vn;
+        Raw8<TS> mn, vn;
         if constexpr (BITS == 32) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { mn.v[j] = m[j]; vn.v[j] = v[j]; }
+            mn = narrow_of<float>(m);
+            vn = narrow_of<float>(v);
         } else {
             const BlockScale sm = block_scale(half_warp_max(most_m), 7), sv = block_scale(half_warp_max(most_v), 14);
             if ((threadIdx.x & 15) == 0 && valid) { t.ms[block] = sm.s; t.vs[block] = sv.s; }
@@ -214,13 +182,16 @@ __device__ __forceinline__ void adam_chunk(const AdamCommon& c, const AdamTensor
             for (int k = 0; k < 2; ++k) {
                 const uint4 words = adam_words(c, (uint64_t)at / 4 + k, t.index, s);
                 const uint32_t w[4] = {words.x, words.y, words.z, words.w};
+                uint32_t a = 0, b = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int j = 4 * k + i;
-                    mn.v[j] = (uint8_t)(code_of<3, 7>(m[j], sm.inv, w[i] & 0xFFFFu) | (__float_as_uint(m[j]) >> 31) << 7);
+                    const float x = m.v[4 * k + i], y = v.v[4 * k + i];
+                    a |= (code_of<3, 7>(x, sm.inv, w[i] & 0xFFFFu) | (__float_as_uint(x) >> 31) << 7) << (8 * i);
                     // A positive v stays positive: with v = 0 beside an m that was rounded up the next step would be m / eps.
-                    vn.v[j] = (uint8_t)max(code_of<2, 15>(v[j], sv.inv, w[i] >> 16), v[j] > 0.f && sv.inv > 0.f ? 1u : 0u);
+                    b |= max(code_of<2, 15>(y, sv.inv, w[i] >> 16), y > 0.f && sv.inv > 0.f ? 1u : 0u) << (8 * i);
                 }
+                mn.w[k] = a;
+                vn.w[k] = b;
             }
         }
         if (valid) {

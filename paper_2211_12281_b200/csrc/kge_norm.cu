@@ -25,16 +25,15 @@ struct NormParams {
 
 __device__ __forceinline__ float deviation(const NormParams& p, float squares) { return rsqrtf(fmaf(squares, p.inv_d, p.eps)); }
 
-// Takes the mean out of a row (of its team; zeros beyond it, before and after); returns it and the reciprocal deviation.  Two passes over the registers: a
-// mean far from zero does not eat the deviation's digits.
+// Takes the mean out of a team's row; returns it and the reciprocal deviation.  Two passes over the registers: a mean far from zero does not eat the deviation's digits.
 template <int L, bool WIDE>
 __device__ __forceinline__ float2 centre(const NormParams& p, Team<L>& team, F8& u, const Place<WIDE>& at) {
     float mu = 0.f;
     if (p.layer) {
-        mu = team.sum(total(u)) * p.inv_d;
-        u = u + at.spread(-mu);
+        mu = team.sum(at.total(u)) * p.inv_d;
+        u = u + -mu;
     }
-    return make_float2(mu, deviation(p, team.sum(dot(u, u))));
+    return make_float2(mu, deviation(p, team.sum(at.dot(u, u))));
 }
 
 template <bool WIDE>
@@ -42,9 +41,9 @@ __device__ __forceinline__ void store_z8(const NormParams& p, int64_t row, const
     int8_t* out = static_cast<int8_t*>(p.z) + row * p.ldz;
     int q[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = round_quotient(z.get(e), s);
+    for (int e = 0; e < 8; ++e) q[e] = round_quotient(z.v[e], s);
     if constexpr (WIDE) {
-        if (at.any()) *reinterpret_cast<uint2*>(out + at.first) = pack_bytes(q);
+        if (at.any) *reinterpret_cast<uint2*>(out + at.first) = pack_bytes(q);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) if (at.holds(e)) out[at.at(e)] = (int8_t)q[e];
@@ -53,31 +52,29 @@ __device__ __forceinline__ void store_z8(const NormParams& p, int64_t row, const
 
 template <typename TX, typename TB> struct NormRow { Raw8<TX> x; Raw8<TB> y, gate; };
 template <typename TX, typename TB, bool WIDE>
-__device__ __forceinline__ NormRow<TX, TB> load_norm_row(const NormParams& p, int64_t r, const Place<WIDE>& at) {
-    NormRow<TX, TB> v;
-    v.x = at.load(static_cast<const TX*>(p.x) + r * p.ldx, r < p.n);
-    if (p.y) v.y = at.load(static_cast<const TB*>(p.y) + r * p.ldy, r < p.n);
-    if (p.gate) v.gate = at.load(static_cast<const TB*>(p.gate) + r * p.ldg, r < p.n);
-    return v;
+__device__ __forceinline__ void load_norm_row(const NormParams& p, int64_t r, const Place<WIDE>& at, NormRow<TX, TB>& v) {
+    v.x = at.load(static_cast<const TX*>(p.x) + r * p.ldx);
+    if (p.y) v.y = at.load(static_cast<const TB*>(p.y) + r * p.ldy);
+    if (p.gate) v.gate = at.load(static_cast<const TB*>(p.gate) + r * p.ldg);
 }
 
-// Teams of L threads (L = 0: the CTA) take rows in turn, the next one's loads under way.
+// Teams of L threads (L = 0: the CTA) take rows in turn, the next one's loads under way.  (Teams that have run out of rows go along with the last one.)
 template <typename TX, typename TB, int L, bool WIDE>
 __global__ void __launch_bounds__(L == 0 ? NORM_MOST / 8 : NORM_THREADS, L == 0 ? 1 : NORM_CTAS) norm_kernel(const __grid_constant__ NormParams p) {
     __shared__ float parts[2][2][32];
-    Team<L> team{parts};
-    const int t = Team<L>::thread();
-    const Place<WIDE> row(Team<L>::size(), t, p.d);
+    Team<L> team(parts);
+    const int t = team.thread, last = p.n - 1;
+    const Place<WIDE> at(Team<L>::size(), t, p.d);
     const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
     grid_dependency_wait();
     allow_dependents();
-    NormRow<TX, TB> next = load_norm_row<TX, TB>(p, (int64_t)blockIdx.x * Team<L>::COUNT + Team<L>::index(), row);
+    NormRow<TX, TB> next;
+    load_norm_row<TX, TB>(p, min((int64_t)blockIdx.x * Team<L>::COUNT + team.index, (int64_t)last), at, next);
     for (int64_t r0 = (int64_t)blockIdx.x * Team<L>::COUNT; r0 < p.n; r0 += step) {
-        const int64_t r = r0 + Team<L>::index();
-        const bool live = r < p.n;
-        const Place<WIDE> at(Team<L>::size(), t, live ? p.d : 0);
+        const int64_t mine = r0 + team.index, r = min(mine, (int64_t)last);
+        const bool live = mine <= last;
         const NormRow<TX, TB> now = next;
-        if (r0 + step < p.n) next = load_norm_row<TX, TB>(p, r + step, row);
+        if (r0 + step < p.n) load_norm_row<TX, TB>(p, min(mine + step, (int64_t)last), at, next);
         float* const stats = p.stats && live && t == 0 ? p.stats + 4 * r : nullptr;
         F8 u = wide_of(now.x);
         float2 s = make_float2(0.f, 0.f);
@@ -88,9 +85,12 @@ __global__ void __launch_bounds__(L == 0 ? NORM_MOST / 8 : NORM_THREADS, L == 0 
                 a = a * s.y * at.vector(p.w1);
                 if (p.b1) a = a + at.vector(p.b1);
             }
-            if (p.gate) a = a * act_of(wide_of(now.gate), p.act);
+            if (p.gate) {
+                const F8 g = wide_of(now.gate);
+                a = a * (p.act == NORM_PLAIN ? g : act_with(g, sigmoid_of(g), p.act));
+            }
             u = p.scale ? fma8(a, at.vector(p.scale), u) : a + u;
-            if (p.h) at.store(static_cast<TX*>(p.h) + r * p.ldh, u);
+            if (p.h) at.store(static_cast<TX*>(p.h) + r * p.ldh, u, live);
         }
         if (stats) *reinterpret_cast<float2*>(stats) = s;
         s = make_float2(0.f, 0.f);
@@ -101,12 +101,12 @@ __global__ void __launch_bounds__(L == 0 ? NORM_MOST / 8 : NORM_THREADS, L == 0 
             if (p.z8) {
                 float most = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) most = Team<L>::template join<true>(most, fabsf(u.get(e)));
+                for (int e = 0; e < 8; ++e) if (at.holds(e)) most = Team<L>::template join<true>(most, fabsf(u.v[e]));
                 const RowScale q = row_scale(team.most(most));
                 if (live && t == 0) p.z_scales[r] = q.s;
-                store_z8(p, r, at, u, q);
+                if (live) store_z8(p, r, at, u, q);
             } else {
-                at.store(static_cast<TB*>(p.z) + r * p.ldz, u);
+                at.store(static_cast<TB*>(p.z) + r * p.ldz, u, live);
             }
         }
         if (stats) *reinterpret_cast<float2*>(stats + 2) = s;
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(L == 0 ? NORM_MOST / 8 : NORM_THREADS, L == 0 
 template <typename TX, typename TB>
 __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_loop_kernel(const __grid_constant__ NormParams p) {
     __shared__ float parts[2][2][32];
-    Team<0> team{parts};
+    Team<0> team(parts);
     const int64_t r = blockIdx.x;
     grid_dependency_wait();
     allow_dependents();

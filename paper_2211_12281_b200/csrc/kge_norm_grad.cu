@@ -39,32 +39,32 @@ inline int grad_ctas_of(int64_t n, int d) {
 
 template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y, gate, dz; float4 stats; };
 template <typename TX, typename TB, bool WIDE>
-__device__ __forceinline__ GradRow<TX, TB> load_grad_row(const NormGradParams& p, int64_t r, const Place<WIDE>& at) {
-    GradRow<TX, TB> v{};
-    const bool there = r < p.n;
-    if (p.dh) v.dh = at.load(static_cast<const TX*>(p.dh) + r * p.ldh, there);
+__device__ __forceinline__ void load_grad_row(const NormGradParams& p, int64_t r, const Place<WIDE>& at, GradRow<TX, TB>& v) {
+    if (p.dh) v.dh = at.load(static_cast<const TX*>(p.dh) + r * p.ldh);
     if (p.dz) {
-        v.dz = at.load(static_cast<const TB*>(p.dz) + r * p.ldz, there);
-        v.x = at.load(static_cast<const TX*>(p.x) + r * p.ldx, there);
+        v.dz = at.load(static_cast<const TB*>(p.dz) + r * p.ldz);
+        v.x = at.load(static_cast<const TX*>(p.x) + r * p.ldx);
     }
-    if (p.y) v.y = at.load(static_cast<const TB*>(p.y) + r * p.ldy, there);
-    if (p.gate) v.gate = at.load(static_cast<const TB*>(p.gate) + r * p.ldg, there);
-    if (there) v.stats = __ldg(reinterpret_cast<const float4*>(p.stats + 4 * r));
-    return v;
+    if (p.y) v.y = at.load(static_cast<const TB*>(p.y) + r * p.ldy);
+    if (p.gate) v.gate = at.load(static_cast<const TB*>(p.gate) + r * p.ldg);
+    v.stats = __ldg(reinterpret_cast<const float4*>(p.stats + 4 * r));
 }
 
 struct Sums { F8 t1, s1, t0, s0; };
 __device__ __forceinline__ const F8& sum_of(const Sums& s, int q) { return q == 0 ? s.t1 : (q == 1 ? s.s1 : (q == 2 ? s.t0 : s.s0)); }
 
-// One row of a team.
+// One row of a team (live: it is the team's own).
 template <typename TX, typename TB, int L, bool WIDE>
-__device__ __forceinline__ void grad_row(const NormGradParams& p, Team<L>& team, int64_t r, const Place<WIDE>& at, const GradRow<TX, TB>& v, Sums& sums) {
-    F8 dh = p.dh ? wide_of(v.dh) : all8(0.f), yn = all8(0.f), sigmoid = all8(0.f);
+__device__ __forceinline__ void grad_row(const NormGradParams& p, Team<L>& team, int64_t r, bool live, const Place<WIDE>& at, const GradRow<TX, TB>& v, Sums& sums) {
+    F8 dh = p.dh ? wide_of(v.dh) : all8(0.f), yn = all8(0.f), gate = all8(0.f), act = all8(1.f);
     if (p.y) {
         yn = wide_of(v.y);
-        if (p.post) yn = (yn + at.spread(-v.stats.x)) * v.stats.y;
+        if (p.post) yn = (yn + -v.stats.x) * v.stats.y;
     }
-    if (p.gate && p.act != NORM_PLAIN) sigmoid = each8(wide_of(v.gate), sigmoid_of);
+    if (p.gate) {
+        gate = wide_of(v.gate);
+        act = p.act == NORM_PLAIN ? gate : sigmoid_of(gate);          // (its sigmoid, where there is one)
+    }
     float mean = 0.f, along = 0.f;
     if (p.dz) {
         F8 h = wide_of(v.x);
@@ -72,64 +72,70 @@ __device__ __forceinline__ void grad_row(const NormGradParams& p, Team<L>& team,
             F8 a = yn;
             if (p.w1) a = a * at.vector(p.w1);
             if (p.b1) a = a + at.vector(p.b1);
-            if (p.gate) a = a * act_with(wide_of(v.gate), sigmoid, p.act);
+            if (p.gate) a = a * act_with(gate, act, p.act);
             h = p.scale ? fma8(a, at.vector(p.scale), h) : a + h;
         }
-        const F8 hn = (h + at.spread(-v.stats.z)) * v.stats.w, dz = wide_of(v.dz), c = dz * at.vector(p.w2);
-        sums.t1 = fma8(dz, hn, sums.t1);
-        sums.t0 = sums.t0 + dz;
-        along = dot(c, hn);
-        if (p.layer) { mean = total(c); team.sum(mean, along); }
+        const F8 hn = (h + -v.stats.z) * v.stats.w, dz = wide_of(v.dz), c = dz * at.vector(p.w2);
+        if (live) {
+            sums.t1 = fma8(dz, hn, sums.t1);
+            if (p.sums > 2) sums.t0 = sums.t0 + dz;
+        }
+        along = at.dot(c, hn);
+        if (p.layer) { mean = at.total(c); team.sum(mean, along); }
         else along = team.sum(along);
-        dh = fma8(fma8(hn, -along * p.inv_d, c + at.spread(-mean * p.inv_d)), v.stats.w, dh);
+        dh = fma8(fma8(hn, -along * p.inv_d, p.layer ? c + -mean * p.inv_d : c), v.stats.w, dh);
     }
-    if (p.dx) at.store(static_cast<TX*>(p.dx) + r * p.ldox, dh);
+    if (p.dx) at.store(static_cast<TX*>(p.dx) + r * p.ldox, dh, live);
     if (!p.y) return;
     F8 f = dh;
-    if (p.gate) f = f * act_with(wide_of(v.gate), sigmoid, p.act);
-    sums.s1 = fma8(f, yn, sums.s1);
-    sums.s0 = sums.s0 + f;
+    if (p.gate) f = f * act_with(gate, act, p.act);
+    if (live) {
+        sums.s1 = fma8(f, yn, sums.s1);
+        if (p.sums > 2) sums.s0 = sums.s0 + f;
+    }
     if (p.scale) {
         const F8 s = at.vector(p.scale);
         f = f * s;
         dh = dh * s;
     }
+    const F8 w1 = p.w1 ? at.vector(p.w1) : all8(1.f);
     if (p.dgate) {
         F8 a = yn;
-        if (p.w1) a = a * at.vector(p.w1);
+        if (p.w1) a = a * w1;
         if (p.b1) a = a + at.vector(p.b1);
-        at.store(static_cast<TB*>(p.dgate) + r * p.ldog, slope_with(wide_of(v.gate), sigmoid, p.act) * a * dh);
+        at.store(static_cast<TB*>(p.dgate) + r * p.ldog, slope_with(gate, act, p.act) * a * dh, live);
     }
     if (!p.dy) return;
     if (p.post) {
-        f = f * at.vector(p.w1);
-        along = dot(f, yn);
-        if (p.layer) { mean = total(f); team.sum(mean, along); }
-        else { along = team.sum(along); mean = 0.f; }
-        f = fma8(yn, -along * p.inv_d, f + at.spread(-mean * p.inv_d)) * v.stats.y;
+        f = f * w1;
+        along = at.dot(f, yn);
+        if (p.layer) { mean = at.total(f); team.sum(mean, along); }
+        else along = team.sum(along);
+        f = fma8(yn, -along * p.inv_d, p.layer ? f + -mean * p.inv_d : f) * v.stats.y;
     }
-    at.store(static_cast<TB*>(p.dy) + r * p.ldoy, f);
+    at.store(static_cast<TB*>(p.dy) + r * p.ldoy, f, live);
 }
 
-// Teams take rows in turn, the next one's loads under way, and add up the columns' sums of theirs in registers.
+// Teams take rows in turn, the next one's loads under way, and add up the columns' sums of theirs in registers.  (Teams that have run out of rows go along with
+// the last one.)
 template <typename TX, typename TB, int L, bool WIDE>
 __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
     __shared__ float parts[2][2][32];
     __shared__ float joined[L == 0 ? 1 : NORM_THREADS * 8];
-    Team<L> team{parts};
-    const int t = Team<L>::thread();
-    const Place<WIDE> row(Team<L>::size(), t, p.d);
+    Team<L> team(parts);
+    const int t = team.thread, last = p.n - 1;
+    const Place<WIDE> at(Team<L>::size(), t, p.d);
     const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
     grid_dependency_wait();
     allow_dependents();
     Sums sums{all8(0.f), all8(0.f), all8(0.f), all8(0.f)};
-    GradRow<TX, TB> next = load_grad_row<TX, TB>(p, (int64_t)blockIdx.x * Team<L>::COUNT + Team<L>::index(), row);
+    GradRow<TX, TB> next;
+    load_grad_row<TX, TB>(p, min((int64_t)blockIdx.x * Team<L>::COUNT + team.index, (int64_t)last), at, next);
     for (int64_t r0 = (int64_t)blockIdx.x * Team<L>::COUNT; r0 < p.n; r0 += step) {
-        const int64_t r = r0 + Team<L>::index();
-        const Place<WIDE> at(Team<L>::size(), t, r < p.n ? p.d : 0);
+        const int64_t mine = r0 + team.index;
         const GradRow<TX, TB> now = next;
-        if (r0 + step < p.n) next = load_grad_row<TX, TB>(p, r + step, row);
-        grad_row<TX, TB, L, WIDE>(p, team, r, at, now, sums);
+        if (r0 + step < p.n) load_grad_row<TX, TB>(p, min(mine + step, (int64_t)last), at, next);
+        grad_row<TX, TB, L, WIDE>(p, team, min(mine, (int64_t)last), mine <= last, at, now, sums);
     }
     if (p.sums == 0) return;
     float* part = p.part + (int64_t)blockIdx.x * p.sums * p.d;
@@ -137,14 +143,12 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
     for (int q = 0; q < 4; ++q) {
         if (q >= p.sums) break;
         if constexpr (L == 0) {
-            row.store(part + (int64_t)q * p.d, sum_of(sums, q));
+            at.store(part + (int64_t)q * p.d, sum_of(sums, q), true);
         } else {
             constexpr int WIDTH = L * 8;
             __syncthreads();
-            const Place<WIDE> at(L, t, WIDTH);
-            const Raw8<float> mine = narrow_of<float>(sum_of(sums, q));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) joined[Team<L>::index() * WIDTH + at.at(e)] = mine.v[e];       // (shared memory: no access by load_wide's kind)
+            for (int e = 0; e < 8; ++e) if (at.holds(e)) joined[team.index * WIDTH + at.at(e)] = sum_of(sums, q).v[e];
             __syncthreads();
             for (int i = threadIdx.x; i < p.d; i += NORM_THREADS) {
                 float v = joined[i];
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
 template <typename TX, typename TB>
 __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_grad_loop_kernel(const __grid_constant__ NormGradParams p) {
     __shared__ float parts[2][2][32];
-    Team<0> team{parts};
+    Team<0> team(parts);
     grid_dependency_wait();
     allow_dependents();
     float* part = p.part + (int64_t)blockIdx.x * p.sums * p.d;
@@ -232,26 +236,29 @@ struct NormJoinParams {
     float *dw1, *db1, *dscale, *dw2, *db2;
     int ctas, sums, d, accumulate;
 };
-constexpr int JOIN_COLS = 32, JOIN_ROWS = 8;
+constexpr int JOIN_COLS = 32, JOIN_ROWS = 32;
 __global__ void __launch_bounds__(JOIN_COLS * JOIN_ROWS) norm_join_kernel(const __grid_constant__ NormJoinParams p) {
     __shared__ float part[4][JOIN_ROWS][JOIN_COLS];
     grid_dependency_wait();
     allow_dependents();
-    const int c = blockIdx.x * JOIN_COLS + threadIdx.x % JOIN_COLS, row = threadIdx.x / JOIN_COLS;
+    const int col = threadIdx.x % JOIN_COLS, c = blockIdx.x * JOIN_COLS + col, row = threadIdx.x / JOIN_COLS;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < p.d) {
+#pragma unroll 4
         for (int g = row; g < p.ctas; g += JOIN_ROWS) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) if (q < p.sums) v[q] += p.part[((int64_t)g * p.sums + q) * p.d + c];
         }
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) part[q][row][threadIdx.x % JOIN_COLS] = v[q];
+    for (int q = 0; q < 4; ++q) part[q][row][col] = v[q];
     __syncthreads();
     if (row > 0 || c >= p.d) return;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-        for (int i = 1; i < JOIN_ROWS; ++i) v[q] += part[q][i][threadIdx.x];
+    for (int q = 0; q < 4; ++q) {
+#pragma unroll 8
+        for (int i = 1; i < JOIN_ROWS; ++i) v[q] += part[q][i][col];
+    }
     auto give = [&](float* to, float x) { if (to) to[c] = p.accumulate ? to[c] + x : x; };
     const float s = p.scale ? p.scale[c] : 1.f, w1 = p.w1 ? p.w1[c] : 1.f, b1 = p.b1 ? p.b1[c] : 0.f;
     give(p.dw2, v[0]);

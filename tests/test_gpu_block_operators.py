@@ -46,13 +46,16 @@ def _normed(c, r, rho):
 
 
 def _act64(T, g, kind):
-    """act(g) and its derivative, as Values (expf and the division within two units each: the sigmoid within 10 U of itself)."""
+    """act(g) and its derivative, as Values.  The exponent g log2 e of e = 2^(-g log2 e) is off by half a step of itself and the constant's half step: e by
+    2 U |g| ln 2 log2 e < 2 U |g| at most, the instruction adds 2^-22.5 < 3 U, the sum U, the reciprocal's unit 2 U; s = 1 / (1 + e) has the share e / (1 + e) < 1
+    of what e is off.  The derivative s (1 - s) is off by s's error twice and three roundings, (1 - s) of at most 1."""
     if kind == "plain":
         return Value(g, T.zeros_like(g)), Value(T.ones_like(g), T.zeros_like(g))
     s = 1 / (1 + T.exp(-g))
+    off = (6 + 2 * g.abs()) * U
     if kind == "sigmoid":
-        return Value(s, 10 * U * s), Value(s * (1 - s), 16 * U * s)
-    return Value(g * s, 11 * U * (g * s).abs()), Value(s * (1 + g * (1 - s)), 16 * U * (1 + g.abs()) * s)
+        return Value(s, off * s), Value(s * (1 - s), (2 * off + 3 * U) * s)
+    return Value(g * s, (off + U) * (g * s).abs()), Value(s * (1 + g * (1 - s)), (2 * off + 5 * U) * (1 + g.abs()) * s)
 
 
 def _block64(T, f, act, eps, layer, d):
