@@ -71,8 +71,8 @@ __global__ void __launch_bounds__(L == 0 ? NORM_MOST / 8 : NORM_THREADS, L == 0 
     NormRow<TX, TB> next;
     load_norm_row<TX, TB>(p, min((int64_t)blockIdx.x * Team<L>::COUNT + team.index, (int64_t)last), at, next);
     for (int64_t r0 = (int64_t)blockIdx.x * Team<L>::COUNT; r0 < p.n; r0 += step) {
-        const int64_t mine = r0 + team.index, r = min(mine, (int64_t)last);
-        const bool live = mine <= last;
+        const int64_t mine = r0 + team.index, r = L == 0 ? mine : min(mine, (int64_t)last);
+        const bool live = L == 0 || mine <= last;
         const NormRow<TX, TB> now = next;
         if (r0 + step < p.n) load_norm_row<TX, TB>(p, min(mine + step, (int64_t)last), at, next);
         float* const stats = p.stats && live && t == 0 ? p.stats + 4 * r : nullptr;

@@ -40,8 +40,12 @@ template <bool WIDE> struct Place {
     __device__ __forceinline__ int at(int e) const { return first + e * step; }
     __device__ __forceinline__ bool holds(int e) const { return WIDE ? any : at(e) < d; }
     __device__ __forceinline__ int near(int e) const { return WIDE ? at(e) : min(at(e), d - 1); }
+    // (the row's address is the same for a warp, and a thread's place in it takes 32 bits: one access, no arithmetic of 64 bits in every thread)
+    template <typename T> __device__ __forceinline__ T* mine(T* row) const {
+        return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (uint32_t)first * (uint32_t)sizeof(T));
+    }
     template <typename T> __device__ __forceinline__ Raw8<T> load(const T* row) const {
-        if constexpr (WIDE) return load_wide(row + first);
+        if constexpr (WIDE) return load_wide(mine(row));
         Raw8<T> r;
 #pragma unroll
         for (int e = 0; e < 8; ++e) set_element(r, e, row[near(e)]);
@@ -49,7 +53,7 @@ template <bool WIDE> struct Place {
     }
     template <typename T> __device__ __forceinline__ void store(T* row, const F8& x, bool live) const {
         const Raw8<T> r = narrow_of<T>(x);
-        if constexpr (WIDE) { if (any && live) store_wide(row + first, r); }
+        if constexpr (WIDE) { if (any && live) store_wide(mine(row), r); }
         else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) if (holds(e) && live) row[at(e)] = element(r, e);
@@ -58,7 +62,7 @@ template <bool WIDE> struct Place {
     // A vector of parameters.  (Loaded here, from the L1 cache: the compiler would keep all of them in registers, and spill others.)
     __device__ __forceinline__ F8 vector(const float* p) const {
         if constexpr (WIDE) {
-            const Pack<float, 8> v = load_now<Pack<float, 8>>(p + first);
+            const Pack<float, 8> v = load_now<Pack<float, 8>>(mine(p));
             return make8([&](int e) { return v.v[e]; });
         }
         return make8([&](int e) { return __ldg(p + near(e)); });
