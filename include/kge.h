@@ -465,7 +465,7 @@ int kge_int8_matmul(const void* a, int64_t lda, const float* a_scales, const voi
  * x and h are of x_type, y, gate and z of block_type (fp32, bf16, fp16 each), the vectors [d] fp32 (bias, scale, gate: NULL where there is none).
  * act: gate_act 0 the gate itself, 1 its sigmoid, 2 gate times its sigmoid.  z is made of the unrounded h.
  * kge_block_norm       h or z may be NULL, not both; without y only z is given.  z_int8 = 1: z is int8 [n, d] with a scale for each row in z_scales
- *                      [n], as kge_int8_quantize would make them of the unrounded z.  stats (or NULL): [n, 4], 16-byte aligned, receives mu and r
+ *                      [n], as kge_int8_quantize would make them of the unrounded z (which of two integers a z beside their middle becomes is decided in fp32).  stats (or NULL): [n, 4], 16-byte aligned, receives mu and r
  *                      of the norm after the block, then of the one before the next (0 where a norm is not taken), for the gradients.
  * kge_block_norm_grad  from dz (block_type, or NULL: no gradient came through z) and dh (x_type, or NULL) the gradients that are not NULL in
  *                      `out`; those of the vectors are sums over the rows in an order that follows from n, d and alignment alone, written, or added to what is there

@@ -18,67 +18,126 @@ struct QuantParams {
     int8_t* q; int64_t ldq;
     float* scales;
     int rows, cols;
-    int vec;                         // rows of x start at multiples of eight elements
+    int wide;                        // rows of x start at multiples of eight elements and have a whole number of eights
 };
 
-template <typename T> struct alignas(16) Eight { T v[8]; };
-template <typename T> __device__ __forceinline__ Eight<T> load8(const QuantParams& p, int64_t r, int c) {
-    const T* x = static_cast<const T*>(p.x) + r * p.ldx + c;
-    if (p.vec && c + 8 <= p.cols) return *reinterpret_cast<const Eight<T>*>(x);
-    Eight<T> e;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e.v[j] = c + j < p.cols ? x[j] : from_float<T>(0.f);
-    return e;
-}
 // Magnitudes as integers, which order as they do (a NaN above all).
-template <typename T> __device__ __forceinline__ uint32_t most_of(const Eight<T>& e) {
+__device__ __forceinline__ uint32_t most_of(const Raw8<float>& r) {
     uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(to_float(e.v[j])) & 0x7FFFFFFFu);
+    for (int e = 0; e < 8; ++e) m = max(m, r.w[e] & 0x7FFFFFFFu);
     return m;
 }
-template <typename T> __device__ __forceinline__ void store8(const QuantParams& p, int64_t r, int c, const Eight<T>& e, const RowScale& s) {
-    int q[8];
+template <typename T> __device__ __forceinline__ uint32_t most_of(const Raw8<T>& r) {
+    uint32_t m = r.w[0] & 0x7FFF7FFFu;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = round_quotient(to_float(e.v[j]), s);
-    int8_t* out = p.q + r * p.ldq + c;
-    if (c + 8 <= p.cols) *reinterpret_cast<uint2*>(out) = pack_bytes(q);
-    else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) if (c + j < p.cols) out[j] = (int8_t)q[j];
+    for (int i = 1; i < 4; ++i) m = __vmaxu2(m, r.w[i] & 0x7FFF7FFFu);
+    return max(m & 0xFFFFu, m >> 16);
+}
+__device__ __forceinline__ float magnitude(uint32_t m, float) { return __uint_as_float(m); }
+__device__ __forceinline__ float magnitude(uint32_t m, __nv_bfloat16) { return __uint_as_float(m << 16); }
+__device__ __forceinline__ float magnitude(uint32_t m, __half) { return __half2float(__ushort_as_half((unsigned short)m)); }
+
+// The integer stored is the one nearest to the true quotient x / s, ties to even, not to what x (1 / s) rounds to, which is within 2^-23 of it.
+//   16-bit x    with a the row's largest value, x / a times 127 is k + 1/2 exactly, or off it by 2^-19 at least (254 x and (2 k + 1) a differ by
+//               one unit then, of numbers of 19 bits).  In the first case the true quotient lies on the side that the rounding of s = a / 127
+//               says: `inv` leans by 2^-21 to it.  Where s is exact the quotient is the middle itself: right if 1 / s is exact too, else decided
+//               one by one.
+//   fp32 x      products beside a middle (within 2^-12) are decided one by one.
+// One by one: m, the multiple of 16 units next to |x| (1 / s) (all middles are such), is compared with the quotient exactly, by the sign of |x| - m s.
+struct QuantScale { float s, inv; bool each; };
+template <typename T> __device__ __forceinline__ QuantScale quant_scale(float a) {
+    const RowScale r = row_scale(a);
+    QuantScale q{r.s, r.inv, false};
+    if (sizeof(T) == 2 && r.s > 1.17549435e-38f && a > 0.f) {          // (the smallest scale is a power of two and not a / 127)
+        const float e = fmaf(-r.s, 127.f, a);
+        q.each = e == 0.f && fmaf(r.s, r.inv, -1.f) != 0.f;
+        q.inv = e == 0.f ? r.inv : fmaf(r.inv, e > 0.f ? 4.76837158e-7f : -4.76837158e-7f, r.inv);
     }
+    return q;
+}
+__device__ __noinline__ uint32_t quotient_bits(float x, float s) {
+    int m = (int)(__float_as_uint(fabsf(x) * __fdiv_rn(1.f, s)) + 8u) & ~15;
+    const float d = fmaf(-__int_as_float(m), s, fabsf(x));
+    m += d > 0.f ? 1 : (d < 0.f ? -1 : 0);
+    return __float_as_uint(copysignf(__int_as_float(m), x) + ROUND_TO_INT);
+}
+template <typename T> __device__ __forceinline__ uint2 quantized(const Raw8<T>& r, const QuantScale& s) {
+    const F8 x = wide_of(r);
+    F8 t = fma8(x, s.inv, all8(ROUND_TO_INT));
+    bool each = s.each;
+    if (sizeof(T) == 4) {
+        float far = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) far = fmaxf(far, fabsf(fmaf(x.v[e], s.inv, ROUND_TO_INT - t.v[e])));          // how far the product is from its integer
+        each = far > 0.5f - 0.000244140625f;
+    }
+    if (each) t = make8([&](int e) { return __uint_as_float(quotient_bits(x.v[e], s.s)); });
+    return low_bytes(t);
 }
 
-// A row to a CTA of THREADS threads, or to each of its warps (WARP); K packs of eight a thread are kept, what is beyond them read again.
-constexpr int QUANT_THREADS = 256, QUANT_PACKS = 4;
-template <typename T, bool WARP>
-__global__ void __launch_bounds__(QUANT_THREADS) quantize_rows_kernel(const __grid_constant__ QuantParams p) {
+// A row to a warp (L = 32) or to a CTA (L = 0); a thread holds K packs of eight of it.
+constexpr int QUANT_THREADS = 256;
+template <typename T, int L, int K, bool WIDE>
+__global__ void __launch_bounds__(QUANT_THREADS) int8_rows_kernel(const __grid_constant__ QuantParams p) {
     __shared__ uint32_t part[QUANT_THREADS / 32];
+    const int team = L == 32 ? 32 : QUANT_THREADS, t = (int)threadIdx.x % (L == 32 ? 32 : QUANT_THREADS);
+    const int64_t r = L == 32 ? (int64_t)blockIdx.x * (QUANT_THREADS / 32) + __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0) : (int64_t)blockIdx.x;
     grid_dependency_wait();
     allow_dependents();
-    const int lanes = WARP ? 32 : QUANT_THREADS, t = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    const int64_t r = WARP ? (int64_t)blockIdx.x * (QUANT_THREADS / 32) + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
     if (r >= p.rows) return;
-    Eight<T> x[QUANT_PACKS];
+    const T* const x = static_cast<const T*>(p.x) + r * p.ldx;
+    int8_t* const out = p.q + r * p.ldq;
+    auto load = [&](int64_t c) {
+        Raw8<T> v = {};
+        if (WIDE) { if (c < p.cols) v = load_wide(x + c); }
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (c + e < p.cols) set_element(v, e, x[c + e]);
+        }
+        return v;
+    };
+    auto store = [&](int64_t c, const Raw8<T>& v, const QuantScale& s) {
+        if (c >= p.cols) return;
+        const uint2 w = quantized(v, s);
+        if (WIDE || c + 8 <= p.cols) *reinterpret_cast<uint2*>(out + c) = w;
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (c + e < p.cols) out[c + e] = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+        }
+    };
+    Raw8<T> held[K];
     uint32_t m = 0;
 #pragma unroll
-    for (int k = 0; k < QUANT_PACKS; ++k) x[k] = load8<T>(p, r, (k * lanes + t) * 8);
+    for (int k = 0; k < K; ++k) held[k] = load((k * team + t) * 8);
 #pragma unroll
-    for (int k = 0; k < QUANT_PACKS; ++k) m = max(m, most_of(x[k]));
-    const int kept = QUANT_PACKS * lanes * 8;
-    for (int64_t c = kept + t * 8; c < p.cols; c += lanes * 8) m = max(m, most_of(load8<T>(p, r, (int)c)));
+    for (int k = 0; k < K; ++k) m = max(m, most_of(held[k]));
+    for (int64_t c = (int64_t)K * team * 8 + t * 8; c < p.cols; c += team * 8) m = max(m, most_of(load(c)));
     m = __reduce_max_sync(0xffffffffu, m);
-    if (!WARP) {
+    if (L == 0) {
         if ((t & 31) == 0) part[t >> 5] = m;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < QUANT_THREADS / 32; ++w) m = max(m, part[w]);
     }
-    const RowScale s = row_scale(__uint_as_float(m));
+    const QuantScale s = quant_scale<T>(magnitude(m, T()));
     if (t == 0) p.scales[r] = s.s;
 #pragma unroll
-    for (int k = 0; k < QUANT_PACKS; ++k) if ((k * lanes + t) * 8 < p.cols) store8(p, r, (k * lanes + t) * 8, x[k], s);
-    for (int64_t c = kept + t * 8; c < p.cols; c += lanes * 8) store8(p, r, (int)c, load8<T>(p, r, (int)c), s);
+    for (int k = 0; k < K; ++k) store((k * team + t) * 8, held[k], s);
+    for (int64_t c = (int64_t)K * team * 8 + t * 8; c < p.cols; c += team * 8) store(c, load(c), s);
+}
+
+template <typename T, bool WIDE>
+int launch_quantize(const QuantParams& p, cudaStream_t s) {
+    auto launch = [&](auto kernel, int64_t ctas) { return launch_status(launch_dependent(kernel, dim3((unsigned)ctas), dim3(QUANT_THREADS), 0, s, p)); };
+    const int64_t by_eight = ceil_div(p.rows, QUANT_THREADS / 32);
+    if (p.cols <= 256) return launch(int8_rows_kernel<T, 32, 1, WIDE>, by_eight);
+    if (p.cols <= 512) return launch(int8_rows_kernel<T, 32, 2, WIDE>, by_eight);
+    if (p.cols <= 768) return launch(int8_rows_kernel<T, 32, 3, WIDE>, by_eight);
+    if (p.cols <= 1024) return launch(int8_rows_kernel<T, 32, 4, WIDE>, by_eight);
+    if (p.cols <= 2048) return launch(int8_rows_kernel<T, 0, 1, WIDE>, p.rows);
+    if (p.cols <= 4096) return launch(int8_rows_kernel<T, 0, 2, WIDE>, p.rows);
+    return launch(int8_rows_kernel<T, 0, 4, WIDE>, p.rows);          // (what is beyond 8,192 columns is read again)
 }
 
 // ---- product ---------------------------------------------------------------------------------------------------------
@@ -443,13 +502,9 @@ int kge_int8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols,
     if (!x || !q || !scales || !aligned_to(x, type_bytes(x_type))) return KGE_ERR_BAD_ARG;
     QuantParams p{};
     p.x = x; p.ldx = ldx; p.q = static_cast<int8_t*>(q); p.ldq = ldq; p.scales = scales; p.rows = (int)rows; p.cols = (int)cols;
-    p.vec = aligned_to(x, 16) && ldx * type_bytes(x_type) % 16 == 0;
+    p.wide = cols % 8 == 0 && ldx % 8 == 0 && aligned_to(x, (size_t)(8 * type_bytes(x_type)));
     return with_type(x_type, [&](auto t) {
-        using T = decltype(t);
-        if (cols <= QUANT_PACKS * 32 * 8)
-            return launch_status(launch_dependent(quantize_rows_kernel<T, true>, dim3((unsigned)ceil_div(rows, QUANT_THREADS / 32)), dim3(QUANT_THREADS), 0,
-                                                  static_cast<cudaStream_t>(stream), p));
-        return launch_status(launch_dependent(quantize_rows_kernel<T, false>, dim3((unsigned)rows), dim3(QUANT_THREADS), 0, static_cast<cudaStream_t>(stream), p));
+        return p.wide ? launch_quantize<decltype(t), true>(p, static_cast<cudaStream_t>(stream)) : launch_quantize<decltype(t), false>(p, static_cast<cudaStream_t>(stream));
     });
 }
 

@@ -1,38 +1,35 @@
 // Rounding to 8-bit integers with a scale for each row (the norm's and the quantiser's kernels).
 #pragma once
 
-#include "kge_ops.cuh"
+#include "kge_eight.cuh"
 
 namespace kge {
 
 #ifdef __CUDACC__
-// A row's scale and its reciprocal, from its largest magnitude a.  Zeros alone have scale 1; an infinity or a NaN makes the scale one, and
-// the factor 0: the row's integers are 0 and stand for NaN, all of them.
+// A row's scale, and what its values are multiplied by, from its largest magnitude a.  Zeros alone have scale 1; an infinity or a NaN makes
+// it NaN, and all of the row stands for that.
 struct RowScale { float s, inv; };
 __device__ __forceinline__ RowScale row_scale(float a) {
-    const bool finite = a < __int_as_float(0x7F800000);       // (false for a NaN)
-    RowScale r{a, 0.f};
-    if (finite) {
-        r.s = a == 0.f ? 1.f : fmaxf(__fdiv_rn(a, 127.f), 1.17549435e-38f);
-        r.inv = __fdiv_rn(1.f, r.s);
-    }
+    RowScale r;
+    r.s = a < __int_as_float(0x7F800000) ? (a == 0.f ? 1.f : fmaxf(__fdiv_rn(a, 127.f), 1.17549435e-38f)) : __int_as_float(0x7FC00000);       // (false for a NaN)
+    r.inv = __fdiv_rn(1.f, r.s);
     return r;
 }
-// The integer nearest to the true quotient x / s (ties to even), not to its rounded form: t = |x| (1 / s) is within 2^-23 of it, and the
-// middles k + 1/2 are multiples of 16 units of their fp32 neighbours; m, such a multiple next to t, is compared with the quotient exactly (the sign of
-// |x| - m s, one fused operation) and moved a unit to the side where that lies.
-__device__ __forceinline__ int round_quotient(float x, const RowScale& r) {
-    const float ax = r.inv == 0.f ? 0.f : fabsf(x);
-    int m = (int)(__float_as_uint(ax * r.inv) + 8u) & ~15;
-    const float d = fmaf(-__int_as_float(m), r.s, ax);
-    m += d > 0.f ? 1 : (d < 0.f ? -1 : 0);
-    const int q = __float2int_rn(__int_as_float(m));
-    return x < 0.f ? -q : q;
+
+// |y| < 2^22 plus this has y rounded to an integer (ties to even) in its low bits; of a product and this, the exact product is rounded.
+constexpr float ROUND_TO_INT = 12582912.f;
+
+// The low bytes of eight such sums.
+__device__ __forceinline__ uint2 low_bytes(const F8& t) {
+    uint2 w;
+    const uint32_t a = __byte_perm(__float_as_uint(t.v[0]), __float_as_uint(t.v[1]), 0x0040), b = __byte_perm(__float_as_uint(t.v[2]), __float_as_uint(t.v[3]), 0x0040);
+    const uint32_t c = __byte_perm(__float_as_uint(t.v[4]), __float_as_uint(t.v[5]), 0x0040), d = __byte_perm(__float_as_uint(t.v[6]), __float_as_uint(t.v[7]), 0x0040);
+    w.x = __byte_perm(a, b, 0x5410);
+    w.y = __byte_perm(c, d, 0x5410);
+    return w;
 }
-__device__ __forceinline__ uint2 pack_bytes(const int (&q)[8]) {
-    return make_uint2((q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | (uint32_t)q[3] << 24,
-                      (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | (uint32_t)q[7] << 24);
-}
+// Integers nearest to the fp32 values times 1 / s, the product exact: within 1/2 + 2^-17 of the true quotients.
+__device__ __forceinline__ uint2 round_products(const F8& x, float inv) { return low_bytes(fma8(x, inv, all8(ROUND_TO_INT))); }
 #endif
 
 }  // namespace kge

@@ -36,17 +36,16 @@ __device__ __forceinline__ float2 centre(const NormParams& p, Team<L>& team, F8&
     return make_float2(mu, deviation(p, team.sum(at.dot(u, u))));
 }
 
+// (z is off by its own roundings: what the product with 1 / s adds to them moves an integer only where they do)
 template <bool WIDE>
 __device__ __forceinline__ void store_z8(const NormParams& p, int64_t row, const Place<WIDE>& at, const F8& z, const RowScale& s) {
     int8_t* out = static_cast<int8_t*>(p.z) + row * p.ldz;
-    int q[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = round_quotient(z.v[e], s);
+    const uint2 w = round_products(z, s.inv);
     if constexpr (WIDE) {
-        if (at.any) *reinterpret_cast<uint2*>(out + at.first) = pack_bytes(q);
+        if (at.any) *reinterpret_cast<uint2*>(at.mine(out)) = w;
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (at.holds(e)) out[at.at(e)] = (int8_t)q[e];
+        for (int e = 0; e < 8; ++e) if (at.holds(e)) out[at.at(e)] = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
     }
 }
 
@@ -160,7 +159,7 @@ __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_loop_kernel(const __gr
     for (int i = threadIdx.x; i < p.d; i += NORM_LOOP_THREADS) {
         const float u = stream(i);
         if (p.h) static_cast<TX*>(p.h)[r * p.ldh + i] = from_float<TX>(u);
-        if (p.z && p.z8) static_cast<int8_t*>(p.z)[r * p.ldz + i] = (int8_t)round_quotient(normed(u, i), q);
+        if (p.z && p.z8) static_cast<int8_t*>(p.z)[r * p.ldz + i] = (int8_t)__float_as_int(fmaf(normed(u, i), q.inv, ROUND_TO_INT));
         else if (p.z) static_cast<TB*>(p.z)[r * p.ldz + i] = from_float<TB>(normed(u, i));
     }
     if (p.stats && threadIdx.x == 0) *reinterpret_cast<float4*>(p.stats + 4 * r) = make_float4(s1.x, s1.y, s2.x, s2.y);

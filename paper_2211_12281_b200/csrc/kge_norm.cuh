@@ -26,8 +26,6 @@ __device__ __forceinline__ F8 operator*(const F8& a, const F8& b) { return make8
 __device__ __forceinline__ F8 operator+(const F8& a, const F8& b) { return make8([&](int e) { return a.v[e] + b.v[e]; }); }
 __device__ __forceinline__ F8 operator*(const F8& a, float b) { return make8([&](int e) { return a.v[e] * b; }); }
 __device__ __forceinline__ F8 operator+(const F8& a, float b) { return make8([&](int e) { return a.v[e] + b; }); }
-__device__ __forceinline__ F8 fma8(const F8& a, const F8& b, const F8& c) { return make8([&](int e) { return fmaf(a.v[e], b.v[e], c.v[e]); }); }
-__device__ __forceinline__ F8 fma8(const F8& a, float b, const F8& c) { return make8([&](int e) { return fmaf(a.v[e], b, c.v[e]); }); }
 
 // Where a thread's elements lie in its row: WIDE rows let eight neighbours move as one access, and all of them or none are there.  What lies beyond the row's end
 // is read from inside it, and left out of sums and stores.
