@@ -32,7 +32,9 @@ __device__ __forceinline__ F8 operator+(const F8& a, float b) { return make8([&]
 template <bool WIDE> struct Place {
     int first, step, d;
     bool any;
-    __device__ __forceinline__ Place(int team, int t, int width) : first(WIDE ? t * 8 : t), step(WIDE ? 1 : team), d(width), any(first < width) {
+    Place() = default;
+    __device__ __forceinline__ Place(int team, int t, int k, int width)
+        : first(WIDE ? (k * team + t) * 8 : k * team * 8 + t), step(WIDE ? 1 : team), d(width), any(first < width) {
         if (WIDE && !any) first = 0;
     }
     __device__ __forceinline__ int at(int e) const { return first + e * step; }

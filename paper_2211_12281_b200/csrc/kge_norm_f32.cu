@@ -1,0 +1,10 @@
+// The norms' forward kernels for fp32 rows of the residual stream.
+#include "kge_norm_forward.cuh"
+
+namespace kge {
+
+int launch_norm_f32(const NormParams& p, int block_type, cudaStream_t s) {
+    return with_type(block_type, [&](auto tb) { return launch_norm<float, decltype(tb)>(p, s); });
+}
+
+}  // namespace kge

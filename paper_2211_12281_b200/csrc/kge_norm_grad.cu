@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
     __shared__ float joined[L == 0 ? 1 : NORM_THREADS * 8];
     Team<L> team(parts);
     const int t = team.thread, last = p.n - 1;
-    const Place<WIDE> at(Team<L>::size(), t, p.d);
+    const Place<WIDE> at(Team<L>::size(), t, 0, p.d);
     const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
     grid_dependency_wait();
     allow_dependents();
