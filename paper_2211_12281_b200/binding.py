@@ -8,6 +8,7 @@ if the shared library is missing or cannot be loaded, importing the symbols rais
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from pathlib import Path
 
 _PKG = Path(__file__).resolve().parent
@@ -65,17 +66,9 @@ class KgeConfig(C.Structure):
                    lr, beta1, beta2, eps, seed, reg_lambda, reg_form, feat_dim, feat_shared)
 
 
-class KgeNormBlock(C.Structure):
-    """Mirror of ``kge_norm_block``."""
-    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("gate", C.c_void_p), ("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("scale", C.c_void_p),
-                ("pre_weight", C.c_void_p), ("pre_bias", C.c_void_p), ("ldx", C.c_int64), ("ldy", C.c_int64), ("ld_gate", C.c_int64),
-                ("x_type", C.c_int32), ("block_type", C.c_int32), ("gate_act", C.c_int32), ("layer", C.c_int32)]
-
-
-class KgeNormGrads(C.Structure):
-    """Mirror of ``kge_norm_grads``."""
-    _fields_ = [("dx", C.c_void_p), ("dy", C.c_void_p), ("dgate", C.c_void_p), ("dpost_weight", C.c_void_p), ("dpost_bias", C.c_void_p), ("dscale", C.c_void_p),
-                ("dpre_weight", C.c_void_p), ("dpre_bias", C.c_void_p), ("ld_dx", C.c_int64), ("ld_dy", C.c_int64), ("ld_dgate", C.c_int64)]
+# kge_norm_block and kge_norm_grads, packed (a ctypes structure takes five times as long to fill, a microsecond of a call of nine)
+KGE_NORM_BLOCK = struct.Struct("8Q3q4i")      # x, y, gate, post_weight, post_bias, scale, pre_weight, pre_bias; ldx, ldy, ld_gate; x_type, block_type, gate_act, layer
+KGE_NORM_GRADS = struct.Struct("8Q3q")        # dx, dy, dgate, dpost_weight, dpost_bias, dscale, dpre_weight, dpre_bias; ld_dx, ld_dy, ld_dgate
 
 
 class KgeAdamwTensor(C.Structure):
@@ -143,9 +136,9 @@ SIGNATURES = {
                                  C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, _vp, _vp]),
     "kge_int8_quantize": (C.c_int, [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int64, _vp, _vp]),
     "kge_int8_matmul": (C.c_int, [_vp, C.c_int64, _vp, _vp, C.c_int64, _vp, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_int64, _vp, _vp]),
-    "kge_block_norm": (C.c_int, [C.POINTER(KgeNormBlock), C.c_int64, C.c_int32, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, _vp, C.c_float, _vp, _vp]),
+    "kge_block_norm": (C.c_int, [_vp, C.c_int64, C.c_int32, _vp, C.c_int64, _vp, C.c_int32, C.c_int64, _vp, C.c_float, _vp, _vp]),
     "kge_block_norm_grad_scratch_bytes": (C.c_size_t, [C.c_int64, C.c_int32]),
-    "kge_block_norm_grad": (C.c_int, [C.POINTER(KgeNormBlock), C.c_int64, C.c_int32, _vp, _vp, C.c_int64, _vp, C.c_int64, C.POINTER(KgeNormGrads), C.c_int32,
+    "kge_block_norm_grad": (C.c_int, [_vp, C.c_int64, C.c_int32, _vp, _vp, C.c_int64, _vp, C.c_int64, _vp, C.c_int32,
                                       _vp, C.c_size_t, _vp]),
     "kge_adamw": (C.c_int, [_vp, C.c_int32, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, C.c_uint64, _vp, _vp, _vp, C.c_uint64, _vp]),
     "kge_get_status": (C.c_int, [_vp, _vp]),
@@ -441,11 +434,9 @@ def _int8_operand(q, scales, where, name):
     if q.dtype is not _torch.int8:
         raise _bad(where, f"{name} has type {q.dtype}")
     rows, k, ld = _matrix(q, where, name)
-    if rows <= 1:
-        ld = (ld + 15) // 16 * 16
-    if scales is None or scales.dtype is not _torch.float32 or not scales.is_contiguous() or scales.dim() != 1 or scales.shape[0] != rows:
+    if scales is None or scales.dtype is not _torch.float32 or scales.shape != (rows,) or not scales.is_contiguous():
         raise _bad(where, f"the scales of {name} are not a contiguous float32 list of its {rows} rows")
-    return rows, k, ld
+    return rows, k, ld if rows > 1 else (ld + 15) // 16 * 16
 
 
 def int8_quantize(x, q, scales):
@@ -480,38 +471,43 @@ _GATE_ACTS = {"plain": 0, "sigmoid": 1, "silu": 2}
 _NORM_KINDS = {"rms": 0, "layer": 1}
 
 
-def _norm_block(w, x, block, y, gate, gate_act, vectors, kind):
-    """(kge_norm_block, rows, columns) of the operands: block is a tensor that says what type y, gate and z are of; vectors by their field's name."""
-    b = KgeNormBlock()
-    n, d, b.ldx = _matrix(x, w, "x")
-    b.x_type, b.block_type, b.x = _type_of(x, w, "x", _FLOAT), _type_of(block, w, "y, gate, z or dz", _FLOAT), x.data_ptr()
-    for name, t, field in (("y", y, "ldy"), ("gate", gate, "ld_gate")):
-        if t is None:
-            continue
-        rows, cols, ld = _matrix(t, w, name)
-        if rows != n or cols != d or t.dtype is not block.dtype:
-            raise _bad(w, f"{name} has another shape than x or another type than the block's other tensors")
-        setattr(b, name, t.data_ptr())
-        setattr(b, field, ld)
-    for name, v in vectors.items():
-        if v is not None:
-            _vector(v, d, w, name)
-            setattr(b, name, v.data_ptr())
-    if gate_act not in _GATE_ACTS or kind not in _NORM_KINDS:
+def _like(t, shape, dtype, where, name):
+    """Distance of rows of a matrix of the shape and type given."""
+    stride = t.stride()
+    if t.shape != shape or t.dtype is not dtype or (stride[1] != 1 and shape[1] > 1) or (stride[0] < shape[1] and shape[0] > 1):
+        raise _bad(where, f"{name} is not a {list(shape)} matrix of contiguous rows and of type {dtype}")
+    return stride[0] if stride[0] > shape[1] else shape[1]
+
+
+def _vector(v, d, where, name):
+    """Address of a vector of parameters, 0 for None."""
+    if v is None:
+        return 0
+    if v.dtype is not _torch.float32 or v.shape != (d,) or not v.is_contiguous():
+        raise _bad(where, f"{name} is not a contiguous float32 vector of {d}")
+    return v.data_ptr()
+
+
+def _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, pre_bias, kind):
+    """(kge_norm_block, shape) of the operands: block is a tensor that says what type y, gate and z are of."""
+    n, d, ldx = _matrix(x, w, "x")
+    shape = x.shape
+    tx, tb = _type_of(x, w, "x", _FLOAT), _type_of(block, w, "y, gate, z or dz", _FLOAT)
+    act, layer = _GATE_ACTS.get(gate_act), _NORM_KINDS.get(kind)
+    if act is None or layer is None:
         raise _bad(w, f"gate_act is one of {list(_GATE_ACTS)}, kind one of {list(_NORM_KINDS)}")
-    b.gate_act, b.layer = _GATE_ACTS[gate_act], _NORM_KINDS[kind]
-    return b, n, _int32(d, w, "width")
-
-
-def _vector(v, d, w, name):
-    if v.dtype is not _torch.float32 or v.dim() != 1 or v.shape[0] != d or not v.is_contiguous():
-        raise _bad(w, f"{name} is not a contiguous float32 vector of {d}")
+    return KGE_NORM_BLOCK.pack(x.data_ptr(), 0 if y is None else y.data_ptr(), 0 if gate is None else gate.data_ptr(), _vector(post_weight, d, w, "post_weight"), _vector(post_bias, d, w, "post_bias"),
+                               _vector(scale, d, w, "scale"), _vector(pre_weight, d, w, "pre_weight"), _vector(pre_bias, d, w, "pre_bias"), ldx,
+                               0 if y is None else _like(y, shape, block.dtype, w, "y"), 0 if gate is None else _like(gate, shape, block.dtype, w, "gate"),
+                               tx, tb, act, layer), shape, n, _int32(d, w, "width")
 
 
 def _stats_of(stats, n, w):
-    if stats is not None and (stats.dtype is not _torch.float32 or tuple(stats.shape) != (n, 4) or not stats.is_contiguous()):
+    if stats is None:
+        return None
+    if stats.dtype is not _torch.float32 or stats.shape != (n, 4) or not stats.is_contiguous():
         raise _bad(w, f"stats is not a contiguous float32 matrix [{n}, 4]")
-    return _addr(stats)
+    return stats.data_ptr()
 
 
 def block_norm(x, z=None, pre_weight=None, pre_bias=None, y=None, h=None, gate=None, gate_act="plain", post_weight=None, post_bias=None, scale=None, kind="rms",
@@ -526,22 +522,19 @@ def block_norm(x, z=None, pre_weight=None, pre_bias=None, y=None, h=None, gate=N
         _load_torch()
     z8 = z is not None and z.dtype is _torch.int8
     block = y if y is not None else (x if z8 or z is None else z)
-    b, n, d = _norm_block(w, x, block, y, gate, gate_act, dict(post_weight=post_weight, post_bias=post_bias, scale=scale, pre_weight=pre_weight, pre_bias=pre_bias), kind)
-    ldh = ldz = 0
-    if h is not None:
-        hr, hd, ldh = _matrix(h, w, "h")
-        if hr != n or hd != d or h.dtype is not x.dtype:
-            raise _bad(w, "h is not of x's shape and type")
+    b, shape, n, d = _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, pre_bias, kind)
+    ldh = 0 if h is None else _like(h, shape, x.dtype, w, "h")
+    ldz = 0
     if z8:
-        zr, zd, ldz = _int8_operand(z, z_scales, w, "z")
+        _, _, ldz = _int8_operand(z, z_scales, w, "z")
+        if z.shape != shape:
+            raise _bad(w, "z is not of x's shape")
     elif z is not None:
-        zr, zd, ldz = _matrix(z, w, "z")
-        if z.dtype is not block.dtype or z_scales is not None:
-            raise _bad(w, "z is not of y's type, or scales are given for a z that is not int8")
-    if z is not None and (zr != n or zd != d):
-        raise _bad(w, "z is not of x's shape")
+        ldz = _like(z, shape, block.dtype, w, "z")
+        if z_scales is not None:
+            raise _bad(w, "scales are given for a z that is not int8")
     at = _stats_of(stats, n, w)
-    dev = _device_of(w, x, y, gate, h, z, post_weight, post_bias, scale, pre_weight, pre_bias, stats, z_scales)
+    dev = _device_of(w, x, *[t for t in (y, gate, h, z, post_weight, post_bias, scale, pre_weight, pre_bias, stats, z_scales) if t is not None])
     _call(w, lib().kge_block_norm, dev, b, n, d, _addr(h), ldh, _addr(z), 1 if z8 else 0, ldz, _addr(z_scales), eps, at)
 
 
@@ -556,29 +549,22 @@ def block_norm_grad(x, stats, dx=None, dz=None, dh=None, pre_weight=None, dpre_w
     """kge_block_norm_grad: the gradients of block_norm's operands from dz (of z's type, or None) and dh (of h's, or None), those that are given; dx, dy, dgate of their operands' types,
     the vectors' float32, written or (accumulate) added to what is there.  x, y, gate and the vectors are the forward call's, stats what it left."""
     w = "kge_block_norm_grad"
+    if _torch is None:
+        _load_torch()
     block = y if y is not None else (dz if dz is not None else x)
-    b, n, d = _norm_block(w, x, block, y, gate, gate_act, dict(post_weight=post_weight, post_bias=post_bias, scale=scale, pre_weight=pre_weight), kind)
-    ld = {}
-    for name, t, like in (("dz", dz, block), ("dh", dh, x), ("dx", dx, x), ("dy", dy, block), ("dgate", dgate, block)):
-        if t is None:
-            ld[name] = 0
-            continue
-        rows, cols, ld[name] = _matrix(t, w, name)
-        if rows != n or cols != d or t.dtype is not like.dtype:
-            raise _bad(w, f"{name} has another shape than x or another type than its operand")
-    o, wanted = KgeNormGrads(), False
-    o.dx, o.dy, o.dgate, o.ld_dx, o.ld_dy, o.ld_dgate = _addr(dx), _addr(dy), _addr(dgate), ld["dx"], ld["dy"], ld["dgate"]
-    for name, v in (("dpost_weight", dpost_weight), ("dpost_bias", dpost_bias), ("dscale", dscale), ("dpre_weight", dpre_weight), ("dpre_bias", dpre_bias)):
-        if v is not None:
-            _vector(v, d, w, name)
-            setattr(o, name, v.data_ptr())
-            wanted = True
+    b, shape, n, d = _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, None, kind)
+    ld = lambda t, like, name: 0 if t is None else _like(t, shape, like.dtype, w, name)
+    o = KGE_NORM_GRADS.pack(_addr(dx) or 0, _addr(dy) or 0, _addr(dgate) or 0, _vector(dpost_weight, d, w, "dpost_weight"), _vector(dpost_bias, d, w, "dpost_bias"), _vector(dscale, d, w, "dscale"),
+                            _vector(dpre_weight, d, w, "dpre_weight"), _vector(dpre_bias, d, w, "dpre_bias"), ld(dx, x, "dx"), ld(dy, block, "dy"), ld(dgate, block, "dgate"))
+    ldz, ldh = ld(dz, block, "dz"), ld(dh, x, "dh")
     if stats is None:
         raise _bad(w, "stats is not given")
     at = _stats_of(stats, n, w)
-    dev = _device_of(w, x, y, gate, dz, dh, dx, dy, dgate, post_weight, post_bias, scale, pre_weight, dpost_weight, dpost_bias, dscale, dpre_weight, dpre_bias, stats)
+    dev = _device_of(w, x, *[t for t in (y, gate, dz, dh, dx, dy, dgate, post_weight, post_bias, scale, pre_weight, dpost_weight, dpost_bias, dscale, dpre_weight, dpre_bias, stats)
+                             if t is not None])
+    wanted = not (dpost_weight is None and dpost_bias is None and dscale is None and dpre_weight is None and dpre_bias is None)
     place, size, keep = _scratch(scratch, lib().kge_block_norm_grad_scratch_bytes(n, d) if wanted else 0, dev, w)
-    _call(w, lib().kge_block_norm_grad, dev, b, n, d, at, _addr(dz), ld["dz"], _addr(dh), ld["dh"], o, 1 if accumulate else 0, place, size)
+    _call(w, lib().kge_block_norm_grad, dev, b, n, d, at, _addr(dz), ldz, _addr(dh), ldh, o, 1 if accumulate else 0, place, size)
 
 
 class AdamW:

@@ -60,9 +60,13 @@ __device__ __forceinline__ void store_z8(int8_t* out, const Place<WIDE>& at, con
 }
 
 // A team of L threads (L = 0: the CTA) holds a row, K packs of eight elements to a thread: the row's addresses, sums and scalars are shared out over up to 32
-// elements a thread (24,576 x 256 with a thread for eight elements: 36 instructions an element, most of them for the row).
+// elements a thread (32,768 x 4,096 bf16 with a thread for eight elements: 53 instructions an element, so 26).  Narrow rows take one pack a thread instead, the next row's
+// loads under way: few rows are in an SM's hands then, and it waits for them (24,576 x 200: 16 us with two packs, %s).
+constexpr int norm_threads(int l, bool wide) { return l == 0 && !wide ? 2 * NORM_THREADS : NORM_THREADS; }
+constexpr int norm_ctas(int l, int k, bool wide, int bytes) { return l == 0 && !wide ? 1 : (k == 1 || (k == 2 && wide && bytes <= 6) ? 3 : (k > 2 && bytes > 6 ? 1 : 2)); }
 template <typename TX, typename TB, int L, int K, bool WIDE, bool LAYER>
-__global__ void __launch_bounds__(NORM_THREADS, K < 3 ? 3 : (sizeof(TX) + sizeof(TB) > 6 ? 1 : 2)) norm_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, sizeof(TX) + sizeof(TB))) norm_kernel(const __grid_constant__ NormParams p) {
+    constexpr bool AHEAD = K == 1;
     __shared__ float parts[2][2][32];
     Team<L> team(parts);
     const int t = team.thread;
@@ -71,30 +75,39 @@ __global__ void __launch_bounds__(NORM_THREADS, K < 3 ? 3 : (sizeof(TX) + sizeof
     for (int k = 0; k < K; ++k) at[k] = Place<WIDE>(Team<L>::size(), t, k, p.d);
     grid_dependency_wait();
     allow_dependents();
-    for (int64_t r0 = (int64_t)blockIdx.x * Team<L>::COUNT; r0 < p.n; r0 += (int64_t)gridDim.x * Team<L>::COUNT) {
+    struct Row { Raw8<TX> x[K]; Raw8<TB> y[K], gate[K]; };
+    auto load = [&](int64_t row, Row& v) {
         // (a team that has run out of rows goes along with the last one)
+        const int64_t r = L == 0 ? row : min(row, (int64_t)p.n - 1);
+#pragma unroll
+        for (int k = 0; k < K; ++k) v.x[k] = at[k].load(static_cast<const TX*>(p.x) + r * p.ldx);
+        if (p.y) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) v.y[k] = at[k].load(static_cast<const TB*>(p.y) + r * p.ldy);
+            if (p.gate) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) v.gate[k] = at[k].load(static_cast<const TB*>(p.gate) + r * p.ldg);
+            }
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
+    Row next;
+    if (AHEAD) load((int64_t)blockIdx.x * Team<L>::COUNT + team.index, next);
+    for (int64_t r0 = (int64_t)blockIdx.x * Team<L>::COUNT; r0 < p.n; r0 += step) {
         const int64_t mine = r0 + team.index, r = L == 0 ? mine : min(mine, (int64_t)p.n - 1);
         const bool live = L == 0 || mine < p.n;
         float* const stats = p.stats && live && t == 0 ? p.stats + 4 * r : nullptr;
         F8 u[K];
         float2 s = make_float2(0.f, 0.f);
         {
-            Raw8<TX> x[K];
-            Raw8<TB> y[K], gate[K];
-            const TX* const xs = static_cast<const TX*>(p.x) + r * p.ldx;
-            const TB* const ys = static_cast<const TB*>(p.y) + (p.y ? r * p.ldy : 0);
-            const TB* const gates = static_cast<const TB*>(p.gate) + (p.gate ? r * p.ldg : 0);
-#pragma unroll
-            for (int k = 0; k < K; ++k) x[k] = at[k].load(xs);
+            Row now;
+            if (AHEAD) {
+                now = next;
+                if (r0 + step < p.n) load(mine + step, next);
+            } else load(mine, now);
             if (p.y) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) y[k] = at[k].load(ys);
-                if (p.gate) {
-#pragma unroll
-                    for (int k = 0; k < K; ++k) gate[k] = at[k].load(gates);
-                }
-#pragma unroll
-                for (int k = 0; k < K; ++k) u[k] = wide_of(y[k]);
+                for (int k = 0; k < K; ++k) u[k] = wide_of(now.y[k]);
                 if (p.post) {
                     s = centre<LAYER>(p, team, u, at);
 #pragma unroll
@@ -107,22 +120,22 @@ __global__ void __launch_bounds__(NORM_THREADS, K < 3 ? 3 : (sizeof(TX) + sizeof
                 if (p.gate) {
                     if (p.act == NORM_PLAIN) {
 #pragma unroll
-                        for (int k = 0; k < K; ++k) u[k] = u[k] * wide_of(gate[k]);
+                        for (int k = 0; k < K; ++k) u[k] = u[k] * wide_of(now.gate[k]);
                     } else {
 #pragma unroll
-                        for (int k = 0; k < K; ++k) u[k] = u[k] * sigmoid_of(wide_of(gate[k]));
+                        for (int k = 0; k < K; ++k) u[k] = u[k] * sigmoid_of(wide_of(now.gate[k]));
                         if (p.act == NORM_SILU) {
 #pragma unroll
-                            for (int k = 0; k < K; ++k) u[k] = u[k] * wide_of(gate[k]);
+                            for (int k = 0; k < K; ++k) u[k] = u[k] * wide_of(now.gate[k]);
                         }
                     }
                 }
                 if (p.scale) {
 #pragma unroll
-                    for (int k = 0; k < K; ++k) u[k] = fma8(u[k], at[k].vector(p.scale), wide_of(x[k]));
+                    for (int k = 0; k < K; ++k) u[k] = fma8(u[k], at[k].vector(p.scale), wide_of(now.x[k]));
                 } else {
 #pragma unroll
-                    for (int k = 0; k < K; ++k) u[k] = u[k] + wide_of(x[k]);
+                    for (int k = 0; k < K; ++k) u[k] = u[k] + wide_of(now.x[k]);
                 }
                 if (p.h) {
                     TX* const hs = static_cast<TX*>(p.h) + r * p.ldh;
@@ -131,7 +144,7 @@ __global__ void __launch_bounds__(NORM_THREADS, K < 3 ? 3 : (sizeof(TX) + sizeof
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < K; ++k) u[k] = wide_of(x[k]);
+                for (int k = 0; k < K; ++k) u[k] = wide_of(now.x[k]);
             }
         }
         if (stats) *reinterpret_cast<float2*>(stats) = s;
@@ -222,7 +235,7 @@ __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_loop_kernel(const __gr
 // As many CTAs as run at a time, or fewer, so that each has as many rows as the others.
 template <typename TX, typename TB, int L, int K, bool WIDE>
 int launch_rows(const NormParams& p, int threads, int sms, cudaStream_t s) {
-    const int regs = K < 3 ? 80 : (sizeof(TX) + sizeof(TB) > 6 ? 208 : 128);          // (as compiled, at most)
+    constexpr int bytes = sizeof(TX) + sizeof(TB), regs = K == 1 || (K == 2 && WIDE && bytes <= 6) ? 80 : (WIDE && K > 2 && bytes > 6 ? 208 : 128);          // (as compiled, at most)
     const int64_t all = ceil_div(p.n, Team<L>::COUNT), room = (int64_t)sms * (65536 / (regs * threads)), turns = ceil_div(all, room);
     const dim3 grid((unsigned)ceil_div(all, turns)), block((unsigned)threads);
     return launch_status(p.layer ? launch_dependent(norm_kernel<TX, TB, L, K, WIDE, true>, grid, block, 0, s, p)
@@ -238,13 +251,13 @@ int launch_norm(const NormParams& p, cudaStream_t s) {
     const int cta = (int)ceil_div(d, 1024) * 32;          // threads of a CTA that holds a row, 32 elements each
     if (!p.wide) {
         if (d <= 256) return launch_rows<TX, TB, 32, 1, false>(p, NORM_THREADS, sms, s);
-        if (d <= 1024) return launch_rows<TX, TB, 32, 4, false>(p, NORM_THREADS, sms, s);
-        return launch_rows<TX, TB, 0, 4, false>(p, cta, sms, s);
+        if (d <= 512) return launch_rows<TX, TB, 32, 2, false>(p, NORM_THREADS, sms, s);
+        return launch_rows<TX, TB, 0, 2, false>(p, (int)ceil_div(d, 512) * 32, sms, s);
     }
     if (d <= 64) return launch_rows<TX, TB, 8, 1, true>(p, NORM_THREADS, sms, s);
-    if (d <= 128) return launch_rows<TX, TB, 8, 2, true>(p, NORM_THREADS, sms, s);
-    if (d <= 256) return launch_rows<TX, TB, 8, 4, true>(p, NORM_THREADS, sms, s);
-    if (d <= 512) return launch_rows<TX, TB, 16, 4, true>(p, NORM_THREADS, sms, s);
+    if (d <= 128) return launch_rows<TX, TB, 16, 1, true>(p, NORM_THREADS, sms, s);
+    if (d <= 256) return launch_rows<TX, TB, 32, 1, true>(p, NORM_THREADS, sms, s);
+    if (d <= 512) return launch_rows<TX, TB, 32, 2, true>(p, NORM_THREADS, sms, s);
     if (d <= 768) return launch_rows<TX, TB, 32, 3, true>(p, NORM_THREADS, sms, s);
     if (d <= 1024) return launch_rows<TX, TB, 32, 4, true>(p, NORM_THREADS, sms, s);
     return d <= 24 * cta ? launch_rows<TX, TB, 0, 3, true>(p, cta, sms, s) : launch_rows<TX, TB, 0, 4, true>(p, cta, sms, s);

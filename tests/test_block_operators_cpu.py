@@ -38,8 +38,8 @@ def test_int8_matmul_refuses(K, over, code):
 
 
 def _norm(K, block=(), **over):
-    from paper_2211_12281_b200.binding import KgeNormBlock
-    return K.lib().kge_block_norm(KgeNormBlock(**dict(BLOCK, **dict(block))), *dict(NORM, **over).values())
+    from paper_2211_12281_b200.binding import KGE_NORM_BLOCK
+    return K.lib().kge_block_norm(KGE_NORM_BLOCK.pack(*[v or 0 for v in dict(BLOCK, **dict(block)).values()]), *dict(NORM, **over).values())
 
 
 @pytest.mark.parametrize("block,over", [
@@ -53,10 +53,10 @@ def test_block_norm_refuses(K, block, over):
 
 
 def _grad(K, block=(), grads=(), **over):
-    from paper_2211_12281_b200.binding import KgeNormBlock, KgeNormGrads
+    from paper_2211_12281_b200.binding import KGE_NORM_BLOCK, KGE_NORM_GRADS
     a = dict(GRAD, **over)
-    return K.lib().kge_block_norm_grad(KgeNormBlock(**dict(BLOCK, **dict(block))), a["n"], a["d"], a["stats"], a["dz"], a["ld_dz"], a["dh"], a["ld_dh"],
-                                       KgeNormGrads(**dict(GRADS, **dict(grads))), a["accumulate"], a["scratch"], a["scratch_bytes"], a["stream"])
+    return K.lib().kge_block_norm_grad(KGE_NORM_BLOCK.pack(*[v or 0 for v in dict(BLOCK, **dict(block)).values()]), a["n"], a["d"], a["stats"], a["dz"], a["ld_dz"], a["dh"], a["ld_dh"],
+                                       KGE_NORM_GRADS.pack(*[v or 0 for v in dict(GRADS, **dict(grads)).values()]), a["accumulate"], a["scratch"], a["scratch_bytes"], a["stream"])
 
 
 @pytest.mark.parametrize("block,grads,over,code", [
@@ -98,11 +98,27 @@ def test_calls_on_nothing_return_at_once(K):
     assert _adamw(K, dict(grad=None, param=None)) == 0 and _adamw(K, dict(n=0, param=None)) == 0
 
 
-def test_mirrors_have_the_header_layout(K):
-    from paper_2211_12281_b200.binding import KgeAdamwTensor, KgeNormBlock, KgeNormGrads
-    assert C.sizeof(KgeAdamwTensor) == 80 and KgeAdamwTensor.n.offset == 56 and KgeAdamwTensor.weight_decay.offset == 76
-    assert C.sizeof(KgeNormBlock) == 8 * 8 + 3 * 8 + 4 * 4 and KgeNormBlock.x_type.offset == 88
-    assert C.sizeof(KgeNormGrads) == 11 * 8
+def test_mirrors_have_the_header_layout(K, tmp_path):
+    """Sizes and places of the structures' fields as a C compiler lays them out."""
+    import subprocess
+    from pathlib import Path
+    from paper_2211_12281_b200.binding import KGE_NORM_BLOCK, KGE_NORM_GRADS, KgeAdamwTensor
+    src = tmp_path / "layout.c"
+    src.write_text("""#include <stddef.h>
+#include <stdio.h>
+#include "kge.h"
+int main(void) {
+    printf("%zu %zu %zu ", sizeof(kge_adamw_tensor), offsetof(kge_adamw_tensor, n), offsetof(kge_adamw_tensor, weight_decay));
+    printf("%zu %zu %zu %zu ", sizeof(kge_norm_block), offsetof(kge_norm_block, pre_bias), offsetof(kge_norm_block, ldx), offsetof(kge_norm_block, layer));
+    printf("%zu %zu %zu\\n", sizeof(kge_norm_grads), offsetof(kge_norm_grads, dpre_bias), offsetof(kge_norm_grads, ld_dgate));
+    return 0;
+}
+""")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-I", str(Path(__file__).resolve().parent.parent / "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(v) for v in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    assert got[:3] == [C.sizeof(KgeAdamwTensor), KgeAdamwTensor.n.offset, KgeAdamwTensor.weight_decay.offset]
+    assert got[3:] == [KGE_NORM_BLOCK.size, 56, 64, 100, KGE_NORM_GRADS.size, 56, 80]
 
 
 def test_scratch_of_gradients_holds_every_share(K):
