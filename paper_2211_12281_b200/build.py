@@ -18,7 +18,7 @@ OBJ = PKG / "_build"
 SOURCES = ["kge_api.cu", "kge_sample.cu", "kge_train.cu", "kge_pair_backward.cu", "kge_tc.cu", "kge_update.cu", "kge_infer.cu",
            "kge_graph.cu", "kge_ensemble.cu", "kge_bench.cu", "kge_transh.cu", "kge_encoder.cu",
            "kge_rows.cu", "kge_dropout.cu", "kge_fp8.cu",
-           "kge_int8.cu", "kge_norm.cu", "kge_norm_f32.cu", "kge_norm_bf16.cu", "kge_norm_f16.cu", "kge_norm_grad.cu",
+           "kge_int8.cu", "kge_norm.cu", "kge_norm_f32.cu", "kge_norm_bf16.cu", "kge_norm_f16.cu", "kge_norm_grad.cu", "kge_norm_grad_f32.cu", "kge_norm_grad_bf16.cu", "kge_norm_grad_f16.cu",
            "kge_adamw.cu"]
 ARCH = ["-gencode", "arch=compute_100a,code=sm_100a"]
 
