@@ -506,7 +506,7 @@ int kge_block_norm_grad(const kge_norm_block* block /*[host]*/, int64_t n, int32
  *                   never becomes 0.  scale = 2^(e - 7) for m, 2^(e - 14) for v, 2^e <= largest magnitude < 2^(e + 1), at least 2^-126; 1 for
  *                   zeros alone.  A block of 128 in which a new m (or v) is infinite or NaN stands for NaN from then on.
  * step_dev, lr_dev, grad_scale_dev: device numbers added to step, multiplied by lr, multiplied by grad_scale when the call runs (or
- * NULL), so that a captured call can be replayed.  eps > 0 in fp32; 0 <= beta1, beta2 < 1; step (with *step_dev) < 2^62.
+ * NULL), so that a captured call can be replayed.  eps at least 2^-126; 0 <= beta1, beta2 < 1; step (with *step_dev) < 2^62.
  * A launch carries up to 340 tensors.
  */
 typedef struct {

@@ -104,9 +104,10 @@ __device__ __forceinline__ F8 decode_v(const Raw8<uint8_t>& q, float scale) {
 
 // The scale of a block whose largest magnitude has the bits `most`: the power of two that puts it into the binade of exponent `top`,
 // one below the type's last (a value rounded up may reach that).  1 for a block of zeros, NaN for one that holds an infinity or a
-// NaN; `inv` is its reciprocal (0 for NaN: the codes are 0 then, and the block stands for NaN).
+// NaN; `inv` is its reciprocal (0 for NaN: the block stands for NaN whatever its codes are).
 struct BlockScale { float s, inv; };
-__device__ __forceinline__ BlockScale block_scale(uint32_t most, int top) {
+__device__ __forceinline__ BlockScale block_scale(float largest, int top) {
+    const uint32_t most = __float_as_uint(largest);
     const int e = max((int)(most >> 23) - top, 1);
     BlockScale b{__int_as_float(e << 23), __int_as_float((254 - e) << 23)};
     if (most == 0) b = {1.f, 1.f};
@@ -114,17 +115,29 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t most, int top) {
     return b;
 }
 // |x| / scale times 2^(bias - 127) has the 8-bit type's exponent in the fp32 exponent field, its subnormal values being fp32's own; the
-// bits below the type's last one are added to and cut off.
-template <int BITS, int BIAS> __device__ __forceinline__ uint32_t code_of(float x, float inv, uint32_t half) {
-    constexpr int SHIFT = 23 - BITS;
-    const float y = (inv == 0.f ? 0.f : fabsf(x) * inv) * __int_as_float(BIAS << 23);
-    return (__float_as_uint(y) + (half << (SHIFT - 16)) + (1u << (SHIFT - 17))) >> SHIFT;
+// bits below the type's last one are added to and cut off.  The code is the result's low byte.
+template <int BITS, int BIAS> __device__ __forceinline__ uint32_t code_of(float x, float inv, uint32_t noise) {
+    return (__float_as_uint((fabsf(x) * inv) * __int_as_float(BIAS << 23)) + noise) >> (23 - BITS);
 }
-__device__ __forceinline__ uint32_t half_warp_max(uint32_t x) {
+// A half of a random word, and half a unit of it, below the last bit that stays.
+template <int BITS, bool HIGH> __device__ __forceinline__ uint32_t noise_of(uint32_t word) {
+    constexpr int UP = 23 - BITS - 16;
+    return (HIGH ? (word >> (16 - UP)) & (0xFFFFu << UP) : (word << UP) & (0xFFFFu << UP)) | (1u << (UP - 1));
+}
+// Byte B of four words.
+template <int B> __device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    constexpr uint32_t PICK = B | (4 + B) << 4;
+    return __byte_perm(__byte_perm(a, b, PICK), __byte_perm(c, d, PICK), 0x5410);
+}
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float half_warp_max(float x) {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+    for (int o = 8; o > 0; o >>= 1) x = max_nan(x, __shfl_xor_sync(0xffffffffu, x, o));
     return x;
 }
+// Square root and reciprocal as one instruction each: within 2 units of 2^-24 both.
+__device__ __forceinline__ float root_of(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float over(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
 template <int BITS, typename TP, typename TG>
 __device__ __forceinline__ void adam_chunk(const AdamCommon& c, const AdamTensor& t, const AdamScalars& s, int64_t from) {
@@ -153,17 +166,17 @@ __device__ __forceinline__ void adam_chunk(const AdamCommon& c, const AdamTensor
         const F8 g = wide_of(g8);
         F8 p = wide_of(p8);
         // products and sums of the moments are rounded one by one: the 8-bit rounding below is a function of their last bits
-        uint32_t most_m = 0, most_v = 0;
+        float most_m = 0.f, most_v = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = __fmul_rn(g.v[e], s.grad_scale);
             m.v[e] = __fadd_rn(__fmul_rn(m.v[e], c.b1), __fmul_rn(x, c.o1));
             v.v[e] = __fadd_rn(__fmul_rn(v.v[e], c.b2), __fmul_rn(__fmul_rn(x, x), c.o2));
-            const float change = __fdiv_rn(m.v[e], fmaf(__fsqrt_rn(v.v[e]), s.root, c.eps));
+            const float change = m.v[e] * over(fmaf(root_of(v.v[e]), s.root, c.eps));
             p.v[e] = fmaf(-s.size, change, p.v[e] * s.keep);
             if (BITS == 8) {
-                most_m = max(most_m, __float_as_uint(m.v[e]) & 0x7FFFFFFFu);
-                most_v = max(most_v, __float_as_uint(v.v[e]) & 0x7FFFFFFFu);
+                most_m = max_nan(most_m, fabsf(m.v[e]));
+                most_v = max_nan(most_v, fabsf(v.v[e]));
             }
         }
         if (valid) {
@@ -182,16 +195,16 @@ __device__ __forceinline__ void adam_chunk(const AdamCommon& c, const AdamTensor
             for (int k = 0; k < 2; ++k) {
                 const uint4 words = adam_words(c, (uint64_t)at / 4 + k, t.index, s);
                 const uint32_t w[4] = {words.x, words.y, words.z, words.w};
-                uint32_t a = 0, b = 0;
+                uint32_t a[4], b[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = m.v[4 * k + i], y = v.v[4 * k + i];
-                    a |= (code_of<3, 7>(x, sm.inv, w[i] & 0xFFFFu) | (__float_as_uint(x) >> 31) << 7) << (8 * i);
+                    a[i] = code_of<3, 7>(m.v[4 * k + i], sm.inv, noise_of<3, false>(w[i]));
                     // A positive v stays positive: with v = 0 beside an m that was rounded up the next step would be m / eps.
-                    b |= max(code_of<2, 15>(y, sv.inv, w[i] >> 16), y > 0.f && sv.inv > 0.f ? 1u : 0u) << (8 * i);
+                    b[i] = max(code_of<2, 15>(v.v[4 * k + i], sv.inv, noise_of<2, true>(w[i])), min(__float_as_uint(v.v[4 * k + i]), 1u));
                 }
-                mn.w[k] = a;
-                vn.w[k] = b;
+                const uint32_t signs = four_bytes<3>(__float_as_uint(m.v[4 * k]), __float_as_uint(m.v[4 * k + 1]), __float_as_uint(m.v[4 * k + 2]), __float_as_uint(m.v[4 * k + 3]));
+                mn.w[k] = (four_bytes<0>(a[0], a[1], a[2], a[3]) & 0x7F7F7F7Fu) | (signs & 0x80808080u);
+                vn.w[k] = four_bytes<0>(b[0], b[1], b[2], b[3]);
             }
         }
         if (valid) {
@@ -284,7 +297,7 @@ extern "C" int kge_adamw(const kge_adamw_tensor* tensors, int32_t count, int32_t
                          double grad_scale, uint64_t step, const int64_t* step_dev, const float* lr_dev, const float* grad_scale_dev, uint64_t seed,
                          void* stream) {
     if (count < 0 || count > (1 << 26) || (count && !tensors) || (state_bits != 32 && state_bits != 8) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) ||
-        !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps > 0.f) || !std::isfinite((float)eps) || !std::isfinite(grad_scale) || step >= 1ull << 62 || !aligned_to(step_dev, 8) ||
+        !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 1.17549435e-38f) || !std::isfinite((float)eps) || !std::isfinite(grad_scale) || step >= 1ull << 62 || !aligned_to(step_dev, 8) ||
         !aligned_to(lr_dev, 4) || !aligned_to(grad_scale_dev, 4)) return KGE_ERR_BAD_ARG;
     int live = 0;
     for (int32_t i = 0; i < count; ++i) {

@@ -576,8 +576,9 @@ def _adamw64(T, p, g, m, v, i, lr, b1, b2, eps, wd, step, seed, bits, gs=1.0):
     t = step + 1
     change = lr / (1 - b1 ** t) * m / (T.sqrt(v / (1 - b2 ** t)) + float(np.float32(eps)))
     new = p.double() * (1 - lr * wd) - change
-    # 1 - lr wd, its product, the final sum; the square root, the reciprocal it is multiplied by, their sum, the quotient, lr / (1 - b1^t)
-    tol = U * (2 * p.double().abs() + 6 * change.abs() + new.abs())
+    # 1 - lr wd, its product, the final sum; of the change: the square root's instruction (2^-23, two units), the constant it is multiplied by and their sum
+    # with eps (one each), the reciprocal's instruction (two), the product with m, lr / (1 - b1^t) (one each)
+    tol = U * (2 * p.double().abs() + 8 * change.abs() + new.abs())
     if bits == 32:
         return new, tol, m, v, None, None
     w = _words(p.numel(), i, step, seed)
