@@ -15,8 +15,10 @@ namespace kge {
 namespace {
 
 constexpr int ADAM_THREADS = 256, ADAM_PER = 8;                        // elements per thread and turn
-constexpr int ADAM_TURNS = 2;
-constexpr int ADAM_CHUNK = ADAM_THREADS * ADAM_PER * ADAM_TURNS;       // elements of one tensor per CTA
+constexpr int ADAM_TURN = ADAM_THREADS * ADAM_PER;                     // elements of a CTA at a time
+// Five CTAs an SM (48 registers); each takes one or two turns of one tensor, two where the CTAs of one turn each would not all run at a time (64 M elements with
+// 8-bit states: 193 us with two turns, 198 with two on four CTAs an SM, 190 with one; a hundred tensors of 20 M, whose search for the tensor costs a CTA more: 71, 73, 80).
+constexpr int ADAM_CTAS = 5, ADAM_SMS = 148;
 constexpr int ADAM_BLOCK = 128;                                        // elements to a scale: the sixteen lanes of half a warp
 static_assert(ADAM_BLOCK == 16 * ADAM_PER, "a block is half a warp's");
 
@@ -36,7 +38,7 @@ struct AdamCommon {
     const int64_t* step_dev;
     const float *lr_dev, *grad_scale_dev;
     uint32_t key[20];
-    int count;
+    int count, turns;
 };
 
 // A launch's tensors travel with its parameters: few with little to copy, many with what a launch may carry.
@@ -143,7 +145,7 @@ template <int BITS, typename TP, typename TG>
 __device__ __forceinline__ void adam_chunk(const AdamCommon& c, const AdamTensor& t, const AdamScalars& s, int64_t from) {
     using TS = typename std::conditional<BITS == 32, float, uint8_t>::type;
 #pragma unroll 1
-    for (int turn = 0; turn < ADAM_TURNS; ++turn) {
+    for (int turn = 0; turn < c.turns; ++turn) {
         const int64_t at = from + (turn * ADAM_THREADS + threadIdx.x) * ADAM_PER;
         const int valid = (int)max((int64_t)0, min((int64_t)8, t.n - at));
         if (BITS == 32 && valid == 0) return;
@@ -215,7 +217,7 @@ __device__ __forceinline__ void adam_chunk(const AdamCommon& c, const AdamTensor
 }
 
 template <int BITS, int CAP>
-__global__ void __launch_bounds__(ADAM_THREADS) adamw_kernel(const __grid_constant__ AdamParams<CAP> q) {
+__global__ void __launch_bounds__(ADAM_THREADS, ADAM_CTAS) adamw_kernel(const __grid_constant__ AdamParams<CAP> q) {
     __shared__ AdamScalars shared;
     const AdamCommon& c = q.c;
     int i = 0;
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(ADAM_THREADS) adamw_kernel(const __grid_consta
         __syncthreads();
         s = shared;
     }
-    const int64_t from = (int64_t)(blockIdx.x - q.first[i]) * ADAM_CHUNK;
+    const int64_t from = (int64_t)(blockIdx.x - q.first[i]) * (ADAM_TURN * c.turns);
     auto with_grad = [&](auto tp) {
         using TP = decltype(tp);
         if (t.g_type == KGE_F32) adam_chunk<BITS, TP, float>(c, t, s, from);
@@ -271,7 +273,7 @@ int adamw_part(const kge_adamw_tensor* tensors, int32_t count, int32_t* at, int3
     for (; *at < count && k < CAP; ++*at) {
         const kge_adamw_tensor& t = tensors[*at];
         if (t.n == 0 || !t.grad) continue;
-        const int64_t more = ceil_div(t.n, ADAM_CHUNK);
+        const int64_t more = ceil_div(t.n, ADAM_TURN * common.turns);
         if (chunks + more > INT32_MAX) break;
         AdamTensor& d = q.t[k];
         const int ps = type_bytes(t.param_type), gs = type_bytes(t.grad_type), ss = bits == 32 ? 4 : 1;
@@ -300,6 +302,7 @@ extern "C" int kge_adamw(const kge_adamw_tensor* tensors, int32_t count, int32_t
         !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 1.17549435e-38f) || !std::isfinite((float)eps) || !std::isfinite(grad_scale) || step >= 1ull << 62 || !aligned_to(step_dev, 8) ||
         !aligned_to(lr_dev, 4) || !aligned_to(grad_scale_dev, 4)) return KGE_ERR_BAD_ARG;
     int live = 0;
+    int64_t turns = 0;
     for (int32_t i = 0; i < count; ++i) {
         const kge_adamw_tensor& t = tensors[i];
         if (t.n < 0 || !is_float_type(t.param_type) || !is_float_type(t.grad_type) || !std::isfinite(t.weight_decay)) return KGE_ERR_BAD_ARG;
@@ -311,6 +314,7 @@ extern "C" int kge_adamw(const kge_adamw_tensor* tensors, int32_t count, int32_t
             !aligned_to(t.v, ss) || (t.copy && !aligned_to(t.copy, 2))) return KGE_ERR_BAD_ARG;
         if (state_bits == 8 && (!t.m_scales || !t.v_scales || !aligned_to(t.m_scales, 4) || !aligned_to(t.v_scales, 4))) return KGE_ERR_BAD_ARG;
         ++live;
+        turns += ceil_div(t.n, ADAM_TURN);
     }
     AdamCommon c{};
     c.b1 = (float)beta1; c.o1 = (float)(1.0 - beta1); c.b2 = (float)beta2; c.o2 = (float)(1.0 - beta2);
@@ -319,6 +323,7 @@ extern "C" int kge_adamw(const kge_adamw_tensor* tensors, int32_t count, int32_t
     const double n = (double)step + 1.0;
     c.size = (float)(lr / -std::expm1(n * c.log_b1));
     c.root = (float)(1.0 / std::sqrt(-std::expm1(n * c.log_b2)));
+    c.turns = turns > ADAM_SMS * ADAM_CTAS ? 2 : 1;
     c.step = step; c.step_dev = step_dev; c.lr_dev = lr_dev; c.grad_scale_dev = grad_scale_dev;
     for (uint32_t r = 0; r < 10; ++r) { c.key[2 * r] = (uint32_t)seed + r * 0x9E3779B9u; c.key[2 * r + 1] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u; }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
