@@ -145,15 +145,18 @@ int launch_quantize(const QuantParams& p, cudaStream_t s) {
 constexpr int I8_BM = 128;
 constexpr uint32_t I8_BOX_BYTES = 128 * OPERAND_BK;
 constexpr int I8_NACC = 2;                                // accumulators in tensor memory: one is stored while the other is summed up
-enum { I8_WIDE = 0, I8_PAIR = 1, I8_NARROW = 2, I8_SPLIT = 3 };
+// Four forms of the kernel: tiles of 256 x 256 that a pair of CTAs shares, 128 rows and half of B's rows each; tiles of 128 x 128, two CTAs an SM (one loads and
+// multiplies while the other stores), or of 128 x 64, three CTAs an SM; tiles of 128 x 128 whose K a cluster shares, where tiles are few.
+enum { I8_TWO = 0, I8_PAIR = 1, I8_NARROW = 2, I8_SPLIT = 3 };
 constexpr int I8_MAX_SPLIT = 8;           // CTAs that share a tile's K
-__host__ __device__ constexpr int i8_bn(int form) { return form == I8_WIDE ? 256 : (form == I8_NARROW ? 64 : 128); }
-__host__ __device__ constexpr int i8_box_rows(int form) { return form == I8_NARROW ? 64 : 128; }             // of B per copy
-__host__ __device__ constexpr int i8_stages(int form) { return form == I8_WIDE ? 3 : (form == I8_SPLIT ? 6 : 2); }
-__host__ __device__ constexpr int i8_epi_warps(int form) { return 4 * i8_bn(form) / OUT_COLS; }
+__host__ __device__ constexpr int i8_bn(int form) { return form == I8_TWO ? 256 : (form == I8_NARROW ? 64 : 128); }
+__host__ __device__ constexpr int i8_box_rows(int form) { return form == I8_NARROW ? 64 : 128; }             // of B per copy and CTA
+__host__ __device__ constexpr int i8_stages(int form) { return form == I8_TWO || form == I8_SPLIT ? 6 : 2; }
+__host__ __device__ constexpr int i8_epi_warps(int form) { return form == I8_NARROW ? 4 : 8; }
+__host__ __device__ constexpr int i8_groups(int form) { return i8_bn(form) / OUT_COLS * 4 / i8_epi_warps(form); }     // of 64 columns per epilogue warp
 __host__ __device__ constexpr int i8_threads(int form) { return 32 * (4 + i8_epi_warps(form)); }     // (four more: copies, MMAs, two idle)
 __host__ __device__ constexpr int i8_ctas_per_sm(int form) { return form == I8_PAIR ? 2 : (form == I8_NARROW ? 3 : 1); }
-__host__ __device__ constexpr uint32_t i8_stage_bytes(int form) { return I8_BOX_BYTES + (uint32_t)i8_bn(form) * OPERAND_BK; }
+__host__ __device__ constexpr uint32_t i8_stage_bytes(int form) { return I8_BOX_BYTES + (uint32_t)i8_box_rows(form) * OPERAND_BK; }
 constexpr uint32_t I8_STORE_ROW = 128;                    // bytes of a row on their way to memory, per epilogue warp and turn
 __host__ __device__ constexpr size_t i8_smem_bytes(int form) {
     return (size_t)i8_stages(form) * i8_stage_bytes(form) + i8_epi_warps(form) * (32 * I8_STORE_ROW + OUT_COLS * 4) + 256;
@@ -171,6 +174,10 @@ struct IntProductParams : ProductOut {
 constexpr uint32_t i8_idesc(int m, int n) { return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
 __device__ __forceinline__ void i8_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void i8_mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n}\n"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
@@ -263,15 +270,15 @@ __device__ __forceinline__ void i8_join(const IntProductParams& p, uint32_t part
     }
 }
 
-// A 128 x BN tile of C at a time (persistent CTAs), or one per cluster, whose CTAs share its K (SPLIT).  Warp 0 feeds a ring of
-// shared-memory stages by TMA, warp 1 issues the MMAs of a whole tile into one of two accumulators in tensor memory; the other warps, 64
-// columns each, scale and store the tile before it meanwhile.
+// A 128 x BN tile of C at a time (persistent CTAs), the same for 256 x 256 and a pair of CTAs (TWO), or one tile per cluster, whose CTAs share its K (SPLIT).
+// Warp 0 feeds a ring of shared-memory stages by TMA, warp 1 (of a pair: the first CTA's) issues the MMAs of a whole tile into one of two accumulators in
+// tensor memory; the other warps, 64 columns at a time, scale and store the tile before it meanwhile.
 template <int FORM>
 __global__ void __launch_bounds__(i8_threads(FORM), i8_ctas_per_sm(FORM)) int8_product_kernel(const __grid_constant__ CUtensorMap tmA,
                                                                                                const __grid_constant__ CUtensorMap tmB,
                                                                                                const __grid_constant__ IntProductParams p) {
-    constexpr bool SPLIT = FORM == I8_SPLIT;
-    constexpr int BN = i8_bn(FORM), STAGES = i8_stages(FORM), EW = i8_epi_warps(FORM);
+    constexpr bool SPLIT = FORM == I8_SPLIT, TWO = FORM == I8_TWO;
+    constexpr int BN = i8_bn(FORM), STAGES = i8_stages(FORM), EW = i8_epi_warps(FORM), GROUPS = i8_groups(FORM), TILE_M = TWO ? 2 * I8_BM : I8_BM;
     constexpr uint32_t STAGE = i8_stage_bytes(FORM), TMEM_COLS = I8_NACC * BN;
     extern __shared__ __align__(1024) unsigned char i8_smem[];
     float4* const stores = reinterpret_cast<float4*>(i8_smem + (size_t)STAGES * STAGE);
@@ -285,66 +292,83 @@ __global__ void __launch_bounds__(i8_threads(FORM), i8_ctas_per_sm(FORM)) int8_p
     volatile uint32_t* stop = tmem_slot + 1;
     volatile uint32_t* filled = tmem_slot + 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = TWO || SPLIT ? cluster_rank() : 0u;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < I8_NACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], EW); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], TWO ? 2 : 1); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < I8_NACC; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], TWO ? 2 * EW : EW); }
         mbar_init(done, 1);
         *stop = 0;
         *filled = 0;
         mbar_init_fence();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (TWO) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     tmem_fence_before();
     __syncthreads();
+    if (TWO) cluster_sync();         // (the pair's barriers and tensor memory are there)
     tmem_fence_after();
     const uint32_t tmem = *tmem_slot;
     grid_dependency_wait();          // (nothing of global memory was touched so far)
     allow_dependents();
 
-    const int step = SPLIT ? p.items : (int)gridDim.x;
-    const int first = SPLIT ? (int)(blockIdx.x / cluster_size()) : (int)blockIdx.x;
-    const int kb0 = SPLIT ? (int)cluster_rank() * p.kper : 0, kb1 = SPLIT ? min(p.kblocks, kb0 + p.kper) : p.kblocks;
+    const int step = SPLIT ? p.items : (int)(TWO ? gridDim.x / 2 : gridDim.x);
+    const int first = SPLIT ? (int)(blockIdx.x / cluster_size()) : (int)(TWO ? blockIdx.x / 2 : blockIdx.x);
+    const int kb0 = SPLIT ? (int)rank * p.kper : 0, kb1 = SPLIT ? min(p.kblocks, kb0 + p.kper) : p.kblocks;
 
     if (warp < 4) {
         if (warp == 0 && lane == 0) {
             uint32_t s = 0, phase = 1, count = 0;
             bool ok = true;
             for (int item = first; item < p.items && ok; item += step) {
-                const int m0 = item / p.tiles_n * I8_BM, n0 = item % p.tiles_n * BN;
+                const int m0 = item / p.tiles_n * TILE_M + (TWO ? (int)rank * I8_BM : 0), n0 = item % p.tiles_n * BN + (TWO ? (int)rank * 128 : 0);
                 for (int kb = kb0; kb < kb1; ++kb) {
                     ok = mbar_wait_idle(&empty[s], phase, p.wait_limit) && !*stop;
                     if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); break; }
                     unsigned char* sa = i8_smem + s * STAGE;
-                    mbar_arrive_expect_tx(&full[s], STAGE);
-                    tma_load_2d(sa, &tmA, kb * OPERAND_BK, m0, &full[s]);
-#pragma unroll
-                    for (int g = 0; g < (BN + 127) / 128; ++g) tma_load_2d(sa + I8_BOX_BYTES * (1 + g), &tmB, kb * OPERAND_BK, n0 + 128 * g, &full[s]);
+                    if constexpr (TWO) {
+                        const uint32_t bar = cluster_addr(&full[s], 0);
+                        mbar_arrive_expect_tx_cluster(bar, STAGE);
+                        tma_load_pair(sa, &tmA, kb * OPERAND_BK, m0, bar);
+                        tma_load_pair(sa + I8_BOX_BYTES, &tmB, kb * OPERAND_BK, n0, bar);
+                    } else {
+                        mbar_arrive_expect_tx(&full[s], STAGE);
+                        tma_load_2d(sa, &tmA, kb * OPERAND_BK, m0, &full[s]);
+                        tma_load_2d(sa + I8_BOX_BYTES, &tmB, kb * OPERAND_BK, n0, &full[s]);
+                    }
                     ++count;
                     if (++s == STAGES) { s = 0; phase ^= 1; }
                 }
             }
             *filled = count;
-        } else if (warp == 1 && lane == 0) {
+        } else if (warp == 1 && lane == 0 && (!TWO || rank == 0)) {
             uint32_t s = 0, phase = 0, buf = 0, acc_phase = 1;
             bool ok = true;
             for (int item = first; item < p.items && ok && !*stop; item += step) {
-                ok = mbar_wait_idle(&acc_empty[buf], acc_phase, p.wait_limit);
+                ok = TWO ? mbar_wait_cluster(&acc_empty[buf], acc_phase, p.wait_limit) : mbar_wait_idle(&acc_empty[buf], acc_phase, p.wait_limit);
                 for (int kb = kb0; kb < kb1 && ok; ++kb) {
                     ok = mbar_wait_idle(&full[s], phase, p.wait_limit);
                     if (!ok) break;
                     tmem_fence_after();
                     const uint32_t sa = smem_u32(i8_smem + s * STAGE);
 #pragma unroll
-                    for (int k = 0; k < OPERAND_BK / 32; ++k)
-                        i8_mma(tmem + buf * BN, operand_desc(sa + k * 32), operand_desc(sa + I8_BOX_BYTES + k * 32), p.idesc, kb != kb0 || k != 0);
-                    mma_commit(&empty[s]);
+                    for (int k = 0; k < OPERAND_BK / 32; ++k) {
+                        if constexpr (TWO) i8_mma_pair(tmem + buf * BN, operand_desc(sa + k * 32), operand_desc(sa + I8_BOX_BYTES + k * 32), p.idesc, kb != kb0 || k != 0);
+                        else i8_mma(tmem + buf * BN, operand_desc(sa + k * 32), operand_desc(sa + I8_BOX_BYTES + k * 32), p.idesc, kb != kb0 || k != 0);
+                    }
+                    if constexpr (TWO) mma_commit_pair(&empty[s]);
+                    else mma_commit(&empty[s]);
                     if (++s == STAGES) { s = 0; phase ^= 1; }
                 }
-                mma_commit(&acc_full[buf]);
+                if constexpr (TWO) mma_commit_pair(&acc_full[buf]);
+                else mma_commit(&acc_full[buf]);
                 if (++buf == I8_NACC) { buf = 0; acc_phase ^= 1; }
             }
             if (!ok) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); }
@@ -352,46 +376,57 @@ __global__ void __launch_bounds__(i8_threads(FORM), i8_ctas_per_sm(FORM)) int8_p
         __syncwarp();
         if (SPLIT) { cluster_sync(); cluster_sync(); }
     } else {
-        const int quarter = warp & 3, group = (warp - 4) >> 2;      // tensor-memory lanes and columns of this warp
+        const int quarter = warp & 3, first_group = (warp - 4) >> 2;      // tensor-memory lanes and columns of this warp
         float4* const st = stores + (warp - 4) * (32 * I8_STORE_ROW / 16);
         float* const sb = column_scales + (warp - 4) * OUT_COLS;
-        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(group * OUT_COLS);
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
         uint32_t buf = 0, phase = 0;
         bool ok = true;
         for (int item = first; item < p.items && ok; item += step) {
-            const int m0 = item / p.tiles_n * I8_BM + quarter * 32, n0 = item % p.tiles_n * BN + group * OUT_COLS;
+            const int m0 = item / p.tiles_n * TILE_M + (TWO ? (int)rank * I8_BM : 0) + quarter * 32, nt = item % p.tiles_n * BN;
             float sa = 0.f;
-            if (!SPLIT) {
-                sa = m0 + lane < p.M ? __ldg(p.sa + m0 + lane) : 0.f;
+            auto begin = [&](int n0) {              // what a group of columns needs beside the sums
 #pragma unroll
                 for (int i = 0; i < OUT_COLS; i += 32) sb[i + lane] = n0 + i + lane < p.N ? __ldg(p.sb + n0 + i + lane) : 0.f;
                 if (p.addend) with_out_type(p.out_type, [&](auto t) { out_fetch_addend<decltype(t)>(p, m0, n0, 0, st, lane); });
                 __syncwarp();
+            };
+            if (!SPLIT) {
+                sa = m0 + lane < p.M ? __ldg(p.sa + m0 + lane) : 0.f;
+                begin(nt + first_group * OUT_COLS);
             }
             ok = __all_sync(0xffffffffu, mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit)) && !*stop;
             tmem_fence_after();
             if (!__all_sync(0xffffffffu, ok)) { ok = false; if (lane == 0) { *stop = 1; note_status(p.status, KGE_ERR_TIMEOUT); } break; }
-            const uint32_t from = taddr + buf * BN;
-            auto hand_back = [&] {                 // the accumulator is read: another tile's MMAs may begin
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&acc_empty[buf]);
-            };
             if (SPLIT) {       // the ring's stages are free: every copy has been multiplied
                 float4* part = reinterpret_cast<float4*>(i8_smem);
                 const int r = quarter * 32 + lane;
 #pragma unroll
                 for (int c = 0; c < OUT_COLS; c += 16) {
                     uint32_t v[16];
-                    tmem_ld16(from + c, v);
+                    tmem_ld16(taddr + buf * BN + first_group * OUT_COLS + c, v);
                     tmem_wait16(v);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        part[r * (BN / 4) + ((group * (OUT_COLS / 4) + c / 4 + i) ^ (r & 7))] =
+                        part[r * (BN / 4) + ((first_group * (OUT_COLS / 4) + c / 4 + i) ^ (r & 7))] =
                             make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
                 }
             } else {
-                with_out_type(p.out_type, [&](auto t) { i8_store<decltype(t)>(p, m0, n0, from, sa, sb, st, lane, hand_back); });
+#pragma unroll 1
+                for (int g = 0; g < GROUPS; ++g) {
+                    const int col = (first_group + g * (EW / 4)) * OUT_COLS;
+                    if (g > 0) begin(nt + col);
+                    auto read_all = [&] {                 // the accumulator is read: another tile's MMAs may begin
+                        if (g + 1 < GROUPS) return;
+                        tmem_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if constexpr (TWO) mbar_arrive_cluster(cluster_addr(&acc_empty[buf], 0));
+                            else mbar_arrive(&acc_empty[buf]);
+                        }
+                    };
+                    with_out_type(p.out_type, [&](auto t) { i8_store<decltype(t)>(p, m0, nt + col, taddr + buf * BN + col, sa, sb, st, lane, read_all); });
+                }
             }
             if (++buf == I8_NACC) { buf = 0; phase ^= 1; }
         }
@@ -405,17 +440,33 @@ __global__ void __launch_bounds__(i8_threads(FORM), i8_ctas_per_sm(FORM)) int8_p
     }
     tmem_fence_before();
     __syncthreads();
-    if (*stop) {       // copies and MMAs in flight are waited for before the CTA's memory is given back
-        if (lane == 0) {
-            if (warp == 0) {
-                const int n = (int)*filled;
+    // Copies and MMAs in flight are waited for before a CTA's memory is given back, where a wait ran out; of a pair, the first CTA does so for both.
+    if constexpr (TWO) {
+        cluster_sync();
+        if (rank == 0 && (*stop || cluster_ld_word(cluster_addr((const void*)stop, 1)))) {
+            if (lane == 0 && warp == 0) {
+                const int a = (int)*filled, b = (int)cluster_ld_word(cluster_addr((const void*)filled, 1)), n = max(a, b);
+                for (int r = min(a, b); r < n; ++r) mbar_arrive(&full[r % STAGES]);          // (a stage that one of the two did not come to)
                 for (int r = max(0, n - STAGES); r < n; ++r) mbar_wait_idle(&full[r % STAGES], (r / STAGES) & 1, kDefaultWaitLimit);
             }
-            if (warp == 1) { mma_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
+            if (lane == 0 && warp == 1) { mma_commit_pair(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
+            __syncwarp();
         }
-        __syncthreads();
+        cluster_sync();
+        if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+    } else {
+        if (*stop) {
+            if (lane == 0) {
+                if (warp == 0) {
+                    const int n = (int)*filled;
+                    for (int r = max(0, n - STAGES); r < n; ++r) mbar_wait_idle(&full[r % STAGES], (r / STAGES) & 1, kDefaultWaitLimit);
+                }
+                if (warp == 1) { mma_commit(done); mbar_wait_idle(done, 0, kDefaultWaitLimit); }
+            }
+            __syncthreads();
+        }
+        if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     }
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
 }
 
 template <int FORM> int configure_product() {
@@ -425,43 +476,48 @@ template <int FORM> int configure_product() {
     }) == cudaSuccess ? KGE_OK : KGE_ERR_CUDA;
 }
 
-// How many clusters of `split` CTAs the device runs at a time: asked for once (what is left of a part of the chip takes none).
-int split_clusters(int split, int* clusters) {
+// How many clusters of `size` CTAs of a form the device runs at a time: asked for once (what is left of a part of the chip takes none).
+template <int FORM> int clusters_at_a_time(int size, int* clusters) {
     static std::atomic<int> known[kMaxDevices][I8_MAX_SPLIT + 1];        // one more than their number
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) return KGE_ERR_CUDA;
     const bool tracked = dev >= 0 && dev < kMaxDevices;
-    int state = tracked ? known[dev][split].load(std::memory_order_acquire) : 0;
+    int state = tracked ? known[dev][size].load(std::memory_order_acquire) : 0;
     if (state == 0) {
-        const int rc = configure_product<I8_SPLIT>();
+        const int rc = configure_product<FORM>();
         if (rc != KGE_OK) return rc;
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)split); cfg.blockDim = dim3(i8_threads(I8_SPLIT)); cfg.dynamicSmemBytes = i8_smem_bytes(I8_SPLIT);
+        cfg.gridDim = dim3((unsigned)size); cfg.blockDim = dim3(i8_threads(FORM)); cfg.dynamicSmemBytes = i8_smem_bytes(FORM);
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+        attr[0].val.clusterDim.x = (unsigned)size; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = 1;
         int fit = 0;
-        if (cudaOccupancyMaxActiveClusters(&fit, int8_product_kernel<I8_SPLIT>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); fit = 0; }
+        if (cudaOccupancyMaxActiveClusters(&fit, int8_product_kernel<FORM>, &cfg) != cudaSuccess) { (void)cudaGetLastError(); fit = 0; }
         state = 1 + std::max(fit, 0);
-        if (tracked) known[dev][split].store(state, std::memory_order_release);
+        if (tracked) known[dev][size].store(state, std::memory_order_release);
     }
     *clusters = state - 1;
     return KGE_OK;
 }
 
-struct ProductPlan { int form, split; };
+struct ProductPlan { int form, split; };          // split: CTAs that share a tile's K; pairs of CTAs that run at a time (TWO)
 int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) {
-    const int64_t tiles128 = ceil_div(M, I8_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, I8_BM) * ceil_div(N, 256);
+    const int64_t tiles128 = ceil_div(M, I8_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, 256) * ceil_div(N, 256);
     for (int most = (int)std::min<int64_t>({I8_MAX_SPLIT, kblocks, sms / tiles128}); most > 1; --most) {
         const int per = (kblocks + most - 1) / most, split = (kblocks + per - 1) / per;          // every CTA has a block
         if (128 * (kblocks - per - 1) <= 5 * std::min<int64_t>(M, I8_BM)) break;
         int room = 0;
-        const int rc = split_clusters(split, &room);
+        const int rc = clusters_at_a_time<I8_SPLIT>(split, &room);
         if (rc != KGE_OK) return rc;
         if (tiles128 <= room) { *plan = {I8_SPLIT, split}; return KGE_OK; }
     }
-    if (tiles256 >= sms && kblocks >= 16) { *plan = {I8_WIDE, 1}; return KGE_OK; }
+    if (kblocks >= 8) {
+        int room = 0;
+        const int rc = clusters_at_a_time<I8_TWO>(2, &room);
+        if (rc != KGE_OK) return rc;
+        if (room > 0 && tiles256 >= room) { *plan = {I8_TWO, (int)std::min<int64_t>(room, tiles256)}; return KGE_OK; }
+    }
     const int64_t pair = ceil_div(tiles128, 2 * sms) * 256, narrow = ceil_div(ceil_div(M, I8_BM) * ceil_div(N, 64), 3 * sms) * 192;
     *plan = {narrow < pair ? I8_NARROW : I8_PAIR, 1};
     return KGE_OK;
@@ -474,17 +530,17 @@ int launch_product(const CUtensorMap& a, const CUtensorMap& b, IntProductParams&
     const int rc = configure_product<FORM>();
     if (rc != KGE_OK) return rc;
     p.tiles_n = (int)ceil_div(p.N, i8_bn(FORM));
-    p.items = (int)(ceil_div(p.M, I8_BM) * p.tiles_n);
-    p.kper = (p.kblocks + split - 1) / split;
+    p.items = (int)(ceil_div(p.M, FORM == I8_TWO ? 2 * I8_BM : I8_BM) * p.tiles_n);
+    p.kper = FORM == I8_SPLIT ? (p.kblocks + split - 1) / split : p.kblocks;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(FORM == I8_SPLIT ? p.items * split : std::min<int64_t>(p.items, (int64_t)sms * i8_ctas_per_sm(FORM))));
+    cfg.gridDim = dim3((unsigned)(FORM == I8_SPLIT ? p.items * split : (FORM == I8_TWO ? 2 * split : std::min<int64_t>(p.items, (int64_t)sms * i8_ctas_per_sm(FORM)))));
     cfg.blockDim = dim3(i8_threads(FORM)); cfg.dynamicSmemBytes = smem; cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = FORM == I8_SPLIT ? 2 : 1;
+    attr[1].val.clusterDim.x = (unsigned)(FORM == I8_TWO ? 2 : split); attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = FORM == I8_SPLIT || FORM == I8_TWO ? 2 : 1;
     return launch_status(cudaLaunchKernelEx(&cfg, int8_product_kernel<FORM>, a, b, p));
 }
 
@@ -534,11 +590,11 @@ int kge_int8_matmul(const void* a, int64_t lda, const float* a_scales, const voi
     rc = operand_map(&ma, a, M, K, lda, I8_BM);
     if (rc == KGE_OK) rc = operand_map(&mb, b, N, K, ldb, i8_box_rows(plan.form));
     if (rc != KGE_OK) return rc;
-    p.idesc = i8_idesc(I8_BM, i8_bn(plan.form));
+    p.idesc = i8_idesc(plan.form == I8_TWO ? 2 * I8_BM : I8_BM, i8_bn(plan.form));
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     switch (plan.form) {
         case I8_SPLIT: return launch_product<I8_SPLIT>(ma, mb, p, plan.split, sms, s);
-        case I8_WIDE: return launch_product<I8_WIDE>(ma, mb, p, 1, sms, s);
+        case I8_TWO: return launch_product<I8_TWO>(ma, mb, p, plan.split, sms, s);
         case I8_NARROW: return launch_product<I8_NARROW>(ma, mb, p, 1, sms, s);
         default: return launch_product<I8_PAIR>(ma, mb, p, 1, sms, s);
     }
