@@ -181,42 +181,65 @@ __device__ __forceinline__ void i8_mma_pair(uint32_t d, uint64_t a, uint64_t b, 
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// A sum times its two scales, the smaller one first: |x| >= 1 keeps that product a normal number where the scale is one, and it leaves the
-// range upwards only where the result does.  (The sum's own rounding to fp32 is half a step of 24 bits.)
-__device__ __forceinline__ float scaled(int x, float a, float b) { return (float)x * fminf(a, b) * fmaxf(a, b); }
-// (fminf and fmaxf drop a NaN: a row that stands for NaN has an infinite or a NaN scale, and this looks after it.)
-__device__ __forceinline__ float scaled_any(int x, float a, float b) {
-    const float y = scaled(x, a, b);
+// A sum times its two scales (the sum's own rounding to fp32 is half a step of 24 bits).  Scales between 2^-63 and 2^63 are multiplied one after the other: no
+// intermediate value leaves the normal numbers.  Others too, the smaller one first: |x| >= 1 keeps that product a normal number where the scale is one, and it leaves the
+// range upwards only where the result does.  (fminf and fmaxf drop a NaN: a row that stands for NaN has an infinite or a NaN scale.)
+__device__ __forceinline__ bool near_one(float s) { return __float_as_uint(s) - 0x20000000u <= 0x3F000000u; }
+__device__ __forceinline__ float scaled_far(int x, float a, float b) {
+    const float y = (float)x * fminf(a, b) * fmaxf(a, b);
     return a != a || b != b ? a + b : y;
 }
 
-// A warp's 32 rows x 64 columns: 128 bytes of each row at a time from tensor memory through shared memory, so that a store instruction covers whole lines.
-template <typename TO, class F>
+// A warp's 32 rows x 64 columns: 128 bytes of each row at a time from tensor memory through shared memory, so that a store instruction covers whole lines.  The
+// next sixteen columns' sums are on their way while sixteen are scaled.
+template <typename TO, bool NEAR, bool ADD, class F>
 __device__ __forceinline__ void i8_store(const IntProductParams& p, int row0, int col0, uint32_t from, float sa, const float* sb, float4* st, int lane, F&& read_all) {
     constexpr int V = 16 / sizeof(TO), PASS = 128 / sizeof(TO);
     const bool inside = p.vec && row0 + 32 <= p.M && col0 + OUT_COLS <= p.N;
+    uint32_t v[2][16];
+    tmem_ld16(from, v[0]);
 #pragma unroll
     for (int c = 0; c < OUT_COLS; c += PASS) {
-        if (p.addend) {
+        if (ADD) {
             if (c > 0) out_fetch_addend<TO>(p, row0, col0, c, st, lane);
             asm volatile("cp.async.wait_all;" ::: "memory");
             __syncwarp();
         }
 #pragma unroll
         for (int h = 0; h < PASS; h += 16) {
-            uint32_t v[16];
-            tmem_ld16(from + c + h, v);
-            tmem_wait16(v);
-            if (c + h + 16 == OUT_COLS) read_all();
+            const int at16 = (c + h) / 16;
+            tmem_wait16(v[at16 & 1]);
+            uint32_t x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = v[at16 & 1][i];
+            if (at16 + 1 < OUT_COLS / 16) tmem_ld16(from + 16 * (at16 + 1), v[(at16 + 1) & 1]);
+            else read_all();
 #pragma unroll
             for (int i = 0; i < 16 / V; ++i) {
                 float4* const at = st + lane * 8 + ((h / V + i) ^ (lane & 7));
                 Pack<TO, V> o;
-                if (p.addend) o = *reinterpret_cast<const Pack<TO, V>*>(at);
+                if (ADD) o = *reinterpret_cast<const Pack<TO, V>*>(at);
+                float y[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float x = scaled_any((int)v[i * V + e], sa, sb[c + h + i * V + e]);
-                    o.v[e] = from_float<TO>(p.addend ? x + to_float(o.v[e]) : x);
+                for (int e = 0; e < V; e += 4) {
+                    const float4 b = *reinterpret_cast<const float4*>(sb + c + h + i * V + e);
+                    const float bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int sum = (int)x[i * V + e + k];
+                        y[e + k] = NEAR ? (float)sum * sa * bs[k] : scaled_far(sum, sa, bs[k]);
+                        if (ADD) y[e + k] += to_float(o.v[e + k]);
+                    }
+                }
+                if constexpr (sizeof(TO) == 4) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) o.v[e] = y[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; e += 2) {
+                        if constexpr (std::is_same<TO, __nv_bfloat16>::value) *reinterpret_cast<__nv_bfloat162*>(&o.v[e]) = __floats2bfloat162_rn(y[e], y[e + 1]);
+                        else *reinterpret_cast<__half2*>(&o.v[e]) = __floats2half2_rn(y[e], y[e + 1]);
+                    }
                 }
                 *at = *reinterpret_cast<const float4*>(&o);
             }
@@ -263,7 +286,7 @@ __device__ __forceinline__ void i8_join(const IntProductParams& p, uint32_t part
         Pack<TO, 4> o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x = col + e < p.N ? scaled_any(sum[e], sa, p.sb[col + e]) : 0.f;
+            const float x = col + e < p.N ? scaled_far(sum[e], sa, p.sb[col + e]) : 0.f;
             o.v[e] = from_float<TO>(p.addend && col + e < p.N ? x + to_float(add[e]) : x);
         }
         out_put<TO, 4>(p, row, col, o);
@@ -384,15 +407,22 @@ __global__ void __launch_bounds__(i8_threads(FORM), i8_ctas_per_sm(FORM)) int8_p
         bool ok = true;
         for (int item = first; item < p.items && ok; item += step) {
             const int m0 = item / p.tiles_n * TILE_M + (TWO ? (int)rank * I8_BM : 0) + quarter * 32, nt = item % p.tiles_n * BN;
-            float sa = 0.f;
+            float sa = 1.f;
+            bool near = true;
             auto begin = [&](int n0) {              // what a group of columns needs beside the sums
+                near = near_one(sa);
 #pragma unroll
-                for (int i = 0; i < OUT_COLS; i += 32) sb[i + lane] = n0 + i + lane < p.N ? __ldg(p.sb + n0 + i + lane) : 0.f;
+                for (int i = 0; i < OUT_COLS; i += 32) {
+                    const float s = n0 + i + lane < p.N ? __ldg(p.sb + n0 + i + lane) : 1.f;
+                    near &= near_one(s);
+                    sb[i + lane] = s;
+                }
+                near = __all_sync(0xffffffffu, near);
                 if (p.addend) with_out_type(p.out_type, [&](auto t) { out_fetch_addend<decltype(t)>(p, m0, n0, 0, st, lane); });
                 __syncwarp();
             };
             if (!SPLIT) {
-                sa = m0 + lane < p.M ? __ldg(p.sa + m0 + lane) : 0.f;
+                sa = m0 + lane < p.M ? __ldg(p.sa + m0 + lane) : 1.f;
                 begin(nt + first_group * OUT_COLS);
             }
             ok = __all_sync(0xffffffffu, mbar_wait_bounded(&acc_full[buf], phase, p.wait_limit)) && !*stop;
@@ -425,7 +455,15 @@ __global__ void __launch_bounds__(i8_threads(FORM), i8_ctas_per_sm(FORM)) int8_p
                             else mbar_arrive(&acc_empty[buf]);
                         }
                     };
-                    with_out_type(p.out_type, [&](auto t) { i8_store<decltype(t)>(p, m0, nt + col, taddr + buf * BN + col, sa, sb, st, lane, read_all); });
+                    with_out_type(p.out_type, [&](auto t) {
+                        using TO = decltype(t);
+                        const uint32_t from = taddr + buf * BN + col;
+                        if (!near) {
+                            if (p.addend) i8_store<TO, false, true>(p, m0, nt + col, from, sa, sb, st, lane, read_all);
+                            else i8_store<TO, false, false>(p, m0, nt + col, from, sa, sb, st, lane, read_all);
+                        } else if (p.addend) i8_store<TO, true, true>(p, m0, nt + col, from, sa, sb, st, lane, read_all);
+                        else i8_store<TO, true, false>(p, m0, nt + col, from, sa, sb, st, lane, read_all);
+                    });
                 }
             }
             if (++buf == I8_NACC) { buf = 0; phase ^= 1; }
@@ -502,6 +540,12 @@ template <int FORM> int clusters_at_a_time(int size, int* clusters) {
 }
 
 struct ProductPlan { int form, split; };          // split: CTAs that share a tile's K; pairs of CTAs that run at a time (TWO)
+// How a product is cut up.
+//   shared K      as many CTAs to a tile as run at a time, where the blocks that a CTA is spared outweigh the join: a block takes 0.4 us, the join 0.4 + 2 for 128 rows
+//                 (16 x 4,096 x 4,096: four CTAs to each of 32 tiles, 9.3 us)
+//   256 x 256     on pairs of CTAs where those tiles fill the pairs and K is long enough for its MMAs to cover the stores of the tile before: 8,192 x 4,096 x 8,192
+//                 174 us, in tiles of 128 x 256 on one CTA 213; 16,384 x 8,192 x 512 101 us, in tiles of 128 x 128 112; 8,192 x 4,096 x 256 30 and 22
+//   128 or 64 columns   two or three CTAs an SM: what counts is how well whole rounds of tiles fill the SMs
 int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) {
     const int64_t tiles128 = ceil_div(M, I8_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, 256) * ceil_div(N, 256);
     for (int most = (int)std::min<int64_t>({I8_MAX_SPLIT, kblocks, sms / tiles128}); most > 1; --most) {
@@ -512,7 +556,7 @@ int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) 
         if (rc != KGE_OK) return rc;
         if (tiles128 <= room) { *plan = {I8_SPLIT, split}; return KGE_OK; }
     }
-    if (kblocks >= 8) {
+    if (kblocks >= 4) {
         int room = 0;
         const int rc = clusters_at_a_time<I8_TWO>(2, &room);
         if (rc != KGE_OK) return rc;
