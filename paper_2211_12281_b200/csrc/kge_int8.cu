@@ -544,7 +544,8 @@ struct ProductPlan { int form, split; };          // split: CTAs that share a ti
 //   shared K      as many CTAs to a tile as run at a time, where the blocks that a CTA is spared outweigh the join: a block takes 0.4 us, the join 0.4 + 2 for 128 rows
 //                 (16 x 4,096 x 4,096: four CTAs to each of 32 tiles, 9.3 us)
 //   256 x 256     on pairs of CTAs where those tiles fill the pairs and K is long enough for its MMAs to cover the stores of the tile before: 8,192 x 4,096 x 8,192
-//                 174 us, in tiles of 128 x 256 on one CTA 213; 16,384 x 8,192 x 512 101 us, in tiles of 128 x 128 112; 8,192 x 4,096 x 256 30 and 22
+//                 174 us, in tiles of 128 x 256 on one CTA 213; 16,384 x 8,192 x 512 101 us, in tiles of 128 x 128 112; 8,192 x 4,096 x 256 30 and 22; and, where K is
+//                 short, whole rounds of tiles are seven tenths full (24,576 x 256 x 768 after its quantisation, 96 tiles for 74 pairs: 29 us, in tiles of 128 x 64 26)
 //   128 or 64 columns   two or three CTAs an SM: what counts is how well whole rounds of tiles fill the SMs
 int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) {
     const int64_t tiles128 = ceil_div(M, I8_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, 256) * ceil_div(N, 256);
@@ -560,7 +561,7 @@ int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) 
         int room = 0;
         const int rc = clusters_at_a_time<I8_TWO>(2, &room);
         if (rc != KGE_OK) return rc;
-        if (room > 0 && tiles256 >= room) { *plan = {I8_TWO, (int)std::min<int64_t>(room, tiles256)}; return KGE_OK; }
+        if (room > 0 && tiles256 >= room && (kblocks >= 16 || 10 * tiles256 >= 7 * room * ceil_div(tiles256, room))) { *plan = {I8_TWO, (int)std::min<int64_t>(room, tiles256)}; return KGE_OK; }
     }
     const int64_t pair = ceil_div(tiles128, 2 * sms) * 256, narrow = ceil_div(ceil_div(M, I8_BM) * ceil_div(N, 64), 3 * sms) * 192;
     *plan = {narrow < pair ? I8_NARROW : I8_PAIR, 1};

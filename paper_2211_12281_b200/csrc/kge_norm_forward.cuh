@@ -63,9 +63,14 @@ __device__ __forceinline__ void store_z8(int8_t* out, const Place<WIDE>& at, con
 // elements a thread (32,768 x 4,096 bf16 with a thread for eight elements: 53 instructions an element, so 26).  Narrow rows take one pack a thread instead, the next row's
 // loads under way: few rows are in an SM's hands then, and it waits for them (24,576 x 200: 16 us with two packs, %s).
 constexpr int norm_threads(int l, bool wide) { return l == 0 && !wide ? 2 * NORM_THREADS : NORM_THREADS; }
-constexpr int norm_ctas(int l, int k, bool wide, int bytes) { return l == 0 && !wide ? 1 : (k == 1 || (k == 2 && wide && bytes <= 6) ? 3 : (k > 2 && bytes > 6 ? 1 : 2)); }
-template <typename TX, typename TB, int L, int K, bool WIDE, bool LAYER>
-__global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, sizeof(TX) + sizeof(TB))) norm_kernel(const __grid_constant__ NormParams p) {
+// CTAs on an SM, and so registers a thread; rows that are only normalised (Y = false) need few.
+constexpr int norm_ctas(int l, int k, bool wide, int x_bytes, int block_bytes, bool y) {
+    if (!y && (wide || l > 0)) return k == 1 || (x_bytes == 2 && wide) ? 4 : (k == 2 ? 3 : 2);
+    if (l == 0 && !wide) return 1;
+    return (k == 1 || (k == 2 && wide && x_bytes + block_bytes <= 6) ? 3 : (k > 2 && x_bytes + block_bytes > 6 ? 1 : 2));
+}
+template <typename TX, typename TB, int L, int K, bool WIDE, bool LAYER, bool Y>
+__global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, sizeof(TX), sizeof(TB), Y)) norm_kernel(const __grid_constant__ NormParams p) {
     constexpr bool AHEAD = K == 1;
     __shared__ float parts[2][2][32];
     Team<L> team(parts);
@@ -81,7 +86,7 @@ __global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, s
         const int64_t r = L == 0 ? row : min(row, (int64_t)p.n - 1);
 #pragma unroll
         for (int k = 0; k < K; ++k) v.x[k] = at[k].load(static_cast<const TX*>(p.x) + r * p.ldx);
-        if (p.y) {
+        if (Y) {
 #pragma unroll
             for (int k = 0; k < K; ++k) v.y[k] = at[k].load(static_cast<const TB*>(p.y) + r * p.ldy);
             if (p.gate) {
@@ -105,7 +110,7 @@ __global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, s
                 now = next;
                 if (r0 + step < p.n) load(mine + step, next);
             } else load(mine, now);
-            if (p.y) {
+            if (Y) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) u[k] = wide_of(now.y[k]);
                 if (p.post) {
@@ -233,13 +238,25 @@ __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_loop_kernel(const __gr
 }
 
 // As many CTAs as run at a time, or fewer, so that each has as many rows as the others.
-template <typename TX, typename TB, int L, int K, bool WIDE>
+template <typename TX, typename TB, int L, int K, bool WIDE, bool Y>
 int launch_rows(const NormParams& p, int threads, int sms, cudaStream_t s) {
-    constexpr int bytes = sizeof(TX) + sizeof(TB), regs = K == 1 || (K == 2 && WIDE && bytes <= 6) ? 80 : (WIDE && K > 2 && bytes > 6 ? 208 : 128);          // (as compiled, at most)
-    const int64_t all = ceil_div(p.n, Team<L>::COUNT), room = (int64_t)sms * (65536 / (regs * threads)), turns = ceil_div(all, room);
+    constexpr int ctas = norm_ctas(L, K, WIDE, sizeof(TX), sizeof(TB), Y), regs = ctas == 1 ? (WIDE ? 240 : 128) : 65536 / (ctas * NORM_THREADS) / 8 * 8;          // (at most)
+    const int64_t all = ceil_div(p.n, Team<L>::COUNT), room = (int64_t)sms * std::max(1, 65536 / (regs * threads)), turns = ceil_div(all, room);
     const dim3 grid((unsigned)ceil_div(all, turns)), block((unsigned)threads);
-    return launch_status(p.layer ? launch_dependent(norm_kernel<TX, TB, L, K, WIDE, true>, grid, block, 0, s, p)
-                                 : launch_dependent(norm_kernel<TX, TB, L, K, WIDE, false>, grid, block, 0, s, p));
+    return launch_status(p.layer ? launch_dependent(norm_kernel<TX, TB, L, K, WIDE, true, Y>, grid, block, 0, s, p)
+                                 : launch_dependent(norm_kernel<TX, TB, L, K, WIDE, false, Y>, grid, block, 0, s, p));
+}
+
+template <typename TX, typename TB, bool Y>
+int launch_wide(const NormParams& p, int sms, cudaStream_t s) {
+    const int d = p.d, cta = (int)ceil_div(d, 1024) * 32;          // threads of a CTA that holds a row, 32 elements each
+    if (d <= 64) return launch_rows<TX, TB, 8, 1, true, Y>(p, NORM_THREADS, sms, s);
+    if (d <= 128) return launch_rows<TX, TB, 16, 1, true, Y>(p, NORM_THREADS, sms, s);
+    if (d <= 256) return launch_rows<TX, TB, 32, 1, true, Y>(p, NORM_THREADS, sms, s);
+    if (d <= 512) return launch_rows<TX, TB, 32, 2, true, Y>(p, NORM_THREADS, sms, s);
+    if (d <= 768) return launch_rows<TX, TB, 32, 3, true, Y>(p, NORM_THREADS, sms, s);
+    if (d <= 1024) return launch_rows<TX, TB, 32, 4, true, Y>(p, NORM_THREADS, sms, s);
+    return d <= 24 * cta ? launch_rows<TX, TB, 0, 3, true, Y>(p, cta, sms, s) : launch_rows<TX, TB, 0, 4, true, Y>(p, cta, sms, s);
 }
 
 template <typename TX, typename TB>
@@ -248,19 +265,14 @@ int launch_norm(const NormParams& p, cudaStream_t s) {
     const int rc = sm_count(&sms), d = p.d;
     if (rc != KGE_OK) return rc;
     if (d > NORM_MOST) return launch_status(launch_dependent(norm_loop_kernel<TX, TB>, dim3((unsigned)p.n), dim3(NORM_LOOP_THREADS), 0, s, p));
-    const int cta = (int)ceil_div(d, 1024) * 32;          // threads of a CTA that holds a row, 32 elements each
-    if (!p.wide) {
-        if (d <= 256) return launch_rows<TX, TB, 32, 1, false>(p, NORM_THREADS, sms, s);
-        if (d <= 512) return launch_rows<TX, TB, 32, 2, false>(p, NORM_THREADS, sms, s);
-        return launch_rows<TX, TB, 0, 2, false>(p, (int)ceil_div(d, 512) * 32, sms, s);
-    }
-    if (d <= 64) return launch_rows<TX, TB, 8, 1, true>(p, NORM_THREADS, sms, s);
-    if (d <= 128) return launch_rows<TX, TB, 16, 1, true>(p, NORM_THREADS, sms, s);
-    if (d <= 256) return launch_rows<TX, TB, 32, 1, true>(p, NORM_THREADS, sms, s);
-    if (d <= 512) return launch_rows<TX, TB, 32, 2, true>(p, NORM_THREADS, sms, s);
-    if (d <= 768) return launch_rows<TX, TB, 32, 3, true>(p, NORM_THREADS, sms, s);
-    if (d <= 1024) return launch_rows<TX, TB, 32, 4, true>(p, NORM_THREADS, sms, s);
-    return d <= 24 * cta ? launch_rows<TX, TB, 0, 3, true>(p, cta, sms, s) : launch_rows<TX, TB, 0, 4, true>(p, cta, sms, s);
+    if (p.wide) return p.y ? launch_wide<TX, TB, true>(p, sms, s) : launch_wide<TX, TB, false>(p, sms, s);
+    auto rows = [&](auto y) {
+        constexpr bool Y = decltype(y)::value;
+        if (d <= 256) return launch_rows<TX, TB, 32, 1, false, Y>(p, NORM_THREADS, sms, s);
+        if (d <= 512) return launch_rows<TX, TB, 32, 2, false, Y>(p, NORM_THREADS, sms, s);
+        return launch_rows<TX, TB, 0, 2, false, Y>(p, (int)ceil_div(d, 512) * 32, sms, s);
+    };
+    return p.y ? rows(std::true_type()) : rows(std::false_type());
 }
 
 }  // namespace
