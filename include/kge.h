@@ -472,7 +472,7 @@ int kge_int8_matmul(const void* a, int64_t lda, const float* a_scales, const voi
  *                      (accumulate = 1).  x, y, gate and the vectors are the forward pass's, stats what it left.  scratch: kge_block_norm_grad_scratch_bytes(n, d)
  *                      bytes, 256-byte aligned, where a vector's gradient is asked for; calls that may overlap need one each.
  * h, z, dx, dy, dgate may be one of the call's inputs of the same type whose rows lie at the same distance; they overlap nothing otherwise.
- * Rows of more than 8,192 (gradients: 4,096) columns are read from cache several times.
+ * Rows of more than 8,192 columns are read from cache several times.
  */
 typedef struct {
     const void *x, *y, *gate;

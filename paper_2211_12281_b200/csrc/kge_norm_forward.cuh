@@ -55,13 +55,13 @@ __device__ __forceinline__ void store_z8(int8_t* out, const Place<WIDE>& at, con
         if (at.any) *reinterpret_cast<uint2*>(at.mine(out)) = w;
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (at.holds(e)) out[at.at(e)] = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+        for (int e = 0; e < 8; ++e) if (at.holds(e)) *at.mine(out, e) = (int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
     }
 }
 
 // A team of L threads (L = 0: the CTA) holds a row, K packs of eight elements to a thread: the row's addresses, sums and scalars are shared out over up to 32
 // elements a thread (32,768 x 4,096 bf16 with a thread for eight elements: 53 instructions an element, so 26).  Narrow rows take one pack a thread instead, the next row's
-// loads under way: few rows are in an SM's hands then, and it waits for them (24,576 x 200: 16 us with two packs, %s).
+// loads under way: few rows are in an SM's hands then, and it waits for them (24,576 x 200: 16.3 us with two packs, 14.2).
 constexpr int norm_threads(int l, bool wide) { return l == 0 && !wide ? 2 * NORM_THREADS : NORM_THREADS; }
 // CTAs on an SM, and so registers a thread; rows that are only normalised (Y = false) need few.
 constexpr int norm_ctas(int l, int k, bool wide, int x_bytes, int block_bytes, bool y) {
@@ -268,6 +268,7 @@ int launch_norm(const NormParams& p, cudaStream_t s) {
     if (p.wide) return p.y ? launch_wide<TX, TB, true>(p, sms, s) : launch_wide<TX, TB, false>(p, sms, s);
     auto rows = [&](auto y) {
         constexpr bool Y = decltype(y)::value;
+        if (d <= 64) return launch_rows<TX, TB, 8, 1, false, Y>(p, NORM_THREADS, sms, s);
         if (d <= 256) return launch_rows<TX, TB, 32, 1, false, Y>(p, NORM_THREADS, sms, s);
         if (d <= 512) return launch_rows<TX, TB, 32, 2, false, Y>(p, NORM_THREADS, sms, s);
         return launch_rows<TX, TB, 0, 2, false, Y>(p, (int)ceil_div(d, 512) * 32, sms, s);

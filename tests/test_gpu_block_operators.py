@@ -173,6 +173,9 @@ NORM_CASES = [
     (700, 2048, "bf16", "bf16", "both", True, "sigmoid", True, False, "rms"), (6, 4095, "f16", "f16", "both", True, "sigmoid", True, True, "layer"),
     (5, 4096, "f32", "f32", "both", True, "silu", True, True, "layer"), (4, 4104, "f32", "bf16", "both", True, "silu", True, True, "layer"),
     (3, 8192, "bf16", "bf16", "both", True, "plain", True, False, "rms"), (2, 8193, "f32", "f16", "both", True, "sigmoid", True, True, "layer"),
+    (70, 96, "bf16", "bf16", "both", True, "silu", True, False, "rms"), (11, 768, "bf16", "f16", "both", True, "sigmoid", True, True, "layer"), (40, 704, "f32", "f32", "both", True, "silu", True, False, "rms"),
+    (9, 1200, "f32", "bf16", "both", False, "plain", True, True, "layer"), (160, 1600, "bf16", "bf16", "both", True, "none", False, False, "rms"), (5, 5001, "bf16", "f32", "both", True, "silu", True, True, "layer"),
+    (300, 5000, "bf16", "bf16", "both", True, "sigmoid", True, False, "rms"), (2, 6144, "f32", "f32", "post", True, "plain", True, False, "layer"),
     (3, 20_000, "bf16", "f32", "both", True, "silu", True, True, "rms"), (2, 9000, "f16", "f16", "pre", False, "none", False, True, "layer")]
 LAYOUTS = [(0, 0), (8, 8), (3, 1)]
 
@@ -254,6 +257,29 @@ def test_block_norm_grad(T, K, n, d, tx, tb, form, post, gate, scale, bias, kind
         # in place of the operands
         call({k: f[of[k]] for k in got if k in ("dx", "dy", "dgate")})
         assert all(T.equal(f[of[k]], got[k]) for k in got if k in ("dx", "dy", "dgate"))
+
+
+@pytest.mark.parametrize("d", [64, 256, 1024, 4096])
+def test_block_norm_takes_vectors_that_start_anywhere(T, K, d):
+    """Vectors between multiples of 16 bytes, beside rows that are not: within the roundings of the aligned ones."""
+    n, g = 33, _gen(T, d)
+    f = _inputs(T, g, n, d, "bf16", "bf16", "both", True, "silu", True, True)
+    dz = T.randn((n, d), generator=g, device="cuda").to(T.bfloat16)
+    for k in ("w1", "b1", "scale", "w2", "b2"):
+        f[k] = T.cat([f[k][:1], f[k]])[1:]
+        assert f[k].data_ptr() % 16 == 4
+    o = _block64(T, _double(f), "silu", float(np.float32(1e-6)), 1.0, d)
+    z, h, stats = T.empty_like(f["y"]), T.empty_like(f["x"]), T.empty((n, 4), device="cuda")
+    args = dict(pre_weight=f["w2"], y=f["y"], gate=f["gate"], gate_act="silu", post_weight=f["w1"], post_bias=f["b1"], scale=f["scale"], kind="layer")
+    K.block_norm(f["x"], z=z, h=h, pre_bias=f["b2"], stats=stats, **args)
+    _check(T, z, o["z"].v, 1.05 * o["z"].tol, "z")
+    _check(T, h, o["h"].v, 1.05 * o["h"].tol, "h")
+    want = _block_grad64(T, _double(f), o, "silu", 1.0, d, dz.double(), None)
+    out = T.zeros(5 * d + 1, device="cuda")[1:].view(5, d)
+    dy = T.empty_like(f["y"])
+    K.block_norm_grad(f["x"], stats, dz=dz, dy=dy, dpost_weight=out[0], dpost_bias=out[1], dscale=out[2], dpre_weight=out[3], dpre_bias=out[4], **args)
+    for got, k in ((dy, "dy"), (out[0], "dw1"), (out[1], "db1"), (out[2], "dscale"), (out[3], "dw2"), (out[4], "db2")):
+        _check(T, got, want[k].v, 1.05 * want[k].tol, k)
 
 
 @pytest.mark.parametrize("kind,act", [("rms", "plain"), ("layer", "sigmoid"), ("layer", "silu")])
