@@ -7,6 +7,7 @@ if the shared library is missing or cannot be loaded, importing the symbols rais
 """
 from __future__ import annotations
 
+import bisect
 import ctypes as C
 import struct
 from pathlib import Path
@@ -590,8 +591,9 @@ class AdamW:
             _load_torch()
         self._at = (KgeAdamwTensor * max(count, 1))()
         self._count, self._dev, self.bits = count, -1, 32
-        self._keep = (params, lists)
+        self._keep, self._spans, self._ends = (params, lists), [], []
         if count == 0:
+            self.set_grads(grads)
             return
         self.bits = 32 if lists["m"][0] is not None and lists["m"][0].dtype is _torch.float32 else 8
         self._dev = params[0].get_device()
@@ -625,7 +627,7 @@ class AdamW:
         spans.sort()
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise _bad(w, "two of the tensors overlap")
-        self._spans = spans
+        self._spans, self._ends = spans, [s[1] for s in spans]
         self.set_grads(grads)
 
     def set_grads(self, grads):
@@ -641,7 +643,11 @@ class AdamW:
             code = _type_of(g, w, f"grads[{i}]", _FLOAT)
             if g.numel() != self._at[i].n or not g.is_contiguous() or g.get_device() != self._dev:
                 raise _bad(w, f"grads[{i}] is not a contiguous tensor of {self._at[i].n} elements on the parameters' GPU")
-            at.append((code, g.data_ptr()))
+            begin, end = g.data_ptr(), g.data_ptr() + g.numel() * g.element_size()
+            k = bisect.bisect_left(self._ends, begin + 1)          # the first of the step's results that ends behind the gradient's beginning
+            if begin < end and k < len(self._spans) and self._spans[k][0] < end:
+                raise _bad(w, f"grads[{i}] overlaps a tensor that the step writes")
+            at.append((code, begin))
         for t, (code, ptr) in zip(self._at, at):
             t.grad_type, t.grad = code, ptr
         self._grads = grads

@@ -1,7 +1,6 @@
 // Rows of a residual block in registers: what the norms' forward and backward kernels share.
 //
-// A thread holds eight elements of a row; a row belongs to a team of 8, 16 or 32 lanes of a warp, of two or four warps, or of all warps of a CTA, the
-// least that hold it.
+// A row belongs to a team of 8, 16 or 32 lanes of a warp, of two or four warps, or of all warps of a CTA, whose threads hold packs of eight elements of it.
 #pragma once
 
 #include "kge_eight.cuh"
@@ -10,7 +9,6 @@ namespace kge {
 
 enum { NORM_PLAIN = 0, NORM_SIGMOID = 1, NORM_SILU = 2 };
 constexpr int NORM_THREADS = 256;              // of a CTA of several teams
-constexpr int NORM_CTAS = 3;                   // of these on an SM
 constexpr int NORM_MOST = 8192;                // widest row that a CTA's threads hold
 constexpr int NORM_LOOP_THREADS = 1024;        // of a CTA that goes over wider rows again and again
 
@@ -41,7 +39,8 @@ template <bool WIDE> struct Place {
     __device__ __forceinline__ bool holds(int e) const { return WIDE ? any : at(e) < d; }
     // (a row's address is the same for a warp, and a thread's place in it takes 32 bits: one access, no arithmetic of 64 bits in every thread)
     template <typename T> __device__ __forceinline__ T* mine(T* row, int e = 0) const {
-        return reinterpret_cast<T*>(reinterpret_cast<uintptr_t>(row) + (uint32_t)at(e) * (uint32_t)sizeof(T));
+        using Byte = typename std::conditional<std::is_const<T>::value, const char, char>::type;
+        return reinterpret_cast<T*>(reinterpret_cast<Byte*>(row) + (uint32_t)at(e) * (uint32_t)sizeof(T));
     }
     template <typename T> __device__ __forceinline__ Raw8<T> load(const T* row) const {
         if constexpr (WIDE) return load_wide(mine(row));

@@ -714,6 +714,21 @@ def test_adamw_from_nothing_and_on_device_numbers(T, K, bits):
         assert ((one[0][i] - start[i] * (1 - 0.01 * 0.1) + 0.01 * grads[i].sign()).abs() <= 1e-6 + 0.01 * 1e-8 / grads[i].abs()).all()
 
 
+def test_adamw_refuses_tensors_that_overlap(T, K):
+    flat, g = T.zeros(4096, device="cuda"), T.zeros(1000, device="cuda")
+    p, m, v = flat[:1000], flat[1000:2000], flat[2000:3000]
+    K.AdamW([p], [g], [m], [v]).step(0, 0.1)
+    K.AdamW([p], [flat[3000:4000]], [m], [v]).step(0, 0.1)
+    for bad in (lambda: K.AdamW([p], [g], [flat[999:1999]], [v]), lambda: K.AdamW([p, p], [g, g], [m, flat[3000:4000]], [v, T.zeros(1000, device="cuda")]),
+                lambda: K.AdamW([p], [p], [m], [v]), lambda: K.AdamW([p], [flat[2999:3999]], [m], [v]), lambda: K.AdamW([p], [g], [m], [v]).set_grads([m]),
+                lambda: K.AdamW([p], [g], [m], [v]).set_grads([g, g]), lambda: K.AdamW([], [g], [], []), lambda: K.AdamW([p], [g.double()], [m], [v]),
+                lambda: K.AdamW([p], [g.cpu()], [m], [v])):
+        with pytest.raises(K.KgeError) as e:
+            bad()
+        assert e.value.code == -1
+    K.AdamW([], [], [], []).step(0, 0.1)
+
+
 def test_adamw_rounds_right_on_average(T, K):
     """What a state in 8 bits is on average over elements (and so over steps) is what it would be in 32: within five standard deviations."""
     n = 1 << 20
