@@ -54,10 +54,7 @@ template <class F> __device__ __forceinline__ F8 make8(F&& f) { F8 r;
 #pragma unroll
     for (int e = 0; e < 8; ++e) r.v[e] = f(e);
     return r; }
-__device__ __forceinline__ F8 all8(float x) { return make8([&](int) { return x; }); }
 
-__device__ __forceinline__ F8 fma8(const F8& a, const F8& b, const F8& c) { return make8([&](int e) { return fmaf(a.v[e], b.v[e], c.v[e]); }); }
-__device__ __forceinline__ F8 fma8(const F8& a, float b, const F8& c) { return make8([&](int e) { return fmaf(a.v[e], b, c.v[e]); }); }
 
 __device__ __forceinline__ F8 wide_of(const Raw8<float>& r) { return make8([&](int e) { return __uint_as_float(r.w[e]); }); }
 __device__ __forceinline__ F8 wide_of(const Raw8<__nv_bfloat16>& r) { return make8([&](int e) { return __uint_as_float(e & 1 ? r.w[e >> 1] & 0xFFFF0000u : r.w[e >> 1] << 16); }); }

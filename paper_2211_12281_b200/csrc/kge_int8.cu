@@ -64,7 +64,7 @@ __device__ __noinline__ uint32_t quotient_bits(float x, float s) {
 }
 template <typename T> __device__ __forceinline__ uint2 quantized(const Raw8<T>& r, const QuantScale& s) {
     const F8 x = wide_of(r);
-    F8 t = fma8(x, s.inv, all8(ROUND_TO_INT));
+    F8 t = make8([&](int e) { return fmaf(x.v[e], s.inv, ROUND_TO_INT); });
     bool each = s.each;
     if (sizeof(T) == 4) {
         float far = 0.f;

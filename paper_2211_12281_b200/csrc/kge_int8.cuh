@@ -29,7 +29,7 @@ __device__ __forceinline__ uint2 low_bytes(const F8& t) {
     return w;
 }
 // Integers nearest to the fp32 values times 1 / s, the product exact: within 1/2 + 2^-17 of the true quotients.
-__device__ __forceinline__ uint2 round_products(const F8& x, float inv) { return low_bytes(fma8(x, inv, all8(ROUND_TO_INT))); }
+__device__ __forceinline__ uint2 round_products(const F8& x, float inv) { return low_bytes(make8([&](int e) { return fmaf(x.v[e], inv, ROUND_TO_INT); })); }
 #endif
 
 }  // namespace kge

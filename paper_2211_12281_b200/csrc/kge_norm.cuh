@@ -20,10 +20,34 @@ inline int norm_team(int d) {
 }
 
 #ifdef __CUDACC__
-__device__ __forceinline__ F8 operator*(const F8& a, const F8& b) { return make8([&](int e) { return a.v[e] * b.v[e]; }); }
-__device__ __forceinline__ F8 operator+(const F8& a, const F8& b) { return make8([&](int e) { return a.v[e] + b.v[e]; }); }
-__device__ __forceinline__ F8 operator*(const F8& a, float b) { return make8([&](int e) { return a.v[e] * b; }); }
-__device__ __forceinline__ F8 operator+(const F8& a, float b) { return make8([&](int e) { return a.v[e] + b; }); }
+// Eight fp32 numbers as four pairs: an instruction adds or multiplies two, which leaves the issue slots to the conversions.
+struct P8 { uint64_t v[4]; };
+template <class F> __device__ __forceinline__ P8 make_pairs(F&& f) { P8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = pair(f(2 * i), f(2 * i + 1));
+    return r; }
+__device__ __forceinline__ float element(const P8& a, int e) { const float2 f = unpair(a.v[e >> 1]); return e & 1 ? f.y : f.x; }
+__device__ __forceinline__ P8 all8(float x) { const uint64_t p = pair(x, x); return P8{{p, p, p, p}}; }
+__device__ __forceinline__ P8 operator*(const P8& a, const P8& b) { P8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = mul2(a.v[i], b.v[i]);
+    return r; }
+__device__ __forceinline__ P8 operator+(const P8& a, const P8& b) { P8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = add2(a.v[i], b.v[i]);
+    return r; }
+__device__ __forceinline__ P8 operator*(const P8& a, float b) { return a * all8(b); }
+__device__ __forceinline__ P8 operator+(const P8& a, float b) { return a + all8(b); }
+__device__ __forceinline__ P8 fma8(const P8& a, const P8& b, const P8& c) { P8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = fma2(a.v[i], b.v[i], c.v[i]);
+    return r; }
+__device__ __forceinline__ P8 fma8(const P8& a, float b, const P8& c) { return fma8(a, all8(b), c); }
+template <typename T> __device__ __forceinline__ P8 pairs_of(const Raw8<T>& r) {
+    const F8 x = wide_of(r);
+    return make_pairs([&](int e) { return x.v[e]; });
+}
+__device__ __forceinline__ F8 singles_of(const P8& a) { return make8([&](int e) { return element(a, e); }); }
 
 // Where a thread's elements lie in its row: WIDE rows let eight neighbours move as one access, and all of them or none are there.  What lies beyond the row's end
 // (of a wide row: other elements of it) is left out of sums and stores.
@@ -49,8 +73,8 @@ template <bool WIDE> struct Place {
         for (int e = 0; e < 8; ++e) set_element(r, e, holds(e) ? *mine(row, e) : from_float<T>(0.f));
         return r;
     }
-    template <typename T> __device__ __forceinline__ void store(T* row, const F8& x, bool live) const {
-        const Raw8<T> r = narrow_of<T>(x);
+    template <typename T> __device__ __forceinline__ void store(T* row, const P8& x, bool live) const {
+        const Raw8<T> r = narrow_of<T>(singles_of(x));
         if constexpr (WIDE) { if (any && live) store_wide(mine(row), r); }
         else {
 #pragma unroll
@@ -58,25 +82,27 @@ template <bool WIDE> struct Place {
         }
     }
     // A vector of parameters.  (Loaded here, from the L1 cache: the compiler would keep all of them in registers, and spill others.)
-    __device__ __forceinline__ F8 vector(const float* p) const {
+    __device__ __forceinline__ P8 vector(const float* p) const {
         if constexpr (WIDE) {
             const Pack<float, 8> v = load_now<Pack<float, 8>>(mine(p));
-            return make8([&](int e) { return v.v[e]; });
+            return make_pairs([&](int e) { return v.v[e]; });
         }
-        return make8([&](int e) { return holds(e) ? load_now<Pack<float, 1>>(mine(p, e)).v[0] : 0.f; });
+        return make_pairs([&](int e) { return holds(e) ? load_now<Pack<float, 1>>(mine(p, e)).v[0] : 0.f; });
     }
     // Sums over the thread's elements.
-    __device__ __forceinline__ float total(const F8& a) const {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += WIDE || holds(e) ? a.v[e] : 0.f;
-        return WIDE && !any ? 0.f : s;
+    __device__ __forceinline__ P8 there(const P8& a) const { return WIDE ? a : make_pairs([&](int e) { return holds(e) ? element(a, e) : 0.f; }); }
+    __device__ __forceinline__ float total(const P8& x) const {
+        const P8 a = there(x);
+        const float2 s = unpair(add2(add2(a.v[0], a.v[1]), add2(a.v[2], a.v[3])));
+        return WIDE && !any ? 0.f : s.x + s.y;
     }
-    __device__ __forceinline__ float dot(const F8& a, const F8& b) const {
-        float s = 0.f;
+    __device__ __forceinline__ float dot(const P8& x, const P8& b) const {
+        const P8 a = there(x);
+        uint64_t s = mul2(a.v[0], b.v[0]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s = WIDE || holds(e) ? fmaf(a.v[e], b.v[e], s) : s;
-        return WIDE && !any ? 0.f : s;
+        for (int i = 1; i < 4; ++i) s = fma2(a.v[i], b.v[i], s);
+        const float2 f = unpair(s);
+        return WIDE && !any ? 0.f : f.x + f.y;
     }
 };
 
@@ -150,14 +176,7 @@ __device__ __forceinline__ float sigmoid_of(float g) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return r;
 }
-__device__ __forceinline__ F8 sigmoid_of(const F8& g) { return make8([&](int e) { return sigmoid_of(g.v[e]); }); }
-// act(g) and its derivative, from g and its sigmoid.
-__device__ __forceinline__ F8 act_with(const F8& g, const F8& sigmoid, int act) { return act == NORM_PLAIN ? g : (act == NORM_SIGMOID ? sigmoid : g * sigmoid); }
-__device__ __forceinline__ F8 slope_with(const F8& g, const F8& sigmoid, int act) {
-    if (act == NORM_PLAIN) return all8(1.f);
-    const F8 rest = fma8(sigmoid, -1.f, all8(1.f));
-    return sigmoid * (act == NORM_SIGMOID ? rest : fma8(g, rest, all8(1.f)));
-}
+__device__ __forceinline__ P8 sigmoid_of(const P8& g) { return make_pairs([&](int e) { return sigmoid_of(element(g, e)); }); }
 __device__ __forceinline__ float act_of(float g, int act) { return act == NORM_PLAIN ? g : (act == NORM_SIGMOID ? sigmoid_of(g) : g * sigmoid_of(g)); }
 __device__ __forceinline__ float2 act_and_slope(float g, int act) {
     if (act == NORM_PLAIN) return make_float2(g, 1.f);

@@ -49,9 +49,10 @@ template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y,
 // the last one.)  The vectors enter as sw = s w1, sb = s b1 and w2, which a thread keeps: with q = yn sw + sb
 //   h = x + act q,  dgate = act' q dh',  f = act dh' sw
 // FULL: norms that take a mean, or biases; without them sb, T0 and S0 are not there.
-// AHEAD: the next row's loads are under way where registers hold it too.
+// AHEAD: the next row's loads are under way where registers hold it too.  (Two or three rows ahead, copied into shared memory asynchronously: 16,384 x 4,096 bf16 229
+// instead of 234 us, 8,192 x 4,096 fp32 330 instead of 204, 24,576 x 256 46 instead of 38: it is not memory that they wait for.)
 // SHARED: a CTA of up to 1,024 threads for a row of up to 8,192 columns, whose registers hold neither: the sums are in shared memory, a thread's own places, and the
-// vectors are loaded where they are used (8,192 x 8,192 bf16: 425 us; gone over in three passes 2,284).
+// vectors are loaded where they are used (8,192 x 8,192 bf16: 407 us; gone over in three passes 2,284).
 template <typename TX, typename TB, int L, bool WIDE, bool FULL, bool SHARED>
 __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD / 8 : NORM_THREADS), L == 0 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
     constexpr bool AHEAD = !SHARED && (!FULL || L >= 32) && (!FULL || sizeof(TX) + sizeof(TB) <= 6);
@@ -67,20 +68,19 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
     auto scaled = [&](const float* v) { return p.scale ? at.vector(v) * at.vector(p.scale) : at.vector(v); };
     auto make_sw = [&] { return p.w1 ? scaled(p.w1) : (p.scale ? at.vector(p.scale) : all8(1.f)); };
     auto make_sb = [&] { return FULL && p.b1 ? scaled(p.b1) : all8(0.f); };
-    F8 sw_held, sb_held, w2_held;
+    P8 sw_held, sb_held, w2_held;
     if (!SHARED) { sw_held = make_sw(); sb_held = make_sb(); w2_held = p.w2 ? at.vector(p.w2) : all8(0.f); }
     // T1, S1, T0, S0
-    F8 held[4] = {all8(0.f), all8(0.f), all8(0.f), all8(0.f)};
+    P8 held[4] = {all8(0.f), all8(0.f), all8(0.f), all8(0.f)};
     auto place = [&](int q, int half) { return sums_in_shared + (2 * q + half) * (int)blockDim.x + t; };
-    auto add = [&](int q, const F8& x, const F8& y) {
+    auto add = [&](int q, const P8& x, const P8& y) {
         if (!SHARED) { held[q] = fma8(x, y, held[q]); return; }
         if (q >= p.sums) return;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            float4 s = *place(q, half);
-            s.x = fmaf(x.v[4 * half], y.v[4 * half], s.x); s.y = fmaf(x.v[4 * half + 1], y.v[4 * half + 1], s.y);
-            s.z = fmaf(x.v[4 * half + 2], y.v[4 * half + 2], s.z); s.w = fmaf(x.v[4 * half + 3], y.v[4 * half + 3], s.w);
-            *place(q, half) = s;
+            const float4 s = *place(q, half);
+            const float2 a = unpair(fma2(x.v[2 * half], y.v[2 * half], pair(s.x, s.y))), b = unpair(fma2(x.v[2 * half + 1], y.v[2 * half + 1], pair(s.z, s.w)));
+            *place(q, half) = make_float4(a.x, a.y, b.x, b.y);
         }
     };
     if (SHARED) {
@@ -108,23 +108,23 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
             if (r0 + step < p.n) load(mine + step, next);
         } else load(mine, v);
 
-        F8 dh = p.dh ? wide_of(v.dh) : all8(0.f), yn = all8(0.f), act = all8(1.f);
+        P8 dh = p.dh ? pairs_of(v.dh) : all8(0.f), yn = all8(0.f), act = all8(1.f);
         if (p.y) {
-            yn = wide_of(v.y);
+            yn = pairs_of(v.y);
             if (p.post) yn = FULL ? fma8(yn, v.stats.y, all8(-v.stats.x * v.stats.y)) : yn * v.stats.y;
         }
         // act: the gate, or its sigmoid (of which a silu gate takes the gate's multiple wherever it is used)
-        if (p.gate) act = p.act == NORM_PLAIN ? wide_of(v.gate) : sigmoid_of(wide_of(v.gate));
+        if (p.gate) act = p.act == NORM_PLAIN ? pairs_of(v.gate) : sigmoid_of(pairs_of(v.gate));
         float mean = 0.f, along = 0.f;
         if (p.dz) {
-            F8 h = wide_of(v.x);
+            P8 h = pairs_of(v.x);
             if (p.y) {
-                const F8 sw = SHARED ? make_sw() : sw_held;
-                F8 q = FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw;
-                if (p.gate && p.act == NORM_SILU) q = q * wide_of(v.gate);
+                const P8 sw = SHARED ? make_sw() : sw_held;
+                P8 q = FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw;
+                if (p.gate && p.act == NORM_SILU) q = q * pairs_of(v.gate);
                 h = fma8(q, act, h);
             }
-            const F8 hn = FULL ? fma8(h, v.stats.w, all8(-v.stats.z * v.stats.w)) : h * v.stats.w, dz = wide_of(v.dz), c = dz * (SHARED ? at.vector(p.w2) : w2_held);
+            const P8 hn = FULL ? fma8(h, v.stats.w, all8(-v.stats.z * v.stats.w)) : h * v.stats.w, dz = pairs_of(v.dz), c = dz * (SHARED ? at.vector(p.w2) : w2_held);
             if (live) {
                 add(0, dz, hn);
                 if (FULL) add(2, dz, all8(1.f));
@@ -137,20 +137,20 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
         }
         if (p.dx) at.store(static_cast<TX*>(p.dx) + r * p.ldox, dh, live);
         if (!p.y) continue;
-        const F8 sw = SHARED ? make_sw() : sw_held;
+        const P8 sw = SHARED ? make_sw() : sw_held;
         if (p.dgate) {
-            F8 q = (FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw) * dh;
+            P8 q = (FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw) * dh;
             if (p.act != NORM_PLAIN) {
-                F8 slope = make8([&](int e) { return fmaf(-act.v[e], act.v[e], act.v[e]); });          // s (1 - s), and s + g s (1 - s)
-                if (p.act == NORM_SILU) slope = fma8(wide_of(v.gate), slope, act);
+                P8 slope = act * fma8(act, -1.f, all8(1.f));          // s (1 - s), and s + g s (1 - s)
+                if (p.act == NORM_SILU) slope = fma8(pairs_of(v.gate), slope, act);
                 q = q * slope;
             }
             at.store(static_cast<TB*>(p.dgate) + r * p.ldog, q, live);
         }
-        F8 f = dh;
+        P8 f = dh;
         if (p.gate) {
             f = f * act;
-            if (p.act == NORM_SILU) f = f * wide_of(v.gate);
+            if (p.act == NORM_SILU) f = f * pairs_of(v.gate);
         }
         if (live) {
             add(1, f, yn);
@@ -172,10 +172,10 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
 #pragma unroll
     for (int q = 0; q < (FULL ? 4 : 2); ++q) {
         if (q >= p.sums) break;
-        F8 sum = held[q];
+        P8 sum = held[q];
         if (SHARED) {
             const float4 a = *place(q, 0), b = *place(q, 1);
-            sum = F8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+            sum = P8{{pair(a.x, a.y), pair(a.z, a.w), pair(b.x, b.y), pair(b.z, b.w)}};
         }
         if constexpr (L == 0) {
             at.store(part + (int64_t)q * p.d, sum, true);
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
             constexpr int WIDTH = L * 8;
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) if (at.holds(e)) joined[team.index * WIDTH + at.at(e)] = sum.v[e];
+            for (int e = 0; e < 8; ++e) if (at.holds(e)) joined[team.index * WIDTH + at.at(e)] = element(sum, e);
             __syncthreads();
             for (int i = threadIdx.x; i < p.d; i += NORM_THREADS) {
                 float v = joined[i];

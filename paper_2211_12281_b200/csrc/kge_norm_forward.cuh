@@ -33,7 +33,7 @@ __device__ __forceinline__ float deviation(const NormParams& p, float squares) {
 
 // Takes the mean out of a team's row; returns it and the reciprocal deviation.  Two passes over the registers: a mean far from zero does not eat the deviation's digits.
 template <bool LAYER, int L, int K, bool WIDE>
-__device__ __forceinline__ float2 centre(const NormParams& p, Team<L>& team, F8 (&u)[K], const Place<WIDE> (&at)[K]) {
+__device__ __forceinline__ float2 centre(const NormParams& p, Team<L>& team, P8 (&u)[K], const Place<WIDE> (&at)[K]) {
     float mu = 0.f, sq = 0.f;
     if (LAYER) {
 #pragma unroll
@@ -49,8 +49,8 @@ __device__ __forceinline__ float2 centre(const NormParams& p, Team<L>& team, F8 
 
 // (z is off by its own roundings: what the product with 1 / s adds to them moves an integer only where they do)
 template <bool WIDE>
-__device__ __forceinline__ void store_z8(int8_t* out, const Place<WIDE>& at, const F8& z, const RowScale& s) {
-    const uint2 w = round_products(z, s.inv);
+__device__ __forceinline__ void store_z8(int8_t* out, const Place<WIDE>& at, const P8& z, const RowScale& s) {
+    const uint2 w = round_products(singles_of(z), s.inv);
     if constexpr (WIDE) {
         if (at.any) *reinterpret_cast<uint2*>(at.mine(out)) = w;
     } else {
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, s
         const int64_t mine = r0 + team.index, r = L == 0 ? mine : min(mine, (int64_t)p.n - 1);
         const bool live = L == 0 || mine < p.n;
         float* const stats = p.stats && live && t == 0 ? p.stats + 4 * r : nullptr;
-        F8 u[K];
+        P8 u[K];
         float2 s = make_float2(0.f, 0.f);
         {
             Row now;
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, s
             } else load(mine, now);
             if (Y) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) u[k] = wide_of(now.y[k]);
+                for (int k = 0; k < K; ++k) u[k] = pairs_of(now.y[k]);
                 if (p.post) {
                     s = centre<LAYER>(p, team, u, at);
 #pragma unroll
@@ -125,22 +125,22 @@ __global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, s
                 if (p.gate) {
                     if (p.act == NORM_PLAIN) {
 #pragma unroll
-                        for (int k = 0; k < K; ++k) u[k] = u[k] * wide_of(now.gate[k]);
+                        for (int k = 0; k < K; ++k) u[k] = u[k] * pairs_of(now.gate[k]);
                     } else {
 #pragma unroll
-                        for (int k = 0; k < K; ++k) u[k] = u[k] * sigmoid_of(wide_of(now.gate[k]));
+                        for (int k = 0; k < K; ++k) u[k] = u[k] * sigmoid_of(pairs_of(now.gate[k]));
                         if (p.act == NORM_SILU) {
 #pragma unroll
-                            for (int k = 0; k < K; ++k) u[k] = u[k] * wide_of(now.gate[k]);
+                            for (int k = 0; k < K; ++k) u[k] = u[k] * pairs_of(now.gate[k]);
                         }
                     }
                 }
                 if (p.scale) {
 #pragma unroll
-                    for (int k = 0; k < K; ++k) u[k] = fma8(u[k], at[k].vector(p.scale), wide_of(now.x[k]));
+                    for (int k = 0; k < K; ++k) u[k] = fma8(u[k], at[k].vector(p.scale), pairs_of(now.x[k]));
                 } else {
 #pragma unroll
-                    for (int k = 0; k < K; ++k) u[k] = u[k] + wide_of(now.x[k]);
+                    for (int k = 0; k < K; ++k) u[k] = u[k] + pairs_of(now.x[k]);
                 }
                 if (p.h) {
                     TX* const hs = static_cast<TX*>(p.h) + r * p.ldh;
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, s
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < K; ++k) u[k] = wide_of(now.x[k]);
+                for (int k = 0; k < K; ++k) u[k] = pairs_of(now.x[k]);
             }
         }
         if (stats) *reinterpret_cast<float2*>(stats) = s;
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, s
 #pragma unroll
                 for (int k = 0; k < K; ++k)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) if (at[k].holds(e)) most = Team<L>::template join<true>(most, fabsf(u[k].v[e]));
+                    for (int e = 0; e < 8; ++e) if (at[k].holds(e)) most = Team<L>::template join<true>(most, fabsf(element(u[k], e)));
                 const RowScale q = row_scale(team.most(most));
                 if (live) {
                     if (t == 0) p.z_scales[r] = q.s;
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_loop_kernel(const __gr
 // As many CTAs as run at a time, or fewer, so that each has as many rows as the others.
 template <typename TX, typename TB, int L, int K, bool WIDE, bool Y>
 int launch_rows(const NormParams& p, int threads, int sms, cudaStream_t s) {
-    constexpr int ctas = norm_ctas(L, K, WIDE, sizeof(TX), sizeof(TB), Y), regs = ctas == 1 ? (WIDE ? 240 : 128) : 65536 / (ctas * NORM_THREADS) / 8 * 8;          // (at most)
+    constexpr int ctas = norm_ctas(L, K, WIDE, sizeof(TX), sizeof(TB), Y), regs = ctas == 1 ? (WIDE ? (L == 0 ? 168 : 240) : 128) : 65536 / (ctas * NORM_THREADS) / 8 * 8;          // (at most)
     const int64_t all = ceil_div(p.n, Team<L>::COUNT), room = (int64_t)sms * std::max(1, 65536 / (regs * threads)), turns = ceil_div(all, room);
     const dim3 grid((unsigned)ceil_div(all, turns)), block((unsigned)threads);
     return launch_status(p.layer ? launch_dependent(norm_kernel<TX, TB, L, K, WIDE, true, Y>, grid, block, 0, s, p)
