@@ -299,7 +299,7 @@ extern "C" int kge_adamw(const kge_adamw_tensor* tensors, int32_t count, int32_t
                          double grad_scale, uint64_t step, const int64_t* step_dev, const float* lr_dev, const float* grad_scale_dev, uint64_t seed,
                          void* stream) {
     if (count < 0 || count > (1 << 26) || (count && !tensors) || (state_bits != 32 && state_bits != 8) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) ||
-        !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 1.17549435e-38f) || !std::isfinite((float)eps) || !std::isfinite(grad_scale) || step >= 1ull << 62 || !aligned_to(step_dev, 8) ||
+        !(beta2 >= 0.0 && beta2 < 1.0) || !((float)eps >= 1.17549435e-38f) || !std::isfinite((float)eps) || !std::isfinite((float)grad_scale) || step >= 1ull << 62 || !aligned_to(step_dev, 8) ||
         !aligned_to(lr_dev, 4) || !aligned_to(grad_scale_dev, 4)) return KGE_ERR_BAD_ARG;
     int live = 0;
     int64_t turns = 0;

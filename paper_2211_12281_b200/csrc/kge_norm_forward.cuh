@@ -62,15 +62,15 @@ __device__ __forceinline__ void store_z8(int8_t* out, const Place<WIDE>& at, con
 // A team of L threads (L = 0: the CTA) holds a row, K packs of eight elements to a thread: the row's addresses, sums and scalars are shared out over up to 32
 // elements a thread (32,768 x 4,096 bf16 with a thread for eight elements: 53 instructions an element, so 26).  Narrow rows take one pack a thread instead, the next row's
 // loads under way: few rows are in an SM's hands then, and it waits for them (24,576 x 200: 16.3 us with two packs, 14.2).
-constexpr int norm_threads(int l, bool wide) { return l == 0 && !wide ? 2 * NORM_THREADS : NORM_THREADS; }
+constexpr int norm_threads(int l, int k, bool wide) { return l == 0 && !wide && k > 1 ? 2 * NORM_THREADS : NORM_THREADS; }
 // CTAs on an SM, and so registers a thread; rows that are only normalised (Y = false) need few.
 constexpr int norm_ctas(int l, int k, bool wide, int x_bytes, int block_bytes, bool y) {
-    if (!y && (wide || l > 0)) return k == 1 || (x_bytes == 2 && wide) ? 4 : (k == 2 ? 3 : 2);
-    if (l == 0 && !wide) return 1;
+    if (!y && (wide || l > 0 || k == 1)) return k == 1 || (x_bytes == 2 && wide) ? 4 : (k == 2 ? 3 : 2);
+    if (l == 0 && !wide && k > 1) return 1;
     return (k == 1 || (k == 2 && wide && x_bytes + block_bytes <= 6) ? 3 : (k > 2 && x_bytes + block_bytes > 6 ? 1 : 2));
 }
 template <typename TX, typename TB, int L, int K, bool WIDE, bool LAYER, bool Y>
-__global__ void __launch_bounds__(norm_threads(L, WIDE), norm_ctas(L, K, WIDE, sizeof(TX), sizeof(TB), Y)) norm_kernel(const __grid_constant__ NormParams p) {
+__global__ void __launch_bounds__(norm_threads(L, K, WIDE), norm_ctas(L, K, WIDE, sizeof(TX), sizeof(TB), Y)) norm_kernel(const __grid_constant__ NormParams p) {
     constexpr bool AHEAD = K == 1;
     __shared__ float parts[2][2][32];
     Team<L> team(parts);
@@ -270,7 +270,7 @@ int launch_norm(const NormParams& p, cudaStream_t s) {
         constexpr bool Y = decltype(y)::value;
         if (d <= 64) return launch_rows<TX, TB, 8, 1, false, Y>(p, NORM_THREADS, sms, s);
         if (d <= 256) return launch_rows<TX, TB, 32, 1, false, Y>(p, NORM_THREADS, sms, s);
-        if (d <= 512) return launch_rows<TX, TB, 32, 2, false, Y>(p, NORM_THREADS, sms, s);
+        if (d <= 2048) return launch_rows<TX, TB, 0, 1, false, Y>(p, (int)ceil_div(d, 256) * 32, sms, s);
         return launch_rows<TX, TB, 0, 2, false, Y>(p, (int)ceil_div(d, 512) * 32, sms, s);
     };
     return p.y ? rows(std::true_type()) : rows(std::false_type());
