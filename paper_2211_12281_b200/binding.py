@@ -472,42 +472,50 @@ _GATE_ACTS = {"plain": 0, "sigmoid": 1, "silu": 2}
 _NORM_KINDS = {"rms": 0, "layer": 1}
 
 
-def _like(t, shape, dtype, where, name):
-    """Distance of rows of a matrix of the shape and type given."""
+def _like(t, shape, dtype, dev, where, name):
+    """Distance of rows of a matrix of the shape and type given, on that device."""
     stride = t.stride()
     if t.shape != shape or t.dtype is not dtype or (stride[1] != 1 and shape[1] > 1) or (stride[0] < shape[1] and shape[0] > 1):
         raise _bad(where, f"{name} is not a {list(shape)} matrix of contiguous rows and of type {dtype}")
+    if t.get_device() != dev:
+        raise _bad(where, "tensors are not on one GPU")
     return stride[0] if stride[0] > shape[1] else shape[1]
 
 
-def _vector(v, d, where, name):
-    """Address of a vector of parameters, 0 for None."""
+def _vector(v, d, dev, where, name):
+    """Address of a vector of parameters on the device given, 0 for None."""
     if v is None:
         return 0
     if v.dtype is not _torch.float32 or v.shape != (d,) or not v.is_contiguous():
         raise _bad(where, f"{name} is not a contiguous float32 vector of {d}")
+    if v.get_device() != dev:
+        raise _bad(where, "tensors are not on one GPU")
     return v.data_ptr()
 
 
 def _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, pre_bias, kind):
-    """(kge_norm_block, shape) of the operands: block is a tensor that says what type y, gate and z are of."""
+    """(kge_norm_block, shape, rows, columns, device) of the operands: block is a tensor that says what type y, gate and z are of."""
     n, d, ldx = _matrix(x, w, "x")
-    shape = x.shape
-    tx, tb = _type_of(x, w, "x", _FLOAT), _type_of(block, w, "y, gate, z or dz", _FLOAT)
+    shape, dev, dtype = x.shape, x.get_device(), block.dtype
+    tx, tb = _FLOAT.get(x.dtype), _FLOAT.get(dtype)
+    if tx is None or tb is None:
+        raise _bad(w, f"x has type {x.dtype}, the block's tensors {dtype}")
     act, layer = _GATE_ACTS.get(gate_act), _NORM_KINDS.get(kind)
     if act is None or layer is None:
         raise _bad(w, f"gate_act is one of {list(_GATE_ACTS)}, kind one of {list(_NORM_KINDS)}")
-    return KGE_NORM_BLOCK.pack(x.data_ptr(), 0 if y is None else y.data_ptr(), 0 if gate is None else gate.data_ptr(), _vector(post_weight, d, w, "post_weight"), _vector(post_bias, d, w, "post_bias"),
-                               _vector(scale, d, w, "scale"), _vector(pre_weight, d, w, "pre_weight"), _vector(pre_bias, d, w, "pre_bias"), ldx,
-                               0 if y is None else _like(y, shape, block.dtype, w, "y"), 0 if gate is None else _like(gate, shape, block.dtype, w, "gate"),
-                               tx, tb, act, layer), shape, n, _int32(d, w, "width")
+    if dev < 0:
+        raise _bad(w, "tensors are not on one GPU")
+    return KGE_NORM_BLOCK.pack(x.data_ptr(), 0 if y is None else y.data_ptr(), 0 if gate is None else gate.data_ptr(), _vector(post_weight, d, dev, w, "post_weight"),
+                               _vector(post_bias, d, dev, w, "post_bias"), _vector(scale, d, dev, w, "scale"), _vector(pre_weight, d, dev, w, "pre_weight"),
+                               _vector(pre_bias, d, dev, w, "pre_bias"), ldx, 0 if y is None else _like(y, shape, dtype, dev, w, "y"),
+                               0 if gate is None else _like(gate, shape, dtype, dev, w, "gate"), tx, tb, act, layer), shape, n, _int32(d, w, "width"), dev
 
 
-def _stats_of(stats, n, w):
+def _stats_of(stats, n, dev, w):
     if stats is None:
         return None
-    if stats.dtype is not _torch.float32 or stats.shape != (n, 4) or not stats.is_contiguous():
-        raise _bad(w, f"stats is not a contiguous float32 matrix [{n}, 4]")
+    if stats.dtype is not _torch.float32 or stats.shape != (n, 4) or not stats.is_contiguous() or stats.get_device() != dev:
+        raise _bad(w, f"stats is not a contiguous float32 matrix [{n}, 4] on the operands' GPU")
     return stats.data_ptr()
 
 
@@ -523,20 +531,18 @@ def block_norm(x, z=None, pre_weight=None, pre_bias=None, y=None, h=None, gate=N
         _load_torch()
     z8 = z is not None and z.dtype is _torch.int8
     block = y if y is not None else (x if z8 or z is None else z)
-    b, shape, n, d = _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, pre_bias, kind)
-    ldh = 0 if h is None else _like(h, shape, x.dtype, w, "h")
+    b, shape, n, d, dev = _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, pre_bias, kind)
+    ldh = 0 if h is None else _like(h, shape, x.dtype, dev, w, "h")
     ldz = 0
     if z8:
         _, _, ldz = _int8_operand(z, z_scales, w, "z")
-        if z.shape != shape:
-            raise _bad(w, "z is not of x's shape")
+        if z.shape != shape or z.get_device() != dev or z_scales.get_device() != dev:
+            raise _bad(w, "z is not of x's shape, or it or its scales are not on x's GPU")
     elif z is not None:
-        ldz = _like(z, shape, block.dtype, w, "z")
+        ldz = _like(z, shape, block.dtype, dev, w, "z")
         if z_scales is not None:
             raise _bad(w, "scales are given for a z that is not int8")
-    at = _stats_of(stats, n, w)
-    dev = _device_of(w, x, *[t for t in (y, gate, h, z, post_weight, post_bias, scale, pre_weight, pre_bias, stats, z_scales) if t is not None])
-    _call(w, lib().kge_block_norm, dev, b, n, d, _addr(h), ldh, _addr(z), 1 if z8 else 0, ldz, _addr(z_scales), eps, at)
+    _call(w, lib().kge_block_norm, dev, b, n, d, _addr(h), ldh, _addr(z), 1 if z8 else 0, ldz, _addr(z_scales), eps, _stats_of(stats, n, dev, w))
 
 
 def block_norm_grad_scratch_bytes(n, d) -> int:
@@ -553,19 +559,17 @@ def block_norm_grad(x, stats, dx=None, dz=None, dh=None, pre_weight=None, dpre_w
     if _torch is None:
         _load_torch()
     block = y if y is not None else (dz if dz is not None else x)
-    b, shape, n, d = _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, None, kind)
-    ld = lambda t, like, name: 0 if t is None else _like(t, shape, like.dtype, w, name)
-    o = KGE_NORM_GRADS.pack(_addr(dx) or 0, _addr(dy) or 0, _addr(dgate) or 0, _vector(dpost_weight, d, w, "dpost_weight"), _vector(dpost_bias, d, w, "dpost_bias"), _vector(dscale, d, w, "dscale"),
-                            _vector(dpre_weight, d, w, "dpre_weight"), _vector(dpre_bias, d, w, "dpre_bias"), ld(dx, x, "dx"), ld(dy, block, "dy"), ld(dgate, block, "dgate"))
-    ldz, ldh = ld(dz, block, "dz"), ld(dh, x, "dh")
+    b, shape, n, d, dev = _norm_block(w, x, block, y, gate, gate_act, post_weight, post_bias, scale, pre_weight, None, kind)
+    tx, tb = x.dtype, block.dtype
+    at = lambda t, dtype, name: (0, 0) if t is None else (t.data_ptr(), _like(t, shape, dtype, dev, w, name))
+    (px, lx), (py, ly), (pg, lg), (pz, lz), (ph, lh) = at(dx, tx, "dx"), at(dy, tb, "dy"), at(dgate, tb, "dgate"), at(dz, tb, "dz"), at(dh, tx, "dh")
+    v = [_vector(dpost_weight, d, dev, w, "dpost_weight"), _vector(dpost_bias, d, dev, w, "dpost_bias"), _vector(dscale, d, dev, w, "dscale"),
+         _vector(dpre_weight, d, dev, w, "dpre_weight"), _vector(dpre_bias, d, dev, w, "dpre_bias")]
     if stats is None:
         raise _bad(w, "stats is not given")
-    at = _stats_of(stats, n, w)
-    dev = _device_of(w, x, *[t for t in (y, gate, dz, dh, dx, dy, dgate, post_weight, post_bias, scale, pre_weight, dpost_weight, dpost_bias, dscale, dpre_weight, dpre_bias, stats)
-                             if t is not None])
-    wanted = not (dpost_weight is None and dpost_bias is None and dscale is None and dpre_weight is None and dpre_bias is None)
-    place, size, keep = _scratch(scratch, lib().kge_block_norm_grad_scratch_bytes(n, d) if wanted else 0, dev, w)
-    _call(w, lib().kge_block_norm_grad, dev, b, n, d, at, _addr(dz), ldz, _addr(dh), ldh, o, 1 if accumulate else 0, place, size)
+    place, size, keep = _scratch(scratch, lib().kge_block_norm_grad_scratch_bytes(n, d) if any(v) else 0, dev, w)
+    _call(w, lib().kge_block_norm_grad, dev, b, n, d, _stats_of(stats, n, dev, w), pz, lz, ph, lh, KGE_NORM_GRADS.pack(px, py, pg, *v, lx, ly, lg), 1 if accumulate else 0,
+          place, size)
 
 
 class AdamW:
