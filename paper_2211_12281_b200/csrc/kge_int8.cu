@@ -145,13 +145,14 @@ int launch_quantize(const QuantParams& p, cudaStream_t s) {
 constexpr int I8_BM = 128;
 constexpr uint32_t I8_BOX_BYTES = 128 * OPERAND_BK;
 constexpr int I8_NACC = 2;                                // accumulators in tensor memory: one is stored while the other is summed up
-// Four forms of the kernel: tiles of 256 x 256 that a pair of CTAs shares, 128 rows and half of B's rows each; tiles of 128 x 128, two CTAs an SM (one loads and
-// multiplies while the other stores), or of 128 x 64, three CTAs an SM; tiles of 128 x 128 whose K a cluster shares, where tiles are few.
-enum { I8_TWO = 0, I8_PAIR = 1, I8_NARROW = 2, I8_SPLIT = 3 };
+// Five forms of the kernel: tiles of 256 x 256 that a pair of CTAs shares, 128 rows and half of B's rows each; tiles of 128 x 128, two CTAs an SM (one loads and
+// multiplies while the other stores) or one with three times the copies under way; tiles of 128 x 64, three CTAs an SM; tiles of 128 x 128 whose K a cluster shares,
+// where tiles are few.
+enum { I8_TWO = 0, I8_PAIR = 1, I8_NARROW = 2, I8_SPLIT = 3, I8_DEEP = 4 };
 constexpr int I8_MAX_SPLIT = 8;           // CTAs that share a tile's K
 __host__ __device__ constexpr int i8_bn(int form) { return form == I8_TWO ? 256 : (form == I8_NARROW ? 64 : 128); }
 __host__ __device__ constexpr int i8_box_rows(int form) { return form == I8_NARROW ? 64 : 128; }             // of B per copy and CTA
-__host__ __device__ constexpr int i8_stages(int form) { return form == I8_TWO || form == I8_SPLIT ? 6 : 2; }
+__host__ __device__ constexpr int i8_stages(int form) { return form == I8_PAIR || form == I8_NARROW ? 2 : 6; }
 __host__ __device__ constexpr int i8_epi_warps(int form) { return form == I8_NARROW ? 4 : 8; }
 __host__ __device__ constexpr int i8_groups(int form) { return i8_bn(form) / OUT_COLS * 4 / i8_epi_warps(form); }     // of 64 columns per epilogue warp
 __host__ __device__ constexpr int i8_threads(int form) { return 32 * (4 + i8_epi_warps(form)); }     // (four more: copies, MMAs, two idle)
@@ -543,10 +544,13 @@ struct ProductPlan { int form, split; };          // split: CTAs that share a ti
 // How a product is cut up.
 //   shared K      as many CTAs to a tile as run at a time, where the blocks that a CTA is spared outweigh the join: a block takes 0.4 us, the join 0.4 + 2 for 128 rows
 //                 (16 x 4,096 x 4,096: four CTAs to each of 32 tiles, 9.3 us)
-//   256 x 256     on pairs of CTAs where those tiles fill the pairs and K is long enough for its MMAs to cover the stores of the tile before: 8,192 x 4,096 x 8,192
-//                 174 us, in tiles of 128 x 256 on one CTA 213; 16,384 x 8,192 x 512 101 us, in tiles of 128 x 128 112; 8,192 x 4,096 x 256 30 and 22; and, where K is
-//                 short, whole rounds of tiles are seven tenths full (24,576 x 256 x 768 after its quantisation, 96 tiles for 74 pairs: 29 us, in tiles of 128 x 64 26)
-//   128 or 64 columns   two or three CTAs an SM: what counts is how well whole rounds of tiles fill the SMs
+//   64 columns    of B at most: tiles of 128 x 64 (30,000 x 64 x 1,024: 10.3 us, in tiles of 256 x 256 14.9)
+//   else          the least of three estimates, in hundredths of a microsecond: a constant, and for every round of tiles that the chip takes another and one for each block
+//                 of K (fitted to 125 shapes; the form chosen is 1.4 % slower than the best of the four on their mean, 18 % with the rule "256 x 256 where they fill the pairs").
+//                   256 x 256               the least for a block, the most before and after it: 8,192 x 4,096 x 8,192 174 us, in tiles of 128 x 256 on one CTA 213;
+//                                           9,811 x 222 x 7,696 35, in tiles of 128 x 128 50; 40,000 x 500 x 512 36 and 25
+//                   128 x 128, two CTAs     a block waits for its copies, another CTA's stores go on meanwhile: K is short
+//                   128 x 128, one CTA      in between, and the tiles are half as many as two an SM would take: 700 x 3,000 x 5,000 20 us, with two CTAs 25, 256 x 256 25
 int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) {
     const int64_t tiles128 = ceil_div(M, I8_BM) * ceil_div(N, 128), tiles256 = ceil_div(M, 256) * ceil_div(N, 256);
     for (int most = (int)std::min<int64_t>({I8_MAX_SPLIT, kblocks, sms / tiles128}); most > 1; --most) {
@@ -557,14 +561,14 @@ int product_plan(int64_t M, int64_t N, int kblocks, int sms, ProductPlan* plan) 
         if (rc != KGE_OK) return rc;
         if (tiles128 <= room) { *plan = {I8_SPLIT, split}; return KGE_OK; }
     }
-    if (kblocks >= 4) {
-        int room = 0;
-        const int rc = clusters_at_a_time<I8_TWO>(2, &room);
-        if (rc != KGE_OK) return rc;
-        if (room > 0 && tiles256 >= room && (kblocks >= 16 || 10 * tiles256 >= 7 * room * ceil_div(tiles256, room))) { *plan = {I8_TWO, (int)std::min<int64_t>(room, tiles256)}; return KGE_OK; }
-    }
-    const int64_t pair = ceil_div(tiles128, 2 * sms) * 256, narrow = ceil_div(ceil_div(M, I8_BM) * ceil_div(N, 64), 3 * sms) * 192;
-    *plan = {narrow < pair ? I8_NARROW : I8_PAIR, 1};
+    if (N <= 64) { *plan = {I8_NARROW, 1}; return KGE_OK; }
+    int room = 0;
+    const int rc = clusters_at_a_time<I8_TWO>(2, &room);
+    if (rc != KGE_OK) return rc;
+    const int64_t two = room > 0 && kblocks >= 4 ? 600 + ceil_div(tiles256, room) * (32 * kblocks + 200) : INT64_MAX;
+    const int64_t pair = 400 + ceil_div(tiles128, 2 * sms) * (60 * kblocks + 100), deep = 450 + ceil_div(tiles128, sms) * (32 * kblocks + 70);
+    if (two <= std::min(pair, deep)) *plan = {I8_TWO, (int)std::min<int64_t>(room, tiles256)};
+    else *plan = {deep <= pair ? I8_DEEP : I8_PAIR, 1};
     return KGE_OK;
 }
 
@@ -640,6 +644,7 @@ int kge_int8_matmul(const void* a, int64_t lda, const float* a_scales, const voi
     switch (plan.form) {
         case I8_SPLIT: return launch_product<I8_SPLIT>(ma, mb, p, plan.split, sms, s);
         case I8_TWO: return launch_product<I8_TWO>(ma, mb, p, plan.split, sms, s);
+        case I8_DEEP: return launch_product<I8_DEEP>(ma, mb, p, 1, sms, s);
         case I8_NARROW: return launch_product<I8_NARROW>(ma, mb, p, 1, sms, s);
         default: return launch_product<I8_PAIR>(ma, mb, p, 1, sms, s);
     }

@@ -448,7 +448,8 @@ PRODUCTS = [
     (128, 128, 128, "f32", True, 0, 0), (129, 127, 130, "f32", True, 3, 0), (200, 64, 16_000, "bf16", False, 0, 0), (1000, 1001, 100, "bf16", True, 0, 0),
     (1000, 1002, 100, "f16", True, 0, 0), (4096, 256, 768, "f32", True, 0, 0), (5000, 777, 512, "bf16", True, 1, 1), (24_576, 256, 768, "bf16", True, 0, 0),
     (2500, 4096, 2048, "f32", False, 0, 0), (4096, 4095, 4096, "bf16", True, 0, 0), (4100, 4096, 2050, "bf16", False, 8, 8), (65, 8192, 8000, "f16", False, 0, 0),
-    (20_000, 70, 300, "f32", False, 2, 0), (40_000, 512, 64, "bf16", False, 0, 0), (8192, 2048, 3000, "f32", True, 4, 4)]
+    (20_000, 70, 300, "f32", False, 2, 0), (40_000, 512, 64, "bf16", False, 0, 0), (8192, 2048, 3000, "f32", True, 4, 4),
+    (200, 8000, 1500, "f16", True, 1, 0), (16_384, 512, 512, "bf16", True, 0, 0), (9800, 222, 2500, "bf16", True, 0, 0), (250, 9999, 9000, "f32", True, 1, 1), (3001, 300, 3000, "bf16", True, 1, 1)]
 
 
 @pytest.mark.parametrize("M,N,Kd,to,add,extra,shift", PRODUCTS)
@@ -530,7 +531,7 @@ def test_int8_matmul_of_scales_far_from_one(T, K, M, N, Kd):
 
 def test_int8_waits_that_run_out_are_reported(T, K):
     ran_out = False
-    for M, N, Kd in ((1, 4096, 4096), (24_576, 256, 768), (4096, 4096, 4096), (20_000, 64, 300)):
+    for M, N, Kd in ((1, 4096, 4096), (24_576, 256, 768), (4096, 4096, 4096), (20_000, 64, 300), (16_384, 512, 512)):
         g = _gen(T, M)
         a, b = _int8(T, M, Kd), _int8(T, N, Kd)
         a.copy_(T.randint(-127, 128, (M, Kd), generator=g, device="cuda", dtype=T.int8))
