@@ -192,7 +192,22 @@ __device__ __forceinline__ void out_fetch_addend(const ProductOut& p, int row0, 
     } else if (sizeof(TO) == 4 || p.twos) {
         out_each<TO, 128, FOUR>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { copy4_async(smem_u32(at), reinterpret_cast<const float*>(add + row * p.ld_addend + col)); });
     } else {
-        out_each<TO, 128, 1>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { *at = add[row * p.ld_addend + col]; });
+        // (sixteen loads under way: 13,555 x 1,119 bf16 in 8 bits, K = 2,536, with an addend: 123 us with four, 80)
+        constexpr int ROWS = 8, COLS = 128 / (int)sizeof(TO) / 32;
+        TO* const own = reinterpret_cast<TO*>(st);
+        for (int r0 = 0; r0 < 32; r0 += ROWS) {
+            TO v[ROWS * COLS];
+#pragma unroll
+            for (int i = 0; i < ROWS * COLS; ++i) {
+                const int row = row0 + r0 + i / COLS, col = col0 + c + i % COLS * 32 + lane;
+                v[i] = row < p.M && col < p.N ? add[row * p.ld_addend + col] : from_float<TO>(0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < ROWS * COLS; ++i) {
+                const int r = r0 + i / COLS, x = i % COLS * 32 + lane;
+                own[(r * 8 + ((x / V) ^ (r & 7))) * V + x % V] = v[i];
+            }
+        }
     }
 }
 template <typename TO>
