@@ -641,7 +641,7 @@ SIZES = [1, 127, 0, 128, 129, 4095, 4096, 4097, 2048, 100_003]
 @pytest.mark.parametrize("tp,tg,copy,shift,sizes,step,gs", [
     ("f32", "f32", None, 0, SIZES, 0, 1.0), ("f32", "bf16", "bf16", 0, SIZES, 7, 0.5), ("bf16", "bf16", None, 0, SIZES, 999, 1.0), ("f16", "f32", "bf16", 0, [5000], 3, 0.1),
     ("f32", "f16", "f16", 1, SIZES, 12_345_678_901, 1.0), ("bf16", "f32", "f16", 3, SIZES, 1, 1.0), ("f32", "f32", None, 0, [300 + 7 * i for i in range(41)], 50, 1.0),
-    ("f32", "f32", "bf16", 0, [1 + i % 400 for i in range(1000)], 2, 2.0)])
+    ("f32", "f32", "bf16", 0, [1 + i % 400 for i in range(1000)], 2, 2.0), ("f32", "bf16", None, 0, [200 + 9 * i for i in range(30)], 4, 1.0)])
 def test_adamw(T, K, bits, tp, tg, copy, shift, sizes, step, gs):
     g = _gen(T, len(sizes) + step % 1000)
     at = lambda n, t: T.zeros(n + shift, dtype=_type(T, t), device="cuda")[shift:]
