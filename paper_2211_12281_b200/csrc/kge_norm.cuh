@@ -49,18 +49,18 @@ template <typename T> __device__ __forceinline__ P8 pairs_of(const Raw8<T>& r) {
 }
 __device__ __forceinline__ F8 singles_of(const P8& a) { return make8([&](int e) { return element(a, e); }); }
 
-// Where a thread's elements lie in its row: WIDE rows let eight neighbours move as one access, and all of them or none are there.  What lies beyond the row's end
-// (of a wide row: other elements of it) is left out of sums and stores.
-template <bool WIDE> struct Place {
+// Where a thread's elements lie in its row, W neighbours moving as one access: all eight of them (and all or none are there), pairs, or each alone.  What lies beyond
+// the row's end is zero when loaded (with W = 8: other elements of the row) and is left out of stores and sums.
+template <int W> struct Place {
+    static constexpr bool WIDE = W == 8;
     int first, step, d;
     bool any;
     Place() = default;
-    __device__ __forceinline__ Place(int team, int t, int k, int width)
-        : first(WIDE ? (k * team + t) * 8 : k * team * 8 + t), step(WIDE ? 1 : team), d(width), any(first < width) {
+    __device__ __forceinline__ Place(int team, int t, int k, int width) : first(WIDE ? (k * team + t) * 8 : k * team * 8 + t * W), step(W * team), d(width), any(first < width) {
         if (WIDE && !any) first = 0;
     }
-    __device__ __forceinline__ int at(int e) const { return first + e * step; }
-    __device__ __forceinline__ bool holds(int e) const { return WIDE ? any : at(e) < d; }
+    __device__ __forceinline__ int at(int e) const { return first + e / W * step + e % W; }
+    __device__ __forceinline__ bool holds(int e) const { return WIDE ? any : at(e / W * W) < d; }
     // (a row's address is the same for a warp, and a thread's place in it takes 32 bits: one access, no arithmetic of 64 bits in every thread)
     template <typename T> __device__ __forceinline__ T* mine(T* row, int e = 0) const {
         using Byte = typename std::conditional<std::is_const<T>::value, const char, char>::type;
@@ -69,14 +69,31 @@ template <bool WIDE> struct Place {
     template <typename T> __device__ __forceinline__ Raw8<T> load(const T* row) const {
         if constexpr (WIDE) return load_wide(mine(row));
         Raw8<T> r;
+        if constexpr (W == 2) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) set_element(r, e, holds(e) ? *mine(row, e) : from_float<T>(0.f));
+            for (int e = 0; e < 8; e += 2) {
+                if constexpr (sizeof(T) == 4) {
+                    const uint2 w = holds(e) ? *reinterpret_cast<const uint2*>(mine(row, e)) : make_uint2(0u, 0u);
+                    r.w[e] = w.x; r.w[e + 1] = w.y;
+                } else r.w[e / 2] = holds(e) ? *reinterpret_cast<const uint32_t*>(mine(row, e)) : 0u;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) set_element(r, e, holds(e) ? *mine(row, e) : from_float<T>(0.f));
+        }
         return r;
     }
     template <typename T> __device__ __forceinline__ void store(T* row, const P8& x, bool live) const {
         const Raw8<T> r = narrow_of<T>(singles_of(x));
         if constexpr (WIDE) { if (any && live) store_wide(mine(row), r); }
-        else {
+        else if constexpr (W == 2) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                if (!holds(e) || !live) continue;
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint2*>(mine(row, e)) = make_uint2(r.w[e], r.w[e + 1]);
+                else *reinterpret_cast<uint32_t*>(mine(row, e)) = r.w[e / 2];
+            }
+        } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) if (holds(e) && live) *mine(row, e) = element(r, e);
         }
@@ -86,18 +103,27 @@ template <bool WIDE> struct Place {
         if constexpr (WIDE) {
             const Pack<float, 8> v = load_now<Pack<float, 8>>(mine(p));
             return make_pairs([&](int e) { return v.v[e]; });
+        } else if constexpr (W == 2) {
+            P8 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r.v[i] = 0;
+                if (!holds(2 * i)) continue;
+                const Pack<float, 2> v = load_now<Pack<float, 2>>(mine(p, 2 * i));
+                r.v[i] = pair(v.v[0], v.v[1]);
+            }
+            return r;
         }
         return make_pairs([&](int e) { return holds(e) ? load_now<Pack<float, 1>>(mine(p, e)).v[0] : 0.f; });
     }
-    // Sums over the thread's elements.
+    // Zero beyond the row's end (W < 8).
     __device__ __forceinline__ P8 there(const P8& a) const { return WIDE ? a : make_pairs([&](int e) { return holds(e) ? element(a, e) : 0.f; }); }
-    __device__ __forceinline__ float total(const P8& x) const {
-        const P8 a = there(x);
+    // Sums over the thread's elements; with W < 8 one factor is zero beyond the row's end.
+    __device__ __forceinline__ float total(const P8& a) const {
         const float2 s = unpair(add2(add2(a.v[0], a.v[1]), add2(a.v[2], a.v[3])));
         return WIDE && !any ? 0.f : s.x + s.y;
     }
-    __device__ __forceinline__ float dot(const P8& x, const P8& b) const {
-        const P8 a = there(x);
+    __device__ __forceinline__ float dot(const P8& a, const P8& b) const {
         uint64_t s = mul2(a.v[0], b.v[0]);
 #pragma unroll
         for (int i = 1; i < 4; ++i) s = fma2(a.v[i], b.v[i], s);

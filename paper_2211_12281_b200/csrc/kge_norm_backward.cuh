@@ -21,7 +21,7 @@ struct NormGradParams {
     float* part;                       // [CTAs][sums][d]
     int64_t ldx, ldy, ldg, ldz, ldh, ldox, ldoy, ldog;
     int n, d;
-    int post, layer, act, wide;
+    int post, layer, act, access;         // access: elements that move as one in every array, 8, 2 or 1
     int sums;                          // 0: no gradients of vectors; 2: T1, S1; 4: T0 and S0 too
     float inv_d;
 };
@@ -53,14 +53,14 @@ template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y,
 // instead of 234 us, 8,192 x 4,096 fp32 330 instead of 204, 24,576 x 256 46 instead of 38: it is not memory that they wait for.)
 // SHARED: a CTA of up to 1,024 threads for a row of up to 8,192 columns, whose registers hold neither: the sums are in shared memory, a thread's own places, and the
 // vectors are loaded where they are used (8,192 x 8,192 bf16: 407 us; gone over in three passes 2,284).
-template <typename TX, typename TB, int L, bool WIDE, bool FULL, bool SHARED>
+template <typename TX, typename TB, int L, int W, bool FULL, bool SHARED>
 __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD / 8 : NORM_THREADS), L == 0 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
     constexpr bool AHEAD = !SHARED && (!FULL || L >= 32) && (!FULL || sizeof(TX) + sizeof(TB) <= 6);
     __shared__ float parts[2][2][32];
     __shared__ float joined[L == 0 ? 1 : NORM_THREADS * 8];
     Team<L> team(parts);
     const int t = team.thread, last = p.n - 1;
-    const Place<WIDE> at(Team<L>::size(), t, 0, p.d);
+    const Place<W> at(Team<L>::size(), t, 0, p.d);
     const int64_t step = (int64_t)gridDim.x * Team<L>::COUNT;
     grid_dependency_wait();
     allow_dependents();
@@ -264,24 +264,26 @@ __global__ void __launch_bounds__(NORM_LOOP_THREADS) norm_grad_loop_kernel(const
     }
 }
 
-template <typename TX, typename TB, bool WIDE, bool FULL>
+template <typename TX, typename TB, int W, bool FULL>
 int launch_held(const NormGradParams& p, int ctas, cudaStream_t s) {
     auto launch = [&](auto kernel, int threads) { return launch_status(launch_dependent(kernel, dim3((unsigned)ctas), dim3((unsigned)threads), 0, s, p)); };
     const int threads = (int)ceil_div(p.d, 256) * 32;
-    if (p.d > GRAD_HELD) {
-        auto kernel = norm_grad_kernel<TX, TB, 0, WIDE, FULL, true>;
-        static DeviceOnce configured;
-        constexpr int most = (FULL ? 4 : 2) * NORM_MOST * (int)sizeof(float);
-        if (once_per_device(configured, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most); }) != cudaSuccess) return KGE_ERR_CUDA;
-        return launch_status(launch_dependent(kernel, dim3((unsigned)ctas), dim3((unsigned)threads), (size_t)p.sums * threads * 8 * sizeof(float), s, p));
+    if constexpr (W != 2) {
+        if (p.d > GRAD_HELD) {
+            auto kernel = norm_grad_kernel<TX, TB, 0, W, FULL, true>;
+            static DeviceOnce configured;
+            constexpr int most = (FULL ? 4 : 2) * NORM_MOST * (int)sizeof(float);
+            if (once_per_device(configured, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most); }) != cudaSuccess) return KGE_ERR_CUDA;
+            return launch_status(launch_dependent(kernel, dim3((unsigned)ctas), dim3((unsigned)threads), (size_t)p.sums * threads * 8 * sizeof(float), s, p));
+        }
     }
     switch (norm_team(p.d)) {
-        case 8: return launch(norm_grad_kernel<TX, TB, 8, WIDE, FULL, false>, NORM_THREADS);
-        case 16: return launch(norm_grad_kernel<TX, TB, 16, WIDE, FULL, false>, NORM_THREADS);
-        case 32: return launch(norm_grad_kernel<TX, TB, 32, WIDE, FULL, false>, NORM_THREADS);
-        case 64: return launch(norm_grad_kernel<TX, TB, 64, WIDE, FULL, false>, NORM_THREADS);
-        case 128: return launch(norm_grad_kernel<TX, TB, 128, WIDE, FULL, false>, NORM_THREADS);
-        default: return launch(norm_grad_kernel<TX, TB, 0, WIDE, FULL, false>, threads);
+        case 8: return launch(norm_grad_kernel<TX, TB, 8, W, FULL, false>, NORM_THREADS);
+        case 16: return launch(norm_grad_kernel<TX, TB, 16, W, FULL, false>, NORM_THREADS);
+        case 32: return launch(norm_grad_kernel<TX, TB, 32, W, FULL, false>, NORM_THREADS);
+        case 64: return launch(norm_grad_kernel<TX, TB, 64, W, FULL, false>, NORM_THREADS);
+        case 128: return launch(norm_grad_kernel<TX, TB, 128, W, FULL, false>, NORM_THREADS);
+        default: return launch(norm_grad_kernel<TX, TB, 0, W, FULL, false>, threads);
     }
 }
 
@@ -290,8 +292,10 @@ template <typename TX, typename TB>
 int launch_norm_grad(const NormGradParams& p, int ctas, cudaStream_t s) {
     if (p.d > NORM_MOST)
         return launch_status(launch_dependent(norm_grad_loop_kernel<TX, TB>, dim3((unsigned)ctas), dim3(NORM_LOOP_THREADS), 0, s, p));
-    if (!p.wide) return launch_held<TX, TB, false, true>(p, ctas, s);
-    return p.layer || p.b1 || p.sums > 2 ? launch_held<TX, TB, true, true>(p, ctas, s) : launch_held<TX, TB, true, false>(p, ctas, s);
+    // (pairs: 60,000 x 998 bf16 280 us, one by one 526; where the sums are in shared memory 64 registers do not hold them: 5,000 x 6,002 456 us, one by one 359)
+    if (p.access == 2 && p.d <= GRAD_HELD) return launch_held<TX, TB, 2, true>(p, ctas, s);
+    if (p.access < 8) return launch_held<TX, TB, 1, true>(p, ctas, s);
+    return p.layer || p.b1 || p.sums > 2 ? launch_held<TX, TB, 8, true>(p, ctas, s) : launch_held<TX, TB, 8, false>(p, ctas, s);
 }
 
 }  // namespace

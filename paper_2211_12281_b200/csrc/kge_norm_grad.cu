@@ -88,11 +88,14 @@ int kge_block_norm_grad(const kge_norm_block* b, int64_t n, int32_t d, const flo
         auto ok = [&](const void* p, int64_t ld, int size) { return !p || (ld >= d && aligned_to(p, (size_t)size)); };
         if (!stats || !aligned_to(stats, 16) || !b->x || !ok(b->x, b->ldx, xs) || !ok(b->y, b->ldy, bs) || !ok(b->gate, b->ld_gate, bs) || !ok(dz, ld_dz, bs) ||
             !ok(dh, ld_dh, xs) || !ok(o->dx, o->ld_dx, xs) || !ok(o->dy, o->ld_dy, bs) || !ok(o->dgate, o->ld_dgate, bs)) return KGE_ERR_BAD_ARG;
-        auto packs = [&](const void* p, int64_t ld, int size) { return !p || (ld % 8 == 0 && aligned_to(p, (size_t)(8 * size))); };
+        auto moves = [&](int w) {
+            auto packs = [&](const void* p, int64_t ld, int size) { return !p || (ld % w == 0 && aligned_to(p, (size_t)(w * size))); };
+            for (int i = 0; i < 4; ++i) if (!aligned_to(vectors[i], (size_t)(4 * std::min(w, 4)))) return false;
+            return d % w == 0 && packs(b->x, b->ldx, xs) && packs(b->y, b->ldy, bs) && packs(b->gate, b->ld_gate, bs) && packs(dz, ld_dz, bs) && packs(dh, ld_dh, xs) &&
+                   packs(o->dx, o->ld_dx, xs) && packs(o->dy, o->ld_dy, bs) && packs(o->dgate, o->ld_dgate, bs);
+        };
         NormGradParams p{};
-        p.wide = d % 8 == 0 && packs(b->x, b->ldx, xs) && packs(b->y, b->ldy, bs) && packs(b->gate, b->ld_gate, bs) && packs(dz, ld_dz, bs) && packs(dh, ld_dh, xs) &&
-                 packs(o->dx, o->ld_dx, xs) && packs(o->dy, o->ld_dy, bs) && packs(o->dgate, o->ld_dgate, bs);
-        for (int i = 0; i < 4; ++i) p.wide = p.wide && aligned_to(vectors[i], 16);
+        p.access = moves(8) ? 8 : (moves(2) ? 2 : 1);
         p.x = b->x; p.y = b->y; p.gate = b->gate; p.dz = dz; p.dh = dh; p.dx = o->dx; p.dy = o->dy; p.dgate = o->dgate;
         p.w1 = b->post_weight; p.b1 = b->post_bias; p.scale = b->scale; p.w2 = b->pre_weight; p.stats = stats;
         p.ldx = b->ldx; p.ldy = b->ldy; p.ldg = b->ld_gate; p.ldz = ld_dz; p.ldh = ld_dh; p.ldox = o->ld_dx; p.ldoy = o->ld_dy; p.ldog = o->ld_dgate;

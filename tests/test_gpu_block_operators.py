@@ -176,7 +176,10 @@ NORM_CASES = [
     (70, 96, "bf16", "bf16", "both", True, "silu", True, False, "rms"), (11, 768, "bf16", "f16", "both", True, "sigmoid", True, True, "layer"), (40, 704, "f32", "f32", "both", True, "silu", True, False, "rms"),
     (9, 1200, "f32", "bf16", "both", False, "plain", True, True, "layer"), (160, 1600, "bf16", "bf16", "both", True, "none", False, False, "rms"), (5, 5001, "bf16", "f32", "both", True, "silu", True, True, "layer"),
     (300, 5000, "bf16", "bf16", "both", True, "sigmoid", True, False, "rms"), (2, 6144, "f32", "f32", "post", True, "plain", True, False, "layer"),
-    (3, 20_000, "bf16", "f32", "both", True, "silu", True, True, "rms"), (2, 9000, "f16", "f16", "pre", False, "none", False, True, "layer")]
+    (3, 20_000, "bf16", "f32", "both", True, "silu", True, True, "rms"), (2, 9000, "f16", "f16", "pre", False, "none", False, True, "layer"),
+    (70, 50, "f32", "bf16", "both", True, "sigmoid", True, True, "layer"), (9, 100, "bf16", "bf16", "both", True, "silu", True, False, "rms"), (33, 250, "f16", "f32", "pre", False, "none", False, True, "layer"),
+    (200, 1002, "bf16", "bf16", "both", True, "sigmoid", True, True, "layer"), (6, 2050, "f32", "f32", "both", True, "plain", True, False, "rms"), (5, 4098, "bf16", "f16", "both", True, "silu", True, True, "layer"),
+    (3, 8190, "f32", "bf16", "post", True, "sigmoid", True, True, "layer")]
 LAYOUTS = [(0, 0), (8, 8), (3, 1)]
 
 
