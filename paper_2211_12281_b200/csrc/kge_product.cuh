@@ -192,9 +192,10 @@ __device__ __forceinline__ void out_fetch_addend(const ProductOut& p, int row0, 
     } else if (sizeof(TO) == 4 || p.twos) {
         out_each<TO, 128, FOUR>(p, row0, col0 + c, st, lane, [&](int row, int col, TO* at) { copy4_async(smem_u32(at), reinterpret_cast<const float*>(add + row * p.ld_addend + col)); });
     } else {
-        // (sixteen loads under way: 13,555 x 1,119 bf16 in 8 bits, K = 2,536, with an addend: 123 us with four, 80)
+        // (sixteen loads under way: 13,555 x 1,119 bf16 in 8 bits, K = 2,536, with an addend: 121 us with four, 80)
         constexpr int ROWS = 8, COLS = 128 / (int)sizeof(TO) / 32;
         TO* const own = reinterpret_cast<TO*>(st);
+#pragma unroll 1
         for (int r0 = 0; r0 < 32; r0 += ROWS) {
             TO v[ROWS * COLS];
 #pragma unroll
