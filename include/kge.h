@@ -450,8 +450,10 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
  *                    a row of zeros), q the integer nearest to x / scale, ties to even.  A row that holds an infinity or a NaN stands
  *                    for NaN throughout.
  * kge_int8_matmul    out [M, N] = A [M, K] . B [N, K]^T (+ addend [M, N], of out's type; it may be out itself): the products summed exactly
- *                    in 32-bit integers (K at most 131,071, else KGE_ERR_UNSUPPORTED), the sum times its two scales and the addend in fp32.  out fp32,
- *                    bf16 or fp16.  The same bits on every GPU and however the work is shared out.
+ *                    in 32-bit integers (K at most 131,071, else KGE_ERR_UNSUPPORTED), the sum times its two scales and the addend in fp32: times A's scale,
+ *                    then B's (or, where one of them is below 2^-63 or above 2^63 in magnitude, the smaller, then the larger), this second product and
+ *                    the addend's sum rounded once.  out fp32, bf16 or fp16.  The same bits on every GPU, however the work is shared
+ *                    out, and whatever the other rows and columns hold.
  *                    status receives KGE_ERR_TIMEOUT if a wait in the kernel ran out; out is not what it should be then.
  */
 int kge_int8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, void* q, int64_t ldq, float* scales, void* stream);

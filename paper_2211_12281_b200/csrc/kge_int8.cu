@@ -182,13 +182,15 @@ __device__ __forceinline__ void i8_mma_pair(uint32_t d, uint64_t a, uint64_t b, 
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// A sum times its two scales (the sum's own rounding to fp32 is half a step of 24 bits).  Scales between 2^-63 and 2^63 are multiplied one after the other: no
-// intermediate value leaves the normal numbers.  Others too, the smaller one first: |x| >= 1 keeps that product a normal number where the scale is one, and it leaves the
-// range upwards only where the result does.  (fminf and fmaxf drop a NaN: a row that stands for NaN has an infinite or a NaN scale.)
-__device__ __forceinline__ bool near_one(float s) { return __float_as_uint(s) - 0x20000000u <= 0x3F000000u; }
-__device__ __forceinline__ float scaled_far(int x, float a, float b) {
-    const float y = (float)x * fminf(a, b) * fmaxf(a, b);
-    return a != a || b != b ? a + b : y;
+// A sum times its two scales (the sum's own rounding to fp32 is half a step of 24 bits), and the addend with the second of them, in an order that the two scales alone
+// decide and in operations that the compiler may not join, so that an element has the same bits in every form of the kernel and whatever its neighbours are.  Scales of
+// magnitudes between 2^-63 and 2^63 are multiplied one after the other: no intermediate value leaves the normal numbers.  Others too, the smaller one first: |x| >= 1 keeps
+// that product a normal number where the scale is one, and it leaves the range upwards only where the result does.
+__device__ __forceinline__ bool near_one(float s) { return (__float_as_uint(s) & 0x7FFFFFFFu) - 0x20000000u <= 0x3F000000u; }
+template <bool NEAR> __device__ __forceinline__ float scaled(int x, float a, float b, bool add, float addend) {
+    const bool swap = !NEAR && !(near_one(a) && near_one(b)) && fabsf(b) < fabsf(a);
+    const float y = __fmul_rn((float)x, swap ? b : a), last = swap ? a : b;
+    return add ? __fmaf_rn(y, last, addend) : __fmul_rn(y, last);
 }
 
 // 128 bytes of each of a warp's rows from shared memory in units of one or two elements, sixteen of them under way (15,348 x 3,109 f16 in 8 bits, K = 279: 85 us with
@@ -248,8 +250,7 @@ __device__ __forceinline__ void i8_store(const IntProductParams& p, int row0, in
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int sum = (int)x[i * V + e + k];
-                        y[e + k] = NEAR ? (float)sum * sa * bs[k] : scaled_far(sum, sa, bs[k]);
-                        if (ADD) y[e + k] += to_float(o.v[e + k]);
+                        y[e + k] = scaled<NEAR>(sum, sa, bs[k], ADD, ADD ? to_float(o.v[e + k]) : 0.f);
                     }
                 }
                 if constexpr (sizeof(TO) == 4) {
@@ -305,8 +306,8 @@ __device__ __forceinline__ void i8_join(const IntProductParams& p, uint32_t part
         Pack<TO, 4> o;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x = col + e < p.N ? scaled_far(sum[e], sa, p.sb[col + e]) : 0.f;
-            o.v[e] = from_float<TO>(p.addend && col + e < p.N ? x + to_float(add[e]) : x);
+            const bool there = col + e < p.N;
+            o.v[e] = from_float<TO>(there ? scaled<false>(sum[e], sa, p.sb[col + e], p.addend, p.addend ? to_float(add[e]) : 0.f) : 0.f);
         }
         out_put<TO, 4>(p, row, col, o);
     }
