@@ -58,7 +58,8 @@ template <typename T> __device__ __forceinline__ QuantScale quant_scale(float a)
 }
 __device__ __noinline__ uint32_t quotient_bits(float x, float s) {
     int m = (int)(__float_as_uint(fabsf(x) * __fdiv_rn(1.f, s)) + 8u) & ~15;
-    const float d = fmaf(-__int_as_float(m), s, fabsf(x));
+    const float up = s < 2.35098870e-38f ? 2.f : 1.f;          // (half a unit of 2^-149, of scales below 2^-125, is none)
+    const float d = fmaf(-__int_as_float(m), up * s, up * fabsf(x));
     m += d > 0.f ? 1 : (d < 0.f ? -1 : 0);
     return __float_as_uint(copysignf(__int_as_float(m), x) + ROUND_TO_INT);
 }
