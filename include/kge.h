@@ -447,7 +447,7 @@ int kge_fp8_matmul(const void* a, int32_t a_type, int64_t lda, const float* a_sc
  * q times its row's scale.  What lies between K and ld is neither read nor written.
  *
  * kge_int8_quantize  x [rows, cols] (fp32, bf16, fp16) -> q, scales: scale = largest magnitude of the row / 127 (at least 2^-126; 1 for
- *                    a row of zeros), q the integer nearest to x / scale, ties to even.  A row that holds an infinity or a NaN stands
+ *                    a row of zeros or of no columns), q the integer nearest to x / scale, ties to even.  A row that holds an infinity or a NaN stands
  *                    for NaN throughout.
  * kge_int8_matmul    out [M, N] = A [M, K] . B [N, K]^T (+ addend [M, N], of out's type; it may be out itself): the products summed exactly
  *                    in 32-bit integers (K at most 131,071, else KGE_ERR_UNSUPPORTED), the sum times its two scales and the addend in fp32: times A's scale,

@@ -623,8 +623,8 @@ extern "C" {
 int kge_int8_quantize(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, void* q, int64_t ldq, float* scales, void* stream) {
     if (!is_float_type(x_type) || rows < 0 || rows > INT32_MAX || cols < 0 || cols > INT32_MAX - 65536 || ldx < cols || ldq < cols || ldq % 16 || !aligned_to(q, 16) ||
         !aligned_to(scales, 4)) return KGE_ERR_BAD_ARG;
-    if (rows == 0 || cols == 0) return KGE_OK;
-    if (!x || !q || !scales || !aligned_to(x, type_bytes(x_type))) return KGE_ERR_BAD_ARG;
+    if (rows == 0) return KGE_OK;
+    if ((cols > 0 && (!x || !q)) || !scales || !aligned_to(x, type_bytes(x_type))) return KGE_ERR_BAD_ARG;          // (rows of no columns have a scale)
     QuantParams p{};
     p.x = x; p.ldx = ldx; p.q = static_cast<int8_t*>(q); p.ldq = ldq; p.scales = scales; p.rows = (int)rows; p.cols = (int)cols;
     p.wide = cols % 8 == 0 && ldx % 8 == 0 && aligned_to(x, (size_t)(8 * type_bytes(x_type)));

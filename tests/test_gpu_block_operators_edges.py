@@ -21,3 +21,12 @@ def test_int8_quantize_of_middles_at_the_smallest_scales(T, K):
     wq, ws = _quantized64(T, x)          # (quotients of integers below 2^31: in 64 bits right, or a middle exactly)
     assert T.equal(scales, ws) and T.equal(scales.double() / least, s[:, 0])
     assert T.equal(q, wq)
+
+
+@pytest.mark.parametrize("tx", ["float32", "bfloat16"])
+def test_int8_quantize_of_rows_without_columns(T, K, tx):
+    """They hold no value but zero: scale 1."""
+    for rows in (1, 9, 3000):
+        scales = T.full((rows + 1,), float("nan"), device="cuda")
+        K.int8_quantize(T.empty((rows, 0), dtype=getattr(T, tx), device="cuda"), _int8(T, rows, 16)[:, :0], scales[:rows])
+        assert (scales[:rows] == 1).all() and T.isnan(scales[rows])
