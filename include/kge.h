@@ -465,7 +465,8 @@ int kge_int8_matmul(const void* a, int64_t lda, const float* a_scales, const voi
  *   a = N1(y), or y where post_weight is NULL;   h = x + scale act(gate) a, or x where y is NULL;   z = N2(h)
  *   N(u) = (u - mu) r weight + bias,  r = 1 / sqrt(mean((u - mu)^2) + eps),  mu = mean(u) where layer = 1, else 0
  * x and h are of x_type, y, gate and z of block_type (fp32, bf16, fp16 each), the vectors [d] fp32 (bias, scale, gate: NULL where there is none).
- * act: gate_act 0 the gate itself, 1 its sigmoid, 2 gate times its sigmoid.  z is made of the unrounded h.
+ * act: gate_act 0 the gate itself, 1 its sigmoid, 2 gate times its sigmoid.  A sigmoid is within 8 units of 2^-24 of itself, and 2^-147; where x and the block
+ * are of 16 bits both, the forward pass's within 2^-16 of itself, and 0 below 2^-126.  z is made of the unrounded h.
  * kge_block_norm       h or z may be NULL, not both; without y only z is given.  z_int8 = 1: z is int8 [n, d] with a scale for each row in z_scales
  *                      [n], as kge_int8_quantize would make them of the unrounded z (which of two integers a z beside their middle becomes is decided in fp32).  stats (or NULL): [n, 4], 16-byte aligned, receives mu and r
  *                      of the norm after the block, then of the one before the next (0 where a norm is not taken), for the gradients.

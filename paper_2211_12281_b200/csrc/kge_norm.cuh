@@ -194,15 +194,55 @@ template <int L> struct Team {
     __device__ __forceinline__ float most(float x) { float v[1] = {x}; all<true>(v); return v[0]; }
 };
 
-// 1 / (1 + exp(-g)) within 6 + 1.5 |g| units of 2^-24 of itself (its share of |g| for g < 0 only): the product g log2 e is rounded, the power and the reciprocal
-// are one instruction each.
-__device__ __forceinline__ float sigmoid_of(float g) {
-    float e, r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-1.44269504f * g));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
-    return r;
+// 1 / (1 + exp(-g)) within 8 units of 2^-24 of itself, and 2^-147.  Where |g| < 80 (neither the power nor its reciprocal leaves the normal numbers there) both are one
+// instruction each: t = -g log2 e is rounded, so 2^t is off by exp(r) with r = -g - t ln 2, some 2^-17 at most; ln 2 in two parts gives r (Cody and Waite), and
+// 2^t (1 + r) is off by the instruction's 4 units and one more.  (Without it gates far below zero were off by 1.5 |g| units.)
+constexpr float LOG2_E = 1.44269504f, LN_2 = 0.693147182f, LN_2_REST = -1.90465430e-9f;
+__device__ __forceinline__ float power_of_two(float t) { float x; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(t)); return x; }
+__device__ __forceinline__ float one_over(float y) { float x; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(y)); return x; }
+static __device__ __noinline__ float sigmoid_of(float g) {
+    if (fabsf(g) < 80.f) {
+        const float t = g * -LOG2_E, r = fmaf(t, -LN_2_REST, fmaf(t, -LN_2, -g)), power = power_of_two(t);
+        return one_over(fmaf(power, r, power) + 1.f);
+    }
+    const float e = expf(-fabsf(g)), r = __fdiv_rn(1.f, 1.f + e);
+    return g < 0.f ? e * r : r;
 }
-__device__ __forceinline__ P8 sigmoid_of(const P8& g) { return make_pairs([&](int e) { return sigmoid_of(element(g, e)); }); }
+// The same bits for a thread's gates: f(k, sigmoids of pack k), in pairs where all of them are near.
+// BRIEF: without the remainder, and 0 below the normal numbers: within 6 + 1.5 |g| units of 2^-24 of itself (its share of |g| for g < 0 only), less than 2^-16.  Enough where
+// all that is made of it is rounded to 16 bits (h and z of 16-bit rows and blocks; 32,768 x 4,096 bf16: 245 us, 255 with the remainder).
+__device__ __forceinline__ float most_of(float a, float b, float c) { float m; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c)); return m; }
+template <bool BRIEF, int K, typename T, class F> __device__ __forceinline__ void with_sigmoids(const Raw8<T> (&gate)[K], F&& f) {
+    if constexpr (BRIEF) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const P8 g = pairs_of(gate[k]);
+            f(k, make_pairs([&](int e) { return one_over(1.f + power_of_two(-LOG2_E * element(g, e))); }));
+        }
+        return;
+    }
+    float most = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const F8 g = wide_of(gate[k]);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) most = most_of(most, fabsf(g.v[e]), fabsf(g.v[e + 1]));
+    }
+    if (!(most < 80.f)) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const F8 g = wide_of(gate[k]);
+            f(k, make_pairs([&](int e) { return sigmoid_of(g.v[e]); }));
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const P8 g = pairs_of(gate[k]), t = g * -LOG2_E, r = fma8(t, -LN_2_REST, fma8(t, -LN_2, g * -1.f)), power = make_pairs([&](int e) { return power_of_two(element(t, e)); });
+        const P8 sum = fma8(power, r, power) + 1.f;
+        f(k, make_pairs([&](int e) { return one_over(element(sum, e)); }));
+    }
+}
 __device__ __forceinline__ float act_of(float g, int act) { return act == NORM_PLAIN ? g : (act == NORM_SIGMOID ? sigmoid_of(g) : g * sigmoid_of(g)); }
 __device__ __forceinline__ float2 act_and_slope(float g, int act) {
     if (act == NORM_PLAIN) return make_float2(g, 1.f);

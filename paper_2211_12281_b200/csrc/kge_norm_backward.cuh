@@ -43,7 +43,7 @@ int launch_norm_grad_f16(const NormGradParams& p, int block_type, int ctas, cuda
 
 namespace {
 
-template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y, gate, dz; float4 stats; };
+template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y, gate[1], dz; float4 stats; };
 
 // Teams take rows in turn, the next one's loads under way, and add up the columns' sums of theirs in registers.  (Teams that have run out of rows go along with
 // the last one.)  The vectors enter as sw = s w1, sb = s b1 and w2, which a thread keeps: with q = yn sw + sb
@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
             v.x = at.load(static_cast<const TX*>(p.x) + r * p.ldx);
         }
         if (p.y) v.y = at.load(static_cast<const TB*>(p.y) + r * p.ldy);
-        if (p.gate) v.gate = at.load(static_cast<const TB*>(p.gate) + r * p.ldg);
+        if (p.gate) v.gate[0] = at.load(static_cast<const TB*>(p.gate) + r * p.ldg);
         v.stats = __ldg(reinterpret_cast<const float4*>(p.stats + 4 * r));
     };
     if (AHEAD) load((int64_t)blockIdx.x * Team<L>::COUNT + team.index, next);
@@ -114,14 +114,15 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
             if (p.post) yn = FULL ? fma8(yn, v.stats.y, all8(-v.stats.x * v.stats.y)) : yn * v.stats.y;
         }
         // act: the gate, or its sigmoid (of which a silu gate takes the gate's multiple wherever it is used)
-        if (p.gate) act = p.act == NORM_PLAIN ? pairs_of(v.gate) : sigmoid_of(pairs_of(v.gate));
+        if (p.gate && p.act == NORM_PLAIN) act = pairs_of(v.gate[0]);
+        else if (p.gate) with_sigmoids<false>(v.gate, [&](int, const P8& s) { act = s; });
         float mean = 0.f, along = 0.f;
         if (p.dz) {
             P8 h = pairs_of(v.x);
             if (p.y) {
                 const P8 sw = SHARED ? make_sw() : sw_held;
                 P8 q = FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw;
-                if (p.gate && p.act == NORM_SILU) q = q * pairs_of(v.gate);
+                if (p.gate && p.act == NORM_SILU) q = q * pairs_of(v.gate[0]);
                 h = fma8(q, act, h);
             }
             const P8 hn = FULL ? fma8(h, v.stats.w, all8(-v.stats.z * v.stats.w)) : h * v.stats.w, dz = pairs_of(v.dz), c = dz * (SHARED ? at.vector(p.w2) : w2_held);
@@ -142,7 +143,7 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
             P8 q = (FULL ? fma8(yn, sw, SHARED ? make_sb() : sb_held) : yn * sw) * dh;
             if (p.act != NORM_PLAIN) {
                 P8 slope = act * fma8(act, -1.f, all8(1.f));          // s (1 - s), and s + g s (1 - s)
-                if (p.act == NORM_SILU) slope = fma8(pairs_of(v.gate), slope, act);
+                if (p.act == NORM_SILU) slope = fma8(pairs_of(v.gate[0]), slope, act);
                 q = q * slope;
             }
             at.store(static_cast<TB*>(p.dgate) + r * p.ldog, q, live);
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD /
         P8 f = dh;
         if (p.gate) {
             f = f * act;
-            if (p.act == NORM_SILU) f = f * pairs_of(v.gate);
+            if (p.act == NORM_SILU) f = f * pairs_of(v.gate[0]);
         }
         if (live) {
             add(1, f, yn);

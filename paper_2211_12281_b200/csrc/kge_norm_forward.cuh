@@ -130,8 +130,7 @@ __global__ void __launch_bounds__(norm_threads(L, K, W == 8), norm_ctas(L, K, W 
 #pragma unroll
                         for (int k = 0; k < K; ++k) u[k] = u[k] * pairs_of(now.gate[k]);
                     } else {
-#pragma unroll
-                        for (int k = 0; k < K; ++k) u[k] = u[k] * sigmoid_of(pairs_of(now.gate[k]));
+                        with_sigmoids<sizeof(TX) + sizeof(TB) == 4>(now.gate, [&](int k, const P8& act) { u[k] = u[k] * act; });
                         if (p.act == NORM_SILU) {
 #pragma unroll
                             for (int k = 0; k < K; ++k) u[k] = u[k] * pairs_of(now.gate[k]);
