@@ -2,6 +2,7 @@
 that a kernel comes to in its second and third turn."""
 import pytest
 
+import test_gpu_block_operators as block
 from test_gpu_block_operators import _int8
 from test_gpu_row_operators import K, T, _gen  # noqa: F401
 
@@ -43,3 +44,59 @@ def test_int8_matmul_of_a_row_does_not_depend_on_the_others(T, K, M, N, Kd):
                 some = T.empty((rows.stop - rows.start, N), device="cuda")
                 K.int8_matmul(a[rows], sa[rows], b, sb, some, addend=None if plus is None else plus[rows])
                 assert T.equal(some, out[rows])
+
+
+# Rows enough for every team of every kernel to come to its second and third (with the next row's loads under way, where the kernel has them), and a rest: one team for
+# each width that has its own, rows that move eight elements at a time, two, or one.
+TURNS = [
+    # n, d, x type, block type, form, post, gate, scale, bias, kind
+    (40_001, 8, "f32", "bf16", "both", True, "silu", True, True, "layer"), (40_001, 50, "bf16", "bf16", "both", True, "sigmoid", True, False, "rms"),
+    (40_001, 64, "bf16", "f16", "both", True, "plain", True, True, "layer"), (40_001, 64, "f32", "f32", "pre", False, "none", False, False, "rms"),
+    (20_003, 128, "f32", "f32", "both", True, "sigmoid", True, True, "layer"), (30_011, 104, "bf16", "bf16", "pre", False, "none", False, True, "layer"),
+    (10_007, 200, "f32", "bf16", "both", False, "none", True, True, "layer"), (10_007, 250, "f16", "f16", "both", True, "silu", True, False, "rms"),
+    (10_007, 256, "bf16", "bf16", "both", True, "silu", True, True, "layer"), (8003, 400, "f32", "bf16", "both", True, "silu", True, True, "layer"),
+    (8003, 512, "bf16", "bf16", "both", True, "sigmoid", False, False, "rms"), (6003, 768, "f16", "bf16", "both", True, "plain", True, False, "rms"),
+    (3001, 998, "bf16", "bf16", "both", True, "sigmoid", True, True, "layer"), (6003, 1000, "bf16", "f32", "both", True, "silu", True, False, "rms"),
+    (6003, 1024, "f32", "f32", "post", True, "sigmoid", True, True, "layer"), (2501, 1600, "bf16", "bf16", "both", True, "sigmoid", True, True, "layer"),
+    (3001, 1400, "f32", "bf16", "pre", False, "none", False, True, "rms"), (2501, 2050, "bf16", "bf16", "both", True, "none", True, False, "rms"),
+    (2501, 4096, "bf16", "bf16", "both", True, "sigmoid", True, False, "rms"), (2501, 4096, "f32", "bf16", "both", True, "silu", True, True, "layer"),
+    (701, 5000, "f32", "f16", "both", True, "sigmoid", True, True, "layer"), (1203, 8192, "bf16", "bf16", "both", True, "silu", True, False, "rms"), (400, 9002, "bf16", "bf16", "both", True, "silu", True, True, "layer")]
+
+
+@pytest.mark.parametrize("n,d,tx,tb,form,post,gate,scale,bias,kind", TURNS)
+def test_block_norm_over_several_turns(T, K, n, d, tx, tb, form, post, gate, scale, bias, kind):
+    block.test_block_norm(T, K, n, d, tx, tb, form, post, gate, scale, bias, kind)
+
+
+@pytest.mark.parametrize("n,d,tx,tb,form,post,gate,scale,bias,kind", TURNS)
+def test_block_norm_grad_over_several_turns(T, K, n, d, tx, tb, form, post, gate, scale, bias, kind):
+    block.test_block_norm_grad(T, K, n, d, tx, tb, form, post, gate, scale, bias, kind)
+
+
+# (more than 740 CTAs' elements: each takes two turns; with room for 12, 40 and 340 tensors in a launch)
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("tp,tg,copy,shift,sizes,step,gs", [
+    ("f32", "f32", "bf16", 0, [1_000_003, 700_001, 2049, 300_007, 129], 3, 1.0), ("bf16", "bf16", None, 1, [2_000_001, 4097, 5, 4095], 8, 0.5),
+    ("f32", "bf16", None, 0, [70_001 + 511 * i for i in range(30)], 5, 1.0), ("f16", "f16", "bf16", 0, [50_001 + 97 * i for i in range(60)], 1, 1.0)])
+def test_adamw_of_two_turns(T, K, bits, tp, tg, copy, shift, sizes, step, gs):
+    block.test_adamw(T, K, bits, tp, tg, copy, shift, sizes, step, gs)
+
+
+@pytest.mark.parametrize("n,d", [(40_001, 48), (20_003, 120), (10_007, 256), (10_007, 250), (8003, 512), (6003, 768), (6003, 1000), (3001, 1001), (2501, 4096), (300, 9000)])
+def test_norms_of_a_row_do_not_depend_on_the_others(T, K, n, d):
+    """h, z, statistics, integers and their scales of rows among many are what they are alone."""
+    g = _gen(T, n)
+    f = block._inputs(T, g, n, d, "f32", "bf16", "both", True, "silu", True, True)
+    args = dict(pre_weight=f["w2"], pre_bias=f["b2"], gate_act="silu", post_weight=f["w1"], post_bias=f["b1"], scale=f["scale"], kind="layer")
+
+    def call(rows, in8):
+        x, y, gate = (f[k][rows] for k in ("x", "y", "gate"))
+        m = x.shape[0]
+        z = _int8(T, m, d) if in8 else T.empty((m, d), dtype=T.bfloat16, device="cuda")
+        h, stats, scales = T.empty((m, d), device="cuda"), T.empty((m, 4), device="cuda"), T.empty(m, device="cuda") if in8 else None
+        K.block_norm(x, z=z, y=y, h=h, gate=gate, stats=stats, z_scales=scales, **args)
+        return [h, z, stats] + ([scales] if in8 else [])
+    for in8 in (False, True):
+        whole = call(slice(0, n), in8)
+        for rows in (slice(0, 2), slice(n // 2, n // 2 + 33), slice(n - 7, n)):
+            assert all(T.equal(a[rows], b) for a, b in zip(whole, call(rows, in8)))
