@@ -1,10 +1,11 @@
 """Results of the operators for a residual block that must not depend on how a call is cut up: products in 8-bit integers row by row, and rows, columns and tensors
 that a kernel comes to in its second and third turn."""
+import numpy as np
 import pytest
 
 import test_gpu_block_operators as block
 from test_gpu_block_operators import _int8
-from test_gpu_row_operators import K, T, _gen  # noqa: F401
+from test_gpu_row_operators import K, T, _check, _gen  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +101,35 @@ def test_norms_of_a_row_do_not_depend_on_the_others(T, K, n, d):
         whole = call(slice(0, n), in8)
         for rows in (slice(0, 2), slice(n // 2, n // 2 + 33), slice(n - 7, n)):
             assert all(T.equal(a[rows], b) for a, b in zip(whole, call(rows, in8)))
+
+
+@pytest.mark.parametrize("n,d", [(8_400_000, 256), (8_360_000, 257)])
+def test_block_norm_grad_of_few_rows_beyond_two_to_the_31_elements(T, K, n, d):
+    """dz is zero but in nine rows, on both sides of element 2^31 and at the ends: the vectors' gradients are those rows' alone, and all other rows' are zero."""
+    at = (1 << 31) // d
+    at = T.tensor([0, 4999, at - 2, at - 1, at, at + 1, n - 600, n - 2, n - 1], device="cuda")
+    g = _gen(T, d)
+    few = block._inputs(T, g, 9, d, "bf16", "bf16", "both", True, "silu", True, True)
+    dz = T.randn((9, d), generator=g, device="cuda").to(T.bfloat16)
+    f = dict(few)
+    for k in ("x", "y", "gate"):
+        f[k] = T.full((n, d), 1.0, dtype=T.bfloat16, device="cuda")
+        f[k][at] = few[k]
+    f64 = block._double(few)
+    o = block._block64(T, f64, "silu", float(np.float32(1e-5)), 1.0, d)
+    args = dict(pre_weight=f["w2"], y=f["y"], gate=f["gate"], gate_act="silu", post_weight=f["w1"], post_bias=f["b1"], scale=f["scale"], kind="layer")
+    z, stats = T.empty((n, d), dtype=T.bfloat16, device="cuda"), T.empty((n, 4), device="cuda")
+    K.block_norm(f["x"], z=z, pre_bias=f["b2"], stats=stats, eps=1e-5, **args)
+    _check(T, z[at], o["z"].v, 1.05 * o["z"].tol, "z")
+    z.zero_()
+    z[at] = dz
+    want = block._block_grad64(T, f64, o, "silu", 1.0, d, dz.double(), None)
+    names = dict(dw1="dpost_weight", db1="dpost_bias", dscale="dscale", dw2="dpre_weight", db2="dpre_bias")
+    got = {k: T.empty(d, device="cuda") for k in names}
+    K.block_norm_grad(f["x"], stats, dx=z, dz=z, dy=f["y"], dgate=f["gate"], **{names[k]: v for k, v in got.items()}, **args)
+    got.update(dx=z[at], dy=f["y"][at], dgate=f["gate"][at])
+    for k, v in got.items():
+        _check(T, v, want[k].v, 1.05 * want[k].tol, k)
+    for rows in (z, f["y"], f["gate"]):
+        rows[at] = 0
+        assert not rows.any()
