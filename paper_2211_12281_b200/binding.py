@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import bisect
 import ctypes as C
+import numbers
 import struct
 from pathlib import Path
 
@@ -588,7 +589,7 @@ class AdamW:
             lists[name] = [None] * count if given is None else list(given)
             if len(lists[name]) != count:
                 raise _bad(w, f"{name} is not a list of {count}")
-        decay = [float(weight_decay)] * count if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+        decay = [float(weight_decay)] * count if isinstance(weight_decay, numbers.Real) else [float(d) for d in weight_decay]
         if len(decay) != count:
             raise _bad(w, f"weight_decay is not a number or a list of {count}")
         if _torch is None:
