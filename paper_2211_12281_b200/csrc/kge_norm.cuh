@@ -200,6 +200,7 @@ template <int L> struct Team {
 constexpr float LOG2_E = 1.44269504f, LN_2 = 0.693147182f, LN_2_REST = -1.90465430e-9f;
 __device__ __forceinline__ float power_of_two(float t) { float x; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(t)); return x; }
 __device__ __forceinline__ float one_over(float y) { float x; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(x) : "f"(y)); return x; }
+// (A call, rare in the kernels that hold a row and cheap beside the loops' loads: inline it takes registers from both, the fp32 gradients of 3,000 x 20,000 2,095 us, so 2,320.)
 static __device__ __noinline__ float sigmoid_of(float g) {
     if (fabsf(g) < 80.f) {
         const float t = g * -LOG2_E, r = fmaf(t, -LN_2_REST, fmaf(t, -LN_2, -g)), power = power_of_two(t);
@@ -208,6 +209,7 @@ static __device__ __noinline__ float sigmoid_of(float g) {
     const float e = expf(-fabsf(g)), r = __fdiv_rn(1.f, 1.f + e);
     return g < 0.f ? e * r : r;
 }
+__device__ __forceinline__ float sigmoid_brief(float g) { return one_over(1.f + power_of_two(-LOG2_E * g)); }
 // The same bits for a thread's gates: f(k, sigmoids of pack k), in pairs where all of them are near.
 // BRIEF: without the remainder, and 0 below the normal numbers: within 6 + 1.5 |g| units of 2^-24 of itself (its share of |g| for g < 0 only), less than 2^-16.  Enough where
 // all that is made of it is rounded to 16 bits (h and z of 16-bit rows and blocks; 32,768 x 4,096 bf16: 245 us, 255 with the remainder).
@@ -217,7 +219,7 @@ template <bool BRIEF, int K, typename T, class F> __device__ __forceinline__ voi
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const P8 g = pairs_of(gate[k]);
-            f(k, make_pairs([&](int e) { return one_over(1.f + power_of_two(-LOG2_E * element(g, e))); }));
+            f(k, make_pairs([&](int e) { return sigmoid_brief(element(g, e)); }));
         }
         return;
     }
@@ -243,7 +245,11 @@ template <bool BRIEF, int K, typename T, class F> __device__ __forceinline__ voi
         f(k, make_pairs([&](int e) { return one_over(element(sum, e)); }));
     }
 }
-__device__ __forceinline__ float act_of(float g, int act) { return act == NORM_PLAIN ? g : (act == NORM_SIGMOID ? sigmoid_of(g) : g * sigmoid_of(g)); }
+template <bool BRIEF> __device__ __forceinline__ float act_of(float g, int act) {
+    if (act == NORM_PLAIN) return g;
+    const float s = BRIEF ? sigmoid_brief(g) : sigmoid_of(g);
+    return act == NORM_SIGMOID ? s : g * s;
+}
 __device__ __forceinline__ float2 act_and_slope(float g, int act) {
     if (act == NORM_PLAIN) return make_float2(g, 1.f);
     const float s = sigmoid_of(g);
