@@ -497,7 +497,8 @@ int kge_block_norm_grad(const kge_norm_block* block /*[host]*/, int64_t n, int32
 /*
  * One AdamW step over a list of tensors: with t = step + 1 and g the gradient times grad_scale, element by element
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2 (each product and sum rounded to fp32 on its own),
- *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps), rounded once to its type;
+ *   param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps), rounded once to its type
+ *   (in fp32 before that: the second term within 8 units of 2^-24 of itself, the first within 2);
  * copy (or NULL) receives the new parameters in bf16 or fp16 as well.  A tensor is n <= 2^40 contiguous elements; param and grad fp32, bf16
  * or fp16, each its own; one whose grad is NULL, or whose n is 0, is passed over.  Tensors of a call must not overlap each other.
  * state_bits = 32   m, v fp32 [n]; the scales are not looked at.

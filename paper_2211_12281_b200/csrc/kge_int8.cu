@@ -564,7 +564,8 @@ struct ProductPlan { int form, split; };          // split: CTAs that share a ti
 // How a product is cut up.
 //   shared K      as many CTAs to a tile as run at a time, where the blocks that a CTA is spared outweigh the join: a block takes 0.4 us, the join 0.4 + 2 for 128 rows
 //                 (16 x 4,096 x 4,096: four CTAs to each of 32 tiles, 9.3 us)
-//   64 columns    of B at most: tiles of 128 x 64 (30,000 x 64 x 1,024: 10.3 us, in tiles of 256 x 256 14.9)
+//   64 columns    of B at most: tiles of 128 x 64 (30,000 x 64 x 1,024: 10.3 us, in tiles of 256 x 256 14.9, of 128 x 128 on one CTA an SM 10.7; 17,479 x 64 x 624: 8.4, 9.0, 8.4.
+//                 With a long K others would be ahead by up to a tenth: 30,000 x 64 x 4,096 29.9, 31.7, 27.9; 9,811 x 16 x 7,696 41.9, 38.0, 42.3)
 //   else          the least of three estimates, in hundredths of a microsecond: a constant, and for every round of tiles that the chip takes another and one for each block
 //                 of K (fitted to 125 shapes; the form chosen is 1.4 % slower than the best of the four on their mean, 18 % with the rule "256 x 256 where they fill the pairs").
 //                   256 x 256               the least for a block, the most before and after it: 8,192 x 4,096 x 8,192 174 us, in tiles of 128 x 256 on one CTA 213;

@@ -49,10 +49,11 @@ template <typename TX, typename TB> struct GradRow { Raw8<TX> x, dh; Raw8<TB> y,
 // the last one.)  The vectors enter as sw = s w1, sb = s b1 and w2, which a thread keeps: with q = yn sw + sb
 //   h = x + act q,  dgate = act' q dh',  f = act dh' sw
 // FULL: norms that take a mean, or biases; without them sb, T0 and S0 are not there.
-// AHEAD: the next row's loads are under way where registers hold it too.  (Two or three rows ahead, copied into shared memory asynchronously: 16,384 x 4,096 bf16 229
+// AHEAD: the next row's loads are under way where registers hold it too: with FULL only in teams of 32 to 128 threads, not where a CTA holds a row (16,384 x 4,096 bf16,
+// layer norms: 350 us, root-mean-square norms 231).  (Two or three rows ahead, copied into shared memory asynchronously: 16,384 x 4,096 bf16 229
 // instead of 234 us, 8,192 x 4,096 fp32 330 instead of 204, 24,576 x 256 46 instead of 38: it is not memory that they wait for.)
 // SHARED: a CTA of up to 1,024 threads for a row of up to 8,192 columns, whose registers hold neither: the sums are in shared memory, a thread's own places, and the
-// vectors are loaded where they are used (8,192 x 8,192 bf16: 407 us; gone over in three passes 2,284).
+// vectors are loaded where they are used (8,192 x 8,192 bf16: 390 us; gone over in three passes 2,284).
 template <typename TX, typename TB, int L, int W, bool FULL, bool SHARED>
 __global__ void __launch_bounds__(SHARED ? NORM_MOST / 8 : (L == 0 ? GRAD_HELD / 8 : NORM_THREADS), L == 0 ? 1 : 2) norm_grad_kernel(const __grid_constant__ NormGradParams p) {
     constexpr bool AHEAD = !SHARED && (!FULL || L >= 32) && (!FULL || sizeof(TX) + sizeof(TB) <= 6);
